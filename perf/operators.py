@@ -249,8 +249,6 @@ def prepare(case, seed):
                                     window=c["window"])
             s["workspace"] = torch.empty(lib.attn_workspace_bytes(s["cache"].fmt, H * G, max(1, c["draft"]),
                                                                   c["op"] == "mass"), dtype=torch.uint8, device=dev)
-        if c["op"] == "evict":
-            s["workspace"] = torch.empty(lib.evict_workspace_bytes(s["cache"].fmt, c["budget"]), dtype=torch.uint8, device=dev)
     return s
 
 
@@ -390,7 +388,7 @@ def run(state):
     if c["op"] == "evict":
         if own:
             kept, new = lib.evict(s["cache"], s["lens"], s["mass"], c["budget"], c["sink"], c["recent"], dst=s["to_cache"],
-                                  dst_mass=s["to_mass"], workspace=s["workspace"])
+                                  dst_mass=s["to_mass"])
         else:
             kept, new = _evict(s)
         return {"kept": kept, "lens": new, "mass": s["to_mass"], **s["to"]}
