@@ -246,6 +246,104 @@ kvbfp_status kvbfp_decode_attn_rope(const kvbfp_cache* cache, const void* q, kvb
                                     void* stream);
 
 /*
+ * Scores beyond the scaled product (the paper has no counterpart; models that cap their scores, position them by
+ * distance or restrict what a token sees need them next to the cache).  For a query at position pos_q and a cached
+ * token at position pos_k, with x = scale * q.k:
+ *   cap      x = softcap * tanh(x / softcap)              (0: none)
+ *   bias     x = x - slopes[h] * (pos_q - pos_k)          (NULL: none; h = query head)
+ *   visible  pos_k < prefix[b], or pos_k >= first[b] and pos_q - pos_k < window   (NULL / 0: no such limit)
+ * first[b] is where the current document begins, prefix[b] tokens stay visible whatever the window hides.  Values are
+ * read clamped to [0, cached tokens].  A query that sees nothing gives zeros.
+ */
+typedef struct {
+    float softcap;           /* >= 0, finite */
+    int32_t window;          /* >= 0 */
+    const float* slopes;     /* device [n_q_heads] or NULL */
+    const int32_t* first;    /* device [batch] or NULL */
+    const int32_t* prefix;   /* device [batch] or NULL */
+} kvbfp_score_mod;
+
+/* Bytes of workspace of kvbfp_tree_attn (n_draft tokens), kvbfp_decode_attn_mod (n_draft = 1, with_mass = 0) and
+ * kvbfp_decode_attn_mass (n_draft = 1, with_mass = 1); 0 on invalid arguments.  Contents need no initialisation; calls
+ * that may overlap on the GPU need one each. */
+size_t kvbfp_attn_workspace_bytes(const kvbfp_format* fmt, int32_t n_q_heads, int32_t n_draft, int32_t with_mass);
+
+/*
+ * Attention of a tree of drafted tokens over the packed cache: one call scores every candidate of a speculative step.
+ * The drafted tokens' K and V rows have been appended behind the sequence's ctx_lens[b] cached tokens (kvbfp_append,
+ * n_new = n_draft, start_pos = ctx_lens).  Drafted token i stands at position ctx_lens[b] + depth[b, i] and sees the
+ * cached tokens (as `mod` allows) and those drafted tokens j whose bit j is set in tree_mask[b, i] (and that lie in
+ * the window; first and prefix do not apply to them).
+ *   q           [batch, n_draft, n_q_heads, head_dim] of `dt`, original channel order; n_draft <= 64
+ *   ctx_lens    [batch] i32; draft_lens [batch] i32 or NULL (all n_draft): drafted tokens of each sequence.  Rows of q
+ *               behind them give zeros.  batch <= 1024
+ *   tree_mask   [batch, n_draft] or NULL: a chain, token i sees drafted tokens 0..i
+ *   depth       [batch, n_draft] i32 or NULL: depth = index; read clamped to [0, n_draft - 1]
+ *   mod         host struct or NULL
+ *   out         [batch, n_draft, n_q_heads, head_dim] of `dt`
+ * n_q_heads, perm_k, inv_perm_v, softmax_scale as in kvbfp_decode_attn.  bf16 queries are used exactly, softmax
+ * weights are rounded to bf16 for the product with V and the output to bf16; fp32 queries give fp32 accuracy (slower).
+ * Sums, maxima and scores are fp32 in both.  Lengths beyond the cache are read clamped and set KVBFP_FLAG_POSITION.
+ * The result does not depend on anything but the arguments (no atomics).
+ */
+kvbfp_status kvbfp_tree_attn(const kvbfp_cache* cache, const void* q, kvbfp_dtype dt, int32_t n_q_heads,
+                             int32_t n_draft, const int32_t* ctx_lens, const int32_t* draft_lens,
+                             const uint64_t* tree_mask, const int32_t* depth, const int32_t* perm_k,
+                             const int32_t* inv_perm_v, float softmax_scale, const kvbfp_score_mod* mod, void* out,
+                             void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * kvbfp_decode_attn with modified scores: q [batch, n_q_heads, head_dim] of `dt` is the last cached token, at position
+ * seq_lens[b] - 1; out is of `dt`.  Cached tokens that the window hides from every query are not read.
+ */
+kvbfp_status kvbfp_decode_attn_mod(const kvbfp_cache* cache, const void* q, kvbfp_dtype dt, int32_t n_q_heads,
+                                   const int32_t* seq_lens, const int32_t* perm_k, const int32_t* inv_perm_v,
+                                   float softmax_scale, const kvbfp_score_mod* mod, void* out, void* workspace,
+                                   size_t workspace_bytes, void* stream);
+
+/*
+ * kvbfp_decode_attn_mod that also gathers where the attention went:
+ *   mass [batch, n_kv_heads, max_seq] f32: mass[b, h, t] += sum over the query heads of kv head h of the softmax weight
+ *   of token t.  Entries of tokens that are not visible, and those behind seq_lens[b], are left as they are.
+ * mod may be NULL.  The workspace holds the scores: 4 * batch * n_q_heads * max_seq bytes more.
+ */
+kvbfp_status kvbfp_decode_attn_mass(const kvbfp_cache* cache, const void* q, kvbfp_dtype dt, int32_t n_q_heads,
+                                    const int32_t* seq_lens, const int32_t* perm_k, const int32_t* inv_perm_v,
+                                    float softmax_scale, const kvbfp_score_mod* mod, float* mass, void* out,
+                                    void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Eviction by accumulated weight.  For each (sequence, kv head) of more than `budget` cached tokens the first n_sink,
+ * the last n_recent and the budget - n_sink - n_recent tokens of the largest mass between them are kept (equal masses:
+ * the lower position; NaN counts as the least), in position order; shorter sequences are kept whole.  The kept packed
+ * rows go to rows 0.. of `dst`, their masses to dst_mass [batch, n_kv_heads, dst max_seq], whose entries behind them
+ * are set to zero; packed rows of dst behind them are left as they are.
+ *   dst       another cache of the same batch, heads, block and mantissa width with max_seq >= budget that shares no
+ *             memory with src, or src itself (then dst_mass is mass)
+ *   new_lens  [batch] i32 out: min(seq_lens, budget); may be seq_lens
+ *   kept      [batch, n_kv_heads, budget] i32 out: the kept positions, -1 behind the last
+ * Heads keep different tokens, so row numbers are no positions any more: keys have to be cached with their position
+ * already in them (rotated), and masks or biases by position no longer apply.
+ */
+kvbfp_status kvbfp_evict(const kvbfp_cache* src, const int32_t* seq_lens, const float* mass, int32_t budget,
+                         int32_t n_sink, int32_t n_recent, const kvbfp_cache* dst, float* dst_mass, int32_t* new_lens,
+                         int32_t* kept, void* stream);
+
+/*
+ * Moves listed rows together in all four planes: row src_base[b] + index[b, h, i] of src becomes row dst_base[b] + i
+ * of dst, i < count[b].  With src = dst and both bases the context length this commits the accepted branch of a
+ * drafted tree.
+ *   index     [batch, index_heads, n_index] i32, index_heads 1 (all heads alike) or n_kv_heads; in place index[i] >= i
+ *             and ascending (other orders give unspecified rows)
+ *   count     [batch] i32, read clamped to [0, n_index];  src_base, dst_base [batch] i32 or NULL (0)
+ *   dst       as in kvbfp_evict
+ * Rows outside a cache are skipped and set KVBFP_FLAG_POSITION.
+ */
+kvbfp_status kvbfp_gather_rows(const kvbfp_cache* src, const kvbfp_cache* dst, const int32_t* index,
+                               int32_t index_heads, int32_t n_index, const int32_t* count, const int32_t* src_base,
+                               const int32_t* dst_base, void* stream);
+
+/*
  * kvbfp_decode_attn for callers that must not allocate device memory (the paper has no counterpart:
  * this is a deployment aid, not a step of the method).  Who needs it: code that runs after a serving
  * process has frozen its memory pool, plug-ins that are handed tensors but no allocator, and loops

@@ -26,7 +26,8 @@ EXPORTS = ["kvbfp_version", "kvbfp_status_string", "kvbfp_last_cuda_error", "kvb
            "kvbfp_profile_decode_events", "kvbfp_static_scratch_bytes", "kvbfp_decode_attn_static",
            "kvbfp_rope_tables", "kvbfp_rope_apply", "kvbfp_decode_attn_rope", "kvbfp_split_plan",
            "kvbfp_split_range_start", "kvbfp_split_range_of", "kvbfp_split_partial_slot",
-           "kvbfp_selftest_wait_timeout"]
+           "kvbfp_selftest_wait_timeout", "kvbfp_attn_workspace_bytes", "kvbfp_tree_attn", "kvbfp_decode_attn_mod",
+           "kvbfp_decode_attn_mass", "kvbfp_evict", "kvbfp_gather_rows"]
 
 
 class KvbfpError(RuntimeError):
@@ -51,6 +52,11 @@ class Format(C.Structure):
 class CacheStruct(C.Structure):
     _fields_ = [("fmt", Format), ("k_mant", C.c_void_p), ("k_exp", C.c_void_p),
                 ("v_mant", C.c_void_p), ("v_exp", C.c_void_p)]
+
+
+class ScoreModStruct(C.Structure):
+    _fields_ = [("softcap", C.c_float), ("window", C.c_int32), ("slopes", C.c_void_p), ("first", C.c_void_p),
+                ("prefix", C.c_void_p)]
 
 
 _lib = None
@@ -112,6 +118,21 @@ def lib():
             getattr(L, name).argtypes = [C.c_int32] * 3
             getattr(L, name).restype = C.c_int32
         L.kvbfp_selftest_wait_timeout.argtypes = [C.c_uint32, C.c_uint32, C.c_void_p]
+        L.kvbfp_attn_workspace_bytes.restype = C.c_size_t
+        L.kvbfp_attn_workspace_bytes.argtypes = [C.c_void_p, C.c_int32, C.c_int32, C.c_int32]
+        L.kvbfp_tree_attn.argtypes = [C.c_void_p, C.c_void_p, C.c_int, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p,
+                                      C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_float, C.c_void_p, C.c_void_p,
+                                      C.c_void_p, C.c_size_t, C.c_void_p]
+        L.kvbfp_decode_attn_mod.argtypes = [C.c_void_p, C.c_void_p, C.c_int, C.c_int32, C.c_void_p, C.c_void_p,
+                                            C.c_void_p, C.c_float, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t,
+                                            C.c_void_p]
+        L.kvbfp_decode_attn_mass.argtypes = [C.c_void_p, C.c_void_p, C.c_int, C.c_int32, C.c_void_p, C.c_void_p,
+                                             C.c_void_p, C.c_float, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
+                                             C.c_size_t, C.c_void_p]
+        L.kvbfp_evict.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_void_p,
+                                  C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]
+        L.kvbfp_gather_rows.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p,
+                                        C.c_void_p, C.c_void_p]
         L.kvbfp_split_partial_slot.argtypes = [C.c_int32] * 4
         L.kvbfp_split_partial_slot.restype = C.c_int32
         _lib = L
@@ -283,6 +304,140 @@ def decode_attn_rope(cache, q, seq_lens, theta, partner, sign, perm_k=None, inv_
                                         _ptr(_dev(sign, torch.float32)), _ptr(_dev(out, torch.float32)),
                                         _ptr(workspace), workspace.numel(), flags, _stream(stream)))
     return out
+
+
+class ScoreMod:
+    """kvbfp_score_mod: cap, distance bias and masks of the scores.  slopes f32 [H_q], first and prefix i32 [B]."""
+
+    def __init__(self, softcap=0.0, slopes=None, first=None, prefix=None, window=0):
+        self.softcap, self.window = float(softcap), int(window)
+        self.slopes, self.first, self.prefix = _dev(slopes, torch.float32), _dev(first, torch.int32), _dev(prefix, torch.int32)
+
+    def struct(self):
+        p = lambda t: None if t is None else t.data_ptr()
+        return ScoreModStruct(self.softcap, self.window, p(self.slopes), p(self.first), p(self.prefix))
+
+    def check(self, batch, n_q_heads):
+        for name, t, n in (("slopes", self.slopes, n_q_heads), ("first", self.first, batch), ("prefix", self.prefix, batch)):
+            if t is not None and t.numel() != n:
+                raise ValueError(f"{name}: expected {n} values, got {t.numel()}")
+
+
+def _sized(name, t, shape):
+    if t is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
+    return t
+
+
+def attn_workspace_bytes(fmt, n_q_heads, n_draft=1, with_mass=False):
+    return int(lib().kvbfp_attn_workspace_bytes(C.byref(fmt), n_q_heads, n_draft, int(with_mass)))
+
+
+def _attn_buffers(cache, q, n_draft, with_mass, mod, out, workspace):
+    f = cache.fmt
+    n_q_heads = q.shape[-2]
+    if q.shape[0] != f.batch or q.shape[-1] != f.head_dim:
+        raise ValueError(f"q: shape {tuple(q.shape)} does not fit a cache of batch {f.batch}, head_dim {f.head_dim}")
+    if out is None:
+        out = torch.empty_like(q)
+    elif _dev(out, q.dtype).shape != q.shape:
+        raise ValueError("out: expected the shape of q")
+    if workspace is None:
+        workspace = torch.empty(attn_workspace_bytes(f, n_q_heads, n_draft, with_mass), dtype=torch.uint8, device=q.device)
+    ms = None
+    if mod is not None:
+        mod.check(f.batch, n_q_heads)
+        ms = mod.struct()
+    return n_q_heads, out, workspace, ms
+
+
+def tree_attn(cache, q, ctx_lens, draft_lens=None, tree_mask=None, depth=None, perm_k=None, inv_perm_v=None,
+              softmax_scale=0.0, mod=None, out=None, workspace=None, stream=None):
+    """kvbfp_tree_attn: q [B, T, H_q, d] of T drafted tokens appended at ctx_lens; tree_mask int64 [B, T] (bit j of row
+    i: token i sees drafted token j), depth i32 [B, T] -> out [B, T, H_q, d] of q's type."""
+    q = _dev(q)
+    Bn, T = q.shape[0], q.shape[1]
+    n_q_heads, out, workspace, ms = _attn_buffers(cache, q, T, False, mod, out, workspace)
+    cs = cache.struct()
+    _check(lib().kvbfp_tree_attn(C.byref(cs), _ptr(q), _dt(q), n_q_heads, T,
+                                 _ptr(_sized("ctx_lens", _dev(ctx_lens, torch.int32), (Bn,))),
+                                 _ptr(_sized("draft_lens", _dev(draft_lens, torch.int32), (Bn,))),
+                                 _ptr(_sized("tree_mask", _dev(tree_mask, torch.int64), (Bn, T))),
+                                 _ptr(_sized("depth", _dev(depth, torch.int32), (Bn, T))),
+                                 _ptr(_dev(perm_k, torch.int32)), _ptr(_dev(inv_perm_v, torch.int32)),
+                                 float(softmax_scale), None if ms is None else C.byref(ms), _ptr(out), _ptr(workspace),
+                                 workspace.numel(), _stream(stream)))
+    return out
+
+
+def decode_attn_mod(cache, q, seq_lens, mod, perm_k=None, inv_perm_v=None, softmax_scale=0.0, out=None, workspace=None,
+                    stream=None):
+    """kvbfp_decode_attn_mod: q [B, H_q, d], the last cached token of each sequence -> out of q's type."""
+    q = _dev(q)
+    n_q_heads, out, workspace, ms = _attn_buffers(cache, q, 1, False, mod, out, workspace)
+    cs = cache.struct()
+    _check(lib().kvbfp_decode_attn_mod(C.byref(cs), _ptr(q), _dt(q), n_q_heads,
+                                       _ptr(_sized("seq_lens", _dev(seq_lens, torch.int32), (q.shape[0],))),
+                                       _ptr(_dev(perm_k, torch.int32)), _ptr(_dev(inv_perm_v, torch.int32)),
+                                       float(softmax_scale), None if ms is None else C.byref(ms), _ptr(out),
+                                       _ptr(workspace), workspace.numel(), _stream(stream)))
+    return out
+
+
+def decode_attn_mass(cache, q, seq_lens, mass, mod=None, perm_k=None, inv_perm_v=None, softmax_scale=0.0, out=None,
+                     workspace=None, stream=None):
+    """kvbfp_decode_attn_mass: decode_attn_mod that adds every token's softmax weight to mass f32 [B, H_kv, max_seq]."""
+    q = _dev(q)
+    f = cache.fmt
+    n_q_heads, out, workspace, ms = _attn_buffers(cache, q, 1, True, mod, out, workspace)
+    cs = cache.struct()
+    _check(lib().kvbfp_decode_attn_mass(C.byref(cs), _ptr(q), _dt(q), n_q_heads,
+                                        _ptr(_sized("seq_lens", _dev(seq_lens, torch.int32), (q.shape[0],))),
+                                        _ptr(_dev(perm_k, torch.int32)), _ptr(_dev(inv_perm_v, torch.int32)),
+                                        float(softmax_scale), None if ms is None else C.byref(ms),
+                                        _ptr(_sized("mass", _dev(mass, torch.float32), (f.batch, f.n_kv_heads, f.max_seq))),
+                                        _ptr(out), _ptr(workspace), workspace.numel(), _stream(stream)))
+    return out
+
+
+def evict(cache, seq_lens, mass, budget, n_sink=0, n_recent=0, dst=None, dst_mass=None, new_lens=None, kept=None,
+          stream=None):
+    """kvbfp_evict -> (kept i32 [B, H_kv, budget], new_lens i32 [B]).  dst: another Cache (with dst_mass), or None: in
+    place, in cache and mass."""
+    f = cache.fmt
+    if dst is None:
+        dst, dst_mass = cache, mass
+    d = dst.fmt
+    if kept is None:
+        kept = torch.empty(f.batch, f.n_kv_heads, budget, dtype=torch.int32, device=mass.device)
+    if new_lens is None:
+        new_lens = torch.empty(f.batch, dtype=torch.int32, device=mass.device)
+    cs, ds = cache.struct(), dst.struct()
+    _check(lib().kvbfp_evict(C.byref(cs), _ptr(_sized("seq_lens", _dev(seq_lens, torch.int32), (f.batch,))),
+                             _ptr(_sized("mass", _dev(mass, torch.float32), (f.batch, f.n_kv_heads, f.max_seq))), budget,
+                             n_sink, n_recent, C.byref(ds),
+                             _ptr(_sized("dst_mass", _dev(dst_mass, torch.float32), (d.batch, d.n_kv_heads, d.max_seq))),
+                             _ptr(_sized("new_lens", _dev(new_lens, torch.int32), (f.batch,))),
+                             _ptr(_sized("kept", _dev(kept, torch.int32), (f.batch, f.n_kv_heads, budget))),
+                             _stream(stream)))
+    return kept, new_lens
+
+
+def gather_rows(cache, index, count, src_base=None, dst=None, dst_base=None, stream=None):
+    """kvbfp_gather_rows: rows src_base + index[.., i] -> dst_base + i; index i32 [B, n] (every head alike) or
+    [B, H_kv, n].  dst None: in place, at src_base."""
+    f = cache.fmt
+    if dst is None:
+        dst, dst_base = cache, src_base if dst_base is None else dst_base
+    heads = 1 if index.dim() == 2 else f.n_kv_heads
+    n = index.shape[-1]
+    cs, ds = cache.struct(), dst.struct()
+    _check(lib().kvbfp_gather_rows(C.byref(cs), C.byref(ds),
+                                   _ptr(_sized("index", _dev(index, torch.int32), (f.batch, n) if heads == 1 and index.dim() == 2
+                                               else (f.batch, heads, n))), heads, n,
+                                   _ptr(_sized("count", _dev(count, torch.int32), (f.batch,))),
+                                   _ptr(_sized("src_base", _dev(src_base, torch.int32), (f.batch,))),
+                                   _ptr(_sized("dst_base", _dev(dst_base, torch.int32), (f.batch,))), _stream(stream)))
 
 
 def device_status(stream=None):

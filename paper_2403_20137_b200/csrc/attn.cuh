@@ -1,0 +1,108 @@
+// Attention of several query rows per kv head over the packed cache (drafted trees, masked / capped / biased scores,
+// attention weights): arguments, the visible tiles of a sequence and the split of all tiles over the thread blocks.
+#pragma once
+#include "common.cuh"
+
+namespace kvbfp {
+
+constexpr int kAttnTile = 128;         // tokens per tile, the unit of the work split
+constexpr int kAttnMaxWorkers = 320;   // thread blocks that write partial results (two per SM at most)
+constexpr int kAttnMaxBatch = 1024;    // sequences whose tile counts fit in shared memory
+constexpr int kAttnPart = kHeadDim + 4;    // floats of a partial row: o[128], max (log2 units), sum, 2 unused
+constexpr int kAttnMaxDraft = 64;      // drafted tokens per sequence (bits of a mask word)
+
+struct AttnArgs {
+    kvbfp_format fmt;
+    const uint8_t *k_mant, *k_exp, *v_mant, *v_exp;
+    const void* q;                 // [B, T, Hq, d]
+    int q_is_bf16;                 // the output has the same type
+    int n_q_heads, group;
+    int n_draft;                   // T (1 for a single token)
+    int tree;                      // 0: the query is the last cached token, no drafted rows
+    int rows_tile, n_row_tiles;    // query rows (draft-major, group-minor) per work item and items per (batch, kv head)
+    const int32_t* ctx_lens;
+    const int32_t* draft_lens;     // or NULL: all T
+    const uint64_t* tree_mask;     // [B, T] or NULL: a chain
+    const int32_t* depth;          // [B, T] or NULL: depth = index
+    const int32_t* perm_k;
+    const int32_t* inv_perm_v;
+    float scale;
+    float softcap;
+    int window;
+    const float* slopes;
+    const int32_t* first;
+    const int32_t* prefix;
+    void* out;
+    int* plan;                     // workspace: cumulative tile counts of the sequences, [B + 1]
+    float* lse;                    // workspace: [B, Hq] log2-sum-exp2, with mass only (else NULL)
+    float* scores;                 // workspace: [B, Hq, max_seq] scores in log2 units, with mass only (else NULL)
+    float* mass;                   // [B, Hkv, max_seq] or NULL
+    float* partials;               // workspace: [2 * workers, rows_tile, kAttnPart]
+    int workers;                   // thread blocks of the main kernel
+    uint32_t* status;
+};
+
+// What of one sequence any query may see, in tiles: the prefix tiles [0, np), then the tiles from `lo` on, n in all.
+struct SeqView {
+    int ctx;       // cached tokens under the context rule
+    int nd;        // drafted rows that exist behind them
+    int first, pf; // tokens below `pf` are always visible, others from `first` on (and inside the window)
+    int lo, np, n;
+    bool clamped;  // a length was outside the cache
+    __device__ __forceinline__ int tile_token(int k) const { return (k < np ? k : k - np + lo) * kAttnTile; }
+};
+
+__device__ __forceinline__ SeqView seq_view(const AttnArgs& a, int b) {
+    SeqView s;
+    const int raw = a.ctx_lens[b], S = a.fmt.max_seq;
+    s.ctx = min(max(raw, 0), S);
+    s.clamped = s.ctx != raw;
+    s.nd = 0;
+    if (a.tree) {
+        int want = a.n_draft;
+        if (a.draft_lens) want = min(max(a.draft_lens[b], 0), a.n_draft);
+        s.nd = min(want, S - s.ctx);
+        s.clamped |= s.nd != want;
+    }
+    s.first = a.first ? min(max(a.first[b], 0), s.ctx) : 0;
+    s.pf = a.prefix ? min(max(a.prefix[b], 0), s.ctx) : 0;
+    int lo = s.first;
+    const int nearest = a.tree ? s.ctx : s.ctx - 1;              // the lowest query position
+    if (a.window > 0 && nearest - a.window + 1 > lo) lo = min(nearest - a.window + 1, s.ctx);
+    const int end = s.ctx + s.nd;
+    int t0 = lo / kAttnTile, t1 = (end + kAttnTile - 1) / kAttnTile;
+    if (lo >= end) t1 = t0;                                       // nothing but the prefix
+    int np = (s.pf + kAttnTile - 1) / kAttnTile;
+    if (np >= t0) {                                               // the two ranges touch
+        t1 = (t1 > t0) ? t1 : np;
+        if (t1 < np) t1 = np;
+        t0 = 0;
+        np = 0;
+    }
+    s.lo = t0;
+    s.np = np;
+    s.n = np + t1 - t0;
+    return s;
+}
+
+// All tiles, ordered by sequence, kv head, row tile, tile, are cut into `workers` contiguous ranges of at least one
+// (so workers <= n_items: the merge reads a partial of every worker between a row's first and last).
+__host__ __device__ __forceinline__ int worker_start(int w, int n_items, int workers) {
+    return (int)((int64_t)n_items * w / workers);
+}
+__host__ __device__ __forceinline__ int worker_of(int x, int n_items, int workers) {
+    return (int)(((int64_t)(x + 1) * workers - 1) / n_items);
+}
+
+// Channel slot 16 a + s sits at position 8 s + a of a partial row (the order the accumulators are in).
+__device__ __forceinline__ int part_pos(int slot) { return (slot & 15) * 8 + (slot >> 4); }
+
+// Cached values are carried times 2^-8 inside the kernels, so that no exponent byte leaves the bf16 range with the
+// conversion's offset; undone on scores and outputs.
+constexpr float kValueUp = 256.f;
+
+kvbfp_status launch_attn_rows4(const AttnArgs& a, cudaStream_t s);
+kvbfp_status launch_attn_rows6(const AttnArgs& a, cudaStream_t s);
+kvbfp_status launch_attn_rows8(const AttnArgs& a, cudaStream_t s);
+
+}  // namespace kvbfp

@@ -1,0 +1,6 @@
+// The 6-bit instantiations of attn_rows.
+#include "attn_rows.cuh"
+
+namespace kvbfp {
+kvbfp_status launch_attn_rows6(const AttnArgs& a, cudaStream_t s) { return launch_attn_p<6>(a, s); }
+}  // namespace kvbfp

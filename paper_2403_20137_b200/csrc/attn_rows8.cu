@@ -1,0 +1,6 @@
+// The 8-bit instantiations of attn_rows.
+#include "attn_rows.cuh"
+
+namespace kvbfp {
+kvbfp_status launch_attn_rows8(const AttnArgs& a, cudaStream_t s) { return launch_attn_p<8>(a, s); }
+}  // namespace kvbfp

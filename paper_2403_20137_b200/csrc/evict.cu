@@ -1,0 +1,306 @@
+// Dropping and moving cached rows: eviction by accumulated attention weight, and the gather of listed rows (the
+// accepted branch of a drafted tree) in all four planes of the packed cache.
+#include "common.cuh"
+
+namespace kvbfp {
+namespace {
+
+constexpr int kSelThreads = 1024, kSelWarps = kSelThreads / 32, kHistCopies = 8;
+
+// Weights in the order of unsigned integers: -0 as 0, NaN below everything.
+__device__ __forceinline__ uint32_t mass_key(float x) {
+    const uint32_t u = __float_as_uint(x + 0.f);
+    if ((u & 0x7fffffffu) > 0x7f800000u) return 0u;
+    return (u >> 31) ? ~u : (u | 0x80000000u);
+}
+
+// A block per (sequence, kv head): the rows to keep, in position order.  The heaviest `need` of the middle region are
+// found by radix selection (four digits of eight bits, histograms in shared memory); of equals to the threshold the
+// lowest positions are kept.  Each warp owns a contiguous piece of the region, so one scan over the warps' counts
+// places every kept row.
+__global__ void __launch_bounds__(kSelThreads) evict_select(const float* __restrict__ mass, const int32_t* __restrict__ seq_lens,
+                                                            int max_seq, int n_heads, int budget, int n_sink, int n_recent,
+                                                            int32_t* __restrict__ kept, uint32_t* status) {
+    __shared__ uint32_t hist[kHistCopies][256];
+    __shared__ uint32_t s_digit, s_need;
+    __shared__ int s_gt[kSelWarps], s_eq[kSelWarps];
+    pdl_wait();
+    pdl_trigger();
+    const int pair = blockIdx.x, b = pair / n_heads, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int raw = seq_lens[b], len = min(max(raw, 0), max_seq);
+    if (raw != len && tid == 0) raise_flag(status, KVBFP_FLAG_POSITION);
+    int32_t* out = kept + (int64_t)pair * budget;
+    if (len <= budget) {
+        for (int i = tid; i < budget; i += kSelThreads) out[i] = i < len ? i : -1;
+        return;
+    }
+    const int m0 = n_sink, m1 = len - n_recent;                   // the middle region; m1 - m0 > need
+    uint32_t need = (uint32_t)(budget - n_sink - n_recent);
+    for (int i = tid; i < n_sink; i += kSelThreads) out[i] = i;
+    for (int i = tid; i < n_recent; i += kSelThreads) out[budget - n_recent + i] = m1 + i;
+    if (need == 0) return;
+    const float* x = mass + (int64_t)pair * max_seq;
+    uint32_t thr = 0;
+    for (int shift = 24; shift >= 0; shift -= 8) {
+        for (int i = tid; i < kHistCopies * 256; i += kSelThreads) (&hist[0][0])[i] = 0;
+        __syncthreads();
+        uint32_t* h = hist[warp % kHistCopies];
+#pragma unroll 8
+        for (int i = m0 + tid; i < m1; i += kSelThreads) {
+            const uint32_t key = mass_key(x[i]);
+            if (shift == 24 || (key >> (shift + 8)) == (thr >> (shift + 8))) atomicAdd(&h[(key >> shift) & 255u], 1u);
+        }
+        __syncthreads();
+        if (warp == 0) {       // bins from the top: lane l holds bins 255 - 8 l .. 248 - 8 l
+            uint32_t c[8], sum = 0;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                c[j] = 0;
+#pragma unroll
+                for (int k = 0; k < kHistCopies; ++k) c[j] += hist[k][255 - 8 * lane - j];
+                sum += c[j];
+            }
+            uint32_t above = sum;
+#pragma unroll
+            for (int off = 1; off < 32; off <<= 1) {
+                const uint32_t y = __shfl_up_sync(0xffffffffu, above, off);
+                if (lane >= off) above += y;
+            }
+            above -= sum;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                if (above < need && above + c[j] >= need) { s_digit = 255u - 8u * lane - j; s_need = need - above; }
+                above += c[j];
+            }
+        }
+        __syncthreads();
+        thr |= s_digit << shift;
+        need = s_need;                     // of the rows that share the digits so far
+        __syncthreads();
+    }
+    // need = rows equal to the threshold that are kept
+    const int per = ((m1 - m0 + kSelWarps - 1) / kSelWarps + 31) & ~31;
+    const int w0 = min(m0 + warp * per, m1), w1 = min(w0 + per, m1);
+    int gt = 0, eq = 0;
+#pragma unroll 8
+    for (int i = w0 + lane; i < w1; i += 32) {
+        const uint32_t key = mass_key(x[i]);
+        gt += key > thr;
+        eq += key == thr;
+    }
+#pragma unroll
+    for (int off = 16; off; off >>= 1) {
+        gt += __shfl_xor_sync(0xffffffffu, gt, off);
+        eq += __shfl_xor_sync(0xffffffffu, eq, off);
+    }
+    if (lane == 0) { s_gt[warp] = gt; s_eq[warp] = eq; }
+    __syncthreads();
+    int gt0 = 0, eq0 = 0;
+    for (int w = 0; w < warp; ++w) { gt0 += s_gt[w]; eq0 += s_eq[w]; }
+    const int quota = (int)need;
+    for (int i0 = w0; i0 < w1; i0 += 32) {
+        const int i = i0 + lane;
+        const uint32_t key = i < w1 ? mass_key(x[i]) : 0u;
+        const bool is_gt = i < w1 && key > thr, is_eq = i < w1 && key == thr;
+        const uint32_t bg = __ballot_sync(0xffffffffu, is_gt), be = __ballot_sync(0xffffffffu, is_eq);
+        const uint32_t below = (1u << lane) - 1u;
+        const int eq_rank = eq0 + __popc(be & below);
+        if (is_gt || (is_eq && eq_rank < quota)) out[n_sink + gt0 + __popc(bg & below) + min(eq_rank, quota)] = i;
+        gt0 += __popc(bg);
+        eq0 += __popc(be);
+    }
+}
+
+struct MoveArgs {
+    kvbfp_format src, dst;              // same batch, heads and row format
+    const uint8_t* from[4];             // k_mant, k_exp, v_mant, v_exp
+    uint8_t* to[4];
+    const int32_t* index;               // [batch, heads or 1, n_index]
+    int index_heads, n_index;
+    const int32_t* count;               // [batch] or NULL: up to the first negative index
+    const int32_t* src_base;            // [batch] or NULL: 0
+    const int32_t* dst_base;
+    const float* mass;                  // [batch, heads, src.max_seq] or NULL
+    float* to_mass;                     // [batch, heads, dst.max_seq], zero behind the moved rows
+    int32_t* new_lens;                  // eviction: [batch], the number of kept rows
+    uint32_t* status;
+};
+
+constexpr int kMoveThreads = 256, kMoveRows = 128;
+
+// Rows src_base + index[i] -> dst_base + i of all planes, kMoveRows at a time through registers.  A block per (chunk,
+// pair) where the caches differ; in place one block per pair walks the chunks upwards: every row of a chunk is read
+// before any is written, and with ascending indices (index[i] >= i) later chunks read only rows behind the written
+// ones.
+template <bool IN_PLACE, int PIECES>      // 16-byte pieces of a mantissa row: 4, 6, 8
+__global__ void __launch_bounds__(kMoveThreads) move_rows(const MoveArgs a) {
+    constexpr int PER = kMoveRows * PIECES / kMoveThreads;      // pieces per thread and plane
+    __shared__ int src_row[kMoveRows];
+    pdl_wait();
+    pdl_trigger();
+    const int H = a.src.n_kv_heads, pair = blockIdx.x, b = pair / H, h = pair - b * H, tid = threadIdx.x;
+    const int row_e = kHeadDim / a.src.block;
+    const int32_t* idx = a.index + ((int64_t)b * a.index_heads + (a.index_heads == 1 ? 0 : h)) * a.n_index;
+    const int n = a.count ? min(max(a.count[b], 0), a.n_index) : a.n_index;
+    const int sb = a.src_base ? a.src_base[b] : 0, db = a.dst_base ? a.dst_base[b] : 0;
+    const int64_t src0 = (int64_t)pair * a.src.max_seq, dst0 = (int64_t)pair * a.dst.max_seq;
+    for (int c = IN_PLACE ? 0 : blockIdx.y; c * kMoveRows < n; c += IN_PLACE ? 1 : gridDim.y) {
+        __syncthreads();
+        if (tid < kMoveRows) {
+            const int i = c * kMoveRows + tid;
+            int r = -1;
+            if (i < n) {
+                const int v = idx[i];
+                const int64_t s = (int64_t)sb + v, d = (int64_t)db + i;
+                if (v >= 0) {
+                    if (s >= 0 && s < a.src.max_seq && d >= 0 && d < a.dst.max_seq) r = (IN_PLACE && s == d) ? -1 : (int)s;
+                    else raise_flag(a.status, KVBFP_FLAG_POSITION);
+                } else if (a.count) {
+                    raise_flag(a.status, KVBFP_FLAG_POSITION);
+                }
+            }
+            src_row[tid] = r;
+        }
+        __syncthreads();
+        uint4 km[PER], vm[PER];
+#pragma unroll
+        for (int j = 0; j < PER; ++j) {
+            const int x = tid + j * kMoveThreads, r = src_row[x / PIECES];
+            if (r >= 0) {
+                const int64_t at = (src0 + r) * (PIECES * 16) + (x % PIECES) * 16;
+                km[j] = *reinterpret_cast<const uint4*>(a.from[0] + at);
+                vm[j] = *reinterpret_cast<const uint4*>(a.from[2] + at);
+            }
+        }
+        // exponent bytes: a thread per (row, plane)
+        const int er = tid & (kMoveRows - 1), ep = 1 + 2 * (tid / kMoveRows);
+        const int es = src_row[er];
+        uint8_t eb[8];
+        if (es >= 0)
+            for (int j = 0; j < row_e; ++j) eb[j] = a.from[ep][(src0 + es) * row_e + j];
+        float w = 0.f;
+        if (a.mass && tid < kMoveRows && src_row[tid] >= 0) w = a.mass[src0 + src_row[tid]];
+        if (IN_PLACE) __syncthreads();
+        const int64_t d0 = dst0 + db + (int64_t)c * kMoveRows;
+#pragma unroll
+        for (int j = 0; j < PER; ++j) {
+            const int x = tid + j * kMoveThreads, r = x / PIECES;
+            if (src_row[r] >= 0) {
+                const int64_t at = (d0 + r) * (PIECES * 16) + (x % PIECES) * 16;
+                *reinterpret_cast<uint4*>(a.to[0] + at) = km[j];
+                *reinterpret_cast<uint4*>(a.to[2] + at) = vm[j];
+            }
+        }
+        if (es >= 0)
+            for (int j = 0; j < row_e; ++j) a.to[ep][(d0 + er) * row_e + j] = eb[j];
+        if (a.mass && tid < kMoveRows && src_row[tid] >= 0) a.to_mass[d0 + tid] = w;
+    }
+    if (a.new_lens && (IN_PLACE || blockIdx.y == 0)) {
+        // behind the moved rows: weights zero, so that rows appended there start from nothing
+        __shared__ int s_kept;
+        if (tid == 0) s_kept = 0;
+        __syncthreads();
+        int mine = 0;
+        for (int i = tid; i < a.n_index; i += kMoveThreads) mine += idx[i] >= 0;
+        if (mine) atomicAdd(&s_kept, mine);
+        __syncthreads();
+        const int kept = s_kept;
+        for (int i = kept + tid; i < a.dst.max_seq; i += kMoveThreads) a.to_mass[dst0 + i] = 0.f;
+        if (h == 0 && tid == 0) a.new_lens[b] = kept;
+    }
+}
+
+kvbfp_status launch_move(const MoveArgs& a, cudaStream_t s) {
+    const int64_t pairs = (int64_t)a.src.batch * a.src.n_kv_heads;
+    const bool in_place = a.to[0] == a.from[0];
+    const int chunks = (a.n_index + kMoveRows - 1) / kMoveRows;
+    const dim3 grid((unsigned)pairs, in_place ? 1u : (unsigned)(chunks < 65535 ? chunks : 65535));
+    const int pieces = a.src.mant_bits;      // 16-byte pieces: 128 p / 8 / 16 = p
+    cudaError_t e;
+    if (in_place)
+        e = pieces == 4 ? launch_pdl(move_rows<true, 4>, grid, dim3(kMoveThreads), 0, s, a)
+            : pieces == 6 ? launch_pdl(move_rows<true, 6>, grid, dim3(kMoveThreads), 0, s, a)
+                          : launch_pdl(move_rows<true, 8>, grid, dim3(kMoveThreads), 0, s, a);
+    else
+        e = pieces == 4 ? launch_pdl(move_rows<false, 4>, grid, dim3(kMoveThreads), 0, s, a)
+            : pieces == 6 ? launch_pdl(move_rows<false, 6>, grid, dim3(kMoveThreads), 0, s, a)
+                          : launch_pdl(move_rows<false, 8>, grid, dim3(kMoveThreads), 0, s, a);
+    KVBFP_CUDA(e);
+    KVBFP_LAUNCH_CHECK("move_rows");
+    return KVBFP_OK;
+}
+
+// Fills the caches of `a`; in place means the same four planes, anything else has to be apart.
+kvbfp_status set_caches(const kvbfp_cache* src, const kvbfp_cache* dst, MoveArgs* a) {
+    if (!src || !dst) return KVBFP_ERR_INVALID_ARG;
+    kvbfp_status st = check_format(&src->fmt);
+    if (st == KVBFP_OK) st = check_format(&dst->fmt);
+    if (st != KVBFP_OK) return st;
+    const kvbfp_format &f = src->fmt, &d = dst->fmt;
+    if (f.batch != d.batch || f.n_kv_heads != d.n_kv_heads || f.block != d.block || f.mant_bits != d.mant_bits)
+        return KVBFP_ERR_INVALID_ARG;
+    if ((int64_t)f.batch * f.n_kv_heads >= (int64_t)1 << 31) return KVBFP_ERR_UNSUPPORTED;
+    a->src = f;
+    a->dst = d;
+    const uint8_t* from[4] = {src->k_mant, src->k_exp, src->v_mant, src->v_exp};
+    uint8_t* to[4] = {dst->k_mant, dst->k_exp, dst->v_mant, dst->v_exp};
+    int same = 0;
+    for (int i = 0; i < 4; ++i) {
+        if (!from[i] || !to[i]) return KVBFP_ERR_INVALID_ARG;
+        if (!aligned16(from[i]) || !aligned16(to[i])) return KVBFP_ERR_ALIGNMENT;
+        a->from[i] = from[i];
+        a->to[i] = to[i];
+        same += from[i] == to[i];
+    }
+    if (same != 0 && (same != 4 || f.max_seq != d.max_seq)) return KVBFP_ERR_INVALID_ARG;
+    const size_t pairs = (size_t)f.batch * f.n_kv_heads;
+    for (int i = 0; i < 4 && same == 0; ++i) {        // different caches must not overlap
+        const size_t row = (i & 1) ? row_e_bytes(f) : row_m_bytes(f);
+        const uintptr_t x = (uintptr_t)from[i], y = (uintptr_t)to[i];
+        if (x < y + pairs * d.max_seq * row && y < x + pairs * f.max_seq * row) return KVBFP_ERR_INVALID_ARG;
+    }
+    return KVBFP_OK;
+}
+
+}  // namespace
+}  // namespace kvbfp
+
+extern "C" kvbfp_status kvbfp_gather_rows(const kvbfp_cache* src, const kvbfp_cache* dst, const int32_t* index,
+                                          int32_t index_heads, int32_t n_index, const int32_t* count,
+                                          const int32_t* src_base, const int32_t* dst_base, void* stream) {
+    using namespace kvbfp;
+    MoveArgs a = {};
+    if (!index || !count || n_index < 1) return KVBFP_ERR_INVALID_ARG;
+    kvbfp_status st = set_caches(src, dst, &a);
+    if (st != KVBFP_OK) return st;
+    if (index_heads != 1 && index_heads != src->fmt.n_kv_heads) return KVBFP_ERR_INVALID_ARG;
+    a.index = index; a.index_heads = index_heads; a.n_index = n_index; a.count = count;
+    a.src_base = src_base; a.dst_base = dst_base;
+    st = status_word(&a.status);
+    if (st != KVBFP_OK) return st;
+    return launch_move(a, (cudaStream_t)stream);
+}
+
+extern "C" kvbfp_status kvbfp_evict(const kvbfp_cache* src, const int32_t* seq_lens, const float* mass, int32_t budget,
+                                    int32_t n_sink, int32_t n_recent, const kvbfp_cache* dst, float* dst_mass,
+                                    int32_t* new_lens, int32_t* kept, void* stream) {
+    using namespace kvbfp;
+    MoveArgs a = {};
+    if (!seq_lens || !mass || !dst_mass || !new_lens || !kept) return KVBFP_ERR_INVALID_ARG;
+    if (budget < 1 || n_sink < 0 || n_recent < 0 || n_sink > budget || n_recent > budget - n_sink)
+        return KVBFP_ERR_INVALID_ARG;
+    kvbfp_status st = set_caches(src, dst, &a);
+    if (st != KVBFP_OK) return st;
+    if (budget > dst->fmt.max_seq) return KVBFP_ERR_CAPACITY;
+    if (!aligned16(mass) || !aligned16(dst_mass) || !aligned16(kept)) return KVBFP_ERR_ALIGNMENT;
+    if ((dst_mass == mass) != (a.from[0] == a.to[0])) return KVBFP_ERR_INVALID_ARG;
+    st = status_word(&a.status);
+    if (st != KVBFP_OK) return st;
+    cudaStream_t s = (cudaStream_t)stream;
+    KVBFP_CUDA(launch_pdl(evict_select, dim3((unsigned)(src->fmt.batch * src->fmt.n_kv_heads)), dim3(kSelThreads), 0, s,
+                          mass, seq_lens, src->fmt.max_seq, src->fmt.n_kv_heads, budget, n_sink, n_recent, kept, a.status));
+    KVBFP_LAUNCH_CHECK("evict_select");
+    a.index = kept; a.index_heads = src->fmt.n_kv_heads; a.n_index = budget;
+    a.mass = mass; a.to_mass = dst_mass; a.new_lens = new_lens;
+    return launch_move(a, s);
+}
