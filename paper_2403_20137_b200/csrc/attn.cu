@@ -8,7 +8,7 @@ namespace kvbfp {
 namespace {
 
 // One warp (SPLIT: one block of four) per query row: out = sum_w 2^(m_w - m) o_w / sum_w 2^(m_w - m) l_w over the
-// partials of the blocks that share the row's tiles.  Rows whose tiles one block had are written already; rows that
+// partials of the warps that share the row's tiles.  Rows whose tiles one warp had are written already; rows that
 // see no tile are zeros.
 template <bool SPLIT>
 __global__ void __launch_bounds__(128) attn_merge(const AttnArgs a, int64_t n_rows) {
@@ -35,7 +35,7 @@ __global__ void __launch_bounds__(128) attn_merge(const AttnArgs a, int64_t n_ro
         if (w0 == w1) return;
     }
     auto part = [&](int w) {
-        return a.partials + ((int64_t)(2 * w + (w == w0 ? 1 : 0)) * a.rows_tile + r) * kAttnPart;
+        return a.partials + ((int64_t)(2 * w + (w == w0 ? 1 : 0)) * a.part_rows + r) * kAttnPart;
     };
     float m = -INFINITY, l = 0.f;
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -96,14 +96,14 @@ __global__ void __launch_bounds__(128) attn_merge(const AttnArgs a, int64_t n_ro
     __syncwarp();
     const float* src = so[SPLIT ? 0 : warp];
     bool live = n > 0;
-    if (live && a.tree) live = i < seq_view(a, b).nd;
+    if (live && a.tree) live = i < a.views[b].nd;
     const float inv = (live && l != 0.f) ? kValueUp / l : 0.f;
     float v[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
         const int c = 4 * lane + e;
         const int slot = a.inv_perm_v ? (a.inv_perm_v[hk * D + c] & (D - 1)) : c;
-        v[e] = inv == 0.f ? 0.f : src[part_pos(slot)] * inv;
+        v[e] = inv == 0.f ? 0.f : src[slot] * inv;
     }
     const int64_t at = (((int64_t)b * a.n_draft + i) * a.n_q_heads + hq) * D + 4 * lane;
     if (a.q_is_bf16)
@@ -114,15 +114,16 @@ __global__ void __launch_bounds__(128) attn_merge(const AttnArgs a, int64_t n_ro
     if (a.lse && lane == 0) a.lse[(int64_t)b * a.n_q_heads + hq] = l > 0.f ? m + log2f(l) : (l == 0.f ? INFINITY : l);
 }
 
-// mass[b, h, t] += sum over the group's query heads of 2^(score - lse).  A warp per 128-token tile, each lane four
-// tokens; the tiles are those the scores were written for.  Memory-bound: 4 G + 8 bytes a token.
+// mass[b, h, t] += sum over the group's query heads of 2^(score - lse).  tile / 4 lanes per tile, four tokens a lane;
+// the tiles are those the scores were written for.  Memory-bound: 4 G + 8 bytes a token.
 __global__ void __launch_bounds__(128) attn_mass(const AttnArgs a) {
     pdl_wait();
     pdl_trigger();
-    const int B = a.fmt.batch, Hkv = a.fmt.n_kv_heads, max_seq = a.fmt.max_seq, lane = threadIdx.x & 31;
-    const int n_items = a.plan[B] * Hkv, workers = gridDim.x * 4, me = blockIdx.x * 4 + (threadIdx.x >> 5);
+    const int B = a.fmt.batch, Hkv = a.fmt.n_kv_heads, max_seq = a.fmt.max_seq;
+    const int lanes = a.tile / 4, teams = gridDim.x * (128 / lanes), me = (blockIdx.x * 128 + threadIdx.x) / lanes;
+    const int n_items = a.plan[B] * Hkv;
     if (n_items == 0) return;
-    const int i0 = worker_start(me, n_items, workers), i1 = worker_start(me + 1, n_items, workers);
+    const int i0 = worker_start(me, n_items, teams), i1 = worker_start(me + 1, n_items, teams);
     if (i0 >= i1) return;
     int lo = 0, hi = B - 1;
     while (lo < hi) {
@@ -131,9 +132,9 @@ __global__ void __launch_bounds__(128) attn_mass(const AttnArgs a) {
     }
     int b = lo, n = a.plan[lo + 1] - a.plan[lo];
     int h = (i0 - a.plan[lo] * Hkv) / n, k = i0 - a.plan[lo] * Hkv - h * n;
-    SeqView sv = seq_view(a, b);
+    SeqView sv = a.views[b];
     for (int item = i0; item < i1; ++item) {
-        const int tok = sv.tile_token(k) + 4 * lane;
+        const int tok = tile_token(sv, k, a.tile) + 4 * (threadIdx.x % lanes);
         if (tok < sv.ctx) {
             float4* to = reinterpret_cast<float4*>(a.mass + ((int64_t)b * Hkv + h) * max_seq + tok);
             float4 acc = *to;
@@ -143,7 +144,7 @@ __global__ void __launch_bounds__(128) attn_mass(const AttnArgs a) {
                 const float4 s = *reinterpret_cast<const float4*>(y + (int64_t)q * max_seq);
                 const float z = ls[q];
                 acc.x += exp2f(s.x - z);
-                if (tok + 1 < sv.ctx) acc.y += exp2f(s.y - z);       // (scores past the end were not written)
+                if (tok + 1 < sv.ctx) acc.y += exp2f(s.y - z);       // (behind the end there is nothing of this call)
                 if (tok + 2 < sv.ctx) acc.z += exp2f(s.z - z);
                 if (tok + 3 < sv.ctx) acc.w += exp2f(s.w - z);
             }
@@ -156,17 +157,53 @@ __global__ void __launch_bounds__(128) attn_mass(const AttnArgs a) {
                 do { ++b; } while (b < B && a.plan[b + 1] == a.plan[b]);
                 if (b < B) {
                     n = a.plan[b + 1] - a.plan[b];
-                    sv = seq_view(a, b);
+                    sv = a.views[b];
                 }
             }
         }
     }
 }
 
-// Query rows per work item: all rows of a kv head up to 64 share its tiles; fp32 queries take 16 at a time.
+// Query rows per work item: up to 64 bf16 rows of a kv head share its tiles; fp32 queries take 16 at a time (their three
+// bf16 terms fill the registers of the warp-level kernel).
 inline int rows_tile_for(int rows, bool bf16) { return !bf16 || rows <= 16 ? 16 : rows <= 32 ? 32 : 64; }
+inline int max_workers(bool bf16) { return bf16 ? 160 : kAttnMaxBlocks * kAttnWarps; }
 
 inline size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
+
+// Workspace regions in order; returns the size and, with `a`, sets the pointers.
+size_t lay_out(const kvbfp_format& f, int n_q_heads, int n_draft, bool bf16, bool with_mass, AttnArgs* a, uint8_t* base) {
+    const int rows = n_draft * (n_q_heads / f.n_kv_heads), tile = rows_tile_for(rows, bf16);
+    const size_t items = (size_t)f.batch * f.n_kv_heads * ((rows + tile - 1) / tile);
+    size_t at = 0;
+    auto take = [&](size_t bytes) {
+        uint8_t* p = base + at;
+        at += up256(bytes);
+        return p;
+    };
+    uint8_t* plan = take((size_t)(f.batch + 1) * sizeof(int));
+    uint8_t* views = take((size_t)f.batch * sizeof(SeqView));
+    uint8_t* dpos = take((size_t)f.batch * kAttnMaxDraft * sizeof(int));
+    uint8_t* info = take(items * tile * sizeof(RowInfo));
+    uint8_t* frag = take(items * tile * kHeadDim * 2 * (bf16 ? 1 : 3));
+    uint8_t *lse = nullptr, *scores = nullptr;
+    if (with_mass) {
+        lse = take((size_t)f.batch * n_q_heads * 4);
+        scores = take((size_t)f.batch * n_q_heads * f.max_seq * 4);
+    }
+    uint8_t* part = take((size_t)2 * max_workers(bf16) * (rows < tile ? rows : tile) * kAttnPart * 4);
+    if (a) {
+        a->plan = reinterpret_cast<int*>(plan);
+        a->views = reinterpret_cast<SeqView*>(views);
+        a->dpos = reinterpret_cast<int*>(dpos);
+        a->rows = reinterpret_cast<RowInfo*>(info);
+        a->qfrag = reinterpret_cast<uint4*>(frag);
+        a->lse = reinterpret_cast<float*>(lse);
+        a->scores = reinterpret_cast<float*>(scores);
+        a->partials = reinterpret_cast<float*>(part);
+    }
+    return at;
+}
 
 struct AttnCall {
     const kvbfp_cache* cache;
@@ -207,9 +244,10 @@ kvbfp_status attn_common(const AttnCall& c) {
         if (p && !aligned16(p)) return KVBFP_ERR_ALIGNMENT;
     const int rows = c.n_draft * group;
     const int rows_tile = rows_tile_for(rows, c.dt == KVBFP_BF16), n_row_tiles = (rows + rows_tile - 1) / rows_tile;
-    const int64_t most = (int64_t)f.batch * f.n_kv_heads * n_row_tiles * (f.max_seq / kAttnTile + 2);
     const int64_t n_rows = (int64_t)f.batch * f.n_kv_heads * rows;
-    if (most >= (int64_t)1 << 31 || n_rows >= (int64_t)1 << 31) return KVBFP_ERR_UNSUPPORTED;    // item numbers are 32-bit
+    // tile numbers and row numbers are 32-bit
+    if ((int64_t)f.batch * f.n_kv_heads * n_row_tiles * (f.max_seq / 32 + 2) >= (int64_t)1 << 31 || n_rows >= (int64_t)1 << 31)
+        return KVBFP_ERR_UNSUPPORTED;
     const size_t need = kvbfp_attn_workspace_bytes(&f, c.n_q_heads, c.n_draft, c.with_mass);
     if (!c.workspace || c.workspace_bytes < need) return KVBFP_ERR_WORKSPACE;
 
@@ -218,7 +256,7 @@ kvbfp_status attn_common(const AttnCall& c) {
     a.k_mant = c.cache->k_mant; a.k_exp = c.cache->k_exp; a.v_mant = c.cache->v_mant; a.v_exp = c.cache->v_exp;
     a.q = c.q; a.q_is_bf16 = c.dt == KVBFP_BF16; a.n_q_heads = c.n_q_heads; a.group = group; a.n_draft = c.n_draft;
     a.tree = c.tree;
-    a.rows_tile = rows_tile; a.n_row_tiles = n_row_tiles;
+    a.rows_tile = rows_tile; a.n_row_tiles = n_row_tiles; a.part_rows = rows < rows_tile ? rows : rows_tile;
     a.ctx_lens = c.ctx_lens; a.draft_lens = c.draft_lens; a.tree_mask = c.tree_mask; a.depth = c.depth;
     a.perm_k = c.perm_k; a.inv_perm_v = c.inv_perm_v;
     a.scale = c.softmax_scale > 0.f ? c.softmax_scale : 1.0f / sqrtf((float)f.head_dim);
@@ -227,35 +265,29 @@ kvbfp_status attn_common(const AttnCall& c) {
         a.first = c.mod->first; a.prefix = c.mod->prefix;
     }
     a.out = c.out;
-    uint8_t* w = static_cast<uint8_t*>(c.workspace);
-    a.plan = reinterpret_cast<int*>(w);
-    w += up256((size_t)(f.batch + 1) * 4);
-    if (c.with_mass) {
-        a.mass = c.mass;
-        a.lse = reinterpret_cast<float*>(w);
-        w += up256((size_t)f.batch * c.n_q_heads * 4);
-        a.scores = reinterpret_cast<float*>(w);
-        w += (size_t)f.batch * c.n_q_heads * f.max_seq * 4;
-    }
-    a.partials = reinterpret_cast<float*>(w);
+    a.mass = c.mass;
+    (void)lay_out(f, c.n_q_heads, c.n_draft, c.dt == KVBFP_BF16, c.with_mass, &a, static_cast<uint8_t*>(c.workspace));
     st = status_word(&a.status);
     if (st != KVBFP_OK) return st;
     int n_sm = 0;
     st = sm_count(&n_sm);
     if (st != KVBFP_OK) return st;
-    // Two blocks per SM where their shared memory allows it (64 query rows over 6- and 8-bit tiles take over half).
-    int64_t workers = (int64_t)n_sm * (rows_tile == 64 && f.mant_bits != 4 ? 1 : 2);
-    if (workers > kAttnMaxWorkers) workers = kAttnMaxWorkers;
-    if (workers > most) workers = most;
-    a.workers = (int)workers;
+    const bool bf16 = c.dt == KVBFP_BF16;
+    const AttnShape shape = bf16 ? AttnShape{128, 1} : f.mant_bits == 4 ? attn_shape4(a) : f.mant_bits == 6 ? attn_shape6(a) : attn_shape8(a);
+    a.tile = shape.tile;
+    const int64_t most = (int64_t)f.batch * f.n_kv_heads * n_row_tiles * (f.max_seq / shape.tile + 2);    // tiles at the longest
+    int64_t grid = (int64_t)n_sm * shape.blocks_per_sm;
+    const int per_block = bf16 ? 1 : kAttnWarps;
+    if (grid * per_block > max_workers(bf16)) grid = max_workers(bf16) / per_block;
+    if (grid > most) grid = most;
+    a.workers = (int)grid * per_block;
 
     cudaStream_t s = (cudaStream_t)c.stream;
-    if (f.mant_bits == 4) st = launch_attn_rows4(a, s);
-    else if (f.mant_bits == 6) st = launch_attn_rows6(a, s);
-    else st = launch_attn_rows8(a, s);
+    if (bf16) st = f.mant_bits == 4 ? launch_attn_umma4(a, (int)grid, s) : f.mant_bits == 6 ? launch_attn_umma6(a, (int)grid, s) : launch_attn_umma8(a, (int)grid, s);
+    else st = f.mant_bits == 4 ? launch_attn_rows4(a, (int)grid, s) : f.mant_bits == 6 ? launch_attn_rows6(a, (int)grid, s) : launch_attn_rows8(a, (int)grid, s);
     if (st != KVBFP_OK) return st;
     // partials of a row, about: a block per row where they are many
-    const bool split = workers / ((int64_t)f.batch * f.n_kv_heads * n_row_tiles) >= 8;
+    const bool split = a.workers / ((int64_t)f.batch * f.n_kv_heads * n_row_tiles) >= 8;
     if (split) KVBFP_CUDA(launch_pdl(attn_merge<true>, dim3((unsigned)n_rows), dim3(128), 0, s, a, n_rows));
     else KVBFP_CUDA(launch_pdl(attn_merge<false>, dim3((unsigned)((n_rows + 3) / 4)), dim3(128), 0, s, a, n_rows));
     KVBFP_LAUNCH_CHECK("attn_merge");
@@ -274,10 +306,10 @@ extern "C" size_t kvbfp_attn_workspace_bytes(const kvbfp_format* fmt, int32_t n_
                                              int32_t with_mass) {
     using namespace kvbfp;
     if (check_format(fmt) != KVBFP_OK || n_q_heads < 1 || n_q_heads % fmt->n_kv_heads != 0 || n_draft < 1) return 0;
-    const int64_t rows = (int64_t)n_draft * (n_q_heads / fmt->n_kv_heads);
-    size_t n = up256((size_t)(fmt->batch + 1) * 4);
-    if (with_mass) n += up256((size_t)fmt->batch * n_q_heads * 4) + (size_t)fmt->batch * n_q_heads * fmt->max_seq * 4;
-    return n + (size_t)2 * kAttnMaxWorkers * rows_tile_for(rows > 64 ? 64 : (int)rows, true) * kAttnPart * sizeof(float);
+    if (n_draft > kAttnMaxDraft || n_q_heads / fmt->n_kv_heads > 8) return 0;
+    const size_t x = lay_out(*fmt, n_q_heads, n_draft, true, with_mass != 0, nullptr, nullptr);
+    const size_t y = lay_out(*fmt, n_q_heads, n_draft, false, with_mass != 0, nullptr, nullptr);
+    return x > y ? x : y;
 }
 
 extern "C" kvbfp_status kvbfp_tree_attn(const kvbfp_cache* cache, const void* q, kvbfp_dtype dt, int32_t n_q_heads,

@@ -5,11 +5,27 @@
 
 namespace kvbfp {
 
-constexpr int kAttnTile = 128;         // tokens per tile, the unit of the work split
-constexpr int kAttnMaxWorkers = 320;   // thread blocks that write partial results (two per SM at most)
-constexpr int kAttnMaxBatch = 1024;    // sequences whose tile counts fit in shared memory
+constexpr int kAttnWarps = 4;          // warps per thread block of attn_rows; every warp is a worker of its own
+constexpr int kAttnMaxBlocks = 3 * 160;    // thread blocks of attn_rows
+constexpr int kAttnMaxBatch = 1024;    // sequences
 constexpr int kAttnPart = kHeadDim + 4;    // floats of a partial row: o[128], max (log2 units), sum, 2 unused
 constexpr int kAttnMaxDraft = 64;      // drafted tokens per sequence (bits of a mask word)
+
+// What of one sequence any query may see, in tiles: the prefix tiles [0, np), then the tiles from `lo` on, n in all.
+struct SeqView {
+    int ctx;       // cached tokens under the context rule
+    int nd;        // drafted rows that exist behind them
+    int first, pf; // tokens below `pf` are always visible, others from `first` on (and inside the window)
+    int lo, np, n;
+    int clamped;   // a length was outside the cache
+};
+__device__ __forceinline__ int tile_token(const SeqView& s, int k, int tile) { return (k < s.np ? k : k - s.np + s.lo) * tile; }
+
+struct RowInfo {
+    int pos;           // position of the query row's token
+    float slope;
+    uint32_t m0, m1;   // drafted tokens it sees (all clear for rows that do not exist)
+};
 
 struct AttnArgs {
     kvbfp_format fmt;
@@ -20,6 +36,8 @@ struct AttnArgs {
     int n_draft;                   // T (1 for a single token)
     int tree;                      // 0: the query is the last cached token, no drafted rows
     int rows_tile, n_row_tiles;    // query rows (draft-major, group-minor) per work item and items per (batch, kv head)
+    int part_rows;                 // rows of a partial: min(all rows, rows_tile)
+    int tile;                      // tokens per tile, the unit of the work split
     const int32_t* ctx_lens;
     const int32_t* draft_lens;     // or NULL: all T
     const uint64_t* tree_mask;     // [B, T] or NULL: a chain
@@ -34,22 +52,16 @@ struct AttnArgs {
     const int32_t* prefix;
     void* out;
     int* plan;                     // workspace: cumulative tile counts of the sequences, [B + 1]
+    SeqView* views;                // workspace: [B]
+    int* dpos;                     // workspace: [B, 64] positions of the drafted rows
+    RowInfo* rows;                 // workspace: [B * Hkv * n_row_tiles, rows_tile]
+    uint4* qfrag;                  // workspace: pi(q) in fragment order, [B * Hkv * n_row_tiles][split][m tile][k step][lane]
     float* lse;                    // workspace: [B, Hq] log2-sum-exp2, with mass only (else NULL)
     float* scores;                 // workspace: [B, Hq, max_seq] scores in log2 units, with mass only (else NULL)
     float* mass;                   // [B, Hkv, max_seq] or NULL
-    float* partials;               // workspace: [2 * workers, rows_tile, kAttnPart]
-    int workers;                   // thread blocks of the main kernel
+    float* partials;               // workspace: [2 * workers, part_rows, kAttnPart]
+    int workers;                   // warps of the main kernel
     uint32_t* status;
-};
-
-// What of one sequence any query may see, in tiles: the prefix tiles [0, np), then the tiles from `lo` on, n in all.
-struct SeqView {
-    int ctx;       // cached tokens under the context rule
-    int nd;        // drafted rows that exist behind them
-    int first, pf; // tokens below `pf` are always visible, others from `first` on (and inside the window)
-    int lo, np, n;
-    bool clamped;  // a length was outside the cache
-    __device__ __forceinline__ int tile_token(int k) const { return (k < np ? k : k - np + lo) * kAttnTile; }
 };
 
 __device__ __forceinline__ SeqView seq_view(const AttnArgs& a, int b) {
@@ -62,7 +74,7 @@ __device__ __forceinline__ SeqView seq_view(const AttnArgs& a, int b) {
         int want = a.n_draft;
         if (a.draft_lens) want = min(max(a.draft_lens[b], 0), a.n_draft);
         s.nd = min(want, S - s.ctx);
-        s.clamped |= s.nd != want;
+        s.clamped |= (int)(s.nd != want);
     }
     s.first = a.first ? min(max(a.first[b], 0), s.ctx) : 0;
     s.pf = a.prefix ? min(max(a.prefix[b], 0), s.ctx) : 0;
@@ -70,9 +82,9 @@ __device__ __forceinline__ SeqView seq_view(const AttnArgs& a, int b) {
     const int nearest = a.tree ? s.ctx : s.ctx - 1;              // the lowest query position
     if (a.window > 0 && nearest - a.window + 1 > lo) lo = min(nearest - a.window + 1, s.ctx);
     const int end = s.ctx + s.nd;
-    int t0 = lo / kAttnTile, t1 = (end + kAttnTile - 1) / kAttnTile;
+    int t0 = lo / a.tile, t1 = (end + a.tile - 1) / a.tile;
     if (lo >= end) t1 = t0;                                       // nothing but the prefix
-    int np = (s.pf + kAttnTile - 1) / kAttnTile;
+    int np = (s.pf + a.tile - 1) / a.tile;
     if (np >= t0) {                                               // the two ranges touch
         t1 = (t1 > t0) ? t1 : np;
         if (t1 < np) t1 = np;
@@ -94,15 +106,24 @@ __host__ __device__ __forceinline__ int worker_of(int x, int n_items, int worker
     return (int)(((int64_t)(x + 1) * workers - 1) / n_items);
 }
 
-// Channel slot 16 a + s sits at position 8 s + a of a partial row (the order the accumulators are in).
-__device__ __forceinline__ int part_pos(int slot) { return (slot & 15) * 8 + (slot >> 4); }
-
 // Cached values are carried times 2^-8 inside the kernels, so that no exponent byte leaves the bf16 range with the
 // conversion's offset; undone on scores and outputs.
 constexpr float kValueUp = 256.f;
 
-kvbfp_status launch_attn_rows4(const AttnArgs& a, cudaStream_t s);
-kvbfp_status launch_attn_rows6(const AttnArgs& a, cudaStream_t s);
-kvbfp_status launch_attn_rows8(const AttnArgs& a, cudaStream_t s);
+// How the kernel for `mant_bits` cuts and splits: tokens per tile; thread blocks per SM.
+struct AttnShape {
+    int tile, blocks_per_sm;
+};
+AttnShape attn_shape4(const AttnArgs& a);
+AttnShape attn_shape6(const AttnArgs& a);
+AttnShape attn_shape8(const AttnArgs& a);
+// attn_prep and attn_rows
+kvbfp_status launch_attn_rows4(const AttnArgs& a, int grid, cudaStream_t s);
+kvbfp_status launch_attn_rows6(const AttnArgs& a, int grid, cudaStream_t s);
+kvbfp_status launch_attn_rows8(const AttnArgs& a, int grid, cudaStream_t s);
+// umma_prep and attn_umma: bf16 queries, tiles of 128 tokens, one thread block per SM
+kvbfp_status launch_attn_umma4(const AttnArgs& a, int grid, cudaStream_t s);
+kvbfp_status launch_attn_umma6(const AttnArgs& a, int grid, cudaStream_t s);
+kvbfp_status launch_attn_umma8(const AttnArgs& a, int grid, cudaStream_t s);
 
 }  // namespace kvbfp

@@ -3,10 +3,11 @@
 //   S[rows x tokens] = pi(Q) . K^T ;  y = log2(e) * (cap * tanh(scale * S / cap) - slope * distance) ;  P = 2^(y - m)
 //   O[rows x slots] += P . V ;  l += rowsum(P)
 //
-// Work split.  Persistent thread blocks; all 128-token tiles of all (sequence, kv head, row tile) are cut into one
-// contiguous range per block, counted on the device from the real lengths and windows, so ragged batches and windows
-// stay balanced.  A block walks its range as runs (the tiles of one (sequence, head, row tile)); a run that covers all
-// tiles writes the result itself, others leave a partial for attn_merge.  The tiles come through a ring of
+// Work split.  attn_prep writes, per (sequence, kv head, row tile), pi(q) in fragment order, and the tiles each sequence
+// has to read (counted from the real lengths and windows, so ragged batches and windows stay balanced).  attn_rows is
+// persistent: all tiles are cut into one contiguous range per warp; a warp walks its range as runs (the tiles of one
+// (sequence, head, row tile)), shares nothing with other warps and meets no barrier.  A run that covers all tiles
+// writes the result itself, others leave a partial for attn_merge.  The tiles come through a per-warp ring of
 // shared-memory stages filled by asynchronous copies that run ahead across run boundaries.
 //
 // Fragments.  Query rows are the M rows of m16n8k16, so the scores' accumulators are the A fragment of P . V as they
@@ -20,50 +21,10 @@
 // rounded to bf16 too).  fp32 queries are three bf16 terms (24 bits) and P two (16 bits, 2^-17); their O is summed
 // outside the MMAs because the tensor cores cut, not round, the running sum.  m, l, O and scores are fp32.
 #pragma once
-#include <math.h>
-
-#include <atomic>
-
-#include "attn.cuh"
-#include "ptx.cuh"
+#include "attn_common.cuh"
 
 namespace kvbfp {
 namespace {
-
-constexpr int kAW = 4;      // warps per thread block
-
-template <int P> struct AFmt;
-template <> struct AFmt<4> { static constexpr uint32_t mask = 0x000F000Fu, magic = 0x43004300u, bias = 0xC308C308u; };  // -136
-template <> struct AFmt<6> { static constexpr uint32_t mask = 0x003F003Fu, magic = 0x43004300u, bias = 0xC320C320u; };  // -160
-template <> struct AFmt<8> { static constexpr uint32_t mask = 0x000F000Fu, magic = 0x43004300u, bias = 0xC510C510u; };  // -2304
-
-// bf16 bits of 2^(e8 - 127 - (P-2) - 8); 0 below the smallest subnormal.
-template <int P>
-__device__ __forceinline__ uint32_t attn_weight(int e8) {
-    const int f = e8 - (P - 2) - 8;
-    return f >= 1 ? ((uint32_t)f << 7) : (f > -7 ? (0x40u >> (-f)) : 0u);
-}
-
-struct AW {
-    uint32_t s, c, s16;      // weight pair, -offset * weight, 16 * weight (8-bit fields)
-};
-template <int P>
-__device__ __forceinline__ AW aw_make(uint32_t s, uint32_t c) {
-    AW w;
-    w.s = s;
-    w.c = c;
-    w.s16 = (P == 8) ? mul_bf16x2(s, 0x41804180u) : 0u;
-    return w;
-}
-template <int P>
-__device__ __forceinline__ uint32_t acvt(uint32_t x, const AW& w) {
-    if (P == 8) {
-        const uint32_t lo = lop3<0xEA>(x, 0x000F000Fu, 0x43004300u);
-        const uint32_t hi = lop3<0xEA>(x >> 4, 0x000F000Fu, 0x43004300u);
-        return fma_bf16x2(lo, w.s, fma_bf16x2(hi, w.s16, w.c));
-    }
-    return fma_bf16x2(lop3<0xEA>(x, AFmt<P>::mask, AFmt<P>::magic), w.s, w.c);
-}
 
 // Slot that k position kk (0..3 = k 2t, 2t+1, 2t+8, 2t+9) of k-step ks holds in lane column t.
 template <int P>
@@ -132,7 +93,7 @@ __device__ __forceinline__ int tok_of(int t, int e, int j) {
     if (P == 6) return ((t + 2 * e) & 3) + 4 * (e + 2 * j);
     return 2 * t + e + 8 * j;
 }
-// Byte offset of 16-byte-or-smaller piece at byte `x` of row `row` in a staged tile.
+// Byte offset of the piece at byte `x` of row `row` (0..15) of a 16-row group; groups follow each other 16 rows on.
 template <int P>
 __device__ __forceinline__ int tile_at(int row, int x) {
     if (P == 4) {
@@ -143,243 +104,205 @@ __device__ __forceinline__ int tile_at(int row, int x) {
     return row * 96 + x;
 }
 
-struct RowInfo {
-    int pos;           // position of the query row's token
-    float slope;
-    uint32_t m0, m1;   // drafted tokens it sees (all clear for rows that do not exist)
-};
+// Query fragments of one (sequence, kv head, row tile) per block.
+template <int P, int MT, bool F32>
+__global__ void __launch_bounds__(128) attn_prep(const AttnArgs a) {
+    constexpr int ROWS = 16 * MT, SPLIT = F32 ? 3 : 1;
+    __shared__ float sq[ROWS][kHeadDim + 4];
+    __shared__ int sp[kHeadDim];
+    prep_common<ROWS, F32>(a, sq, sp);
+    const int tid = threadIdx.x, x0 = blockIdx.x;
+    uint4* to = a.qfrag + (int64_t)x0 * (SPLIT * MT * 8 * 32);
+#pragma unroll 2
+    for (int x = tid; x < MT * 8 * 32; x += 128) {
+        const int ln = x & 31, ks = (x >> 5) & 7, mt = x >> 8, g = ln >> 2, t = ln & 3;
+        uint32_t reg[SPLIT][4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {       // row g | g + 8, k positions 0, 1 | 2, 3
+            const float* row = sq[mt * 16 + g + 8 * (k & 1)];
+            float v0 = row[sp[attn_k_slot<P>(ks, t, (k & 2))]], v1 = row[sp[attn_k_slot<P>(ks, t, (k & 2) + 1)]];
+#pragma unroll
+            for (int s = 0; s < SPLIT; ++s) {
+                reg[s][k] = pack_bf16x2_rn(v0, v1);
+                v0 -= __uint_as_float(reg[s][k] << 16);
+                v1 -= __uint_as_float(reg[s][k] & 0xffff0000u);
+            }
+        }
+#pragma unroll
+        for (int s = 0; s < SPLIT; ++s) to[s * MT * 256 + x] = make_uint4(reg[s][0], reg[s][1], reg[s][2], reg[s][3]);
+    }
+}
 
-template <int P, int MT, int RG, bool F32>
+template <int P>
 struct AGeo {
     static constexpr int ROW_M = kHeadDim * P / 8;
-    static constexpr int STAGES = (P == 8) ? 2 : 3;
-    static constexpr int VM_OFF = kAttnTile * ROW_M;
-    static constexpr int KE_OFF = 2 * kAttnTile * ROW_M;
-    static constexpr int VE_OFF = KE_OFF + kAttnTile * 8;
-    static constexpr int STAGE_BYTES = VE_OFF + kAttnTile * 8;       // a multiple of 1024
-    static constexpr int ROWS = 16 * MT * RG;
-    static constexpr int QSPLIT = F32 ? 3 : 1;
-    static constexpr int OSTRIDE = kHeadDim + 8;
-    static constexpr int QF_OFF = STAGES * STAGE_BYTES;
-    static constexpr int O_OFF = QF_OFF + QSPLIT * MT * RG * 8 * 512;
-    static constexpr int ML_OFF = O_OFF + ROWS * OSTRIDE * 4;        // per (token group, row): max, sum
-    static constexpr int RI_OFF = ML_OFF + (kAW / RG) * ROWS * 8;
-    static constexpr int DP_OFF = RI_OFF + ROWS * 16;                // positions of the drafted rows
-    static constexpr int LUT_OFF = DP_OFF + kAttnMaxDraft * 4;
-    static constexpr int BAR_OFF = LUT_OFF + 256 * 8;
-    static constexpr int SCAN_OFF = BAR_OFF + 2 * STAGES * 8;
-    static constexpr int CUM_OFF = SCAN_OFF + kAW * 32 * 4;
-    static int smem_bytes(int batch) { return CUM_OFF + (batch + 1) * 4 + 1024; }    // + alignment of the base
+    static constexpr int TILE = P == 8 ? 32 : 64;       // tokens per stage
+    static constexpr int STAGES = 2;
+    static constexpr int VM_OFF = TILE * ROW_M, KE_OFF = 2 * VM_OFF;
+    // exponent bytes of a stage: 2 * TILE * row_e, the stage rounded up to the swizzle's 1024 bytes for the tiled copies
+    __host__ __device__ static int exp_bytes(int row_e) { return 2 * TILE * row_e; }
+    static constexpr int LUT_BYTES = 256 * 8;
+    static constexpr int WARP_SMALL = STAGES * 8 + 32 * 16 + kAttnMaxDraft * 4;    // barriers, rows (one output row at the end of a run), positions
+    __host__ __device__ static int smem_bytes(int row_e) {
+        return kAttnWarps * STAGES * (KE_OFF + exp_bytes(row_e)) + LUT_BYTES + kAttnWarps * WARP_SMALL;
+    }
 };
 
-template <int P, int MT, int RG, bool F32>
-__global__ void __launch_bounds__(kAW * 32, 2) attn_rows(const AttnArgs a, const __grid_constant__ CUtensorMap k_map,
-                                                         const __grid_constant__ CUtensorMap v_map) {
-    using G_ = AGeo<P, MT, RG, F32>;
-    constexpr int D = kHeadDim, ROW_M = G_::ROW_M, STAGES = G_::STAGES, TG = kAW / RG, ROWS = G_::ROWS;
-    constexpr bool Q_REGS = MT == 1 && !F32;
-    extern __shared__ uint8_t smem_raw[];
-    uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+template <int P, bool N16, int MT, bool F32, int MINB>
+__global__ void __launch_bounds__(kAttnWarps * 32, MINB) attn_rows(const AttnArgs a, const __grid_constant__ CUtensorMap k_map,
+                                                                   const __grid_constant__ CUtensorMap v_map) {
+    using G_ = AGeo<P>;
+    constexpr int D = kHeadDim, ROW_M = G_::ROW_M, STAGES = G_::STAGES, TILE = G_::TILE, ROWS = 16 * MT;
+    constexpr int SPLIT = F32 ? 3 : 1, GROUP = 16 * ROW_M;
+    extern __shared__ __align__(1024) uint8_t smem[];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
-    const int rg = warp % RG, tg = warp / RG;
+    const int row_e = D / a.fmt.block, exp_half = TILE * row_e;
+    // mantissa tiles of all warps and stages first (whole swizzle periods), then the exponent bytes, then the rest
+    uint8_t* my_m = smem + warp * STAGES * G_::KE_OFF;
+    uint8_t* my_e = smem + kAttnWarps * STAGES * G_::KE_OFF + warp * STAGES * 2 * exp_half;
+    uint8_t* rest = smem + kAttnWarps * STAGES * (G_::KE_OFF + 2 * exp_half);
+    uint2* lut = reinterpret_cast<uint2*>(rest);
+    uint8_t* small = rest + G_::LUT_BYTES + warp * G_::WARP_SMALL;
+    RowInfo* ri = reinterpret_cast<RowInfo*>(small);
+    float* orow = reinterpret_cast<float*>(small);
+    int* dpos = reinterpret_cast<int*>(small + 32 * 16);
+    const uint32_t bar = smem_u32(small + 32 * 16 + kAttnMaxDraft * 4);
 
-    uint4* qf = reinterpret_cast<uint4*>(smem + G_::QF_OFF);
-    float* ob = reinterpret_cast<float*>(smem + G_::O_OFF);
-    float2* ml = reinterpret_cast<float2*>(smem + G_::ML_OFF);
-    RowInfo* ri = reinterpret_cast<RowInfo*>(smem + G_::RI_OFF);
-    int* dpos = reinterpret_cast<int*>(smem + G_::DP_OFF);
-    uint2* lut = reinterpret_cast<uint2*>(smem + G_::LUT_OFF);
-    int* scan = reinterpret_cast<int*>(smem + G_::SCAN_OFF);
-    int* cum = reinterpret_cast<int*>(smem + G_::CUM_OFF);
-    const uint32_t bar_full = smem_u32(smem + G_::BAR_OFF), bar_empty = bar_full + 8 * STAGES;
-
-    for (int e = tid; e < 256; e += kAW * 32) {
+    for (int e = tid; e < 256; e += kAttnWarps * 32) {
         const uint32_t s2 = attn_weight<P>(e) * 0x00010001u;
         lut[e] = make_uint2(s2, mul_bf16x2(s2, AFmt<P>::bias));
     }
-    if (tid == 0) {
-        for (int s = 0; s < STAGES; ++s) {
-            mbar_init(bar_full + 8 * s, 1);
-            mbar_init(bar_empty + 8 * s, kAW);
-        }
+    if (lane == 0) {
+        for (int s = 0; s < STAGES; ++s) mbar_init(bar + 8 * s, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
-    pdl_wait();
+    __syncthreads();
+    pdl_wait();       // what attn_prep wrote is read by plain loads below: read-only ones could be moved above this line
 
-    // ---- tiles per sequence, summed over the batch
     const int B = a.fmt.batch, Hkv = a.fmt.n_kv_heads, HR = Hkv * a.n_row_tiles, max_seq = a.fmt.max_seq;
-    {
-        const int per = (B + kAW * 32 - 1) / (kAW * 32);
-        int mine = 0;
-        for (int i = 0; i < per; ++i) {
-            const int b = tid * per + i;
-            if (b < B) mine += seq_view(a, b).n;
-        }
-        int x = mine;
-#pragma unroll
-        for (int off = 1; off < 32; off <<= 1) {
-            const int y = __shfl_up_sync(0xffffffffu, x, off);
-            if (lane >= off) x += y;
-        }
-        if (lane == 31) scan[warp] = x;
-        __syncthreads();
-        int before = x - mine;
-        for (int w = 0; w < warp; ++w) before += scan[w];
-        for (int i = 0; i < per; ++i) {
-            const int b = tid * per + i;
-            if (b < B) {
-                cum[b] = before;
-                const SeqView sv = seq_view(a, b);
-                before += sv.n;
-                if (b == B - 1) cum[B] = before;
-                if (sv.clamped && blockIdx.x == 0) raise_flag(a.status, KVBFP_FLAG_POSITION);
-            }
-        }
-        __syncthreads();
-        if (blockIdx.x == 0)
-            for (int b = tid; b <= B; b += kAW * 32) a.plan[b] = cum[b];
-    }
-    const int n_items = cum[B] * HR;
-    const int workers = min(a.workers, n_items);
-    const int i0 = (int)blockIdx.x < workers ? worker_start(blockIdx.x, n_items, workers) : 0;
-    const int i1 = (int)blockIdx.x < workers ? worker_start(blockIdx.x + 1, n_items, workers) : 0;
+    const int n_items = a.plan[B] * HR;
+    const int workers = min(a.workers, n_items), me = blockIdx.x + gridDim.x * warp;      // neighbouring ranges on different SMs
+    const int i0 = me < workers ? worker_start(me, n_items, workers) : 0;
+    const int i1 = me < workers ? worker_start(me + 1, n_items, workers) : 0;
     const int n_mine = i1 - i0;
     if (n_mine <= 0) {
         pdl_trigger();
         return;
     }
-    struct Cursor {      // an item: sequence, kv head and row tile (hr), tile of n
+    struct Cursor {      // an item: sequence, kv head and row tile (hr), tile k of n
         int b, hr, k, n;
     };
-    auto seek = [&](int item) {
-        int lo = 0, hi = B - 1;                 // last sequence whose first item is not behind `item` and that has tiles
-        while (lo < hi) {
-            const int mid = (lo + hi + 1) >> 1;
-            if (cum[mid] * HR <= item) lo = mid; else hi = mid - 1;
+    Cursor cc;
+    {
+        // last sequence that begins at or before the item and has tiles: 32 looked at per step
+        int last = 0;
+        for (int b0 = 0; b0 < B; b0 += 32) {
+            const bool in = b0 + lane < B && a.plan[b0 + lane] * HR <= i0;
+            const uint32_t v = __ballot_sync(0xffffffffu, in);
+            if (v) last = b0 + 31 - __clz(v);
+            if (v != 0xffffffffu) break;
         }
-        Cursor c;
-        c.b = lo;
-        c.n = cum[lo + 1] - cum[lo];
-        const int in = item - cum[lo] * HR;
-        c.hr = in / c.n;
-        c.k = in - c.hr * c.n;
-        return c;
-    };
+        const int c0 = a.plan[last];
+        cc.b = last;
+        cc.n = a.plan[last + 1] - c0;
+        const int in = i0 - c0 * HR;
+        cc.hr = in / cc.n;
+        cc.k = in - cc.hr * cc.n;
+    }
     auto next_pair = [&](Cursor& c) {           // to the first tile of the next (sequence, head, row tile)
         c.k = 0;
         if (++c.hr == HR) {
             c.hr = 0;
-            do { ++c.b; } while (c.b < B && cum[c.b + 1] == cum[c.b]);
-            c.n = c.b < B ? cum[c.b + 1] - cum[c.b] : 0;
+            c.n = 0;
+            while (c.n == 0 && ++c.b < B) c.n = a.plan[c.b + 1] - a.plan[c.b];
         }
     };
+    auto view = [&](int b) {
+        const int4 x = reinterpret_cast<const int4*>(a.views + b)[0], y = reinterpret_cast<const int4*>(a.views + b)[1];
+        SeqView s;
+        s.ctx = x.x; s.nd = x.y; s.first = x.z; s.pf = x.w; s.lo = y.x; s.np = y.y; s.n = y.z; s.clamped = y.w;
+        return s;
+    };
 
-    // ---- copies: warp 0, lane 0 walks the same items STAGES ahead
-    const int row_e = D / a.fmt.block;
-    Cursor pc = seek(i0);
-    SeqView psv = seq_view(a, pc.b);
+    // ---- copies: the same items, STAGES ahead (every lane keeps the cursor, lane 0 issues)
+    Cursor pc = cc;
+    SeqView psv = view(pc.b);
     int issued = 0;
     auto issue = [&]() {
         const int s = issued % STAGES;
-        const int tt = psv.tile_token(pc.k);
-        const int64_t row0 = ((int64_t)pc.b * Hkv + pc.hr / a.n_row_tiles) * max_seq + tt;
-        const int rows = min(kAttnTile, max_seq - tt);           // a multiple of 16
-        const uint32_t dst = smem_u32(smem) + s * G_::STAGE_BYTES, bar = bar_full + 8 * s;
-        const uint32_t mant = (P == 6 ? rows : kAttnTile) * ROW_M;       // a tiled copy always brings its whole box
-        mbar_expect_tx(bar, 2 * mant + 2 * rows * row_e);
-        if (P == 6) {
-            bulk_g2s(dst, a.k_mant + row0 * ROW_M, mant, bar);
-            bulk_g2s(dst + G_::VM_OFF, a.v_mant + row0 * ROW_M, mant, bar);
-        } else {
-            const int y = (int)(P == 4 ? row0 >> 1 : row0);
-            tensor_g2s_2d(dst, &k_map, 0, y, bar);
-            tensor_g2s_2d(dst + G_::VM_OFF, &v_map, 0, y, bar);
+        if (lane == 0) {
+            const int tt = tile_token(psv, pc.k, TILE);
+            const int64_t row0 = ((int64_t)pc.b * Hkv + pc.hr / a.n_row_tiles) * max_seq + tt;
+            const int rows = min(TILE, max_seq - tt);           // a multiple of 16
+            const uint32_t dst = smem_u32(my_m) + s * G_::KE_OFF, de = smem_u32(my_e) + s * 2 * exp_half, br = bar + 8 * s;
+            const uint32_t mant = (P == 6 ? rows : TILE) * ROW_M;       // a tiled copy always brings its whole box
+            mbar_expect_tx(br, 2 * mant + 2 * rows * row_e);
+            if (P == 6) {
+                bulk_g2s(dst, a.k_mant + row0 * ROW_M, mant, br);
+                bulk_g2s(dst + G_::VM_OFF, a.v_mant + row0 * ROW_M, mant, br);
+            } else {
+                const int y = (int)(P == 4 ? row0 >> 1 : row0);
+                tensor_g2s_2d(dst, &k_map, 0, y, br);
+                tensor_g2s_2d(dst + G_::VM_OFF, &v_map, 0, y, br);
+            }
+            bulk_g2s(de, a.k_exp + row0 * row_e, rows * row_e, br);
+            bulk_g2s(de + exp_half, a.v_exp + row0 * row_e, rows * row_e, br);
         }
-        bulk_g2s(dst + G_::KE_OFF, a.k_exp + row0 * row_e, rows * row_e, bar);
-        bulk_g2s(dst + G_::VE_OFF, a.v_exp + row0 * row_e, rows * row_e, bar);
         ++issued;
         if (++pc.k == pc.n) {
             const int b = pc.b;
             next_pair(pc);
-            if (pc.b != b && pc.b < B) psv = seq_view(a, pc.b);
+            if (pc.b != b && pc.b < B) psv = view(pc.b);
         }
     };
-    if (tid == 0)
-        for (int s = 0; s < STAGES && issued < n_mine; ++s) issue();
+    for (int s = 0; s < STAGES && issued < n_mine; ++s) issue();
 
-    Cursor cc = seek(i0);
     const int R = a.n_draft * a.group;
-    const float up = a.scale * kValueUp;
-    const float to_log2 = 1.4426950408889634f;
+    const float up = a.scale * kValueUp, to_log2 = 1.4426950408889634f, plain = up * to_log2;
     const float cap_in = a.softcap > 0.f ? up / a.softcap : 0.f;
-    const int ke_lane = (a.fmt.block == 16) ? 2 * t : (32 * t) / a.fmt.block;
-    const int ve_lane = (16 * g) / a.fmt.block;
-    const bool n16 = a.fmt.block == 16;
+    const bool reshape = a.softcap > 0.f || a.slopes != nullptr;
+    // lane offsets inside a 16-token group: K rows of column g in both score tiles, V rows of the lane's four k positions
+    int ko[2], ke[2], vo[4], ve[4];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        const int row = tok_of<P>(g >> 1, g & 1, j);
+        ko[j] = P == 4 ? tile_at<P>(row, 16 * t) : (P == 8 ? row * 128 : tile_at<P>(row, 24 * t));
+        ke[j] = row * row_e + (N16 ? 2 * t : (32 * t) / a.fmt.block);
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const int row = tok_of<P>(t, e & 1, e >> 1);
+        vo[e] = G_::VM_OFF + tile_at<P>(row, 2 * P * g);
+        ve[e] = exp_half + row * row_e + (16 * g) / a.fmt.block;
+    }
+    const int kx = (tok_of<P>(g >> 1, g & 1, 0) & 7) << 4;       // 8-bit rows: swizzle of the lane's K rows (both tiles alike)
+
     bool dead = false;            // a copy did not arrive: no more waits, no more work, the flag is up
     int it = 0;
     while (it < n_mine) {
         // ================================================================ a run: tiles [k0, k1) of one (b, head, row tile)
         const int b = cc.b, hk = cc.hr / a.n_row_tiles, rt = cc.hr - hk * a.n_row_tiles;
         const int k0 = cc.k, k1 = min(cc.n, k0 + n_mine - it);
-        const SeqView sv = seq_view(a, b);
-        __syncthreads();
-        for (int r = tid; r < ROWS; r += kAW * 32) {
-            const int row = rt * ROWS + r, i = row / a.group;
-            RowInfo x;
-            x.pos = sv.ctx - 1;
-            x.slope = 0.f;
-            x.m0 = x.m1 = 0u;
-            if (row < R) {
-                if (a.slopes) x.slope = a.slopes[hk * a.group + row - i * a.group];
-                if (a.tree) {
-                    const int64_t at = (int64_t)b * a.n_draft + i;
-                    const int dep = a.depth ? min(max(a.depth[at], 0), a.n_draft - 1) : i;
-                    const uint64_t m = a.tree_mask ? a.tree_mask[at] : (i == 63 ? ~0ull : (2ull << i) - 1ull);
-                    x.pos = sv.ctx + dep;
-                    x.m0 = (uint32_t)m;
-                    x.m1 = (uint32_t)(m >> 32);
-                }
-            }
-            ri[r] = x;
-        }
-        if (a.tree)
-            for (int j = tid; j < a.n_draft; j += kAW * 32)
-                dpos[j] = sv.ctx + (a.depth ? min(max(a.depth[(int64_t)b * a.n_draft + j], 0), a.n_draft - 1) : j);
-        // pi(q) as A fragments: [split][m tile][k step][lane] of four registers
-#pragma unroll 4
-        for (int x = tid; x < MT * RG * 8 * 32 * 4; x += kAW * 32) {
-            const int reg = x & 3, ln = (x >> 2) & 31, ks = (x >> 7) & 7, mt = x >> 10;
-            const int r = mt * 16 + (ln >> 2) + 8 * (reg & 1), row = rt * ROWS + r;
-            const int i = row / a.group, hq = hk * a.group + row - i * a.group;
-            float v[2] = {0.f, 0.f};
-            if (row < R) {
-                const int64_t base = (((int64_t)b * a.n_draft + i) * a.n_q_heads + hq) * D;
+        const SeqView sv = view(b);
+        const int64_t item = (int64_t)b * HR + cc.hr;
+        uint4 qr[SPLIT][MT][8];
+        {
+            const uint4* src = a.qfrag + item * (SPLIT * MT * 256) + lane;
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const int slot = attn_k_slot<P>(ks, ln & 3, (reg & 2) + e);
-                    const int ch = a.perm_k ? (a.perm_k[hk * D + slot] & (D - 1)) : slot;
-                    v[e] = F32 ? static_cast<const float*>(a.q)[base + ch]
-                               : __bfloat162float(static_cast<const __nv_bfloat16*>(a.q)[base + ch]);
-                }
-            }
-            uint32_t* to = reinterpret_cast<uint32_t*>(qf) + x;
+            for (int s = 0; s < SPLIT; ++s)
 #pragma unroll
-            for (int sp = 0; sp < G_::QSPLIT; ++sp) {
-                const uint32_t p = pack_bf16x2_rn(v[0], v[1]);
-                to[sp * MT * RG * 8 * 32 * 4] = p;
-                if (F32) {
-                    v[0] -= __uint_as_float(p << 16);
-                    v[1] -= __uint_as_float(p & 0xffff0000u);
-                }
-            }
-        }
-        __syncthreads();
-        uint4 qr[Q_REGS ? 8 : 1];
-        if (Q_REGS) {
+                for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-            for (int ks = 0; ks < 8; ++ks) qr[Q_REGS ? ks : 0] = qf[(rg * 8 + ks) * 32 + lane];
+                    for (int ks = 0; ks < 8; ++ks) qr[s][mt][ks] = src[((s * MT + mt) * 8 + ks) * 32];
         }
+        __syncwarp();
+        if (lane < ROWS) reinterpret_cast<uint4*>(ri)[lane] = reinterpret_cast<const uint4*>(a.rows)[item * ROWS + lane];
+        if (a.tree) {
+            dpos[lane] = a.dpos[b * kAttnMaxDraft + lane];
+            dpos[lane + 32] = a.dpos[b * kAttnMaxDraft + lane + 32];
+        }
+        __syncwarp();
 
         float o[MT][16][4];
         float m_run[MT][2], l_run[MT][2];
@@ -395,265 +318,225 @@ __global__ void __launch_bounds__(kAW * 32, 2) attn_rows(const AttnArgs a, const
         // tokens [clear_lo, ctx) and [0, pf) are visible to every row
         int clear_lo = sv.first;
         if (a.window > 0) clear_lo = max(clear_lo, sv.ctx + (a.tree ? a.n_draft - 1 : -1) - a.window + 1);
+        const int end = sv.ctx + sv.nd;
 
         for (int k = k0; k < k1; ++k, ++it) {
             const int stage = it % STAGES;
-            const uint32_t phase = (uint32_t)(it / STAGES) & 1u;
-            if (warp == 0 && it > 0 && issued < n_mine) {      // refill the stage used one tile ago (lane 0 counts `issued`)
-                if (lane == 0 && !dead) {
-                    const int pi = it - 1;
-                    if (mbar_wait_bounded(bar_empty + 8 * (pi % STAGES), (uint32_t)(pi / STAGES) & 1u)) issue();
-                    else dead = true;
-                }
-            }
-            __syncwarp();
+            if (!dead && !mbar_wait_bounded(bar + 8 * stage, (uint32_t)(it / STAGES) & 1u)) dead = true;
             dead = __any_sync(0xffffffffu, dead);
-            if (!dead && !mbar_wait_bounded(bar_full + 8 * stage, phase)) dead = true;
-            dead = __any_sync(0xffffffffu, dead);
-            if (!dead) {
-                const uint8_t* st = smem + stage * G_::STAGE_BYTES;
-                const int tt = sv.tile_token(k);
-                const int end = sv.ctx + sv.nd;
+            if (dead) continue;
+            const int tt = tile_token(sv, k, TILE);
+            const uint8_t* stm = my_m + stage * G_::KE_OFF;
+            const uint8_t* ste = my_e + stage * 2 * exp_half;
 #pragma unroll 1
-                for (int u = tg; u < kAttnTile / 32; u += TG) {          // 32 tokens at a time
-                    const int u0 = u * 32, tok0 = tt + u0;
-                    if (tok0 >= end) break;
-                    // ---- scores: sc[m tile][16-token group * 2 + column tile][...]
-                    float sc[MT][4][4];
-                    {
-                        uint32_t kw[4][P];
-                        AW kg[4][2];
+            for (int u = 0; u < TILE / 16; ++u, stm += GROUP, ste += 16 * row_e) {
+                const int tok0 = tt + 16 * u;
+                if (tok0 >= end) break;
+                // ---- scores of 16 tokens: sc[m tile][column tile][...]
+                float sc[MT][2][4];
+                {
+                    float s2[MT][2][4];        // odd k steps: two chains of MMAs per column tile
+                    uint32_t kw[2][P];
+                    AW kg[2][N16 ? 2 : 1];
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            const int row = u0 + 16 * (j >> 1) + tok_of<P>(g >> 1, g & 1, j & 1);
-                            if (P == 6) {
+                    for (int j = 0; j < 2; ++j) {
+                        if (P == 6) {
 #pragma unroll
-                                for (int i = 0; i < 3; ++i) {
-                                    const uint2 x = *reinterpret_cast<const uint2*>(st + tile_at<P>(row, 24 * t + 8 * i));
-                                    kw[j][2 * i] = x.x; kw[j][2 * i + 1] = x.y;
-                                }
-                            } else {
-#pragma unroll
-                                for (int i = 0; i < P / 4; ++i) {
-                                    const uint4 x = *reinterpret_cast<const uint4*>(st + tile_at<P>(row, 4 * P * t + 16 * i));
-                                    kw[j][4 * i] = x.x; kw[j][4 * i + 1] = x.y; kw[j][4 * i + 2] = x.z; kw[j][4 * i + 3] = x.w;
-                                }
+                            for (int i = 0; i < 3; ++i) {
+                                const uint2 x = *reinterpret_cast<const uint2*>(stm + ko[j] + 8 * i);
+                                kw[j][2 * i] = x.x; kw[j][2 * i + 1] = x.y;
                             }
-                            const uint8_t* pe = st + G_::KE_OFF + row * row_e + ke_lane;
-                            const uint2 l0 = lut[pe[0]];
-                            kg[j][0] = aw_make<P>(l0.x, l0.y);
-                            kg[j][1] = kg[j][0];
-                            if (n16) {
-                                const uint2 l1 = lut[pe[1]];
-                                kg[j][1] = aw_make<P>(l1.x, l1.y);
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < P / 4; ++i) {
+                                const uint4 x = *reinterpret_cast<const uint4*>(stm + ko[j] + (P == 8 ? ((32 * t + 16 * i) ^ kx) : 0));
+                                kw[j][4 * i] = x.x; kw[j][4 * i + 1] = x.y; kw[j][4 * i + 2] = x.z; kw[j][4 * i + 3] = x.w;
                             }
                         }
 #pragma unroll
-                        for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-                            for (int j = 0; j < 4; ++j) sc[mt][j][0] = sc[mt][j][1] = sc[mt][j][2] = sc[mt][j][3] = 0.f;
-#pragma unroll
-                        for (int ks = 0; ks < 8; ks += 2) {
-                            uint32_t r[4][4];
-#pragma unroll
-                            for (int j = 0; j < 4; ++j) attn_k<P>(kw[j], ks, kg[j][ks >> 2], r[j]);
-#pragma unroll
-                            for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-                                for (int sp = 0; sp < G_::QSPLIT; ++sp) {
-                                    const uint4* qp = qf + ((sp * MT * RG + rg * MT + mt) * 8 + ks) * 32 + lane;
-                                    const uint4 q0 = Q_REGS ? qr[Q_REGS ? ks : 0] : qp[0];
-                                    const uint4 q1 = Q_REGS ? qr[Q_REGS ? ks + 1 : 0] : qp[32];
-#pragma unroll
-                                    for (int j = 0; j < 4; ++j) {
-                                        mma_bf16(sc[mt][j], q0.x, q0.y, q0.z, q0.w, r[j][0], r[j][1]);
-                                        mma_bf16(sc[mt][j], q1.x, q1.y, q1.z, q1.w, r[j][2], r[j][3]);
-                                    }
-                                }
+                        for (int i = 0; i < (N16 ? 2 : 1); ++i) {
+                            const uint2 l = lut[ste[ke[j] + i]];
+                            kg[j][i] = aw_make<P>(l.x, l.y);
                         }
                     }
-                    // ---- cap, bias, masks; log2 units
-                    const bool clear = tok0 + 32 <= sv.ctx && (tok0 >= clear_lo || tok0 + 32 <= sv.pf);
-                    const bool bias = a.slopes != nullptr;
-                    if (a.softcap > 0.f) {
 #pragma unroll
-                        for (int mt = 0; mt < MT; ++mt)
+                    for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-                            for (int j = 0; j < 4; ++j)
+                        for (int j = 0; j < 2; ++j)
 #pragma unroll
-                                for (int e = 0; e < 4; ++e) {
-                                    const float x = sc[mt][j][e] * cap_in;
-                                    float th;
-                                    if (F32) {
-                                        th = tanhf(x);
-                                    } else {                       // 1 - 2 / (1 + e^2x): about 2e-7 absolute
-                                        th = 1.f - __fdividef(2.f, 1.f + ex2_approx(x * 2.8853900817779268f));
-                                    }
-                                    sc[mt][j][e] = th * a.softcap;
-                                }
-                    } else {
+                            for (int e = 0; e < 4; ++e) sc[mt][j][e] = s2[mt][j][e] = 0.f;
 #pragma unroll
-                        for (int mt = 0; mt < MT; ++mt)
+                    for (int ks = 0; ks < 8; ks += 2) {
+                        uint32_t r[2][4];
 #pragma unroll
-                            for (int j = 0; j < 4; ++j)
+                        for (int j = 0; j < 2; ++j) attn_k<P>(kw[j], ks, kg[j][N16 ? ks >> 2 : 0], r[j]);
 #pragma unroll
-                                for (int e = 0; e < 4; ++e) sc[mt][j][e] *= up;
-                    }
-                    if (bias || !clear) {
+                        for (int s = 0; s < SPLIT; ++s)
 #pragma unroll
-                        for (int mt = 0; mt < MT; ++mt)
+                            for (int mt = 0; mt < MT; ++mt) {
+                                const uint4 q0 = qr[s][mt][ks], q1 = qr[s][mt][ks + 1];
 #pragma unroll
-                            for (int hh = 0; hh < 2; ++hh) {
-                                const RowInfo x = ri[(rg * MT + mt) * 16 + g + 8 * hh];
+                                for (int j = 0; j < 2; ++j) mma_bf16(sc[mt][j], q0.x, q0.y, q0.z, q0.w, r[j][0], r[j][1]);
 #pragma unroll
-                                for (int j = 0; j < 4; ++j)
-#pragma unroll
-                                    for (int e = 0; e < 2; ++e) {
-                                        const int tok = tok0 + 16 * (j >> 1) + tok_of<P>(t, e, j & 1);
-                                        float& y = sc[mt][j][2 * hh + e];
-                                        bool see;
-                                        int dist;
-                                        if (tok < sv.ctx) {
-                                            dist = x.pos - tok;
-                                            see = (tok >= sv.first && (a.window == 0 || dist < a.window)) || tok < sv.pf;
-                                        } else {
-                                            const int jd = tok - sv.ctx;
-                                            const bool in = jd < sv.nd;
-                                            dist = x.pos - dpos[in ? jd : 0];
-                                            see = in && (((jd < 32 ? x.m0 >> (jd & 31) : x.m1 >> (jd & 31)) & 1u) != 0u) &&
-                                                  (a.window == 0 || dist < a.window);
-                                        }
-                                        y -= x.slope * (float)dist;
-                                        if (!see) y = -INFINITY;
-                                    }
+                                for (int j = 0; j < 2; ++j) mma_bf16(s2[mt][j], q1.x, q1.y, q1.z, q1.w, r[j][2], r[j][3]);
                             }
                     }
 #pragma unroll
                     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-                        for (int j = 0; j < 4; ++j)
+                        for (int j = 0; j < 2; ++j)
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) sc[mt][j][e] *= to_log2;
-                    if (a.scores) {
-#pragma unroll
-                        for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-                            for (int hh = 0; hh < 2; ++hh) {
-                                const int row = rt * ROWS + (rg * MT + mt) * 16 + g + 8 * hh;
-                                if (row < R) {
-                                    float* to = a.scores + ((int64_t)b * a.n_q_heads + hk * a.group + row) * max_seq;
-#pragma unroll
-                                    for (int j = 0; j < 4; ++j)
-#pragma unroll
-                                        for (int e = 0; e < 2; ++e) {
-                                            const int tok = tok0 + 16 * (j >> 1) + tok_of<P>(t, e, j & 1);
-                                            if (tok < max_seq) to[tok] = sc[mt][j][2 * hh + e];
-                                        }
-                                }
-                            }
-                    }
-                    // ---- running softmax: the reference moves only when a score passes it by 8 (2^8 keeps P in range)
-                    float top[MT][2];
-                    bool grow = false;
+                            for (int e = 0; e < 4; ++e) sc[mt][j][e] += s2[mt][j][e];
+                }
+                // ---- cap, bias, masks: y = mul * sc in log2 units; tiles that every row sees whole need only the factor
+                float mul = plain;
+                if (reshape || !(tok0 + 16 <= sv.ctx && (tok0 >= clear_lo || tok0 + 16 <= sv.pf))) {
+                    mul = 1.f;
 #pragma unroll
                     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
                         for (int hh = 0; hh < 2; ++hh) {
-                            float x = -INFINITY;
+                            const RowInfo x = ri[mt * 16 + g + 8 * hh];
 #pragma unroll
-                            for (int j = 0; j < 4; ++j) x = fmaxf(x, fmaxf(sc[mt][j][2 * hh], sc[mt][j][2 * hh + 1]));
-                            top[mt][hh] = x;
-                            grow |= x > m_run[mt][hh] + 8.f;
+                            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                                for (int e = 0; e < 2; ++e) {
+                                    float y = sc[mt][j][2 * hh + e];
+                                    if (a.softcap > 0.f) {
+                                        y *= cap_in;
+                                        if (F32) y = tanhf(y);
+                                        else y = 1.f - __fdividef(2.f, 1.f + ex2_approx(y * 2.8853900817779268f));    // 1 - 2 / (1 + e^2y): about 2e-7 absolute
+                                        y *= a.softcap;
+                                    } else {
+                                        y *= up;
+                                    }
+                                    const int tok = tok0 + tok_of<P>(t, e, j);
+                                    bool see;
+                                    int dist;
+                                    if (tok < sv.ctx) {
+                                        dist = x.pos - tok;
+                                        see = (tok >= sv.first && (a.window == 0 || dist < a.window)) || tok < sv.pf;
+                                    } else {
+                                        const int jd = tok - sv.ctx;
+                                        const bool in = jd < sv.nd;
+                                        dist = x.pos - dpos[in ? jd : 0];
+                                        see = in && (((jd < 32 ? x.m0 >> (jd & 31) : x.m1 >> (jd & 31)) & 1u) != 0u) &&
+                                              (a.window == 0 || dist < a.window);
+                                    }
+                                    y = (y - x.slope * (float)dist) * to_log2;
+                                    sc[mt][j][2 * hh + e] = see ? y : -INFINITY;
+                                }
                         }
-                    if (__any_sync(0xffffffffu, grow)) {
-#pragma unroll
-                        for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-                            for (int hh = 0; hh < 2; ++hh) {
-                                float x = top[mt][hh];
-                                x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 1));
-                                x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 2));
-                                x = fmaxf(x, m_run[mt][hh]);
-                                const float al = ex2_approx(m_run[mt][hh] - x);
-                                m_run[mt][hh] = x;
-                                l_run[mt][hh] *= al;
-#pragma unroll
-                                for (int s = 0; s < 16; ++s) { o[mt][s][2 * hh] *= al; o[mt][s][2 * hh + 1] *= al; }
-                            }
-                    }
+                }
+                if (a.scores) {
 #pragma unroll
                     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-                        for (int j = 0; j < 4; ++j)
+                        for (int hh = 0; hh < 2; ++hh) {
+                            const int row = rt * ROWS + mt * 16 + g + 8 * hh;
+                            if (row < R) {
+                                float* to = a.scores + ((int64_t)b * a.n_q_heads + hk * a.group + row) * max_seq + tok0;
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) {
-                                const float p = ex2_approx(sc[mt][j][e] - m_run[mt][e >> 1]);
-                                sc[mt][j][e] = p;
-                                l_run[mt][e >> 1] += p;
+                                for (int j = 0; j < 2; ++j)
+#pragma unroll
+                                    for (int e = 0; e < 2; ++e) to[tok_of<P>(t, e, j)] = sc[mt][j][2 * hh + e] * mul;
                             }
-                    // ---- P . V, 16 tokens at a time
-#pragma unroll
-                    for (int h16 = 0; h16 < 2; ++h16) {
-                        if (tok0 + 16 * h16 >= end) break;
-                        uint32_t vw[4][P / 2];
-                        uint2 lv[4];
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {       // k = 2t, 2t+1, 2t+8, 2t+9
-                            const int row = u0 + 16 * h16 + tok_of<P>(t, e & 1, e >> 1);
-                            if (P == 4) {
-                                const uint2 x = *reinterpret_cast<const uint2*>(st + G_::VM_OFF + tile_at<P>(row, 8 * g));
-                                vw[e][0] = x.x; vw[e][1] = x.y;
-                            } else if (P == 6) {
-#pragma unroll
-                                for (int i = 0; i < 3; ++i)
-                                    vw[e][i] = *reinterpret_cast<const uint32_t*>(st + G_::VM_OFF + tile_at<P>(row, 12 * g + 4 * i));
-                            } else {
-                                const uint4 x = *reinterpret_cast<const uint4*>(st + G_::VM_OFF + tile_at<P>(row, 16 * g));
-                                vw[e][0] = x.x; vw[e][1] = x.y; vw[e][P / 2 - 2] = x.z; vw[e][P / 2 - 1] = x.w;
-                            }
-                            lv[e] = lut[st[G_::VE_OFF + row * row_e + ve_lane]];
                         }
-                        const AW ga = aw_make<P>(prmt(lv[0].x, lv[1].x, 0x7610u), prmt(lv[0].y, lv[1].y, 0x7610u));
-                        const AW gb = aw_make<P>(prmt(lv[2].x, lv[3].x, 0x7610u), prmt(lv[2].y, lv[3].y, 0x7610u));
-                        uint32_t pa[MT][4], pl[F32 ? MT : 1][4];
+                }
+                // ---- running softmax: the reference moves only when a score passes it by 8 (2^8 keeps P in range)
+                float top[MT][2];
+                bool grow = false;
 #pragma unroll
-                        for (int mt = 0; mt < MT; ++mt)
+                for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-                            for (int x = 0; x < 4; ++x) {      // (row g, tile 0), (row g+8, tile 0), (row g, tile 1), (row g+8, tile 1)
-                                const float p0 = sc[mt][2 * h16 + (x >> 1)][2 * (x & 1)], p1 = sc[mt][2 * h16 + (x >> 1)][2 * (x & 1) + 1];
-                                pa[mt][x] = pack_bf16x2_rn(p0, p1);
-                                if (F32)
-                                    pl[F32 ? mt : 0][x] = pack_bf16x2_rn(p0 - __uint_as_float(pa[mt][x] << 16),
-                                                                         p1 - __uint_as_float(pa[mt][x] & 0xffff0000u));
-                            }
+                    for (int hh = 0; hh < 2; ++hh) {
+                        const float x = mul * fmaxf(fmaxf(sc[mt][0][2 * hh], sc[mt][0][2 * hh + 1]),
+                                                    fmaxf(sc[mt][1][2 * hh], sc[mt][1][2 * hh + 1]));
+                        top[mt][hh] = x;
+                        grow |= x > m_run[mt][hh] + 8.f;
+                    }
+                if (__any_sync(0xffffffffu, grow)) {
 #pragma unroll
-                        for (int r = 0; r < 8; r += 2) {
-                            uint32_t xa[4], xb[4];
-                            attn_v<P>(vw[0], vw[1], r, ga, xa);
-                            attn_v<P>(vw[2], vw[3], r, gb, xb);
+                    for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-                            for (int mt = 0; mt < MT; ++mt)
+                        for (int hh = 0; hh < 2; ++hh) {
+                            float x = top[mt][hh];
+                            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 1));
+                            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 2));
+                            x = fmaxf(x, m_run[mt][hh]);
+                            const float al = ex2_approx(m_run[mt][hh] - x);
+                            m_run[mt][hh] = x;
+                            l_run[mt][hh] *= al;
 #pragma unroll
-                                for (int s = 0; s < 4; ++s) {
-                                    float (&acc)[4] = o[mt][2 * r + s];
-                                    if (F32) {
-                                        float d[4] = {0.f, 0.f, 0.f, 0.f};
-                                        mma_bf16(d, pl[F32 ? mt : 0][0], pl[F32 ? mt : 0][1], pl[F32 ? mt : 0][2], pl[F32 ? mt : 0][3], xa[s], xb[s]);
-                                        mma_bf16(d, pa[mt][0], pa[mt][1], pa[mt][2], pa[mt][3], xa[s], xb[s]);
-                                        acc[0] += d[0]; acc[1] += d[1]; acc[2] += d[2]; acc[3] += d[3];
-                                    } else {
-                                        mma_bf16(acc, pa[mt][0], pa[mt][1], pa[mt][2], pa[mt][3], xa[s], xb[s]);
-                                    }
-                                }
+                            for (int s = 0; s < 16; ++s) { o[mt][s][2 * hh] *= al; o[mt][s][2 * hh + 1] *= al; }
+                        }
+                }
+                // P as A fragments: (row g, tile 0), (row g+8, tile 0), (row g, tile 1), (row g+8, tile 1); fp32: three terms
+                uint32_t pa[MT][F32 ? 3 : 1][4];
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) {
+                        const int hh = x & 1, j = x >> 1;
+                        float p0 = ex2_approx(fmaf(sc[mt][j][2 * hh], mul, -m_run[mt][hh]));
+                        float p1 = ex2_approx(fmaf(sc[mt][j][2 * hh + 1], mul, -m_run[mt][hh]));
+                        l_run[mt][hh] += p0 + p1;
+#pragma unroll
+                        for (int s = 0; s < (F32 ? 3 : 1); ++s) {
+                            pa[mt][s][x] = pack_bf16x2_rn(p0, p1);
+                            p0 -= __uint_as_float(pa[mt][s][x] << 16);
+                            p1 -= __uint_as_float(pa[mt][s][x] & 0xffff0000u);
                         }
                     }
+                // ---- P . V
+                uint32_t vw[4][P / 2];
+                uint2 lv[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {       // k = 2t, 2t+1, 2t+8, 2t+9
+                    if (P == 4) {
+                        const uint2 x = *reinterpret_cast<const uint2*>(stm + vo[e]);
+                        vw[e][0] = x.x; vw[e][1] = x.y;
+                    } else if (P == 6) {
+#pragma unroll
+                        for (int i = 0; i < 3; ++i) vw[e][i] = *reinterpret_cast<const uint32_t*>(stm + vo[e] + 4 * i);
+                    } else {
+                        const uint4 x = *reinterpret_cast<const uint4*>(stm + vo[e]);
+                        vw[e][0] = x.x; vw[e][1] = x.y; vw[e][P / 2 - 2] = x.z; vw[e][P / 2 - 1] = x.w;
+                    }
+                    lv[e] = lut[ste[ve[e]]];
+                }
+                const AW ga = aw_make<P>(prmt(lv[0].x, lv[1].x, 0x7610u), prmt(lv[0].y, lv[1].y, 0x7610u));
+                const AW gb = aw_make<P>(prmt(lv[2].x, lv[3].x, 0x7610u), prmt(lv[2].y, lv[3].y, 0x7610u));
+#pragma unroll
+                for (int r = 0; r < 8; r += 2) {
+                    uint32_t xa[4], xb[4];
+                    attn_v<P>(vw[0], vw[1], r, ga, xa);
+                    attn_v<P>(vw[2], vw[3], r, gb, xb);
+#pragma unroll
+                    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                        for (int s = 0; s < 4; ++s) {
+                            float (&acc)[4] = o[mt][2 * r + s];
+                            if (F32) {
+                                float d[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                                for (int c = 2; c >= 0; --c) {
+                                    const uint32_t (&p)[4] = pa[mt][F32 ? c : 0];
+                                    mma_bf16(d, p[0], p[1], p[2], p[3], xa[s], xb[s]);
+                                }
+                                acc[0] += d[0]; acc[1] += d[1]; acc[2] += d[2]; acc[3] += d[3];
+                            } else {
+                                mma_bf16(acc, pa[mt][0][0], pa[mt][0][1], pa[mt][0][2], pa[mt][0][3], xa[s], xb[s]);
+                            }
+                        }
                 }
             }
-            __syncwarp();
-            if (lane == 0) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar_empty + 8 * stage) : "memory");
+            __syncwarp();                      // every lane has read the stage
+            if (issued < n_mine) issue();
         }
 
-        // ---- the token groups' results into one: o, max, sum per row
+        // ---- the run's result: a lane holds slots [32t, 32t + 32) of rows g and g + 8 of each m tile
+        const bool whole = k0 == 0 && k1 == cc.n;
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
@@ -661,71 +544,67 @@ __global__ void __launch_bounds__(kAW * 32, 2) attn_rows(const AttnArgs a, const
                 float l = l_run[mt][hh];
                 l += __shfl_xor_sync(0xffffffffu, l, 1);
                 l += __shfl_xor_sync(0xffffffffu, l, 2);
-                l_run[mt][hh] = l;
-                if (t == 0) ml[tg * ROWS + (rg * MT + mt) * 16 + g + 8 * hh] = make_float2(m_run[mt][hh], l);
-            }
-        __syncthreads();
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-            for (int hh = 0; hh < 2; ++hh) {
-                const int r = (rg * MT + mt) * 16 + g + 8 * hh;
-                float m = -INFINITY;
-#pragma unroll
-                for (int w = 0; w < TG; ++w) m = fmaxf(m, ml[w * ROWS + r].x);
-                const float al = ex2_approx(m_run[mt][hh] - m);
-#pragma unroll
-                for (int s = 0; s < 16; ++s) { o[mt][s][2 * hh] *= al; o[mt][s][2 * hh + 1] *= al; }
-            }
-#pragma unroll 1
-        for (int w = 0; w < TG; ++w) {
-            if (tg == w) {
-#pragma unroll
-                for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-                    for (int s = 0; s < 16; ++s)
-#pragma unroll
-                        for (int hh = 0; hh < 2; ++hh) {
-                            float2* p = reinterpret_cast<float2*>(ob + ((rg * MT + mt) * 16 + g + 8 * hh) * G_::OSTRIDE + 8 * s + 2 * t);
-                            float2 v = make_float2(o[mt][s][2 * hh], o[mt][s][2 * hh + 1]);
-                            if (w > 0) { const float2 y = *p; v.x += y.x; v.y += y.y; }
-                            *p = v;
-                        }
-            }
-            __syncthreads();
-        }
-        const bool whole = k0 == 0 && k1 == cc.n;
-        for (int r = warp; r < ROWS; r += kAW) {
-            const int row = rt * ROWS + r;
-            if (row >= R) break;
-            float m = -INFINITY, l = 0.f;
-#pragma unroll
-            for (int w = 0; w < TG; ++w) m = fmaxf(m, ml[w * ROWS + r].x);
-#pragma unroll
-            for (int w = 0; w < TG; ++w) { const float2 x = ml[w * ROWS + r]; l += x.y * ex2_approx(x.x - m); }
-            const float* src = ob + r * G_::OSTRIDE;
-            if (whole) {
+                const int r = mt * 16 + g + 8 * hh, row = rt * ROWS + r;
                 const int i = row / a.group, hq = hk * a.group + row - i * a.group;
-                const bool live = !a.tree || i < sv.nd;
-                const float inv = (live && l != 0.f) ? kValueUp / l : 0.f;
-                const int64_t at = (((int64_t)b * a.n_draft + i) * a.n_q_heads + hq) * D + 4 * lane;
-                float v[4];
+                const float m = m_run[mt][hh];
+                if (!whole) {
+                    if (row < R) {
+                        float* dst = a.partials + ((int64_t)(2 * me + (k0 == 0 ? 1 : 0)) * a.part_rows + r) * kAttnPart;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int c = 4 * lane + e;
-                    const int slot = a.inv_perm_v ? (a.inv_perm_v[hk * D + c] & (D - 1)) : c;
-                    v[e] = inv == 0.f ? 0.f : src[part_pos(slot)] * inv;
+                        for (int c = 0; c < 4; ++c) {
+                            reinterpret_cast<float4*>(dst + 32 * t)[c] = make_float4(o[mt][4 * c][2 * hh], o[mt][4 * c + 1][2 * hh], o[mt][4 * c + 2][2 * hh], o[mt][4 * c + 3][2 * hh]);
+                            reinterpret_cast<float4*>(dst + 32 * t + 16)[c] = make_float4(o[mt][4 * c][2 * hh + 1], o[mt][4 * c + 1][2 * hh + 1], o[mt][4 * c + 2][2 * hh + 1], o[mt][4 * c + 3][2 * hh + 1]);
+                        }
+                        if (t == 0) { dst[D] = m; dst[D + 1] = l; }
+                    }
+                    continue;
                 }
-                if (F32) *reinterpret_cast<float4*>(static_cast<float*>(a.out) + at) = make_float4(v[0], v[1], v[2], v[3]);
-                else *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(a.out) + at) =
-                         make_uint2(pack_bf16x2_rn(v[0], v[1]), pack_bf16x2_rn(v[2], v[3]));
-                if (a.lse && lane == 0) a.lse[(int64_t)b * a.n_q_heads + hq] = l > 0.f ? m + log2f(l) : (l == 0.f ? INFINITY : l);
-            } else {
-                float* dst = a.partials + ((int64_t)(2 * blockIdx.x + (k0 == 0 ? 1 : 0)) * ROWS + r) * kAttnPart;
-                reinterpret_cast<float4*>(dst)[lane] = *reinterpret_cast<const float4*>(src + 4 * lane);
-                if (lane == 0) { dst[D] = m; dst[D + 1] = l; }
+                const bool live = row < R && (!a.tree || i < sv.nd) && l != 0.f;
+                const float inv = live ? kValueUp / l : 0.f;
+                float v[2][16];
+#pragma unroll
+                for (int s = 0; s < 16; ++s)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) v[e][s] = live ? o[mt][s][2 * hh + e] * inv : 0.f;
+                const int64_t at = (((int64_t)b * a.n_draft + i) * a.n_q_heads + hq) * D;
+                if (a.lse && row < R && t == 0) a.lse[(int64_t)b * a.n_q_heads + hq] = l > 0.f ? m + log2f(l) : (l == 0.f ? INFINITY : l);
+                if (!a.inv_perm_v) {
+                    if (row < R) {
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            if (F32) {
+                                float4* to = reinterpret_cast<float4*>(static_cast<float*>(a.out) + at + 32 * t + 16 * e);
+#pragma unroll
+                                for (int c = 0; c < 4; ++c) to[c] = make_float4(v[e][4 * c], v[e][4 * c + 1], v[e][4 * c + 2], v[e][4 * c + 3]);
+                            } else {
+                                uint4* to = reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(a.out) + at + 32 * t + 16 * e);
+#pragma unroll
+                                for (int c = 0; c < 2; ++c)
+                                    to[c] = make_uint4(pack_bf16x2_rn(v[e][8 * c], v[e][8 * c + 1]), pack_bf16x2_rn(v[e][8 * c + 2], v[e][8 * c + 3]),
+                                                       pack_bf16x2_rn(v[e][8 * c + 4], v[e][8 * c + 5]), pack_bf16x2_rn(v[e][8 * c + 6], v[e][8 * c + 7]));
+                            }
+                        }
+                    }
+                } else {          // channels in their own order: one row at a time through shared memory
+                    const int32_t* ip = a.inv_perm_v + hk * D;
+                    int sl[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) sl[e] = ip[4 * lane + e] & (D - 1);
+                    for (int gg = 0; gg < 8; ++gg) {
+                        if (rt * ROWS + mt * 16 + gg + 8 * hh >= R) break;
+                        __syncwarp();
+                        if (g == gg) {
+#pragma unroll
+                            for (int s = 0; s < 16; ++s) { orow[32 * t + s] = v[0][s]; orow[32 * t + 16 + s] = v[1][s]; }
+                        }
+                        __syncwarp();
+                        const int64_t to = __shfl_sync(0xffffffffu, at, gg * 4) + 4 * lane;
+                        const float y0 = orow[sl[0]], y1 = orow[sl[1]], y2 = orow[sl[2]], y3 = orow[sl[3]];
+                        if (F32) *reinterpret_cast<float4*>(static_cast<float*>(a.out) + to) = make_float4(y0, y1, y2, y3);
+                        else *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(a.out) + to) = make_uint2(pack_bf16x2_rn(y0, y1), pack_bf16x2_rn(y2, y3));
+                    }
+                }
             }
-        }
         cc.k = k1;
         if (k1 == cc.n) next_pair(cc);
     }
@@ -733,44 +612,58 @@ __global__ void __launch_bounds__(kAW * 32, 2) attn_rows(const AttnArgs a, const
         // give the copies still in flight a bounded chance to land before the shared memory is released
         if (lane == 0) raise_flag(a.status, KVBFP_FLAG_WAIT_TIMEOUT);
         for (int s = 0; s < STAGES; ++s) {
-            (void)mbar_wait_bounded(bar_full + 8 * s, 0);
-            (void)mbar_wait_bounded(bar_full + 8 * s, 1);
+            (void)mbar_wait_bounded(bar + 8 * s, 0);
+            (void)mbar_wait_bounded(bar + 8 * s, 1);
         }
     }
     pdl_trigger();
 }
 
-template <int P, int MT, int RG, bool F32>
-kvbfp_status launch_attn(const AttnArgs& a, cudaStream_t s) {
-    using G_ = AGeo<P, MT, RG, F32>;
+// Three blocks of one m tile per SM (168 registers a thread) where their shared memory fits, two otherwise.
+template <int P, int MT, bool F32>
+int attn_blocks(const AttnArgs& a) {
+    if (MT == 2 || F32) return 2;
+    return 3 * (AGeo<P>::smem_bytes(kHeadDim / a.fmt.block) + 1024) <= 228 * 1024 ? 3 : 2;
+}
+
+template <int P, bool N16, int MT, bool F32>
+kvbfp_status launch_attn(const AttnArgs& a, int grid, cudaStream_t s) {
+    constexpr int MINB = (MT == 2 || F32 || P != 4) ? 2 : 3;
+    auto kernel = attn_rows<P, N16, MT, F32, MINB>;
     static std::atomic<bool> attr_set[64];      // per device; setting the attribute twice is harmless
     int dev = 0;
     KVBFP_CUDA(cudaGetDevice(&dev));
-    const int smem = G_::smem_bytes(a.fmt.batch);
     if (dev < 0 || dev >= 64) return KVBFP_ERR_UNSUPPORTED;
     if (!attr_set[dev].load(std::memory_order_acquire)) {
-        KVBFP_CUDA(cudaFuncSetAttribute(attn_rows<P, MT, RG, F32>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                        G_::smem_bytes(kAttnMaxBatch)));
+        KVBFP_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, AGeo<P>::smem_bytes(8)));
         attr_set[dev].store(true, std::memory_order_release);
     }
     CUtensorMap k_map, v_map;
     if (P != 6) {
         const uint64_t rows = (uint64_t)a.fmt.batch * a.fmt.n_kv_heads * a.fmt.max_seq * P / 8;     // lines of 128 bytes
-        kvbfp_status st = make_row_map(&k_map, a.k_mant, rows, 128, kAttnTile * P / 8);
-        if (st == KVBFP_OK) st = make_row_map(&v_map, a.v_mant, rows, 128, kAttnTile * P / 8);
+        kvbfp_status st = make_row_map(&k_map, a.k_mant, rows, 128, AGeo<P>::TILE * P / 8);
+        if (st == KVBFP_OK) st = make_row_map(&v_map, a.v_mant, rows, 128, AGeo<P>::TILE * P / 8);
         if (st != KVBFP_OK) return st;
     }
-    KVBFP_CUDA(launch_pdl(attn_rows<P, MT, RG, F32>, dim3(a.workers), dim3(kAW * 32), smem, s, a, k_map, v_map));
+    KVBFP_CUDA(launch_pdl(attn_prep<P, MT, F32>, dim3(a.fmt.batch * a.fmt.n_kv_heads * a.n_row_tiles), dim3(128), 0, s, a));
+    KVBFP_LAUNCH_CHECK("attn_prep");
+    KVBFP_CUDA(launch_pdl(kernel, dim3(grid), dim3(kAttnWarps * 32), AGeo<P>::smem_bytes(kHeadDim / a.fmt.block), s, a, k_map, v_map));
     KVBFP_LAUNCH_CHECK("attn_rows");
     return KVBFP_OK;
 }
 
 template <int P>
-kvbfp_status launch_attn_p(const AttnArgs& a, cudaStream_t s) {
-    if (!a.q_is_bf16) return a.rows_tile == 16 ? launch_attn<P, 1, 1, true>(a, s) : KVBFP_ERR_UNSUPPORTED;
-    if (a.rows_tile == 16) return launch_attn<P, 1, 1, false>(a, s);
-    if (a.rows_tile == 32) return launch_attn<P, 2, 1, false>(a, s);
-    return launch_attn<P, 2, 2, false>(a, s);
+AttnShape attn_shape_p(const AttnArgs& a) {
+    const int blocks = P != 4 || a.rows_tile == 32 || !a.q_is_bf16 ? 2 : attn_blocks<P, 1, false>(a);
+    return {AGeo<P>::TILE, blocks};
+}
+
+template <int P>
+kvbfp_status launch_attn_p(const AttnArgs& a, int grid, cudaStream_t s) {
+    const bool n16 = a.fmt.block == 16;
+    if (!a.q_is_bf16) return n16 ? launch_attn<P, true, 1, true>(a, grid, s) : launch_attn<P, false, 1, true>(a, grid, s);
+    if (a.rows_tile == 16) return n16 ? launch_attn<P, true, 1, false>(a, grid, s) : launch_attn<P, false, 1, false>(a, grid, s);
+    return n16 ? launch_attn<P, true, 2, false>(a, grid, s) : launch_attn<P, false, 2, false>(a, grid, s);
 }
 
 }  // namespace

@@ -1,6 +1,7 @@
-// The 6-bit instantiations of attn_rows.
+// The 6-bit instantiations of attn_prep and attn_rows.
 #include "attn_rows.cuh"
 
 namespace kvbfp {
-kvbfp_status launch_attn_rows6(const AttnArgs& a, cudaStream_t s) { return launch_attn_p<6>(a, s); }
+AttnShape attn_shape6(const AttnArgs& a) { return attn_shape_p<6>(a); }
+kvbfp_status launch_attn_rows6(const AttnArgs& a, int grid, cudaStream_t s) { return launch_attn_p<6>(a, grid, s); }
 }  // namespace kvbfp

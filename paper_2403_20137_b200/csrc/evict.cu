@@ -18,9 +18,9 @@ __device__ __forceinline__ uint32_t mass_key(float x) {
 // found by radix selection (four digits of eight bits, histograms in shared memory); of equals to the threshold the
 // lowest positions are kept.  Each warp owns a contiguous piece of the region, so one scan over the warps' counts
 // places every kept row.
-__global__ void __launch_bounds__(kSelThreads) evict_select(const float* __restrict__ mass, const int32_t* __restrict__ seq_lens,
+__global__ void __launch_bounds__(kSelThreads) evict_select(const float* mass, const int32_t* seq_lens,
                                                             int max_seq, int n_heads, int budget, int n_sink, int n_recent,
-                                                            int32_t* __restrict__ kept, uint32_t* status) {
+                                                            int32_t* kept, uint32_t* status) {
     __shared__ uint32_t hist[kHistCopies][256];
     __shared__ uint32_t s_digit, s_need;
     __shared__ int s_gt[kSelWarps], s_eq[kSelWarps];
