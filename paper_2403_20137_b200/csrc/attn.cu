@@ -97,7 +97,7 @@ __global__ void __launch_bounds__(128) attn_merge(const AttnArgs a, int64_t n_ro
     const float* src = so[SPLIT ? 0 : warp];
     bool live = n > 0;
     if (live && a.tree) live = i < a.views[b].nd;
-    const float inv = (live && l != 0.f) ? kValueUp / l : 0.f;
+    const float inv = (live && l != 0.f) ? a.out_up / l : 0.f;
     float v[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
@@ -275,6 +275,7 @@ kvbfp_status attn_common(const AttnCall& c) {
     const bool bf16 = c.dt == KVBFP_BF16;
     const AttnShape shape = bf16 ? AttnShape{128, 1} : f.mant_bits == 4 ? attn_shape4(a) : f.mant_bits == 6 ? attn_shape6(a) : attn_shape8(a);
     a.tile = shape.tile;
+    a.out_up = bf16 ? (float)(1 << (19 - f.mant_bits)) : kValueUp;      // attn_umma: 2^(17 - (p - 2))
     const int64_t most = (int64_t)f.batch * f.n_kv_heads * n_row_tiles * (f.max_seq / shape.tile + 2);    // tiles at the longest
     int64_t grid = (int64_t)n_sm * shape.blocks_per_sm;
     const int per_block = bf16 ? 1 : kAttnWarps;

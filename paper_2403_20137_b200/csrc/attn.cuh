@@ -61,6 +61,7 @@ struct AttnArgs {
     float* mass;                   // [B, Hkv, max_seq] or NULL
     float* partials;               // workspace: [2 * workers, part_rows, kAttnPart]
     int workers;                   // warps of the main kernel
+    float out_up;                  // sums of P and V as the kernel carries them -> values
     uint32_t* status;
 };
 
@@ -106,7 +107,7 @@ __host__ __device__ __forceinline__ int worker_of(int x, int n_items, int worker
     return (int)(((int64_t)(x + 1) * workers - 1) / n_items);
 }
 
-// Cached values are carried times 2^-8 inside the kernels, so that no exponent byte leaves the bf16 range with the
+// Cached values are carried times 2^-8 inside attn_rows, so that no exponent byte leaves the bf16 range with the
 // conversion's offset; undone on scores and outputs.
 constexpr float kValueUp = 256.f;
 

@@ -15,6 +15,8 @@
 //   warp 17      issues the matrix instructions: S of tile i, then O of tile i - 1
 //   warps 0..7   softmax, a thread per token, each group half of the query rows: scores from tensor memory, masks,
 //                running maximum, P to shared memory; at the end of a run O^T from tensor memory to the result
+// Cached values are converted relative to their row's largest exponent (see below); magnitudes of 2^118 and above are
+// outside the range.
 // The row maximum runs across threads here, so it is only taken when a score passes the reference by 8 (a factor 2^8),
 // which a barrier over the group tells; then O is rescaled in tensor memory.  Sums are kept per thread and reduced at
 // the end of a run.
@@ -34,25 +36,25 @@ constexpr int kUThreads = 18 * 32;
 // Slot at position `m` of a converted row (the order the fields unpack in); K and V alike.
 template <int P>
 __device__ __forceinline__ int umma_slot(int m) {
-    if (P == 4) return (m & ~7) | ((m & 1) << 2) | ((m >> 1) & 3);
-    if (P == 8) return (m & ~3) | ((m & 1) << 1) | ((m >> 1) & 1);
-    return m;
+    if (P != 8) return (m & ~7) | ((m & 1) << 2) | ((m >> 1) & 3);
+    return (m & ~3) | ((m & 1) << 1) | ((m >> 1) & 1);
 }
 
 template <int P, int N>
 struct UGeo {
     static constexpr int ROW_M = kHeadDim * P / 8;
-    static constexpr int STAGES = P == 4 ? 4 : (P == 8 && N == 64) ? 2 : 3;
+    static constexpr int STAGES = P == 4 ? (N == 64 ? 3 : 4) : 2;
+    static constexpr int VBUF = P == 8 && N == 64 ? 2 : 3;       // converted V tiles: one being written, the others in use
     static constexpr int MANT = 2 * kUTile * ROW_M;              // K and V rows of a stage
-    static constexpr int V_OFF = STAGES * MANT;                  // converted V, two buffers of 32 KB
+    static constexpr int V_OFF = STAGES * MANT;                  // converted V, buffers of 32 KB
     static constexpr int V_BYTES = kUTile * kHeadDim * 2;
-    static constexpr int P_OFF = V_OFF + 2 * V_BYTES;
+    static constexpr int P_OFF = V_OFF + VBUF * V_BYTES;
     static constexpr int P_BYTES = kUTile * N * 2;
     static constexpr int Q_OFF = P_OFF + 2 * P_BYTES;
     static constexpr int Q_BYTES = N * kHeadDim * 2;
     static constexpr int E_OFF = Q_OFF + 2 * Q_BYTES;            // exponent bytes: STAGES x 2 x 128 x row_e
-    // behind them: weight table, row data, drafted positions, channel table, references, reduction, barriers
-    static constexpr int SMALL = 256 * 8 + N * 16 + 2 * kAttnMaxDraft * 4 + 2 * kHeadDim * 4 + N * 4 * 4 + 8 * N / 2 * 4 + 16 +
+    // behind them: factors of the tokens, row data, drafted positions, channel table, references, reduction, barriers
+    static constexpr int SMALL = 8 * kUTile * 4 + N * 16 + 2 * kAttnMaxDraft * 4 + 2 * kHeadDim * 4 + N * 4 * 4 + 8 * N / 2 * 4 + 16 +
                                  (2 * STAGES + 12) * 8 + 16;
     __host__ __device__ static int smem_bytes(int row_e) { return E_OFF + STAGES * 2 * kUTile * row_e + SMALL; }
 };
@@ -75,31 +77,77 @@ __global__ void __launch_bounds__(128) umma_prep(const AttnArgs a) {
     }
 }
 
+// Conversion.  A field that lies within the low eight bits of a 16-bit half IS a bf16 number: the half masked down to
+// it, read as bf16, is the field times 2^-133 (times 4 or 16 where it lies higher), for below 2^-125 bf16 counts in equal
+// steps.  One bf16x2 fma turns two of them into (field - offset) times the block's weight, exactly; nothing is or-ed
+// under an exponent and fields need no shift to bit 0, which takes a third of the integer instructions out (the integer
+// pipe bounds the conversion).  For the multiplier 2^133 to stay in range the weights are relative to the row's largest
+// exponent E (2^-8 for the block that has it, down to 2^-108); 2^E comes back as a factor per token: on the scores for K,
+// on the weights P for V.
+struct UW {
+    uint32_t s, s2, c;      // multipliers of fields at bit 0 and higher up, -offset * weight
+};
+template <int P>
+__device__ __forceinline__ UW umma_weights(int below) {      // steps of two below the row's largest exponent
+    const uint32_t d = (uint32_t)min(below, 100) * 0x00800080u;
+    UW w;
+    w.s = 0x7E007E00u - d;                                             // 2^(133 - 8 - d)
+    w.s2 = (P == 4 ? 0x7C007C00u : 0x7D007D00u) - d;                   // / 16, / 4
+    w.c = (P == 4 ? 0xBD00BD00u : P == 6 ? 0xBE00BE00u : 0xBF00BF00u) - d;     // -8, -32, -128 times 2^(-8 - d)
+    return w;
+}
+// Exponent bytes of a row as (byte j: slots 32 j ..) or, for blocks of 16, two words (byte j: slots 16 j ..).
+template <bool N16>
+__device__ __forceinline__ void umma_exps(const uint8_t* e, int row_e, uint32_t (&w)[2]) {
+    if (N16) {
+        const uint2 x = *reinterpret_cast<const uint2*>(e);
+        w[0] = x.x;
+        w[1] = x.y;
+    } else {
+        w[0] = row_e == 4 ? *reinterpret_cast<const uint32_t*>(e)
+               : row_e == 2 ? prmt(*reinterpret_cast<const uint16_t*>(e), 0u, 0x1100u) : prmt(*e, 0u, 0u);
+        w[1] = w[0];
+    }
+}
+// The row's blocks (4 or 8) relative to its largest exponent byte, which is returned (254 at most).
+template <int P, bool N16>
+__device__ __forceinline__ int umma_row(const uint32_t (&w)[2], UW (&g)[N16 ? 8 : 4]) {
+    int e[N16 ? 8 : 4], top = 0;
+#pragma unroll
+    for (int j = 0; j < (N16 ? 8 : 4); ++j) {
+        e[j] = (int)((w[j >> 2] >> (8 * (j & 3))) & 0xffu);
+        top = max(top, e[j]);
+    }
+#pragma unroll
+    for (int j = 0; j < (N16 ? 8 : 4); ++j) g[j] = umma_weights<P>(top - e[j]);
+    return min(top, 254);
+}
 // 32 slots (four 16-byte pieces of bf16) of a packed row, from slot 32 i on.
 template <int P>
-__device__ __forceinline__ void convert32(const uint8_t* tile, int row, int i, const AW& g0, const AW& g1, uint32_t (&r)[16]) {
+__device__ __forceinline__ void convert32(const uint8_t* tile, int row, int i, const UW& g0, const UW& g1, uint32_t (&r)[16]) {
     if (P == 4) {
-        const int line = row >> 1, p = ((row & 1) << 6) + 16 * i;
-        const uint4 x = *reinterpret_cast<const uint4*>(tile + line * 128 + (p ^ ((line & 7) << 4)));
+        const int line = row >> 1, at = ((row & 1) << 6) ^ ((line & 7) << 4);
+        const uint4 x = *reinterpret_cast<const uint4*>(tile + line * 128 + (at ^ (16 * i)));
         const uint32_t w[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const AW& g = j < 2 ? g0 : g1;
-            r[4 * j] = acvt<4>(w[j], g);
-            r[4 * j + 1] = acvt<4>(w[j] >> 4, g);
-            r[4 * j + 2] = acvt<4>(w[j] >> 8, g);
-            r[4 * j + 3] = acvt<4>(w[j] >> 12, g);
+            const UW& g = j < 2 ? g0 : g1;
+            const uint32_t y = w[j] >> 8;
+            r[4 * j] = fma_bf16x2(w[j] & 0x000F000Fu, g.s, g.c);
+            r[4 * j + 1] = fma_bf16x2(w[j] & 0x00F000F0u, g.s2, g.c);
+            r[4 * j + 2] = fma_bf16x2(y & 0x000F000Fu, g.s, g.c);
+            r[4 * j + 3] = fma_bf16x2(y & 0x00F000F0u, g.s2, g.c);
         }
     } else if (P == 8) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const uint4 x = *reinterpret_cast<const uint4*>(tile + row * 128 + ((32 * i + 16 * h) ^ ((row & 7) << 4)));
             const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-            const AW& g = h ? g1 : g0;
+            const UW& g = h ? g1 : g0;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                r[8 * h + 2 * j] = acvt<8>(w[j], g);
-                r[8 * h + 2 * j + 1] = acvt<8>(w[j] >> 8, g);
+                r[8 * h + 2 * j] = fma_bf16x2(w[j] & 0x00FF00FFu, g.s, g.c);
+                r[8 * h + 2 * j + 1] = fma_bf16x2(prmt(w[j], 0u, 0x4341u), g.s, g.c);
             }
         }
     } else {
@@ -110,15 +158,18 @@ __device__ __forceinline__ void convert32(const uint8_t* tile, int row, int i, c
             w[2 * j] = x.x;
             w[2 * j + 1] = x.y;
         }
+        // eight slots are two runs of three bytes; a 16-bit half holds bytes 0, 1 (then 1, 2) of the first run, the other
+        // half those of the second: slots 0 | 4, 1 | 5 and 2 | 6, 3 | 7
 #pragma unroll
-        for (int j = 0; j < 16; ++j) {
-            uint32_t f[2];
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const int bit = 6 * (2 * j + e), word = bit >> 5, s = bit & 31;
-                f[e] = (s + 6 > 32) ? __funnelshift_r(w[word], w[(word + 1) % 6], s) : (w[word] >> s);
-            }
-            r[j] = acvt<6>(prmt(f[0], f[1], 0x5410u), j < 8 ? g0 : g1);
+        for (int j = 0; j < 4; ++j) {
+            const int b = 6 * j, word = b >> 2;                      // first byte of the eight slots: 0, 6, 12, 18
+            const bool odd = (b & 3) != 0;
+            const uint32_t lo = prmt(w[word], w[word + 1], odd ? 0x6532u : 0x4310u), hi = prmt(w[word], w[word + 1], odd ? 0x7643u : 0x5421u);
+            const UW& g = j < 2 ? g0 : g1;
+            r[4 * j] = fma_bf16x2(lo & 0x003F003Fu, g.s, g.c);
+            r[4 * j + 1] = fma_bf16x2((lo >> 4) & 0x00FC00FCu, g.s2, g.c);
+            r[4 * j + 2] = fma_bf16x2((hi >> 2) & 0x00FC00FCu, g.s2, g.c);
+            r[4 * j + 3] = fma_bf16x2((hi >> 8) & 0x00FC00FCu, g.s2, g.c);
         }
     }
 }
@@ -156,9 +207,10 @@ __global__ void __launch_bounds__(kUThreads, 1) attn_umma(const AttnArgs a, cons
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int row_e = D / a.fmt.block, exp_half = kUTile * row_e;
     uint8_t* rest = smem + G_::E_OFF + STAGES * 2 * exp_half;
-    uint2* lut = reinterpret_cast<uint2*>(rest);
-    RowInfo* ri_all = reinterpret_cast<RowInfo*>(rest + 2048);
-    int* dpos_all = reinterpret_cast<int*>(rest + 2048 + N * 16);
+    float* kfac = reinterpret_cast<float*>(rest);            // 2^E of the K and V rows of four tiles
+    float* vfac = kfac + 4 * kUTile;
+    RowInfo* ri_all = reinterpret_cast<RowInfo*>(vfac + 4 * kUTile);
+    int* dpos_all = reinterpret_cast<int*>(ri_all + N);
     int* chan_all = dpos_all + 2 * kAttnMaxDraft;
     float* mref_all = reinterpret_cast<float*>(chan_all + 2 * D);
     float* mstep_all = mref_all + N;        // step of a reference change, and the factor of the sums so far
@@ -171,10 +223,6 @@ __global__ void __launch_bounds__(kUThreads, 1) attn_umma(const AttnArgs a, cons
     const uint32_t b_full = bars, b_empty = bars + 8 * STAGES, b_kv = b_empty + 8 * STAGES, b_qk = b_kv + 16, b_p = b_qk + 16,
                    b_pv = b_p + 16, b_qfull = b_pv + 16, b_qfree = b_qfull + 16;
 
-    for (int e = tid; e < 256; e += kUThreads) {
-        const uint32_t s2 = attn_weight<P>(e) * 0x00010001u;
-        lut[e] = make_uint2(s2, mul_bf16x2(s2, AFmt<P>::bias));
-    }
     if (tid == 0) {
         for (int s = 0; s < STAGES; ++s) {
             mbar_init(b_full + 8 * s, 1);
@@ -230,7 +278,7 @@ __global__ void __launch_bounds__(kUThreads, 1) attn_umma(const AttnArgs a, cons
     };
     bool dead = false;          // a wait ran out: no more waits, the flag is up, results are void
     auto wait = [&](uint32_t bar, uint32_t parity) {
-        if (!dead && !mbar_wait_bounded(bar, parity)) {
+        if (!dead && !mbar_try(bar, parity) && !mbar_wait_bounded(bar, parity)) {
             dead = true;
             raise_flag(a.status, KVBFP_FLAG_WAIT_TIMEOUT);
         }
@@ -289,58 +337,57 @@ __global__ void __launch_bounds__(kUThreads, 1) attn_umma(const AttnArgs a, cons
         }
     } else if (warp == 17) {
         // ================================================================ matrix instructions
-        if (lane == 0) {
-            constexpr uint32_t id_s = umma_idesc(128, N, false, false), id_o = umma_idesc(128, N, true, true);
-            Cursor c = seek();
-            int run = 0;
-            bool first = true, o_first = true;       // first tile of its run: the tile whose S comes next / whose O comes next
-            auto product_o = [&](int i) {
-                const int b = i & 1;
-                wait(b_p + 8 * b, (uint32_t)(i >> 1) & 1u);
-                if (dead) return;
-                tmem_fence_after();
-                const uint32_t v = smem_u32(smem) + G_::V_OFF + b * G_::V_BYTES, p = smem_u32(smem) + G_::P_OFF + b * G_::P_BYTES;
+        constexpr uint32_t id_s = umma_idesc(128, N, false, false), id_o = umma_idesc(128, N, true, true);
+        const uint32_t tmu = __shfl_sync(0xffffffffu, tm, 0), base = smem_u32(smem);
+        Cursor c = seek();
+        int run = 0, vslot = 0;
+        bool first = true, o_first = true;       // first tile of its run: the tile whose S comes next / whose O comes next
+        auto product_o = [&](int i) {
+            const int b = i & 1;
+            wait(b_p + 8 * b, (uint32_t)(i >> 1) & 1u);
+            __syncwarp();
+            tmem_fence_after();
+            const uint64_t v = umma_desc<128>(base + G_::V_OFF + vslot * G_::V_BYTES, kUTile * 128, 1024);
+            const uint64_t p = umma_desc<SWP>(base + G_::P_OFF + b * G_::P_BYTES, 16, 8 * SWP);
 #pragma unroll
-                for (int ks = 0; ks < kUTile / 16; ++ks)
-                    umma_ss(tm + TM_O, umma_desc<128>(v + ks * 2048, kUTile * 128, 1024), umma_desc<SWP>(p + ks * 16 * SWP, 16, 8 * SWP), id_o,
-                            ks > 0 || !o_first);
-                umma_commit(b_pv + 8 * b);
-            };
-            for (int i = 0; i < n_mine && !dead; ++i) {
-                const int b = i & 1, q = run & 1;
-                wait(b_kv + 8 * b, (uint32_t)(i >> 1) & 1u);
-                if (first) wait(b_qfull + 8 * q, (uint32_t)(run >> 1) & 1u);
-                if (dead) break;
-                tmem_fence_after();
-                const uint32_t qb = smem_u32(smem) + G_::Q_OFF + q * G_::Q_BYTES;
+            for (int ks = 0; ks < kUTile / 16; ++ks)
+                umma_ss(tmu + TM_O, v + ks * (2048 >> 4), p + ks * (16 * SWP >> 4), id_o, ks > 0 || !o_first);
+            umma_commit(b_pv + 8 * b);
+            vslot = vslot == G_::VBUF - 1 ? 0 : vslot + 1;
+        };
+        for (int i = 0; i < n_mine; ++i) {
+            const int b = i & 1, q = run & 1;
+            wait(b_kv + 8 * b, (uint32_t)(i >> 1) & 1u);
+            if (first) wait(b_qfull + 8 * q, (uint32_t)(run >> 1) & 1u);
+            __syncwarp();
+            tmem_fence_after();
+            const uint64_t qd = umma_desc<128>(base + G_::Q_OFF + q * G_::Q_BYTES, 16, 1024);
 #pragma unroll
-                for (int ks = 0; ks < 8; ++ks)
-                    umma_ts(tm + TM_S + b * N, tm + TM_K + b * 64 + ks * 8, umma_desc<128>(qb + (ks >> 2) * (N * 128) + (ks & 3) * 32, 16, 1024),
-                            id_s, ks > 0);
-                umma_commit(b_qk + 8 * b);
-                const bool was_first = first;
-                first = false;
-                if (++c.k == c.n) {
-                    umma_commit(b_qfree + 8 * q);
-                    next_pair(c);
-                    first = true;
-                    ++run;
-                }
-                if (i > 0) product_o(i - 1);
-                o_first = was_first;
+            for (int ks = 0; ks < 8; ++ks)
+                umma_ts(tmu + TM_S + b * N, tmu + TM_K + b * 64 + ks * 8, qd + (((ks >> 2) * (N * 128) + (ks & 3) * 32) >> 4), id_s, ks > 0);
+            umma_commit(b_qk + 8 * b);
+            const bool was_first = first;
+            first = false;
+            if (++c.k == c.n) {
+                umma_commit(b_qfree + 8 * q);
+                next_pair(c);
+                first = true;
+                ++run;
             }
-            if (!dead) product_o(n_mine - 1);
-            if (dead) {       // let what was issued come to its end before the tensor memory goes
-                umma_commit(b_qfree);
-                (void)mbar_wait_bounded(b_qfree, 0);
-                (void)mbar_wait_bounded(b_qfree, 1);
-            }
+            if (i > 0) product_o(i - 1);
+            o_first = was_first;
+        }
+        product_o(n_mine - 1);
+        if (__any_sync(0xffffffffu, dead)) {       // let what was issued come to its end before the tensor memory goes
+            umma_commit(b_qfree);
+            (void)mbar_wait_bounded(b_qfree, 0);
+            (void)mbar_wait_bounded(b_qfree, 1);
         }
     } else if (warp >= 8) {
         // ================================================================ conversion: a thread per token
         const int grp = (warp - 8) >> 2, row = tid & 127;
         const uint32_t tk = tm + TM_K + grp * 64 + ((uint32_t)(warp & 3) << 21);        // lane field: 32 * quarter << 16
-        uint8_t* vb = smem + G_::V_OFF + grp * G_::V_BYTES + row * 128;
+        int vslot = grp;
         for (int i = grp; i < n_mine; i += 2) {
             const int s = i % STAGES;
             wait(b_full + 8 * s, (uint32_t)(i / STAGES) & 1u);
@@ -351,38 +398,33 @@ __global__ void __launch_bounds__(kUThreads, 1) attn_umma(const AttnArgs a, cons
                 tmem_fence_after();
             }
             __syncwarp();
+            UW g[N16 ? 8 : 4];
+            uint32_t ew[2];
+            umma_exps<N16>(ke, row_e, ew);
+            int top = umma_row<P, N16>(ew, g);
+            kfac[(i & 3) * kUTile + row] = __uint_as_float((uint32_t)top << 23);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const uint2 w0 = lut[ke[N16 ? 2 * j : (32 * j) / a.fmt.block]];
-                const AW g0 = aw_make<P>(w0.x, w0.y);
-                AW g1 = g0;
-                if (N16) {
-                    const uint2 w1 = lut[ke[2 * j + 1]];
-                    g1 = aw_make<P>(w1.x, w1.y);
-                }
                 uint32_t r[16];
-                convert32<P>(km, row, j, g0, g1, r);
+                convert32<P>(km, row, j, g[N16 ? 2 * j : j], g[N16 ? 2 * j + 1 : j], r);
                 tmem_st<16>(tk + 16 * j, r);
             }
-            if (i >= 2) wait(b_pv + 8 * grp, (uint32_t)((i >> 1) - 1) & 1u);    // V of the tile before is used up
+            umma_exps<N16>(ke + exp_half, row_e, ew);
+            top = umma_row<P, N16>(ew, g);
+            vfac[(i & 3) * kUTile + row] = __uint_as_float((uint32_t)max(top - 9, 0) << 23);
+            // the buffer's last tile was i - VBUF
+            if (i >= G_::VBUF) wait(b_pv + 8 * ((i - G_::VBUF) & 1), (uint32_t)((i - G_::VBUF) >> 1) & 1u);
+            uint8_t* vb = smem + G_::V_OFF + vslot * G_::V_BYTES + row * 128;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const uint2 w0 = lut[ke[exp_half + (N16 ? 2 * j : (32 * j) / a.fmt.block)]];
-                const AW g0 = aw_make<P>(w0.x, w0.y);
-                AW g1 = g0;
-                if (N16) {
-                    const uint2 w1 = lut[ke[exp_half + 2 * j + 1]];
-                    g1 = aw_make<P>(w1.x, w1.y);
-                }
                 uint32_t r[16];
-                convert32<P>(km + G_::MANT / 2, row, j, g0, g1, r);
+                convert32<P>(km + G_::MANT / 2, row, j, g[N16 ? 2 * j : j], g[N16 ? 2 * j + 1 : j], r);
+                uint8_t* to = vb + (j >> 1) * (kUTile * 128);
 #pragma unroll
-                for (int x = 0; x < 4; ++x) {       // 16-byte pieces 4 j + x of the row: panel of 64 slots, swizzled
-                    const int c = 4 * j + x;
-                    *reinterpret_cast<uint4*>(vb + (c >> 3) * (kUTile * 128) + (((c & 7) ^ (row & 7)) << 4)) =
-                        make_uint4(r[4 * x], r[4 * x + 1], r[4 * x + 2], r[4 * x + 3]);
-                }
+                for (int x = 0; x < 4; ++x)       // 16-byte pieces 4 j + x of the row: panel of 64 slots, swizzled
+                    *reinterpret_cast<uint4*>(to + (((4 * (j & 1) + x) ^ (row & 7)) << 4)) = make_uint4(r[4 * x], r[4 * x + 1], r[4 * x + 2], r[4 * x + 3]);
             }
+            vslot = (vslot + 2) % G_::VBUF;
             __syncwarp();
             tmem_wait_st();
             fence_async_shared();
@@ -403,7 +445,7 @@ __global__ void __launch_bounds__(kUThreads, 1) attn_umma(const AttnArgs a, cons
         float *mref = mref_all + wg * C, *mstep = mstep_all + wg * C, *mfac = mfac_all + wg * C, *lsum = lsum_all + wg * C, *red = red_all + wg * 4 * C;
         int* unset = unset_all + wg;
         const int R = a.n_draft * a.group;
-        const float up = a.scale * kValueUp, to_log2 = 1.4426950408889634f;
+        const float up = a.scale * (P == 4 ? 64.f : P == 6 ? 16.f : 4.f), to_log2 = 1.4426950408889634f;      // 2^8 2^-(P-2)
         const float cap_in = a.softcap > 0.f ? up / a.softcap * 2.8853900817779268f : 0.f;
         // the column a lane ends up with: its upper log2(C) lane bits
         const int my_col = C == 32 ? lane : C == 16 ? lane >> 1 : lane >> 2;
@@ -441,11 +483,13 @@ __global__ void __launch_bounds__(kUThreads, 1) attn_umma(const AttnArgs a, cons
 #pragma unroll
                 for (int j = 0; j < C; ++j) y[j] = __uint_as_float(raw[j]);
                 // ---- cap, bias, masks: y * mul in log2 units
-                float mul = up * to_log2;
+                const float kf = kfac[(it & 3) * kUTile + m_pos];
+                float mul = up * to_log2 * kf;
                 if (a.softcap > 0.f) {
                     mul = a.softcap * to_log2;
+                    const float in = cap_in * kf;
 #pragma unroll
-                    for (int j = 0; j < C; ++j) y[j] = 1.f - __fdividef(2.f, 1.f + ex2_approx(y[j] * cap_in));      // tanh x = 1 - 2 / (1 + e^2x): about 2e-7 absolute
+                    for (int j = 0; j < C; ++j) y[j] = 1.f - __fdividef(2.f, 1.f + ex2_approx(y[j] * in));      // tanh x = 1 - 2 / (1 + e^2x): about 2e-7 absolute
                 }
                 if (a.slopes != nullptr || !(tt + kUTile <= sv.ctx && (tt >= clear_lo || tt + kUTile <= sv.pf))) {
                     const bool in_ctx = tok < sv.ctx;
@@ -525,6 +569,7 @@ __global__ void __launch_bounds__(kUThreads, 1) attn_umma(const AttnArgs a, cons
                 // ---- P: weights of this token, bf16, a line of 2 N bytes
                 if (it >= 2) wait(b_pv + 8 * s, (uint32_t)((it >> 1) - 1) & 1u);
                 uint8_t* pb = smem + G_::P_OFF + s * G_::P_BYTES;
+                const float vf = vfac[(it & 3) * kUTile + m_pos];
 #pragma unroll
                 for (int j = 0; j < C; j += 8) {
                     uint32_t w[4];
@@ -533,7 +578,7 @@ __global__ void __launch_bounds__(kUThreads, 1) attn_umma(const AttnArgs a, cons
                         const float p0 = ex2_approx(y[j + 2 * e]), p1 = ex2_approx(y[j + 2 * e + 1]);
                         l[j + 2 * e] += p0;
                         l[j + 2 * e + 1] += p1;
-                        w[e] = pack_bf16x2_rn(p0, p1);
+                        w[e] = pack_bf16x2_rn(p0 * vf, p1 * vf);
                     }
                     const uint32_t off = m_pos * SWP + (wg * C + j) * 2;
                     *reinterpret_cast<uint4*>(pb + (off ^ (((off >> 7) & (SWP / 16 - 1)) << 4))) = make_uint4(w[0], w[1], w[2], w[3]);
@@ -585,7 +630,7 @@ __global__ void __launch_bounds__(kUThreads, 1) attn_umma(const AttnArgs a, cons
                             const int i = row / a.group, hq = hk * a.group + row - i * a.group;
                             const float ls = lsum[j + e];
                             const bool live = (!a.tree || i < sv.nd) && ls != 0.f;
-                            const float v = live ? __uint_as_float(o[e]) * (kValueUp / ls) : 0.f;
+                            const float v = live ? __uint_as_float(o[e]) * (a.out_up / ls) : 0.f;
                             static_cast<__nv_bfloat16*>(a.out)[(((int64_t)b * a.n_draft + i) * a.n_q_heads + hq) * D + ch] = __float2bfloat16_rn(v);
                         } else {
                             part[(j + e) * kAttnPart + slot] = __uint_as_float(o[e]);
