@@ -8,13 +8,16 @@
 // cycles per product, so what is left to do per cached element is its conversion, and that is done once for all rows
 // (the warp-level kernel converts per 16 rows and its matrix instructions run at a third of the rate).
 //
-// One persistent thread block per SM, tiles of 128 tokens, a contiguous range of tiles per block (attn.cuh).  Roles:
-//   warp 16      copies packed tiles into a ring of stages and pi(Q) of the next (sequence, head, row tile) ahead
-//   warps 8..15  conversion, two groups on alternate tiles, a thread per token: its K row goes to tensor memory (the A
-//                operand of the first product), its V row to shared memory (the A operand of the second, slots contiguous)
-//   warp 17      issues the matrix instructions: S of tile i, then O of tile i - 1
-//   warps 0..7   softmax, a thread per token, each group half of the query rows: scores from tensor memory, masks,
-//                running maximum, P to shared memory; at the end of a run O^T from tensor memory to the result
+// One persistent thread block per SM, tiles of 128 tokens.  Two teams of eight warps, each a worker with a contiguous
+// range of tiles of its own (attn.cuh); two threads per token:
+//   K rows converted to tensor memory (the A operand of the first product), half a row a thread
+//   V rows converted to shared memory (the A operand of the second, slots contiguous) while the first product runs
+//   scores from tensor memory, half of the query rows a thread: masks, running maximum, P to shared memory
+//   at the end of a run O^T from tensor memory to the result or a partial
+// While one team waits (for a product, a barrier, a copy) the other works.  Warp 16 copies packed tiles into a ring of
+// units that both teams draw from in turn and pi(Q) of the runs, warp 17 issues the matrix instructions of both.
+// (Groups of their own for conversion and softmax, with two to three tiles between them, took twice as long: four warps
+// a phase are slow and the buffers between the phases were what everything waited for.)
 // Cached values are converted relative to their row's largest exponent (see below); magnitudes of 2^118 and above are
 // outside the range.
 // The row maximum runs across threads here, so it is only taken when a score passes the reference by 8 (a factor 2^8),
@@ -43,20 +46,26 @@ __device__ __forceinline__ int umma_slot(int m) {
 template <int P, int N>
 struct UGeo {
     static constexpr int ROW_M = kHeadDim * P / 8;
-    static constexpr int STAGES = P == 4 ? (N == 64 ? 3 : 4) : 2;
-    static constexpr int VBUF = P == 8 && N == 64 ? 2 : 3;       // converted V tiles: one being written, the others in use
-    static constexpr int MANT = 2 * kUTile * ROW_M;              // K and V rows of a stage
-    static constexpr int V_OFF = STAGES * MANT;                  // converted V, buffers of 32 KB
+    static constexpr int C = N / 2;                              // query rows of a thread
+    static constexpr int UNIT = kUTile * ROW_M;                  // a tile's K or V rows
+    static constexpr int UNITS = P == 4 ? (N == 64 ? 9 : N == 32 ? 11 : 12) : P == 6 ? (N == 64 ? 6 : N == 32 ? 8 : 10) : (N == 64 ? 5 : N == 32 ? 6 : 7);
+    static constexpr int QBUF = N == 64 ? 1 : 2;
+    static constexpr int V_OFF = UNITS * UNIT;                   // per team: converted V
     static constexpr int V_BYTES = kUTile * kHeadDim * 2;
-    static constexpr int P_OFF = V_OFF + VBUF * V_BYTES;
+    static constexpr int P_OFF = V_OFF + 2 * V_BYTES;            // per team: P
     static constexpr int P_BYTES = kUTile * N * 2;
-    static constexpr int Q_OFF = P_OFF + 2 * P_BYTES;
+    static constexpr int Q_OFF = P_OFF + 2 * P_BYTES;            // per team: pi(Q)
     static constexpr int Q_BYTES = N * kHeadDim * 2;
-    static constexpr int E_OFF = Q_OFF + 2 * Q_BYTES;            // exponent bytes: STAGES x 2 x 128 x row_e
-    // behind them: factors of the tokens, row data, drafted positions, channel table, references, reduction, barriers
-    static constexpr int SMALL = 8 * kUTile * 4 + N * 16 + 2 * kAttnMaxDraft * 4 + 2 * kHeadDim * 4 + N * 4 * 4 + 8 * N / 2 * 4 + 16 +
-                                 (2 * STAGES + 12) * 8 + 16;
-    __host__ __device__ static int smem_bytes(int row_e) { return E_OFF + STAGES * 2 * kUTile * row_e + SMALL; }
+    static constexpr int E_OFF = Q_OFF + 2 * QBUF * Q_BYTES;     // exponent bytes: UNITS x 128 x row_e
+    // behind them (in floats), per group of four warps: row data, drafted positions and view of two runs, references,
+    // steps, factors, sums, reduction, channel table; then barriers
+    static constexpr int F_RI = 0, F_DPOS = F_RI + 4 * 2 * C * 4, F_VIEW = F_DPOS + 4 * 2 * kAttnMaxDraft,
+                         F_MREF = F_VIEW + 4 * 2 * 8, F_STEP = F_MREF + 4 * C, F_FAC = F_STEP + 4 * C, F_SUM = F_FAC + 4 * C,
+                         F_RED = F_SUM + 4 * C, F_CHAN = F_RED + 4 * 4 * C, F_UNSET = F_CHAN + 4 * kHeadDim, F_END = F_UNSET + 6;
+    static constexpr int SMALL = F_END * 4 + (2 * UNITS + 2 * (4 + 2 * QBUF)) * 8;
+    __host__ __device__ static int smem_bytes(int row_e) { return E_OFF + UNITS * kUTile * row_e + SMALL; }
+    // tensor memory columns of a team: K, S, O
+    static constexpr uint32_t TM_K = 0, TM_S = 64, TM_O = 64 + N, TM_TEAM = 64 + 2 * N, TM_COLS = 2 * TM_TEAM <= 256 ? 256 : 512;
 };
 
 // pi(Q) of one (sequence, kv head, row tile) per block, as the shared-memory image of the B operand: two panels of 64
@@ -109,17 +118,16 @@ __device__ __forceinline__ void umma_exps(const uint8_t* e, int row_e, uint32_t 
         w[1] = w[0];
     }
 }
-// The row's blocks (4 or 8) relative to its largest exponent byte, which is returned (254 at most).
+// The blocks of half a row (slots 64 half ..) relative to the whole row's largest exponent byte, which is returned (254
+// at most).
 template <int P, bool N16>
-__device__ __forceinline__ int umma_row(const uint32_t (&w)[2], UW (&g)[N16 ? 8 : 4]) {
-    int e[N16 ? 8 : 4], top = 0;
+__device__ __forceinline__ int umma_row(const uint32_t (&w)[2], int half, UW (&g)[N16 ? 4 : 2]) {
+    int top = 0;
 #pragma unroll
-    for (int j = 0; j < (N16 ? 8 : 4); ++j) {
-        e[j] = (int)((w[j >> 2] >> (8 * (j & 3))) & 0xffu);
-        top = max(top, e[j]);
-    }
+    for (int j = 0; j < (N16 ? 8 : 4); ++j) top = max(top, (int)((w[j >> 2] >> (8 * (j & 3))) & 0xffu));
+    const uint32_t mine = N16 ? (half ? w[1] : w[0]) : w[0] >> (16 * half);
 #pragma unroll
-    for (int j = 0; j < (N16 ? 8 : 4); ++j) g[j] = umma_weights<P>(top - e[j]);
+    for (int j = 0; j < (N16 ? 4 : 2); ++j) g[j] = umma_weights<P>(top - (int)((mine >> (8 * j)) & 0xffu));
     return min(top, 254);
 }
 // 32 slots (four 16-byte pieces of bf16) of a packed row, from slot 32 i on.
@@ -201,45 +209,42 @@ template <int P, bool N16, int N>
 __global__ void __launch_bounds__(kUThreads, 1) attn_umma(const AttnArgs a, const __grid_constant__ CUtensorMap k_map,
                                                           const __grid_constant__ CUtensorMap v_map) {
     using G_ = UGeo<P, N>;
-    constexpr int D = kHeadDim, ROW_M = G_::ROW_M, STAGES = G_::STAGES, C = N / 2, SWP = 2 * N;      // bytes of a P line
-    constexpr uint32_t TM_S = 0, TM_O = 2 * N, TM_K = 4 * N, TM_COLS = 4 * N + 128 <= 256 ? 256 : 512;
+    constexpr int D = kHeadDim, ROW_M = G_::ROW_M, UNITS = G_::UNITS, QBUF = G_::QBUF, C = G_::C, SWP = 2 * N;      // bytes of a P line
     extern __shared__ __align__(1024) uint8_t smem[];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const int row_e = D / a.fmt.block, exp_half = kUTile * row_e;
-    uint8_t* rest = smem + G_::E_OFF + STAGES * 2 * exp_half;
-    float* kfac = reinterpret_cast<float*>(rest);            // 2^E of the K and V rows of four tiles
-    float* vfac = kfac + 4 * kUTile;
-    RowInfo* ri_all = reinterpret_cast<RowInfo*>(vfac + 4 * kUTile);
-    int* dpos_all = reinterpret_cast<int*>(ri_all + N);
-    int* chan_all = dpos_all + 2 * kAttnMaxDraft;
-    float* mref_all = reinterpret_cast<float*>(chan_all + 2 * D);
-    float* mstep_all = mref_all + N;        // step of a reference change, and the factor of the sums so far
-    float* mfac_all = mstep_all + N;
-    float* lsum_all = mfac_all + N;
-    float* red_all = lsum_all + N;          // [8 warps][C]
-    int* unset_all = reinterpret_cast<int*>(red_all + 8 * C);     // [2] rows that have seen nothing yet, as a bit mask
-    uint32_t* tm_slot = reinterpret_cast<uint32_t*>(unset_all + 2);
-    const uint32_t bars = (smem_u32(tm_slot) + 4 + 7) & ~7u;
-    const uint32_t b_full = bars, b_empty = bars + 8 * STAGES, b_kv = b_empty + 8 * STAGES, b_qk = b_kv + 16, b_p = b_qk + 16,
-                   b_pv = b_p + 16, b_qfull = b_pv + 16, b_qfree = b_qfull + 16;
+    const int row_e = D / a.fmt.block, exp_unit = kUTile * row_e;
+    float* fl = reinterpret_cast<float*>(smem + G_::E_OFF + UNITS * exp_unit);
+    uint32_t* tm_slot = reinterpret_cast<uint32_t*>(fl + G_::F_UNSET + 4);
+    const uint32_t bars = smem_u32(fl + G_::F_END);
+    // ring: full, empty; per team: K ready, S done, P ready, O done, pi(Q) full, pi(Q) free
+    const uint32_t b_full = bars, b_empty = bars + 8 * UNITS, b_team = b_empty + 8 * UNITS;
+    constexpr int TB = 8 * (4 + 2 * QBUF);
+    auto b_k = [&](int t) { return b_team + t * TB; };
+    auto b_s = [&](int t) { return b_team + t * TB + 8; };
+    auto b_p = [&](int t) { return b_team + t * TB + 16; };
+    auto b_o = [&](int t) { return b_team + t * TB + 24; };
+    auto b_qfull = [&](int t, int q) { return b_team + t * TB + 32 + 8 * q; };
+    auto b_qfree = [&](int t, int q) { return b_team + t * TB + 32 + 8 * (QBUF + q); };
 
     if (tid == 0) {
-        for (int s = 0; s < STAGES; ++s) {
+        for (int s = 0; s < UNITS; ++s) {
             mbar_init(b_full + 8 * s, 1);
-            mbar_init(b_empty + 8 * s, 4);
+            mbar_init(b_empty + 8 * s, 8);
         }
-        for (int i = 0; i < 2; ++i) {
-            mbar_init(b_kv + 8 * i, 4);
-            mbar_init(b_qk + 8 * i, 1);
-            mbar_init(b_p + 8 * i, 8);
-            mbar_init(b_pv + 8 * i, 1);
-            mbar_init(b_qfull + 8 * i, 1);
-            mbar_init(b_qfree + 8 * i, 1);
+        for (int t = 0; t < 2; ++t) {
+            mbar_init(b_k(t), 8);
+            mbar_init(b_s(t), 1);
+            mbar_init(b_p(t), 8);
+            mbar_init(b_o(t), 1);
+            for (int q = 0; q < QBUF; ++q) {
+                mbar_init(b_qfull(t, q), 1);
+                mbar_init(b_qfree(t, q), 1);
+            }
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         fence_async_shared();
     }
-    if (warp == 17) tmem_alloc(smem_u32(tm_slot), TM_COLS);
+    if (warp == 17) tmem_alloc(smem_u32(tm_slot), G_::TM_COLS);
     tmem_fence_before();
     __syncthreads();
     tmem_fence_after();
@@ -247,23 +252,35 @@ __global__ void __launch_bounds__(kUThreads, 1) attn_umma(const AttnArgs a, cons
     pdl_wait();       // what umma_prep wrote is read by plain loads below: read-only ones could be moved above this line
 
     const int B = a.fmt.batch, Hkv = a.fmt.n_kv_heads, HR = Hkv * a.n_row_tiles, max_seq = a.fmt.max_seq;
-    const int n_items = a.plan[B] * HR, workers = min(a.workers, n_items), me = blockIdx.x;
-    const int i0 = me < workers ? worker_start(me, n_items, workers) : 0;
-    const int i1 = me < workers ? worker_start(me + 1, n_items, workers) : 0;
-    const int n_mine = i1 - i0;
+    const int n_items = a.plan[B] * HR, workers = min(a.workers, n_items);
+    // team t of this block is worker blockIdx + t * blocks: few tiles are spread over the blocks first
+    auto range = [&](int t, int& first) {
+        const int w = blockIdx.x + t * gridDim.x;
+        first = w < workers ? worker_start(w, n_items, workers) : 0;
+        return w < workers ? worker_start(w + 1, n_items, workers) - first : 0;
+    };
+    int start[2], count[2];
+    count[0] = range(0, start[0]);
+    count[1] = range(1, start[1]);
+    // units of the ring in the order they are filled and drawn: tile s of team 0 (K, V), tile s of team 1, tile s + 1 ..
+    // (a team's count is the other's or one more)
+    auto unit_of = [&](int t, int s) { return 4 * s + (t == 1 && s < count[0] ? 2 : 0); };
     struct Cursor {      // an item: sequence, kv head and row tile (hr), tile k of n
         int b, hr, k, n;
     };
-    auto seek = [&]() {
-        int lo = 0, hi = B - 1;                 // last sequence that begins at or before the item
-        while (lo < hi) {
-            const int mid = (lo + hi + 1) >> 1;
-            if (a.plan[mid] * HR <= i0) lo = mid; else hi = mid - 1;
+    auto seek = [&](int item) {
+        // last sequence that begins at or before the item: 32 looked at per step
+        int last = 0;
+        for (int b0 = 0; b0 < B; b0 += 32) {
+            const bool in = b0 + lane < B && a.plan[b0 + lane] * HR <= item;
+            const uint32_t v = __ballot_sync(0xffffffffu, in);
+            if (v) last = b0 + 31 - __clz(v);
+            if (v != 0xffffffffu) break;
         }
         Cursor c;
-        const int c0 = a.plan[lo], in = i0 - c0 * HR;
-        c.b = lo;
-        c.n = a.plan[lo + 1] - c0;
+        const int c0 = a.plan[last], in = item - c0 * HR;
+        c.b = last;
+        c.n = max(a.plan[last + 1] - c0, 1);
         c.hr = in / c.n;
         c.k = in - c.hr * c.n;
         return c;
@@ -277,60 +294,60 @@ __global__ void __launch_bounds__(kUThreads, 1) attn_umma(const AttnArgs a, cons
         }
     };
     bool dead = false;          // a wait ran out: no more waits, the flag is up, results are void
-    auto wait = [&](uint32_t bar, uint32_t parity) {
-        if (!dead && !mbar_try(bar, parity) && !mbar_wait_bounded(bar, parity)) {
+    auto wait = [&](uint32_t bar, int phase) {
+        if (!dead && !mbar_try(bar, (uint32_t)phase & 1u) && !mbar_wait_bounded(bar, (uint32_t)phase & 1u)) {
             dead = true;
             raise_flag(a.status, KVBFP_FLAG_WAIT_TIMEOUT);
         }
     };
 
-    if (n_mine <= 0) {
+    if (count[0] + count[1] == 0) {
         // nothing to do
     } else if (warp == 16) {
         // ================================================================ copies
+        Cursor c[2] = {seek(start[0]), seek(start[1])};
         if (lane == 0) {
-            Cursor c = seek();
-            SeqView sv = a.views[c.b];
-            bool first = true;
-            int run = 0;
-            for (int i = 0; i < n_mine && !dead; ++i) {
-                if (first) {
-                    const int q = run & 1;
-                    if (run >= 2) wait(b_qfree + 8 * q, (uint32_t)((run >> 1) - 1) & 1u);
-                    mbar_expect_tx(b_qfull + 8 * q, G_::Q_BYTES);
-                    bulk_g2s(smem_u32(smem) + G_::Q_OFF + q * G_::Q_BYTES,
-                             reinterpret_cast<const uint8_t*>(a.qfrag) + ((int64_t)c.b * HR + c.hr) * G_::Q_BYTES, G_::Q_BYTES, b_qfull + 8 * q);
-                    first = false;
-                }
-                const int s = i % STAGES;
-                if (i >= STAGES) wait(b_empty + 8 * s, (uint32_t)(i / STAGES - 1) & 1u);
-                if (dead) break;
-                const int tt = tile_token(sv, c.k, kUTile);
-                const int64_t row0 = ((int64_t)c.b * Hkv + c.hr / a.n_row_tiles) * max_seq + tt;
-                const int rows = min(kUTile, max_seq - tt);           // a multiple of 16
-                const uint32_t dst = smem_u32(smem) + s * G_::MANT, de = smem_u32(smem) + G_::E_OFF + s * 2 * exp_half, br = b_full + 8 * s;
-                const uint32_t mant = (P == 6 ? rows : kUTile) * ROW_M;       // a tiled copy always brings its whole box
-                mbar_expect_tx(br, 2 * mant + 2 * rows * row_e);
-                if (P == 6) {
-                    bulk_g2s(dst, a.k_mant + row0 * ROW_M, mant, br);
-                    bulk_g2s(dst + G_::MANT / 2, a.v_mant + row0 * ROW_M, mant, br);
-                } else {
-                    const int y = (int)(P == 4 ? row0 >> 1 : row0);
-                    tensor_g2s_2d(dst, &k_map, 0, y, br);
-                    tensor_g2s_2d(dst + G_::MANT / 2, &v_map, 0, y, br);
-                }
-                bulk_g2s(de, a.k_exp + row0 * row_e, rows * row_e, br);
-                bulk_g2s(de + exp_half, a.v_exp + row0 * row_e, rows * row_e, br);
-                if (++c.k == c.n) {
-                    const int b = c.b;
-                    next_pair(c);
-                    if (c.b != b && c.b < B) sv = a.views[c.b];
-                    first = true;
-                    ++run;
+            bool first[2] = {true, true};
+            int run[2] = {0, 0}, issued = 0;
+            for (int s = 0; s < max(count[0], count[1]) && !dead; ++s) {
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    if (s >= count[t] || dead) continue;
+                    Cursor& x = c[t];
+                    if (first[t]) {
+                        const int q = run[t] % QBUF, n = run[t] / QBUF;
+                        if (n > 0) wait(b_qfree(t, q), n - 1);
+                        if (dead) break;
+                        mbar_expect_tx(b_qfull(t, q), G_::Q_BYTES);
+                        bulk_g2s(smem_u32(smem) + G_::Q_OFF + (t * QBUF + q) * G_::Q_BYTES,
+                                 reinterpret_cast<const uint8_t*>(a.qfrag) + ((int64_t)x.b * HR + x.hr) * G_::Q_BYTES, G_::Q_BYTES, b_qfull(t, q));
+                        first[t] = false;
+                    }
+                    const SeqView sv = a.views[x.b];
+                    const int tt = tile_token(sv, x.k, kUTile);
+                    const int64_t row0 = ((int64_t)x.b * Hkv + x.hr / a.n_row_tiles) * max_seq + tt;
+                    const int rows = min(kUTile, max_seq - tt);           // a multiple of 16
+                    const uint32_t mant = (P == 6 ? rows : kUTile) * ROW_M;       // a tiled copy always brings its whole box
+#pragma unroll
+                    for (int kv = 0; kv < 2; ++kv, ++issued) {
+                        const int u = issued % UNITS;
+                        if (issued >= UNITS) wait(b_empty + 8 * u, issued / UNITS - 1);
+                        if (dead) break;
+                        const uint32_t dst = smem_u32(smem) + u * G_::UNIT, de = smem_u32(smem) + G_::E_OFF + u * exp_unit, br = b_full + 8 * u;
+                        mbar_expect_tx(br, mant + rows * row_e);
+                        if (P == 6) bulk_g2s(dst, (kv ? a.v_mant : a.k_mant) + row0 * ROW_M, mant, br);
+                        else tensor_g2s_2d(dst, kv ? &v_map : &k_map, 0, (int)(P == 4 ? row0 >> 1 : row0), br);
+                        bulk_g2s(de, (kv ? a.v_exp : a.k_exp) + row0 * row_e, rows * row_e, br);
+                    }
+                    if (++x.k == x.n) {
+                        next_pair(x);
+                        first[t] = true;
+                        ++run[t];
+                    }
                 }
             }
             if (dead)       // give the copies still in flight a bounded chance to land before the shared memory is released
-                for (int s = 0; s < STAGES; ++s) {
+                for (int s = 0; s < UNITS; ++s) {
                     (void)mbar_wait_bounded(b_full + 8 * s, 0);
                     (void)mbar_wait_bounded(b_full + 8 * s, 1);
                 }
@@ -339,151 +356,165 @@ __global__ void __launch_bounds__(kUThreads, 1) attn_umma(const AttnArgs a, cons
         // ================================================================ matrix instructions
         constexpr uint32_t id_s = umma_idesc(128, N, false, false), id_o = umma_idesc(128, N, true, true);
         const uint32_t tmu = __shfl_sync(0xffffffffu, tm, 0), base = smem_u32(smem);
-        Cursor c = seek();
-        int run = 0, vslot = 0;
-        bool first = true, o_first = true;       // first tile of its run: the tile whose S comes next / whose O comes next
-        auto product_o = [&](int i) {
-            const int b = i & 1;
-            wait(b_p + 8 * b, (uint32_t)(i >> 1) & 1u);
-            __syncwarp();
-            tmem_fence_after();
-            const uint64_t v = umma_desc<128>(base + G_::V_OFF + vslot * G_::V_BYTES, kUTile * 128, 1024);
-            const uint64_t p = umma_desc<SWP>(base + G_::P_OFF + b * G_::P_BYTES, 16, 8 * SWP);
+        Cursor c[2] = {seek(start[0]), seek(start[1])};
+        int run[2] = {0, 0}, ns[2] = {0, 0}, no[2] = {0, 0}, idle = 0;
+        bool first[2] = {true, true}, fresh[2] = {true, true};        // the next tile begins a run: S, O
+        auto ready = [&](uint32_t bar, int phase) { return __all_sync(0xffffffffu, mbar_try(bar, (uint32_t)phase & 1u)); };      // alike in all lanes
+        // S of a tile needs its K rows (and, at the start of a run, pi(Q)), O its V rows and P.  A bounded number of looks
+        // without progress ends it.
+        while (no[0] < count[0] || no[1] < count[1]) {
+            bool moved = false;
 #pragma unroll
-            for (int ks = 0; ks < kUTile / 16; ++ks)
-                umma_ss(tmu + TM_O, v + ks * (2048 >> 4), p + ks * (16 * SWP >> 4), id_o, ks > 0 || !o_first);
-            umma_commit(b_pv + 8 * b);
-            vslot = vslot == G_::VBUF - 1 ? 0 : vslot + 1;
-        };
-        for (int i = 0; i < n_mine; ++i) {
-            const int b = i & 1, q = run & 1;
-            wait(b_kv + 8 * b, (uint32_t)(i >> 1) & 1u);
-            if (first) wait(b_qfull + 8 * q, (uint32_t)(run >> 1) & 1u);
-            __syncwarp();
-            tmem_fence_after();
-            const uint64_t qd = umma_desc<128>(base + G_::Q_OFF + q * G_::Q_BYTES, 16, 1024);
+            for (int t = 0; t < 2; ++t) {
+                const uint32_t tmt = tmu + t * G_::TM_TEAM;
+                if (no[t] == ns[t]) {
+                    const int q = run[t] % QBUF;
+                    if (ns[t] < count[t] && ready(b_k(t), ns[t]) && (!first[t] || ready(b_qfull(t, q), run[t] / QBUF))) {
+                        tmem_fence_after();
+                        const uint64_t qd = umma_desc<128>(base + G_::Q_OFF + (t * QBUF + q) * G_::Q_BYTES, 16, 1024);
 #pragma unroll
-            for (int ks = 0; ks < 8; ++ks)
-                umma_ts(tmu + TM_S + b * N, tmu + TM_K + b * 64 + ks * 8, qd + (((ks >> 2) * (N * 128) + (ks & 3) * 32) >> 4), id_s, ks > 0);
-            umma_commit(b_qk + 8 * b);
-            const bool was_first = first;
-            first = false;
-            if (++c.k == c.n) {
-                umma_commit(b_qfree + 8 * q);
-                next_pair(c);
-                first = true;
-                ++run;
+                        for (int ks = 0; ks < 8; ++ks)
+                            umma_ts(tmt + G_::TM_S, tmt + G_::TM_K + ks * 8, qd + (((ks >> 2) * (N * 128) + (ks & 3) * 32) >> 4), id_s, ks > 0);
+                        umma_commit(b_s(t));
+                        fresh[t] = first[t];
+                        first[t] = false;
+                        if (++c[t].k == c[t].n) {
+                            umma_commit(b_qfree(t, q));
+                            next_pair(c[t]);
+                            first[t] = true;
+                            ++run[t];
+                        }
+                        ++ns[t];
+                        moved = true;
+                    }
+                } else if (ready(b_p(t), no[t])) {
+                    tmem_fence_after();
+                    const uint64_t v = umma_desc<128>(base + G_::V_OFF + t * G_::V_BYTES, kUTile * 128, 1024);
+                    const uint64_t p = umma_desc<SWP>(base + G_::P_OFF + t * G_::P_BYTES, 16, 8 * SWP);
+#pragma unroll
+                    for (int ks = 0; ks < kUTile / 16; ++ks)
+                        umma_ss(tmt + G_::TM_O, v + ks * (2048 >> 4), p + ks * (16 * SWP >> 4), id_o, ks > 0 || !fresh[t]);
+                    umma_commit(b_o(t));
+                    ++no[t];
+                    moved = true;
+                }
             }
-            if (i > 0) product_o(i - 1);
-            o_first = was_first;
+            if (moved) {
+                idle = 0;
+            } else if (++idle > (1 << 24)) {
+                dead = true;
+                if (lane == 0) raise_flag(a.status, KVBFP_FLAG_WAIT_TIMEOUT);
+                break;
+            }
         }
-        product_o(n_mine - 1);
-        if (__any_sync(0xffffffffu, dead)) {       // let what was issued come to its end before the tensor memory goes
-            umma_commit(b_qfree);
-            (void)mbar_wait_bounded(b_qfree, 0);
-            (void)mbar_wait_bounded(b_qfree, 1);
-        }
-    } else if (warp >= 8) {
-        // ================================================================ conversion: a thread per token
-        const int grp = (warp - 8) >> 2, row = tid & 127;
-        const uint32_t tk = tm + TM_K + grp * 64 + ((uint32_t)(warp & 3) << 21);        // lane field: 32 * quarter << 16
-        int vslot = grp;
-        for (int i = grp; i < n_mine; i += 2) {
-            const int s = i % STAGES;
-            wait(b_full + 8 * s, (uint32_t)(i / STAGES) & 1u);
-            const uint8_t* km = smem + s * G_::MANT;
-            const uint8_t* ke = smem + G_::E_OFF + s * 2 * exp_half + row * row_e;
-            if (i >= 2) {
-                wait(b_qk + 8 * grp, (uint32_t)((i >> 1) - 1) & 1u);            // K of the tile before is used up
-                tmem_fence_after();
-            }
-            __syncwarp();
-            UW g[N16 ? 8 : 4];
-            uint32_t ew[2];
-            umma_exps<N16>(ke, row_e, ew);
-            int top = umma_row<P, N16>(ew, g);
-            kfac[(i & 3) * kUTile + row] = __uint_as_float((uint32_t)top << 23);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                uint32_t r[16];
-                convert32<P>(km, row, j, g[N16 ? 2 * j : j], g[N16 ? 2 * j + 1 : j], r);
-                tmem_st<16>(tk + 16 * j, r);
-            }
-            umma_exps<N16>(ke + exp_half, row_e, ew);
-            top = umma_row<P, N16>(ew, g);
-            vfac[(i & 3) * kUTile + row] = __uint_as_float((uint32_t)max(top - 9, 0) << 23);
-            // the buffer's last tile was i - VBUF
-            if (i >= G_::VBUF) wait(b_pv + 8 * ((i - G_::VBUF) & 1), (uint32_t)((i - G_::VBUF) >> 1) & 1u);
-            uint8_t* vb = smem + G_::V_OFF + vslot * G_::V_BYTES + row * 128;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                uint32_t r[16];
-                convert32<P>(km + G_::MANT / 2, row, j, g[N16 ? 2 * j : j], g[N16 ? 2 * j + 1 : j], r);
-                uint8_t* to = vb + (j >> 1) * (kUTile * 128);
-#pragma unroll
-                for (int x = 0; x < 4; ++x)       // 16-byte pieces 4 j + x of the row: panel of 64 slots, swizzled
-                    *reinterpret_cast<uint4*>(to + (((4 * (j & 1) + x) ^ (row & 7)) << 4)) = make_uint4(r[4 * x], r[4 * x + 1], r[4 * x + 2], r[4 * x + 3]);
-            }
-            vslot = (vslot + 2) % G_::VBUF;
-            __syncwarp();
-            tmem_wait_st();
-            fence_async_shared();
-            tmem_fence_before();
-            __syncwarp();
-            if (lane == 0) {
-                mbar_arrive(b_kv + 8 * grp);
-                mbar_arrive(b_empty + 8 * s);
-            }
+        if (dead) {       // let what was issued come to its end before the tensor memory goes
+            umma_commit(b_qfree(0, 0));
+            (void)mbar_wait_bounded(b_qfree(0, 0), 0);
+            (void)mbar_wait_bounded(b_qfree(0, 0), 1);
         }
     } else {
-        // ================================================================ softmax: a thread per token, C of the rows
-        const int wg = warp >> 2, m_pos = tid & 127, w4 = warp & 3, bar_id = 1 + wg;
-        const uint32_t quarter = (uint32_t)w4 << 21;
-        RowInfo* ri = ri_all + wg * C;
-        int* dpos = dpos_all + wg * kAttnMaxDraft;
-        int* chan = chan_all + wg * D;
-        float *mref = mref_all + wg * C, *mstep = mstep_all + wg * C, *mfac = mfac_all + wg * C, *lsum = lsum_all + wg * C, *red = red_all + wg * 4 * C;
-        int* unset = unset_all + wg;
+        // ================================================================ a team: two threads per token
+        const int team = warp >> 3, wg = warp >> 2, half = wg & 1, m_pos = tid & 127, w4 = warp & 3, bar_id = 1 + wg;
+        const uint32_t tmt = tm + team * G_::TM_TEAM + ((uint32_t)w4 << 21);        // lane field: 32 * quarter << 16
+        float *mref = fl + G_::F_MREF + wg * C, *mstep = fl + G_::F_STEP + wg * C, *mfac = fl + G_::F_FAC + wg * C,
+              *lsum = fl + G_::F_SUM + wg * C, *red = fl + G_::F_RED + wg * 4 * C;
+        int* chan = reinterpret_cast<int*>(fl + G_::F_CHAN) + wg * D;
+        int* unset = reinterpret_cast<int*>(fl + G_::F_UNSET) + wg;         // rows that have seen nothing yet, as a bit mask
+        uint8_t* vline = smem + G_::V_OFF + team * G_::V_BYTES + half * (kUTile * 128) + m_pos * 128;       // half a row: a panel of 64 slots
+        const int n_mine = team ? count[1] : count[0], me = blockIdx.x + team * gridDim.x;
         const int R = a.n_draft * a.group;
         const float up = a.scale * (P == 4 ? 64.f : P == 6 ? 16.f : 4.f), to_log2 = 1.4426950408889634f;      // 2^8 2^-(P-2)
         const float cap_in = a.softcap > 0.f ? up / a.softcap * 2.8853900817779268f : 0.f;
-        // the column a lane ends up with: its upper log2(C) lane bits
+        // the column a lane ends up with after across_lanes: its upper log2(C) lane bits
         const int my_col = C == 32 ? lane : C == 16 ? lane >> 1 : lane >> 2;
         const bool my_first = C == 32 || (C == 16 ? (lane & 1) == 0 : (lane & 3) == 0);
-
-        Cursor c = seek();
-        int it = 0;
-        while (it < n_mine) {
-            const int b = c.b, hk = c.hr / a.n_row_tiles, rt = c.hr - hk * a.n_row_tiles;
-            const int k0 = c.k, k1 = min(c.n, k0 + n_mine - it), row0 = rt * N + wg * C;
-            const SeqView sv = a.views[b];
-            named_sync(bar_id, 128);
-            if (m_pos < C) {
-                ri[m_pos] = a.rows[((int64_t)b * HR + c.hr) * N + wg * C + m_pos];
-                mref[m_pos] = 0.f;
+        // row data, drafted positions and view of a run, asynchronously into the buffers of its parity
+        auto fetch = [&](const Cursor& c, int par) {
+            if (c.b < B) {
+                if (m_pos < C)
+                    cp_async16(smem_u32(fl + G_::F_RI + ((wg * 2 + par) * C + m_pos) * 4), a.rows + ((int64_t)c.b * HR + c.hr) * N + half * C + m_pos);
+                else if (m_pos >= 64 && m_pos < 64 + kAttnMaxDraft / 4 && a.tree)
+                    cp_async16(smem_u32(fl + G_::F_DPOS + (wg * 2 + par) * kAttnMaxDraft + (m_pos - 64) * 4), a.dpos + c.b * kAttnMaxDraft + (m_pos - 64) * 4);
+                else if (m_pos >= 96 && m_pos < 98)
+                    cp_async16(smem_u32(fl + G_::F_VIEW + (wg * 2 + par) * 8 + (m_pos - 96) * 4), reinterpret_cast<const int*>(a.views + c.b) + (m_pos - 96) * 4);
             }
+            asm volatile("cp.async.commit_group;" ::: "memory");
+        };
+        // 64 slots of a unit's row to `put`, sixteen registers (32 slots) at a time; returns the row's largest exponent
+        auto convert = [&](int u, auto put) {
+            const uint8_t* tile = smem + u * G_::UNIT;
+            uint32_t ew[2];
+            umma_exps<N16>(smem + G_::E_OFF + u * exp_unit + m_pos * row_e, row_e, ew);
+            UW g[N16 ? 4 : 2];
+            const int top = umma_row<P, N16>(ew, half, g);
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                uint32_t r[16];
+                convert32<P>(tile, m_pos, 2 * half + j, g[N16 ? 2 * j : j], g[N16 ? 2 * j + 1 : j], r);
+                put(j, r);
+            }
+            return top;
+        };
+
+        Cursor c = seek(team ? start[1] : start[0]), cn = c;
+        fetch(c, 0);
+        int it = 0, run = 0;
+        while (it < n_mine) {
+            const int b = c.b, hk = c.hr / a.n_row_tiles, rt = c.hr - hk * a.n_row_tiles, par = run & 1;
+            const int k0 = c.k, k1 = min(c.n, k0 + n_mine - it), row0 = rt * N + half * C;
+            cn = c;
+            next_pair(cn);
+            asm volatile("cp.async.wait_group 0;" ::: "memory");
+            if (m_pos < C) mref[m_pos] = 0.f;
             if (m_pos == 0) *unset = (int)(C == 32 ? 0xffffffffu : (1u << C) - 1u);
-            if (a.tree && m_pos < kAttnMaxDraft) dpos[m_pos] = a.dpos[b * kAttnMaxDraft + m_pos];
             if (a.inv_perm_v) chan[a.inv_perm_v[hk * D + m_pos] & (D - 1)] = m_pos;
             named_sync(bar_id, 128);
+            if (it + k1 - k0 < n_mine) fetch(cn, par ^ 1);
+            const RowInfo* ri = reinterpret_cast<const RowInfo*>(fl + G_::F_RI) + (wg * 2 + par) * C;
+            const int* dpos = reinterpret_cast<const int*>(fl + G_::F_DPOS) + (wg * 2 + par) * kAttnMaxDraft;
+            const SeqView sv = *reinterpret_cast<const SeqView*>(fl + G_::F_VIEW + (wg * 2 + par) * 8);
+            const uint32_t tm_o = tmt + G_::TM_O + half * C;
             int clear_lo = sv.first;      // tokens [clear_lo, ctx) and [0, pf) are visible to every row
             if (a.window > 0) clear_lo = max(clear_lo, sv.ctx + (a.tree ? a.n_draft - 1 : -1) - a.window + 1);
             float l[C];
 #pragma unroll
             for (int j = 0; j < C; ++j) l[j] = 0.f;
             for (int k = k0; k < k1; ++k, ++it) {
-                const int s = it & 1, tt = tile_token(sv, k, kUTile), tok = tt + m_pos;
-                wait(b_qk + 8 * s, (uint32_t)(it >> 1) & 1u);
+                const int uk = unit_of(team, it), uv = uk + 1;
+                // ---- K: the tensor memory it goes to was read by the product of the tile before, which this thread has waited for
+                wait(b_full + 8 * (uk % UNITS), uk / UNITS);
+                __syncwarp();
+                const int k_top = convert(uk % UNITS, [&](int j, const uint32_t (&r)[16]) { tmem_st<16>(tmt + G_::TM_K + half * 32 + 16 * j, r); });
+                tmem_wait_st();
+                tmem_fence_before();
+                __syncwarp();
+                if (lane == 0) {
+                    mbar_arrive(b_k(team));
+                    mbar_arrive(b_empty + 8 * (uk % UNITS));
+                }
+                // ---- V, while the tensor cores are on S
+                wait(b_full + 8 * (uv % UNITS), uv / UNITS);
+                if (it > 0) wait(b_o(team), it - 1);          // the product of the tile before has read V and P
+                const int v_top = convert(uv % UNITS, [&](int j, const uint32_t (&r)[16]) {
+#pragma unroll
+                    for (int x = 0; x < 4; ++x)       // 16-byte pieces 4 j + x, swizzled
+                        *reinterpret_cast<uint4*>(vline + (((4 * j + x) ^ (m_pos & 7)) << 4)) = make_uint4(r[4 * x], r[4 * x + 1], r[4 * x + 2], r[4 * x + 3]);
+                });
+                __syncwarp();
+                if (lane == 0) mbar_arrive(b_empty + 8 * (uv % UNITS));
+                // ---- scores
+                const int tt = tile_token(sv, k, kUTile), tok = tt + m_pos;
+                const float kf = __uint_as_float((uint32_t)k_top << 23), vf = __uint_as_float((uint32_t)max(v_top - 9, 0) << 23);
+                wait(b_s(team), it);
                 __syncwarp();
                 tmem_fence_after();
                 uint32_t raw[C];
-                tmem_ld<C>(tm + TM_S + s * N + wg * C + quarter, raw);
+                tmem_ld<C>(tmt + G_::TM_S + half * C, raw);
                 tmem_wait_ld(raw);
                 float y[C];
 #pragma unroll
                 for (int j = 0; j < C; ++j) y[j] = __uint_as_float(raw[j]);
                 // ---- cap, bias, masks: y * mul in log2 units
-                const float kf = kfac[(it & 3) * kUTile + m_pos];
                 float mul = up * to_log2 * kf;
                 if (a.softcap > 0.f) {
                     mul = a.softcap * to_log2;
@@ -529,13 +560,12 @@ __global__ void __launch_bounds__(kUThreads, 1) attn_umma(const AttnArgs a, cons
                     if (my_first) red[w4 * C + my_col] = mine;
                     named_sync(bar_id, 128);
                     if (m_pos < 32) {
-                        float step = 0.f;
                         bool none = false;
                         if (lane < C) {
                             const float x = fmaxf(fmaxf(red[lane], red[C + lane]), fmaxf(red[2 * C + lane], red[3 * C + lane]));
                             const bool is_unset = (*unset >> lane) & 1;
                             none = is_unset && x == -INFINITY;
-                            step = none ? 0.f : (is_unset ? x : fmaxf(x, 0.f));
+                            const float step = none ? 0.f : (is_unset ? x : fmaxf(x, 0.f));
                             mstep[lane] = step;
                             mfac[lane] = is_unset ? 1.f : ex2_approx(-step);      // (a row that has seen nothing has sums 0)
                             mref[lane] += step;
@@ -549,27 +579,22 @@ __global__ void __launch_bounds__(kUThreads, 1) attn_umma(const AttnArgs a, cons
                         y[j] -= mstep[j];
                         l[j] *= mfac[j];
                     }
-                    if (k > k0) {
-                        wait(b_pv + 8 * (s ^ 1), (uint32_t)((it - 1) >> 1) & 1u);
-                        __syncwarp();
+                    if (k > k0) {          // (the product of the tile before is done: waited for above)
                         tmem_fence_after();
 #pragma unroll
                         for (int j = 0; j < C; j += 8) {
                             uint32_t o[8];
-                            const uint32_t at = tm + TM_O + wg * C + j + quarter;
-                            tmem_ld<8>(at, o);
+                            tmem_ld<8>(tm_o + j, o);
                             tmem_wait_ld(o);
 #pragma unroll
                             for (int e = 0; e < 8; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * mfac[j + e]);
-                            tmem_st<8>(at, o);
+                            tmem_st<8>(tm_o + j, o);
                         }
                         tmem_wait_st();
                     }
                 }
-                // ---- P: weights of this token, bf16, a line of 2 N bytes
-                if (it >= 2) wait(b_pv + 8 * s, (uint32_t)((it >> 1) - 1) & 1u);
-                uint8_t* pb = smem + G_::P_OFF + s * G_::P_BYTES;
-                const float vf = vfac[(it & 3) * kUTile + m_pos];
+                // ---- P: weights of this token times its V row's 2^E, bf16, a line of 2 N bytes
+                uint8_t* pb = smem + G_::P_OFF + team * G_::P_BYTES;
 #pragma unroll
                 for (int j = 0; j < C; j += 8) {
                     uint32_t w[4];
@@ -580,74 +605,75 @@ __global__ void __launch_bounds__(kUThreads, 1) attn_umma(const AttnArgs a, cons
                         l[j + 2 * e + 1] += p1;
                         w[e] = pack_bf16x2_rn(p0 * vf, p1 * vf);
                     }
-                    const uint32_t off = m_pos * SWP + (wg * C + j) * 2;
+                    const uint32_t off = m_pos * SWP + (half * C + j) * 2;
                     *reinterpret_cast<uint4*>(pb + (off ^ (((off >> 7) & (SWP / 16 - 1)) << 4))) = make_uint4(w[0], w[1], w[2], w[3]);
                 }
                 fence_async_shared();
                 tmem_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(b_p + 8 * s);
+                if (lane == 0) mbar_arrive(b_p(team));
             }
             // ---- the run's result: this thread holds slot umma_slot(m_pos) of C rows
             {
                 const float mine = across_lanes<C, false>(l, lane);
                 if (my_first) red[w4 * C + my_col] = mine;
             }
-            wait(b_pv + 8 * ((it - 1) & 1), (uint32_t)((it - 1) >> 1) & 1u);
-            __syncwarp();
-            tmem_fence_after();
             named_sync(bar_id, 128);
             const bool whole = k0 == 0 && k1 == c.n;
             const int slot = umma_slot<P>(m_pos);
-            float* part = a.partials + ((int64_t)(2 * me + (k0 == 0 ? 1 : 0)) * a.part_rows + wg * C) * kAttnPart;
+            float* part = a.partials + ((int64_t)(2 * me + (k0 == 0 ? 1 : 0)) * a.part_rows + half * C) * kAttnPart;
             if (m_pos < C) {
                 const int row = row0 + m_pos;
                 const float ls = red[m_pos] + red[C + m_pos] + red[2 * C + m_pos] + red[3 * C + m_pos];
                 const float m = ((*unset >> m_pos) & 1) ? -3.4028235e38f : mref[m_pos];
                 lsum[m_pos] = ls;
                 if (row < R) {
-                    const int i = row / a.group, hq = hk * a.group + row - i * a.group;
                     if (!whole) {
                         part[m_pos * kAttnPart + D] = m;
                         part[m_pos * kAttnPart + D + 1] = ls;
                     } else if (a.lse) {
+                        const int i = row / a.group, hq = hk * a.group + row - i * a.group;
                         a.lse[(int64_t)b * a.n_q_heads + hq] = ls > 0.f ? m + log2f(ls) : (ls == 0.f ? INFINITY : ls);
                     }
                 }
             }
+            wait(b_o(team), it - 1);
+            __syncwarp();
+            tmem_fence_after();
             named_sync(bar_id, 128);
             const int ch = a.inv_perm_v ? chan[slot] : slot;
-#pragma unroll
+#pragma unroll 1
             for (int j = 0; j < C; j += 8) {
                 uint32_t o[8];
-                tmem_ld<8>(tm + TM_O + wg * C + j + quarter, o);
+                tmem_ld<8>(tm_o + j, o);
                 tmem_wait_ld(o);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     const int row = row0 + j + e;
-                    if (row < R) {
-                        if (whole) {
-                            const int i = row / a.group, hq = hk * a.group + row - i * a.group;
-                            const float ls = lsum[j + e];
-                            const bool live = (!a.tree || i < sv.nd) && ls != 0.f;
-                            const float v = live ? __uint_as_float(o[e]) * (a.out_up / ls) : 0.f;
-                            static_cast<__nv_bfloat16*>(a.out)[(((int64_t)b * a.n_draft + i) * a.n_q_heads + hq) * D + ch] = __float2bfloat16_rn(v);
-                        } else {
-                            part[(j + e) * kAttnPart + slot] = __uint_as_float(o[e]);
-                        }
+                    if (row >= R) break;
+                    if (whole) {
+                        const int i = row / a.group, hq = hk * a.group + row - i * a.group;
+                        const float ls = lsum[j + e];
+                        const bool live = (!a.tree || i < sv.nd) && ls != 0.f;
+                        static_cast<__nv_bfloat16*>(a.out)[(((int64_t)b * a.n_draft + i) * a.n_q_heads + hq) * D + ch] =
+                            __float2bfloat16_rn(live ? __uint_as_float(o[e]) * (a.out_up / ls) : 0.f);
+                    } else {
+                        part[(j + e) * kAttnPart + slot] = __uint_as_float(o[e]);
                     }
                 }
             }
             tmem_fence_before();
             c.k = k1;
-            if (k1 == c.n) next_pair(c);
+            if (k1 == c.n) c = cn;
+            ++run;
         }
+        asm volatile("cp.async.wait_group 0;" ::: "memory");
     }
     __syncwarp();
     tmem_fence_before();
     __syncthreads();
     tmem_fence_after();
-    if (warp == 17) tmem_dealloc(tm, TM_COLS);
+    if (warp == 17) tmem_dealloc(tm, G_::TM_COLS);
     pdl_trigger();
 }
 

@@ -111,6 +111,10 @@ __device__ __forceinline__ void mbar_arrive(uint32_t bar) {
 }
 // Writes of this thread to shared memory become visible to the matrix instructions (and bulk copies).
 __device__ __forceinline__ void fence_async_shared() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+// 16 bytes from global to shared memory without passing through registers; waited for with cp.async.wait_group.
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
 // Barrier of `threads` threads (whole warps), one of 1..15; true if any of them says so.
 __device__ __forceinline__ void named_sync(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
 __device__ __forceinline__ bool named_any(int id, int threads, bool x) {
