@@ -167,7 +167,7 @@ __global__ void __launch_bounds__(128) attn_mass(const AttnArgs a) {
 // Query rows per work item: up to 64 bf16 rows of a kv head share its tiles; fp32 queries take 16 at a time (their three
 // bf16 terms fill the registers of the warp-level kernel).
 inline int rows_tile_for(int rows, bool bf16) { return !bf16 || rows <= 16 ? 16 : rows <= 32 ? 32 : 64; }
-inline int max_workers(bool bf16) { return bf16 ? 2 * 160 : kAttnMaxBlocks * kAttnWarps; }
+inline int max_workers(bool bf16) { return bf16 ? 3 * 160 : kAttnMaxBlocks * kAttnWarps; }
 
 inline size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
 
@@ -278,7 +278,7 @@ kvbfp_status attn_common(const AttnCall& c) {
     a.out_up = bf16 ? (float)(1 << (19 - f.mant_bits)) : kValueUp;      // attn_umma: 2^(17 - (p - 2))
     const int64_t most = (int64_t)f.batch * f.n_kv_heads * n_row_tiles * (f.max_seq / shape.tile + 2);    // tiles at the longest
     int64_t grid = (int64_t)n_sm * shape.blocks_per_sm;
-    const int per_block = bf16 ? 2 : kAttnWarps;
+    const int per_block = bf16 ? attn_teams(f.mant_bits, rows_tile) : kAttnWarps;      // teams or warps
     if (grid * per_block > max_workers(bf16)) grid = max_workers(bf16) / per_block;
     if (grid > most) grid = most;
     a.workers = (int)grid * per_block;

@@ -8,16 +8,17 @@
 // cycles per product, so what is left to do per cached element is its conversion, and that is done once for all rows
 // (the warp-level kernel converts per 16 rows and its matrix instructions run at a third of the rate).
 //
-// One persistent thread block per SM, tiles of 128 tokens.  Two teams of eight warps, each a worker with a contiguous
-// range of tiles of its own (attn.cuh); two threads per token:
-//   K rows converted to tensor memory (the A operand of the first product), half a row a thread
+// One persistent thread block per SM, tiles of 128 tokens.  Teams of warps, each a worker with a contiguous range of
+// tiles of its own (attn.cuh), a thread per token (three teams of four warps: 4-bit
+// rows, up to 32 query rows) or two (two teams of eight: what shared memory holds of wider rows):
+//   K rows converted to tensor memory (the A operand of the first product)
 //   V rows converted to shared memory (the A operand of the second, slots contiguous) while the first product runs
-//   scores from tensor memory, half of the query rows a thread: masks, running maximum, P to shared memory
+//   scores from tensor memory: masks, running maximum, P to shared memory
 //   at the end of a run O^T from tensor memory to the result or a partial
-// While one team waits (for a product, a barrier, a copy) the other works.  Warp 16 copies packed tiles into a ring of
-// units that both teams draw from in turn and pi(Q) of the runs, warp 17 issues the matrix instructions of both.
-// (Groups of their own for conversion and softmax, with two to three tiles between them, took twice as long: four warps
-// a phase are slow and the buffers between the phases were what everything waited for.)
+// While one team waits (for a product, a barrier, a copy) the others work.  A warp per team issues its matrix
+// instructions, one warp copies packed tiles into a ring of units that the teams draw from in turn and pi(Q) of the runs.
+// (Groups of their own for conversion and softmax, with two to three tiles between them, took twice as long: the buffers
+// between the phases were what everything waited for.)
 // Cached values are converted relative to their row's largest exponent (see below); magnitudes of 2^118 and above are
 // outside the range.
 // The row maximum runs across threads here, so it is only taken when a score passes the reference by 8 (a factor 2^8),
@@ -34,7 +35,6 @@ namespace kvbfp {
 namespace {
 
 constexpr int kUTile = 128;
-constexpr int kUThreads = 18 * 32;
 
 // Slot at position `m` of a converted row (the order the fields unpack in); K and V alike.
 template <int P>
@@ -46,26 +46,30 @@ __device__ __forceinline__ int umma_slot(int m) {
 template <int P, int N>
 struct UGeo {
     static constexpr int ROW_M = kHeadDim * P / 8;
-    static constexpr int C = N / 2;                              // query rows of a thread
+    static constexpr int TEAMS = attn_teams(P, N);
+    static constexpr int H = TEAMS == 3 ? 1 : 2;                 // threads per token
+    static constexpr int WGS = TEAMS * H;                        // groups of four warps
+    static constexpr int THREADS = (WGS * 4 + TEAMS + 1) * 32;
+    static constexpr int C = N / H;                              // query rows of a thread
     static constexpr int UNIT = kUTile * ROW_M;                  // a tile's K or V rows
-    static constexpr int UNITS = P == 4 ? (N == 64 ? 9 : N == 32 ? 11 : 12) : P == 6 ? (N == 64 ? 6 : N == 32 ? 8 : 10) : (N == 64 ? 5 : N == 32 ? 6 : 7);
-    static constexpr int QBUF = N == 64 ? 1 : 2;
+    static constexpr int UNITS = P == 4 ? (N == 32 ? 8 : 9) : P == 6 ? (N == 64 ? 6 : 8) : (N == 64 ? 5 : 6);
+    static constexpr int QBUF = N == 16 ? 2 : 1;
     static constexpr int V_OFF = UNITS * UNIT;                   // per team: converted V
     static constexpr int V_BYTES = kUTile * kHeadDim * 2;
-    static constexpr int P_OFF = V_OFF + 2 * V_BYTES;            // per team: P
+    static constexpr int P_OFF = V_OFF + TEAMS * V_BYTES;        // per team: P
     static constexpr int P_BYTES = kUTile * N * 2;
-    static constexpr int Q_OFF = P_OFF + 2 * P_BYTES;            // per team: pi(Q)
+    static constexpr int Q_OFF = P_OFF + TEAMS * P_BYTES;        // per team: pi(Q)
     static constexpr int Q_BYTES = N * kHeadDim * 2;
-    static constexpr int E_OFF = Q_OFF + 2 * QBUF * Q_BYTES;     // exponent bytes: UNITS x 128 x row_e
+    static constexpr int E_OFF = Q_OFF + TEAMS * QBUF * Q_BYTES; // exponent bytes: UNITS x 128 x row_e
     // behind them (in floats), per group of four warps: row data, drafted positions and view of two runs, references,
     // steps, factors, sums, reduction, channel table; then barriers
-    static constexpr int F_RI = 0, F_DPOS = F_RI + 4 * 2 * C * 4, F_VIEW = F_DPOS + 4 * 2 * kAttnMaxDraft,
-                         F_MREF = F_VIEW + 4 * 2 * 8, F_STEP = F_MREF + 4 * C, F_FAC = F_STEP + 4 * C, F_SUM = F_FAC + 4 * C,
-                         F_RED = F_SUM + 4 * C, F_CHAN = F_RED + 4 * 4 * C, F_UNSET = F_CHAN + 4 * kHeadDim, F_END = F_UNSET + 6;
-    static constexpr int SMALL = F_END * 4 + (2 * UNITS + 2 * (4 + 2 * QBUF)) * 8;
+    static constexpr int F_RI = 0, F_DPOS = F_RI + WGS * 2 * C * 4, F_VIEW = F_DPOS + WGS * 2 * kAttnMaxDraft,
+                         F_MREF = F_VIEW + WGS * 2 * 8, F_STEP = F_MREF + WGS * C, F_FAC = F_STEP + WGS * C, F_SUM = F_FAC + WGS * C,
+                         F_RED = F_SUM + WGS * C, F_CHAN = F_RED + WGS * 4 * C, F_UNSET = F_CHAN + WGS * kHeadDim, F_END = F_UNSET + 6;
+    static constexpr int SMALL = F_END * 4 + (2 * UNITS + TEAMS * (4 + 2 * QBUF)) * 8;
     __host__ __device__ static int smem_bytes(int row_e) { return E_OFF + UNITS * kUTile * row_e + SMALL; }
     // tensor memory columns of a team: K, S, O
-    static constexpr uint32_t TM_K = 0, TM_S = 64, TM_O = 64 + N, TM_TEAM = 64 + 2 * N, TM_COLS = 2 * TM_TEAM <= 256 ? 256 : 512;
+    static constexpr uint32_t TM_K = 0, TM_S = 64, TM_O = 64 + N, TM_TEAM = 64 + 2 * N, TM_COLS = TEAMS * TM_TEAM <= 256 ? 256 : 512;
 };
 
 // pi(Q) of one (sequence, kv head, row tile) per block, as the shared-memory image of the B operand: two panels of 64
@@ -118,16 +122,20 @@ __device__ __forceinline__ void umma_exps(const uint8_t* e, int row_e, uint32_t 
         w[1] = w[0];
     }
 }
-// The blocks of half a row (slots 64 half ..) relative to the whole row's largest exponent byte, which is returned (254
-// at most).
-template <int P, bool N16>
-__device__ __forceinline__ int umma_row(const uint32_t (&w)[2], int half, UW (&g)[N16 ? 4 : 2]) {
+// The blocks of a row (H = 1) or of its half (slots 64 half ..) relative to the whole row's largest exponent byte, which
+// is returned (254 at most).
+template <int P, bool N16, int H>
+__device__ __forceinline__ int umma_row(const uint32_t (&w)[2], int half, UW (&g)[(N16 ? 8 : 4) / H]) {
+    constexpr int NB = N16 ? 8 : 4;
     int top = 0;
 #pragma unroll
-    for (int j = 0; j < (N16 ? 8 : 4); ++j) top = max(top, (int)((w[j >> 2] >> (8 * (j & 3))) & 0xffu));
-    const uint32_t mine = N16 ? (half ? w[1] : w[0]) : w[0] >> (16 * half);
+    for (int j = 0; j < NB; ++j) top = max(top, (int)((w[j >> 2] >> (8 * (j & 3))) & 0xffu));
 #pragma unroll
-    for (int j = 0; j < (N16 ? 4 : 2); ++j) g[j] = umma_weights<P>(top - (int)((mine >> (8 * j)) & 0xffu));
+    for (int j = 0; j < NB / H; ++j) {
+        uint32_t e = w[j >> 2] >> (8 * (j & 3));
+        if (H == 2) e = (N16 ? (half ? w[1] : w[0]) : w[0] >> (16 * half)) >> (8 * j);
+        g[j] = umma_weights<P>(top - (int)(e & 0xffu));
+    }
     return min(top, 254);
 }
 // 32 slots (four 16-byte pieces of bf16) of a packed row, from slot 32 i on.
@@ -206,10 +214,11 @@ __device__ __forceinline__ float across_lanes(float (&v)[C], int lane) {
 }
 
 template <int P, bool N16, int N>
-__global__ void __launch_bounds__(kUThreads, 1) attn_umma(const AttnArgs a, const __grid_constant__ CUtensorMap k_map,
+__global__ void __launch_bounds__(UGeo<P, N>::THREADS, 1) attn_umma(const AttnArgs a, const __grid_constant__ CUtensorMap k_map,
                                                           const __grid_constant__ CUtensorMap v_map) {
     using G_ = UGeo<P, N>;
-    constexpr int D = kHeadDim, ROW_M = G_::ROW_M, UNITS = G_::UNITS, QBUF = G_::QBUF, C = G_::C, SWP = 2 * N;      // bytes of a P line
+    constexpr int D = kHeadDim, ROW_M = G_::ROW_M, UNITS = G_::UNITS, QBUF = G_::QBUF, C = G_::C, H = G_::H, TEAMS = G_::TEAMS;
+    constexpr int TEAM_WARPS = G_::WGS * 4, SWP = 2 * N;      // bytes of a P line
     extern __shared__ __align__(1024) uint8_t smem[];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int row_e = D / a.fmt.block, exp_unit = kUTile * row_e;
@@ -229,12 +238,12 @@ __global__ void __launch_bounds__(kUThreads, 1) attn_umma(const AttnArgs a, cons
     if (tid == 0) {
         for (int s = 0; s < UNITS; ++s) {
             mbar_init(b_full + 8 * s, 1);
-            mbar_init(b_empty + 8 * s, 8);
+            mbar_init(b_empty + 8 * s, 4 * H);
         }
-        for (int t = 0; t < 2; ++t) {
-            mbar_init(b_k(t), 8);
+        for (int t = 0; t < TEAMS; ++t) {
+            mbar_init(b_k(t), 4 * H);
             mbar_init(b_s(t), 1);
-            mbar_init(b_p(t), 8);
+            mbar_init(b_p(t), 4 * H);
             mbar_init(b_o(t), 1);
             for (int q = 0; q < QBUF; ++q) {
                 mbar_init(b_qfull(t, q), 1);
@@ -244,7 +253,7 @@ __global__ void __launch_bounds__(kUThreads, 1) attn_umma(const AttnArgs a, cons
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         fence_async_shared();
     }
-    if (warp == 17) tmem_alloc(smem_u32(tm_slot), G_::TM_COLS);
+    if (warp == TEAM_WARPS) tmem_alloc(smem_u32(tm_slot), G_::TM_COLS);
     tmem_fence_before();
     __syncthreads();
     tmem_fence_after();
@@ -259,12 +268,22 @@ __global__ void __launch_bounds__(kUThreads, 1) attn_umma(const AttnArgs a, cons
         first = w < workers ? worker_start(w, n_items, workers) : 0;
         return w < workers ? worker_start(w + 1, n_items, workers) - first : 0;
     };
-    int start[2], count[2];
-    count[0] = range(0, start[0]);
-    count[1] = range(1, start[1]);
-    // units of the ring in the order they are filled and drawn: tile s of team 0 (K, V), tile s of team 1, tile s + 1 ..
-    // (a team's count is the other's or one more)
-    auto unit_of = [&](int t, int s) { return 4 * s + (t == 1 && s < count[0] ? 2 : 0); };
+    int start[TEAMS], count[TEAMS], least, last_rank[TEAMS];
+#pragma unroll
+    for (int t = 0; t < TEAMS; ++t) count[t] = range(t, start[t]);
+    // units of the ring in the order they are filled and drawn: K, V of tile s of every team, then those of tile s + 1 ..
+    // (counts differ by one at most: behind the least of them some teams are left)
+    least = count[0];
+#pragma unroll
+    for (int t = 1; t < TEAMS; ++t) least = min(least, count[t]);
+#pragma unroll
+    for (int t = 0, left = 0; t < TEAMS; ++t) {
+        last_rank[t] = left;
+        left += count[t] > least;
+    }
+    int total = 0;
+#pragma unroll
+    for (int t = 0; t < TEAMS; ++t) total += count[t];
     struct Cursor {      // an item: sequence, kv head and row tile (hr), tile k of n
         int b, hr, k, n;
     };
@@ -301,23 +320,30 @@ __global__ void __launch_bounds__(kUThreads, 1) attn_umma(const AttnArgs a, cons
         }
     };
 
-    if (count[0] + count[1] == 0) {
+    if (total == 0) {
         // nothing to do
-    } else if (warp == 16) {
+    } else if (warp == TEAM_WARPS + TEAMS) {
         // ================================================================ copies
-        Cursor c[2] = {seek(start[0]), seek(start[1])};
-        if (lane == 0) {
-            bool first[2] = {true, true};
-            int run[2] = {0, 0}, issued = 0;
-            for (int s = 0; s < max(count[0], count[1]) && !dead; ++s) {
+        Cursor c[TEAMS];
 #pragma unroll
-                for (int t = 0; t < 2; ++t) {
+        for (int t = 0; t < TEAMS; ++t) c[t] = seek(start[t]);
+        if (lane == 0) {
+            bool first[TEAMS];
+            int run[TEAMS], issued = 0;
+#pragma unroll
+            for (int t = 0; t < TEAMS; ++t) {
+                first[t] = true;
+                run[t] = 0;
+            }
+            for (int s = 0; s < least + 1 && !dead; ++s) {
+#pragma unroll
+                for (int t = 0; t < TEAMS; ++t) {
                     if (s >= count[t] || dead) continue;
                     Cursor& x = c[t];
                     if (first[t]) {
                         const int q = run[t] % QBUF, n = run[t] / QBUF;
                         if (n > 0) wait(b_qfree(t, q), n - 1);
-                        if (dead) break;
+                        if (dead) continue;
                         mbar_expect_tx(b_qfull(t, q), G_::Q_BYTES);
                         bulk_g2s(smem_u32(smem) + G_::Q_OFF + (t * QBUF + q) * G_::Q_BYTES,
                                  reinterpret_cast<const uint8_t*>(a.qfrag) + ((int64_t)x.b * HR + x.hr) * G_::Q_BYTES, G_::Q_BYTES, b_qfull(t, q));
@@ -352,76 +378,65 @@ __global__ void __launch_bounds__(kUThreads, 1) attn_umma(const AttnArgs a, cons
                     (void)mbar_wait_bounded(b_full + 8 * s, 1);
                 }
         }
-    } else if (warp == 17) {
-        // ================================================================ matrix instructions
+    } else if (warp >= TEAM_WARPS) {
+        // ================================================================ matrix instructions of a team
         constexpr uint32_t id_s = umma_idesc(128, N, false, false), id_o = umma_idesc(128, N, true, true);
-        const uint32_t tmu = __shfl_sync(0xffffffffu, tm, 0), base = smem_u32(smem);
-        Cursor c[2] = {seek(start[0]), seek(start[1])};
-        int run[2] = {0, 0}, ns[2] = {0, 0}, no[2] = {0, 0}, idle = 0;
-        bool first[2] = {true, true}, fresh[2] = {true, true};        // the next tile begins a run: S, O
-        auto ready = [&](uint32_t bar, int phase) { return __all_sync(0xffffffffu, mbar_try(bar, (uint32_t)phase & 1u)); };      // alike in all lanes
-        // S of a tile needs its K rows (and, at the start of a run, pi(Q)), O its V rows and P.  A bounded number of looks
-        // without progress ends it.
-        while (no[0] < count[0] || no[1] < count[1]) {
-            bool moved = false;
+        const int t = __shfl_sync(0xffffffffu, warp - TEAM_WARPS, 0);
+        const uint32_t tmt = __shfl_sync(0xffffffffu, tm, 0) + t * G_::TM_TEAM, base = smem_u32(smem);
+        const uint64_t vd = umma_desc<128>(base + G_::V_OFF + t * G_::V_BYTES, kUTile * 128, 1024);
+        const uint64_t pd = umma_desc<SWP>(base + G_::P_OFF + t * G_::P_BYTES, 16, 8 * SWP);
+        int n_mine = 0, first_item = 0;
 #pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                const uint32_t tmt = tmu + t * G_::TM_TEAM;
-                if (no[t] == ns[t]) {
-                    const int q = run[t] % QBUF;
-                    if (ns[t] < count[t] && ready(b_k(t), ns[t]) && (!first[t] || ready(b_qfull(t, q), run[t] / QBUF))) {
-                        tmem_fence_after();
-                        const uint64_t qd = umma_desc<128>(base + G_::Q_OFF + (t * QBUF + q) * G_::Q_BYTES, 16, 1024);
+        for (int x = 0; x < TEAMS; ++x)
+            if (x == t) { n_mine = count[x]; first_item = start[x]; }
+        Cursor c = seek(first_item);
+        int run = 0;
+        bool first = true;                       // the tile begins a run
+        for (int i = 0; i < n_mine; ++i) {
+            const int q = run % QBUF;
+            if (first) wait(b_qfull(t, q), run / QBUF);
+            wait(b_k(t), i);
+            __syncwarp();
+            tmem_fence_after();
+            const uint64_t qd = umma_desc<128>(base + G_::Q_OFF + (t * QBUF + q) * G_::Q_BYTES, 16, 1024);
 #pragma unroll
-                        for (int ks = 0; ks < 8; ++ks)
-                            umma_ts(tmt + G_::TM_S, tmt + G_::TM_K + ks * 8, qd + (((ks >> 2) * (N * 128) + (ks & 3) * 32) >> 4), id_s, ks > 0);
-                        umma_commit(b_s(t));
-                        fresh[t] = first[t];
-                        first[t] = false;
-                        if (++c[t].k == c[t].n) {
-                            umma_commit(b_qfree(t, q));
-                            next_pair(c[t]);
-                            first[t] = true;
-                            ++run[t];
-                        }
-                        ++ns[t];
-                        moved = true;
-                    }
-                } else if (ready(b_p(t), no[t])) {
-                    tmem_fence_after();
-                    const uint64_t v = umma_desc<128>(base + G_::V_OFF + t * G_::V_BYTES, kUTile * 128, 1024);
-                    const uint64_t p = umma_desc<SWP>(base + G_::P_OFF + t * G_::P_BYTES, 16, 8 * SWP);
-#pragma unroll
-                    for (int ks = 0; ks < kUTile / 16; ++ks)
-                        umma_ss(tmt + G_::TM_O, v + ks * (2048 >> 4), p + ks * (16 * SWP >> 4), id_o, ks > 0 || !fresh[t]);
-                    umma_commit(b_o(t));
-                    ++no[t];
-                    moved = true;
-                }
+            for (int ks = 0; ks < 8; ++ks)
+                umma_ts(tmt + G_::TM_S, tmt + G_::TM_K + ks * 8, qd + (((ks >> 2) * (N * 128) + (ks & 3) * 32) >> 4), id_s, ks > 0);
+            umma_commit(b_s(t));
+            const bool fresh = first;
+            first = ++c.k == c.n;
+            if (first) {
+                umma_commit(b_qfree(t, q));
+                next_pair(c);
+                ++run;
             }
-            if (moved) {
-                idle = 0;
-            } else if (++idle > (1 << 24)) {
-                dead = true;
-                if (lane == 0) raise_flag(a.status, KVBFP_FLAG_WAIT_TIMEOUT);
-                break;
-            }
+            wait(b_p(t), i);
+            __syncwarp();
+            tmem_fence_after();
+#pragma unroll
+            for (int ks = 0; ks < kUTile / 16; ++ks)
+                umma_ss(tmt + G_::TM_O, vd + ks * (2048 >> 4), pd + ks * (16 * SWP >> 4), id_o, ks > 0 || !fresh);
+            umma_commit(b_o(t));
         }
-        if (dead) {       // let what was issued come to its end before the tensor memory goes
-            umma_commit(b_qfree(0, 0));
-            (void)mbar_wait_bounded(b_qfree(0, 0), 0);
-            (void)mbar_wait_bounded(b_qfree(0, 0), 1);
+        if (__any_sync(0xffffffffu, dead)) {       // let what was issued come to its end before the tensor memory goes
+            umma_commit(b_s(t));
+            (void)mbar_wait_bounded(b_s(t), 0);
+            (void)mbar_wait_bounded(b_s(t), 1);
         }
     } else {
-        // ================================================================ a team: two threads per token
-        const int team = warp >> 3, wg = warp >> 2, half = wg & 1, m_pos = tid & 127, w4 = warp & 3, bar_id = 1 + wg;
+        // ================================================================ a team: H threads per token
+        const int wg = warp >> 2, team = wg / H, half = H == 2 ? wg & 1 : 0, m_pos = tid & 127, w4 = warp & 3, bar_id = 1 + wg;
         const uint32_t tmt = tm + team * G_::TM_TEAM + ((uint32_t)w4 << 21);        // lane field: 32 * quarter << 16
         float *mref = fl + G_::F_MREF + wg * C, *mstep = fl + G_::F_STEP + wg * C, *mfac = fl + G_::F_FAC + wg * C,
               *lsum = fl + G_::F_SUM + wg * C, *red = fl + G_::F_RED + wg * 4 * C;
         int* chan = reinterpret_cast<int*>(fl + G_::F_CHAN) + wg * D;
         int* unset = reinterpret_cast<int*>(fl + G_::F_UNSET) + wg;         // rows that have seen nothing yet, as a bit mask
-        uint8_t* vline = smem + G_::V_OFF + team * G_::V_BYTES + half * (kUTile * 128) + m_pos * 128;       // half a row: a panel of 64 slots
-        const int n_mine = team ? count[1] : count[0], me = blockIdx.x + team * gridDim.x;
+        uint8_t* vline = smem + G_::V_OFF + team * G_::V_BYTES + half * (kUTile * 128) + m_pos * 128;       // (a panel holds 64 slots)
+        int n_mine = 0, first_item = 0, rank = 0;
+#pragma unroll
+        for (int x = 0; x < TEAMS; ++x)
+            if (x == team) { n_mine = count[x]; first_item = start[x]; rank = last_rank[x]; }
+        const int me = blockIdx.x + team * gridDim.x;
         const int R = a.n_draft * a.group;
         const float up = a.scale * (P == 4 ? 64.f : P == 6 ? 16.f : 4.f), to_log2 = 1.4426950408889634f;      // 2^8 2^-(P-2)
         const float cap_in = a.softcap > 0.f ? up / a.softcap * 2.8853900817779268f : 0.f;
@@ -440,23 +455,8 @@ __global__ void __launch_bounds__(kUThreads, 1) attn_umma(const AttnArgs a, cons
             }
             asm volatile("cp.async.commit_group;" ::: "memory");
         };
-        // 64 slots of a unit's row to `put`, sixteen registers (32 slots) at a time; returns the row's largest exponent
-        auto convert = [&](int u, auto put) {
-            const uint8_t* tile = smem + u * G_::UNIT;
-            uint32_t ew[2];
-            umma_exps<N16>(smem + G_::E_OFF + u * exp_unit + m_pos * row_e, row_e, ew);
-            UW g[N16 ? 4 : 2];
-            const int top = umma_row<P, N16>(ew, half, g);
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                uint32_t r[16];
-                convert32<P>(tile, m_pos, 2 * half + j, g[N16 ? 2 * j : j], g[N16 ? 2 * j + 1 : j], r);
-                put(j, r);
-            }
-            return top;
-        };
-
-        Cursor c = seek(team ? start[1] : start[0]), cn = c;
+        Cursor c = seek(first_item), cn = c;
+        int unit = 2 * (least > 0 ? team : rank), round = 0;          // the ring's next unit of this team, and how often the ring went round
         fetch(c, 0);
         int it = 0, run = 0;
         while (it < n_mine) {
@@ -480,31 +480,51 @@ __global__ void __launch_bounds__(kUThreads, 1) attn_umma(const AttnArgs a, cons
 #pragma unroll
             for (int j = 0; j < C; ++j) l[j] = 0.f;
             for (int k = k0; k < k1; ++k, ++it) {
-                const int uk = unit_of(team, it), uv = uk + 1;
-                // ---- K: the tensor memory it goes to was read by the product of the tile before, which this thread has waited for
-                wait(b_full + 8 * (uk % UNITS), uk / UNITS);
-                __syncwarp();
-                const int k_top = convert(uk % UNITS, [&](int j, const uint32_t (&r)[16]) { tmem_st<16>(tmt + G_::TM_K + half * 32 + 16 * j, r); });
-                tmem_wait_st();
-                tmem_fence_before();
-                __syncwarp();
-                if (lane == 0) {
-                    mbar_arrive(b_k(team));
-                    mbar_arrive(b_empty + 8 * (uk % UNITS));
-                }
-                // ---- V, while the tensor cores are on S
-                wait(b_full + 8 * (uv % UNITS), uv / UNITS);
-                if (it > 0) wait(b_o(team), it - 1);          // the product of the tile before has read V and P
-                const int v_top = convert(uv % UNITS, [&](int j, const uint32_t (&r)[16]) {
+                // ---- K to tensor memory (the product of the tile before has read it: waited for below, a tile ago), then, while the
+                // tensor cores are on S, V to shared memory.  (One loop for both: the code of a tile has to stay in the
+                // instruction cache.)
+                uint32_t top2[2];
+#pragma unroll 1
+                for (int kv = 0; kv < 2; ++kv) {
+                    wait(b_full + 8 * unit, round);
+                    if (kv == 1 && it > 0) wait(b_o(team), it - 1);          // the product of the tile before has read V and P
+                    __syncwarp();
+                    const uint8_t* tile = smem + unit * G_::UNIT;
+                    uint32_t ew[2];
+                    umma_exps<N16>(smem + G_::E_OFF + unit * exp_unit + m_pos * row_e, row_e, ew);
+                    UW g[(N16 ? 8 : 4) / H];
+                    const uint32_t top = (uint32_t)umma_row<P, N16, H>(ew, half, g);
+                    if (kv == 0) top2[0] = top; else top2[1] = top;
 #pragma unroll
-                    for (int x = 0; x < 4; ++x)       // 16-byte pieces 4 j + x, swizzled
-                        *reinterpret_cast<uint4*>(vline + (((4 * j + x) ^ (m_pos & 7)) << 4)) = make_uint4(r[4 * x], r[4 * x + 1], r[4 * x + 2], r[4 * x + 3]);
-                });
-                __syncwarp();
-                if (lane == 0) mbar_arrive(b_empty + 8 * (uv % UNITS));
+                    for (int j = 0; j < 4 / H; ++j) {
+                        uint32_t r[16];
+                        convert32<P>(tile, m_pos, 2 * half + j, g[N16 ? 2 * j : j], g[N16 ? 2 * j + 1 : j], r);
+                        if (kv == 0) {
+                            tmem_st<16>(tmt + G_::TM_K + half * 32 + 16 * j, r);
+                        } else {
+                            uint8_t* to = vline + (j >> 1) * (kUTile * 128);
+#pragma unroll
+                            for (int x = 0; x < 4; ++x)       // 16-byte pieces 4 j + x, swizzled
+                                *reinterpret_cast<uint4*>(to + (((4 * (j & 1) + x) ^ (m_pos & 7)) << 4)) = make_uint4(r[4 * x], r[4 * x + 1], r[4 * x + 2], r[4 * x + 3]);
+                        }
+                    }
+                    if (kv == 0) {
+                        tmem_wait_st();
+                        tmem_fence_before();
+                    }
+                    __syncwarp();
+                    if (lane == 0) {
+                        if (kv == 0) mbar_arrive(b_k(team));
+                        mbar_arrive(b_empty + 8 * unit);
+                    }
+                    if (kv == 0 && ++unit == UNITS) { unit = 0; ++round; }
+                }
+                unit += 2 * TEAMS - 1 - (it + 1 == least ? 2 * (team - rank) : 0);
+                while (unit >= UNITS) { unit -= UNITS; ++round; }
+                const uint32_t k_top = top2[0], v_top = top2[1];
                 // ---- scores
                 const int tt = tile_token(sv, k, kUTile), tok = tt + m_pos;
-                const float kf = __uint_as_float((uint32_t)k_top << 23), vf = __uint_as_float((uint32_t)max(v_top - 9, 0) << 23);
+                const float kf = __uint_as_float(k_top << 23), vf = __uint_as_float((uint32_t)max((int)v_top - 9, 0) << 23);
                 wait(b_s(team), it);
                 __syncwarp();
                 tmem_fence_after();
@@ -673,7 +693,7 @@ __global__ void __launch_bounds__(kUThreads, 1) attn_umma(const AttnArgs a, cons
     tmem_fence_before();
     __syncthreads();
     tmem_fence_after();
-    if (warp == 17) tmem_dealloc(tm, G_::TM_COLS);
+    if (warp == TEAM_WARPS) tmem_dealloc(tm, G_::TM_COLS);
     pdl_trigger();
 }
 
@@ -698,7 +718,7 @@ kvbfp_status launch_umma(const AttnArgs& a, int grid, cudaStream_t s) {
     }
     KVBFP_CUDA(launch_pdl(umma_prep<P, N>, dim3(a.fmt.batch * a.fmt.n_kv_heads * a.n_row_tiles), dim3(128), 0, s, a));
     KVBFP_LAUNCH_CHECK("umma_prep");
-    KVBFP_CUDA(launch_pdl(kernel, dim3(grid), dim3(kUThreads), G_::smem_bytes(kHeadDim / a.fmt.block), s, a, k_map, v_map));
+    KVBFP_CUDA(launch_pdl(kernel, dim3(grid), dim3(G_::THREADS), G_::smem_bytes(kHeadDim / a.fmt.block), s, a, k_map, v_map));
     KVBFP_LAUNCH_CHECK("attn_umma");
     return KVBFP_OK;
 }
