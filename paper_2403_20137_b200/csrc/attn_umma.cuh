@@ -9,16 +9,19 @@
 // (the warp-level kernel converts per 16 rows and its matrix instructions run at a third of the rate).
 //
 // One persistent thread block per SM, tiles of 128 tokens.  Teams of warps, each a worker with a contiguous range of
-// tiles of its own (attn.cuh), a thread per token (three teams of four warps: 4-bit
-// rows, up to 32 query rows) or two (two teams of eight: what shared memory holds of wider rows):
-//   K rows converted to tensor memory (the A operand of the first product)
-//   V rows converted to shared memory (the A operand of the second, slots contiguous) while the first product runs
-//   scores from tensor memory: masks, running maximum, P to shared memory
-//   at the end of a run O^T from tensor memory to the result or a partial
-// While one team waits (for a product, a barrier, a copy) the others work.  A warp per team issues its matrix
-// instructions, one warp copies packed tiles into a ring of units that the teams draw from in turn and pi(Q) of the runs.
+// tiles of its own (attn.cuh), a thread per token (three teams of four warps: 4-bit rows, up to 32 query rows) or two
+// (two teams of eight: what shared memory holds of wider rows).  Per tile i a team
+//   converts the K rows of tile i + 1 to tensor memory (the A operand of the first product)
+//   converts the V rows of tile i to shared memory (the A operand of the second, slots contiguous)
+//   reads the scores of tile i from tensor memory: masks, running maximum, P to shared memory
+// so that what it needs next was started most of a tile ago: a hand-over between warps takes some 250 cycles, a product
+// 150 to 400, a copy 1500.  At the end of a run O^T goes from tensor memory to the result or a partial.  A warp per team
+// issues its matrix instructions and the copies of its packed rows and pi(Q).  (One warp that copied for all teams took
+// 500 to 1000 cycles per copy: its code had gone from the instruction cache each time.)
 // (Groups of their own for conversion and softmax, with two to three tiles between them, took twice as long: the buffers
 // between the phases were what everything waited for.)
+// Rare paths (masks, raising a reference, results) are loops over eight columns of tensor memory: straight code that is
+// not in the instruction cache runs at some nine cycles an instruction.
 // Cached values are converted relative to their row's largest exponent (see below); magnitudes of 2^118 and above are
 // outside the range.
 // The row maximum runs across threads here, so it is only taken when a score passes the reference by 8 (a factor 2^8),
@@ -49,27 +52,28 @@ struct UGeo {
     static constexpr int TEAMS = attn_teams(P, N);
     static constexpr int H = TEAMS == 3 ? 1 : 2;                 // threads per token
     static constexpr int WGS = TEAMS * H;                        // groups of four warps
-    static constexpr int THREADS = (WGS * 4 + TEAMS + 1) * 32;
+    static constexpr int THREADS = (WGS * 4 + TEAMS) * 32;
     static constexpr int C = N / H;                              // query rows of a thread
     static constexpr int UNIT = kUTile * ROW_M;                  // a tile's K or V rows
-    static constexpr int UNITS = P == 4 ? (N == 32 ? 8 : 9) : P == 6 ? (N == 64 ? 6 : 8) : (N == 64 ? 5 : 6);
-    static constexpr int QBUF = N == 16 ? 2 : 1;
+    static constexpr int KS = P == 4 && N == 32 || P == 8 && N == 64 ? 1 : 2;       // packed K rows a team keeps
+    static constexpr int VS = P == 4 && N == 64 || P == 6 && N <= 32 ? 2 : 1;       // and V rows
+    static constexpr int RING = KS + VS, UNITS = TEAMS * RING;
     static constexpr int V_OFF = UNITS * UNIT;                   // per team: converted V
     static constexpr int V_BYTES = kUTile * kHeadDim * 2;
     static constexpr int P_OFF = V_OFF + TEAMS * V_BYTES;        // per team: P
     static constexpr int P_BYTES = kUTile * N * 2;
     static constexpr int Q_OFF = P_OFF + TEAMS * P_BYTES;        // per team: pi(Q)
     static constexpr int Q_BYTES = N * kHeadDim * 2;
-    static constexpr int E_OFF = Q_OFF + TEAMS * QBUF * Q_BYTES; // exponent bytes: UNITS x 128 x row_e
+    static constexpr int E_OFF = Q_OFF + TEAMS * Q_BYTES;        // exponent bytes: UNITS x 128 x row_e
     // behind them (in floats), per group of four warps: row data, drafted positions and view of two runs, references,
     // steps, factors, sums, reduction, channel table; then barriers
     static constexpr int F_RI = 0, F_DPOS = F_RI + WGS * 2 * C * 4, F_VIEW = F_DPOS + WGS * 2 * kAttnMaxDraft,
                          F_MREF = F_VIEW + WGS * 2 * 8, F_STEP = F_MREF + WGS * C, F_FAC = F_STEP + WGS * C, F_SUM = F_FAC + WGS * C,
-                         F_RED = F_SUM + WGS * C, F_CHAN = F_RED + WGS * 4 * C, F_UNSET = F_CHAN + WGS * kHeadDim, F_END = F_UNSET + 6;
-    static constexpr int SMALL = F_END * 4 + (2 * UNITS + TEAMS * (4 + 2 * QBUF)) * 8;
+                         F_RED = F_SUM + WGS * C, F_CHAN = F_RED + WGS * 4 * C, F_UNSET = F_CHAN + WGS * kHeadDim, F_END = F_UNSET + 8;
+    static constexpr int SMALL = F_END * 4 + TEAMS * (RING + 7) * 8;
     __host__ __device__ static int smem_bytes(int row_e) { return E_OFF + UNITS * kUTile * row_e + SMALL; }
-    // tensor memory columns of a team: K, S, O
-    static constexpr uint32_t TM_K = 0, TM_S = 64, TM_O = 64 + N, TM_TEAM = 64 + 2 * N, TM_COLS = TEAMS * TM_TEAM <= 256 ? 256 : 512;
+    // tensor memory columns of a team: K, two S, O
+    static constexpr uint32_t TM_K = 0, TM_S = 64, TM_O = 64 + 2 * N, TM_TEAM = 64 + 3 * N, TM_COLS = TEAMS * TM_TEAM <= 256 ? 256 : 512;
 };
 
 // pi(Q) of one (sequence, kv head, row tile) per block, as the shared-memory image of the B operand: two panels of 64
@@ -213,42 +217,43 @@ __device__ __forceinline__ float across_lanes(float (&v)[C], int lane) {
     return v[0];
 }
 
+__device__ __noinline__ bool umma_wait_slow(uint32_t bar, uint32_t parity) { return mbar_wait_bounded(bar, parity); }
+
 template <int P, bool N16, int N>
 __global__ void __launch_bounds__(UGeo<P, N>::THREADS, 1) attn_umma(const AttnArgs a, const __grid_constant__ CUtensorMap k_map,
-                                                          const __grid_constant__ CUtensorMap v_map) {
+                                                                    const __grid_constant__ CUtensorMap v_map) {
     using G_ = UGeo<P, N>;
-    constexpr int D = kHeadDim, ROW_M = G_::ROW_M, UNITS = G_::UNITS, QBUF = G_::QBUF, C = G_::C, H = G_::H, TEAMS = G_::TEAMS;
+    constexpr int D = kHeadDim, ROW_M = G_::ROW_M, UNITS = G_::UNITS, RING = G_::RING, KS = G_::KS, VS = G_::VS, C = G_::C, H = G_::H, TEAMS = G_::TEAMS;
     constexpr int TEAM_WARPS = G_::WGS * 4, SWP = 2 * N;      // bytes of a P line
     extern __shared__ __align__(1024) uint8_t smem[];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int row_e = D / a.fmt.block, exp_unit = kUTile * row_e;
     float* fl = reinterpret_cast<float*>(smem + G_::E_OFF + UNITS * exp_unit);
-    uint32_t* tm_slot = reinterpret_cast<uint32_t*>(fl + G_::F_UNSET + 4);
+    uint32_t* tm_slot = reinterpret_cast<uint32_t*>(fl + G_::F_UNSET + 6);
+    // barriers of a team: packed K rows there (KS), packed V rows there (VS), pi(Q) there, K converted, V converted, P written,
+    // S done (two), O done
     const uint32_t bars = smem_u32(fl + G_::F_END);
-    // ring: full, empty; per team: K ready, S done, P ready, O done, pi(Q) full, pi(Q) free
-    const uint32_t b_full = bars, b_empty = bars + 8 * UNITS, b_team = b_empty + 8 * UNITS;
-    constexpr int TB = 8 * (4 + 2 * QBUF);
-    auto b_k = [&](int t) { return b_team + t * TB; };
-    auto b_s = [&](int t) { return b_team + t * TB + 8; };
-    auto b_p = [&](int t) { return b_team + t * TB + 16; };
-    auto b_o = [&](int t) { return b_team + t * TB + 24; };
-    auto b_qfull = [&](int t, int q) { return b_team + t * TB + 32 + 8 * q; };
-    auto b_qfree = [&](int t, int q) { return b_team + t * TB + 32 + 8 * (QBUF + q); };
+    constexpr int TB = 8 * (RING + 7);
+    auto b_kf = [&](int t, int i) { return bars + t * TB + 8 * (i % KS); };
+    auto b_vf = [&](int t, int i) { return bars + t * TB + 8 * (KS + i % VS); };
+    auto b_q = [&](int t) { return bars + t * TB + 8 * RING; };
+    auto b_k = [&](int t) { return bars + t * TB + 8 * RING + 8; };
+    auto b_v = [&](int t) { return bars + t * TB + 8 * RING + 16; };
+    auto b_p = [&](int t) { return bars + t * TB + 8 * RING + 24; };
+    auto b_s = [&](int t, int i) { return bars + t * TB + 8 * RING + 32 + 8 * (i & 1); };
+    auto b_o = [&](int t) { return bars + t * TB + 8 * RING + 48; };
 
     if (tid == 0) {
-        for (int s = 0; s < UNITS; ++s) {
-            mbar_init(b_full + 8 * s, 1);
-            mbar_init(b_empty + 8 * s, 4 * H);
-        }
         for (int t = 0; t < TEAMS; ++t) {
+            for (int i = 0; i < KS; ++i) mbar_init(b_kf(t, i), 1);
+            for (int i = 0; i < VS; ++i) mbar_init(b_vf(t, i), 1);
+            mbar_init(b_q(t), 1);
             mbar_init(b_k(t), 4 * H);
-            mbar_init(b_s(t), 1);
+            mbar_init(b_v(t), 4 * H);
             mbar_init(b_p(t), 4 * H);
+            mbar_init(b_s(t, 0), 1);
+            mbar_init(b_s(t, 1), 1);
             mbar_init(b_o(t), 1);
-            for (int q = 0; q < QBUF; ++q) {
-                mbar_init(b_qfull(t, q), 1);
-                mbar_init(b_qfree(t, q), 1);
-            }
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         fence_async_shared();
@@ -268,22 +273,6 @@ __global__ void __launch_bounds__(UGeo<P, N>::THREADS, 1) attn_umma(const AttnAr
         first = w < workers ? worker_start(w, n_items, workers) : 0;
         return w < workers ? worker_start(w + 1, n_items, workers) - first : 0;
     };
-    int start[TEAMS], count[TEAMS], least, last_rank[TEAMS];
-#pragma unroll
-    for (int t = 0; t < TEAMS; ++t) count[t] = range(t, start[t]);
-    // units of the ring in the order they are filled and drawn: K, V of tile s of every team, then those of tile s + 1 ..
-    // (counts differ by one at most: behind the least of them some teams are left)
-    least = count[0];
-#pragma unroll
-    for (int t = 1; t < TEAMS; ++t) least = min(least, count[t]);
-#pragma unroll
-    for (int t = 0, left = 0; t < TEAMS; ++t) {
-        last_rank[t] = left;
-        left += count[t] > least;
-    }
-    int total = 0;
-#pragma unroll
-    for (int t = 0; t < TEAMS; ++t) total += count[t];
     struct Cursor {      // an item: sequence, kv head and row tile (hr), tile k of n
         int b, hr, k, n;
     };
@@ -314,114 +303,110 @@ __global__ void __launch_bounds__(UGeo<P, N>::THREADS, 1) attn_umma(const AttnAr
     };
     bool dead = false;          // a wait ran out: no more waits, the flag is up, results are void
     auto wait = [&](uint32_t bar, int phase) {
-        if (!dead && !mbar_try(bar, (uint32_t)phase & 1u) && !mbar_wait_bounded(bar, (uint32_t)phase & 1u)) {
+        if (!mbar_try(bar, (uint32_t)phase & 1u) && !dead && !umma_wait_slow(bar, (uint32_t)phase & 1u)) {
             dead = true;
             raise_flag(a.status, KVBFP_FLAG_WAIT_TIMEOUT);
         }
     };
 
-    if (total == 0) {
-        // nothing to do
-    } else if (warp == TEAM_WARPS + TEAMS) {
-        // ================================================================ copies
-        Cursor c[TEAMS];
-#pragma unroll
-        for (int t = 0; t < TEAMS; ++t) c[t] = seek(start[t]);
-        if (lane == 0) {
-            bool first[TEAMS];
-            int run[TEAMS], issued = 0;
-#pragma unroll
-            for (int t = 0; t < TEAMS; ++t) {
-                first[t] = true;
-                run[t] = 0;
-            }
-            for (int s = 0; s < least + 1 && !dead; ++s) {
-#pragma unroll
-                for (int t = 0; t < TEAMS; ++t) {
-                    if (s >= count[t] || dead) continue;
-                    Cursor& x = c[t];
-                    if (first[t]) {
-                        const int q = run[t] % QBUF, n = run[t] / QBUF;
-                        if (n > 0) wait(b_qfree(t, q), n - 1);
-                        if (dead) continue;
-                        mbar_expect_tx(b_qfull(t, q), G_::Q_BYTES);
-                        bulk_g2s(smem_u32(smem) + G_::Q_OFF + (t * QBUF + q) * G_::Q_BYTES,
-                                 reinterpret_cast<const uint8_t*>(a.qfrag) + ((int64_t)x.b * HR + x.hr) * G_::Q_BYTES, G_::Q_BYTES, b_qfull(t, q));
-                        first[t] = false;
-                    }
-                    const SeqView sv = a.views[x.b];
-                    const int tt = tile_token(sv, x.k, kUTile);
-                    const int64_t row0 = ((int64_t)x.b * Hkv + x.hr / a.n_row_tiles) * max_seq + tt;
-                    const int rows = min(kUTile, max_seq - tt);           // a multiple of 16
-                    const uint32_t mant = (P == 6 ? rows : kUTile) * ROW_M;       // a tiled copy always brings its whole box
-#pragma unroll
-                    for (int kv = 0; kv < 2; ++kv, ++issued) {
-                        const int u = issued % UNITS;
-                        if (issued >= UNITS) wait(b_empty + 8 * u, issued / UNITS - 1);
-                        if (dead) break;
-                        const uint32_t dst = smem_u32(smem) + u * G_::UNIT, de = smem_u32(smem) + G_::E_OFF + u * exp_unit, br = b_full + 8 * u;
-                        mbar_expect_tx(br, mant + rows * row_e);
-                        if (P == 6) bulk_g2s(dst, (kv ? a.v_mant : a.k_mant) + row0 * ROW_M, mant, br);
-                        else tensor_g2s_2d(dst, kv ? &v_map : &k_map, 0, (int)(P == 4 ? row0 >> 1 : row0), br);
-                        bulk_g2s(de, (kv ? a.v_exp : a.k_exp) + row0 * row_e, rows * row_e, br);
-                    }
-                    if (++x.k == x.n) {
-                        next_pair(x);
-                        first[t] = true;
-                        ++run[t];
-                    }
-                }
-            }
-            if (dead)       // give the copies still in flight a bounded chance to land before the shared memory is released
-                for (int s = 0; s < UNITS; ++s) {
-                    (void)mbar_wait_bounded(b_full + 8 * s, 0);
-                    (void)mbar_wait_bounded(b_full + 8 * s, 1);
-                }
-        }
-    } else if (warp >= TEAM_WARPS) {
-        // ================================================================ matrix instructions of a team
+    if (warp >= TEAM_WARPS) {
+        // ================================================================ matrix instructions and copies of a team
         constexpr uint32_t id_s = umma_idesc(128, N, false, false), id_o = umma_idesc(128, N, true, true);
         const int t = __shfl_sync(0xffffffffu, warp - TEAM_WARPS, 0);
         const uint32_t tmt = __shfl_sync(0xffffffffu, tm, 0) + t * G_::TM_TEAM, base = smem_u32(smem);
         const uint64_t vd = umma_desc<128>(base + G_::V_OFF + t * G_::V_BYTES, kUTile * 128, 1024);
         const uint64_t pd = umma_desc<SWP>(base + G_::P_OFF + t * G_::P_BYTES, 16, 8 * SWP);
-        int n_mine = 0, first_item = 0;
-#pragma unroll
-        for (int x = 0; x < TEAMS; ++x)
-            if (x == t) { n_mine = count[x]; first_item = start[x]; }
+        const uint64_t qd = umma_desc<128>(base + G_::Q_OFF + t * G_::Q_BYTES, 16, 1024);
+        int first_item;
+        const int n_mine = range(t, first_item);
+        struct Walk {                  // the next packed rows to copy: cursor, np and lo of the sequence's view
+            Cursor c;
+            int np, lo;
+        };
         Cursor c = seek(first_item);
-        int run = 0;
-        bool first = true;                       // the tile begins a run
-        for (int i = 0; i < n_mine; ++i) {
-            const int q = run % QBUF;
-            if (first) wait(b_qfull(t, q), run / QBUF);
-            wait(b_k(t), i);
-            __syncwarp();
-            tmem_fence_after();
-            const uint64_t qd = umma_desc<128>(base + G_::Q_OFF + (t * QBUF + q) * G_::Q_BYTES, 16, 1024);
-#pragma unroll
-            for (int ks = 0; ks < 8; ++ks)
-                umma_ts(tmt + G_::TM_S, tmt + G_::TM_K + ks * 8, qd + (((ks >> 2) * (N * 128) + (ks & 3) * 32) >> 4), id_s, ks > 0);
-            umma_commit(b_s(t));
-            const bool fresh = first;
-            first = ++c.k == c.n;
-            if (first) {
-                umma_commit(b_qfree(t, q));
-                next_pair(c);
-                ++run;
+        Walk wk = {c, a.views[c.b].np, a.views[c.b].lo}, wv = wk;
+        auto copy = [&](Walk& w, int u, uint32_t bar, const uint8_t* mant_plane, const CUtensorMap* map, const uint8_t* exp_plane) {
+            const int tt = (w.c.k < w.np ? w.c.k : w.c.k - w.np + w.lo) * kUTile;
+            const int64_t row0 = ((int64_t)w.c.b * Hkv + w.c.hr / a.n_row_tiles) * max_seq + tt;
+            const int rows = min(kUTile, max_seq - tt);           // a multiple of 16
+            const uint32_t mant = (P == 6 ? rows : kUTile) * ROW_M;       // a tiled copy always brings its whole box
+            if (lane == 0) {
+                mbar_expect_tx(bar, mant + rows * row_e);
+                if (P == 6) bulk_g2s(base + u * G_::UNIT, mant_plane + row0 * ROW_M, mant, bar);
+                else tensor_g2s_2d(base + u * G_::UNIT, map, 0, (int)(P == 4 ? row0 >> 1 : row0), bar);
+                bulk_g2s(base + G_::E_OFF + u * exp_unit, exp_plane + row0 * row_e, rows * row_e, bar);
             }
-            wait(b_p(t), i);
+            if (++w.c.k == w.c.n) {
+                const int b = w.c.b;
+                next_pair(w.c);
+                if (w.c.b != b && w.c.b < B) { w.np = a.views[w.c.b].np; w.lo = a.views[w.c.b].lo; }
+            }
             __syncwarp();
-            tmem_fence_after();
-#pragma unroll
-            for (int ks = 0; ks < kUTile / 16; ++ks)
-                umma_ss(tmt + G_::TM_O, vd + ks * (2048 >> 4), pd + ks * (16 * SWP >> 4), id_o, ks > 0 || !fresh);
-            umma_commit(b_o(t));
+        };
+        auto copy_k = [&](int i) { copy(wk, t * RING + i % KS, b_kf(t, i), a.k_mant, &k_map, a.k_exp); };
+        auto copy_v = [&](int i) { copy(wv, t * RING + KS + i % VS, b_vf(t, i), a.v_mant, &v_map, a.v_exp); };
+        auto copy_q = [&]() {
+            if (lane == 0) {
+                mbar_expect_tx(b_q(t), G_::Q_BYTES);
+                bulk_g2s(base + G_::Q_OFF + t * G_::Q_BYTES, reinterpret_cast<const uint8_t*>(a.qfrag) + ((int64_t)c.b * HR + c.hr) * G_::Q_BYTES, G_::Q_BYTES, b_q(t));
+            }
+            __syncwarp();
+        };
+        if (n_mine > 0) {
+            copy_k(0);
+            copy_q();
+            copy_v(0);
+            if (KS > 1 && n_mine > 1) copy_k(1);
+            if (VS > 1 && n_mine > 1) copy_v(1);
         }
-        if (__any_sync(0xffffffffu, dead)) {       // let what was issued come to its end before the tensor memory goes
-            umma_commit(b_s(t));
-            (void)mbar_wait_bounded(b_s(t), 0);
-            (void)mbar_wait_bounded(b_s(t), 1);
+        int run = 0;
+        bool first = true, fresh = true, fresh_next = true;             // the tile of the next S, of this O, of the next O begins a run
+        for (int i = -1; i < n_mine && !__any_sync(0xffffffffu, dead); ++i) {
+            if (i + 1 < n_mine) {            // S of tile i + 1; its packed K rows are used up
+                if (first) wait(b_q(t), run);
+                wait(b_k(t), i + 1);
+                __syncwarp();
+                tmem_fence_after();
+#pragma unroll
+                for (int ks = 0; ks < 8; ++ks)
+                    umma_ts(tmt + G_::TM_S + ((i + 1) & 1) * N, tmt + G_::TM_K + ks * 8, qd + (((ks >> 2) * (N * 128) + (ks & 3) * 32) >> 4), id_s, ks > 0);
+                umma_commit(b_s(t, i + 1));
+                if (i + 1 + KS < n_mine) copy_k(i + 1 + KS);
+                fresh_next = first;
+                first = ++c.k == c.n;
+                if (first) {
+                    next_pair(c);
+                    ++run;
+                }
+            }
+            if (i >= 0) {                    // O of tile i
+                wait(b_v(t), i);
+                __syncwarp();
+                if (i + VS < n_mine) copy_v(i + VS);
+                wait(b_p(t), i);
+                __syncwarp();
+                tmem_fence_after();
+#pragma unroll
+                for (int ks = 0; ks < kUTile / 16; ++ks)
+                    umma_ss(tmt + G_::TM_O, vd + ks * (2048 >> 4), pd + ks * (16 * SWP >> 4), id_o, ks > 0 || !fresh);
+                umma_commit(b_o(t));
+            }
+            if (first && i + 2 < n_mine) {   // the next S is of another run
+                wait(b_s(t, i + 1), (i + 1) >> 1);
+                __syncwarp();
+                copy_q();
+            }
+            fresh = fresh_next;
+        }
+        if (__any_sync(0xffffffffu, dead)) {
+            // let what was issued come to its end, and copies in flight land, before the memory goes
+            umma_commit(b_o(t));
+            for (int x = 0; x < RING + 1; ++x) {
+                (void)mbar_wait_bounded(bars + t * TB + 8 * x, 0);
+                (void)mbar_wait_bounded(bars + t * TB + 8 * x, 1);
+            }
+            (void)mbar_wait_bounded(b_o(t), 0);
+            (void)mbar_wait_bounded(b_o(t), 1);
         }
     } else {
         // ================================================================ a team: H threads per token
@@ -432,17 +417,12 @@ __global__ void __launch_bounds__(UGeo<P, N>::THREADS, 1) attn_umma(const AttnAr
         int* chan = reinterpret_cast<int*>(fl + G_::F_CHAN) + wg * D;
         int* unset = reinterpret_cast<int*>(fl + G_::F_UNSET) + wg;         // rows that have seen nothing yet, as a bit mask
         uint8_t* vline = smem + G_::V_OFF + team * G_::V_BYTES + half * (kUTile * 128) + m_pos * 128;       // (a panel holds 64 slots)
-        int n_mine = 0, first_item = 0, rank = 0;
-#pragma unroll
-        for (int x = 0; x < TEAMS; ++x)
-            if (x == team) { n_mine = count[x]; first_item = start[x]; rank = last_rank[x]; }
-        const int me = blockIdx.x + team * gridDim.x;
+        int first_item;
+        const int n_mine = range(team, first_item), me = blockIdx.x + team * gridDim.x;
         const int R = a.n_draft * a.group;
         const float up = a.scale * (P == 4 ? 64.f : P == 6 ? 16.f : 4.f), to_log2 = 1.4426950408889634f;      // 2^8 2^-(P-2)
         const float cap_in = a.softcap > 0.f ? up / a.softcap * 2.8853900817779268f : 0.f;
-        // the column a lane ends up with after across_lanes: its upper log2(C) lane bits
-        const int my_col = C == 32 ? lane : C == 16 ? lane >> 1 : lane >> 2;
-        const bool my_first = C == 32 || (C == 16 ? (lane & 1) == 0 : (lane & 3) == 0);
+        const bool reshape = a.softcap > 0.f || a.slopes != nullptr || a.scores != nullptr;
         // row data, drafted positions and view of a run, asynchronously into the buffers of its parity
         auto fetch = [&](const Cursor& c, int par) {
             if (c.b < B) {
@@ -455,10 +435,36 @@ __global__ void __launch_bounds__(UGeo<P, N>::THREADS, 1) attn_umma(const AttnAr
             }
             asm volatile("cp.async.commit_group;" ::: "memory");
         };
+        // Converts this thread's slots of the packed rows in unit `u` and hands them to `put` (part j: 32 slots, 16
+        // registers); returns the row's largest exponent byte.
+        auto convert = [&](int u, auto put) {
+            const uint8_t* tile = smem + u * G_::UNIT;
+            uint32_t ew[2];
+            umma_exps<N16>(smem + G_::E_OFF + u * exp_unit + m_pos * row_e, row_e, ew);
+            UW g[(N16 ? 8 : 4) / H];
+            const int top = umma_row<P, N16, H>(ew, half, g);
+#pragma unroll
+            for (int j = 0; j < 4 / H; ++j) {
+                uint32_t r[16];
+                convert32<P>(tile, m_pos, 2 * half + j, g[N16 ? 2 * j : j], g[N16 ? 2 * j + 1 : j], r);
+                put(j, r);
+            }
+            return top;
+        };
+        auto convert_k = [&](int i) {
+            wait(b_kf(team, i), i / KS);
+            __syncwarp();
+            const int top = convert(team * RING + i % KS, [&](int j, const uint32_t (&r)[16]) { tmem_st<16>(tmt + G_::TM_K + half * 32 + 16 * j, r); });
+            tmem_wait_st();
+            tmem_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(b_k(team));
+            return top;
+        };
+
         Cursor c = seek(first_item), cn = c;
-        int unit = 2 * (least > 0 ? team : rank), round = 0;          // the ring's next unit of this team, and how often the ring went round
         fetch(c, 0);
-        int it = 0, run = 0;
+        int it = 0, run = 0, k_next = n_mine > 0 ? convert_k(0) : 0;
         while (it < n_mine) {
             const int b = c.b, hk = c.hr / a.n_row_tiles, rt = c.hr - hk * a.n_row_tiles, par = run & 1;
             const int k0 = c.k, k1 = min(c.n, k0 + n_mine - it), row0 = rt * N + half * C;
@@ -480,104 +486,83 @@ __global__ void __launch_bounds__(UGeo<P, N>::THREADS, 1) attn_umma(const AttnAr
 #pragma unroll
             for (int j = 0; j < C; ++j) l[j] = 0.f;
             for (int k = k0; k < k1; ++k, ++it) {
-                // ---- K to tensor memory (the product of the tile before has read it: waited for below, a tile ago), then, while the
-                // tensor cores are on S, V to shared memory.  (One loop for both: the code of a tile has to stay in the
-                // instruction cache.)
-                uint32_t top2[2];
-#pragma unroll 1
-                for (int kv = 0; kv < 2; ++kv) {
-                    wait(b_full + 8 * unit, round);
-                    if (kv == 1 && it > 0) wait(b_o(team), it - 1);          // the product of the tile before has read V and P
-                    __syncwarp();
-                    const uint8_t* tile = smem + unit * G_::UNIT;
-                    uint32_t ew[2];
-                    umma_exps<N16>(smem + G_::E_OFF + unit * exp_unit + m_pos * row_e, row_e, ew);
-                    UW g[(N16 ? 8 : 4) / H];
-                    const uint32_t top = (uint32_t)umma_row<P, N16, H>(ew, half, g);
-                    if (kv == 0) top2[0] = top; else top2[1] = top;
-#pragma unroll
-                    for (int j = 0; j < 4 / H; ++j) {
-                        uint32_t r[16];
-                        convert32<P>(tile, m_pos, 2 * half + j, g[N16 ? 2 * j : j], g[N16 ? 2 * j + 1 : j], r);
-                        if (kv == 0) {
-                            tmem_st<16>(tmt + G_::TM_K + half * 32 + 16 * j, r);
-                        } else {
-                            uint8_t* to = vline + (j >> 1) * (kUTile * 128);
-#pragma unroll
-                            for (int x = 0; x < 4; ++x)       // 16-byte pieces 4 j + x, swizzled
-                                *reinterpret_cast<uint4*>(to + (((4 * (j & 1) + x) ^ (m_pos & 7)) << 4)) = make_uint4(r[4 * x], r[4 * x + 1], r[4 * x + 2], r[4 * x + 3]);
-                        }
-                    }
-                    if (kv == 0) {
-                        tmem_wait_st();
-                        tmem_fence_before();
-                    }
-                    __syncwarp();
-                    if (lane == 0) {
-                        if (kv == 0) mbar_arrive(b_k(team));
-                        mbar_arrive(b_empty + 8 * unit);
-                    }
-                    if (kv == 0 && ++unit == UNITS) { unit = 0; ++round; }
-                }
-                unit += 2 * TEAMS - 1 - (it + 1 == least ? 2 * (team - rank) : 0);
-                while (unit >= UNITS) { unit -= UNITS; ++round; }
-                const uint32_t k_top = top2[0], v_top = top2[1];
-                // ---- scores
-                const int tt = tile_token(sv, k, kUTile), tok = tt + m_pos;
-                const float kf = __uint_as_float(k_top << 23), vf = __uint_as_float((uint32_t)max((int)v_top - 9, 0) << 23);
-                wait(b_s(team), it);
-                __syncwarp();
+                const uint32_t k_top = (uint32_t)k_next;
+                wait(b_s(team, it), it >> 1);                 // S of this tile is there, its K rows are used up
                 tmem_fence_after();
-                uint32_t raw[C];
-                tmem_ld<C>(tmt + G_::TM_S + half * C, raw);
-                tmem_wait_ld(raw);
-                float y[C];
+                if (it + 1 < n_mine) k_next = convert_k(it + 1);
+                if (it > 0) wait(b_o(team), it - 1);          // V and P of the tile before are used up
+                wait(b_vf(team, it), it / VS);
+                __syncwarp();
+                const uint32_t v_top = (uint32_t)convert(team * RING + KS + it % VS, [&](int j, const uint32_t (&r)[16]) {
 #pragma unroll
-                for (int j = 0; j < C; ++j) y[j] = __uint_as_float(raw[j]);
-                // ---- cap, bias, masks: y * mul in log2 units
-                float mul = up * to_log2 * kf;
-                if (a.softcap > 0.f) {
-                    mul = a.softcap * to_log2;
-                    const float in = cap_in * kf;
-#pragma unroll
-                    for (int j = 0; j < C; ++j) y[j] = 1.f - __fdividef(2.f, 1.f + ex2_approx(y[j] * in));      // tanh x = 1 - 2 / (1 + e^2x): about 2e-7 absolute
-                }
-                if (a.slopes != nullptr || !(tt + kUTile <= sv.ctx && (tt >= clear_lo || tt + kUTile <= sv.pf))) {
+                    for (int x = 0; x < 4; ++x)       // 16-byte pieces 4 j + x, swizzled
+                        *reinterpret_cast<uint4*>(vline + (j >> 1) * (kUTile * 128) + (((4 * (j & 1) + x) ^ (m_pos & 7)) << 4)) = make_uint4(r[4 * x], r[4 * x + 1], r[4 * x + 2], r[4 * x + 3]);
+                });
+                __syncwarp();
+                if (lane == 0) mbar_arrive(b_v(team));
+                // ---- scores
+                const uint32_t tm_s = tmt + G_::TM_S + (it & 1) * N + half * C;
+                const int tt = tile_token(sv, k, kUTile);
+                float mul = up * to_log2 * __uint_as_float(k_top << 23);
+                if (reshape || !(tt + kUTile <= sv.ctx && (tt >= clear_lo || tt + kUTile <= sv.pf))) {
+                    // cap, bias and masks, in tensor memory: log2 units afterwards
+                    const int tok = tt + m_pos;
                     const bool in_ctx = tok < sv.ctx;
                     const int jd = in_ctx ? 0 : min(tok - sv.ctx, kAttnMaxDraft - 1);
                     const bool drafted = !in_ctx && tok - sv.ctx < sv.nd;
                     const int kpos = in_ctx || !drafted ? tok : dpos[jd];
                     const bool always = tok < sv.pf, from = tok >= sv.first;
+                    const float in = cap_in * __uint_as_float(k_top << 23);
+                    if (a.softcap > 0.f) mul = a.softcap * to_log2;
+#pragma unroll 1
+                    for (int j = 0; j < C; j += 8) {
+                        uint32_t r[8];
+                        tmem_ld<8>(tm_s + j, r);
+                        tmem_wait_ld(r);
+                        float* to = a.scores ? a.scores + ((int64_t)b * a.n_q_heads + hk * a.group + row0 + j) * max_seq + tok : nullptr;
 #pragma unroll
-                    for (int j = 0; j < C; ++j) {
-                        const RowInfo x = ri[j];
-                        const int dist = x.pos - kpos;
-                        const bool near = a.window == 0 || dist < a.window;
-                        const bool bit = (((jd < 32 ? x.m0 : x.m1) >> (jd & 31)) & 1u) != 0u;
-                        const bool see = in_ctx ? (from && near) || always : drafted && bit && near;
-                        y[j] = see ? y[j] * mul - x.slope * to_log2 * (float)dist : -INFINITY;
+                        for (int e = 0; e < 8; ++e) {
+                            float y = __uint_as_float(r[e]);
+                            if (a.softcap > 0.f) y = 1.f - __fdividef(2.f, 1.f + ex2_approx(y * in));      // tanh x = 1 - 2 / (1 + e^2x): about 2e-7 absolute
+                            const RowInfo x = ri[j + e];
+                            const int dist = x.pos - kpos;
+                            const bool near = a.window == 0 || dist < a.window;
+                            const bool bit = (((jd < 32 ? x.m0 : x.m1) >> (jd & 31)) & 1u) != 0u;
+                            const bool see = in_ctx ? (from && near) || always : drafted && bit && near;
+                            y = see ? y * mul - x.slope * to_log2 * (float)dist : -INFINITY;
+                            if (to && tok < max_seq && row0 + j + e < R) to[(int64_t)e * max_seq] = y;
+                            r[e] = __float_as_uint(y);
+                        }
+                        tmem_st<8>(tm_s + j, r);
                     }
+                    tmem_wait_st();
                     mul = 1.f;
                 }
-                if (a.scores && tok < max_seq) {
-                    float* to = a.scores + ((int64_t)b * a.n_q_heads + hk * a.group + row0) * max_seq + tok;
+                // ---- running softmax against the references, which are raised at most once per tile
+                float y[C];
+#pragma unroll 1
+                for (int pass = 0;; ++pass) {
+                    uint32_t raw[C];
+                    tmem_ld<C>(tm_s, raw);
+                    tmem_wait_ld(raw);
+                    float top = -INFINITY;
 #pragma unroll
-                    for (int j = 0; j < C; ++j)
-                        if (row0 + j < R) to[(int64_t)j * max_seq] = y[j] * mul;
-                }
-                // ---- running softmax against the references
-                float top = -INFINITY;
+                    for (int j = 0; j < C; ++j) {
+                        y[j] = fmaf(__uint_as_float(raw[j]), mul, -mref[j]);
+                        top = fmaxf(top, y[j]);
+                    }
+                    if (pass != 0 || !named_any(bar_id, 128, top > 8.f || *unset != 0)) break;
+#pragma unroll 1
+                    for (int j = 0; j < C; j += 8) {
+                        uint32_t r[8];
+                        tmem_ld<8>(tm_s + j, r);
+                        tmem_wait_ld(r);
+                        float v[8];
 #pragma unroll
-                for (int j = 0; j < C; ++j) {
-                    y[j] = fmaf(y[j], mul, -mref[j]);
-                    top = fmaxf(top, y[j]);
-                }
-                if (named_any(bar_id, 128, top > 8.f || *unset != 0)) {
-                    float v[C];
-#pragma unroll
-                    for (int j = 0; j < C; ++j) v[j] = y[j];
-                    const float mine = across_lanes<C, true>(v, lane);
-                    if (my_first) red[w4 * C + my_col] = mine;
+                        for (int e = 0; e < 8; ++e) v[e] = fmaf(__uint_as_float(r[e]), mul, -mref[j + e]);
+                        const float mine = across_lanes<8, true>(v, lane);
+                        if ((lane & 3) == 0) red[w4 * C + j + (lane >> 2)] = mine;
+                    }
                     named_sync(bar_id, 128);
                     if (m_pos < 32) {
                         bool none = false;
@@ -586,7 +571,6 @@ __global__ void __launch_bounds__(UGeo<P, N>::THREADS, 1) attn_umma(const AttnAr
                             const bool is_unset = (*unset >> lane) & 1;
                             none = is_unset && x == -INFINITY;
                             const float step = none ? 0.f : (is_unset ? x : fmaxf(x, 0.f));
-                            mstep[lane] = step;
                             mfac[lane] = is_unset ? 1.f : ex2_approx(-step);      // (a row that has seen nothing has sums 0)
                             mref[lane] += step;
                         }
@@ -595,13 +579,10 @@ __global__ void __launch_bounds__(UGeo<P, N>::THREADS, 1) attn_umma(const AttnAr
                     }
                     named_sync(bar_id, 128);
 #pragma unroll
-                    for (int j = 0; j < C; ++j) {
-                        y[j] -= mstep[j];
-                        l[j] *= mfac[j];
-                    }
+                    for (int j = 0; j < C; ++j) l[j] *= mfac[j];
                     if (k > k0) {          // (the product of the tile before is done: waited for above)
                         tmem_fence_after();
-#pragma unroll
+#pragma unroll 1
                         for (int j = 0; j < C; j += 8) {
                             uint32_t o[8];
                             tmem_ld<8>(tm_o + j, o);
@@ -615,6 +596,7 @@ __global__ void __launch_bounds__(UGeo<P, N>::THREADS, 1) attn_umma(const AttnAr
                 }
                 // ---- P: weights of this token times its V row's 2^E, bf16, a line of 2 N bytes
                 uint8_t* pb = smem + G_::P_OFF + team * G_::P_BYTES;
+                const float vf = __uint_as_float((uint32_t)max((int)v_top - 9, 0) << 23);
 #pragma unroll
                 for (int j = 0; j < C; j += 8) {
                     uint32_t w[4];
@@ -636,11 +618,12 @@ __global__ void __launch_bounds__(UGeo<P, N>::THREADS, 1) attn_umma(const AttnAr
             // ---- the run's result: this thread holds slot umma_slot(m_pos) of C rows
             {
                 const float mine = across_lanes<C, false>(l, lane);
-                if (my_first) red[w4 * C + my_col] = mine;
+                constexpr int GAP = 32 / C;                   // lanes that end up with the same column
+                if (lane % GAP == 0) red[w4 * C + lane / GAP] = mine;
             }
             named_sync(bar_id, 128);
             const bool whole = k0 == 0 && k1 == c.n;
-            const int slot = umma_slot<P>(m_pos);
+            const int slot_of = umma_slot<P>(m_pos);
             float* part = a.partials + ((int64_t)(2 * me + (k0 == 0 ? 1 : 0)) * a.part_rows + half * C) * kAttnPart;
             if (m_pos < C) {
                 const int row = row0 + m_pos;
@@ -661,7 +644,7 @@ __global__ void __launch_bounds__(UGeo<P, N>::THREADS, 1) attn_umma(const AttnAr
             __syncwarp();
             tmem_fence_after();
             named_sync(bar_id, 128);
-            const int ch = a.inv_perm_v ? chan[slot] : slot;
+            const int ch = a.inv_perm_v ? chan[slot_of] : slot_of;
 #pragma unroll 1
             for (int j = 0; j < C; j += 8) {
                 uint32_t o[8];
@@ -678,7 +661,7 @@ __global__ void __launch_bounds__(UGeo<P, N>::THREADS, 1) attn_umma(const AttnAr
                         static_cast<__nv_bfloat16*>(a.out)[(((int64_t)b * a.n_draft + i) * a.n_q_heads + hq) * D + ch] =
                             __float2bfloat16_rn(live ? __uint_as_float(o[e]) * (a.out_up / ls) : 0.f);
                     } else {
-                        part[(j + e) * kAttnPart + slot] = __uint_as_float(o[e]);
+                        part[(j + e) * kAttnPart + slot_of] = __uint_as_float(o[e]);
                     }
                 }
             }
