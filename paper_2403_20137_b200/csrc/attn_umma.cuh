@@ -106,11 +106,11 @@ struct UW {
 };
 template <int P>
 __device__ __forceinline__ UW umma_weights(int below) {      // steps of two below the row's largest exponent
-    const uint32_t d = (uint32_t)min(below, 100) * 0x00800080u;
+    const uint32_t d = (uint32_t)min(below, 100);
     UW w;
-    w.s = 0x7E007E00u - d;                                             // 2^(133 - 8 - d)
-    w.s2 = (P == 4 ? 0x7C007C00u : 0x7D007D00u) - d;                   // / 16, / 4
-    w.c = (P == 4 ? 0xBD00BD00u : P == 6 ? 0xBE00BE00u : 0xBF00BF00u) - d;     // -8, -32, -128 times 2^(-8 - d)
+    w.s = 0x7E007E00u - d * 0x00800080u;                                             // 2^(133 - 8 - d)
+    w.s2 = (P == 4 ? 0x7C007C00u : 0x7D007D00u) - d * 0x00800080u;                   // / 16, / 4
+    w.c = (P == 4 ? 0xBD00BD00u : P == 6 ? 0xBE00BE00u : 0xBF00BF00u) - d * 0x00800080u;     // -8, -32, -128 times 2^(-8 - d)
     return w;
 }
 // Exponent bytes of a row as (byte j: slots 32 j ..) or, for blocks of 16, two words (byte j: slots 16 j ..).
@@ -142,12 +142,19 @@ __device__ __forceinline__ int umma_row(const uint32_t (&w)[2], int half, UW (&g
     }
     return min(top, 254);
 }
-// 32 slots (four 16-byte pieces of bf16) of a packed row, from slot 32 i on.
+// Where a thread finds the row `row` of a unit: the offset whose exclusive or with 16 i (bytes of the row, 16-byte pieces)
+// is the piece's place (units start on multiples of 1024).  96-byte rows are not swizzled.
 template <int P>
-__device__ __forceinline__ void convert32(const uint8_t* tile, int row, int i, const UW& g0, const UW& g1, uint32_t (&r)[16]) {
+__device__ __forceinline__ uint32_t row_place(int row) {
+    if (P == 4) return (row >> 1) * 128 + (((row & 1) << 6) ^ (((row >> 1) & 7) << 4));
+    if (P == 8) return row * 128 + ((row & 7) << 4);
+    return row * 96;
+}
+// 32 slots (four 16-byte pieces of bf16) of a packed row, from slot 32 i on; `at`: unit plus row_place.
+template <int P>
+__device__ __forceinline__ void convert32(uint32_t at, int i, const UW& g0, const UW& g1, uint32_t (&r)[16]) {
     if (P == 4) {
-        const int line = row >> 1, at = ((row & 1) << 6) ^ ((line & 7) << 4);
-        const uint4 x = *reinterpret_cast<const uint4*>(tile + line * 128 + (at ^ (16 * i)));
+        const uint4 x = lds128(at ^ (16 * i));
         const uint32_t w[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -161,7 +168,7 @@ __device__ __forceinline__ void convert32(const uint8_t* tile, int row, int i, c
     } else if (P == 8) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const uint4 x = *reinterpret_cast<const uint4*>(tile + row * 128 + ((32 * i + 16 * h) ^ ((row & 7) << 4)));
+            const uint4 x = lds128(at ^ (32 * i + 16 * h));
             const uint32_t w[4] = {x.x, x.y, x.z, x.w};
             const UW& g = h ? g1 : g0;
 #pragma unroll
@@ -174,7 +181,7 @@ __device__ __forceinline__ void convert32(const uint8_t* tile, int row, int i, c
         uint32_t w[6];
 #pragma unroll
         for (int j = 0; j < 3; ++j) {
-            const uint2 x = *reinterpret_cast<const uint2*>(tile + row * 96 + 24 * i + 8 * j);
+            const uint2 x = lds64(at + 24 * i + 8 * j);
             w[2 * j] = x.x;
             w[2 * j + 1] = x.y;
         }
@@ -416,13 +423,15 @@ __global__ void __launch_bounds__(UGeo<P, N>::THREADS, 1) attn_umma(const AttnAr
               *lsum = fl + G_::F_SUM + wg * C, *red = fl + G_::F_RED + wg * 4 * C;
         int* chan = reinterpret_cast<int*>(fl + G_::F_CHAN) + wg * D;
         int* unset = reinterpret_cast<int*>(fl + G_::F_UNSET) + wg;         // rows that have seen nothing yet, as a bit mask
-        uint8_t* vline = smem + G_::V_OFF + team * G_::V_BYTES + half * (kUTile * 128) + m_pos * 128;       // (a panel holds 64 slots)
+        // places whose exclusive or with 16 times the piece's number is the piece's: packed row, V row (panels of 64 slots), P line
+        const uint32_t place = row_place<P>(m_pos);
+        const uint32_t vline = smem_u32(smem) + G_::V_OFF + team * G_::V_BYTES + half * (kUTile * 128) + m_pos * 128 + ((m_pos & 7) << 4);
+        const uint32_t pline = smem_u32(smem) + G_::P_OFF + team * G_::P_BYTES + ((m_pos * SWP) ^ ((((m_pos * SWP) >> 7) & (SWP / 16 - 1)) << 4));
         int first_item;
         const int n_mine = range(team, first_item), me = blockIdx.x + team * gridDim.x;
         const int R = a.n_draft * a.group;
         const float up = a.scale * (P == 4 ? 64.f : P == 6 ? 16.f : 4.f), to_log2 = 1.4426950408889634f;      // 2^8 2^-(P-2)
         const float cap_in = a.softcap > 0.f ? up / a.softcap * 2.8853900817779268f : 0.f;
-        const bool reshape = a.softcap > 0.f || a.slopes != nullptr || a.scores != nullptr;
         // row data, drafted positions and view of a run, asynchronously into the buffers of its parity
         auto fetch = [&](const Cursor& c, int par) {
             if (c.b < B) {
@@ -438,7 +447,7 @@ __global__ void __launch_bounds__(UGeo<P, N>::THREADS, 1) attn_umma(const AttnAr
         // Converts this thread's slots of the packed rows in unit `u` and hands them to `put` (part j: 32 slots, 16
         // registers); returns the row's largest exponent byte.
         auto convert = [&](int u, auto put) {
-            const uint8_t* tile = smem + u * G_::UNIT;
+            const uint32_t at = smem_u32(smem) + u * G_::UNIT + place;
             uint32_t ew[2];
             umma_exps<N16>(smem + G_::E_OFF + u * exp_unit + m_pos * row_e, row_e, ew);
             UW g[(N16 ? 8 : 4) / H];
@@ -446,7 +455,7 @@ __global__ void __launch_bounds__(UGeo<P, N>::THREADS, 1) attn_umma(const AttnAr
 #pragma unroll
             for (int j = 0; j < 4 / H; ++j) {
                 uint32_t r[16];
-                convert32<P>(tile, m_pos, 2 * half + j, g[N16 ? 2 * j : j], g[N16 ? 2 * j + 1 : j], r);
+                convert32<P>(at, 2 * half + j, g[N16 ? 2 * j : j], g[N16 ? 2 * j + 1 : j], r);
                 put(j, r);
             }
             return top;
@@ -482,9 +491,10 @@ __global__ void __launch_bounds__(UGeo<P, N>::THREADS, 1) attn_umma(const AttnAr
             const uint32_t tm_o = tmt + G_::TM_O + half * C;
             int clear_lo = sv.first;      // tokens [clear_lo, ctx) and [0, pf) are visible to every row
             if (a.window > 0) clear_lo = max(clear_lo, sv.ctx + (a.tree ? a.n_draft - 1 : -1) - a.window + 1);
-            float l[C];
+            F2 l[C / 2];
 #pragma unroll
-            for (int j = 0; j < C; ++j) l[j] = 0.f;
+            for (int j = 0; j < C / 2; ++j) l[j] = f2(0.f, 0.f);
+            bool behind = true;           // a row of the group has seen nothing yet
             for (int k = k0; k < k1; ++k, ++it) {
                 const uint32_t k_top = (uint32_t)k_next;
                 wait(b_s(team, it), it >> 1);                 // S of this tile is there, its K rows are used up
@@ -496,7 +506,7 @@ __global__ void __launch_bounds__(UGeo<P, N>::THREADS, 1) attn_umma(const AttnAr
                 const uint32_t v_top = (uint32_t)convert(team * RING + KS + it % VS, [&](int j, const uint32_t (&r)[16]) {
 #pragma unroll
                     for (int x = 0; x < 4; ++x)       // 16-byte pieces 4 j + x, swizzled
-                        *reinterpret_cast<uint4*>(vline + (j >> 1) * (kUTile * 128) + (((4 * (j & 1) + x) ^ (m_pos & 7)) << 4)) = make_uint4(r[4 * x], r[4 * x + 1], r[4 * x + 2], r[4 * x + 3]);
+                        sts128((vline ^ ((4 * (j & 1) + x) << 4)) + (j >> 1) * (kUTile * 128), r[4 * x], r[4 * x + 1], r[4 * x + 2], r[4 * x + 3]);
                 });
                 __syncwarp();
                 if (lane == 0) mbar_arrive(b_v(team));
@@ -504,16 +514,30 @@ __global__ void __launch_bounds__(UGeo<P, N>::THREADS, 1) attn_umma(const AttnAr
                 const uint32_t tm_s = tmt + G_::TM_S + (it & 1) * N + half * C;
                 const int tt = tile_token(sv, k, kUTile);
                 float mul = up * to_log2 * __uint_as_float(k_top << 23);
-                if (reshape || !(tt + kUTile <= sv.ctx && (tt >= clear_lo || tt + kUTile <= sv.pf))) {
-                    // cap, bias and masks, in tensor memory: log2 units afterwards
+                if (a.softcap > 0.f) {       // cap, in tensor memory
+                    const float in = cap_in * __uint_as_float(k_top << 23);
+                    mul = a.softcap * to_log2;
+#pragma unroll 1
+                    for (int j = 0; j < C; j += 8) {
+                        uint32_t r[8];
+                        tmem_ld<8>(tm_s + j, r);
+                        tmem_wait_ld(r);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e)      // tanh x = 1 - 2 / (1 + e^2x): about 2e-7 absolute
+                            r[e] = __float_as_uint(fmaf(-2.f, rcp_approx(1.f + ex2_approx(__uint_as_float(r[e]) * in)), 1.f));
+                        tmem_st<8>(tm_s + j, r);
+                    }
+                    tmem_wait_st();
+                }
+                const bool masked = a.slopes != nullptr || !(tt + kUTile <= sv.ctx && (tt >= clear_lo || tt + kUTile <= sv.pf));
+                if (masked || a.scores) {
+                    // bias and masks, in tensor memory: log2 units afterwards
                     const int tok = tt + m_pos;
                     const bool in_ctx = tok < sv.ctx;
                     const int jd = in_ctx ? 0 : min(tok - sv.ctx, kAttnMaxDraft - 1);
                     const bool drafted = !in_ctx && tok - sv.ctx < sv.nd;
                     const int kpos = in_ctx || !drafted ? tok : dpos[jd];
                     const bool always = tok < sv.pf, from = tok >= sv.first;
-                    const float in = cap_in * __uint_as_float(k_top << 23);
-                    if (a.softcap > 0.f) mul = a.softcap * to_log2;
 #pragma unroll 1
                     for (int j = 0; j < C; j += 8) {
                         uint32_t r[8];
@@ -523,23 +547,26 @@ __global__ void __launch_bounds__(UGeo<P, N>::THREADS, 1) attn_umma(const AttnAr
 #pragma unroll
                         for (int e = 0; e < 8; ++e) {
                             float y = __uint_as_float(r[e]);
-                            if (a.softcap > 0.f) y = 1.f - __fdividef(2.f, 1.f + ex2_approx(y * in));      // tanh x = 1 - 2 / (1 + e^2x): about 2e-7 absolute
                             const RowInfo x = ri[j + e];
                             const int dist = x.pos - kpos;
                             const bool near = a.window == 0 || dist < a.window;
                             const bool bit = (((jd < 32 ? x.m0 : x.m1) >> (jd & 31)) & 1u) != 0u;
                             const bool see = in_ctx ? (from && near) || always : drafted && bit && near;
-                            y = see ? y * mul - x.slope * to_log2 * (float)dist : -INFINITY;
+                            y *= mul;
+                            if (masked) y = see ? y - x.slope * to_log2 * (float)dist : -INFINITY;
                             if (to && tok < max_seq && row0 + j + e < R) to[(int64_t)e * max_seq] = y;
                             r[e] = __float_as_uint(y);
                         }
-                        tmem_st<8>(tm_s + j, r);
+                        if (masked) tmem_st<8>(tm_s + j, r);
                     }
-                    tmem_wait_st();
-                    mul = 1.f;
+                    if (masked) {
+                        tmem_wait_st();
+                        mul = 1.f;
+                    }
                 }
                 // ---- running softmax against the references, which are raised at most once per tile
-                float y[C];
+                F2 y[C / 2];
+                const F2 mul2 = f2(mul, mul);
 #pragma unroll 1
                 for (int pass = 0;; ++pass) {
                     uint32_t raw[C];
@@ -547,11 +574,17 @@ __global__ void __launch_bounds__(UGeo<P, N>::THREADS, 1) attn_umma(const AttnAr
                     tmem_wait_ld(raw);
                     float top = -INFINITY;
 #pragma unroll
-                    for (int j = 0; j < C; ++j) {
-                        y[j] = fmaf(__uint_as_float(raw[j]), mul, -mref[j]);
-                        top = fmaxf(top, y[j]);
+                    for (int j = 0; j < C; j += 4) {
+                        const float4 m = *reinterpret_cast<const float4*>(mref + j);       // (negative references)
+                        y[j / 2] = f2_fma(f2(__uint_as_float(raw[j]), __uint_as_float(raw[j + 1])), mul2, f2(m.x, m.y));
+                        y[j / 2 + 1] = f2_fma(f2(__uint_as_float(raw[j + 2]), __uint_as_float(raw[j + 3])), mul2, f2(m.z, m.w));
+                        float y0, y1;
+                        f2_split(y[j / 2], y0, y1);
+                        top = max3(top, y0, y1);
+                        f2_split(y[j / 2 + 1], y0, y1);
+                        top = max3(top, y0, y1);
                     }
-                    if (pass != 0 || !named_any(bar_id, 128, top > 8.f || *unset != 0)) break;
+                    if (pass != 0 || !named_any(bar_id, 128, top > 8.f || behind)) break;
 #pragma unroll 1
                     for (int j = 0; j < C; j += 8) {
                         uint32_t r[8];
@@ -559,7 +592,7 @@ __global__ void __launch_bounds__(UGeo<P, N>::THREADS, 1) attn_umma(const AttnAr
                         tmem_wait_ld(r);
                         float v[8];
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) v[e] = fmaf(__uint_as_float(r[e]), mul, -mref[j + e]);
+                        for (int e = 0; e < 8; ++e) v[e] = fmaf(__uint_as_float(r[e]), mul, mref[j + e]);
                         const float mine = across_lanes<8, true>(v, lane);
                         if ((lane & 3) == 0) red[w4 * C + j + (lane >> 2)] = mine;
                     }
@@ -572,14 +605,15 @@ __global__ void __launch_bounds__(UGeo<P, N>::THREADS, 1) attn_umma(const AttnAr
                             none = is_unset && x == -INFINITY;
                             const float step = none ? 0.f : (is_unset ? x : fmaxf(x, 0.f));
                             mfac[lane] = is_unset ? 1.f : ex2_approx(-step);      // (a row that has seen nothing has sums 0)
-                            mref[lane] += step;
+                            mref[lane] -= step;
                         }
                         const uint32_t left = __ballot_sync(0xffffffffu, none);
                         if (lane == 0) *unset = (int)left;
                     }
                     named_sync(bar_id, 128);
+                    behind = *unset != 0;
 #pragma unroll
-                    for (int j = 0; j < C; ++j) l[j] *= mfac[j];
+                    for (int j = 0; j < C; j += 2) l[j / 2] = f2_mul(l[j / 2], *reinterpret_cast<const F2*>(mfac + j));
                     if (k > k0) {          // (the product of the tile before is done: waited for above)
                         tmem_fence_after();
 #pragma unroll 1
@@ -595,20 +629,22 @@ __global__ void __launch_bounds__(UGeo<P, N>::THREADS, 1) attn_umma(const AttnAr
                     }
                 }
                 // ---- P: weights of this token times its V row's 2^E, bf16, a line of 2 N bytes
-                uint8_t* pb = smem + G_::P_OFF + team * G_::P_BYTES;
                 const float vf = __uint_as_float((uint32_t)max((int)v_top - 9, 0) << 23);
+                const F2 vf2 = f2(vf, vf);
 #pragma unroll
                 for (int j = 0; j < C; j += 8) {
                     uint32_t w[4];
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        const float p0 = ex2_approx(y[j + 2 * e]), p1 = ex2_approx(y[j + 2 * e + 1]);
-                        l[j + 2 * e] += p0;
-                        l[j + 2 * e + 1] += p1;
-                        w[e] = pack_bf16x2_rn(p0 * vf, p1 * vf);
+                        float y0, y1;
+                        f2_split(y[j / 2 + e], y0, y1);
+                        const F2 p = f2(ex2_approx(y0), ex2_approx(y1));
+                        l[j / 2 + e] = f2_add(l[j / 2 + e], p);
+                        float p0, p1;
+                        f2_split(f2_mul(p, vf2), p0, p1);
+                        w[e] = pack_bf16x2_rn(p0, p1);
                     }
-                    const uint32_t off = m_pos * SWP + (half * C + j) * 2;
-                    *reinterpret_cast<uint4*>(pb + (off ^ (((off >> 7) & (SWP / 16 - 1)) << 4))) = make_uint4(w[0], w[1], w[2], w[3]);
+                    sts128(pline ^ ((half * C + j) * 2), w[0], w[1], w[2], w[3]);
                 }
                 fence_async_shared();
                 tmem_fence_before();
@@ -617,7 +653,10 @@ __global__ void __launch_bounds__(UGeo<P, N>::THREADS, 1) attn_umma(const AttnAr
             }
             // ---- the run's result: this thread holds slot umma_slot(m_pos) of C rows
             {
-                const float mine = across_lanes<C, false>(l, lane);
+                float v[C];
+#pragma unroll
+                for (int j = 0; j < C / 2; ++j) f2_split(l[j], v[2 * j], v[2 * j + 1]);
+                const float mine = across_lanes<C, false>(v, lane);
                 constexpr int GAP = 32 / C;                   // lanes that end up with the same column
                 if (lane % GAP == 0) red[w4 * C + lane / GAP] = mine;
             }
@@ -628,7 +667,7 @@ __global__ void __launch_bounds__(UGeo<P, N>::THREADS, 1) attn_umma(const AttnAr
             if (m_pos < C) {
                 const int row = row0 + m_pos;
                 const float ls = red[m_pos] + red[C + m_pos] + red[2 * C + m_pos] + red[3 * C + m_pos];
-                const float m = ((*unset >> m_pos) & 1) ? -3.4028235e38f : mref[m_pos];
+                const float m = ((*unset >> m_pos) & 1) ? -3.4028235e38f : -mref[m_pos];
                 lsum[m_pos] = ls;
                 if (row < R) {
                     if (!whole) {
