@@ -530,7 +530,7 @@ __global__ void __launch_bounds__(UGeo<P, N>::THREADS, 1) attn_umma(const AttnAr
                     tmem_wait_st();
                 }
                 const bool masked = a.slopes != nullptr || !(tt + kUTile <= sv.ctx && (tt >= clear_lo || tt + kUTile <= sv.pf));
-                if (masked || a.scores) {
+                if (masked) {
                     // bias and masks, in tensor memory: log2 units afterwards
                     const int tok = tt + m_pos;
                     const bool in_ctx = tok < sv.ctx;
@@ -543,7 +543,6 @@ __global__ void __launch_bounds__(UGeo<P, N>::THREADS, 1) attn_umma(const AttnAr
                         uint32_t r[8];
                         tmem_ld<8>(tm_s + j, r);
                         tmem_wait_ld(r);
-                        float* to = a.scores ? a.scores + ((int64_t)b * a.n_q_heads + hk * a.group + row0 + j) * max_seq + tok : nullptr;
 #pragma unroll
                         for (int e = 0; e < 8; ++e) {
                             float y = __uint_as_float(r[e]);
@@ -552,17 +551,13 @@ __global__ void __launch_bounds__(UGeo<P, N>::THREADS, 1) attn_umma(const AttnAr
                             const bool near = a.window == 0 || dist < a.window;
                             const bool bit = (((jd < 32 ? x.m0 : x.m1) >> (jd & 31)) & 1u) != 0u;
                             const bool see = in_ctx ? (from && near) || always : drafted && bit && near;
-                            y *= mul;
-                            if (masked) y = see ? y - x.slope * to_log2 * (float)dist : -INFINITY;
-                            if (to && tok < max_seq && row0 + j + e < R) to[(int64_t)e * max_seq] = y;
+                            y = see ? y * mul - x.slope * to_log2 * (float)dist : -INFINITY;
                             r[e] = __float_as_uint(y);
                         }
-                        if (masked) tmem_st<8>(tm_s + j, r);
+                        tmem_st<8>(tm_s + j, r);
                     }
-                    if (masked) {
-                        tmem_wait_st();
-                        mul = 1.f;
-                    }
+                    tmem_wait_st();
+                    mul = 1.f;
                 }
                 // ---- running softmax against the references, which are raised at most once per tile
                 F2 y[C / 2];
@@ -627,6 +622,16 @@ __global__ void __launch_bounds__(UGeo<P, N>::THREADS, 1) attn_umma(const AttnAr
                         }
                         tmem_wait_st();
                     }
+                }
+                if (a.scores && tt + m_pos < max_seq) {       // for the weight pass: y against the reference, plus the reference
+                    float* to = a.scores + ((int64_t)b * a.n_q_heads + hk * a.group + row0) * max_seq + tt + m_pos;
+#pragma unroll
+                    for (int j = 0; j < (C < 8 ? C : 8); ++j)            // (one token: at most eight rows, the first)
+                        if (row0 + j < R) {
+                            float y0, y1;
+                            f2_split(y[j / 2], y0, y1);
+                            to[(int64_t)j * max_seq] = (j & 1 ? y1 : y0) - mref[j];
+                        }
                 }
                 // ---- P: weights of this token times its V row's 2^E, bf16, a line of 2 N bytes
                 const float vf = __uint_as_float((uint32_t)max((int)v_top - 9, 0) << 23);

@@ -1,11 +1,15 @@
 // Dropping and moving cached rows: eviction by accumulated attention weight, and the gather of listed rows (the
 // accepted branch of a drafted tree) in all four planes of the packed cache.
+#include <cooperative_groups.h>
+
 #include "common.cuh"
 
 namespace kvbfp {
 namespace {
 
-constexpr int kSelThreads = 1024, kSelWarps = kSelThreads / 32, kHistCopies = 8;
+constexpr int kSelThreads = 512, kSelWarps = kSelThreads / 32;
+constexpr int kSelKeys = 16;                 // keys a thread keeps in registers
+constexpr int kSelBins = 2048, kSelCluster = 8;
 
 // Weights in the order of unsigned integers: -0 as 0, NaN below everything.
 __device__ __forceinline__ uint32_t mass_key(float x) {
@@ -14,101 +18,151 @@ __device__ __forceinline__ uint32_t mass_key(float x) {
     return (u >> 31) ? ~u : (u | 0x80000000u);
 }
 
-// A block per (sequence, kv head): the rows to keep, in position order.  The heaviest `need` of the middle region are
-// found by radix selection (four digits of eight bits, histograms in shared memory); of equals to the threshold the
-// lowest positions are kept.  Each warp owns a contiguous piece of the region, so one scan over the warps' counts
-// places every kept row.
-__global__ void __launch_bounds__(kSelThreads) evict_select(const float* mass, const int32_t* seq_lens,
-                                                            int max_seq, int n_heads, int budget, int n_sink, int n_recent,
-                                                            int32_t* kept, uint32_t* status) {
-    __shared__ uint32_t hist[kHistCopies][256];
-    __shared__ uint32_t s_digit, s_need;
-    __shared__ int s_gt[kSelWarps], s_eq[kSelWarps];
+// The rows to keep of one (sequence, kv head), in position order, by a block or (CS > 1) a cluster of blocks that share
+// the region.  The heaviest `need` of the middle region are found by radix selection: three digits of 11, 11 and 10 bits,
+// a histogram each in shared memory, the cluster's summed through distributed shared memory; of equals to the threshold
+// the lowest positions are kept.  Each warp owns a contiguous piece of the region, so one scan over the warps' counts
+// places every kept row.  A thread keeps its keys in registers where they fit (CACHED: up to 8192 rows a block) and reads
+// them again otherwise.  What bounds it is the chain of passes, not the bytes (4 per row): a digit of 11 bits spreads the
+// exponents that eight bits pile up in a few bins, and takes one pass less.
+template <int CS, bool CACHED>
+__global__ void __launch_bounds__(kSelThreads) evict_select(const float* mass, const int32_t* seq_lens, int max_seq, int n_heads,
+                                                            int budget, int n_sink, int n_recent, int32_t* kept, uint32_t* status) {
+    __shared__ uint32_t hist[3][kSelBins];
+    __shared__ uint32_t s_scan[kSelWarps], s_digit, s_need;
+    __shared__ int s_gt[kSelWarps], s_eq[kSelWarps], s_tot[2];
+    namespace cg = cooperative_groups;
+    const int pair = blockIdx.x / CS, rank = blockIdx.x % CS, b = pair / n_heads, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    for (int i = tid; i < 3 * kSelBins; i += kSelThreads) (&hist[0][0])[i] = 0;
+    __syncthreads();
     pdl_wait();
     pdl_trigger();
-    const int pair = blockIdx.x, b = pair / n_heads, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int raw = seq_lens[b], len = min(max(raw, 0), max_seq);
-    if (raw != len && tid == 0) raise_flag(status, KVBFP_FLAG_POSITION);
+    if (raw != len && tid == 0 && rank == 0) raise_flag(status, KVBFP_FLAG_POSITION);
     int32_t* out = kept + (int64_t)pair * budget;
-    if (len <= budget) {
-        for (int i = tid; i < budget; i += kSelThreads) out[i] = i < len ? i : -1;
+    if (len <= budget) {                                          // (alike in the whole cluster)
+        for (int i = rank * kSelThreads + tid; i < budget; i += CS * kSelThreads) out[i] = i < len ? i : -1;
         return;
     }
     const int m0 = n_sink, m1 = len - n_recent;                   // the middle region; m1 - m0 > need
     uint32_t need = (uint32_t)(budget - n_sink - n_recent);
-    for (int i = tid; i < n_sink; i += kSelThreads) out[i] = i;
-    for (int i = tid; i < n_recent; i += kSelThreads) out[budget - n_recent + i] = m1 + i;
+    for (int i = rank * kSelThreads + tid; i < n_sink; i += CS * kSelThreads) out[i] = i;
+    for (int i = rank * kSelThreads + tid; i < n_recent; i += CS * kSelThreads) out[budget - n_recent + i] = m1 + i;
     if (need == 0) return;
     const float* x = mass + (int64_t)pair * max_seq;
-    uint32_t thr = 0;
-    for (int shift = 24; shift >= 0; shift -= 8) {
-        for (int i = tid; i < kHistCopies * 256; i += kSelThreads) (&hist[0][0])[i] = 0;
-        __syncthreads();
-        uint32_t* h = hist[warp % kHistCopies];
-#pragma unroll 8
-        for (int i = m0 + tid; i < m1; i += kSelThreads) {
-            const uint32_t key = mass_key(x[i]);
-            if (shift == 24 || (key >> (shift + 8)) == (thr >> (shift + 8))) atomicAdd(&h[(key >> shift) & 255u], 1u);
+    // this warp's piece [w0, w1): the region in CS * kSelWarps pieces of whole 32s
+    const int per = ((m1 - m0 + CS * kSelWarps - 1) / (CS * kSelWarps) + 31) & ~31;
+    const int w0 = min(m0 + (rank * kSelWarps + warp) * per, m1), w1 = min(w0 + per, m1);
+    uint32_t keys[CACHED ? kSelKeys : 1];
+    if (CACHED) {
+#pragma unroll
+        for (int j = 0; j < kSelKeys; ++j) {
+            const int i = w0 + 32 * j + lane;
+            keys[CACHED ? j : 0] = i < w1 ? mass_key(x[i]) : 0u;
         }
+    }
+    // runs f(position, key, in the piece) over the warp's piece, whole warps at a time
+    auto each = [&](auto f) {
+        if (CACHED) {
+#pragma unroll
+            for (int j = 0; j < kSelKeys; ++j)
+                if (w0 + 32 * j < w1) f(w0 + 32 * j + lane, keys[CACHED ? j : 0], w0 + 32 * j + lane < w1);
+        } else {
+#pragma unroll 8
+            for (int i = w0 + lane; i - lane < w1; i += 32) f(i, i < w1 ? mass_key(x[i]) : 0u, i < w1);
+        }
+    };
+    uint32_t thr = 0;
+#pragma unroll
+    for (int pass = 0; pass < 3; ++pass) {
+        const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, above_bit = pass == 1 ? 21 : 10;
+        const uint32_t mask = pass == 2 ? 1023u : 2047u;
+        uint32_t* h = hist[pass];
+        each([&](int, uint32_t key, bool in) {
+            if (in && (pass == 0 || (key >> above_bit) == (thr >> above_bit))) atomicAdd(&h[(key >> shift) & mask], 1u);
+        });
+        if (CS > 1) cg::this_cluster().sync(); else __syncthreads();
+        // thread t holds bins 2047 - 4 t .. 2044 - 4 t, from the top
+        uint32_t c[4] = {0u, 0u, 0u, 0u}, sum = 0;
+#pragma unroll
+        for (int r = 0; r < CS; ++r) {
+            const uint32_t* hr = CS > 1 ? cg::this_cluster().map_shared_rank(h, r) : h;
+            const uint4 v = reinterpret_cast<const uint4*>(hr)[kSelBins / 4 - 1 - tid];
+            c[0] += v.w; c[1] += v.z; c[2] += v.y; c[3] += v.x;
+        }
+        sum = c[0] + c[1] + c[2] + c[3];
+        uint32_t incl = sum;
+#pragma unroll
+        for (int off = 1; off < 32; off <<= 1) {
+            const uint32_t y = __shfl_up_sync(0xffffffffu, incl, off);
+            if (lane >= off) incl += y;
+        }
+        if (lane == 31) s_scan[warp] = incl;
         __syncthreads();
-        if (warp == 0) {       // bins from the top: lane l holds bins 255 - 8 l .. 248 - 8 l
-            uint32_t c[8], sum = 0;
+        uint32_t above = incl - sum;
+        for (int w = 0; w < warp; ++w) above += s_scan[w];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                c[j] = 0;
-#pragma unroll
-                for (int k = 0; k < kHistCopies; ++k) c[j] += hist[k][255 - 8 * lane - j];
-                sum += c[j];
-            }
-            uint32_t above = sum;
-#pragma unroll
-            for (int off = 1; off < 32; off <<= 1) {
-                const uint32_t y = __shfl_up_sync(0xffffffffu, above, off);
-                if (lane >= off) above += y;
-            }
-            above -= sum;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                if (above < need && above + c[j] >= need) { s_digit = 255u - 8u * lane - j; s_need = need - above; }
-                above += c[j];
-            }
+        for (int j = 0; j < 4; ++j) {
+            if (above < need && above + c[j] >= need) { s_digit = (uint32_t)(kSelBins - 1 - 4 * tid - j); s_need = need - above; }
+            above += c[j];
         }
         __syncthreads();
         thr |= s_digit << shift;
         need = s_need;                     // of the rows that share the digits so far
-        __syncthreads();
     }
     // need = rows equal to the threshold that are kept
-    const int per = ((m1 - m0 + kSelWarps - 1) / kSelWarps + 31) & ~31;
-    const int w0 = min(m0 + warp * per, m1), w1 = min(w0 + per, m1);
     int gt = 0, eq = 0;
-#pragma unroll 8
-    for (int i = w0 + lane; i < w1; i += 32) {
-        const uint32_t key = mass_key(x[i]);
-        gt += key > thr;
-        eq += key == thr;
-    }
-#pragma unroll
-    for (int off = 16; off; off >>= 1) {
-        gt += __shfl_xor_sync(0xffffffffu, gt, off);
-        eq += __shfl_xor_sync(0xffffffffu, eq, off);
-    }
+    each([&](int, uint32_t key, bool in) {
+        gt += in && key > thr;
+        eq += in && key == thr;
+    });
+    gt = __reduce_add_sync(0xffffffffu, gt);
+    eq = __reduce_add_sync(0xffffffffu, eq);
     if (lane == 0) { s_gt[warp] = gt; s_eq[warp] = eq; }
     __syncthreads();
     int gt0 = 0, eq0 = 0;
     for (int w = 0; w < warp; ++w) { gt0 += s_gt[w]; eq0 += s_eq[w]; }
+    if (CS > 1) {
+        if (tid == kSelThreads - 1) { s_tot[0] = gt0 + gt; s_tot[1] = eq0 + eq; }       // (a lane of the last warp)
+        cg::this_cluster().sync();
+        for (int r = 0; r < rank; ++r) {
+            const int* t = cg::this_cluster().map_shared_rank(s_tot, r);
+            gt0 += t[0];
+            eq0 += t[1];
+        }
+    }
     const int quota = (int)need;
-    for (int i0 = w0; i0 < w1; i0 += 32) {
-        const int i = i0 + lane;
-        const uint32_t key = i < w1 ? mass_key(x[i]) : 0u;
-        const bool is_gt = i < w1 && key > thr, is_eq = i < w1 && key == thr;
+    each([&](int i, uint32_t key, bool in) {
+        const bool is_gt = in && key > thr, is_eq = in && key == thr;
         const uint32_t bg = __ballot_sync(0xffffffffu, is_gt), be = __ballot_sync(0xffffffffu, is_eq);
         const uint32_t below = (1u << lane) - 1u;
         const int eq_rank = eq0 + __popc(be & below);
         if (is_gt || (is_eq && eq_rank < quota)) out[n_sink + gt0 + __popc(bg & below) + min(eq_rank, quota)] = i;
         gt0 += __popc(bg);
         eq0 += __popc(be);
-    }
+    });
+    if (CS > 1) cg::this_cluster().sync();            // nobody reads a block's shared memory after it has gone
+}
+
+template <int CS, bool CACHED>
+kvbfp_status launch_select(const float* mass, const int32_t* seq_lens, const kvbfp_format& f, int budget, int n_sink, int n_recent,
+                           int32_t* kept, uint32_t* status, cudaStream_t s) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(f.batch * f.n_kv_heads * CS));
+    cfg.blockDim = dim3(kSelThreads);
+    cfg.stream = s;
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = CS;
+    at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = CS > 1 ? 2 : 1;
+    KVBFP_CUDA(cudaLaunchKernelEx(&cfg, evict_select<CS, CACHED>, mass, seq_lens, (int)f.max_seq, (int)f.n_kv_heads, budget, n_sink,
+                                  n_recent, kept, status));
+    KVBFP_LAUNCH_CHECK("evict_select");
+    return KVBFP_OK;
 }
 
 struct MoveArgs {
@@ -175,9 +229,14 @@ __global__ void __launch_bounds__(kMoveThreads) move_rows(const MoveArgs a) {
         // exponent bytes: a thread per (row, plane)
         const int er = tid & (kMoveRows - 1), ep = 1 + 2 * (tid / kMoveRows);
         const int es = src_row[er];
-        uint8_t eb[8];
-        if (es >= 0)
-            for (int j = 0; j < row_e; ++j) eb[j] = a.from[ep][(src0 + es) * row_e + j];
+        uint2 eb = make_uint2(0u, 0u);
+        if (es >= 0) {
+            const uint8_t* p = a.from[ep] + (src0 + es) * row_e;
+            if (row_e == 8) eb = *reinterpret_cast<const uint2*>(p);
+            else if (row_e == 4) eb.x = *reinterpret_cast<const uint32_t*>(p);
+            else if (row_e == 2) eb.x = *reinterpret_cast<const uint16_t*>(p);
+            else eb.x = *p;
+        }
         float w = 0.f;
         if (a.mass && tid < kMoveRows && src_row[tid] >= 0) w = a.mass[src0 + src_row[tid]];
         if (IN_PLACE) __syncthreads();
@@ -191,8 +250,13 @@ __global__ void __launch_bounds__(kMoveThreads) move_rows(const MoveArgs a) {
                 *reinterpret_cast<uint4*>(a.to[2] + at) = vm[j];
             }
         }
-        if (es >= 0)
-            for (int j = 0; j < row_e; ++j) a.to[ep][(d0 + er) * row_e + j] = eb[j];
+        if (es >= 0) {
+            uint8_t* p = a.to[ep] + (d0 + er) * row_e;
+            if (row_e == 8) *reinterpret_cast<uint2*>(p) = eb;
+            else if (row_e == 4) *reinterpret_cast<uint32_t*>(p) = eb.x;
+            else if (row_e == 2) *reinterpret_cast<uint16_t*>(p) = (uint16_t)eb.x;
+            else *p = (uint8_t)eb.x;
+        }
         if (a.mass && tid < kMoveRows && src_row[tid] >= 0) a.to_mass[d0 + tid] = w;
     }
     if (a.new_lens && (IN_PLACE || blockIdx.y == 0)) {
@@ -239,7 +303,7 @@ kvbfp_status set_caches(const kvbfp_cache* src, const kvbfp_cache* dst, MoveArgs
     const kvbfp_format &f = src->fmt, &d = dst->fmt;
     if (f.batch != d.batch || f.n_kv_heads != d.n_kv_heads || f.block != d.block || f.mant_bits != d.mant_bits)
         return KVBFP_ERR_INVALID_ARG;
-    if ((int64_t)f.batch * f.n_kv_heads >= (int64_t)1 << 31) return KVBFP_ERR_UNSUPPORTED;
+    if ((int64_t)f.batch * f.n_kv_heads >= (int64_t)1 << 28) return KVBFP_ERR_UNSUPPORTED;
     a->src = f;
     a->dst = d;
     const uint8_t* from[4] = {src->k_mant, src->k_exp, src->v_mant, src->v_exp};
@@ -297,9 +361,19 @@ extern "C" kvbfp_status kvbfp_evict(const kvbfp_cache* src, const int32_t* seq_l
     st = status_word(&a.status);
     if (st != KVBFP_OK) return st;
     cudaStream_t s = (cudaStream_t)stream;
-    KVBFP_CUDA(launch_pdl(evict_select, dim3((unsigned)(src->fmt.batch * src->fmt.n_kv_heads)), dim3(kSelThreads), 0, s,
-                          mass, seq_lens, src->fmt.max_seq, src->fmt.n_kv_heads, budget, n_sink, n_recent, kept, a.status));
-    KVBFP_LAUNCH_CHECK("evict_select");
+    // A cluster per pair where the pairs alone leave most of the GPU idle and a block would have several rows per thread
+    // (8 x 65536 rows: 58 us with a block each); keys in registers where the longest sequence allowed fits.
+    const kvbfp_format& f = src->fmt;
+    int n_sm = 0;
+    st = sm_count(&n_sm);
+    if (st != KVBFP_OK) return st;
+    const bool wide = (int64_t)f.batch * f.n_kv_heads * kSelCluster <= 2 * n_sm && f.max_seq > kSelThreads * 4;
+    const int64_t region = f.max_seq + 32 * kSelWarps * (wide ? kSelCluster : 1);            // pieces are rounded up to 32 rows
+    const bool cached = region <= (int64_t)kSelThreads * kSelKeys * (wide ? kSelCluster : 1);
+    auto select = wide ? (cached ? launch_select<kSelCluster, true> : launch_select<kSelCluster, false>)
+                       : (cached ? launch_select<1, true> : launch_select<1, false>);
+    st = select(mass, seq_lens, f, budget, n_sink, n_recent, kept, a.status, s);
+    if (st != KVBFP_OK) return st;
     a.index = kept; a.index_heads = src->fmt.n_kv_heads; a.n_index = budget;
     a.mass = mass; a.to_mass = dst_mass; a.new_lens = new_lens;
     return launch_move(a, s);
