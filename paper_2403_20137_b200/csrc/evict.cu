@@ -10,6 +10,7 @@ namespace {
 constexpr int kSelThreads = 512, kSelWarps = kSelThreads / 32;
 constexpr int kSelKeys = 16;                 // keys a thread keeps in registers
 constexpr int kSelBins = 2048, kSelCluster = 8;
+constexpr int kSelCopy = 1024 + 8;           // bins of a copy of the first digit's histogram, eight banks apart from the next
 
 // Weights in the order of unsigned integers: -0 as 0, NaN below everything.
 __device__ __forceinline__ uint32_t mass_key(float x) {
@@ -19,21 +20,21 @@ __device__ __forceinline__ uint32_t mass_key(float x) {
 }
 
 // The rows to keep of one (sequence, kv head), in position order, by a block or (CS > 1) a cluster of blocks that share
-// the region.  The heaviest `need` of the middle region are found by radix selection: three digits of 11, 11 and 10 bits,
-// a histogram each in shared memory, the cluster's summed through distributed shared memory; of equals to the threshold
+// the region.  The heaviest `need` of the middle region are found by radix selection: three digits of 10, 11 and 11 bits,
+// a histogram each in shared memory (the first, where most weights fall into a few bins, in four copies by lane), the cluster's summed through distributed shared memory; of equals to the threshold
 // the lowest positions are kept.  Each warp owns a contiguous piece of the region, so one scan over the warps' counts
 // places every kept row.  A thread keeps its keys in registers where they fit (CACHED: up to 8192 rows a block) and reads
-// them again otherwise.  What bounds it is the chain of passes, not the bytes (4 per row): a digit of 11 bits spreads the
-// exponents that eight bits pile up in a few bins, and takes one pass less.
+// them again otherwise.  What bounds it is the chain of passes, not the bytes (4 per row).
 template <int CS, bool CACHED>
-__global__ void __launch_bounds__(kSelThreads) evict_select(const float* mass, const int32_t* seq_lens, int max_seq, int n_heads,
+__global__ void __launch_bounds__(kSelThreads, CS == 1 ? 3 : 1) evict_select(const float* mass, const int32_t* seq_lens, int max_seq, int n_heads,
                                                             int budget, int n_sink, int n_recent, int32_t* kept, uint32_t* status) {
-    __shared__ uint32_t hist[3][kSelBins];
+    __shared__ __align__(16) uint32_t hist0[4 * kSelCopy], hist[2][kSelBins];
     __shared__ uint32_t s_scan[kSelWarps], s_digit, s_need;
     __shared__ int s_gt[kSelWarps], s_eq[kSelWarps], s_tot[2];
     namespace cg = cooperative_groups;
     const int pair = blockIdx.x / CS, rank = blockIdx.x % CS, b = pair / n_heads, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    for (int i = tid; i < 3 * kSelBins; i += kSelThreads) (&hist[0][0])[i] = 0;
+    for (int i = tid; i < 4 * kSelCopy; i += kSelThreads) hist0[i] = 0;
+    for (int i = tid; i < 2 * kSelBins; i += kSelThreads) (&hist[0][0])[i] = 0;
     __syncthreads();
     pdl_wait();
     pdl_trigger();
@@ -75,20 +76,41 @@ __global__ void __launch_bounds__(kSelThreads) evict_select(const float* mass, c
     uint32_t thr = 0;
 #pragma unroll
     for (int pass = 0; pass < 3; ++pass) {
-        const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, above_bit = pass == 1 ? 21 : 10;
-        const uint32_t mask = pass == 2 ? 1023u : 2047u;
-        uint32_t* h = hist[pass];
+        const int shift = pass == 0 ? 22 : pass == 1 ? 11 : 0, above_bit = pass == 1 ? 22 : 11;
+        const uint32_t mask = pass == 0 ? 1023u : 2047u;
+        uint32_t* h = pass == 0 ? hist0 + (lane & 3) * kSelCopy : hist[pass > 0 ? pass - 1 : 0];
         each([&](int, uint32_t key, bool in) {
-            if (in && (pass == 0 || (key >> above_bit) == (thr >> above_bit))) atomicAdd(&h[(key >> shift) & mask], 1u);
+            const bool take = in && (pass == 0 || (key >> above_bit) == (thr >> above_bit));
+            const uint32_t bin = (key >> shift) & mask;
+            if (pass == 2) {       // the lowest digits of rounded weights are all alike: one addition then
+                const uint32_t who = __ballot_sync(0xffffffffu, take);
+                if (who == 0) return;
+                const uint32_t lead = __shfl_sync(0xffffffffu, bin, __ffs(who) - 1);
+                if (__all_sync(0xffffffffu, !take || bin == lead)) {
+                    if (lane == __ffs(who) - 1) atomicAdd(&h[lead], (uint32_t)__popc(who));
+                    return;
+                }
+            }
+            if (take) atomicAdd(&h[bin], 1u);
         });
+        if (pass == 0) {           // the copies into the first
+            __syncthreads();
+            for (int i = tid; i < 1024; i += kSelThreads) hist0[i] += hist0[kSelCopy + i] + hist0[2 * kSelCopy + i] + hist0[3 * kSelCopy + i];
+        }
         if (CS > 1) cg::this_cluster().sync(); else __syncthreads();
-        // thread t holds bins 2047 - 4 t .. 2044 - 4 t, from the top
+        // thread t holds the last four bins but 4 t (first digit: two), from the top
         uint32_t c[4] = {0u, 0u, 0u, 0u}, sum = 0;
+        const uint32_t* first = pass == 0 ? hist0 : hist[pass > 0 ? pass - 1 : 0];
 #pragma unroll
         for (int r = 0; r < CS; ++r) {
-            const uint32_t* hr = CS > 1 ? cg::this_cluster().map_shared_rank(h, r) : h;
-            const uint4 v = reinterpret_cast<const uint4*>(hr)[kSelBins / 4 - 1 - tid];
-            c[0] += v.w; c[1] += v.z; c[2] += v.y; c[3] += v.x;
+            const uint32_t* hr = CS > 1 ? cg::this_cluster().map_shared_rank(first, r) : first;
+            if (pass == 0) {
+                const uint2 v = reinterpret_cast<const uint2*>(hr)[511 - tid];
+                c[0] += v.y; c[1] += v.x;
+            } else {
+                const uint4 v = reinterpret_cast<const uint4*>(hr)[511 - tid];
+                c[0] += v.w; c[1] += v.z; c[2] += v.y; c[3] += v.x;
+            }
         }
         sum = c[0] + c[1] + c[2] + c[3];
         uint32_t incl = sum;
@@ -102,8 +124,11 @@ __global__ void __launch_bounds__(kSelThreads) evict_select(const float* mass, c
         uint32_t above = incl - sum;
         for (int w = 0; w < warp; ++w) above += s_scan[w];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            if (above < need && above + c[j] >= need) { s_digit = (uint32_t)(kSelBins - 1 - 4 * tid - j); s_need = need - above; }
+        for (int j = 0; j < (pass == 0 ? 2 : 4); ++j) {
+            if (above < need && above + c[j] >= need) {
+                s_digit = (uint32_t)(pass == 0 ? 1023 - 2 * tid - j : kSelBins - 1 - 4 * tid - j);
+                s_need = need - above;
+            }
             above += c[j];
         }
         __syncthreads();
@@ -182,6 +207,14 @@ struct MoveArgs {
 
 constexpr int kMoveThreads = 256, kMoveRows = 128;
 
+// A piece of a scattered row: no more than 64 bytes around it need come from DRAM.
+__device__ __forceinline__ uint4 ld_row(const void* p) {
+    uint4 x;
+    asm volatile("ld.global.L1::no_allocate.L2::64B.v4.u32 {%0,%1,%2,%3}, [%4];"
+                 : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w) : "l"(p) : "memory");
+    return x;
+}
+
 // Rows src_base + index[i] -> dst_base + i of all planes, kMoveRows at a time through registers.  A block per (chunk,
 // pair) where the caches differ; in place one block per pair walks the chunks upwards: every row of a chunk is read
 // before any is written, and with ascending indices (index[i] >= i) later chunks read only rows behind the written
@@ -222,8 +255,8 @@ __global__ void __launch_bounds__(kMoveThreads) move_rows(const MoveArgs a) {
             const int x = tid + j * kMoveThreads, r = src_row[x / PIECES];
             if (r >= 0) {
                 const int64_t at = (src0 + r) * (PIECES * 16) + (x % PIECES) * 16;
-                km[j] = *reinterpret_cast<const uint4*>(a.from[0] + at);
-                vm[j] = *reinterpret_cast<const uint4*>(a.from[2] + at);
+                km[j] = ld_row(a.from[0] + at);
+                vm[j] = ld_row(a.from[2] + at);
             }
         }
         // exponent bytes: a thread per (row, plane)
@@ -368,8 +401,7 @@ extern "C" kvbfp_status kvbfp_evict(const kvbfp_cache* src, const int32_t* seq_l
     st = sm_count(&n_sm);
     if (st != KVBFP_OK) return st;
     const bool wide = (int64_t)f.batch * f.n_kv_heads * kSelCluster <= 2 * n_sm && f.max_seq > kSelThreads * 4;
-    const int64_t region = f.max_seq + 32 * kSelWarps * (wide ? kSelCluster : 1);            // pieces are rounded up to 32 rows
-    const bool cached = region <= (int64_t)kSelThreads * kSelKeys * (wide ? kSelCluster : 1);
+    const bool cached = (int64_t)f.max_seq - n_sink - n_recent <= (int64_t)kSelThreads * kSelKeys * (wide ? kSelCluster : 1);
     auto select = wide ? (cached ? launch_select<kSelCluster, true> : launch_select<kSelCluster, false>)
                        : (cached ? launch_select<1, true> : launch_select<1, false>);
     st = select(mass, seq_lens, f, budget, n_sink, n_recent, kept, a.status, s);
