@@ -8,7 +8,7 @@ namespace kvbfp {
 namespace {
 
 // One warp (SPLIT: one block of four) per query row: out = sum_w 2^(m_w - m) o_w / sum_w 2^(m_w - m) l_w over the
-// partials of the warps that share the row's tiles.  Rows whose tiles one warp had are written already; rows that
+// partials of the workers that share the row's tiles.  Rows whose tiles one worker had are written already; rows that
 // see no tile are zeros.
 template <bool SPLIT>
 __global__ void __launch_bounds__(128) attn_merge(const AttnArgs a, int64_t n_rows) {
@@ -165,9 +165,9 @@ __global__ void __launch_bounds__(128) attn_mass(const AttnArgs a) {
 }
 
 // Query rows per work item: up to 64 bf16 rows of a kv head share its tiles; fp32 queries take 16 at a time (their three
-// bf16 terms fill the registers of the warp-level kernel).
+// bf16 terms fill the registers of attn_rows).
 inline int rows_tile_for(int rows, bool bf16) { return !bf16 || rows <= 16 ? 16 : rows <= 32 ? 32 : 64; }
-inline int max_workers(bool bf16) { return bf16 ? 3 * 160 : kAttnMaxBlocks * kAttnWarps; }
+inline int max_workers(bool bf16) { return (bf16 ? 3 : 2 * kAttnWarps) * kAttnMaxSms; }
 
 inline size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
 
@@ -273,11 +273,10 @@ kvbfp_status attn_common(const AttnCall& c) {
     st = sm_count(&n_sm);
     if (st != KVBFP_OK) return st;
     const bool bf16 = c.dt == KVBFP_BF16;
-    const AttnShape shape = bf16 ? AttnShape{128, 1} : f.mant_bits == 4 ? attn_shape4(a) : f.mant_bits == 6 ? attn_shape6(a) : attn_shape8(a);
-    a.tile = shape.tile;
-    a.out_up = bf16 ? (float)(1 << (19 - f.mant_bits)) : kValueUp;      // attn_umma: 2^(17 - (p - 2))
-    const int64_t most = (int64_t)f.batch * f.n_kv_heads * n_row_tiles * (f.max_seq / shape.tile + 2);    // tiles at the longest
-    int64_t grid = (int64_t)n_sm * shape.blocks_per_sm;
+    a.tile = bf16 ? 128 : attn_rows_tile(f.mant_bits);
+    a.out_up = bf16 ? (float)(1 << (19 - f.mant_bits)) : 256.f;      // 2^(17 - (p - 2)) | 2^8
+    const int64_t most = (int64_t)f.batch * f.n_kv_heads * n_row_tiles * (f.max_seq / a.tile + 2);    // tiles at the longest
+    int64_t grid = (int64_t)n_sm * (bf16 ? 1 : 2);
     const int per_block = bf16 ? attn_teams(f.mant_bits, rows_tile) : kAttnWarps;      // teams or warps
     if (grid * per_block > max_workers(bf16)) grid = max_workers(bf16) / per_block;
     if (grid > most) grid = most;

@@ -6,7 +6,7 @@
 namespace kvbfp {
 
 constexpr int kAttnWarps = 4;          // warps per thread block of attn_rows; every warp is a worker of its own
-constexpr int kAttnMaxBlocks = 3 * 160;    // thread blocks of attn_rows
+constexpr int kAttnMaxSms = 160;       // SMs that workspaces are sized for
 constexpr int kAttnMaxBatch = 1024;    // sequences
 constexpr int kAttnPart = kHeadDim + 4;    // floats of a partial row: o[128], max (log2 units), sum, 2 unused
 constexpr int kAttnMaxDraft = 64;      // drafted tokens per sequence (bits of a mask word)
@@ -55,12 +55,12 @@ struct AttnArgs {
     SeqView* views;                // workspace: [B]
     int* dpos;                     // workspace: [B, 64] positions of the drafted rows
     RowInfo* rows;                 // workspace: [B * Hkv * n_row_tiles, rows_tile]
-    uint4* qfrag;                  // workspace: pi(q) in fragment order, [B * Hkv * n_row_tiles][split][m tile][k step][lane]
+    uint4* qfrag;                  // workspace: pi(q) as the main kernel's operand, [B * Hkv * n_row_tiles]
     float* lse;                    // workspace: [B, Hq] log2-sum-exp2, with mass only (else NULL)
     float* scores;                 // workspace: [B, Hq, max_seq] scores in log2 units, with mass only (else NULL)
     float* mass;                   // [B, Hkv, max_seq] or NULL
     float* partials;               // workspace: [2 * workers, part_rows, kAttnPart]
-    int workers;                   // warps of the main kernel
+    int workers;                   // warps (attn_rows) or teams (attn_umma) of the main kernel
     float out_up;                  // sums of P and V as the kernel carries them -> values
     uint32_t* status;
 };
@@ -107,18 +107,9 @@ __host__ __device__ __forceinline__ int worker_of(int x, int n_items, int worker
     return (int)(((int64_t)(x + 1) * workers - 1) / n_items);
 }
 
-// Cached values are carried times 2^-8 inside attn_rows, so that no exponent byte leaves the bf16 range with the
-// conversion's offset; undone on scores and outputs.
-constexpr float kValueUp = 256.f;
-
-// How the kernel for `mant_bits` cuts and splits: tokens per tile; thread blocks per SM.
-struct AttnShape {
-    int tile, blocks_per_sm;
-};
-AttnShape attn_shape4(const AttnArgs& a);
-AttnShape attn_shape6(const AttnArgs& a);
-AttnShape attn_shape8(const AttnArgs& a);
-// attn_prep and attn_rows
+// Tokens per tile of attn_rows (fp32 queries): two stages of four warps of two blocks fit an SM.
+__host__ __device__ constexpr int attn_rows_tile(int mant_bits) { return mant_bits == 8 ? 32 : 64; }
+// attn_prep and attn_rows: fp32 queries, 16 rows per work item, two thread blocks per SM
 kvbfp_status launch_attn_rows4(const AttnArgs& a, int grid, cudaStream_t s);
 kvbfp_status launch_attn_rows6(const AttnArgs& a, int grid, cudaStream_t s);
 kvbfp_status launch_attn_rows8(const AttnArgs& a, int grid, cudaStream_t s);

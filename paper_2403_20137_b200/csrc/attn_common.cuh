@@ -1,4 +1,4 @@
-// What attn_rows and attn_umma share: the conversion of stored fields to bf16, and the launch that prepares a call.
+// What the launches that prepare attn_rows and attn_umma share.
 #pragma once
 #include <math.h>
 
@@ -9,39 +9,6 @@
 
 namespace kvbfp {
 namespace {
-
-template <int P> struct AFmt;
-template <> struct AFmt<4> { static constexpr uint32_t mask = 0x000F000Fu, magic = 0x43004300u, bias = 0xC308C308u; };  // -136
-template <> struct AFmt<6> { static constexpr uint32_t mask = 0x003F003Fu, magic = 0x43004300u, bias = 0xC320C320u; };  // -160
-template <> struct AFmt<8> { static constexpr uint32_t mask = 0x000F000Fu, magic = 0x43004300u, bias = 0xC510C510u; };  // -2304
-
-// bf16 bits of 2^(e8 - 127 - (P-2) - 8); 0 below the smallest subnormal.
-template <int P>
-__device__ __forceinline__ uint32_t attn_weight(int e8) {
-    const int f = e8 - (P - 2) - 8;
-    return f >= 1 ? ((uint32_t)f << 7) : (f > -7 ? (0x40u >> (-f)) : 0u);
-}
-
-struct AW {
-    uint32_t s, c, s16;      // weight pair, -offset * weight, 16 * weight (8-bit fields)
-};
-template <int P>
-__device__ __forceinline__ AW aw_make(uint32_t s, uint32_t c) {
-    AW w;
-    w.s = s;
-    w.c = c;
-    w.s16 = (P == 8) ? mul_bf16x2(s, 0x41804180u) : 0u;
-    return w;
-}
-template <int P>
-__device__ __forceinline__ uint32_t acvt(uint32_t x, const AW& w) {
-    if (P == 8) {
-        const uint32_t lo = lop3<0xEA>(x, 0x000F000Fu, 0x43004300u);
-        const uint32_t hi = lop3<0xEA>(x >> 4, 0x000F000Fu, 0x43004300u);
-        return fma_bf16x2(lo, w.s, fma_bf16x2(hi, w.s16, w.c));
-    }
-    return fma_bf16x2(lop3<0xEA>(x, AFmt<P>::mask, AFmt<P>::magic), w.s, w.c);
-}
 
 // Everything a call's main kernel reads besides the cache, per (sequence, kv head, row tile) of ROWS query rows: rows of
 // q (stored-slot order through `sp`, zeros behind the last row) to shared memory, per-row data, and from the first

@@ -1,4 +1,4 @@
-// Attention of up to 64 query rows per (batch, kv head) over the packed cache with warp-level bf16 MMAs.
+// Attention of fp32 query rows over the packed cache with warp-level bf16 MMAs, 16 rows of a (batch, kv head) at a time.
 //
 //   S[rows x tokens] = pi(Q) . K^T ;  y = log2(e) * (cap * tanh(scale * S / cap) - slope * distance) ;  P = 2^(y - m)
 //   O[rows x slots] += P . V ;  l += rowsum(P)
@@ -25,6 +25,47 @@
 
 namespace kvbfp {
 namespace {
+
+constexpr int kRows = 16;       // query rows of a work item
+constexpr int kSplit = 3;       // bf16 terms of an fp32 operand
+
+// Cached values are carried times 2^-8, so that no exponent byte leaves the bf16 range with the conversion's offset;
+// undone on scores and outputs.
+constexpr float kValueUp = 256.f;
+
+// Stored fields to bf16 pairs.
+template <int P> struct AFmt;
+template <> struct AFmt<4> { static constexpr uint32_t mask = 0x000F000Fu, magic = 0x43004300u, bias = 0xC308C308u; };  // -136
+template <> struct AFmt<6> { static constexpr uint32_t mask = 0x003F003Fu, magic = 0x43004300u, bias = 0xC320C320u; };  // -160
+template <> struct AFmt<8> { static constexpr uint32_t mask = 0x000F000Fu, magic = 0x43004300u, bias = 0xC510C510u; };  // -2304
+
+// bf16 bits of 2^(e8 - 127 - (P-2) - 8); 0 below the smallest subnormal.
+template <int P>
+__device__ __forceinline__ uint32_t attn_weight(int e8) {
+    const int f = e8 - (P - 2) - 8;
+    return f >= 1 ? ((uint32_t)f << 7) : (f > -7 ? (0x40u >> (-f)) : 0u);
+}
+
+struct AW {
+    uint32_t s, c, s16;      // weight pair, -offset * weight, 16 * weight (8-bit fields)
+};
+template <int P>
+__device__ __forceinline__ AW aw_make(uint32_t s, uint32_t c) {
+    AW w;
+    w.s = s;
+    w.c = c;
+    w.s16 = (P == 8) ? mul_bf16x2(s, 0x41804180u) : 0u;
+    return w;
+}
+template <int P>
+__device__ __forceinline__ uint32_t acvt(uint32_t x, const AW& w) {
+    if (P == 8) {
+        const uint32_t lo = lop3<0xEA>(x, 0x000F000Fu, 0x43004300u);
+        const uint32_t hi = lop3<0xEA>(x >> 4, 0x000F000Fu, 0x43004300u);
+        return fma_bf16x2(lo, w.s, fma_bf16x2(hi, w.s16, w.c));
+    }
+    return fma_bf16x2(lop3<0xEA>(x, AFmt<P>::mask, AFmt<P>::magic), w.s, w.c);
+}
 
 // Slot that k position kk (0..3 = k 2t, 2t+1, 2t+8, 2t+9) of k-step ks holds in lane column t.
 template <int P>
@@ -105,38 +146,37 @@ __device__ __forceinline__ int tile_at(int row, int x) {
 }
 
 // Query fragments of one (sequence, kv head, row tile) per block.
-template <int P, int MT, bool F32>
+template <int P>
 __global__ void __launch_bounds__(128) attn_prep(const AttnArgs a) {
-    constexpr int ROWS = 16 * MT, SPLIT = F32 ? 3 : 1;
-    __shared__ float sq[ROWS][kHeadDim + 4];
+    __shared__ float sq[kRows][kHeadDim + 4];
     __shared__ int sp[kHeadDim];
-    prep_common<ROWS, F32>(a, sq, sp);
+    prep_common<kRows, true>(a, sq, sp);
     const int tid = threadIdx.x, x0 = blockIdx.x;
-    uint4* to = a.qfrag + (int64_t)x0 * (SPLIT * MT * 8 * 32);
-#pragma unroll 2
-    for (int x = tid; x < MT * 8 * 32; x += 128) {
-        const int ln = x & 31, ks = (x >> 5) & 7, mt = x >> 8, g = ln >> 2, t = ln & 3;
-        uint32_t reg[SPLIT][4];
+    uint4* to = a.qfrag + (int64_t)x0 * (kSplit * 8 * 32);
+#pragma unroll
+    for (int x = tid; x < 8 * 32; x += 128) {
+        const int ln = x & 31, ks = x >> 5, g = ln >> 2, t = ln & 3;
+        uint32_t reg[kSplit][4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) {       // row g | g + 8, k positions 0, 1 | 2, 3
-            const float* row = sq[mt * 16 + g + 8 * (k & 1)];
+            const float* row = sq[g + 8 * (k & 1)];
             float v0 = row[sp[attn_k_slot<P>(ks, t, (k & 2))]], v1 = row[sp[attn_k_slot<P>(ks, t, (k & 2) + 1)]];
 #pragma unroll
-            for (int s = 0; s < SPLIT; ++s) {
+            for (int s = 0; s < kSplit; ++s) {
                 reg[s][k] = pack_bf16x2_rn(v0, v1);
                 v0 -= __uint_as_float(reg[s][k] << 16);
                 v1 -= __uint_as_float(reg[s][k] & 0xffff0000u);
             }
         }
 #pragma unroll
-        for (int s = 0; s < SPLIT; ++s) to[s * MT * 256 + x] = make_uint4(reg[s][0], reg[s][1], reg[s][2], reg[s][3]);
+        for (int s = 0; s < kSplit; ++s) to[s * 256 + x] = make_uint4(reg[s][0], reg[s][1], reg[s][2], reg[s][3]);
     }
 }
 
 template <int P>
 struct AGeo {
     static constexpr int ROW_M = kHeadDim * P / 8;
-    static constexpr int TILE = P == 8 ? 32 : 64;       // tokens per stage
+    static constexpr int TILE = attn_rows_tile(P);       // tokens per stage
     static constexpr int STAGES = 2;
     static constexpr int VM_OFF = TILE * ROW_M, KE_OFF = 2 * VM_OFF;
     // exponent bytes of a stage: 2 * TILE * row_e, the stage rounded up to the swizzle's 1024 bytes for the tiled copies
@@ -148,12 +188,12 @@ struct AGeo {
     }
 };
 
-template <int P, bool N16, int MT, bool F32, int MINB>
-__global__ void __launch_bounds__(kAttnWarps * 32, MINB) attn_rows(const AttnArgs a, const __grid_constant__ CUtensorMap k_map,
+template <int P, bool N16>
+__global__ void __launch_bounds__(kAttnWarps * 32, 2) attn_rows(const AttnArgs a, const __grid_constant__ CUtensorMap k_map,
                                                                    const __grid_constant__ CUtensorMap v_map) {
     using G_ = AGeo<P>;
-    constexpr int D = kHeadDim, ROW_M = G_::ROW_M, STAGES = G_::STAGES, TILE = G_::TILE, ROWS = 16 * MT;
-    constexpr int SPLIT = F32 ? 3 : 1, GROUP = 16 * ROW_M;
+    constexpr int D = kHeadDim, ROW_M = G_::ROW_M, STAGES = G_::STAGES, TILE = G_::TILE, ROWS = kRows;
+    constexpr int GROUP = 16 * ROW_M;
     extern __shared__ __align__(1024) uint8_t smem[];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
     const int row_e = D / a.fmt.block, exp_half = TILE * row_e;
@@ -286,15 +326,13 @@ __global__ void __launch_bounds__(kAttnWarps * 32, MINB) attn_rows(const AttnArg
         const int k0 = cc.k, k1 = min(cc.n, k0 + n_mine - it);
         const SeqView sv = view(b);
         const int64_t item = (int64_t)b * HR + cc.hr;
-        uint4 qr[SPLIT][MT][8];
+        uint4 qr[kSplit][8];
         {
-            const uint4* src = a.qfrag + item * (SPLIT * MT * 256) + lane;
+            const uint4* src = a.qfrag + item * (kSplit * 256) + lane;
 #pragma unroll
-            for (int s = 0; s < SPLIT; ++s)
+            for (int s = 0; s < kSplit; ++s)
 #pragma unroll
-                for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-                    for (int ks = 0; ks < 8; ++ks) qr[s][mt][ks] = src[((s * MT + mt) * 8 + ks) * 32];
+                for (int ks = 0; ks < 8; ++ks) qr[s][ks] = src[(s * 8 + ks) * 32];
         }
         __syncwarp();
         if (lane < ROWS) reinterpret_cast<uint4*>(ri)[lane] = reinterpret_cast<const uint4*>(a.rows)[item * ROWS + lane];
@@ -304,16 +342,15 @@ __global__ void __launch_bounds__(kAttnWarps * 32, MINB) attn_rows(const AttnArg
         }
         __syncwarp();
 
-        float o[MT][16][4];
-        float m_run[MT][2], l_run[MT][2];
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt) {
+        float o[16][4];
+        float m_run[2], l_run[2];
+        {
 #pragma unroll
             for (int s = 0; s < 16; ++s)
 #pragma unroll
-                for (int k = 0; k < 4; ++k) o[mt][s][k] = 0.f;
-            m_run[mt][0] = m_run[mt][1] = -3.4028235e38f;
-            l_run[mt][0] = l_run[mt][1] = 0.f;
+                for (int k = 0; k < 4; ++k) o[s][k] = 0.f;
+            m_run[0] = m_run[1] = -3.4028235e38f;
+            l_run[0] = l_run[1] = 0.f;
         }
         // tokens [clear_lo, ctx) and [0, pf) are visible to every row
         int clear_lo = sv.first;
@@ -333,9 +370,9 @@ __global__ void __launch_bounds__(kAttnWarps * 32, MINB) attn_rows(const AttnArg
                 const int tok0 = tt + 16 * u;
                 if (tok0 >= end) break;
                 // ---- scores of 16 tokens: sc[m tile][column tile][...]
-                float sc[MT][2][4];
+                float sc[2][4];
                 {
-                    float s2[MT][2][4];        // odd k steps: two chains of MMAs per column tile
+                    float s2[2][4];        // odd k steps: two chains of MMAs per column tile
                     uint32_t kw[2][P];
                     AW kg[2][N16 ? 2 : 1];
 #pragma unroll
@@ -360,134 +397,117 @@ __global__ void __launch_bounds__(kAttnWarps * 32, MINB) attn_rows(const AttnArg
                         }
                     }
 #pragma unroll
-                    for (int mt = 0; mt < MT; ++mt)
+                    for (int j = 0; j < 2; ++j)
 #pragma unroll
-                        for (int j = 0; j < 2; ++j)
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) sc[mt][j][e] = s2[mt][j][e] = 0.f;
+                        for (int e = 0; e < 4; ++e) sc[j][e] = s2[j][e] = 0.f;
 #pragma unroll
                     for (int ks = 0; ks < 8; ks += 2) {
                         uint32_t r[2][4];
 #pragma unroll
                         for (int j = 0; j < 2; ++j) attn_k<P>(kw[j], ks, kg[j][N16 ? ks >> 2 : 0], r[j]);
 #pragma unroll
-                        for (int s = 0; s < SPLIT; ++s)
+                        for (int s = 0; s < kSplit; ++s)
+                            {
+                                const uint4 q0 = qr[s][ks], q1 = qr[s][ks + 1];
 #pragma unroll
-                            for (int mt = 0; mt < MT; ++mt) {
-                                const uint4 q0 = qr[s][mt][ks], q1 = qr[s][mt][ks + 1];
+                                for (int j = 0; j < 2; ++j) mma_bf16(sc[j], q0.x, q0.y, q0.z, q0.w, r[j][0], r[j][1]);
 #pragma unroll
-                                for (int j = 0; j < 2; ++j) mma_bf16(sc[mt][j], q0.x, q0.y, q0.z, q0.w, r[j][0], r[j][1]);
-#pragma unroll
-                                for (int j = 0; j < 2; ++j) mma_bf16(s2[mt][j], q1.x, q1.y, q1.z, q1.w, r[j][2], r[j][3]);
+                                for (int j = 0; j < 2; ++j) mma_bf16(s2[j], q1.x, q1.y, q1.z, q1.w, r[j][2], r[j][3]);
                             }
                     }
 #pragma unroll
-                    for (int mt = 0; mt < MT; ++mt)
+                    for (int j = 0; j < 2; ++j)
 #pragma unroll
-                        for (int j = 0; j < 2; ++j)
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) sc[mt][j][e] += s2[mt][j][e];
+                        for (int e = 0; e < 4; ++e) sc[j][e] += s2[j][e];
                 }
                 // ---- cap, bias, masks: y = mul * sc in log2 units; tiles that every row sees whole need only the factor
                 float mul = plain;
                 if (reshape || !(tok0 + 16 <= sv.ctx && (tok0 >= clear_lo || tok0 + 16 <= sv.pf))) {
                     mul = 1.f;
 #pragma unroll
-                    for (int mt = 0; mt < MT; ++mt)
+                    for (int hh = 0; hh < 2; ++hh) {
+                        const RowInfo x = ri[g + 8 * hh];
 #pragma unroll
-                        for (int hh = 0; hh < 2; ++hh) {
-                            const RowInfo x = ri[mt * 16 + g + 8 * hh];
+                        for (int j = 0; j < 2; ++j)
 #pragma unroll
-                            for (int j = 0; j < 2; ++j)
-#pragma unroll
-                                for (int e = 0; e < 2; ++e) {
-                                    float y = sc[mt][j][2 * hh + e];
-                                    if (a.softcap > 0.f) {
-                                        y *= cap_in;
-                                        if (F32) y = tanhf(y);
-                                        else y = 1.f - __fdividef(2.f, 1.f + ex2_approx(y * 2.8853900817779268f));    // 1 - 2 / (1 + e^2y): about 2e-7 absolute
-                                        y *= a.softcap;
-                                    } else {
-                                        y *= up;
-                                    }
-                                    const int tok = tok0 + tok_of<P>(t, e, j);
-                                    bool see;
-                                    int dist;
-                                    if (tok < sv.ctx) {
-                                        dist = x.pos - tok;
-                                        see = (tok >= sv.first && (a.window == 0 || dist < a.window)) || tok < sv.pf;
-                                    } else {
-                                        const int jd = tok - sv.ctx;
-                                        const bool in = jd < sv.nd;
-                                        dist = x.pos - dpos[in ? jd : 0];
-                                        see = in && (((jd < 32 ? x.m0 >> (jd & 31) : x.m1 >> (jd & 31)) & 1u) != 0u) &&
-                                              (a.window == 0 || dist < a.window);
-                                    }
-                                    y = (y - x.slope * (float)dist) * to_log2;
-                                    sc[mt][j][2 * hh + e] = see ? y : -INFINITY;
+                            for (int e = 0; e < 2; ++e) {
+                                float y = sc[j][2 * hh + e];
+                                if (a.softcap > 0.f) {
+                                    y *= cap_in;
+                                    y = a.softcap * tanhf(y);
+                                } else {
+                                    y *= up;
                                 }
-                        }
+                                const int tok = tok0 + tok_of<P>(t, e, j);
+                                bool see;
+                                int dist;
+                                if (tok < sv.ctx) {
+                                    dist = x.pos - tok;
+                                    see = (tok >= sv.first && (a.window == 0 || dist < a.window)) || tok < sv.pf;
+                                } else {
+                                    const int jd = tok - sv.ctx;
+                                    const bool in = jd < sv.nd;
+                                    dist = x.pos - dpos[in ? jd : 0];
+                                    see = in && (((jd < 32 ? x.m0 >> (jd & 31) : x.m1 >> (jd & 31)) & 1u) != 0u) &&
+                                    (a.window == 0 || dist < a.window);
+                                }
+                                y = (y - x.slope * (float)dist) * to_log2;
+                                sc[j][2 * hh + e] = see ? y : -INFINITY;
+                            }
+                    }
                 }
                 if (a.scores) {
 #pragma unroll
-                    for (int mt = 0; mt < MT; ++mt)
+                    for (int hh = 0; hh < 2; ++hh) {
+                        const int row = rt * ROWS + g + 8 * hh;
+                        if (row < R) {
+                            float* to = a.scores + ((int64_t)b * a.n_q_heads + hk * a.group + row) * max_seq + tok0;
 #pragma unroll
-                        for (int hh = 0; hh < 2; ++hh) {
-                            const int row = rt * ROWS + mt * 16 + g + 8 * hh;
-                            if (row < R) {
-                                float* to = a.scores + ((int64_t)b * a.n_q_heads + hk * a.group + row) * max_seq + tok0;
+                            for (int j = 0; j < 2; ++j)
 #pragma unroll
-                                for (int j = 0; j < 2; ++j)
-#pragma unroll
-                                    for (int e = 0; e < 2; ++e) to[tok_of<P>(t, e, j)] = sc[mt][j][2 * hh + e] * mul;
-                            }
+                                for (int e = 0; e < 2; ++e) to[tok_of<P>(t, e, j)] = sc[j][2 * hh + e] * mul;
                         }
+                    }
                 }
                 // ---- running softmax: the reference moves only when a score passes it by 8 (2^8 keeps P in range)
-                float top[MT][2];
+                float top[2];
                 bool grow = false;
 #pragma unroll
-                for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-                    for (int hh = 0; hh < 2; ++hh) {
-                        const float x = mul * fmaxf(fmaxf(sc[mt][0][2 * hh], sc[mt][0][2 * hh + 1]),
-                                                    fmaxf(sc[mt][1][2 * hh], sc[mt][1][2 * hh + 1]));
-                        top[mt][hh] = x;
-                        grow |= x > m_run[mt][hh] + 8.f;
-                    }
+                for (int hh = 0; hh < 2; ++hh) {
+                    const float x = mul * fmaxf(fmaxf(sc[0][2 * hh], sc[0][2 * hh + 1]),
+                                                fmaxf(sc[1][2 * hh], sc[1][2 * hh + 1]));
+                    top[hh] = x;
+                    grow |= x > m_run[hh] + 8.f;
+                }
                 if (__any_sync(0xffffffffu, grow)) {
 #pragma unroll
-                    for (int mt = 0; mt < MT; ++mt)
+                    for (int hh = 0; hh < 2; ++hh) {
+                        float x = top[hh];
+                        x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 1));
+                        x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 2));
+                        x = fmaxf(x, m_run[hh]);
+                        const float al = ex2_approx(m_run[hh] - x);
+                        m_run[hh] = x;
+                        l_run[hh] *= al;
 #pragma unroll
-                        for (int hh = 0; hh < 2; ++hh) {
-                            float x = top[mt][hh];
-                            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 1));
-                            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 2));
-                            x = fmaxf(x, m_run[mt][hh]);
-                            const float al = ex2_approx(m_run[mt][hh] - x);
-                            m_run[mt][hh] = x;
-                            l_run[mt][hh] *= al;
-#pragma unroll
-                            for (int s = 0; s < 16; ++s) { o[mt][s][2 * hh] *= al; o[mt][s][2 * hh + 1] *= al; }
-                        }
+                        for (int s = 0; s < 16; ++s) { o[s][2 * hh] *= al; o[s][2 * hh + 1] *= al; }
+                    }
                 }
                 // P as A fragments: (row g, tile 0), (row g+8, tile 0), (row g, tile 1), (row g+8, tile 1); fp32: three terms
-                uint32_t pa[MT][F32 ? 3 : 1][4];
+                uint32_t pa[kSplit][4];
 #pragma unroll
-                for (int mt = 0; mt < MT; ++mt)
+                for (int x = 0; x < 4; ++x) {
+                    const int hh = x & 1, j = x >> 1;
+                    float p0 = ex2_approx(fmaf(sc[j][2 * hh], mul, -m_run[hh]));
+                    float p1 = ex2_approx(fmaf(sc[j][2 * hh + 1], mul, -m_run[hh]));
+                    l_run[hh] += p0 + p1;
 #pragma unroll
-                    for (int x = 0; x < 4; ++x) {
-                        const int hh = x & 1, j = x >> 1;
-                        float p0 = ex2_approx(fmaf(sc[mt][j][2 * hh], mul, -m_run[mt][hh]));
-                        float p1 = ex2_approx(fmaf(sc[mt][j][2 * hh + 1], mul, -m_run[mt][hh]));
-                        l_run[mt][hh] += p0 + p1;
-#pragma unroll
-                        for (int s = 0; s < (F32 ? 3 : 1); ++s) {
-                            pa[mt][s][x] = pack_bf16x2_rn(p0, p1);
-                            p0 -= __uint_as_float(pa[mt][s][x] << 16);
-                            p1 -= __uint_as_float(pa[mt][s][x] & 0xffff0000u);
-                        }
+                    for (int s = 0; s < kSplit; ++s) {
+                        pa[s][x] = pack_bf16x2_rn(p0, p1);
+                        p0 -= __uint_as_float(pa[s][x] << 16);
+                        p1 -= __uint_as_float(pa[s][x] & 0xffff0000u);
                     }
+                }
                 // ---- P . V
                 uint32_t vw[4][P / 2];
                 uint2 lv[4];
@@ -513,22 +533,16 @@ __global__ void __launch_bounds__(kAttnWarps * 32, MINB) attn_rows(const AttnArg
                     attn_v<P>(vw[0], vw[1], r, ga, xa);
                     attn_v<P>(vw[2], vw[3], r, gb, xb);
 #pragma unroll
-                    for (int mt = 0; mt < MT; ++mt)
+                    for (int s = 0; s < 4; ++s) {
+                        float (&acc)[4] = o[2 * r + s];
+                        float d[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                        for (int s = 0; s < 4; ++s) {
-                            float (&acc)[4] = o[mt][2 * r + s];
-                            if (F32) {
-                                float d[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                                for (int c = 2; c >= 0; --c) {
-                                    const uint32_t (&p)[4] = pa[mt][F32 ? c : 0];
-                                    mma_bf16(d, p[0], p[1], p[2], p[3], xa[s], xb[s]);
-                                }
-                                acc[0] += d[0]; acc[1] += d[1]; acc[2] += d[2]; acc[3] += d[3];
-                            } else {
-                                mma_bf16(acc, pa[mt][0][0], pa[mt][0][1], pa[mt][0][2], pa[mt][0][3], xa[s], xb[s]);
-                            }
+                        for (int c = 2; c >= 0; --c) {
+                            const uint32_t (&p)[4] = pa[c];
+                            mma_bf16(d, p[0], p[1], p[2], p[3], xa[s], xb[s]);
                         }
+                        acc[0] += d[0]; acc[1] += d[1]; acc[2] += d[2]; acc[3] += d[3];
+                    }
                 }
             }
             __syncwarp();                      // every lane has read the stage
@@ -538,73 +552,62 @@ __global__ void __launch_bounds__(kAttnWarps * 32, MINB) attn_rows(const AttnArg
         // ---- the run's result: a lane holds slots [32t, 32t + 32) of rows g and g + 8 of each m tile
         const bool whole = k0 == 0 && k1 == cc.n;
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
+        for (int hh = 0; hh < 2; ++hh) {
+            float l = l_run[hh];
+            l += __shfl_xor_sync(0xffffffffu, l, 1);
+            l += __shfl_xor_sync(0xffffffffu, l, 2);
+            const int r = g + 8 * hh, row = rt * ROWS + r;
+            const int i = row / a.group, hq = hk * a.group + row - i * a.group;
+            const float m = m_run[hh];
+            if (!whole) {
+                if (row < R) {
+                    float* dst = a.partials + ((int64_t)(2 * me + (k0 == 0 ? 1 : 0)) * a.part_rows + r) * kAttnPart;
 #pragma unroll
-            for (int hh = 0; hh < 2; ++hh) {
-                float l = l_run[mt][hh];
-                l += __shfl_xor_sync(0xffffffffu, l, 1);
-                l += __shfl_xor_sync(0xffffffffu, l, 2);
-                const int r = mt * 16 + g + 8 * hh, row = rt * ROWS + r;
-                const int i = row / a.group, hq = hk * a.group + row - i * a.group;
-                const float m = m_run[mt][hh];
-                if (!whole) {
-                    if (row < R) {
-                        float* dst = a.partials + ((int64_t)(2 * me + (k0 == 0 ? 1 : 0)) * a.part_rows + r) * kAttnPart;
-#pragma unroll
-                        for (int c = 0; c < 4; ++c) {
-                            reinterpret_cast<float4*>(dst + 32 * t)[c] = make_float4(o[mt][4 * c][2 * hh], o[mt][4 * c + 1][2 * hh], o[mt][4 * c + 2][2 * hh], o[mt][4 * c + 3][2 * hh]);
-                            reinterpret_cast<float4*>(dst + 32 * t + 16)[c] = make_float4(o[mt][4 * c][2 * hh + 1], o[mt][4 * c + 1][2 * hh + 1], o[mt][4 * c + 2][2 * hh + 1], o[mt][4 * c + 3][2 * hh + 1]);
-                        }
-                        if (t == 0) { dst[D] = m; dst[D + 1] = l; }
+                    for (int c = 0; c < 4; ++c) {
+                        reinterpret_cast<float4*>(dst + 32 * t)[c] = make_float4(o[4 * c][2 * hh], o[4 * c + 1][2 * hh], o[4 * c + 2][2 * hh], o[4 * c + 3][2 * hh]);
+                        reinterpret_cast<float4*>(dst + 32 * t + 16)[c] = make_float4(o[4 * c][2 * hh + 1], o[4 * c + 1][2 * hh + 1], o[4 * c + 2][2 * hh + 1], o[4 * c + 3][2 * hh + 1]);
                     }
-                    continue;
+                    if (t == 0) { dst[D] = m; dst[D + 1] = l; }
                 }
-                const bool live = row < R && (!a.tree || i < sv.nd) && l != 0.f;
-                const float inv = live ? kValueUp / l : 0.f;
-                float v[2][16];
+                continue;
+            }
+            const bool live = row < R && (!a.tree || i < sv.nd) && l != 0.f;
+            const float inv = live ? kValueUp / l : 0.f;
+            float v[2][16];
 #pragma unroll
-                for (int s = 0; s < 16; ++s)
+            for (int s = 0; s < 16; ++s)
 #pragma unroll
-                    for (int e = 0; e < 2; ++e) v[e][s] = live ? o[mt][s][2 * hh + e] * inv : 0.f;
-                const int64_t at = (((int64_t)b * a.n_draft + i) * a.n_q_heads + hq) * D;
-                if (a.lse && row < R && t == 0) a.lse[(int64_t)b * a.n_q_heads + hq] = l > 0.f ? m + log2f(l) : (l == 0.f ? INFINITY : l);
-                if (!a.inv_perm_v) {
-                    if (row < R) {
+                for (int e = 0; e < 2; ++e) v[e][s] = live ? o[s][2 * hh + e] * inv : 0.f;
+            const int64_t at = (((int64_t)b * a.n_draft + i) * a.n_q_heads + hq) * D;
+            if (a.lse && row < R && t == 0) a.lse[(int64_t)b * a.n_q_heads + hq] = l > 0.f ? m + log2f(l) : (l == 0.f ? INFINITY : l);
+            if (!a.inv_perm_v) {
+                if (row < R) {
 #pragma unroll
-                        for (int e = 0; e < 2; ++e) {
-                            if (F32) {
-                                float4* to = reinterpret_cast<float4*>(static_cast<float*>(a.out) + at + 32 * t + 16 * e);
+                    for (int e = 0; e < 2; ++e) {
+                        float4* to = reinterpret_cast<float4*>(static_cast<float*>(a.out) + at + 32 * t + 16 * e);
 #pragma unroll
-                                for (int c = 0; c < 4; ++c) to[c] = make_float4(v[e][4 * c], v[e][4 * c + 1], v[e][4 * c + 2], v[e][4 * c + 3]);
-                            } else {
-                                uint4* to = reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(a.out) + at + 32 * t + 16 * e);
-#pragma unroll
-                                for (int c = 0; c < 2; ++c)
-                                    to[c] = make_uint4(pack_bf16x2_rn(v[e][8 * c], v[e][8 * c + 1]), pack_bf16x2_rn(v[e][8 * c + 2], v[e][8 * c + 3]),
-                                                       pack_bf16x2_rn(v[e][8 * c + 4], v[e][8 * c + 5]), pack_bf16x2_rn(v[e][8 * c + 6], v[e][8 * c + 7]));
-                            }
-                        }
+                        for (int c = 0; c < 4; ++c) to[c] = make_float4(v[e][4 * c], v[e][4 * c + 1], v[e][4 * c + 2], v[e][4 * c + 3]);
                     }
-                } else {          // channels in their own order: one row at a time through shared memory
-                    const int32_t* ip = a.inv_perm_v + hk * D;
-                    int sl[4];
+                }
+            } else {          // channels in their own order: one row at a time through shared memory
+                const int32_t* ip = a.inv_perm_v + hk * D;
+                int sl[4];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) sl[e] = ip[4 * lane + e] & (D - 1);
-                    for (int gg = 0; gg < 8; ++gg) {
-                        if (rt * ROWS + mt * 16 + gg + 8 * hh >= R) break;
-                        __syncwarp();
-                        if (g == gg) {
+                for (int e = 0; e < 4; ++e) sl[e] = ip[4 * lane + e] & (D - 1);
+                for (int gg = 0; gg < 8; ++gg) {
+                    if (rt * ROWS + gg + 8 * hh >= R) break;
+                    __syncwarp();
+                    if (g == gg) {
 #pragma unroll
-                            for (int s = 0; s < 16; ++s) { orow[32 * t + s] = v[0][s]; orow[32 * t + 16 + s] = v[1][s]; }
-                        }
-                        __syncwarp();
-                        const int64_t to = __shfl_sync(0xffffffffu, at, gg * 4) + 4 * lane;
-                        const float y0 = orow[sl[0]], y1 = orow[sl[1]], y2 = orow[sl[2]], y3 = orow[sl[3]];
-                        if (F32) *reinterpret_cast<float4*>(static_cast<float*>(a.out) + to) = make_float4(y0, y1, y2, y3);
-                        else *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(a.out) + to) = make_uint2(pack_bf16x2_rn(y0, y1), pack_bf16x2_rn(y2, y3));
+                        for (int s = 0; s < 16; ++s) { orow[32 * t + s] = v[0][s]; orow[32 * t + 16 + s] = v[1][s]; }
                     }
+                    __syncwarp();
+                    const int64_t to = __shfl_sync(0xffffffffu, at, gg * 4) + 4 * lane;
+                    const float y0 = orow[sl[0]], y1 = orow[sl[1]], y2 = orow[sl[2]], y3 = orow[sl[3]];
+                    *reinterpret_cast<float4*>(static_cast<float*>(a.out) + to) = make_float4(y0, y1, y2, y3);
                 }
             }
+        }
         cc.k = k1;
         if (k1 == cc.n) next_pair(cc);
     }
@@ -619,17 +622,9 @@ __global__ void __launch_bounds__(kAttnWarps * 32, MINB) attn_rows(const AttnArg
     pdl_trigger();
 }
 
-// Three blocks of one m tile per SM (168 registers a thread) where their shared memory fits, two otherwise.
-template <int P, int MT, bool F32>
-int attn_blocks(const AttnArgs& a) {
-    if (MT == 2 || F32) return 2;
-    return 3 * (AGeo<P>::smem_bytes(kHeadDim / a.fmt.block) + 1024) <= 228 * 1024 ? 3 : 2;
-}
-
-template <int P, bool N16, int MT, bool F32>
+template <int P, bool N16>
 kvbfp_status launch_attn(const AttnArgs& a, int grid, cudaStream_t s) {
-    constexpr int MINB = (MT == 2 || F32 || P != 4) ? 2 : 3;
-    auto kernel = attn_rows<P, N16, MT, F32, MINB>;
+    auto kernel = attn_rows<P, N16>;
     static std::atomic<bool> attr_set[64];      // per device; setting the attribute twice is harmless
     int dev = 0;
     KVBFP_CUDA(cudaGetDevice(&dev));
@@ -645,7 +640,7 @@ kvbfp_status launch_attn(const AttnArgs& a, int grid, cudaStream_t s) {
         if (st == KVBFP_OK) st = make_row_map(&v_map, a.v_mant, rows, 128, AGeo<P>::TILE * P / 8);
         if (st != KVBFP_OK) return st;
     }
-    KVBFP_CUDA(launch_pdl(attn_prep<P, MT, F32>, dim3(a.fmt.batch * a.fmt.n_kv_heads * a.n_row_tiles), dim3(128), 0, s, a));
+    KVBFP_CUDA(launch_pdl(attn_prep<P>, dim3(a.fmt.batch * a.fmt.n_kv_heads * a.n_row_tiles), dim3(128), 0, s, a));
     KVBFP_LAUNCH_CHECK("attn_prep");
     KVBFP_CUDA(launch_pdl(kernel, dim3(grid), dim3(kAttnWarps * 32), AGeo<P>::smem_bytes(kHeadDim / a.fmt.block), s, a, k_map, v_map));
     KVBFP_LAUNCH_CHECK("attn_rows");
@@ -653,17 +648,8 @@ kvbfp_status launch_attn(const AttnArgs& a, int grid, cudaStream_t s) {
 }
 
 template <int P>
-AttnShape attn_shape_p(const AttnArgs& a) {
-    const int blocks = P != 4 || a.rows_tile == 32 || !a.q_is_bf16 ? 2 : attn_blocks<P, 1, false>(a);
-    return {AGeo<P>::TILE, blocks};
-}
-
-template <int P>
 kvbfp_status launch_attn_p(const AttnArgs& a, int grid, cudaStream_t s) {
-    const bool n16 = a.fmt.block == 16;
-    if (!a.q_is_bf16) return n16 ? launch_attn<P, true, 1, true>(a, grid, s) : launch_attn<P, false, 1, true>(a, grid, s);
-    if (a.rows_tile == 16) return n16 ? launch_attn<P, true, 1, false>(a, grid, s) : launch_attn<P, false, 1, false>(a, grid, s);
-    return n16 ? launch_attn<P, true, 2, false>(a, grid, s) : launch_attn<P, false, 2, false>(a, grid, s);
+    return a.fmt.block == 16 ? launch_attn<P, true>(a, grid, s) : launch_attn<P, false>(a, grid, s);
 }
 
 }  // namespace

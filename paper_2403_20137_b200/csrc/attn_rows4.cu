@@ -2,6 +2,5 @@
 #include "attn_rows.cuh"
 
 namespace kvbfp {
-AttnShape attn_shape4(const AttnArgs& a) { return attn_shape_p<4>(a); }
 kvbfp_status launch_attn_rows4(const AttnArgs& a, int grid, cudaStream_t s) { return launch_attn_p<4>(a, grid, s); }
 }  // namespace kvbfp

@@ -2,6 +2,5 @@
 #include "attn_rows.cuh"
 
 namespace kvbfp {
-AttnShape attn_shape6(const AttnArgs& a) { return attn_shape_p<6>(a); }
 kvbfp_status launch_attn_rows6(const AttnArgs& a, int grid, cudaStream_t s) { return launch_attn_p<6>(a, grid, s); }
 }  // namespace kvbfp

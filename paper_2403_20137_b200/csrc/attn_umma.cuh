@@ -66,9 +66,9 @@ struct UGeo {
     static constexpr int Q_BYTES = N * kHeadDim * 2;
     static constexpr int E_OFF = Q_OFF + TEAMS * Q_BYTES;        // exponent bytes: UNITS x 128 x row_e
     // behind them (in floats), per group of four warps: row data, drafted positions and view of two runs, references,
-    // steps, factors, sums, reduction, channel table; then barriers
+    // factors, sums, reduction, channel table; then barriers
     static constexpr int F_RI = 0, F_DPOS = F_RI + WGS * 2 * C * 4, F_VIEW = F_DPOS + WGS * 2 * kAttnMaxDraft,
-                         F_MREF = F_VIEW + WGS * 2 * 8, F_STEP = F_MREF + WGS * C, F_FAC = F_STEP + WGS * C, F_SUM = F_FAC + WGS * C,
+                         F_MREF = F_VIEW + WGS * 2 * 8, F_FAC = F_MREF + WGS * C, F_SUM = F_FAC + WGS * C,
                          F_RED = F_SUM + WGS * C, F_CHAN = F_RED + WGS * 4 * C, F_UNSET = F_CHAN + WGS * kHeadDim, F_END = F_UNSET + 8;
     static constexpr int SMALL = F_END * 4 + TEAMS * (RING + 7) * 8;
     __host__ __device__ static int smem_bytes(int row_e) { return E_OFF + UNITS * kUTile * row_e + SMALL; }
@@ -419,7 +419,7 @@ __global__ void __launch_bounds__(UGeo<P, N>::THREADS, 1) attn_umma(const AttnAr
         // ================================================================ a team: H threads per token
         const int wg = warp >> 2, team = wg / H, half = H == 2 ? wg & 1 : 0, m_pos = tid & 127, w4 = warp & 3, bar_id = 1 + wg;
         const uint32_t tmt = tm + team * G_::TM_TEAM + ((uint32_t)w4 << 21);        // lane field: 32 * quarter << 16
-        float *mref = fl + G_::F_MREF + wg * C, *mstep = fl + G_::F_STEP + wg * C, *mfac = fl + G_::F_FAC + wg * C,
+        float *mref = fl + G_::F_MREF + wg * C, *mfac = fl + G_::F_FAC + wg * C,
               *lsum = fl + G_::F_SUM + wg * C, *red = fl + G_::F_RED + wg * 4 * C;
         int* chan = reinterpret_cast<int*>(fl + G_::F_CHAN) + wg * D;
         int* unset = reinterpret_cast<int*>(fl + G_::F_UNSET) + wg;         // rows that have seen nothing yet, as a bit mask
@@ -626,7 +626,7 @@ __global__ void __launch_bounds__(UGeo<P, N>::THREADS, 1) attn_umma(const AttnAr
                 if (a.scores && tt + m_pos < max_seq) {       // for the weight pass: y against the reference, plus the reference
                     float* to = a.scores + ((int64_t)b * a.n_q_heads + hk * a.group + row0) * max_seq + tt + m_pos;
 #pragma unroll
-                    for (int j = 0; j < (C < 8 ? C : 8); ++j)            // (one token: at most eight rows, the first)
+                    for (int j = 0; j < 8; ++j)            // (one token: at most eight rows, the first)
                         if (row0 + j < R) {
                             float y0, y1;
                             f2_split(y[j / 2], y0, y1);
