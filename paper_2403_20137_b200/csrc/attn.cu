@@ -166,7 +166,7 @@ __global__ void __launch_bounds__(128) attn_mass(const AttnArgs a) {
 
 // Query rows per work item: up to 64 bf16 rows of a kv head share its tiles; fp32 queries take 16 at a time (their three
 // bf16 terms fill the registers of attn_rows).
-inline int rows_tile_for(int rows, bool bf16) { return !bf16 || rows <= 16 ? 16 : rows <= 32 ? 32 : 64; }
+inline int rows_tile_for(int rows, bool bf16) { return bf16 && rows <= 8 ? 8 : !bf16 || rows <= 16 ? 16 : rows <= 32 ? 32 : 64; }
 inline int max_workers(bool bf16) { return (bf16 ? 3 : 2 * kAttnWarps) * kAttnMaxSms; }
 
 inline size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
@@ -185,7 +185,7 @@ size_t lay_out(const kvbfp_format& f, int n_q_heads, int n_draft, bool bf16, boo
     uint8_t* views = take((size_t)f.batch * sizeof(SeqView));
     uint8_t* dpos = take((size_t)f.batch * kAttnMaxDraft * sizeof(int));
     uint8_t* info = take(items * tile * sizeof(RowInfo));
-    uint8_t* frag = take(items * tile * kHeadDim * 2 * (bf16 ? 1 : 3));
+    uint8_t* frag = take(items * (tile < 16 ? 16 : tile) * kHeadDim * 2 * (bf16 ? 1 : 3));
     uint8_t *lse = nullptr, *scores = nullptr;
     if (with_mass) {
         lse = take((size_t)f.batch * n_q_heads * 4);

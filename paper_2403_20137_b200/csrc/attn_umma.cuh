@@ -46,14 +46,15 @@ __device__ __forceinline__ int umma_slot(int m) {
     return (m & ~3) | ((m & 1) << 1) | ((m >> 1) & 1);
 }
 
-template <int P, int N>
+template <int P, int ROWS>
 struct UGeo {
+    static constexpr int N = ROWS < 16 ? 16 : ROWS;              // columns of the products: 16 at least, zeros behind ROWS
     static constexpr int ROW_M = kHeadDim * P / 8;
-    static constexpr int TEAMS = attn_teams(P, N);
+    static constexpr int TEAMS = attn_teams(P, ROWS);
     static constexpr int H = TEAMS == 3 ? 1 : 2;                 // threads per token
     static constexpr int WGS = TEAMS * H;                        // groups of four warps
     static constexpr int THREADS = (WGS * 4 + TEAMS) * 32;
-    static constexpr int C = N / H;                              // query rows of a thread
+    static constexpr int C = ROWS / H;                           // query rows of a thread
     static constexpr int UNIT = kUTile * ROW_M;                  // a tile's K or V rows
     static constexpr int KS = P == 4 && N == 32 || P == 8 && N == 64 ? 1 : 2;       // packed K rows a team keeps
     static constexpr int VS = P == 4 && N == 64 || P == 6 && N <= 32 ? 2 : 1;       // and V rows
@@ -78,17 +79,18 @@ struct UGeo {
 
 // pi(Q) of one (sequence, kv head, row tile) per block, as the shared-memory image of the B operand: two panels of 64
 // positions, lines of 128 bytes per row, 16-byte pieces at piece ^ (row % 8).
-template <int P, int N>
+template <int P, int ROWS>
 __global__ void __launch_bounds__(128) umma_prep(const AttnArgs a) {
-    __shared__ float sq[N][kHeadDim + 4];
+    constexpr int N = UGeo<P, ROWS>::N;
+    __shared__ float sq[ROWS][kHeadDim + 4];
     __shared__ int sp[kHeadDim];
-    prep_common<N, false>(a, sq, sp);
+    prep_common<ROWS, false>(a, sq, sp);
     uint8_t* to = reinterpret_cast<uint8_t*>(a.qfrag) + (int64_t)blockIdx.x * (N * kHeadDim * 2);
     for (int x = threadIdx.x; x < N * 16; x += 128) {       // 16-byte pieces: row, positions [8 c, 8 c + 8)
         const int c = x & 15, row = x >> 4;
-        uint32_t w[4];
+        uint32_t w[4] = {0u, 0u, 0u, 0u};
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
+        for (int j = 0; j < 4 && row < ROWS; ++j)
             w[j] = pack_bf16x2_rn(sq[row][sp[umma_slot<P>(8 * c + 2 * j)]], sq[row][sp[umma_slot<P>(8 * c + 2 * j + 1)]]);
         *reinterpret_cast<uint4*>(to + (c >> 3) * (N * 128) + row * 128 + (((c & 7) ^ (row & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
     }
@@ -224,13 +226,37 @@ __device__ __forceinline__ float across_lanes(float (&v)[C], int lane) {
     return v[0];
 }
 
+// Changes the scores of a tile by fn(value, column): up to eight columns a thread stay in registers, more are changed in
+// tensor memory, eight at a time.
+template <int C, class F>
+__device__ __forceinline__ void change_scores(uint32_t tm_s, uint32_t (&raw)[C], F fn) {
+    if constexpr (C <= 8) {
+#pragma unroll
+        for (int e = 0; e < C; ++e) raw[e] = __float_as_uint(fn(__uint_as_float(raw[e]), e));
+    } else {
+#pragma unroll 1
+        for (int j = 0; j < C; j += 8) {
+            uint32_t r[8];
+            tmem_ld<8>(tm_s + j, r);
+            tmem_wait_ld(r);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) r[e] = __float_as_uint(fn(__uint_as_float(r[e]), j + e));
+            tmem_st<8>(tm_s + j, r);
+        }
+        tmem_wait_st();
+    }
+}
+
 __device__ __noinline__ bool umma_wait_slow(uint32_t bar, uint32_t parity) { return mbar_wait_bounded(bar, parity); }
 
-template <int P, bool N16, int N>
-__global__ void __launch_bounds__(UGeo<P, N>::THREADS, 1) attn_umma(const AttnArgs a, const __grid_constant__ CUtensorMap k_map,
+template <int P, bool N16, int ROWS>
+__global__ void __launch_bounds__(UGeo<P, ROWS>::THREADS, 1) attn_umma(const AttnArgs a, const __grid_constant__ CUtensorMap k_map,
                                                                     const __grid_constant__ CUtensorMap v_map) {
-    using G_ = UGeo<P, N>;
+    using G_ = UGeo<P, ROWS>;
+    constexpr int N = G_::N;
     constexpr int D = kHeadDim, ROW_M = G_::ROW_M, UNITS = G_::UNITS, RING = G_::RING, KS = G_::KS, VS = G_::VS, C = G_::C, H = G_::H, TEAMS = G_::TEAMS;
+    constexpr int ST = C < 8 ? C : 8;      // columns of a step of the loops over tensor memory
+    constexpr bool KEEP = C <= 8;          // scores stay in registers
     constexpr int TEAM_WARPS = G_::WGS * 4, SWP = 2 * N;      // bytes of a P line
     extern __shared__ __align__(1024) uint8_t smem[];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -436,7 +462,7 @@ __global__ void __launch_bounds__(UGeo<P, N>::THREADS, 1) attn_umma(const AttnAr
         auto fetch = [&](const Cursor& c, int par) {
             if (c.b < B) {
                 if (m_pos < C)
-                    cp_async16(smem_u32(fl + G_::F_RI + ((wg * 2 + par) * C + m_pos) * 4), a.rows + ((int64_t)c.b * HR + c.hr) * N + half * C + m_pos);
+                    cp_async16(smem_u32(fl + G_::F_RI + ((wg * 2 + par) * C + m_pos) * 4), a.rows + ((int64_t)c.b * HR + c.hr) * ROWS + half * C + m_pos);
                 else if (m_pos >= 64 && m_pos < 64 + kAttnMaxDraft / 4 && a.tree)
                     cp_async16(smem_u32(fl + G_::F_DPOS + (wg * 2 + par) * kAttnMaxDraft + (m_pos - 64) * 4), a.dpos + c.b * kAttnMaxDraft + (m_pos - 64) * 4);
                 else if (m_pos >= 96 && m_pos < 98)
@@ -471,12 +497,15 @@ __global__ void __launch_bounds__(UGeo<P, N>::THREADS, 1) attn_umma(const AttnAr
             return top;
         };
 
+        if (ROWS < N && half == 0) sts128(pline ^ (ROWS * 2), 0u, 0u, 0u, 0u);       // columns of P that no row has
+        static_assert(N - ROWS == 0 || (ROWS == 8 && N == 16), "one piece of 16 bytes");
+
         Cursor c = seek(first_item), cn = c;
         fetch(c, 0);
         int it = 0, run = 0, k_next = n_mine > 0 ? convert_k(0) : 0;
         while (it < n_mine) {
             const int b = c.b, hk = c.hr / a.n_row_tiles, rt = c.hr - hk * a.n_row_tiles, par = run & 1;
-            const int k0 = c.k, k1 = min(c.n, k0 + n_mine - it), row0 = rt * N + half * C;
+            const int k0 = c.k, k1 = min(c.n, k0 + n_mine - it), row0 = rt * ROWS + half * C;
             cn = c;
             next_pair(cn);
             asm volatile("cp.async.wait_group 0;" ::: "memory");
@@ -514,49 +543,33 @@ __global__ void __launch_bounds__(UGeo<P, N>::THREADS, 1) attn_umma(const AttnAr
                 const uint32_t tm_s = tmt + G_::TM_S + (it & 1) * N + half * C;
                 const int tt = tile_token(sv, k, kUTile);
                 float mul = up * to_log2 * __uint_as_float(k_top << 23);
-                if (a.softcap > 0.f) {       // cap, in tensor memory
+                uint32_t raw[C];
+                if (KEEP) {
+                    tmem_ld<C>(tm_s, raw);
+                    tmem_wait_ld(raw);
+                }
+                if (a.softcap > 0.f) {
                     const float in = cap_in * __uint_as_float(k_top << 23);
                     mul = a.softcap * to_log2;
-#pragma unroll 1
-                    for (int j = 0; j < C; j += 8) {
-                        uint32_t r[8];
-                        tmem_ld<8>(tm_s + j, r);
-                        tmem_wait_ld(r);
-#pragma unroll
-                        for (int e = 0; e < 8; ++e)      // tanh x = 1 - 2 / (1 + e^2x): about 2e-7 absolute
-                            r[e] = __float_as_uint(fmaf(-2.f, rcp_approx(1.f + ex2_approx(__uint_as_float(r[e]) * in)), 1.f));
-                        tmem_st<8>(tm_s + j, r);
-                    }
-                    tmem_wait_st();
+                    change_scores<C>(tm_s, raw, [&](float y, int) { return fmaf(-2.f, rcp_approx(1.f + ex2_approx(y * in)), 1.f); });      // tanh x = 1 - 2 / (1 + e^2x): about 2e-7 absolute
                 }
                 const bool masked = a.slopes != nullptr || !(tt + kUTile <= sv.ctx && (tt >= clear_lo || tt + kUTile <= sv.pf));
                 if (masked) {
-                    // bias and masks, in tensor memory: log2 units afterwards
+                    // bias and masks: log2 units afterwards
                     const int tok = tt + m_pos;
                     const bool in_ctx = tok < sv.ctx;
                     const int jd = in_ctx ? 0 : min(tok - sv.ctx, kAttnMaxDraft - 1);
                     const bool drafted = !in_ctx && tok - sv.ctx < sv.nd;
                     const int kpos = in_ctx || !drafted ? tok : dpos[jd];
                     const bool always = tok < sv.pf, from = tok >= sv.first;
-#pragma unroll 1
-                    for (int j = 0; j < C; j += 8) {
-                        uint32_t r[8];
-                        tmem_ld<8>(tm_s + j, r);
-                        tmem_wait_ld(r);
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            float y = __uint_as_float(r[e]);
-                            const RowInfo x = ri[j + e];
-                            const int dist = x.pos - kpos;
-                            const bool near = a.window == 0 || dist < a.window;
-                            const bool bit = (((jd < 32 ? x.m0 : x.m1) >> (jd & 31)) & 1u) != 0u;
-                            const bool see = in_ctx ? (from && near) || always : drafted && bit && near;
-                            y = see ? y * mul - x.slope * to_log2 * (float)dist : -INFINITY;
-                            r[e] = __float_as_uint(y);
-                        }
-                        tmem_st<8>(tm_s + j, r);
-                    }
-                    tmem_wait_st();
+                    change_scores<C>(tm_s, raw, [&](float y, int e) {
+                        const RowInfo x = ri[e];
+                        const int dist = x.pos - kpos;
+                        const bool near = a.window == 0 || dist < a.window;
+                        const bool bit = (((jd < 32 ? x.m0 : x.m1) >> (jd & 31)) & 1u) != 0u;
+                        const bool see = in_ctx ? (from && near) || always : drafted && bit && near;
+                        return see ? y * mul - x.slope * to_log2 * (float)dist : -INFINITY;
+                    });
                     mul = 1.f;
                 }
                 // ---- running softmax against the references, which are raised at most once per tile
@@ -564,9 +577,10 @@ __global__ void __launch_bounds__(UGeo<P, N>::THREADS, 1) attn_umma(const AttnAr
                 const F2 mul2 = f2(mul, mul);
 #pragma unroll 1
                 for (int pass = 0;; ++pass) {
-                    uint32_t raw[C];
-                    tmem_ld<C>(tm_s, raw);
-                    tmem_wait_ld(raw);
+                    if (!KEEP) {
+                        tmem_ld<C>(tm_s, raw);
+                        tmem_wait_ld(raw);
+                    }
                     float top = -INFINITY;
 #pragma unroll
                     for (int j = 0; j < C; j += 4) {
@@ -581,15 +595,18 @@ __global__ void __launch_bounds__(UGeo<P, N>::THREADS, 1) attn_umma(const AttnAr
                     }
                     if (pass != 0 || !named_any(bar_id, 128, top > 8.f || behind)) break;
 #pragma unroll 1
-                    for (int j = 0; j < C; j += 8) {
-                        uint32_t r[8];
-                        tmem_ld<8>(tm_s + j, r);
-                        tmem_wait_ld(r);
-                        float v[8];
+                    for (int j = 0; j < C; j += ST) {
+                        uint32_t r[ST];
+                        if (!KEEP) {
+                            tmem_ld<ST>(tm_s + j, r);
+                            tmem_wait_ld(r);
+                        }
+                        float v[ST];
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) v[e] = fmaf(__uint_as_float(r[e]), mul, mref[j + e]);
-                        const float mine = across_lanes<8, true>(v, lane);
-                        if ((lane & 3) == 0) red[w4 * C + j + (lane >> 2)] = mine;
+                        for (int e = 0; e < ST; ++e) v[e] = fmaf(__uint_as_float(KEEP ? raw[e] : r[e]), mul, mref[j + e]);
+                        const float mine = across_lanes<ST, true>(v, lane);
+                        constexpr int GAP = 32 / ST;          // lanes that end up with the same column
+                        if (lane % GAP == 0) red[w4 * C + j + lane / GAP] = mine;
                     }
                     named_sync(bar_id, 128);
                     if (m_pos < 32) {
@@ -612,13 +629,13 @@ __global__ void __launch_bounds__(UGeo<P, N>::THREADS, 1) attn_umma(const AttnAr
                     if (k > k0) {          // (the product of the tile before is done: waited for above)
                         tmem_fence_after();
 #pragma unroll 1
-                        for (int j = 0; j < C; j += 8) {
-                            uint32_t o[8];
-                            tmem_ld<8>(tm_o + j, o);
+                        for (int j = 0; j < C; j += ST) {
+                            uint32_t o[ST];
+                            tmem_ld<ST>(tm_o + j, o);
                             tmem_wait_ld(o);
 #pragma unroll
-                            for (int e = 0; e < 8; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * mfac[j + e]);
-                            tmem_st<8>(tm_o + j, o);
+                            for (int e = 0; e < ST; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * mfac[j + e]);
+                            tmem_st<ST>(tm_o + j, o);
                         }
                         tmem_wait_st();
                     }
@@ -626,7 +643,7 @@ __global__ void __launch_bounds__(UGeo<P, N>::THREADS, 1) attn_umma(const AttnAr
                 if (a.scores && tt + m_pos < max_seq) {       // for the weight pass: y against the reference, plus the reference
                     float* to = a.scores + ((int64_t)b * a.n_q_heads + hk * a.group + row0) * max_seq + tt + m_pos;
 #pragma unroll
-                    for (int j = 0; j < 8; ++j)            // (one token: at most eight rows, the first)
+                    for (int j = 0; j < ST; ++j)           // (one token: eight rows at most)
                         if (row0 + j < R) {
                             float y0, y1;
                             f2_split(y[j / 2], y0, y1);
@@ -637,10 +654,10 @@ __global__ void __launch_bounds__(UGeo<P, N>::THREADS, 1) attn_umma(const AttnAr
                 const float vf = __uint_as_float((uint32_t)max((int)v_top - 9, 0) << 23);
                 const F2 vf2 = f2(vf, vf);
 #pragma unroll
-                for (int j = 0; j < C; j += 8) {
-                    uint32_t w[4];
+                for (int j = 0; j < C; j += ST) {
+                    uint32_t w[ST / 2];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
+                    for (int e = 0; e < ST / 2; ++e) {
                         float y0, y1;
                         f2_split(y[j / 2 + e], y0, y1);
                         const F2 p = f2(ex2_approx(y0), ex2_approx(y1));
@@ -649,7 +666,8 @@ __global__ void __launch_bounds__(UGeo<P, N>::THREADS, 1) attn_umma(const AttnAr
                         f2_split(f2_mul(p, vf2), p0, p1);
                         w[e] = pack_bf16x2_rn(p0, p1);
                     }
-                    sts128(pline ^ ((half * C + j) * 2), w[0], w[1], w[2], w[3]);
+                    if constexpr (ST == 8) sts128(pline ^ ((half * C + j) * 2), w[0], w[1], w[2], w[3]);
+                    else sts64(pline + half * 8, w[0], w[1]);
                 }
                 fence_async_shared();
                 tmem_fence_before();
@@ -690,12 +708,12 @@ __global__ void __launch_bounds__(UGeo<P, N>::THREADS, 1) attn_umma(const AttnAr
             named_sync(bar_id, 128);
             const int ch = a.inv_perm_v ? chan[slot_of] : slot_of;
 #pragma unroll 1
-            for (int j = 0; j < C; j += 8) {
-                uint32_t o[8];
-                tmem_ld<8>(tm_o + j, o);
+            for (int j = 0; j < C; j += ST) {
+                uint32_t o[ST];
+                tmem_ld<ST>(tm_o + j, o);
                 tmem_wait_ld(o);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
+                for (int e = 0; e < ST; ++e) {
                     const int row = row0 + j + e;
                     if (row >= R) break;
                     if (whole) {
@@ -724,10 +742,10 @@ __global__ void __launch_bounds__(UGeo<P, N>::THREADS, 1) attn_umma(const AttnAr
     pdl_trigger();
 }
 
-template <int P, bool N16, int N>
+template <int P, bool N16, int ROWS>
 kvbfp_status launch_umma(const AttnArgs& a, int grid, cudaStream_t s) {
-    using G_ = UGeo<P, N>;
-    auto kernel = attn_umma<P, N16, N>;
+    using G_ = UGeo<P, ROWS>;
+    auto kernel = attn_umma<P, N16, ROWS>;
     static std::atomic<bool> attr_set[64];      // per device; setting the attribute twice is harmless
     int dev = 0;
     KVBFP_CUDA(cudaGetDevice(&dev));
@@ -743,7 +761,7 @@ kvbfp_status launch_umma(const AttnArgs& a, int grid, cudaStream_t s) {
         if (st == KVBFP_OK) st = make_row_map(&v_map, a.v_mant, rows, 128, kUTile * P / 8);
         if (st != KVBFP_OK) return st;
     }
-    KVBFP_CUDA(launch_pdl(umma_prep<P, N>, dim3(a.fmt.batch * a.fmt.n_kv_heads * a.n_row_tiles), dim3(128), 0, s, a));
+    KVBFP_CUDA(launch_pdl(umma_prep<P, ROWS>, dim3(a.fmt.batch * a.fmt.n_kv_heads * a.n_row_tiles), dim3(128), 0, s, a));
     KVBFP_LAUNCH_CHECK("umma_prep");
     KVBFP_CUDA(launch_pdl(kernel, dim3(grid), dim3(G_::THREADS), G_::smem_bytes(kHeadDim / a.fmt.block), s, a, k_map, v_map));
     KVBFP_LAUNCH_CHECK("attn_umma");
@@ -753,6 +771,7 @@ kvbfp_status launch_umma(const AttnArgs& a, int grid, cudaStream_t s) {
 template <int P>
 kvbfp_status launch_umma_p(const AttnArgs& a, int grid, cudaStream_t s) {
     const bool n16 = a.fmt.block == 16;
+    if (a.rows_tile == 8) return n16 ? launch_umma<P, true, 8>(a, grid, s) : launch_umma<P, false, 8>(a, grid, s);
     if (a.rows_tile == 16) return n16 ? launch_umma<P, true, 16>(a, grid, s) : launch_umma<P, false, 16>(a, grid, s);
     if (a.rows_tile == 32) return n16 ? launch_umma<P, true, 32>(a, grid, s) : launch_umma<P, false, 32>(a, grid, s);
     return n16 ? launch_umma<P, true, 64>(a, grid, s) : launch_umma<P, false, 64>(a, grid, s);

@@ -16,11 +16,11 @@ __device__ __forceinline__ void tmem_dealloc(uint32_t addr, uint32_t columns) { 
 // Waits for this thread's loads; the registers are named so that nothing that uses them can be moved above.
 template <int C>
 __device__ __forceinline__ void tmem_wait_ld(uint32_t (&r)[C]) {
-    static_assert(C % 8 == 0, "eight at a time");
+    static_assert(C % 4 == 0, "four at a time");
     asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 #pragma unroll
-    for (int i = 0; i < C; i += 8)
-        asm volatile("" : "+r"(r[i]), "+r"(r[i + 1]), "+r"(r[i + 2]), "+r"(r[i + 3]), "+r"(r[i + 4]), "+r"(r[i + 5]), "+r"(r[i + 6]), "+r"(r[i + 7]));
+    for (int i = 0; i < C; i += 4)
+        asm volatile("" : "+r"(r[i]), "+r"(r[i + 1]), "+r"(r[i + 2]), "+r"(r[i + 3]));
 }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tmem_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
@@ -29,8 +29,10 @@ __device__ __forceinline__ void tmem_fence_after() { asm volatile("tcgen05.fence
 // Thread l of a warp: lane (its quarter of the lanes) + l, consecutive columns.  The values are there after tmem_wait_ld(r).
 template <int C>
 __device__ __forceinline__ void tmem_ld(uint32_t addr, uint32_t (&r)[C]) {
-    static_assert(C == 8 || C == 16 || C == 32, "column counts in use");
-    if constexpr (C == 8)
+    static_assert(C == 4 || C == 8 || C == 16 || C == 32, "column counts in use");
+    if constexpr (C == 4)
+        asm volatile("tcgen05.ld.sync.aligned.32x32b.x4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
+    else if constexpr (C == 8)
         asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
                      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]) : "r"(addr));
     else if constexpr (C == 16)
@@ -47,8 +49,10 @@ __device__ __forceinline__ void tmem_ld(uint32_t addr, uint32_t (&r)[C]) {
 }
 template <int C>
 __device__ __forceinline__ void tmem_st(uint32_t addr, const uint32_t (&r)[C]) {
-    static_assert(C == 8 || C == 16 || C == 32, "column counts in use");
-    if constexpr (C == 8)
+    static_assert(C == 4 || C == 8 || C == 16 || C == 32, "column counts in use");
+    if constexpr (C == 4)
+        asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%4], {%0,%1,%2,%3};" ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(addr) : "memory");
+    else if constexpr (C == 8)
         asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%8], {%0,%1,%2,%3,%4,%5,%6,%7};"
                      ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(addr) : "memory");
     else if constexpr (C == 16)
@@ -123,6 +127,9 @@ __device__ __forceinline__ uint2 lds64(uint32_t at) {
 }
 __device__ __forceinline__ void sts128(uint32_t at, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
     asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+__device__ __forceinline__ void sts64(uint32_t at, uint32_t a, uint32_t b) {
+    asm volatile("st.shared.v2.u32 [%0], {%1,%2};" ::"r"(at), "r"(a), "r"(b) : "memory");
 }
 __device__ __forceinline__ float rcp_approx(float x) {
     float y;
