@@ -114,7 +114,7 @@ kvbfp_status launch_attn_rows4(const AttnArgs& a, int grid, cudaStream_t s);
 kvbfp_status launch_attn_rows6(const AttnArgs& a, int grid, cudaStream_t s);
 kvbfp_status launch_attn_rows8(const AttnArgs& a, int grid, cudaStream_t s);
 // Teams (workers) of a block of attn_umma.
-__host__ __device__ constexpr int attn_teams(int mant_bits, int rows_tile) { return (mant_bits == 4 && rows_tile <= 32) || (mant_bits == 8 && rows_tile <= 16) ? 3 : 2; }
+__host__ __device__ constexpr int attn_teams(int mant_bits, int rows_tile) { return mant_bits == 4 && rows_tile <= 32 ? 3 : 2; }
 // umma_prep and attn_umma: bf16 queries, tiles of 128 tokens, one thread block per SM
 kvbfp_status launch_attn_umma4(const AttnArgs& a, int grid, cudaStream_t s);
 kvbfp_status launch_attn_umma6(const AttnArgs& a, int grid, cudaStream_t s);

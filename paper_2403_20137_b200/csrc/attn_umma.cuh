@@ -50,18 +50,17 @@ template <int P, int ROWS>
 struct UGeo {
     static constexpr int N = ROWS < 16 ? 16 : ROWS;              // columns of the products: 16 at least, zeros behind ROWS
     static constexpr int ROW_M = kHeadDim * P / 8;
-    static constexpr bool VT = P != 6 && ROWS <= 16;             // V^T in tensor memory
     static constexpr int TEAMS = attn_teams(P, ROWS);
     static constexpr int H = TEAMS == 3 ? 1 : 2;                 // threads per token
     static constexpr int WGS = TEAMS * H;                        // groups of four warps
     static constexpr int THREADS = (WGS * 4 + TEAMS) * 32;
     static constexpr int C = ROWS / H;                           // query rows of a thread
     static constexpr int UNIT = kUTile * ROW_M;                  // a tile's K or V rows
-    static constexpr int KS = VT && P == 4 ? 3 : P == 4 && N == 32 || P == 8 && N == 64 ? 1 : 2;       // packed K rows a team keeps
-    static constexpr int VS = VT && P == 4 ? 3 : P == 4 && N == 64 || P == 6 && N <= 32 ? 2 : 1;       // and V rows
+    static constexpr int KS = P == 4 && N == 32 || P == 8 && N == 64 ? 1 : 2;       // packed K rows a team keeps
+    static constexpr int VS = P == 4 && N == 64 || P == 6 && N <= 32 ? 2 : 1;       // and V rows
     static constexpr int RING = KS + VS, UNITS = TEAMS * RING;
-    static constexpr int V_OFF = UNITS * UNIT;                   // per team: converted V, or its weights
-    static constexpr int V_BYTES = VT ? 8 * kUTile * 2 : kUTile * kHeadDim * 2;
+    static constexpr int V_OFF = UNITS * UNIT;                   // per team: converted V
+    static constexpr int V_BYTES = kUTile * kHeadDim * 2;
     static constexpr int P_OFF = V_OFF + TEAMS * V_BYTES;        // per team: P
     static constexpr int P_BYTES = kUTile * N * 2;
     static constexpr int Q_OFF = P_OFF + TEAMS * P_BYTES;        // per team: pi(Q)
@@ -74,10 +73,8 @@ struct UGeo {
                          F_RED = F_SUM + WGS * C, F_CHAN = F_RED + WGS * 4 * C, F_UNSET = F_CHAN + WGS * kHeadDim, F_END = F_UNSET + 8;
     static constexpr int SMALL = F_END * 4 + TEAMS * (RING + 7) * 8;
     __host__ __device__ static int smem_bytes(int row_e) { return E_OFF + UNITS * kUTile * row_e + SMALL; }
-    // tensor memory columns of a team: K, V^T or a second S, S, O
-    static constexpr uint32_t TM_K = 0, TM_V = 64, TM_S = VT ? 128 : 64, S_STEP = VT ? 0 : N, TM_O = VT ? 128 + N : 64 + 2 * N,
-                              TM_TEAM = TM_O + N, TM_COLS = TEAMS * TM_TEAM <= 256 ? 256 : 512;
-    static_assert(TEAMS * TM_TEAM <= 512 && (!VT || H == 1), "tensor memory; a thread per token");
+    // tensor memory columns of a team: K, two S, O
+    static constexpr uint32_t TM_K = 0, TM_S = 64, TM_O = 64 + 2 * N, TM_TEAM = 64 + 3 * N, TM_COLS = TEAMS * TM_TEAM <= 256 ? 256 : 512;
 };
 
 // pi(Q) of one (sequence, kv head, row tile) per block, as the shared-memory image of the B operand: two panels of 64
@@ -206,52 +203,6 @@ __device__ __forceinline__ void convert32(uint32_t at, int i, const UW& g0, cons
     }
 }
 
-// V^T for the second product, in tensor memory.  A warp takes the bytes of its 32 slots (lane quarter `w4`) of all tokens
-// with a transposing load: a lane gets four tokens of a byte column, so that halves of a register are tokens 0 | 2 and
-// 1 | 3 (times two slots for 4-bit fields) and are converted as they are.  What a pair of tokens is multiplied by comes from
-// `wt`: the weights of the 16-slot (32-slot) blocks, [block][token], tokens in the order k_place.  Lane m of the product is
-// slot v_slot(m), tokens are its inner index in the order k_place.
-__device__ __forceinline__ int k_place(int token) { return (token & ~3) | ((token & 1) << 1) | ((token >> 1) & 1); }
-template <int P>
-__device__ __forceinline__ int v_slot(int m) { return P == 4 ? (m & ~15) | ((m & 7) << 1) | ((m >> 3) & 1) : m; }
-template <int P, bool N16>
-__device__ __forceinline__ void convert_vt(uint32_t unit, uint32_t wt, uint32_t tm_v, int w4, int lane) {
-    constexpr uint32_t C_UP = P == 4 ? 0x3F003F00u : 0x41004100u;       // weight -> -offset * weight: sign and exponent
-#pragma unroll
-    for (int t0 = 0; t0 < kUTile; t0 += 32) {
-        uint32_t q[2][4];       // 4 bits: q[0] = tokens 0..15 (slots 0..15 | 16..31), tokens 16..31; 8 bits: q[tokens / 16], eight slots each
-        if (P == 4) ldmatrix_t8(unit + (row_place<P>(t0 + lane) ^ (16 * w4)), q[0]);
-        else {
-#pragma unroll
-            for (int g = 0; g < 2; ++g) ldmatrix_t8(unit + (row_place<P>(t0 + 16 * g + (lane & 15)) ^ (32 * w4 + (lane & 16))), q[g]);
-        }
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {       // slots 16 h .. of the 32
-            uint32_t o[8];
-#pragma unroll
-            for (int g = 0; g < 2; ++g) {
-                const uint2 s = lds64(wt + (N16 ? 2 * w4 + h : w4) * (2 * kUTile) + (t0 + 16 * g + 4 * (lane & 3)) * 2);
-                const uint32_t ca = s.x + C_UP, cb = s.y + C_UP;
-                if (P == 4) {
-                    const uint32_t w = q[0][2 * g + h], y = w >> 8, sa = s.x - 0x02000200u, sb = s.y - 0x02000200u;
-                    o[4 * g] = fma_bf16x2(w & 0x000F000Fu, s.x, ca);
-                    o[4 * g + 1] = fma_bf16x2(y & 0x000F000Fu, s.y, cb);
-                    o[4 * g + 2] = fma_bf16x2(w & 0x00F000F0u, sa, ca);
-                    o[4 * g + 3] = fma_bf16x2(y & 0x00F000F0u, sb, cb);
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        const uint32_t w = q[g][2 * h + e];
-                        o[4 * g + 2 * e] = fma_bf16x2(w & 0x00FF00FFu, s.x, ca);
-                        o[4 * g + 2 * e + 1] = fma_bf16x2(prmt(w, 0u, 0x4341u), s.y, cb);
-                    }
-                }
-            }
-            tmem_st_16x256(tm_v + ((uint32_t)(16 * h) << 16) + t0 / 2, o);
-        }
-    }
-}
-
 // Sums (MAX: maxima) of C values a thread over the lanes of a warp: afterwards lane l holds column l >> (5 - log2 C).
 template <int C, bool MAX>
 __device__ __forceinline__ float across_lanes(float (&v)[C], int lane) {
@@ -275,11 +226,11 @@ __device__ __forceinline__ float across_lanes(float (&v)[C], int lane) {
     return v[0];
 }
 
-// Changes the scores of a tile by fn(value, column): those that are kept in registers there, others in tensor memory,
-// eight columns at a time.
-template <int C, bool KEEP, class F>
+// Changes the scores of a tile by fn(value, column): up to eight columns a thread stay in registers, more are changed in
+// tensor memory, eight at a time.
+template <int C, class F>
 __device__ __forceinline__ void change_scores(uint32_t tm_s, uint32_t (&raw)[C], F fn) {
-    if constexpr (KEEP) {
+    if constexpr (C <= 8) {
 #pragma unroll
         for (int e = 0; e < C; ++e) raw[e] = __float_as_uint(fn(__uint_as_float(raw[e]), e));
     } else {
@@ -305,8 +256,7 @@ __global__ void __launch_bounds__(UGeo<P, ROWS>::THREADS, 1) attn_umma(const Att
     constexpr int N = G_::N;
     constexpr int D = kHeadDim, ROW_M = G_::ROW_M, UNITS = G_::UNITS, RING = G_::RING, KS = G_::KS, VS = G_::VS, C = G_::C, H = G_::H, TEAMS = G_::TEAMS;
     constexpr int ST = C < 8 ? C : 8;      // columns of a step of the loops over tensor memory
-    constexpr bool VT = G_::VT, KEEP = VT || C <= 8;        // KEEP: scores stay in registers
-    constexpr int UR = KEEP ? C / ST : 1;
+    constexpr bool KEEP = C <= 8;          // scores stay in registers
     constexpr int TEAM_WARPS = G_::WGS * 4, SWP = 2 * N;      // bytes of a P line
     extern __shared__ __align__(1024) uint8_t smem[];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -394,7 +344,7 @@ __global__ void __launch_bounds__(UGeo<P, ROWS>::THREADS, 1) attn_umma(const Att
 
     if (warp >= TEAM_WARPS) {
         // ================================================================ matrix instructions and copies of a team
-        constexpr uint32_t id_s = umma_idesc(128, N, false, false), id_o = umma_idesc(128, N, !VT, true);
+        constexpr uint32_t id_s = umma_idesc(128, N, false, false), id_o = umma_idesc(128, N, true, true);
         const int t = __shfl_sync(0xffffffffu, warp - TEAM_WARPS, 0);
         const uint32_t tmt = __shfl_sync(0xffffffffu, tm, 0) + t * G_::TM_TEAM, base = smem_u32(smem);
         const uint64_t vd = umma_desc<128>(base + G_::V_OFF + t * G_::V_BYTES, kUTile * 128, 1024);
@@ -439,11 +389,8 @@ __global__ void __launch_bounds__(UGeo<P, ROWS>::THREADS, 1) attn_umma(const Att
             copy_k(0);
             copy_q();
             copy_v(0);
-#pragma unroll
-            for (int i = 1; i < (KS > VS ? KS : VS); ++i) {
-                if (i < KS && i < n_mine) copy_k(i);
-                if (i < VS && i < n_mine) copy_v(i);
-            }
+            if (KS > 1 && n_mine > 1) copy_k(1);
+            if (VS > 1 && n_mine > 1) copy_v(1);
         }
         int run = 0;
         bool first = true, fresh = true, fresh_next = true;             // the tile of the next S, of this O, of the next O begins a run
@@ -455,7 +402,7 @@ __global__ void __launch_bounds__(UGeo<P, ROWS>::THREADS, 1) attn_umma(const Att
                 tmem_fence_after();
 #pragma unroll
                 for (int ks = 0; ks < 8; ++ks)
-                    umma_ts(tmt + G_::TM_S + ((i + 1) & 1) * G_::S_STEP, tmt + G_::TM_K + ks * 8, qd + (((ks >> 2) * (N * 128) + (ks & 3) * 32) >> 4), id_s, ks > 0);
+                    umma_ts(tmt + G_::TM_S + ((i + 1) & 1) * N, tmt + G_::TM_K + ks * 8, qd + (((ks >> 2) * (N * 128) + (ks & 3) * 32) >> 4), id_s, ks > 0);
                 umma_commit(b_s(t, i + 1));
                 if (i + 1 + KS < n_mine) copy_k(i + 1 + KS);
                 fresh_next = first;
@@ -474,8 +421,7 @@ __global__ void __launch_bounds__(UGeo<P, ROWS>::THREADS, 1) attn_umma(const Att
                 tmem_fence_after();
 #pragma unroll
                 for (int ks = 0; ks < kUTile / 16; ++ks)
-                    if (VT) umma_ts(tmt + G_::TM_O, tmt + G_::TM_V + ks * 8, pd + ks * (16 * SWP >> 4), id_o, ks > 0 || !fresh);
-                    else umma_ss(tmt + G_::TM_O, vd + ks * (2048 >> 4), pd + ks * (16 * SWP >> 4), id_o, ks > 0 || !fresh);
+                    umma_ss(tmt + G_::TM_O, vd + ks * (2048 >> 4), pd + ks * (16 * SWP >> 4), id_o, ks > 0 || !fresh);
                 umma_commit(b_o(t));
             }
             if (first && i + 2 < n_mine) {   // the next S is of another run
@@ -506,9 +452,7 @@ __global__ void __launch_bounds__(UGeo<P, ROWS>::THREADS, 1) attn_umma(const Att
         // places whose exclusive or with 16 times the piece's number is the piece's: packed row, V row (panels of 64 slots), P line
         const uint32_t place = row_place<P>(m_pos);
         const uint32_t vline = smem_u32(smem) + G_::V_OFF + team * G_::V_BYTES + half * (kUTile * 128) + m_pos * 128 + ((m_pos & 7) << 4);
-        const int p_at = (VT ? k_place(m_pos) : m_pos) * SWP;
-        const uint32_t pline = smem_u32(smem) + G_::P_OFF + team * G_::P_BYTES + (p_at ^ (((p_at >> 7) & (SWP / 16 - 1)) << 4));
-        const uint32_t vwt = smem_u32(smem) + G_::V_OFF + team * G_::V_BYTES;
+        const uint32_t pline = smem_u32(smem) + G_::P_OFF + team * G_::P_BYTES + ((m_pos * SWP) ^ ((((m_pos * SWP) >> 7) & (SWP / 16 - 1)) << 4));
         int first_item;
         const int n_mine = range(team, first_item), me = blockIdx.x + team * gridDim.x;
         const int R = a.n_draft * a.group;
@@ -584,31 +528,11 @@ __global__ void __launch_bounds__(UGeo<P, ROWS>::THREADS, 1) attn_umma(const Att
                 const uint32_t k_top = (uint32_t)k_next;
                 wait(b_s(team, it), it >> 1);                 // S of this tile is there, its K rows are used up
                 tmem_fence_after();
-                const uint32_t tm_s = tmt + G_::TM_S + (it & 1) * G_::S_STEP + half * C;
-                uint32_t raw[C];
-                if (KEEP) {                                   // (and, with one buffer, makes room for the next tile's)
-                    tmem_ld<C>(tm_s, raw);
-                    tmem_wait_ld(raw);
-                }
                 if (it + 1 < n_mine) k_next = convert_k(it + 1);
                 if (it > 0) wait(b_o(team), it - 1);          // V and P of the tile before are used up
                 wait(b_vf(team, it), it / VS);
                 __syncwarp();
-                uint32_t v_top;
-                if constexpr (VT) {
-                    tmem_fence_after();
-                    const int u = team * RING + KS + it % VS;
-                    uint32_t ew[2];
-                    umma_exps<N16>(smem + G_::E_OFF + u * exp_unit + m_pos * row_e, row_e, ew);
-                    UW g[N16 ? 8 : 4];
-                    v_top = (uint32_t)umma_row<P, N16, 1>(ew, 0, g);
-#pragma unroll
-                    for (int j = 0; j < (N16 ? 8 : 4); ++j) sts16(vwt + j * (2 * kUTile) + k_place(m_pos) * 2, g[j].s);
-                    named_sync(bar_id, 128);
-                    convert_vt<P, N16>(smem_u32(smem) + u * G_::UNIT, vwt, tmt + G_::TM_V, w4, lane);
-                    tmem_wait_st();
-                    tmem_fence_before();
-                } else v_top = (uint32_t)convert(team * RING + KS + it % VS, [&](int j, const uint32_t (&r)[16]) {
+                const uint32_t v_top = (uint32_t)convert(team * RING + KS + it % VS, [&](int j, const uint32_t (&r)[16]) {
 #pragma unroll
                     for (int x = 0; x < 4; ++x)       // 16-byte pieces 4 j + x, swizzled
                         sts128((vline ^ ((4 * (j & 1) + x) << 4)) + (j >> 1) * (kUTile * 128), r[4 * x], r[4 * x + 1], r[4 * x + 2], r[4 * x + 3]);
@@ -616,12 +540,18 @@ __global__ void __launch_bounds__(UGeo<P, ROWS>::THREADS, 1) attn_umma(const Att
                 __syncwarp();
                 if (lane == 0) mbar_arrive(b_v(team));
                 // ---- scores
+                const uint32_t tm_s = tmt + G_::TM_S + (it & 1) * N + half * C;
                 const int tt = tile_token(sv, k, kUTile);
                 float mul = up * to_log2 * __uint_as_float(k_top << 23);
+                uint32_t raw[C];
+                if (KEEP) {
+                    tmem_ld<C>(tm_s, raw);
+                    tmem_wait_ld(raw);
+                }
                 if (a.softcap > 0.f) {
                     const float in = cap_in * __uint_as_float(k_top << 23);
                     mul = a.softcap * to_log2;
-                    change_scores<C, KEEP>(tm_s, raw, [&](float y, int) { return fmaf(-2.f, rcp_approx(1.f + ex2_approx(y * in)), 1.f); });      // tanh x = 1 - 2 / (1 + e^2x): about 2e-7 absolute
+                    change_scores<C>(tm_s, raw, [&](float y, int) { return fmaf(-2.f, rcp_approx(1.f + ex2_approx(y * in)), 1.f); });      // tanh x = 1 - 2 / (1 + e^2x): about 2e-7 absolute
                 }
                 const bool masked = a.slopes != nullptr || !(tt + kUTile <= sv.ctx && (tt >= clear_lo || tt + kUTile <= sv.pf));
                 if (masked) {
@@ -632,7 +562,7 @@ __global__ void __launch_bounds__(UGeo<P, ROWS>::THREADS, 1) attn_umma(const Att
                     const bool drafted = !in_ctx && tok - sv.ctx < sv.nd;
                     const int kpos = in_ctx || !drafted ? tok : dpos[jd];
                     const bool always = tok < sv.pf, from = tok >= sv.first;
-                    change_scores<C, KEEP>(tm_s, raw, [&](float y, int e) {
+                    change_scores<C>(tm_s, raw, [&](float y, int e) {
                         const RowInfo x = ri[e];
                         const int dist = x.pos - kpos;
                         const bool near = a.window == 0 || dist < a.window;
@@ -664,7 +594,7 @@ __global__ void __launch_bounds__(UGeo<P, ROWS>::THREADS, 1) attn_umma(const Att
                         top = max3(top, y0, y1);
                     }
                     if (pass != 0 || !named_any(bar_id, 128, top > 8.f || behind)) break;
-#pragma unroll UR
+#pragma unroll 1
                     for (int j = 0; j < C; j += ST) {
                         uint32_t r[ST];
                         if (!KEEP) {
@@ -673,7 +603,7 @@ __global__ void __launch_bounds__(UGeo<P, ROWS>::THREADS, 1) attn_umma(const Att
                         }
                         float v[ST];
 #pragma unroll
-                        for (int e = 0; e < ST; ++e) v[e] = fmaf(__uint_as_float(KEEP ? raw[j + e] : r[e]), mul, mref[j + e]);
+                        for (int e = 0; e < ST; ++e) v[e] = fmaf(__uint_as_float(KEEP ? raw[e] : r[e]), mul, mref[j + e]);
                         const float mine = across_lanes<ST, true>(v, lane);
                         constexpr int GAP = 32 / ST;          // lanes that end up with the same column
                         if (lane % GAP == 0) red[w4 * C + j + lane / GAP] = mine;
@@ -744,7 +674,7 @@ __global__ void __launch_bounds__(UGeo<P, ROWS>::THREADS, 1) attn_umma(const Att
                 __syncwarp();
                 if (lane == 0) mbar_arrive(b_p(team));
             }
-            // ---- the run's result: this thread holds a slot of C rows
+            // ---- the run's result: this thread holds slot umma_slot(m_pos) of C rows
             {
                 float v[C];
 #pragma unroll
@@ -755,7 +685,7 @@ __global__ void __launch_bounds__(UGeo<P, ROWS>::THREADS, 1) attn_umma(const Att
             }
             named_sync(bar_id, 128);
             const bool whole = k0 == 0 && k1 == c.n;
-            const int slot_of = VT ? v_slot<P>(m_pos) : umma_slot<P>(m_pos);
+            const int slot_of = umma_slot<P>(m_pos);
             float* part = a.partials + ((int64_t)(2 * me + (k0 == 0 ? 1 : 0)) * a.part_rows + half * C) * kAttnPart;
             if (m_pos < C) {
                 const int row = row0 + m_pos;

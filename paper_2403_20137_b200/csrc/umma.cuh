@@ -128,9 +128,6 @@ __device__ __forceinline__ uint2 lds64(uint32_t at) {
 __device__ __forceinline__ void sts128(uint32_t at, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
     asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
 }
-__device__ __forceinline__ void sts16(uint32_t at, uint32_t a) {
-    asm volatile("st.shared.u16 [%0], %1;" ::"r"(at), "h"((uint16_t)a) : "memory");
-}
 __device__ __forceinline__ void sts64(uint32_t at, uint32_t a, uint32_t b) {
     asm volatile("st.shared.v2.u32 [%0], {%1,%2};" ::"r"(at), "r"(a), "r"(b) : "memory");
 }
@@ -138,18 +135,6 @@ __device__ __forceinline__ float rcp_approx(float x) {
     float y;
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
-}
-// Two 16 x 16 matrices of bytes, transposed: lanes 0..15 (16..31) give the rows of the first (second); lane l receives
-// bytes 4 (l % 4) .. of the transposed rows l / 4 and l / 4 + 8 of the first, then of the second.
-__device__ __forceinline__ void ldmatrix_t8(uint32_t at, uint32_t (&r)[4]) {
-    asm volatile("ldmatrix.sync.aligned.m16n16.x2.trans.shared.b8 {%0,%1,%2,%3}, [%4];"
-                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
-}
-// 16 lanes x 16 columns of tensor memory from fragments: lane l of the warp has columns 2 (l % 4), + 1 of lanes l / 4 (first
-// pair) and l / 4 + 8 (second), then the same eight columns on.
-__device__ __forceinline__ void tmem_st_16x256(uint32_t addr, const uint32_t (&r)[8]) {
-    asm volatile("tcgen05.st.sync.aligned.16x256b.x2.b32 [%8], {%0,%1,%2,%3,%4,%5,%6,%7};"
-                 ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(addr) : "memory");
 }
 // Two fp32 numbers in one 64-bit register: one instruction for two operations.
 struct F2 {
