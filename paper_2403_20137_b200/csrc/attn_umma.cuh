@@ -152,12 +152,31 @@ __device__ __forceinline__ uint32_t row_place(int row) {
     if (P == 8) return row * 128 + ((row & 7) << 4);
     return row * 96;
 }
-// 32 slots (four 16-byte pieces of bf16) of a packed row, from slot 32 i on; `at`: unit plus row_place.
+// 32 slots of a packed row, from slot 32 i on, as they are stored; `at`: unit plus row_place.
 template <int P>
-__device__ __forceinline__ void convert32(uint32_t at, int i, const UW& g0, const UW& g1, uint32_t (&r)[16]) {
+__device__ __forceinline__ void load32(uint32_t at, int i, uint32_t (&w)[P]) {
+    if (P == 6) {
+#pragma unroll
+        for (int j = 0; j < 3; ++j) {
+            const uint2 x = lds64(at + 24 * i + 8 * j);
+            w[2 * j] = x.x;
+            w[2 * j + 1] = x.y;
+        }
+    } else {
+#pragma unroll
+        for (int h = 0; h < P / 4; ++h) {
+            const uint4 x = lds128(at ^ (4 * P * i + 16 * h));
+            w[4 * h] = x.x;
+            w[4 * h + 1] = x.y;
+            w[4 * h + 2] = x.z;
+            w[4 * h + 3] = x.w;
+        }
+    }
+}
+// 32 slots as 16 bf16 pairs (four 16-byte pieces).
+template <int P>
+__device__ __forceinline__ void convert32(const uint32_t (&w)[P], const UW& g0, const UW& g1, uint32_t (&r)[16]) {
     if (P == 4) {
-        const uint4 x = lds128(at ^ (16 * i));
-        const uint32_t w[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const UW& g = j < 2 ? g0 : g1;
@@ -169,31 +188,19 @@ __device__ __forceinline__ void convert32(uint32_t at, int i, const UW& g0, cons
         }
     } else if (P == 8) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const uint4 x = lds128(at ^ (32 * i + 16 * h));
-            const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-            const UW& g = h ? g1 : g0;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                r[8 * h + 2 * j] = fma_bf16x2(w[j] & 0x00FF00FFu, g.s, g.c);
-                r[8 * h + 2 * j + 1] = fma_bf16x2(prmt(w[j], 0u, 0x4341u), g.s, g.c);
-            }
+        for (int j = 0; j < 8; ++j) {
+            const UW& g = j < 4 ? g0 : g1;
+            r[2 * j] = fma_bf16x2(w[j] & 0x00FF00FFu, g.s, g.c);
+            r[2 * j + 1] = fma_bf16x2(prmt(w[j], 0u, 0x4341u), g.s, g.c);
         }
     } else {
-        uint32_t w[6];
-#pragma unroll
-        for (int j = 0; j < 3; ++j) {
-            const uint2 x = lds64(at + 24 * i + 8 * j);
-            w[2 * j] = x.x;
-            w[2 * j + 1] = x.y;
-        }
         // eight slots are two runs of three bytes; a 16-bit half holds bytes 0, 1 (then 1, 2) of the first run, the other
         // half those of the second: slots 0 | 4, 1 | 5 and 2 | 6, 3 | 7
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const int b = 6 * j, word = b >> 2;                      // first byte of the eight slots: 0, 6, 12, 18
             const bool odd = (b & 3) != 0;
-            const uint32_t lo = prmt(w[word], w[word + 1], odd ? 0x6532u : 0x4310u), hi = prmt(w[word], w[word + 1], odd ? 0x7643u : 0x5421u);
+            const uint32_t lo = prmt(w[word], w[(word + 1) % P], odd ? 0x6532u : 0x4310u), hi = prmt(w[word], w[(word + 1) % P], odd ? 0x7643u : 0x5421u);
             const UW& g = j < 2 ? g0 : g1;
             r[4 * j] = fma_bf16x2(lo & 0x003F003Fu, g.s, g.c);
             r[4 * j + 1] = fma_bf16x2((lo >> 4) & 0x00FC00FCu, g.s2, g.c);
@@ -476,12 +483,15 @@ __global__ void __launch_bounds__(UGeo<P, ROWS>::THREADS, 1) attn_umma(const Att
             const uint32_t at = smem_u32(smem) + u * G_::UNIT + place;
             uint32_t ew[2];
             umma_exps<N16>(smem + G_::E_OFF + u * exp_unit + m_pos * row_e, row_e, ew);
+            uint32_t w[4 / H][P];          // (all loads first: they may not be moved across what follows)
+#pragma unroll
+            for (int j = 0; j < 4 / H; ++j) load32<P>(at, 2 * half + j, w[j]);
             UW g[(N16 ? 8 : 4) / H];
             const int top = umma_row<P, N16, H>(ew, half, g);
 #pragma unroll
             for (int j = 0; j < 4 / H; ++j) {
                 uint32_t r[16];
-                convert32<P>(at, 2 * half + j, g[N16 ? 2 * j : j], g[N16 ? 2 * j + 1 : j], r);
+                convert32<P>(w[j], g[N16 ? 2 * j : j], g[N16 ? 2 * j + 1 : j], r);
                 put(j, r);
             }
             return top;
