@@ -256,7 +256,7 @@ kvbfp_status kvbfp_decode_attn_rope(const kvbfp_cache* cache, const void* q, kvb
  * read clamped to [0, cached tokens].  A query that sees nothing gives zeros.
  */
 typedef struct {
-    float softcap;           /* >= 0, finite */
+    float softcap;           /* 0, or 1e-20 and above, finite */
     int32_t window;          /* >= 0 */
     const float* slopes;     /* device [n_q_heads] or NULL */
     const int32_t* first;    /* device [batch] or NULL */
@@ -283,7 +283,8 @@ size_t kvbfp_attn_workspace_bytes(const kvbfp_format* fmt, int32_t n_q_heads, in
  *   out         [batch, n_draft, n_q_heads, head_dim] of `dt`
  * n_q_heads, perm_k, inv_perm_v, softmax_scale as in kvbfp_decode_attn.  bf16 queries are used exactly, softmax
  * weights are rounded to bf16 for the product with V and the output to bf16; fp32 queries give fp32 accuracy (slower).
- * Sums, maxima and scores are fp32 in both.  Lengths beyond the cache are read clamped and set KVBFP_FLAG_POSITION.
+ * Sums, maxima and scores are fp32 in both.  With bf16 queries cached magnitudes of 2^118 and above are out of range
+ * (results unspecified), and rows of magnitudes below 2^-100 may count as zeros.  Lengths beyond the cache are read clamped and set KVBFP_FLAG_POSITION.
  * The result does not depend on anything but the arguments (no atomics).
  */
 kvbfp_status kvbfp_tree_attn(const kvbfp_cache* cache, const void* q, kvbfp_dtype dt, int32_t n_q_heads,
@@ -319,7 +320,7 @@ kvbfp_status kvbfp_decode_attn_mass(const kvbfp_cache* cache, const void* q, kvb
  * rows go to rows 0.. of `dst`, their masses to dst_mass [batch, n_kv_heads, dst max_seq], whose entries behind them
  * are set to zero; packed rows of dst behind them are left as they are.
  *   dst       another cache of the same batch, heads, block and mantissa width with max_seq >= budget that shares no
- *             memory with src, or src itself (then dst_mass is mass)
+ *             memory with src (nor dst_mass with mass), or src itself (then dst_mass is mass)
  *   new_lens  [batch] i32 out: min(seq_lens, budget); may be seq_lens
  *   kept      [batch, n_kv_heads, budget] i32 out: the kept positions, -1 behind the last
  * Heads keep different tokens, so row numbers are no positions any more: keys have to be cached with their position
@@ -333,8 +334,8 @@ kvbfp_status kvbfp_evict(const kvbfp_cache* src, const int32_t* seq_lens, const 
  * Moves listed rows together in all four planes: row src_base[b] + index[b, h, i] of src becomes row dst_base[b] + i
  * of dst, i < count[b].  With src = dst and both bases the context length this commits the accepted branch of a
  * drafted tree.
- *   index     [batch, index_heads, n_index] i32, index_heads 1 (all heads alike) or n_kv_heads; in place index[i] >= i
- *             and ascending (other orders give unspecified rows)
+ *   index     [batch, index_heads, n_index] i32, index_heads 1 (all heads alike) or n_kv_heads; in place the source
+ *             rows have to ascend, none below its destination (other orders give unspecified rows)
  *   count     [batch] i32, read clamped to [0, n_index];  src_base, dst_base [batch] i32 or NULL (0)
  *   dst       as in kvbfp_evict
  * Rows outside a cache are skipped and set KVBFP_FLAG_POSITION.

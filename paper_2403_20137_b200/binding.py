@@ -307,7 +307,7 @@ def decode_attn_rope(cache, q, seq_lens, theta, partner, sign, perm_k=None, inv_
 
 
 class ScoreMod:
-    """kvbfp_score_mod: cap, distance bias and masks of the scores.  slopes f32 [H_q], first and prefix i32 [B]."""
+    """kvbfp_score_mod: cap, distance bias and masks of the scores.  softcap 0 or at least 1e-20; slopes f32 [H_q], first and prefix i32 [B]."""
 
     def __init__(self, softcap=0.0, slopes=None, first=None, prefix=None, window=0):
         self.softcap, self.window = float(softcap), int(window)
@@ -333,17 +333,37 @@ def attn_workspace_bytes(fmt, n_q_heads, n_draft=1, with_mass=False):
     return int(lib().kvbfp_attn_workspace_bytes(C.byref(fmt), n_q_heads, n_draft, int(with_mass)))
 
 
-def _attn_buffers(cache, q, n_draft, with_mass, mod, out, workspace):
+def _same_device(cache, *tensors):
+    """A call is enqueued on the current device: its cache and tensors have to be there."""
+    dev = cache.k_mant.device
+    if dev.index != torch.cuda.current_device() or any(t is not None and t.device != dev for t in tensors):
+        raise ValueError("expected the cache and all tensors on the current device")
+
+
+def _empty(shape, dtype, device, stream):
+    """Memory that a call on `stream` may use at once and that is given back in that stream's order."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _attn_buffers(cache, q, n_draft, with_mass, mod, out, workspace, stream, *tables):
     f = cache.fmt
+    _same_device(cache, q, out, workspace, *tables)
+    for t in tables:
+        if t is not None and t.numel() != f.n_kv_heads * f.head_dim:
+            raise ValueError(f"permutation: expected {f.n_kv_heads} x {f.head_dim} values, got {t.numel()}")
     n_q_heads = q.shape[-2]
     if q.shape[0] != f.batch or q.shape[-1] != f.head_dim:
         raise ValueError(f"q: shape {tuple(q.shape)} does not fit a cache of batch {f.batch}, head_dim {f.head_dim}")
     if out is None:
-        out = torch.empty_like(q)
+        out = _empty(q.shape, q.dtype, q.device, stream)
     elif _dev(out, q.dtype).shape != q.shape:
         raise ValueError("out: expected the shape of q")
     if workspace is None:
-        workspace = torch.empty(attn_workspace_bytes(f, n_q_heads, n_draft, with_mass), dtype=torch.uint8, device=q.device)
+        workspace = _empty(attn_workspace_bytes(f, n_q_heads, n_draft, with_mass), torch.uint8, q.device, stream)
+    _dev(workspace, torch.uint8)
     ms = None
     if mod is not None:
         mod.check(f.batch, n_q_heads)
@@ -357,7 +377,7 @@ def tree_attn(cache, q, ctx_lens, draft_lens=None, tree_mask=None, depth=None, p
     i: token i sees drafted token j), depth i32 [B, T] -> out [B, T, H_q, d] of q's type."""
     q = _dev(q)
     Bn, T = q.shape[0], q.shape[1]
-    n_q_heads, out, workspace, ms = _attn_buffers(cache, q, T, False, mod, out, workspace)
+    n_q_heads, out, workspace, ms = _attn_buffers(cache, q, T, False, mod, out, workspace, stream, perm_k, inv_perm_v)
     cs = cache.struct()
     _check(lib().kvbfp_tree_attn(C.byref(cs), _ptr(q), _dt(q), n_q_heads, T,
                                  _ptr(_sized("ctx_lens", _dev(ctx_lens, torch.int32), (Bn,))),
@@ -374,7 +394,7 @@ def decode_attn_mod(cache, q, seq_lens, mod, perm_k=None, inv_perm_v=None, softm
                     stream=None):
     """kvbfp_decode_attn_mod: q [B, H_q, d], the last cached token of each sequence -> out of q's type."""
     q = _dev(q)
-    n_q_heads, out, workspace, ms = _attn_buffers(cache, q, 1, False, mod, out, workspace)
+    n_q_heads, out, workspace, ms = _attn_buffers(cache, q, 1, False, mod, out, workspace, stream, perm_k, inv_perm_v)
     cs = cache.struct()
     _check(lib().kvbfp_decode_attn_mod(C.byref(cs), _ptr(q), _dt(q), n_q_heads,
                                        _ptr(_sized("seq_lens", _dev(seq_lens, torch.int32), (q.shape[0],))),
@@ -389,7 +409,7 @@ def decode_attn_mass(cache, q, seq_lens, mass, mod=None, perm_k=None, inv_perm_v
     """kvbfp_decode_attn_mass: decode_attn_mod that adds every token's softmax weight to mass f32 [B, H_kv, max_seq]."""
     q = _dev(q)
     f = cache.fmt
-    n_q_heads, out, workspace, ms = _attn_buffers(cache, q, 1, True, mod, out, workspace)
+    n_q_heads, out, workspace, ms = _attn_buffers(cache, q, 1, True, mod, out, workspace, stream, perm_k, inv_perm_v)
     cs = cache.struct()
     _check(lib().kvbfp_decode_attn_mass(C.byref(cs), _ptr(q), _dt(q), n_q_heads,
                                         _ptr(_sized("seq_lens", _dev(seq_lens, torch.int32), (q.shape[0],))),
@@ -409,9 +429,10 @@ def evict(cache, seq_lens, mass, budget, n_sink=0, n_recent=0, dst=None, dst_mas
         dst, dst_mass = cache, mass
     d = dst.fmt
     if kept is None:
-        kept = torch.empty(f.batch, f.n_kv_heads, budget, dtype=torch.int32, device=mass.device)
+        kept = _empty((f.batch, f.n_kv_heads, budget), torch.int32, mass.device, stream)
     if new_lens is None:
-        new_lens = torch.empty(f.batch, dtype=torch.int32, device=mass.device)
+        new_lens = _empty((f.batch,), torch.int32, mass.device, stream)
+    _same_device(cache, dst.k_mant, mass, dst_mass, seq_lens, kept, new_lens)
     cs, ds = cache.struct(), dst.struct()
     _check(lib().kvbfp_evict(C.byref(cs), _ptr(_sized("seq_lens", _dev(seq_lens, torch.int32), (f.batch,))),
                              _ptr(_sized("mass", _dev(mass, torch.float32), (f.batch, f.n_kv_heads, f.max_seq))), budget,
@@ -429,11 +450,12 @@ def gather_rows(cache, index, count, src_base=None, dst=None, dst_base=None, str
     f = cache.fmt
     if dst is None:
         dst, dst_base = cache, src_base if dst_base is None else dst_base
+    _same_device(cache, dst.k_mant, index, count, src_base, dst_base)
     heads = 1 if index.dim() == 2 else f.n_kv_heads
     n = index.shape[-1]
     cs, ds = cache.struct(), dst.struct()
     _check(lib().kvbfp_gather_rows(C.byref(cs), C.byref(ds),
-                                   _ptr(_sized("index", _dev(index, torch.int32), (f.batch, n) if heads == 1 and index.dim() == 2
+                                   _ptr(_sized("index", _dev(index, torch.int32), (f.batch, n) if index.dim() == 2
                                                else (f.batch, heads, n))), heads, n,
                                    _ptr(_sized("count", _dev(count, torch.int32), (f.batch,))),
                                    _ptr(_sized("src_base", _dev(src_base, torch.int32), (f.batch,))),

@@ -238,6 +238,7 @@ kvbfp_status attn_common(const AttnCall& c) {
     if (group > 8 || c.n_draft > kAttnMaxDraft || f.batch > kAttnMaxBatch) return KVBFP_ERR_UNSUPPORTED;
     if (!(c.softmax_scale >= 0.f) || isinf(c.softmax_scale)) return KVBFP_ERR_INVALID_ARG;
     if (c.mod && (!(c.mod->softcap >= 0.f) || isinf(c.mod->softcap) || c.mod->window < 0)) return KVBFP_ERR_INVALID_ARG;
+    if (c.mod && c.mod->softcap != 0.f && c.mod->softcap < 1e-20f) return KVBFP_ERR_INVALID_ARG;       // (its inverse has to stay in range)
     const void* ptrs[] = {c.cache->k_mant, c.cache->k_exp, c.cache->v_mant, c.cache->v_exp, c.q, c.out, c.workspace,
                           c.perm_k, c.inv_perm_v, c.mass, c.tree_mask};
     for (const void* p : ptrs)

@@ -21,8 +21,9 @@ __device__ __forceinline__ uint32_t mass_key(float x) {
 
 // The rows to keep of one (sequence, kv head), in position order, by a block or (CS > 1) a cluster of blocks that share
 // the region.  The heaviest `need` of the middle region are found by radix selection: three digits of 10, 11 and 11 bits,
-// a histogram each in shared memory (the first, where most weights fall into a few bins, in four copies by lane), the cluster's summed through distributed shared memory; of equals to the threshold
-// the lowest positions are kept.  Each warp owns a contiguous piece of the region, so one scan over the warps' counts
+// a histogram each in shared memory (the first, where most weights fall into a few bins, in four copies by lane: 95 -> 87
+// us for 16 x 32 x 8192 rows with the move), the cluster's summed through distributed shared memory; of equals to the
+// threshold the lowest positions are kept.  Counting is by integer atomics: the result does not depend on their order.  Each warp owns a contiguous piece of the region, so one scan over the warps' counts
 // places every kept row.  A thread keeps its keys in registers where they fit (CACHED: up to 8192 rows a block) and reads
 // them again otherwise.  What bounds it is the chain of passes, not the bytes (4 per row).
 template <int CS, bool CACHED>
@@ -391,6 +392,9 @@ extern "C" kvbfp_status kvbfp_evict(const kvbfp_cache* src, const int32_t* seq_l
     if (budget > dst->fmt.max_seq) return KVBFP_ERR_CAPACITY;
     if (!aligned16(mass) || !aligned16(dst_mass) || !aligned16(kept)) return KVBFP_ERR_ALIGNMENT;
     if ((dst_mass == mass) != (a.from[0] == a.to[0])) return KVBFP_ERR_INVALID_ARG;
+    const size_t pairs = (size_t)src->fmt.batch * src->fmt.n_kv_heads;
+    const uintptr_t x = (uintptr_t)mass, y = (uintptr_t)dst_mass;
+    if (x != y && x < y + pairs * dst->fmt.max_seq * 4 && y < x + pairs * src->fmt.max_seq * 4) return KVBFP_ERR_INVALID_ARG;
     st = status_word(&a.status);
     if (st != KVBFP_OK) return st;
     cudaStream_t s = (cudaStream_t)stream;

@@ -96,8 +96,8 @@ def reference(cache, q, lens, perm, perm_v, mod, scale=0.0, drafts=None, mask=No
 def check(got, out, amp, reach, cap=0.0, dt=None):
     """Error bound per output.  Scores: fp32 products in chains of up to 24 tensor-core steps that cut (2^-23 of the
     running sum of |q k| each; fp32 queries drop 2^-25 of q), the cap adds 2^-21 of itself; a score error d changes a
-    weight by d relative, an output by 2 d sum(p|v|).  Weights are rounded to bf16 (half a step) or to two bf16 terms
-    (2^-16), exp2 and the sums add 2^-20; the output is rounded once."""
+    weight by d relative, an output by 2 d sum(p|v|).  Weights are rounded to bf16 (half a step) or, for fp32
+    queries, cut to three bf16 terms (2^-16 allows for two), exp2 and the sums add 2^-20; the output is rounded once."""
     d = 24 * 2.0 ** -23 * reach + cap * 2.0 ** -21
     w = 2.0 ** -8 if got.dtype == torch.bfloat16 else 2.0 ** -16
     bound = amp * (2 * d[..., None] + w + 2.0 ** -20) * 1.01 + HALF[got.dtype] * out.abs() * 1.01 + 1e-35
@@ -547,6 +547,77 @@ def test_speculative_step_then_eviction():
     assert B.device_status() == 0
 
 
+@pytest.mark.gpu
+def test_rows_far_into_a_long_cache():
+    """Offsets past 32 bits: the second head's rows lie 4 GB into the planes."""
+    H, S, n = 2, (1 << 25) + (1 << 24), (1 << 25) + (1 << 24) - 37
+    cache = B.Cache(1, H, D, S, 32, 4, fill=0x88)
+    cache.k_exp.fill_(120)
+    cache.v_exp.fill_(120)
+    assert 2 * S * cache.fmt.row_m > 1 << 32
+    small, _, _ = make_cache(1, H, 288, 4, 32, 31)
+    # rows 0..287 of the small cache become rows n - 288 .. of the long one, and the last 200 of them come back
+    index = torch.arange(288, dtype=torch.int32, device="cuda")[None].contiguous()
+    B.gather_rows(small, index, i32(288), dst=cache, dst_base=i32(n - 288))
+    back = B.Cache(1, H, D, 208, 32, 4, fill=0)
+    B.gather_rows(cache, index[:, :200].contiguous(), i32(200), src_base=i32(n - 200), dst=back)
+    for p, q in zip(planes(back), planes(small)):
+        assert torch.equal(p[:, :, :200], q[:, :, 88:288])
+    g = torch.Generator().manual_seed(8)
+    for dtype in (torch.bfloat16, torch.float32):
+        q = torch.randn(1, 2 * H, D, generator=g).to(dtype).cuda()
+        got = B.decode_attn_mod(cache, q, i32(n), B.ScoreMod(window=200))
+        ref = reference(back, q[:, None].contiguous(), i32(200), None, None, B.ScoreMod())
+        check(got[:, None], *ref[:3])
+    mass = torch.zeros(1, H, S, device="cuda")
+    mass[0, 1, n - 300:n - 150] = 1.0
+    mass[0, 0, 5] = 2.0
+    kept, new = B.evict(cache, i32(n), mass, 208, 2, 50, dst=back, dst_mass=torch.empty(1, H, 208, device="cuda"))
+    want = [list(range(2)) + [2, 3, 4, 5] + list(range(6, 158)) + list(range(n - 50, n)),
+            list(range(2)) + list(range(2, 8)) + list(range(n - 300, n - 150)) + list(range(n - 50, n))]
+    assert kept[0].tolist() == want and new.tolist() == [208]
+    assert torch.equal(back.k_mant[0, 1, 158:], cache.k_mant[0, 1, n - 50:n])
+    assert B.device_status() == 0
+
+
+@pytest.mark.gpu
+def test_calls_on_a_named_stream_own_their_buffers():
+    """stream= with nothing else given: what the call allocates is not handed out again while it runs."""
+    cache, perm, perm_v, q = case(121, 2, 4, 2, 2048, 8, torch.bfloat16, 4, 32)
+    lens = i32(2000, 1333)
+    want = B.tree_attn(cache, q, lens, perm_k=perm)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    outs = []
+    for _ in range(20):
+        outs.append(B.tree_attn(cache, q, lens, perm_k=perm, stream=side))
+        torch.full((1 << 22,), 255, dtype=torch.uint8, device="cuda")          # would land in a freed workspace
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, want) for o in outs)
+
+
+@pytest.mark.gpu
+def test_binding_refuses_what_the_kernels_could_not_read(monkeypatch):
+    cache, perm, perm_v, q = case(131, 1, 2, 1, 64, 2, torch.bfloat16, 4, 32)
+    mass = torch.zeros(1, 2, 64, device="cuda")
+    before = B.launch_count()
+    with pytest.raises(ValueError):
+        B.tree_attn(cache, q, i32(40), perm_k=perm[:1].contiguous())
+    with pytest.raises(ValueError):
+        B.tree_attn(cache, q, i32(40), workspace=torch.empty(1 << 22, dtype=torch.uint8))
+    with pytest.raises(ValueError):
+        B.decode_attn_mass(cache, q[:, 0].contiguous(), i32(40), mass[:, :, :48].contiguous())
+    with pytest.raises(ValueError):
+        B.tree_attn(cache, q, i32(40, 40))
+    here = torch.cuda.current_device()
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: here + 1)
+    for call in (lambda: B.tree_attn(cache, q, i32(40)), lambda: B.evict(cache, i32(40), mass, 16),
+                 lambda: B.gather_rows(cache, i32(0, 1)[None].contiguous(), i32(2))):
+        with pytest.raises(ValueError, match="current device"):
+            call()
+    assert B.launch_count() == before
+
+
 # ----------------------------------------------------------------------------------------------- refusals (CPU)
 def test_workspace_sizes():
     f = B.Format(2, 4, 128, 64, 32, 4)
@@ -571,6 +642,7 @@ def test_attention_refusals():
            dict(scale=-1.0), dict(scale=float("nan")), dict(scale=float("inf")),
            dict(mod=B.ScoreModStruct(-1.0, 0, None, None, None)), dict(mod=B.ScoreModStruct(float("nan"), 0, None, None, None)),
            dict(mod=B.ScoreModStruct(float("inf"), 0, None, None, None)), dict(mod=B.ScoreModStruct(0.0, -1, None, None, None)),
+           dict(mod=B.ScoreModStruct(1e-21, 0, None, None, None)),
            dict(cache=B.CacheStruct(f, 0x1000, 0x2000, 0x3000, None))]
     for kw in bad:
         assert tree(**kw) == B.ERR_INVALID_ARG, kw
@@ -602,6 +674,7 @@ def test_eviction_refusals():
     for kw in (dict(lens=None), dict(mass=None), dict(dm=None), dict(new=None), dict(kept=None), dict(budget=0),
                dict(sink=-1), dict(recent=-1), dict(sink=10, recent=7), dict(sink=17),
                dict(dm=vp(0x10000)),                                                        # another cache, the same masses
+               dict(dm=vp(0x10100)),                                                        # masses that overlap
                dict(d=src),                                                                 # in place, other masses
                dict(d=B.CacheStruct(f, 0x100000, 0x200000, 0x300000, 0x500000)),            # some planes shared
                dict(d=B.CacheStruct(small, 0x100400, 0x600000, 0x700000, 0x800000)),        # planes that overlap
