@@ -166,8 +166,8 @@ __global__ void __launch_bounds__(128) attn_mass(const AttnArgs a) {
 
 // Query rows per work item: up to 64 bf16 rows of a kv head share its tiles; fp32 queries take 16 at a time (their three
 // bf16 terms fill the registers of attn_rows).
-inline int rows_tile_for(int rows, bool bf16) { return bf16 && rows <= 8 ? 8 : !bf16 || rows <= 16 ? 16 : rows <= 32 ? 32 : 64; }
-inline int max_workers(bool bf16) { return (bf16 ? 3 : 2 * kAttnWarps) * kAttnMaxSms; }
+inline int rows_tile_for(int rows, bool bf16) { return !bf16 || rows <= 8 ? 8 : rows <= 16 ? 16 : rows <= 32 ? 32 : 64; }
+inline int max_workers(int rows_tile) { return (rows_tile == 8 ? 3 * kAttnWarps : 3) * kAttnMaxSms; }
 
 inline size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
 
@@ -185,13 +185,13 @@ size_t lay_out(const kvbfp_format& f, int n_q_heads, int n_draft, bool bf16, boo
     uint8_t* views = take((size_t)f.batch * sizeof(SeqView));
     uint8_t* dpos = take((size_t)f.batch * kAttnMaxDraft * sizeof(int));
     uint8_t* info = take(items * tile * sizeof(RowInfo));
-    uint8_t* frag = take(items * (tile < 16 ? 16 : tile) * kHeadDim * 2 * (bf16 ? 1 : 3));
+    uint8_t* frag = take(items * tile * kHeadDim * 2 * (bf16 ? 1 : 3));
     uint8_t *lse = nullptr, *scores = nullptr;
     if (with_mass) {
         lse = take((size_t)f.batch * n_q_heads * 4);
         scores = take((size_t)f.batch * n_q_heads * f.max_seq * 4);
     }
-    uint8_t* part = take((size_t)2 * max_workers(bf16) * (rows < tile ? rows : tile) * kAttnPart * 4);
+    uint8_t* part = take((size_t)2 * max_workers(tile) * (rows < tile ? rows : tile) * kAttnPart * 4);
     if (a) {
         a->plan = reinterpret_cast<int*>(plan);
         a->views = reinterpret_cast<SeqView*>(views);
@@ -274,17 +274,18 @@ kvbfp_status attn_common(const AttnCall& c) {
     st = sm_count(&n_sm);
     if (st != KVBFP_OK) return st;
     const bool bf16 = c.dt == KVBFP_BF16;
-    a.tile = bf16 ? 128 : attn_rows_tile(f.mant_bits);
-    a.out_up = bf16 ? (float)(1 << (19 - f.mant_bits)) : 256.f;      // 2^(17 - (p - 2)) | 2^8
+    const bool few = rows_tile == 8;          // attn_rows, else attn_umma
+    a.tile = few ? attn_rows_tile(f.mant_bits) : 128;
+    a.out_up = few ? 256.f : (float)(1 << (19 - f.mant_bits));      // 2^8 | 2^(17 - (p - 2))
     const int64_t most = (int64_t)f.batch * f.n_kv_heads * n_row_tiles * (f.max_seq / a.tile + 2);    // tiles at the longest
-    int64_t grid = (int64_t)n_sm * (bf16 ? 1 : 2);
-    const int per_block = bf16 ? attn_teams(f.mant_bits, rows_tile) : kAttnWarps;      // teams or warps
-    if (grid * per_block > max_workers(bf16)) grid = max_workers(bf16) / per_block;
+    int64_t grid = (int64_t)n_sm * (few ? attn_rows_blocks(bf16) : 1);
+    const int per_block = few ? kAttnWarps : attn_teams(f.mant_bits, rows_tile);      // warps or teams
+    if (grid * per_block > max_workers(rows_tile)) grid = max_workers(rows_tile) / per_block;
     if (grid > most) grid = most;
     a.workers = (int)grid * per_block;
 
     cudaStream_t s = (cudaStream_t)c.stream;
-    if (bf16) st = f.mant_bits == 4 ? launch_attn_umma4(a, (int)grid, s) : f.mant_bits == 6 ? launch_attn_umma6(a, (int)grid, s) : launch_attn_umma8(a, (int)grid, s);
+    if (!few) st = f.mant_bits == 4 ? launch_attn_umma4(a, (int)grid, s) : f.mant_bits == 6 ? launch_attn_umma6(a, (int)grid, s) : launch_attn_umma8(a, (int)grid, s);
     else st = f.mant_bits == 4 ? launch_attn_rows4(a, (int)grid, s) : f.mant_bits == 6 ? launch_attn_rows6(a, (int)grid, s) : launch_attn_rows8(a, (int)grid, s);
     if (st != KVBFP_OK) return st;
     // partials of a row, about: a block per row where they are many

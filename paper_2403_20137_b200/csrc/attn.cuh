@@ -107,9 +107,12 @@ __host__ __device__ __forceinline__ int worker_of(int x, int n_items, int worker
     return (int)(((int64_t)(x + 1) * workers - 1) / n_items);
 }
 
-// Tokens per tile of attn_rows (fp32 queries): two stages of four warps of two blocks fit an SM.
-__host__ __device__ constexpr int attn_rows_tile(int mant_bits) { return mant_bits == 8 ? 32 : 64; }
-// attn_prep and attn_rows: fp32 queries, 16 rows per work item, two thread blocks per SM
+// Tokens per tile of attn_rows, stages of a warp and thread blocks per SM (what registers and shared memory allow; four
+// blocks spill, shorter tiles pay for the hand-over: 16 x 32 x 8192 rows 193 us with tiles of 32, 173 us with 64).
+__host__ __device__ constexpr int attn_rows_tile(int mant_bits) { return mant_bits == 4 ? 64 : 32; }
+__host__ __device__ constexpr int attn_rows_stages(int) { return 2; }
+__host__ __device__ constexpr int attn_rows_blocks(bool bf16) { return bf16 ? 3 : 2; }
+// attn_prep and attn_rows: up to eight bf16 rows, or fp32 rows in items of eight
 kvbfp_status launch_attn_rows4(const AttnArgs& a, int grid, cudaStream_t s);
 kvbfp_status launch_attn_rows6(const AttnArgs& a, int grid, cudaStream_t s);
 kvbfp_status launch_attn_rows8(const AttnArgs& a, int grid, cudaStream_t s);

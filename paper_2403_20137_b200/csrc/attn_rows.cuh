@@ -26,8 +26,7 @@
 namespace kvbfp {
 namespace {
 
-constexpr int kRows = 16;       // query rows of a work item
-constexpr int kSplit = 3;       // bf16 terms of an fp32 operand
+constexpr int kRows = 8;        // query rows of a work item
 
 // Cached values are carried times 2^-8, so that no exponent byte leaves the bf16 range with the conversion's offset;
 // undone on scores and outputs.
@@ -39,22 +38,17 @@ template <> struct AFmt<4> { static constexpr uint32_t mask = 0x000F000Fu, magic
 template <> struct AFmt<6> { static constexpr uint32_t mask = 0x003F003Fu, magic = 0x43004300u, bias = 0xC320C320u; };  // -160
 template <> struct AFmt<8> { static constexpr uint32_t mask = 0x000F000Fu, magic = 0x43004300u, bias = 0xC510C510u; };  // -2304
 
-// bf16 bits of 2^(e8 - 127 - (P-2) - 8); 0 below the smallest subnormal.
-template <int P>
-__device__ __forceinline__ uint32_t attn_weight(int e8) {
-    const int f = e8 - (P - 2) - 8;
-    return f >= 1 ? ((uint32_t)f << 7) : (f > -7 ? (0x40u >> (-f)) : 0u);
-}
-
 struct AW {
     uint32_t s, c, s16;      // weight pair, -offset * weight, 16 * weight (8-bit fields)
 };
+// Weights of two exponent bytes (in 16-bit halves): 2^(e - 127 - (P - 2) - 8) as bf16, zero where that has no normal number.
 template <int P>
-__device__ __forceinline__ AW aw_make(uint32_t s, uint32_t c) {
+__device__ __forceinline__ AW aw_make(uint32_t e2) {
     AW w;
-    w.s = s;
-    w.c = c;
-    w.s16 = (P == 8) ? mul_bf16x2(s, 0x41804180u) : 0u;
+    asm("max.s16x2 %0, %1, %2;" : "=r"(w.s) : "r"(e2), "r"((P + 6) * 0x00010001u));
+    w.s = w.s * 0x80u - (P + 6) * 0x00800080u;
+    w.c = mul_bf16x2(w.s, AFmt<P>::bias);
+    w.s16 = (P == 8) ? mul_bf16x2(w.s, 0x41804180u) : 0u;
     return w;
 }
 template <int P>
@@ -145,54 +139,59 @@ __device__ __forceinline__ int tile_at(int row, int x) {
     return row * 96 + x;
 }
 
-// Query fragments of one (sequence, kv head, row tile) per block.
-template <int P>
+// An 8 x 8 matrix of 16-bit numbers, a row's pair per lane (row lane / 4), transposed.
+__device__ __forceinline__ uint32_t transpose8(uint32_t x) {
+    uint32_t y;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
+}
+
+// Query fragments of one (sequence, kv head, row tile) per block: B operand, row lane / 4, [term][k step / 2][lane].
+template <int P, bool F32>
 __global__ void __launch_bounds__(128) attn_prep(const AttnArgs a) {
+    constexpr int SPLIT = F32 ? 3 : 1;
     __shared__ float sq[kRows][kHeadDim + 4];
     __shared__ int sp[kHeadDim];
-    prep_common<kRows, true>(a, sq, sp);
-    const int tid = threadIdx.x, x0 = blockIdx.x;
-    uint4* to = a.qfrag + (int64_t)x0 * (kSplit * 8 * 32);
+    prep_common<kRows, F32>(a, sq, sp);
+    const int x = threadIdx.x, ln = x & 31, g = ln >> 2, t = ln & 3;       // two k steps of a lane per thread
+    uint32_t reg[SPLIT][4];
 #pragma unroll
-    for (int x = tid; x < 8 * 32; x += 128) {
-        const int ln = x & 31, ks = x >> 5, g = ln >> 2, t = ln & 3;
-        uint32_t reg[kSplit][4];
+    for (int k = 0; k < 4; ++k) {       // k step, positions 0, 1 | 2, 3
+        const int ks = 2 * (x >> 5) + (k >> 1);
+        float v0 = sq[g][sp[attn_k_slot<P>(ks, t, 2 * (k & 1))]], v1 = sq[g][sp[attn_k_slot<P>(ks, t, 2 * (k & 1) + 1)]];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {       // row g | g + 8, k positions 0, 1 | 2, 3
-            const float* row = sq[g + 8 * (k & 1)];
-            float v0 = row[sp[attn_k_slot<P>(ks, t, (k & 2))]], v1 = row[sp[attn_k_slot<P>(ks, t, (k & 2) + 1)]];
-#pragma unroll
-            for (int s = 0; s < kSplit; ++s) {
-                reg[s][k] = pack_bf16x2_rn(v0, v1);
-                v0 -= __uint_as_float(reg[s][k] << 16);
-                v1 -= __uint_as_float(reg[s][k] & 0xffff0000u);
-            }
+        for (int s = 0; s < SPLIT; ++s) {
+            reg[s][k] = pack_bf16x2_rn(v0, v1);
+            v0 -= __uint_as_float(reg[s][k] << 16);
+            v1 -= __uint_as_float(reg[s][k] & 0xffff0000u);
         }
-#pragma unroll
-        for (int s = 0; s < kSplit; ++s) to[s * 256 + x] = make_uint4(reg[s][0], reg[s][1], reg[s][2], reg[s][3]);
     }
+    uint4* to = a.qfrag + (int64_t)blockIdx.x * (SPLIT * 128);
+#pragma unroll
+    for (int s = 0; s < SPLIT; ++s) to[s * 128 + x] = make_uint4(reg[s][0], reg[s][1], reg[s][2], reg[s][3]);
 }
 
 template <int P>
 struct AGeo {
     static constexpr int ROW_M = kHeadDim * P / 8;
     static constexpr int TILE = attn_rows_tile(P);       // tokens per stage
-    static constexpr int STAGES = 2;
+    static constexpr int STAGES = attn_rows_stages(P);
     static constexpr int VM_OFF = TILE * ROW_M, KE_OFF = 2 * VM_OFF;
     // exponent bytes of a stage: 2 * TILE * row_e, the stage rounded up to the swizzle's 1024 bytes for the tiled copies
     __host__ __device__ static int exp_bytes(int row_e) { return 2 * TILE * row_e; }
-    static constexpr int LUT_BYTES = 256 * 8;
-    static constexpr int WARP_SMALL = STAGES * 8 + 32 * 16 + kAttnMaxDraft * 4;    // barriers, rows (one output row at the end of a run), positions
+    static constexpr int WARP_SMALL = kHeadDim * 4 + (STAGES * 8 + 15) / 16 * 16;    // rows and positions (one output row at the end of a run), barriers
+    static_assert(kRows * 16 + kAttnMaxDraft * 4 <= kHeadDim * 4, "in an output row's place");
     __host__ __device__ static int smem_bytes(int row_e) {
-        return kAttnWarps * STAGES * (KE_OFF + exp_bytes(row_e)) + LUT_BYTES + kAttnWarps * WARP_SMALL;
+        return kAttnWarps * STAGES * (KE_OFF + exp_bytes(row_e)) + kAttnWarps * WARP_SMALL;
     }
 };
 
-template <int P, bool N16>
-__global__ void __launch_bounds__(kAttnWarps * 32, 2) attn_rows(const AttnArgs a, const __grid_constant__ CUtensorMap k_map,
-                                                                   const __grid_constant__ CUtensorMap v_map) {
+template <int P, bool N16, bool F32>
+__global__ void __launch_bounds__(kAttnWarps * 32, attn_rows_blocks(!F32)) attn_rows(const AttnArgs a, const __grid_constant__ CUtensorMap k_map,
+                                                                                       const __grid_constant__ CUtensorMap v_map) {
     using G_ = AGeo<P>;
-    constexpr int D = kHeadDim, ROW_M = G_::ROW_M, STAGES = G_::STAGES, TILE = G_::TILE, ROWS = kRows;
+    static_assert(G_::WARP_SMALL % 16 == 0 && (P == 6 || G_::VM_OFF % 1024 == 0), "vector accesses; whole swizzle periods");
+    constexpr int D = kHeadDim, ROW_M = G_::ROW_M, STAGES = G_::STAGES, TILE = G_::TILE, ROWS = kRows, SPLIT = F32 ? 3 : 1;
     constexpr int GROUP = 16 * ROW_M;
     extern __shared__ __align__(1024) uint8_t smem[];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
@@ -201,17 +200,12 @@ __global__ void __launch_bounds__(kAttnWarps * 32, 2) attn_rows(const AttnArgs a
     uint8_t* my_m = smem + warp * STAGES * G_::KE_OFF;
     uint8_t* my_e = smem + kAttnWarps * STAGES * G_::KE_OFF + warp * STAGES * 2 * exp_half;
     uint8_t* rest = smem + kAttnWarps * STAGES * (G_::KE_OFF + 2 * exp_half);
-    uint2* lut = reinterpret_cast<uint2*>(rest);
-    uint8_t* small = rest + G_::LUT_BYTES + warp * G_::WARP_SMALL;
+    uint8_t* small = rest + warp * G_::WARP_SMALL;
     RowInfo* ri = reinterpret_cast<RowInfo*>(small);
     float* orow = reinterpret_cast<float*>(small);
-    int* dpos = reinterpret_cast<int*>(small + 32 * 16);
-    const uint32_t bar = smem_u32(small + 32 * 16 + kAttnMaxDraft * 4);
+    int* dpos = reinterpret_cast<int*>(small + kRows * 16);
+    const uint32_t bar = smem_u32(small + kHeadDim * 4);
 
-    for (int e = tid; e < 256; e += kAttnWarps * 32) {
-        const uint32_t s2 = attn_weight<P>(e) * 0x00010001u;
-        lut[e] = make_uint2(s2, mul_bf16x2(s2, AFmt<P>::bias));
-    }
     if (lane == 0) {
         for (int s = 0; s < STAGES; ++s) mbar_init(bar + 8 * s, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -318,6 +312,10 @@ __global__ void __launch_bounds__(kAttnWarps * 32, 2) attn_rows(const AttnArgs a
     }
     const int kx = (tok_of<P>(g >> 1, g & 1, 0) & 7) << 4;       // 8-bit rows: swizzle of the lane's K rows (both tiles alike)
 
+    int tk[2];            // the lane's tokens of a group: rows g, g + 8 of the scores
+#pragma unroll
+    for (int j = 0; j < 2; ++j) tk[j] = tok_of<P>(g >> 1, g & 1, j);
+
     bool dead = false;            // a copy did not arrive: no more waits, no more work, the flag is up
     int it = 0;
     while (it < n_mine) {
@@ -326,13 +324,13 @@ __global__ void __launch_bounds__(kAttnWarps * 32, 2) attn_rows(const AttnArgs a
         const int k0 = cc.k, k1 = min(cc.n, k0 + n_mine - it);
         const SeqView sv = view(b);
         const int64_t item = (int64_t)b * HR + cc.hr;
-        uint4 qr[kSplit][8];
+        uint4 qr[SPLIT][4];           // k steps 2 i, 2 i + 1
         {
-            const uint4* src = a.qfrag + item * (kSplit * 256) + lane;
+            const uint4* src = a.qfrag + item * (SPLIT * 128) + lane;
 #pragma unroll
-            for (int s = 0; s < kSplit; ++s)
+            for (int s = 0; s < SPLIT; ++s)
 #pragma unroll
-                for (int ks = 0; ks < 8; ++ks) qr[s][ks] = src[(s * 8 + ks) * 32];
+                for (int i = 0; i < 4; ++i) qr[s][i] = src[(s * 4 + i) * 32];
         }
         __syncwarp();
         if (lane < ROWS) reinterpret_cast<uint4*>(ri)[lane] = reinterpret_cast<const uint4*>(a.rows)[item * ROWS + lane];
@@ -342,16 +340,14 @@ __global__ void __launch_bounds__(kAttnWarps * 32, 2) attn_rows(const AttnArgs a
         }
         __syncwarp();
 
-        float o[16][4];
-        float m_run[2], l_run[2];
-        {
+        float o[8][4];                // slots 16 g + 2 i (+ 1: upper pair) of rows 2 t, 2 t + 1
+        float m_run[2], l_run[2];     // of rows 2 t, 2 t + 1
 #pragma unroll
-            for (int s = 0; s < 16; ++s)
+        for (int i = 0; i < 8; ++i)
 #pragma unroll
-                for (int k = 0; k < 4; ++k) o[s][k] = 0.f;
-            m_run[0] = m_run[1] = -3.4028235e38f;
-            l_run[0] = l_run[1] = 0.f;
-        }
+            for (int k = 0; k < 4; ++k) o[i][k] = 0.f;
+        m_run[0] = m_run[1] = -3.4028235e38f;
+        l_run[0] = l_run[1] = 0.f;
         // tokens [clear_lo, ctx) and [0, pf) are visible to every row
         int clear_lo = sv.first;
         if (a.window > 0) clear_lo = max(clear_lo, sv.ctx + (a.tree ? a.n_draft - 1 : -1) - a.window + 1);
@@ -366,13 +362,14 @@ __global__ void __launch_bounds__(kAttnWarps * 32, 2) attn_rows(const AttnArgs a
             const uint8_t* stm = my_m + stage * G_::KE_OFF;
             const uint8_t* ste = my_e + stage * 2 * exp_half;
 #pragma unroll 1
-            for (int u = 0; u < TILE / 16; ++u, stm += GROUP, ste += 16 * row_e) {
-                const int tok0 = tt + 16 * u;
+            for (int u = 0; u < TILE / 32; ++u, stm += 2 * GROUP, ste += 32 * row_e) {        // 32 tokens: two groups of 16
+                const int tok0 = tt + 32 * u;
                 if (tok0 >= end) break;
-                // ---- scores of 16 tokens: sc[m tile][column tile][...]
+                // ---- scores: sc[g][0..1] = the lane's first token of group g, rows 2 t, 2 t + 1; sc[g][2..3] = its second
                 float sc[2][4];
-                {
-                    float s2[2][4];        // odd k steps: two chains of MMAs per column tile
+#pragma unroll
+                for (int gr = 0; gr < 2; ++gr) {
+                    const uint8_t *gm = stm + gr * GROUP, *ge = ste + gr * 16 * row_e;
                     uint32_t kw[2][P];
                     AW kg[2][N16 ? 2 : 1];
 #pragma unroll
@@ -380,168 +377,160 @@ __global__ void __launch_bounds__(kAttnWarps * 32, 2) attn_rows(const AttnArgs a
                         if (P == 6) {
 #pragma unroll
                             for (int i = 0; i < 3; ++i) {
-                                const uint2 x = *reinterpret_cast<const uint2*>(stm + ko[j] + 8 * i);
+                                const uint2 x = *reinterpret_cast<const uint2*>(gm + ko[j] + 8 * i);
                                 kw[j][2 * i] = x.x; kw[j][2 * i + 1] = x.y;
                             }
                         } else {
 #pragma unroll
                             for (int i = 0; i < P / 4; ++i) {
-                                const uint4 x = *reinterpret_cast<const uint4*>(stm + ko[j] + (P == 8 ? ((32 * t + 16 * i) ^ kx) : 0));
+                                const uint4 x = *reinterpret_cast<const uint4*>(gm + ko[j] + (P == 8 ? ((32 * t + 16 * i) ^ kx) : 0));
                                 kw[j][4 * i] = x.x; kw[j][4 * i + 1] = x.y; kw[j][4 * i + 2] = x.z; kw[j][4 * i + 3] = x.w;
                             }
                         }
 #pragma unroll
-                        for (int i = 0; i < (N16 ? 2 : 1); ++i) {
-                            const uint2 l = lut[ste[ke[j] + i]];
-                            kg[j][i] = aw_make<P>(l.x, l.y);
-                        }
+                        for (int i = 0; i < (N16 ? 2 : 1); ++i) kg[j][i] = aw_make<P>(ge[ke[j] + i] * 0x00010001u);
                     }
+                    float s2[4];        // odd k steps: two chains of MMAs
 #pragma unroll
-                    for (int j = 0; j < 2; ++j)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) sc[j][e] = s2[j][e] = 0.f;
+                    for (int e = 0; e < 4; ++e) sc[gr][e] = s2[e] = 0.f;
 #pragma unroll
                     for (int ks = 0; ks < 8; ks += 2) {
                         uint32_t r[2][4];
 #pragma unroll
                         for (int j = 0; j < 2; ++j) attn_k<P>(kw[j], ks, kg[j][N16 ? ks >> 2 : 0], r[j]);
 #pragma unroll
-                        for (int s = 0; s < kSplit; ++s)
-                            {
-                                const uint4 q0 = qr[s][ks], q1 = qr[s][ks + 1];
-#pragma unroll
-                                for (int j = 0; j < 2; ++j) mma_bf16(sc[j], q0.x, q0.y, q0.z, q0.w, r[j][0], r[j][1]);
-#pragma unroll
-                                for (int j = 0; j < 2; ++j) mma_bf16(s2[j], q1.x, q1.y, q1.z, q1.w, r[j][2], r[j][3]);
-                            }
+                        for (int s = 0; s < SPLIT; ++s) {
+                            const uint4 q = qr[s][ks >> 1];
+                            mma_bf16(sc[gr], r[0][0], r[1][0], r[0][1], r[1][1], q.x, q.y);
+                            mma_bf16(s2, r[0][2], r[1][2], r[0][3], r[1][3], q.z, q.w);
+                        }
                     }
 #pragma unroll
-                    for (int j = 0; j < 2; ++j)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) sc[j][e] += s2[j][e];
+                    for (int e = 0; e < 4; ++e) sc[gr][e] += s2[e];
                 }
-                // ---- cap, bias, masks: y = mul * sc in log2 units; tiles that every row sees whole need only the factor
+                // ---- cap, bias, masks: y = mul * sc in log2 units; tokens that every row sees need only the factor
                 float mul = plain;
-                if (reshape || !(tok0 + 16 <= sv.ctx && (tok0 >= clear_lo || tok0 + 16 <= sv.pf))) {
+                if (reshape || !(tok0 + 32 <= sv.ctx && (tok0 >= clear_lo || tok0 + 32 <= sv.pf))) {
                     mul = 1.f;
 #pragma unroll
-                    for (int hh = 0; hh < 2; ++hh) {
-                        const RowInfo x = ri[g + 8 * hh];
+                    for (int e = 0; e < 2; ++e) {
+                        const RowInfo x = ri[2 * t + e];
 #pragma unroll
-                        for (int j = 0; j < 2; ++j)
-#pragma unroll
-                            for (int e = 0; e < 2; ++e) {
-                                float y = sc[j][2 * hh + e];
-                                if (a.softcap > 0.f) {
-                                    y *= cap_in;
-                                    y = a.softcap * tanhf(y);
-                                } else {
-                                    y *= up;
-                                }
-                                const int tok = tok0 + tok_of<P>(t, e, j);
-                                bool see;
-                                int dist;
-                                if (tok < sv.ctx) {
-                                    dist = x.pos - tok;
-                                    see = (tok >= sv.first && (a.window == 0 || dist < a.window)) || tok < sv.pf;
-                                } else {
-                                    const int jd = tok - sv.ctx;
-                                    const bool in = jd < sv.nd;
-                                    dist = x.pos - dpos[in ? jd : 0];
-                                    see = in && (((jd < 32 ? x.m0 >> (jd & 31) : x.m1 >> (jd & 31)) & 1u) != 0u) &&
-                                    (a.window == 0 || dist < a.window);
-                                }
-                                y = (y - x.slope * (float)dist) * to_log2;
-                                sc[j][2 * hh + e] = see ? y : -INFINITY;
+                        for (int gj = 0; gj < 4; ++gj) {
+                            const int gr = gj >> 1, j = gj & 1;
+                            float y = sc[gr][2 * j + e];
+                            if (a.softcap > 0.f) {
+                                y *= cap_in;
+                                if (F32) y = tanhf(y);
+                                else y = 1.f - __fdividef(2.f, 1.f + ex2_approx(y * 2.8853900817779268f));    // 1 - 2 / (1 + e^2y): about 2e-7 absolute
+                                y *= a.softcap;
+                            } else {
+                                y *= up;
                             }
+                            const int tok = tok0 + 16 * gr + tk[j];
+                            bool see;
+                            int dist;
+                            if (tok < sv.ctx) {
+                                dist = x.pos - tok;
+                                see = (tok >= sv.first && (a.window == 0 || dist < a.window)) || tok < sv.pf;
+                            } else {
+                                const int jd = tok - sv.ctx;
+                                const bool in = jd < sv.nd;
+                                dist = x.pos - dpos[in ? jd : 0];
+                                see = in && (((jd < 32 ? x.m0 >> (jd & 31) : x.m1 >> (jd & 31)) & 1u) != 0u) &&
+                                      (a.window == 0 || dist < a.window);
+                            }
+                            y = (y - x.slope * (float)dist) * to_log2;
+                            sc[gr][2 * j + e] = see ? y : -INFINITY;
+                        }
                     }
                 }
                 if (a.scores) {
 #pragma unroll
-                    for (int hh = 0; hh < 2; ++hh) {
-                        const int row = rt * ROWS + g + 8 * hh;
-                        if (row < R) {
-                            float* to = a.scores + ((int64_t)b * a.n_q_heads + hk * a.group + row) * max_seq + tok0;
+                    for (int e = 0; e < 2; ++e)
+                        if (2 * t + e < R) {                  // (one token: one row tile)
+                            float* to = a.scores + ((int64_t)b * a.n_q_heads + hk * a.group + 2 * t + e) * max_seq + tok0;
 #pragma unroll
-                            for (int j = 0; j < 2; ++j)
-#pragma unroll
-                                for (int e = 0; e < 2; ++e) to[tok_of<P>(t, e, j)] = sc[j][2 * hh + e] * mul;
+                            for (int gj = 0; gj < 4; ++gj)
+                                if (gj < 2 || tok0 + 16 < max_seq) to[16 * (gj >> 1) + tk[gj & 1]] = sc[gj >> 1][2 * (gj & 1) + e] * mul;
                         }
-                    }
                 }
                 // ---- running softmax: the reference moves only when a score passes it by 8 (2^8 keeps P in range)
                 float top[2];
                 bool grow = false;
 #pragma unroll
-                for (int hh = 0; hh < 2; ++hh) {
-                    const float x = mul * fmaxf(fmaxf(sc[0][2 * hh], sc[0][2 * hh + 1]),
-                                                fmaxf(sc[1][2 * hh], sc[1][2 * hh + 1]));
-                    top[hh] = x;
-                    grow |= x > m_run[hh] + 8.f;
+                for (int e = 0; e < 2; ++e) {
+                    top[e] = mul * fmaxf(fmaxf(sc[0][e], sc[0][2 + e]), fmaxf(sc[1][e], sc[1][2 + e]));
+                    grow |= top[e] > m_run[e] + 8.f;
                 }
                 if (__any_sync(0xffffffffu, grow)) {
 #pragma unroll
-                    for (int hh = 0; hh < 2; ++hh) {
-                        float x = top[hh];
-                        x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 1));
-                        x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 2));
-                        x = fmaxf(x, m_run[hh]);
-                        const float al = ex2_approx(m_run[hh] - x);
-                        m_run[hh] = x;
-                        l_run[hh] *= al;
+                    for (int e = 0; e < 2; ++e) {
+                        float x = top[e];
+                        x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
+                        x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
+                        x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
+                        x = fmaxf(x, m_run[e]);
+                        const float al = ex2_approx(m_run[e] - x);
+                        m_run[e] = x;
+                        l_run[e] *= al;
 #pragma unroll
-                        for (int s = 0; s < 16; ++s) { o[s][2 * hh] *= al; o[s][2 * hh + 1] *= al; }
+                        for (int i = 0; i < 8; ++i) { o[i][e] *= al; o[i][2 + e] *= al; }
                     }
                 }
-                // P as A fragments: (row g, tile 0), (row g+8, tile 0), (row g, tile 1), (row g+8, tile 1); fp32: three terms
-                uint32_t pa[kSplit][4];
 #pragma unroll
-                for (int x = 0; x < 4; ++x) {
-                    const int hh = x & 1, j = x >> 1;
-                    float p0 = ex2_approx(fmaf(sc[j][2 * hh], mul, -m_run[hh]));
-                    float p1 = ex2_approx(fmaf(sc[j][2 * hh + 1], mul, -m_run[hh]));
-                    l_run[hh] += p0 + p1;
+                for (int gr = 0; gr < 2; ++gr) {
+                    const uint8_t *gm = stm + gr * GROUP, *ge = ste + gr * 16 * row_e;
+                    // P as B fragments: a token's pair of rows, transposed; fp32: three terms
+                    uint32_t pb[SPLIT][2];
 #pragma unroll
-                    for (int s = 0; s < kSplit; ++s) {
-                        pa[s][x] = pack_bf16x2_rn(p0, p1);
-                        p0 -= __uint_as_float(pa[s][x] << 16);
-                        p1 -= __uint_as_float(pa[s][x] & 0xffff0000u);
-                    }
-                }
-                // ---- P . V
-                uint32_t vw[4][P / 2];
-                uint2 lv[4];
+                    for (int j = 0; j < 2; ++j) {
+                        float p0 = ex2_approx(fmaf(sc[gr][2 * j], mul, -m_run[0]));
+                        float p1 = ex2_approx(fmaf(sc[gr][2 * j + 1], mul, -m_run[1]));
+                        l_run[0] += p0;
+                        l_run[1] += p1;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {       // k = 2t, 2t+1, 2t+8, 2t+9
-                    if (P == 4) {
-                        const uint2 x = *reinterpret_cast<const uint2*>(stm + vo[e]);
-                        vw[e][0] = x.x; vw[e][1] = x.y;
-                    } else if (P == 6) {
-#pragma unroll
-                        for (int i = 0; i < 3; ++i) vw[e][i] = *reinterpret_cast<const uint32_t*>(stm + vo[e] + 4 * i);
-                    } else {
-                        const uint4 x = *reinterpret_cast<const uint4*>(stm + vo[e]);
-                        vw[e][0] = x.x; vw[e][1] = x.y; vw[e][P / 2 - 2] = x.z; vw[e][P / 2 - 1] = x.w;
-                    }
-                    lv[e] = lut[ste[ve[e]]];
-                }
-                const AW ga = aw_make<P>(prmt(lv[0].x, lv[1].x, 0x7610u), prmt(lv[0].y, lv[1].y, 0x7610u));
-                const AW gb = aw_make<P>(prmt(lv[2].x, lv[3].x, 0x7610u), prmt(lv[2].y, lv[3].y, 0x7610u));
-#pragma unroll
-                for (int r = 0; r < 8; r += 2) {
-                    uint32_t xa[4], xb[4];
-                    attn_v<P>(vw[0], vw[1], r, ga, xa);
-                    attn_v<P>(vw[2], vw[3], r, gb, xb);
-#pragma unroll
-                    for (int s = 0; s < 4; ++s) {
-                        float (&acc)[4] = o[2 * r + s];
-                        float d[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                        for (int c = 2; c >= 0; --c) {
-                            const uint32_t (&p)[4] = pa[c];
-                            mma_bf16(d, p[0], p[1], p[2], p[3], xa[s], xb[s]);
+                        for (int s = 0; s < SPLIT; ++s) {
+                            const uint32_t x = pack_bf16x2_rn(p0, p1);
+                            p0 -= __uint_as_float(x << 16);
+                            p1 -= __uint_as_float(x & 0xffff0000u);
+                            pb[s][j] = transpose8(x);
                         }
-                        acc[0] += d[0]; acc[1] += d[1]; acc[2] += d[2]; acc[3] += d[3];
+                    }
+                    // ---- V^T . P^T
+                    uint32_t vw[4][P / 2], ve8[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {       // k = 2t, 2t+1, 2t+8, 2t+9
+                        if (P == 4) {
+                            const uint2 x = *reinterpret_cast<const uint2*>(gm + vo[e]);
+                            vw[e][0] = x.x; vw[e][1] = x.y;
+                        } else if (P == 6) {
+#pragma unroll
+                            for (int i = 0; i < 3; ++i) vw[e][i] = *reinterpret_cast<const uint32_t*>(gm + vo[e] + 4 * i);
+                        } else {
+                            const uint4 x = *reinterpret_cast<const uint4*>(gm + vo[e]);
+                            vw[e][0] = x.x; vw[e][1] = x.y; vw[e][P / 2 - 2] = x.z; vw[e][P / 2 - 1] = x.w;
+                        }
+                        ve8[e] = ge[ve[e]];
+                    }
+                    const AW ga = aw_make<P>(ve8[0] + (ve8[1] << 16)), gb = aw_make<P>(ve8[2] + (ve8[3] << 16));
+#pragma unroll
+                    for (int r = 0; r < 8; r += 2) {
+                        uint32_t xa[4], xb[4];
+                        attn_v<P>(vw[0], vw[1], r, ga, xa);
+                        attn_v<P>(vw[2], vw[3], r, gb, xb);
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            float (&acc)[4] = o[r + h];          // slots 16 g + 2 (r + h), + 1
+                            if (F32) {
+                                float d[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                                for (int c = SPLIT - 1; c >= 0; --c) mma_bf16(d, xa[2 * h], xa[2 * h + 1], xb[2 * h], xb[2 * h + 1], pb[c][0], pb[c][1]);
+                                acc[0] += d[0]; acc[1] += d[1]; acc[2] += d[2]; acc[3] += d[3];
+                            } else {
+                                mma_bf16(acc, xa[2 * h], xa[2 * h + 1], xb[2 * h], xb[2 * h + 1], pb[0][0], pb[0][1]);
+                            }
+                        }
                     }
                 }
             }
@@ -549,62 +538,65 @@ __global__ void __launch_bounds__(kAttnWarps * 32, 2) attn_rows(const AttnArgs a
             if (issued < n_mine) issue();
         }
 
-        // ---- the run's result: a lane holds slots [32t, 32t + 32) of rows g and g + 8 of each m tile
+        // ---- the run's result: a lane holds slots [16 g, 16 g + 16) of rows 2 t and 2 t + 1
         const bool whole = k0 == 0 && k1 == cc.n;
 #pragma unroll
-        for (int hh = 0; hh < 2; ++hh) {
-            float l = l_run[hh];
-            l += __shfl_xor_sync(0xffffffffu, l, 1);
-            l += __shfl_xor_sync(0xffffffffu, l, 2);
-            const int r = g + 8 * hh, row = rt * ROWS + r;
+        for (int e = 0; e < 2; ++e) {
+            float l = l_run[e];
+            l += __shfl_xor_sync(0xffffffffu, l, 4);
+            l += __shfl_xor_sync(0xffffffffu, l, 8);
+            l += __shfl_xor_sync(0xffffffffu, l, 16);
+            const int r = 2 * t + e, row = rt * ROWS + r;
             const int i = row / a.group, hq = hk * a.group + row - i * a.group;
-            const float m = m_run[hh];
+            const float m = m_run[e];
             if (!whole) {
                 if (row < R) {
                     float* dst = a.partials + ((int64_t)(2 * me + (k0 == 0 ? 1 : 0)) * a.part_rows + r) * kAttnPart;
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        reinterpret_cast<float4*>(dst + 32 * t)[c] = make_float4(o[4 * c][2 * hh], o[4 * c + 1][2 * hh], o[4 * c + 2][2 * hh], o[4 * c + 3][2 * hh]);
-                        reinterpret_cast<float4*>(dst + 32 * t + 16)[c] = make_float4(o[4 * c][2 * hh + 1], o[4 * c + 1][2 * hh + 1], o[4 * c + 2][2 * hh + 1], o[4 * c + 3][2 * hh + 1]);
-                    }
-                    if (t == 0) { dst[D] = m; dst[D + 1] = l; }
+                    for (int c = 0; c < 4; ++c)
+                        reinterpret_cast<float4*>(dst + 16 * g)[c] = make_float4(o[2 * c][e], o[2 * c][2 + e], o[2 * c + 1][e], o[2 * c + 1][2 + e]);
+                    if (g == 0) { dst[D] = m; dst[D + 1] = l; }
                 }
                 continue;
             }
             const bool live = row < R && (!a.tree || i < sv.nd) && l != 0.f;
             const float inv = live ? kValueUp / l : 0.f;
-            float v[2][16];
+            float v[16];
 #pragma unroll
-            for (int s = 0; s < 16; ++s)
-#pragma unroll
-                for (int e = 0; e < 2; ++e) v[e][s] = live ? o[s][2 * hh + e] * inv : 0.f;
+            for (int s = 0; s < 16; ++s) v[s] = live ? o[s >> 1][2 * (s & 1) + e] * inv : 0.f;
             const int64_t at = (((int64_t)b * a.n_draft + i) * a.n_q_heads + hq) * D;
-            if (a.lse && row < R && t == 0) a.lse[(int64_t)b * a.n_q_heads + hq] = l > 0.f ? m + log2f(l) : (l == 0.f ? INFINITY : l);
+            if (a.lse && row < R && g == 0) a.lse[(int64_t)b * a.n_q_heads + hq] = l > 0.f ? m + log2f(l) : (l == 0.f ? INFINITY : l);
             if (!a.inv_perm_v) {
                 if (row < R) {
+                    if (F32) {
+                        float4* to = reinterpret_cast<float4*>(static_cast<float*>(a.out) + at + 16 * g);
 #pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        float4* to = reinterpret_cast<float4*>(static_cast<float*>(a.out) + at + 32 * t + 16 * e);
+                        for (int c = 0; c < 4; ++c) to[c] = make_float4(v[4 * c], v[4 * c + 1], v[4 * c + 2], v[4 * c + 3]);
+                    } else {
+                        uint4* to = reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(a.out) + at + 16 * g);
 #pragma unroll
-                        for (int c = 0; c < 4; ++c) to[c] = make_float4(v[e][4 * c], v[e][4 * c + 1], v[e][4 * c + 2], v[e][4 * c + 3]);
+                        for (int c = 0; c < 2; ++c)
+                            to[c] = make_uint4(pack_bf16x2_rn(v[8 * c], v[8 * c + 1]), pack_bf16x2_rn(v[8 * c + 2], v[8 * c + 3]),
+                                               pack_bf16x2_rn(v[8 * c + 4], v[8 * c + 5]), pack_bf16x2_rn(v[8 * c + 6], v[8 * c + 7]));
                     }
                 }
             } else {          // channels in their own order: one row at a time through shared memory
                 const int32_t* ip = a.inv_perm_v + hk * D;
                 int sl[4];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) sl[e] = ip[4 * lane + e] & (D - 1);
-                for (int gg = 0; gg < 8; ++gg) {
-                    if (rt * ROWS + gg + 8 * hh >= R) break;
+                for (int c = 0; c < 4; ++c) sl[c] = ip[4 * lane + c] & (D - 1);
+                for (int tt = 0; tt < 4; ++tt) {
+                    if (rt * ROWS + 2 * tt + e >= R) break;
                     __syncwarp();
-                    if (g == gg) {
+                    if (t == tt) {
 #pragma unroll
-                        for (int s = 0; s < 16; ++s) { orow[32 * t + s] = v[0][s]; orow[32 * t + 16 + s] = v[1][s]; }
+                        for (int s = 0; s < 16; ++s) orow[16 * g + s] = v[s];
                     }
                     __syncwarp();
-                    const int64_t to = __shfl_sync(0xffffffffu, at, gg * 4) + 4 * lane;
+                    const int64_t to = __shfl_sync(0xffffffffu, at, tt) + 4 * lane;
                     const float y0 = orow[sl[0]], y1 = orow[sl[1]], y2 = orow[sl[2]], y3 = orow[sl[3]];
-                    *reinterpret_cast<float4*>(static_cast<float*>(a.out) + to) = make_float4(y0, y1, y2, y3);
+                    if (F32) *reinterpret_cast<float4*>(static_cast<float*>(a.out) + to) = make_float4(y0, y1, y2, y3);
+                    else *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(a.out) + to) = make_uint2(pack_bf16x2_rn(y0, y1), pack_bf16x2_rn(y2, y3));
                 }
             }
         }
@@ -622,9 +614,9 @@ __global__ void __launch_bounds__(kAttnWarps * 32, 2) attn_rows(const AttnArgs a
     pdl_trigger();
 }
 
-template <int P, bool N16>
+template <int P, bool N16, bool F32>
 kvbfp_status launch_attn(const AttnArgs& a, int grid, cudaStream_t s) {
-    auto kernel = attn_rows<P, N16>;
+    auto kernel = attn_rows<P, N16, F32>;
     static std::atomic<bool> attr_set[64];      // per device; setting the attribute twice is harmless
     int dev = 0;
     KVBFP_CUDA(cudaGetDevice(&dev));
@@ -640,7 +632,7 @@ kvbfp_status launch_attn(const AttnArgs& a, int grid, cudaStream_t s) {
         if (st == KVBFP_OK) st = make_row_map(&v_map, a.v_mant, rows, 128, AGeo<P>::TILE * P / 8);
         if (st != KVBFP_OK) return st;
     }
-    KVBFP_CUDA(launch_pdl(attn_prep<P>, dim3(a.fmt.batch * a.fmt.n_kv_heads * a.n_row_tiles), dim3(128), 0, s, a));
+    KVBFP_CUDA(launch_pdl(attn_prep<P, F32>, dim3(a.fmt.batch * a.fmt.n_kv_heads * a.n_row_tiles), dim3(128), 0, s, a));
     KVBFP_LAUNCH_CHECK("attn_prep");
     KVBFP_CUDA(launch_pdl(kernel, dim3(grid), dim3(kAttnWarps * 32), AGeo<P>::smem_bytes(kHeadDim / a.fmt.block), s, a, k_map, v_map));
     KVBFP_LAUNCH_CHECK("attn_rows");
@@ -649,7 +641,9 @@ kvbfp_status launch_attn(const AttnArgs& a, int grid, cudaStream_t s) {
 
 template <int P>
 kvbfp_status launch_attn_p(const AttnArgs& a, int grid, cudaStream_t s) {
-    return a.fmt.block == 16 ? launch_attn<P, true>(a, grid, s) : launch_attn<P, false>(a, grid, s);
+    const bool n16 = a.fmt.block == 16;
+    if (a.q_is_bf16) return n16 ? launch_attn<P, true, false>(a, grid, s) : launch_attn<P, false, false>(a, grid, s);
+    return n16 ? launch_attn<P, true, true>(a, grid, s) : launch_attn<P, false, true>(a, grid, s);
 }
 
 }  // namespace
