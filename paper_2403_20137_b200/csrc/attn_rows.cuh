@@ -295,7 +295,6 @@ __global__ void __launch_bounds__(kAttnWarps * 32, attn_rows_blocks(!F32)) attn_
     const int R = a.n_draft * a.group;
     const float up = a.scale * kValueUp, to_log2 = 1.4426950408889634f, plain = up * to_log2;
     const float cap_in = a.softcap > 0.f ? up / a.softcap : 0.f;
-    const bool reshape = a.softcap > 0.f || a.slopes != nullptr;
     // lane offsets inside a 16-token group: K rows of column g in both score tiles, V rows of the lane's four k positions
     int ko[2], ke[2], vo[4], ve[4];
 #pragma unroll
@@ -315,6 +314,7 @@ __global__ void __launch_bounds__(kAttnWarps * 32, attn_rows_blocks(!F32)) attn_
     int tk[2];            // the lane's tokens of a group: rows g, g + 8 of the scores
 #pragma unroll
     for (int j = 0; j < 2; ++j) tk[j] = tok_of<P>(g >> 1, g & 1, j);
+    const float tkf[2] = {(float)tk[0], (float)tk[1]};
 
     bool dead = false;            // a copy did not arrive: no more waits, no more work, the flag is up
     int it = 0;
@@ -408,42 +408,52 @@ __global__ void __launch_bounds__(kAttnWarps * 32, attn_rows_blocks(!F32)) attn_
 #pragma unroll
                     for (int e = 0; e < 4; ++e) sc[gr][e] += s2[e];
                 }
-                // ---- cap, bias, masks: y = mul * sc in log2 units; tokens that every row sees need only the factor
+                // ---- cap, bias, masks: mul * sc is the score in log2 units; tokens that every row sees have no masks
                 float mul = plain;
-                if (reshape || !(tok0 + 32 <= sv.ctx && (tok0 >= clear_lo || tok0 + 32 <= sv.pf))) {
-                    mul = 1.f;
+                if (a.softcap > 0.f) {
+                    mul = a.softcap * to_log2;
+#pragma unroll
+                    for (int x = 0; x < 8; ++x) {
+                        float& y = sc[x >> 2][x & 3];
+                        if (F32) y = tanhf(y * cap_in);
+                        else y = 1.f - __fdividef(2.f, 1.f + ex2_approx(y * (cap_in * 2.8853900817779268f)));    // 1 - 2 / (1 + e^2y): about 2e-7 absolute
+                    }
+                }
+                const bool clear = tok0 + 32 <= sv.ctx && (tok0 >= clear_lo || tok0 + 32 <= sv.pf);
+                if (!clear || a.slopes) {
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
                         const RowInfo x = ri[2 * t + e];
+                        const float bias = x.slope * to_log2;
+                        if (clear) {
+                            const float far = (float)(x.pos - tok0);
 #pragma unroll
-                        for (int gj = 0; gj < 4; ++gj) {
-                            const int gr = gj >> 1, j = gj & 1;
-                            float y = sc[gr][2 * j + e];
-                            if (a.softcap > 0.f) {
-                                y *= cap_in;
-                                if (F32) y = tanhf(y);
-                                else y = 1.f - __fdividef(2.f, 1.f + ex2_approx(y * 2.8853900817779268f));    // 1 - 2 / (1 + e^2y): about 2e-7 absolute
-                                y *= a.softcap;
-                            } else {
-                                y *= up;
+                            for (int gj = 0; gj < 4; ++gj) {
+                                float& y = sc[gj >> 1][2 * (gj & 1) + e];
+                                y = fmaf(y, mul, -bias * (far - (tkf[gj & 1] + 16.f * (gj >> 1))));
                             }
-                            const int tok = tok0 + 16 * gr + tk[j];
-                            bool see;
-                            int dist;
-                            if (tok < sv.ctx) {
-                                dist = x.pos - tok;
-                                see = (tok >= sv.first && (a.window == 0 || dist < a.window)) || tok < sv.pf;
-                            } else {
-                                const int jd = tok - sv.ctx;
-                                const bool in = jd < sv.nd;
-                                dist = x.pos - dpos[in ? jd : 0];
-                                see = in && (((jd < 32 ? x.m0 >> (jd & 31) : x.m1 >> (jd & 31)) & 1u) != 0u) &&
-                                      (a.window == 0 || dist < a.window);
+                        } else {
+#pragma unroll
+                            for (int gj = 0; gj < 4; ++gj) {
+                                float& y = sc[gj >> 1][2 * (gj & 1) + e];
+                                const int tok = tok0 + 16 * (gj >> 1) + tk[gj & 1];
+                                bool see;
+                                int dist;
+                                if (tok < sv.ctx) {
+                                    dist = x.pos - tok;
+                                    see = (tok >= sv.first && (a.window == 0 || dist < a.window)) || tok < sv.pf;
+                                } else {
+                                    const int jd = tok - sv.ctx;
+                                    const bool in = jd < sv.nd;
+                                    dist = x.pos - dpos[in ? jd : 0];
+                                    see = in && (((jd < 32 ? x.m0 >> (jd & 31) : x.m1 >> (jd & 31)) & 1u) != 0u) &&
+                                          (a.window == 0 || dist < a.window);
+                                }
+                                y = see ? fmaf(y, mul, -bias * (float)dist) : -INFINITY;
                             }
-                            y = (y - x.slope * (float)dist) * to_log2;
-                            sc[gr][2 * j + e] = see ? y : -INFINITY;
                         }
                     }
+                    mul = 1.f;
                 }
                 if (a.scores) {
 #pragma unroll
