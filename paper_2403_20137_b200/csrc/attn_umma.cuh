@@ -1,4 +1,4 @@
-// Attention of up to 64 bf16 query rows per (batch, kv head) over the packed cache on the fifth-generation tensor cores.
+// Attention of drafted trees with 9 to 64 bf16 query rows per (batch, kv head), or more in items of 64, over the packed cache on the fifth-generation tensor cores.
 //
 //   S^T[tokens x rows] = K . pi(Q)^T          K: tensor memory, pi(Q): shared memory
 //   y = log2(e) * (cap * tanh(scale * S / cap) - slope * distance) ;  P = 2^(y - m)
@@ -46,15 +46,14 @@ __device__ __forceinline__ int umma_slot(int m) {
     return (m & ~3) | ((m & 1) << 1) | ((m >> 1) & 1);
 }
 
-template <int P, int ROWS>
+template <int P, int N>
 struct UGeo {
-    static constexpr int N = ROWS < 16 ? 16 : ROWS;              // columns of the products: 16 at least, zeros behind ROWS
     static constexpr int ROW_M = kHeadDim * P / 8;
-    static constexpr int TEAMS = attn_teams(P, ROWS);
+    static constexpr int TEAMS = attn_teams(P, N);
     static constexpr int H = TEAMS == 3 ? 1 : 2;                 // threads per token
     static constexpr int WGS = TEAMS * H;                        // groups of four warps
     static constexpr int THREADS = (WGS * 4 + TEAMS) * 32;
-    static constexpr int C = ROWS / H;                           // query rows of a thread
+    static constexpr int C = N / H;                           // query rows of a thread
     static constexpr int UNIT = kUTile * ROW_M;                  // a tile's K or V rows
     static constexpr int KS = P == 4 && N == 32 || P == 8 && N == 64 ? 1 : 2;       // packed K rows a team keeps
     static constexpr int VS = P == 4 && N == 64 || P == 6 && N <= 32 ? 2 : 1;       // and V rows
@@ -79,18 +78,17 @@ struct UGeo {
 
 // pi(Q) of one (sequence, kv head, row tile) per block, as the shared-memory image of the B operand: two panels of 64
 // positions, lines of 128 bytes per row, 16-byte pieces at piece ^ (row % 8).
-template <int P, int ROWS>
+template <int P, int N>
 __global__ void __launch_bounds__(128) umma_prep(const AttnArgs a) {
-    constexpr int N = UGeo<P, ROWS>::N;
-    __shared__ float sq[ROWS][kHeadDim + 4];
+    __shared__ float sq[N][kHeadDim + 4];
     __shared__ int sp[kHeadDim];
-    prep_common<ROWS, false>(a, sq, sp);
+    prep_common<N, false>(a, sq, sp);
     uint8_t* to = reinterpret_cast<uint8_t*>(a.qfrag) + (int64_t)blockIdx.x * (N * kHeadDim * 2);
     for (int x = threadIdx.x; x < N * 16; x += 128) {       // 16-byte pieces: row, positions [8 c, 8 c + 8)
         const int c = x & 15, row = x >> 4;
-        uint32_t w[4] = {0u, 0u, 0u, 0u};
+        uint32_t w[4];
 #pragma unroll
-        for (int j = 0; j < 4 && row < ROWS; ++j)
+        for (int j = 0; j < 4; ++j)
             w[j] = pack_bf16x2_rn(sq[row][sp[umma_slot<P>(8 * c + 2 * j)]], sq[row][sp[umma_slot<P>(8 * c + 2 * j + 1)]]);
         *reinterpret_cast<uint4*>(to + (c >> 3) * (N * 128) + row * 128 + (((c & 7) ^ (row & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
     }
@@ -256,13 +254,11 @@ __device__ __forceinline__ void change_scores(uint32_t tm_s, uint32_t (&raw)[C],
 
 __device__ __noinline__ bool umma_wait_slow(uint32_t bar, uint32_t parity) { return mbar_wait_bounded(bar, parity); }
 
-template <int P, bool N16, int ROWS>
-__global__ void __launch_bounds__(UGeo<P, ROWS>::THREADS, 1) attn_umma(const AttnArgs a, const __grid_constant__ CUtensorMap k_map,
+template <int P, bool N16, int N>
+__global__ void __launch_bounds__(UGeo<P, N>::THREADS, 1) attn_umma(const AttnArgs a, const __grid_constant__ CUtensorMap k_map,
                                                                     const __grid_constant__ CUtensorMap v_map) {
-    using G_ = UGeo<P, ROWS>;
-    constexpr int N = G_::N;
+    using G_ = UGeo<P, N>;
     constexpr int D = kHeadDim, ROW_M = G_::ROW_M, UNITS = G_::UNITS, RING = G_::RING, KS = G_::KS, VS = G_::VS, C = G_::C, H = G_::H, TEAMS = G_::TEAMS;
-    constexpr int ST = C < 8 ? C : 8;      // columns of a step of the loops over tensor memory
     constexpr bool KEEP = C <= 8;          // scores stay in registers
     constexpr int TEAM_WARPS = G_::WGS * 4, SWP = 2 * N;      // bytes of a P line
     extern __shared__ __align__(1024) uint8_t smem[];
@@ -469,8 +465,8 @@ __global__ void __launch_bounds__(UGeo<P, ROWS>::THREADS, 1) attn_umma(const Att
         auto fetch = [&](const Cursor& c, int par) {
             if (c.b < B) {
                 if (m_pos < C)
-                    cp_async16(smem_u32(fl + G_::F_RI + ((wg * 2 + par) * C + m_pos) * 4), a.rows + ((int64_t)c.b * HR + c.hr) * ROWS + half * C + m_pos);
-                else if (m_pos >= 64 && m_pos < 64 + kAttnMaxDraft / 4 && a.tree)
+                    cp_async16(smem_u32(fl + G_::F_RI + ((wg * 2 + par) * C + m_pos) * 4), a.rows + ((int64_t)c.b * HR + c.hr) * N + half * C + m_pos);
+                else if (m_pos >= 64 && m_pos < 64 + kAttnMaxDraft / 4)
                     cp_async16(smem_u32(fl + G_::F_DPOS + (wg * 2 + par) * kAttnMaxDraft + (m_pos - 64) * 4), a.dpos + c.b * kAttnMaxDraft + (m_pos - 64) * 4);
                 else if (m_pos >= 96 && m_pos < 98)
                     cp_async16(smem_u32(fl + G_::F_VIEW + (wg * 2 + par) * 8 + (m_pos - 96) * 4), reinterpret_cast<const int*>(a.views + c.b) + (m_pos - 96) * 4);
@@ -507,15 +503,13 @@ __global__ void __launch_bounds__(UGeo<P, ROWS>::THREADS, 1) attn_umma(const Att
             return top;
         };
 
-        if (ROWS < N && half == 0) sts128(pline ^ (ROWS * 2), 0u, 0u, 0u, 0u);       // columns of P that no row has
-        static_assert(N - ROWS == 0 || (ROWS == 8 && N == 16), "one piece of 16 bytes");
 
         Cursor c = seek(first_item), cn = c;
         fetch(c, 0);
         int it = 0, run = 0, k_next = n_mine > 0 ? convert_k(0) : 0;
         while (it < n_mine) {
             const int b = c.b, hk = c.hr / a.n_row_tiles, rt = c.hr - hk * a.n_row_tiles, par = run & 1;
-            const int k0 = c.k, k1 = min(c.n, k0 + n_mine - it), row0 = rt * ROWS + half * C;
+            const int k0 = c.k, k1 = min(c.n, k0 + n_mine - it), row0 = rt * N + half * C;
             cn = c;
             next_pair(cn);
             asm volatile("cp.async.wait_group 0;" ::: "memory");
@@ -529,7 +523,7 @@ __global__ void __launch_bounds__(UGeo<P, ROWS>::THREADS, 1) attn_umma(const Att
             const SeqView sv = *reinterpret_cast<const SeqView*>(fl + G_::F_VIEW + (wg * 2 + par) * 8);
             const uint32_t tm_o = tmt + G_::TM_O + half * C;
             int clear_lo = sv.first;      // tokens [clear_lo, ctx) and [0, pf) are visible to every row
-            if (a.window > 0) clear_lo = max(clear_lo, sv.ctx + (a.tree ? a.n_draft - 1 : -1) - a.window + 1);
+            if (a.window > 0) clear_lo = max(clear_lo, sv.ctx + a.n_draft - a.window);
             F2 l[C / 2];
 #pragma unroll
             for (int j = 0; j < C / 2; ++j) l[j] = f2(0.f, 0.f);
@@ -604,18 +598,18 @@ __global__ void __launch_bounds__(UGeo<P, ROWS>::THREADS, 1) attn_umma(const Att
                         top = max3(top, y0, y1);
                     }
                     if (pass != 0 || !named_any(bar_id, 128, top > 8.f || behind)) break;
-#pragma unroll 1
-                    for (int j = 0; j < C; j += ST) {
-                        uint32_t r[ST];
+#pragma unroll (KEEP ? C / 8 : 1)
+                    for (int j = 0; j < C; j += 8) {
+                        uint32_t r[8];
                         if (!KEEP) {
-                            tmem_ld<ST>(tm_s + j, r);
+                            tmem_ld<8>(tm_s + j, r);
                             tmem_wait_ld(r);
                         }
-                        float v[ST];
+                        float v[8];
 #pragma unroll
-                        for (int e = 0; e < ST; ++e) v[e] = fmaf(__uint_as_float(KEEP ? raw[e] : r[e]), mul, mref[j + e]);
-                        const float mine = across_lanes<ST, true>(v, lane);
-                        constexpr int GAP = 32 / ST;          // lanes that end up with the same column
+                        for (int e = 0; e < 8; ++e) v[e] = fmaf(__uint_as_float(KEEP ? raw[j + e] : r[e]), mul, mref[j + e]);
+                        const float mine = across_lanes<8, true>(v, lane);
+                        constexpr int GAP = 32 / 8;          // lanes that end up with the same column
                         if (lane % GAP == 0) red[w4 * C + j + lane / GAP] = mine;
                     }
                     named_sync(bar_id, 128);
@@ -639,35 +633,25 @@ __global__ void __launch_bounds__(UGeo<P, ROWS>::THREADS, 1) attn_umma(const Att
                     if (k > k0) {          // (the product of the tile before is done: waited for above)
                         tmem_fence_after();
 #pragma unroll 1
-                        for (int j = 0; j < C; j += ST) {
-                            uint32_t o[ST];
-                            tmem_ld<ST>(tm_o + j, o);
+                        for (int j = 0; j < C; j += 8) {
+                            uint32_t o[8];
+                            tmem_ld<8>(tm_o + j, o);
                             tmem_wait_ld(o);
 #pragma unroll
-                            for (int e = 0; e < ST; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * mfac[j + e]);
-                            tmem_st<ST>(tm_o + j, o);
+                            for (int e = 0; e < 8; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * mfac[j + e]);
+                            tmem_st<8>(tm_o + j, o);
                         }
                         tmem_wait_st();
                     }
-                }
-                if (a.scores && tt + m_pos < max_seq) {       // for the weight pass: y against the reference, plus the reference
-                    float* to = a.scores + ((int64_t)b * a.n_q_heads + hk * a.group + row0) * max_seq + tt + m_pos;
-#pragma unroll
-                    for (int j = 0; j < ST; ++j)           // (one token: eight rows at most)
-                        if (row0 + j < R) {
-                            float y0, y1;
-                            f2_split(y[j / 2], y0, y1);
-                            to[(int64_t)j * max_seq] = (j & 1 ? y1 : y0) - mref[j];
-                        }
                 }
                 // ---- P: weights of this token times its V row's 2^E, bf16, a line of 2 N bytes
                 const float vf = __uint_as_float((uint32_t)max((int)v_top - 9, 0) << 23);
                 const F2 vf2 = f2(vf, vf);
 #pragma unroll
-                for (int j = 0; j < C; j += ST) {
-                    uint32_t w[ST / 2];
+                for (int j = 0; j < C; j += 8) {
+                    uint32_t w[4];
 #pragma unroll
-                    for (int e = 0; e < ST / 2; ++e) {
+                    for (int e = 0; e < 4; ++e) {
                         float y0, y1;
                         f2_split(y[j / 2 + e], y0, y1);
                         const F2 p = f2(ex2_approx(y0), ex2_approx(y1));
@@ -676,8 +660,7 @@ __global__ void __launch_bounds__(UGeo<P, ROWS>::THREADS, 1) attn_umma(const Att
                         f2_split(f2_mul(p, vf2), p0, p1);
                         w[e] = pack_bf16x2_rn(p0, p1);
                     }
-                    if constexpr (ST == 8) sts128(pline ^ ((half * C + j) * 2), w[0], w[1], w[2], w[3]);
-                    else sts64(pline + half * 8, w[0], w[1]);
+                    sts128(pline ^ ((half * C + j) * 2), w[0], w[1], w[2], w[3]);
                 }
                 fence_async_shared();
                 tmem_fence_before();
@@ -702,14 +685,9 @@ __global__ void __launch_bounds__(UGeo<P, ROWS>::THREADS, 1) attn_umma(const Att
                 const float ls = red[m_pos] + red[C + m_pos] + red[2 * C + m_pos] + red[3 * C + m_pos];
                 const float m = ((*unset >> m_pos) & 1) ? -3.4028235e38f : -mref[m_pos];
                 lsum[m_pos] = ls;
-                if (row < R) {
-                    if (!whole) {
-                        part[m_pos * kAttnPart + D] = m;
-                        part[m_pos * kAttnPart + D + 1] = ls;
-                    } else if (a.lse) {
-                        const int i = row / a.group, hq = hk * a.group + row - i * a.group;
-                        a.lse[(int64_t)b * a.n_q_heads + hq] = ls > 0.f ? m + log2f(ls) : (ls == 0.f ? INFINITY : ls);
-                    }
+                if (row < R && !whole) {
+                    part[m_pos * kAttnPart + D] = m;
+                    part[m_pos * kAttnPart + D + 1] = ls;
                 }
             }
             wait(b_o(team), it - 1);
@@ -718,18 +696,18 @@ __global__ void __launch_bounds__(UGeo<P, ROWS>::THREADS, 1) attn_umma(const Att
             named_sync(bar_id, 128);
             const int ch = a.inv_perm_v ? chan[slot_of] : slot_of;
 #pragma unroll 1
-            for (int j = 0; j < C; j += ST) {
-                uint32_t o[ST];
-                tmem_ld<ST>(tm_o + j, o);
+            for (int j = 0; j < C; j += 8) {
+                uint32_t o[8];
+                tmem_ld<8>(tm_o + j, o);
                 tmem_wait_ld(o);
 #pragma unroll
-                for (int e = 0; e < ST; ++e) {
+                for (int e = 0; e < 8; ++e) {
                     const int row = row0 + j + e;
                     if (row >= R) break;
                     if (whole) {
                         const int i = row / a.group, hq = hk * a.group + row - i * a.group;
                         const float ls = lsum[j + e];
-                        const bool live = (!a.tree || i < sv.nd) && ls != 0.f;
+                        const bool live = i < sv.nd && ls != 0.f;
                         static_cast<__nv_bfloat16*>(a.out)[(((int64_t)b * a.n_draft + i) * a.n_q_heads + hq) * D + ch] =
                             __float2bfloat16_rn(live ? __uint_as_float(o[e]) * (a.out_up / ls) : 0.f);
                     } else {
@@ -752,10 +730,10 @@ __global__ void __launch_bounds__(UGeo<P, ROWS>::THREADS, 1) attn_umma(const Att
     pdl_trigger();
 }
 
-template <int P, bool N16, int ROWS>
+template <int P, bool N16, int N>
 kvbfp_status launch_umma(const AttnArgs& a, int grid, cudaStream_t s) {
-    using G_ = UGeo<P, ROWS>;
-    auto kernel = attn_umma<P, N16, ROWS>;
+    using G_ = UGeo<P, N>;
+    auto kernel = attn_umma<P, N16, N>;
     static std::atomic<bool> attr_set[64];      // per device; setting the attribute twice is harmless
     int dev = 0;
     KVBFP_CUDA(cudaGetDevice(&dev));
@@ -771,7 +749,7 @@ kvbfp_status launch_umma(const AttnArgs& a, int grid, cudaStream_t s) {
         if (st == KVBFP_OK) st = make_row_map(&v_map, a.v_mant, rows, 128, kUTile * P / 8);
         if (st != KVBFP_OK) return st;
     }
-    KVBFP_CUDA(launch_pdl(umma_prep<P, ROWS>, dim3(a.fmt.batch * a.fmt.n_kv_heads * a.n_row_tiles), dim3(128), 0, s, a));
+    KVBFP_CUDA(launch_pdl(umma_prep<P, N>, dim3(a.fmt.batch * a.fmt.n_kv_heads * a.n_row_tiles), dim3(128), 0, s, a));
     KVBFP_LAUNCH_CHECK("umma_prep");
     KVBFP_CUDA(launch_pdl(kernel, dim3(grid), dim3(G_::THREADS), G_::smem_bytes(kHeadDim / a.fmt.block), s, a, k_map, v_map));
     KVBFP_LAUNCH_CHECK("attn_umma");
@@ -781,7 +759,6 @@ kvbfp_status launch_umma(const AttnArgs& a, int grid, cudaStream_t s) {
 template <int P>
 kvbfp_status launch_umma_p(const AttnArgs& a, int grid, cudaStream_t s) {
     const bool n16 = a.fmt.block == 16;
-    if (a.rows_tile == 8) return n16 ? launch_umma<P, true, 8>(a, grid, s) : launch_umma<P, false, 8>(a, grid, s);
     if (a.rows_tile == 16) return n16 ? launch_umma<P, true, 16>(a, grid, s) : launch_umma<P, false, 16>(a, grid, s);
     if (a.rows_tile == 32) return n16 ? launch_umma<P, true, 32>(a, grid, s) : launch_umma<P, false, 32>(a, grid, s);
     return n16 ? launch_umma<P, true, 64>(a, grid, s) : launch_umma<P, false, 64>(a, grid, s);

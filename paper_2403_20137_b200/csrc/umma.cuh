@@ -29,10 +29,8 @@ __device__ __forceinline__ void tmem_fence_after() { asm volatile("tcgen05.fence
 // Thread l of a warp: lane (its quarter of the lanes) + l, consecutive columns.  The values are there after tmem_wait_ld(r).
 template <int C>
 __device__ __forceinline__ void tmem_ld(uint32_t addr, uint32_t (&r)[C]) {
-    static_assert(C == 4 || C == 8 || C == 16 || C == 32, "column counts in use");
-    if constexpr (C == 4)
-        asm volatile("tcgen05.ld.sync.aligned.32x32b.x4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
-    else if constexpr (C == 8)
+    static_assert(C == 8 || C == 16 || C == 32, "column counts in use");
+    if constexpr (C == 8)
         asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
                      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]) : "r"(addr));
     else if constexpr (C == 16)
@@ -49,10 +47,8 @@ __device__ __forceinline__ void tmem_ld(uint32_t addr, uint32_t (&r)[C]) {
 }
 template <int C>
 __device__ __forceinline__ void tmem_st(uint32_t addr, const uint32_t (&r)[C]) {
-    static_assert(C == 4 || C == 8 || C == 16 || C == 32, "column counts in use");
-    if constexpr (C == 4)
-        asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%4], {%0,%1,%2,%3};" ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(addr) : "memory");
-    else if constexpr (C == 8)
+    static_assert(C == 8 || C == 16 || C == 32, "column counts in use");
+    if constexpr (C == 8)
         asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%8], {%0,%1,%2,%3,%4,%5,%6,%7};"
                      ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(addr) : "memory");
     else if constexpr (C == 16)
@@ -127,9 +123,6 @@ __device__ __forceinline__ uint2 lds64(uint32_t at) {
 }
 __device__ __forceinline__ void sts128(uint32_t at, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
     asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
-}
-__device__ __forceinline__ void sts64(uint32_t at, uint32_t a, uint32_t b) {
-    asm volatile("st.shared.v2.u32 [%0], {%1,%2};" ::"r"(at), "r"(a), "r"(b) : "memory");
 }
 __device__ __forceinline__ float rcp_approx(float x) {
     float y;
