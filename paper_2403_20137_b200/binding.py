@@ -153,8 +153,9 @@ def _ptr(t):
 
 
 def _stream(stream=None):
-    s = torch.cuda.current_stream() if stream is None else stream
-    return C.c_void_p(s.cuda_stream)
+    if stream is not None:
+        return C.c_void_p(stream.cuda_stream)
+    return C.c_void_p(torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()))     # (a Stream object costs 3 us)
 
 
 def _dt(t):
@@ -358,7 +359,7 @@ def _attn_buffers(cache, q, n_draft, with_mass, mod, out, workspace, stream, *ta
     if q.shape[0] != f.batch or q.shape[-1] != f.head_dim:
         raise ValueError(f"q: shape {tuple(q.shape)} does not fit a cache of batch {f.batch}, head_dim {f.head_dim}")
     if out is None:
-        out = _empty(q.shape, q.dtype, q.device, stream)
+        out = torch.empty_like(q) if stream is None else _empty(q.shape, q.dtype, q.device, stream)
     elif _dev(out, q.dtype).shape != q.shape:
         raise ValueError("out: expected the shape of q")
     if workspace is None:

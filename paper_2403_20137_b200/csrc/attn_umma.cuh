@@ -6,7 +6,7 @@
 //
 // Why: with the query rows as the narrow side of the product a tile of 128 tokens costs the tensor cores rows / 64 x 128
 // cycles per product, so what is left to do per cached element is its conversion, and that is done once for all rows
-// (the warp-level kernel converts per 16 rows and its matrix instructions run at a third of the rate).
+// (the warp-level kernel converts per eight rows and its matrix instructions run at a third of the rate).
 //
 // One persistent thread block per SM, tiles of 128 tokens.  Teams of warps, each a worker with a contiguous range of
 // tiles of its own (attn.cuh), a thread per token (three teams of four warps: 4-bit rows, up to 32 query rows) or two
@@ -28,8 +28,12 @@
 // which a barrier over the group tells; then O is rescaled in tensor memory.  Sums are kept per thread and reduced at
 // the end of a run.
 //
-// Shared memory traffic per token (4 bits, 64 rows): packed rows 272 bytes in and out, V 256 written and 256 read, P
-// and the re-read pi(Q) 512: 1.3 kB at 128 bytes a cycle, against 1.6 kB that the copy bandwidth would let pass.
+// What bounds it: neither memory (0.44 of the copy rate at 16 rows) nor the tensor cores (7 to 15 % busy) but the warps'
+// instructions and the latency between them: some 700 to 940 a warp and tile, 0.5 to 0.6 issued a cycle by the 12 to 16
+// warps that registers and shared memory allow.  16 x 32 heads of up to 8192 4-bit rows, 16 drafted tokens: 113 us; 8 x 8
+// heads of 32768 rows, 64 query rows: 158 us; 8 x 8 heads of up to 8191 8-bit rows, 256 capped query rows: 165 us.
+// (V^T in tensor memory, filled through transposing loads, halves the shared-memory traffic and was 6 % slower: it costs
+// integer instructions.  Conversion as loops instead of straight code: 2 to 6 % slower.)
 #pragma once
 #include "attn_common.cuh"
 #include "umma.cuh"
