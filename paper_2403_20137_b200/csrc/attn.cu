@@ -185,9 +185,12 @@ size_t lay_out(const kvbfp_format& f, int n_q_heads, int n_draft, bool bf16, boo
     };
     uint8_t* plan = take((size_t)(f.batch + 1) * sizeof(int));
     uint8_t* views = take((size_t)f.batch * sizeof(SeqView));
-    uint8_t* dpos = take((size_t)f.batch * kAttnMaxDraft * sizeof(int));
-    uint8_t* info = take(items * tile * sizeof(RowInfo));
-    uint8_t* frag = take(items * tile * kHeadDim * 2 * (bf16 ? 1 : 3));
+    uint8_t *dpos = nullptr, *info = nullptr, *frag = nullptr;
+    if (tile != 8) {          // attn_umma's
+        dpos = take((size_t)f.batch * kAttnMaxDraft * sizeof(int));
+        info = take(items * tile * sizeof(RowInfo));
+        frag = take(items * tile * kHeadDim * 2);
+    }
     uint8_t *lse = nullptr, *scores = nullptr;
     if (with_mass) {
         lse = take((size_t)f.batch * n_q_heads * 4);

@@ -53,9 +53,9 @@ struct AttnArgs {
     void* out;
     int* plan;                     // workspace: cumulative tile counts of the sequences, [B + 1]
     SeqView* views;                // workspace: [B]
-    int* dpos;                     // workspace: [B, 64] positions of the drafted rows
-    RowInfo* rows;                 // workspace: [B * Hkv * n_row_tiles, rows_tile]
-    uint4* qfrag;                  // workspace: pi(q) as the main kernel's operand, [B * Hkv * n_row_tiles]
+    int* dpos;                     // workspace of attn_umma: [B, 64] positions of the drafted rows
+    RowInfo* rows;                 // workspace of attn_umma: [B * Hkv * n_row_tiles, rows_tile]
+    uint4* qfrag;                  // workspace of attn_umma: pi(q) as its operand, [B * Hkv * n_row_tiles]
     float* lse;                    // workspace: [B, Hq] log2-sum-exp2, with mass only (else NULL)
     float* scores;                 // workspace: [B, Hq, max_seq] scores in log2 units, with mass only (else NULL)
     float* mass;                   // [B, Hkv, max_seq] or NULL
@@ -112,7 +112,7 @@ __host__ __device__ __forceinline__ int worker_of(int x, int n_items, int worker
 __host__ __device__ constexpr int attn_rows_tile(int mant_bits) { return mant_bits == 4 ? 64 : 32; }
 __host__ __device__ constexpr int attn_rows_stages(int) { return 2; }
 __host__ __device__ constexpr int attn_rows_blocks(bool bf16) { return bf16 ? 3 : 2; }
-// attn_prep and attn_rows: up to eight bf16 rows, or fp32 rows in items of eight
+// attn_rows: up to eight bf16 rows, or fp32 rows in items of eight
 kvbfp_status launch_attn_rows4(const AttnArgs& a, int grid, cudaStream_t s);
 kvbfp_status launch_attn_rows6(const AttnArgs& a, int grid, cudaStream_t s);
 kvbfp_status launch_attn_rows8(const AttnArgs& a, int grid, cudaStream_t s);

@@ -1,4 +1,4 @@
-// What the launches that prepare attn_rows and attn_umma share.
+// Row data of attn_rows and attn_umma, and the launch that prepares the latter.
 #pragma once
 #include <math.h>
 
@@ -10,10 +10,32 @@
 namespace kvbfp {
 namespace {
 
-// Everything a call's main kernel reads besides the cache, per (sequence, kv head, row tile) of ROWS query rows: rows of
-// q (stored-slot order through `sp`, zeros behind the last row) to shared memory, per-row data, and from the first
+// Depth of drafted token i, and what a query row (draft-major, group-minor) needs of itself; rows behind R see no draft.
+__device__ __forceinline__ int draft_depth(const AttnArgs& a, int b, int i) {
+    return a.depth ? min(max(a.depth[(int64_t)b * a.n_draft + i], 0), a.n_draft - 1) : i;
+}
+__device__ __forceinline__ RowInfo row_info(const AttnArgs& a, int b, int hk, int row, int R) {
+    const int i = row / a.group, ctx = min(max(a.ctx_lens[b], 0), a.fmt.max_seq);
+    RowInfo x;
+    x.pos = ctx - 1;
+    x.slope = 0.f;
+    x.m0 = x.m1 = 0u;
+    if (row < R) {
+        if (a.slopes) x.slope = a.slopes[hk * a.group + row - i * a.group];
+        if (a.tree) {
+            const uint64_t m = a.tree_mask ? a.tree_mask[(int64_t)b * a.n_draft + i] : (i == 63 ? ~0ull : (2ull << i) - 1ull);
+            x.pos = ctx + draft_depth(a, b, i);
+            x.m0 = (uint32_t)m;
+            x.m1 = (uint32_t)(m >> 32);
+        }
+    }
+    return x;
+}
+
+// Everything attn_umma reads besides the cache, per (sequence, kv head, row tile) of ROWS query rows: rows of q
+// (stored-slot order through `sp`, zeros behind the last row) to shared memory, per-row data, and from the first
 // block the tiles before each sequence.  128 threads; ends with a barrier.
-template <int ROWS, bool F32>
+template <int ROWS>
 __device__ __forceinline__ void prep_common(const AttnArgs& a, float (&sq)[ROWS][kHeadDim + 4], int (&sp)[kHeadDim]) {
     constexpr int D = kHeadDim;
     __shared__ int scan[4];
@@ -24,60 +46,29 @@ __device__ __forceinline__ void prep_common(const AttnArgs& a, float (&sq)[ROWS]
     pdl_trigger();
     sp[tid] = a.perm_k ? (a.perm_k[hk * D + tid] & (D - 1)) : tid;
     // rows of q, 16 bytes a thread and step
-    constexpr int PIECE = F32 ? 4 : 8;      // elements
 #pragma unroll
-    for (int x = tid; x < ROWS * D / PIECE; x += 128) {
-        const int r = x / (D / PIECE), c = x % (D / PIECE) * PIECE, row = rt * ROWS + r;
-        float v[PIECE];
-#pragma unroll
-        for (int e = 0; e < PIECE; ++e) v[e] = 0.f;
+    for (int x = tid; x < ROWS * D / 8; x += 128) {
+        const int r = x / (D / 8), c = x % (D / 8) * 8, row = rt * ROWS + r;
+        uint4 y = make_uint4(0u, 0u, 0u, 0u);
         if (row < R) {
             const int i = row / a.group, hq = hk * a.group + row - i * a.group;
-            const int64_t at = (((int64_t)b * a.n_draft + i) * a.n_q_heads + hq) * D + c;
-            if (F32) {
-                const float4 y = *reinterpret_cast<const float4*>(static_cast<const float*>(a.q) + at);
-                v[0] = y.x; v[1] = y.y; v[2] = y.z; v[3] = y.w;
-            } else {
-                const uint4 y = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.q) + at);
-                const uint32_t w[4] = {y.x, y.y, y.z, y.w};
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    v[(2 * e) % PIECE] = __uint_as_float(w[e] << 16);
-                    v[(2 * e + 1) % PIECE] = __uint_as_float(w[e] & 0xffff0000u);
-                }
-            }
+            y = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.q) + (((int64_t)b * a.n_draft + i) * a.n_q_heads + hq) * D + c);
         }
+        const uint32_t w[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
-        for (int e = 0; e < PIECE; ++e) sq[r][c + e] = v[e];
-    }
-    if (tid < ROWS) {
-        const int row = rt * ROWS + tid, i = row / a.group;
-        const int ctx = min(max(a.ctx_lens[b], 0), a.fmt.max_seq);
-        RowInfo x;
-        x.pos = ctx - 1;
-        x.slope = 0.f;
-        x.m0 = x.m1 = 0u;
-        if (row < R) {
-            if (a.slopes) x.slope = a.slopes[hk * a.group + row - i * a.group];
-            if (a.tree) {
-                const int64_t at = (int64_t)b * a.n_draft + i;
-                const int dep = a.depth ? min(max(a.depth[at], 0), a.n_draft - 1) : i;
-                const uint64_t m = a.tree_mask ? a.tree_mask[at] : (i == 63 ? ~0ull : (2ull << i) - 1ull);
-                x.pos = ctx + dep;
-                x.m0 = (uint32_t)m;
-                x.m1 = (uint32_t)(m >> 32);
-            }
+        for (int e = 0; e < 4; ++e) {
+            sq[r][c + 2 * e] = __uint_as_float(w[e] << 16);
+            sq[r][c + 2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u);
         }
-        a.rows[(int64_t)x0 * ROWS + tid] = x;
     }
+    if (tid < ROWS) a.rows[(int64_t)x0 * ROWS + tid] = row_info(a, b, hk, rt * ROWS + tid, R);
     if (hk == 0 && rt == 0) {
         const SeqView sv = seq_view(a, b);
         if (tid == 0) {
             a.views[b] = sv;
             if (sv.clamped) raise_flag(a.status, KVBFP_FLAG_POSITION);
         }
-        if (a.tree && tid < a.n_draft)
-            a.dpos[b * kAttnMaxDraft + tid] = sv.ctx + (a.depth ? min(max(a.depth[(int64_t)b * a.n_draft + tid], 0), a.n_draft - 1) : tid);
+        if (tid < a.n_draft) a.dpos[b * kAttnMaxDraft + tid] = sv.ctx + draft_depth(a, b, tid);
     }
     if (x0 == 0) {      // tiles before each sequence
         const int per = (B + 127) / 128;

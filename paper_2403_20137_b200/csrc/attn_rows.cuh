@@ -4,8 +4,8 @@
 //   S^T[tokens x rows] = K . pi(Q)^T ;  y = log2(e) * (cap * tanh(scale * S / cap) - slope * distance) ;  P = 2^(y - m)
 //   O^T[slots x rows] += V^T . P^T ;  l += sum of P over tokens
 //
-// Work split.  attn_prep writes, per (sequence, kv head, row tile), pi(q) in fragment order, and the tiles each sequence
-// has to read (counted from the real lengths and windows, so ragged batches and windows stay balanced).  attn_rows is
+// Work split.  Every block counts the tiles each sequence has to read (from the real lengths and windows, so ragged batches
+// and windows stay balanced): that takes about a microsecond, a launch of its own before took three.  The kernel is
 // persistent: all tiles are cut into one contiguous range per warp; a warp walks its range as runs (the tiles of one
 // (sequence, head, row tile)), shares nothing with other warps and meets no barrier.  A run that covers all tiles
 // writes the result itself, others leave a partial for attn_merge.  The tiles come through a per-warp ring of
@@ -154,29 +154,39 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t x) {
     return y;
 }
 
-// Query fragments of one (sequence, kv head, row tile) per block: B operand, row lane / 4, [term][k step / 2][lane].
+// pi(q) of one query row (`q`; NULL: zeros) at a lane's k positions as B operand: [term][k step / 2].
 template <int P, bool F32>
-__global__ void __launch_bounds__(128) attn_prep(const AttnArgs a) {
-    constexpr int SPLIT = F32 ? 3 : 1;
-    __shared__ float sq[kRows][kHeadDim + 4];
-    __shared__ int sp[kHeadDim];
-    prep_common<kRows, F32>(a, sq, sp);
-    const int x = threadIdx.x, ln = x & 31, g = ln >> 2, t = ln & 3;       // two k steps of a lane per thread
-    uint32_t reg[SPLIT][4];
+__device__ __forceinline__ void load_q(const AttnArgs& a, const void* q, int hk, int t, uint4 (&qr)[F32 ? 3 : 1][4]) {
+    int at[32];           // channels of the lane's 32 slots
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {       // k step, positions 0, 1 | 2, 3
-        const int ks = 2 * (x >> 5) + (k >> 1);
-        float v0 = sq[g][sp[attn_k_slot<P>(ks, t, 2 * (k & 1))]], v1 = sq[g][sp[attn_k_slot<P>(ks, t, 2 * (k & 1) + 1)]];
-#pragma unroll
-        for (int s = 0; s < SPLIT; ++s) {
-            reg[s][k] = pack_bf16x2_rn(v0, v1);
-            v0 -= __uint_as_float(reg[s][k] << 16);
-            v1 -= __uint_as_float(reg[s][k] & 0xffff0000u);
-        }
+    for (int i = 0; i < 8; ++i) {
+        int4 x = make_int4(32 * t + 4 * i, 32 * t + 4 * i + 1, 32 * t + 4 * i + 2, 32 * t + 4 * i + 3);
+        if (a.perm_k) x = *reinterpret_cast<const int4*>(a.perm_k + hk * kHeadDim + 32 * t + 4 * i);
+        at[4 * i] = x.x & (kHeadDim - 1); at[4 * i + 1] = x.y & (kHeadDim - 1);
+        at[4 * i + 2] = x.z & (kHeadDim - 1); at[4 * i + 3] = x.w & (kHeadDim - 1);
     }
-    uint4* to = a.qfrag + (int64_t)blockIdx.x * (SPLIT * 128);
+    float v[32];
 #pragma unroll
-    for (int s = 0; s < SPLIT; ++s) to[s * 128 + x] = make_uint4(reg[s][0], reg[s][1], reg[s][2], reg[s][3]);
+    for (int i = 0; i < 32; ++i) {
+        v[i] = 0.f;
+        if (q) v[i] = F32 ? static_cast<const float*>(q)[at[i]] : __bfloat162float(static_cast<const __nv_bfloat16*>(q)[at[i]]);
+    }
+#pragma unroll
+    for (int ks = 0; ks < 8; ks += 2) {
+        uint32_t reg[F32 ? 3 : 1][4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {       // k step, positions 0, 1 | 2, 3
+            float v0 = v[attn_k_slot<P>(ks + (k >> 1), 0, 2 * (k & 1))], v1 = v[attn_k_slot<P>(ks + (k >> 1), 0, 2 * (k & 1) + 1)];
+#pragma unroll
+            for (int c = 0; c < (F32 ? 3 : 1); ++c) {
+                reg[c][k] = pack_bf16x2_rn(v0, v1);
+                v0 -= __uint_as_float(reg[c][k] << 16);
+                v1 -= __uint_as_float(reg[c][k] & 0xffff0000u);
+            }
+        }
+#pragma unroll
+        for (int c = 0; c < (F32 ? 3 : 1); ++c) qr[c][ks >> 1] = make_uint4(reg[c][0], reg[c][1], reg[c][2], reg[c][3]);
+    }
 }
 
 template <int P>
@@ -190,7 +200,7 @@ struct AGeo {
     static constexpr int WARP_SMALL = kHeadDim * 4 + (STAGES * 8 + 15) / 16 * 16;    // rows and positions (one output row at the end of a run), barriers
     static_assert(kRows * 16 + kAttnMaxDraft * 4 <= kHeadDim * 4, "in an output row's place");
     __host__ __device__ static int smem_bytes(int row_e) {
-        return kAttnWarps * STAGES * (KE_OFF + exp_bytes(row_e)) + kAttnWarps * WARP_SMALL;
+        return kAttnWarps * STAGES * (KE_OFF + exp_bytes(row_e)) + kAttnWarps * (WARP_SMALL + 16);
     }
 };
 
@@ -220,11 +230,50 @@ __global__ void __launch_bounds__(kAttnWarps * 32, attn_rows_blocks(!F32)) attn_
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
     __syncthreads();
-    pdl_wait();       // what attn_prep wrote is read by plain loads below: read-only ones could be moved above this line
+    pdl_wait();
 
     const int B = a.fmt.batch, Hkv = a.fmt.n_kv_heads, HR = Hkv * a.n_row_tiles, max_seq = a.fmt.max_seq;
-    const int n_items = a.plan[B] * HR;
+    // ---- the tiles of all sequences, and where this block's warps begin (block 0 leaves the counts for the merge)
+    int *s_scan = reinterpret_cast<int*>(rest + kAttnWarps * G_::WARP_SMALL), *s_b = s_scan + kAttnWarps, *s_c0 = s_b + kAttnWarps, *s_n = s_c0 + kAttnWarps;
+    const int per = (B + kAttnWarps * 32 - 1) / (kAttnWarps * 32);
+    int mine = 0;
+    for (int i = 0; i < per; ++i)
+        if (tid * per + i < B) mine += seq_view(a, tid * per + i).n;
+    int before = mine;
+#pragma unroll
+    for (int off = 1; off < 32; off <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, before, off);
+        if (lane >= off) before += y;
+    }
+    if (lane == 31) s_scan[warp] = before;
+    __syncthreads();
+    before -= mine;
+    int total = 0;
+#pragma unroll
+    for (int w = 0; w < kAttnWarps; ++w) {
+        if (w < warp) before += s_scan[w];
+        total += s_scan[w];
+    }
+    const int n_items = total * HR;
     const int workers = min(a.workers, n_items), me = blockIdx.x + gridDim.x * warp;      // neighbouring ranges on different SMs
+    for (int i = 0; i < per; ++i) {
+        const int bb = tid * per + i;
+        if (bb >= B) break;
+        const SeqView sv = seq_view(a, bb);
+#pragma unroll
+        for (int w = 0; w < kAttnWarps; ++w) {
+            const int m = blockIdx.x + gridDim.x * w, at = m < workers ? worker_start(m, n_items, workers) : -1;
+            if (at >= before * HR && at < (before + sv.n) * HR) { s_b[w] = bb; s_c0[w] = before; s_n[w] = sv.n; }
+        }
+        if (blockIdx.x == 0) {
+            a.plan[bb] = before;
+            a.views[bb] = sv;
+            if (bb == B - 1) a.plan[B] = total;
+            if (sv.clamped) raise_flag(a.status, KVBFP_FLAG_POSITION);
+        }
+        before += sv.n;
+    }
+    __syncthreads();
     const int i0 = me < workers ? worker_start(me, n_items, workers) : 0;
     const int i1 = me < workers ? worker_start(me + 1, n_items, workers) : 0;
     const int n_mine = i1 - i0;
@@ -236,40 +285,22 @@ __global__ void __launch_bounds__(kAttnWarps * 32, attn_rows_blocks(!F32)) attn_
         int b, hr, k, n;
     };
     Cursor cc;
-    {
-        // last sequence that begins at or before the item and has tiles: 32 looked at per step
-        int last = 0;
-        for (int b0 = 0; b0 < B; b0 += 32) {
-            const bool in = b0 + lane < B && a.plan[b0 + lane] * HR <= i0;
-            const uint32_t v = __ballot_sync(0xffffffffu, in);
-            if (v) last = b0 + 31 - __clz(v);
-            if (v != 0xffffffffu) break;
-        }
-        const int c0 = a.plan[last];
-        cc.b = last;
-        cc.n = a.plan[last + 1] - c0;
-        const int in = i0 - c0 * HR;
-        cc.hr = in / cc.n;
-        cc.k = in - cc.hr * cc.n;
-    }
+    cc.b = s_b[warp];
+    cc.n = s_n[warp];
+    cc.hr = (i0 - s_c0[warp] * HR) / cc.n;
+    cc.k = i0 - s_c0[warp] * HR - cc.hr * cc.n;
     auto next_pair = [&](Cursor& c) {           // to the first tile of the next (sequence, head, row tile)
         c.k = 0;
         if (++c.hr == HR) {
             c.hr = 0;
             c.n = 0;
-            while (c.n == 0 && ++c.b < B) c.n = a.plan[c.b + 1] - a.plan[c.b];
+            while (c.n == 0 && ++c.b < B) c.n = seq_view(a, c.b).n;
         }
-    };
-    auto view = [&](int b) {
-        const int4 x = reinterpret_cast<const int4*>(a.views + b)[0], y = reinterpret_cast<const int4*>(a.views + b)[1];
-        SeqView s;
-        s.ctx = x.x; s.nd = x.y; s.first = x.z; s.pf = x.w; s.lo = y.x; s.np = y.y; s.n = y.z; s.clamped = y.w;
-        return s;
     };
 
     // ---- copies: the same items, STAGES ahead (every lane keeps the cursor, lane 0 issues)
     Cursor pc = cc;
-    SeqView psv = view(pc.b);
+    SeqView psv = seq_view(a, pc.b);
     int issued = 0;
     auto issue = [&]() {
         const int s = issued % STAGES;
@@ -295,7 +326,7 @@ __global__ void __launch_bounds__(kAttnWarps * 32, attn_rows_blocks(!F32)) attn_
         if (++pc.k == pc.n) {
             const int b = pc.b;
             next_pair(pc);
-            if (pc.b != b && pc.b < B) psv = view(pc.b);
+            if (pc.b != b && pc.b < B) psv = seq_view(a, pc.b);
         }
     };
     for (int s = 0; s < STAGES && issued < n_mine; ++s) issue();
@@ -330,21 +361,20 @@ __global__ void __launch_bounds__(kAttnWarps * 32, attn_rows_blocks(!F32)) attn_
         // ================================================================ a run: tiles [k0, k1) of one (b, head, row tile)
         const int b = cc.b, hk = cc.hr / a.n_row_tiles, rt = cc.hr - hk * a.n_row_tiles;
         const int k0 = cc.k, k1 = min(cc.n, k0 + n_mine - it);
-        const SeqView sv = view(b);
-        const int64_t item = (int64_t)b * HR + cc.hr;
+        const SeqView sv = seq_view(a, b);
         uint4 qr[SPLIT][4];           // k steps 2 i, 2 i + 1
         {
-            const uint4* src = a.qfrag + item * (SPLIT * 128) + lane;
-#pragma unroll
-            for (int s = 0; s < SPLIT; ++s)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) qr[s][i] = src[(s * 4 + i) * 32];
+            const int row = rt * ROWS + g, i = row / a.group;
+            const int64_t at = (((int64_t)b * a.n_draft + i) * a.n_q_heads + hk * a.group + row - i * a.group) * D;
+            const void* q = F32 ? (const void*)(static_cast<const float*>(a.q) + at) : (const void*)(static_cast<const __nv_bfloat16*>(a.q) + at);
+            load_q<P, F32>(a, row < R ? q : nullptr, hk, t, qr);
         }
         __syncwarp();
-        if (lane < ROWS) reinterpret_cast<uint4*>(ri)[lane] = reinterpret_cast<const uint4*>(a.rows)[item * ROWS + lane];
+        if (lane < ROWS) ri[lane] = row_info(a, b, hk, rt * ROWS + lane, R);
         if (a.tree) {
-            dpos[lane] = a.dpos[b * kAttnMaxDraft + lane];
-            dpos[lane + 32] = a.dpos[b * kAttnMaxDraft + lane + 32];
+#pragma unroll
+            for (int i = 0; i < kAttnMaxDraft; i += 32)
+                if (i + lane < a.n_draft) dpos[i + lane] = sv.ctx + draft_depth(a, b, i + lane);
         }
         __syncwarp();
 
@@ -650,8 +680,6 @@ kvbfp_status launch_attn(const AttnArgs& a, int grid, cudaStream_t s) {
         if (st == KVBFP_OK) st = make_row_map(&v_map, a.v_mant, rows, 128, AGeo<P>::TILE * P / 8);
         if (st != KVBFP_OK) return st;
     }
-    KVBFP_CUDA(launch_pdl(attn_prep<P, F32>, dim3(a.fmt.batch * a.fmt.n_kv_heads * a.n_row_tiles), dim3(128), 0, s, a));
-    KVBFP_LAUNCH_CHECK("attn_prep");
     KVBFP_CUDA(launch_pdl(kernel, dim3(grid), dim3(kAttnWarps * 32), AGeo<P>::smem_bytes(kHeadDim / a.fmt.block), s, a, k_map, v_map));
     KVBFP_LAUNCH_CHECK("attn_rows");
     return KVBFP_OK;

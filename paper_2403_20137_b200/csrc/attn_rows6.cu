@@ -1,4 +1,4 @@
-// The 6-bit instantiations of attn_prep and attn_rows.
+// The 6-bit instantiations of attn_rows.
 #include "attn_rows.cuh"
 
 namespace kvbfp {

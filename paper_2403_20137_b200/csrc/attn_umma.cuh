@@ -86,7 +86,7 @@ template <int P, int N>
 __global__ void __launch_bounds__(128) umma_prep(const AttnArgs a) {
     __shared__ float sq[N][kHeadDim + 4];
     __shared__ int sp[kHeadDim];
-    prep_common<N, false>(a, sq, sp);
+    prep_common<N>(a, sq, sp);
     uint8_t* to = reinterpret_cast<uint8_t*>(a.qfrag) + (int64_t)blockIdx.x * (N * kHeadDim * 2);
     for (int x = threadIdx.x; x < N * 16; x += 128) {       // 16-byte pieces: row, positions [8 c, 8 c + 8)
         const int c = x & 15, row = x >> 4;
