@@ -333,6 +333,29 @@ def test_many_tiles(batch, heads, group, T, S, dtype, bits):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("batch,T,dtype", [(300, 1, torch.bfloat16), (1024, 2, torch.float32), (260, 10, torch.bfloat16)])
+def test_many_sequences(batch, T, dtype):
+    """More sequences than a block has threads, a third of them empty, the first and the last among those."""
+    cache, perm, perm_v, q = case(141, batch, 1, 1, 48, T, dtype, 4, 32)
+    rng = np.random.default_rng(2)
+    n = rng.integers(0, 48 - T + 1, batch)
+    n[rng.random(batch) < 0.3] = 0
+    n[0] = n[-1] = 0
+    drafts = rng.integers(0, T + 1, batch)
+    drafts[[0, -1]] = 0
+    lens, drafts = (torch.from_numpy(x.astype(np.int32)).cuda() for x in (n, drafts))
+    mask, depth = trees(batch, T, drafts, 9)
+    if T == 1:
+        got = B.decode_attn_mod(cache, q[:, 0].contiguous(), lens, None, perm_k=perm, inv_perm_v=inverse(perm_v))[:, None]
+        ref = reference(cache, q, lens, perm, perm_v, B.ScoreMod())
+    else:
+        got = B.tree_attn(cache, q, lens, draft_lens=drafts, tree_mask=mask, depth=depth, perm_k=perm, inv_perm_v=inverse(perm_v))
+        ref = reference(cache, q, lens, perm, perm_v, B.ScoreMod(), drafts=drafts, mask=mask, depth=depth)
+    check(got, *ref[:3])
+    assert bool((got[0] == 0).all()) and bool((got[-1] == 0).all()) and B.device_status() == 0
+
+
+@pytest.mark.gpu
 def test_streams_graphs_and_shared_arguments():
     """The same calls on two streams with a workspace each, and captured into a graph that is replayed on new data."""
     cache, perm, perm_v, q = case(101, 2, 4, 2, 640, 8, torch.bfloat16, 4, 32)
