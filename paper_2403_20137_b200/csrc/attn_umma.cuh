@@ -108,41 +108,57 @@ __global__ void __launch_bounds__(128) umma_prep(const AttnArgs a) {
 struct UW {
     uint32_t s, s2, c;      // multipliers of fields at bit 0 and higher up, -offset * weight
 };
+// Weights of two blocks, `below` (16-bit halves) steps of two below the row's largest exponent.
 template <int P>
-__device__ __forceinline__ UW umma_weights(int below) {      // steps of two below the row's largest exponent
-    const uint32_t d = (uint32_t)min(below, 100);
-    UW w;
-    w.s = 0x7E007E00u - d * 0x00800080u;                                             // 2^(133 - 8 - d)
-    w.s2 = (P == 4 ? 0x7C007C00u : 0x7D007D00u) - d * 0x00800080u;                   // / 16, / 4
-    w.c = (P == 4 ? 0xBD00BD00u : P == 6 ? 0xBE00BE00u : 0xBF00BF00u) - d * 0x00800080u;     // -8, -32, -128 times 2^(-8 - d)
-    return w;
+__device__ __forceinline__ void umma_weights(uint32_t below, UW& a, UW& b) {
+    uint32_t d;
+    asm("min.s16x2 %0, %1, %2;" : "=r"(d) : "r"(below), "r"(100u * 0x00010001u));
+    const uint32_t s = 0x7E007E00u - d * 0x80u;                                      // 2^(133 - 8 - d)
+    a.s = prmt(s, 0u, 0x1010u);
+    b.s = prmt(s, 0u, 0x3232u);
+    a.s2 = a.s - (P == 4 ? 0x02000200u : 0x01000100u);                               // / 16, / 4
+    b.s2 = b.s - (P == 4 ? 0x02000200u : 0x01000100u);
+    a.c = a.s + (P == 4 ? 0x3F003F00u : P == 6 ? 0x40004000u : 0x41004100u);         // -8, -32, -128 times 2^(-8 - d)
+    b.c = b.s + (P == 4 ? 0x3F003F00u : P == 6 ? 0x40004000u : 0x41004100u);
 }
-// Exponent bytes of a row as (byte j: slots 32 j ..) or, for blocks of 16, two words (byte j: slots 16 j ..).
+__device__ __forceinline__ uint32_t max_s16x2(uint32_t a, uint32_t b) {
+    uint32_t d;
+    asm("max.s16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+}
+// Exponent bytes of a row: byte j for slots 32 j .. (longer blocks: repeated, by the selector `sel` from the aligned word
+// that holds them) or, for blocks of 16, two words (byte j: slots 16 j ..).
+__device__ __forceinline__ uint32_t umma_exp_sel(int row, int row_e) {
+    return row_e == 4 ? 0x3210u : row_e == 2 ? ((row & 1) ? 0x3322u : 0x1100u) : (uint32_t)(row & 3) * 0x1111u;
+}
 template <bool N16>
-__device__ __forceinline__ void umma_exps(const uint8_t* e, int row_e, uint32_t (&w)[2]) {
+__device__ __forceinline__ void umma_exps(const uint8_t* e, uint32_t sel, uint32_t (&w)[2]) {
     if (N16) {
         const uint2 x = *reinterpret_cast<const uint2*>(e);
         w[0] = x.x;
         w[1] = x.y;
     } else {
-        w[0] = row_e == 4 ? *reinterpret_cast<const uint32_t*>(e)
-               : row_e == 2 ? prmt(*reinterpret_cast<const uint16_t*>(e), 0u, 0x1100u) : prmt(*e, 0u, 0u);
-        w[1] = w[0];
+        w[0] = w[1] = prmt(*reinterpret_cast<const uint32_t*>(e), 0u, sel);
     }
 }
 // The blocks of a row (H = 1) or of its half (slots 64 half ..) relative to the whole row's largest exponent byte, which
 // is returned (254 at most).
 template <int P, bool N16, int H>
 __device__ __forceinline__ int umma_row(const uint32_t (&w)[2], int half, UW (&g)[(N16 ? 8 : 4) / H]) {
-    constexpr int NB = N16 ? 8 : 4;
-    int top = 0;
+    const uint32_t lo = w[0] & 0x00FF00FFu, hi = prmt(w[0], 0u, 0x4341u);            // blocks 0 | 2, 1 | 3
+    uint32_t m = max_s16x2(lo, hi);
+    if (N16) m = max_s16x2(m, max_s16x2(w[1] & 0x00FF00FFu, prmt(w[1], 0u, 0x4341u)));
+    const int top = max((int)(m & 0xffffu), (int)(m >> 16));
+    const uint32_t t2 = (uint32_t)top * 0x00010001u;
+    if constexpr (!N16 && H == 2) {
+        umma_weights<P>(t2 - prmt(w[0], 0u, half ? 0x4342u : 0x4140u), g[0], g[1]);
+    } else {
 #pragma unroll
-    for (int j = 0; j < NB; ++j) top = max(top, (int)((w[j >> 2] >> (8 * (j & 3))) & 0xffu));
-#pragma unroll
-    for (int j = 0; j < NB / H; ++j) {
-        uint32_t e = w[j >> 2] >> (8 * (j & 3));
-        if (H == 2) e = (N16 ? (half ? w[1] : w[0]) : w[0] >> (16 * half)) >> (8 * j);
-        g[j] = umma_weights<P>(top - (int)(e & 0xffu));
+        for (int j = 0; j < (N16 ? 2 : 1) / (N16 ? H : 1); ++j) {
+            const uint32_t x = N16 && (H == 2 ? half : j) ? w[1] : w[0];
+            umma_weights<P>(t2 - (x & 0x00FF00FFu), g[4 * j], g[4 * j + 2]);
+            umma_weights<P>(t2 - prmt(x, 0u, 0x4341u), g[4 * j + 1], g[4 * j + 3]);
+        }
     }
     return min(top, 254);
 }
@@ -457,7 +473,7 @@ __global__ void __launch_bounds__(UGeo<P, N>::THREADS, 1) attn_umma(const AttnAr
         int* chan = reinterpret_cast<int*>(fl + G_::F_CHAN) + wg * D;
         int* unset = reinterpret_cast<int*>(fl + G_::F_UNSET) + wg;         // rows that have seen nothing yet, as a bit mask
         // places whose exclusive or with 16 times the piece's number is the piece's: packed row, V row (panels of 64 slots), P line
-        const uint32_t place = row_place<P>(m_pos);
+        const uint32_t place = row_place<P>(m_pos), exp_at = N16 ? m_pos * 8 : (m_pos * row_e) & ~3, exp_sel = umma_exp_sel(m_pos, row_e);
         const uint32_t vline = smem_u32(smem) + G_::V_OFF + team * G_::V_BYTES + half * (kUTile * 128) + m_pos * 128 + ((m_pos & 7) << 4);
         const uint32_t pline = smem_u32(smem) + G_::P_OFF + team * G_::P_BYTES + ((m_pos * SWP) ^ ((((m_pos * SWP) >> 7) & (SWP / 16 - 1)) << 4));
         int first_item;
@@ -482,7 +498,7 @@ __global__ void __launch_bounds__(UGeo<P, N>::THREADS, 1) attn_umma(const AttnAr
         auto convert = [&](int u, auto put) {
             const uint32_t at = smem_u32(smem) + u * G_::UNIT + place;
             uint32_t ew[2];
-            umma_exps<N16>(smem + G_::E_OFF + u * exp_unit + m_pos * row_e, row_e, ew);
+            umma_exps<N16>(smem + G_::E_OFF + u * exp_unit + exp_at, exp_sel, ew);
             uint32_t w[4 / H][P];          // (all loads first: they may not be moved across what follows)
 #pragma unroll
             for (int j = 0; j < 4 / H; ++j) load32<P>(at, 2 * half + j, w[j]);
