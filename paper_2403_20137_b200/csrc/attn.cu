@@ -23,7 +23,11 @@ __global__ void __launch_bounds__(128) attn_merge(const AttnArgs a, int64_t n_ro
     const int R = a.n_draft * a.group, Hkv = a.fmt.n_kv_heads, B = a.fmt.batch;
     const int row = (int)(x % R), hk = (int)(x / R % Hkv), b = (int)(x / R / Hkv);
     const int i = row / a.group, hq = hk * a.group + row % a.group;
+    // (all that does not depend on the split first: what bounds this kernel is the chain of loads)
     const int c0 = a.plan[b], n = a.plan[b + 1] - c0;
+    const int nd = a.tree ? a.views[b].nd : a.n_draft;
+    int4 slot = make_int4(4 * lane, 4 * lane + 1, 4 * lane + 2, 4 * lane + 3);
+    if (a.inv_perm_v) slot = *reinterpret_cast<const int4*>(a.inv_perm_v + hk * D + 4 * lane);
     const int HR = Hkv * a.n_row_tiles, n_items = a.plan[B] * HR;
     const int rt = row / a.rows_tile, r = row - rt * a.rows_tile;
     int w0 = 0, w1 = -1;
@@ -39,14 +43,23 @@ __global__ void __launch_bounds__(128) attn_merge(const AttnArgs a, int64_t n_ro
     };
     float m = -INFINITY, l = 0.f;
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    // a batch of 32 partials: a lane each for maximum and sum, then the vectors eight at a time
+    // a batch of 32 partials: a lane each for maximum and sum, the vectors eight at a time, the first of them on their way
+    // before the maximum is known
     const int step = SPLIT ? 4 : 1;
     for (int base = w0 + (SPLIT ? warp : 0); base <= w1; base += 32 * step) {
-        const int w = base + lane * step;
+        const int w = base + lane * step, cnt = min(32, (w1 - base) / step + 1);
         const bool have = w <= w1;
         const float* pk = part(have ? w : w0);
         const float mk = have ? pk[D] : -INFINITY;
         const float lk = have ? pk[D + 1] : 0.f;
+        float4 v[8];
+        auto load = [&](int j0) {
+#pragma unroll
+            for (int u = 0; u < 8; ++u)
+                v[u] = (j0 + u < cnt) ? *reinterpret_cast<const float4*>(part(base + (j0 + u) * step) + 4 * lane)
+                                      : make_float4(0.f, 0.f, 0.f, 0.f);
+        };
+        load(0);
         float mn = mk;
 #pragma unroll
         for (int off = 16; off; off >>= 1) mn = fmaxf(mn, __shfl_xor_sync(0xffffffffu, mn, off));
@@ -59,19 +72,12 @@ __global__ void __launch_bounds__(128) attn_merge(const AttnArgs a, int64_t n_ro
         acc.x *= a1; acc.y *= a1; acc.z *= a1; acc.w *= a1;
         l = l * a1 + ls;
         m = mn;
-        const int cnt = min(32, (w1 - base) / step + 1);
         for (int j0 = 0; j0 < cnt; j0 += 8) {
-            float4 v[8];
-            float f[8];
+            if (j0) load(j0);
 #pragma unroll
             for (int u = 0; u < 8; ++u) {
-                f[u] = __shfl_sync(0xffffffffu, ak, (j0 + u) & 31);
-                v[u] = (j0 + u < cnt) ? *reinterpret_cast<const float4*>(part(base + (j0 + u) * step) + 4 * lane)
-                                      : make_float4(0.f, 0.f, 0.f, 0.f);
-            }
-#pragma unroll
-            for (int u = 0; u < 8; ++u) {
-                acc.x += f[u] * v[u].x; acc.y += f[u] * v[u].y; acc.z += f[u] * v[u].z; acc.w += f[u] * v[u].w;
+                const float f = __shfl_sync(0xffffffffu, ak, (j0 + u) & 31);
+                acc.x += f * v[u].x; acc.y += f * v[u].y; acc.z += f * v[u].z; acc.w += f * v[u].w;
             }
         }
     }
@@ -95,16 +101,12 @@ __global__ void __launch_bounds__(128) attn_merge(const AttnArgs a, int64_t n_ro
     }
     __syncwarp();
     const float* src = so[SPLIT ? 0 : warp];
-    bool live = n > 0;
-    if (live && a.tree) live = i < a.views[b].nd;
+    const bool live = n > 0 && i < nd;
     const float inv = (live && l != 0.f) ? a.out_up / l : 0.f;
+    const int sl[4] = {slot.x & (D - 1), slot.y & (D - 1), slot.z & (D - 1), slot.w & (D - 1)};
     float v[4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        const int c = 4 * lane + e;
-        const int slot = a.inv_perm_v ? (a.inv_perm_v[hk * D + c] & (D - 1)) : c;
-        v[e] = inv == 0.f ? 0.f : src[slot] * inv;
-    }
+    for (int e = 0; e < 4; ++e) v[e] = inv == 0.f ? 0.f : src[sl[e]] * inv;
     const int64_t at = (((int64_t)b * a.n_draft + i) * a.n_q_heads + hq) * D + 4 * lane;
     if (a.q_is_bf16)
         *reinterpret_cast<__nv_bfloat162*>(static_cast<__nv_bfloat16*>(a.out) + at) = __floats2bfloat162_rn(v[0], v[1]),

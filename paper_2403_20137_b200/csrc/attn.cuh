@@ -101,10 +101,12 @@ __device__ __forceinline__ SeqView seq_view(const AttnArgs& a, int b) {
 // All tiles, ordered by sequence, kv head, row tile, tile, are cut into `workers` contiguous ranges of at least one
 // (so workers <= n_items: the merge reads a partial of every worker between a row's first and last).
 __host__ __device__ __forceinline__ int worker_start(int w, int n_items, int workers) {
-    return (int)((int64_t)n_items * w / workers);
+    const uint64_t x = (uint64_t)(uint32_t)n_items * (uint32_t)w;
+    return x >> 32 ? (int)(x / (uint32_t)workers) : (int)((uint32_t)x / (uint32_t)workers);       // (a 64-bit division takes some hundred instructions)
 }
 __host__ __device__ __forceinline__ int worker_of(int x, int n_items, int workers) {
-    return (int)(((int64_t)(x + 1) * workers - 1) / n_items);
+    const uint64_t y = (uint64_t)(uint32_t)(x + 1) * (uint32_t)workers - 1u;
+    return y >> 32 ? (int)(y / (uint32_t)n_items) : (int)((uint32_t)y / (uint32_t)n_items);
 }
 
 // Tokens per tile of attn_rows, stages of a warp and thread blocks per SM (what registers and shared memory allow; four
