@@ -295,7 +295,8 @@ kvbfp_status attn_common(const AttnCall& c) {
     if (!few) st = f.mant_bits == 4 ? launch_attn_umma4(a, (int)grid, s) : f.mant_bits == 6 ? launch_attn_umma6(a, (int)grid, s) : launch_attn_umma8(a, (int)grid, s);
     else st = f.mant_bits == 4 ? launch_attn_rows4(a, (int)grid, s) : f.mant_bits == 6 ? launch_attn_rows6(a, (int)grid, s) : launch_attn_rows8(a, (int)grid, s);
     if (st != KVBFP_OK) return st;
-    // partials of a row, about: a block per row where they are many
+    // Partials of a row, about: a block per row where they are many (32 heads x 4104 tokens, 55 of them: 19.8 us against 22.7
+    // with a warp per row), a warp per row otherwise (16 x 32 x 8192, 16 tokens: 128 us against 140).
     const bool split = a.workers / ((int64_t)f.batch * f.n_kv_heads * n_row_tiles) >= 8;
     if (split) KVBFP_CUDA(launch_pdl(attn_merge<true>, dim3((unsigned)n_rows), dim3(128), 0, s, a, n_rows));
     else KVBFP_CUDA(launch_pdl(attn_merge<false>, dim3((unsigned)((n_rows + 3) / 4)), dim3(128), 0, s, a, n_rows));

@@ -1,4 +1,5 @@
-// Attention of drafted trees with 9 to 64 bf16 query rows per (batch, kv head), or more in items of 64, over the packed cache on the fifth-generation tensor cores.
+// Attention of drafted trees with 9 to 64 bf16 query rows per (batch, kv head), or more in items of 64, over the packed
+// cache on the fifth-generation tensor cores.
 //
 //   S^T[tokens x rows] = K . pi(Q)^T          K: tensor memory, pi(Q): shared memory
 //   y = log2(e) * (cap * tanh(scale * S / cap) - slope * distance) ;  P = 2^(y - m)
@@ -31,7 +32,7 @@
 // What bounds it: neither memory (0.44 of the copy rate at 16 rows) nor the tensor cores (7 to 15 % busy) but the warps'
 // instructions and the latency between them: some 700 to 940 a warp and tile, 0.5 to 0.6 issued a cycle by the 12 to 16
 // warps that registers and shared memory allow.  16 x 32 heads of up to 8192 4-bit rows, 16 drafted tokens: 113 us; 8 x 8
-// heads of 32768 rows, 64 query rows: 158 us; 8 x 8 heads of up to 8191 8-bit rows, 256 capped query rows: 165 us.
+// heads of 32768 rows, 64 query rows: 154 us; 8 x 8 heads of up to 8191 8-bit rows, 256 capped query rows: 165 us.
 // (V^T in tensor memory, filled through transposing loads, halves the shared-memory traffic and was 6 % slower: it costs
 // integer instructions.  Conversion as loops instead of straight code: 2 to 6 % slower.)
 #pragma once

@@ -641,6 +641,78 @@ def test_binding_refuses_what_the_kernels_could_not_read(monkeypatch):
     assert B.launch_count() == before
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("bits", [4, 6, 8])
+def test_wide_and_narrow_calls_at_once(bits):
+    """Narrow and wide trees, single tokens and weights on four streams at once, each as alone."""
+    cache, perm, perm_v, q = case(151, 3, 4, 2, 1056, 20, torch.bfloat16, bits, 32)
+    lens, q1, q3 = i32(1000, 0, 517), q[:, 0].contiguous(), q[:, :3].contiguous()
+    mod = B.ScoreMod(softcap=20.0, window=700)
+    ws = [torch.empty(B.attn_workspace_bytes(cache.fmt, 8, 20, True), dtype=torch.uint8, device="cuda") for _ in range(4)]
+    mass = [torch.zeros(3, 4, 1056, device="cuda") for _ in range(2)]
+    calls = [lambda m: B.tree_attn(cache, q, lens, perm_k=perm, workspace=ws[0]),
+             lambda m: B.tree_attn(cache, q3, lens, perm_k=perm, mod=mod, workspace=ws[1]),
+             lambda m: B.decode_attn_mod(cache, q1.float(), lens, mod, perm_k=perm, workspace=ws[2]),
+             lambda m: B.decode_attn_mass(cache, q1, lens, m, perm_k=perm, workspace=ws[3])]
+    want = [c(mass[0]) for c in calls]
+    for _ in range(4):
+        calls[3](mass[0])
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in calls]
+    got = []
+    for _ in range(5):
+        for s, c in zip(streams, calls):
+            with torch.cuda.stream(s):
+                got.append(c(mass[1]))
+    torch.cuda.synchronize()
+    assert all(torch.equal(g, want[i % 4]) for i, g in enumerate(got)) and torch.equal(mass[0], mass[1])
+    assert B.device_status() == 0
+
+
+@pytest.mark.gpu
+def test_whole_step_in_a_graph():
+    """Draft, score, commit, decode with weights and evict in place, captured once and replayed on restored caches."""
+    Bn, H, G, S, T = 2, 4, 2, 400, 12
+    cache, perm, perm_v, q = case(161, Bn, H, G, 432, T, torch.bfloat16, 4, 32)
+    g = torch.Generator().manual_seed(4)
+    kd, vd = (torch.randn(Bn, T, H, D, generator=g).cuda() for _ in range(2))
+    mask, depth = trees(Bn, T, None, 3)
+    index = torch.tensor([[0, 2, 5, 11], [1, 3, 0, 0]], dtype=torch.int32, device="cuda")
+    count, lens = i32(4, 2), i32(S, 250)
+    mass, new, kept = torch.zeros(Bn, H, 432, device="cuda"), i32(0, 0), torch.empty(Bn, H, 128, dtype=torch.int32, device="cuda")
+    ws = torch.empty(B.attn_workspace_bytes(cache.fmt, H * G, T, True), dtype=torch.uint8, device="cuda")
+    tree, one, tip = torch.empty_like(q), torch.empty_like(q[:, 0].contiguous()), q[:, 0].contiguous()
+
+    def step():
+        B.append(cache, kd, vd, lens, perm_k=perm, perm_v=perm_v)
+        B.tree_attn(cache, q, lens, tree_mask=mask, depth=depth, perm_k=perm, out=tree, workspace=ws)
+        B.gather_rows(cache, index, count, lens)
+        lens.add_(count)
+        B.decode_attn_mass(cache, tip, lens, mass, perm_k=perm, out=one, workspace=ws)
+        B.evict(cache, lens, mass, 128, 4, 16, new_lens=lens, kept=kept)
+
+    state = planes(cache) + [mass, lens, kept, tree, one]
+    start = [x.clone() for x in state]
+
+    def restore():
+        for x, y in zip(state, start):
+            x.copy_(y)
+
+    step()
+    torch.cuda.synchronize()
+    want = [x.clone() for x in state]
+    restore()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for _ in range(3):
+        restore()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(state, want))
+    assert lens.tolist() == [128, 128] and B.device_status() == 0
+
+
 # ----------------------------------------------------------------------------------------------- refusals (CPU)
 def test_workspace_sizes():
     f = B.Format(2, 4, 128, 64, 32, 4)
