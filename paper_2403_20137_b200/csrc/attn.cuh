@@ -118,7 +118,8 @@ __host__ __device__ constexpr int attn_rows_blocks(bool bf16) { return bf16 ? 3 
 kvbfp_status launch_attn_rows4(const AttnArgs& a, int grid, cudaStream_t s);
 kvbfp_status launch_attn_rows6(const AttnArgs& a, int grid, cudaStream_t s);
 kvbfp_status launch_attn_rows8(const AttnArgs& a, int grid, cudaStream_t s);
-// Teams (workers) of a block of attn_umma.
+// Teams (workers) of a block of attn_umma: three where shared memory holds their converted rows (16 x 32 x up to 8192 4-bit
+// rows, 16 tokens: 157 us against 174 with two when it was introduced).
 __host__ __device__ constexpr int attn_teams(int mant_bits, int rows_tile) { return mant_bits == 4 && rows_tile <= 32 ? 3 : 2; }
 // umma_prep and attn_umma: bf16 queries, tiles of 128 tokens, one thread block per SM
 kvbfp_status launch_attn_umma4(const AttnArgs& a, int grid, cudaStream_t s);

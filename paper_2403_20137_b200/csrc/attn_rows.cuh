@@ -9,7 +9,8 @@
 // persistent: all tiles are cut into one contiguous range per warp; a warp walks its range as runs (the tiles of one
 // (sequence, head, row tile)), shares nothing with other warps and meets no barrier.  A run that covers all tiles
 // writes the result itself, others leave a partial for attn_merge.  The tiles come through a per-warp ring of
-// shared-memory stages filled by asynchronous copies that run ahead across run boundaries.
+// shared-memory stages filled by asynchronous copies that run ahead across run boundaries.  (Rows of q are read where a run
+// begins, through the permutation, while the first copies are on their way.)
 //
 // Fragments.  The query rows are the narrow side (N = 8 of m16n8k16) of both products, so that few rows waste nothing: with
 // the rows as the wide side (16) a token costs twice the matrix instructions and the accumulators twice the registers
@@ -195,8 +196,7 @@ struct AGeo {
     static constexpr int TILE = attn_rows_tile(P);       // tokens per stage
     static constexpr int STAGES = attn_rows_stages(P);
     static constexpr int VM_OFF = TILE * ROW_M, KE_OFF = 2 * VM_OFF;
-    // exponent bytes of a stage: 2 * TILE * row_e, the stage rounded up to the swizzle's 1024 bytes for the tiled copies
-    __host__ __device__ static int exp_bytes(int row_e) { return 2 * TILE * row_e; }
+    __host__ __device__ static int exp_bytes(int row_e) { return 2 * TILE * row_e; }       // of a stage
     static constexpr int WARP_SMALL = kHeadDim * 4 + (STAGES * 8 + 15) / 16 * 16;    // rows and positions (one output row at the end of a run), barriers
     static_assert(kRows * 16 + kAttnMaxDraft * 4 <= kHeadDim * 4, "in an output row's place");
     __host__ __device__ static int smem_bytes(int row_e) {
