@@ -336,9 +336,10 @@ def attn_workspace_bytes(fmt, n_q_heads, n_draft=1, with_mass=False):
 
 def _same_device(cache, *tensors):
     """A call is enqueued on the current device: its cache and tensors have to be there."""
-    dev = cache.k_mant.device
-    if dev.index != torch.cuda.current_device() or any(t is not None and t.device != dev for t in tensors):
-        raise ValueError("expected the cache and all tensors on the current device")
+    dev = torch.cuda.current_device()
+    for t in (cache.k_mant, *tensors):
+        if t is not None and t.get_device() != dev:
+            raise ValueError("expected the cache and all tensors on the current device")
 
 
 def _empty(shape, dtype, device, stream):
@@ -349,9 +350,9 @@ def _empty(shape, dtype, device, stream):
         return torch.empty(shape, dtype=dtype, device=device)
 
 
-def _attn_buffers(cache, q, n_draft, with_mass, mod, out, workspace, stream, *tables):
+def _attn_buffers(cache, q, n_draft, with_mass, mod, out, workspace, stream, tables, *others):
     f = cache.fmt
-    _same_device(cache, q, out, workspace, *tables)
+    _same_device(cache, q, out, workspace, *tables, *others)
     for t in tables:
         if t is not None and t.numel() != f.n_kv_heads * f.head_dim:
             raise ValueError(f"permutation: expected {f.n_kv_heads} x {f.head_dim} values, got {t.numel()}")
@@ -367,6 +368,7 @@ def _attn_buffers(cache, q, n_draft, with_mass, mod, out, workspace, stream, *ta
     _dev(workspace, torch.uint8)
     ms = None
     if mod is not None:
+        _same_device(cache, mod.slopes, mod.first, mod.prefix)
         mod.check(f.batch, n_q_heads)
         ms = mod.struct()
     return n_q_heads, out, workspace, ms
@@ -378,7 +380,8 @@ def tree_attn(cache, q, ctx_lens, draft_lens=None, tree_mask=None, depth=None, p
     i: token i sees drafted token j), depth i32 [B, T] -> out [B, T, H_q, d] of q's type."""
     q = _dev(q)
     Bn, T = q.shape[0], q.shape[1]
-    n_q_heads, out, workspace, ms = _attn_buffers(cache, q, T, False, mod, out, workspace, stream, perm_k, inv_perm_v)
+    n_q_heads, out, workspace, ms = _attn_buffers(cache, q, T, False, mod, out, workspace, stream, (perm_k, inv_perm_v), ctx_lens,
+                                                   draft_lens, tree_mask, depth)
     cs = cache.struct()
     _check(lib().kvbfp_tree_attn(C.byref(cs), _ptr(q), _dt(q), n_q_heads, T,
                                  _ptr(_sized("ctx_lens", _dev(ctx_lens, torch.int32), (Bn,))),
@@ -395,7 +398,7 @@ def decode_attn_mod(cache, q, seq_lens, mod, perm_k=None, inv_perm_v=None, softm
                     stream=None):
     """kvbfp_decode_attn_mod: q [B, H_q, d], the last cached token of each sequence -> out of q's type."""
     q = _dev(q)
-    n_q_heads, out, workspace, ms = _attn_buffers(cache, q, 1, False, mod, out, workspace, stream, perm_k, inv_perm_v)
+    n_q_heads, out, workspace, ms = _attn_buffers(cache, q, 1, False, mod, out, workspace, stream, (perm_k, inv_perm_v), seq_lens)
     cs = cache.struct()
     _check(lib().kvbfp_decode_attn_mod(C.byref(cs), _ptr(q), _dt(q), n_q_heads,
                                        _ptr(_sized("seq_lens", _dev(seq_lens, torch.int32), (q.shape[0],))),
@@ -410,7 +413,7 @@ def decode_attn_mass(cache, q, seq_lens, mass, mod=None, perm_k=None, inv_perm_v
     """kvbfp_decode_attn_mass: decode_attn_mod that adds every token's softmax weight to mass f32 [B, H_kv, max_seq]."""
     q = _dev(q)
     f = cache.fmt
-    n_q_heads, out, workspace, ms = _attn_buffers(cache, q, 1, True, mod, out, workspace, stream, perm_k, inv_perm_v)
+    n_q_heads, out, workspace, ms = _attn_buffers(cache, q, 1, True, mod, out, workspace, stream, (perm_k, inv_perm_v), seq_lens, mass)
     cs = cache.struct()
     _check(lib().kvbfp_decode_attn_mass(C.byref(cs), _ptr(q), _dt(q), n_q_heads,
                                         _ptr(_sized("seq_lens", _dev(seq_lens, torch.int32), (q.shape[0],))),
