@@ -334,11 +334,12 @@ kvbfp_status kvbfp_evict(const kvbfp_cache* src, const int32_t* seq_lens, const 
  * Moves listed rows together in all four planes: row src_base[b] + index[b, h, i] of src becomes row dst_base[b] + i
  * of dst, i < count[b].  With src = dst and both bases the context length this commits the accepted branch of a
  * drafted tree.
- *   index     [batch, index_heads, n_index] i32, index_heads 1 (all heads alike) or n_kv_heads; in place the source
- *             rows have to ascend, none below its destination (other orders give unspecified rows)
+ *   index     [batch, index_heads, n_index] i32, index_heads 1 (all heads alike) or n_kv_heads; in place no source
+ *             row may lie below its destination
  *   count     [batch] i32, read clamped to [0, n_index];  src_base, dst_base [batch] i32 or NULL (0)
  *   dst       as in kvbfp_evict
- * Rows outside a cache are skipped and set KVBFP_FLAG_POSITION.
+ * Rows outside a cache, negative indices and, in place, source rows below their destination are skipped and set
+ * KVBFP_FLAG_POSITION.
  */
 kvbfp_status kvbfp_gather_rows(const kvbfp_cache* src, const kvbfp_cache* dst, const int32_t* index,
                                int32_t index_heads, int32_t n_index, const int32_t* count, const int32_t* src_base,

@@ -218,8 +218,8 @@ __device__ __forceinline__ uint4 ld_row(const void* p) {
 
 // Rows src_base + index[i] -> dst_base + i of all planes, kMoveRows at a time through registers.  A block per (chunk,
 // pair) where the caches differ; in place one block per pair walks the chunks upwards: every row of a chunk is read
-// before any is written, and with ascending indices (index[i] >= i) later chunks read only rows behind the written
-// ones.
+// before any is written, and as no source lies below its destination (others are refused) later chunks read only rows
+// behind the written ones.
 template <bool IN_PLACE, int PIECES>      // 16-byte pieces of a mantissa row: 4, 6, 8
 __global__ void __launch_bounds__(kMoveThreads) move_rows(const MoveArgs a) {
     constexpr int PER = kMoveRows * PIECES / kMoveThreads;      // pieces per thread and plane
@@ -241,7 +241,7 @@ __global__ void __launch_bounds__(kMoveThreads) move_rows(const MoveArgs a) {
                 const int v = idx[i];
                 const int64_t s = (int64_t)sb + v, d = (int64_t)db + i;
                 if (v >= 0) {
-                    if (s >= 0 && s < a.src.max_seq && d >= 0 && d < a.dst.max_seq) r = (IN_PLACE && s == d) ? -1 : (int)s;
+                    if (s >= 0 && s < a.src.max_seq && d >= 0 && d < a.dst.max_seq && !(IN_PLACE && s < d)) r = (IN_PLACE && s == d) ? -1 : (int)s;
                     else raise_flag(a.status, KVBFP_FLAG_POSITION);
                 } else if (a.count) {
                     raise_flag(a.status, KVBFP_FLAG_POSITION);

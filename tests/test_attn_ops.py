@@ -533,6 +533,28 @@ def test_gather_rows_outside_the_cache_are_skipped():
 
 
 @pytest.mark.gpu
+def test_gather_rows_in_place_order():
+    """In place: any order whose sources lie at or behind their destinations; others are skipped and flagged."""
+    cache, _, _ = make_cache(1, 2, 448, 4, 32, 6)
+    src = [p.clone() for p in planes(cache)]
+    rng = np.random.default_rng(3)
+    idx = np.minimum(np.arange(200) + rng.integers(0, 200, 200), 399).astype(np.int32)          # not ascending, some twice
+    B.gather_rows(cache, torch.from_numpy(idx)[None].contiguous().cuda(), i32(200), i32(40))
+    assert B.device_status() == 0
+    for p, q in zip(planes(cache), src):
+        want = q.clone()
+        want[:, :, 40:240] = q[:, :, torch.from_numpy(idx).long().cuda() + 40]
+        assert torch.equal(p, want)
+    src = [p.clone() for p in planes(cache)]
+    B.gather_rows(cache, i32(0, 1, 1, 7, 2)[None].contiguous(), i32(5))
+    assert B.device_status() == B.FLAG_POSITION
+    for p, q in zip(planes(cache), src):
+        want = q.clone()
+        want[:, :, 3] = q[:, :, 7]
+        assert torch.equal(p, want)
+
+
+@pytest.mark.gpu
 def test_speculative_step_then_eviction():
     """As they are used together: draft a tree, score it, commit a branch, go on decoding with weights, evict, decode."""
     Bn, H, G, S, T = 2, 2, 2, 300, 7
