@@ -711,11 +711,12 @@ __global__ void __launch_bounds__(UGeo<P, N>::THREADS, 1) attn_umma(const AttnAr
                     part[m_pos * kAttnPart + D + 1] = ls;
                 }
             }
+            // (read before the barrier: a warp that is through with its results writes the next head's table)
+            const int ch = a.inv_perm_v ? chan[slot_of] : slot_of;
             wait(b_o(team), it - 1);
             __syncwarp();
             tmem_fence_after();
             named_sync(bar_id, 128);
-            const int ch = a.inv_perm_v ? chan[slot_of] : slot_of;
 #pragma unroll 1
             for (int j = 0; j < C; j += 8) {
                 uint32_t o[8];

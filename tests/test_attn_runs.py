@@ -1,0 +1,103 @@
+"""Attention over the packed cache where every worker of the kernels has several tiles and several runs (tiles of one
+sequence, head and row tile), against fp64 matrix products on the dequantised cache."""
+import math
+import os
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2403_20137_b200 import binding as B, build
+from test_attn_ops import D, check, i32, inverse, trees
+
+
+# ----------------------------------------------------------------------------------------------- helpers
+def long_case(seed, batch, heads, group, max_seq, T, dtype, bits, block, empty=0.1):
+    """Ragged sequences, made on the GPU; keys grow along the sequence, so that the running maxima keep rising."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    rng = np.random.default_rng(seed)
+    grow = (0.2 + 2.8 * torch.arange(max_seq, device="cuda") / max_seq)[None, :, None, None]
+    k = torch.randn(batch, max_seq, heads, D, generator=g, device="cuda") * grow
+    v = torch.randn(batch, max_seq, heads, D, generator=g, device="cuda")
+    perm, perm_v = (torch.rand(heads, D, generator=g, device="cuda").argsort(-1).to(torch.int32).contiguous() for _ in range(2))
+    cache = B.Cache(batch, heads, D, max_seq, block, bits)
+    B.append(cache, k, v, torch.zeros(batch, dtype=torch.int32, device="cuda"), perm_k=perm, perm_v=perm_v)
+    q = torch.randn(batch, T, heads * group, D, generator=g, device="cuda").to(dtype)
+    lens = rng.integers(1, max_seq - T + 1, batch)
+    lens[rng.random(batch) < empty] = 0
+    lens[batch // 2] = max_seq - T
+    return cache, perm, perm_v, q, torch.from_numpy(lens.astype(np.int32)).cuda()
+
+
+def wide_reference(cache, q, lens, perm, perm_v, mod, scale=0.0, drafts=None, mask=None, depth=None, weights=None):
+    """-> out, the sum of p|v| per output, the largest sum of |q k| scale of a row's visible tokens; all fp64.
+    q [B, T, Hq, D]; drafts None: a single token at lens - 1.  `weights` [B, H, max_seq]: the softmax weights are added."""
+    f = cache.fmt
+    Bn, T, Hq, _ = q.shape
+    H, G = f.n_kv_heads, Hq // f.n_kv_heads
+    scale = scale or 1.0 / math.sqrt(D)
+    k, v = B.dequant_all(cache, "k", f.max_seq, perm=perm), B.dequant_all(cache, "v", f.max_seq, perm=perm_v)
+    out = torch.zeros(Bn, T, Hq, D, dtype=torch.float64, device="cuda")
+    amp, reach = torch.zeros_like(out), torch.zeros(Bn, T, Hq, dtype=torch.float64, device="cuda")
+    back = lambda x: x.reshape(H, T, G, -1).transpose(0, 1).reshape(T, Hq, -1)
+    for b, n in enumerate(lens.tolist()):
+        nd = 0 if drafts is None else int(drafts[b])
+        m = n + nd
+        if m == 0 or (drafts is not None and nd == 0):
+            continue
+        kp = torch.arange(m, device="cuda")
+        pos = torch.tensor([n - 1], device="cuda") if drafts is None else n + depth[b].long()
+        if nd:
+            kp[n:] = n + depth[b, :nd].long()
+        near = (pos[:, None] - kp < mod.window) if mod.window else torch.ones(T, m, dtype=torch.bool, device="cuda")
+        see = near.clone()
+        if mod.first is not None:
+            see[:, :n] &= kp[:n] >= min(max(int(mod.first[b]), 0), n)
+        if mod.prefix is not None:
+            see[:, :n] |= kp[:n] < min(max(int(mod.prefix[b]), 0), n)
+        if nd:
+            see[:, n:] = ((mask[b][:, None] >> torch.arange(nd, device="cuda")) & 1).bool() & near[:, n:]
+            see[nd:] = False
+        kb, vb = (x[b, :m].double().transpose(0, 1) for x in (k, v))                              # [H, m, D]
+        qb = q[b].double().reshape(T, H, G, D).transpose(0, 1).reshape(H, T * G, D)
+        seen = see.repeat_interleave(G, 0)[None]
+        x = qb @ kb.transpose(1, 2) * scale
+        r = (qb.abs() @ kb.abs().transpose(1, 2) * scale).masked_fill(~seen, 0.0).amax(-1)
+        if mod.softcap:
+            x = mod.softcap * torch.tanh(x / mod.softcap)
+        if mod.slopes is not None:
+            x = x - mod.slopes.double().reshape(H, 1, G, 1).expand(H, T, G, 1).reshape(H, T * G, 1) * (pos[:, None] - kp).repeat_interleave(G, 0)
+        p = torch.softmax(x.masked_fill(~seen, -math.inf), -1).nan_to_num(0.0)
+        out[b], amp[b], reach[b] = back(p @ vb), back(p @ vb.abs()), back(r[..., None])[..., 0]
+        if weights is not None:
+            weights[b, :, :m] += p.sum(1)
+    return out, amp, reach
+
+
+# ----------------------------------------------------------------------------------------------- runs after runs
+@pytest.mark.gpu
+@pytest.mark.parametrize("bits", [4, 6, 8])
+@pytest.mark.parametrize("T,group", [(16, 1), (8, 4), (33, 2)])
+def test_value_order_of_each_head(T, group, bits):
+    """Whole runs of one head after another, each head with a value order of its own: a run's results are in its own
+    head's order (three widths of query rows)."""
+    cache, perm, perm_v, q, lens = long_case(5, 128, 8, group, 640, T, torch.bfloat16, bits, 32)
+    drafts = torch.full((128,), T, dtype=torch.int32, device="cuda")
+    mask, depth = trees(128, T, drafts, 4)
+    kw = dict(tree_mask=mask, depth=depth, perm_k=perm, inv_perm_v=inverse(perm_v))
+    got = B.tree_attn(cache, q, lens, **kw)
+    check(got, *wide_reference(cache, q, lens, perm, perm_v, B.ScoreMod(), drafts=drafts, mask=mask, depth=depth))
+    for _ in range(20):
+        assert torch.equal(B.tree_attn(cache, q, lens, **kw), got)
+    assert B.device_status() == 0
+
+
+def test_channel_table_is_read_before_the_last_barrier_of_a_run():
+    """The order that keeps two runs apart, in the source (a run too late by some hundred cycles would not show): the
+    table is written before the first barrier of a run, so it has to be read before the last one."""
+    with open(os.path.join(build.CSRC, "attn_umma.cuh")) as f:
+        code = f.read()
+    write, read = code.index("chan[a.inv_perm_v["), code.index("chan[slot_of]")
+    end = code.index("c = cn;", read)
+    sync = "named_sync(bar_id, 128);"
+    assert code.index(sync, write) < read < code.rindex(sync, write, end)
