@@ -330,6 +330,13 @@ def _sized(name, t, shape):
     return t
 
 
+def _query(q, shape):
+    """The kernels take the numbers of tokens and heads from q's shape: a tensor of another rank would be read past its end."""
+    if q.dim() != len(shape):
+        raise ValueError(f"q: expected [{', '.join(shape)}], got shape {tuple(q.shape)}")
+    return _dev(q)
+
+
 def attn_workspace_bytes(fmt, n_q_heads, n_draft=1, with_mass=False):
     return int(lib().kvbfp_attn_workspace_bytes(C.byref(fmt), n_q_heads, n_draft, int(with_mass)))
 
@@ -378,7 +385,7 @@ def tree_attn(cache, q, ctx_lens, draft_lens=None, tree_mask=None, depth=None, p
               softmax_scale=0.0, mod=None, out=None, workspace=None, stream=None):
     """kvbfp_tree_attn: q [B, T, H_q, d] of T drafted tokens appended at ctx_lens; tree_mask int64 [B, T] (bit j of row
     i: token i sees drafted token j), depth i32 [B, T] -> out [B, T, H_q, d] of q's type."""
-    q = _dev(q)
+    q = _query(q, ("B", "T", "H_q", "d"))
     Bn, T = q.shape[0], q.shape[1]
     n_q_heads, out, workspace, ms = _attn_buffers(cache, q, T, False, mod, out, workspace, stream, (perm_k, inv_perm_v), ctx_lens,
                                                    draft_lens, tree_mask, depth)
@@ -397,7 +404,7 @@ def tree_attn(cache, q, ctx_lens, draft_lens=None, tree_mask=None, depth=None, p
 def decode_attn_mod(cache, q, seq_lens, mod, perm_k=None, inv_perm_v=None, softmax_scale=0.0, out=None, workspace=None,
                     stream=None):
     """kvbfp_decode_attn_mod: q [B, H_q, d], the last cached token of each sequence -> out of q's type."""
-    q = _dev(q)
+    q = _query(q, ("B", "H_q", "d"))
     n_q_heads, out, workspace, ms = _attn_buffers(cache, q, 1, False, mod, out, workspace, stream, (perm_k, inv_perm_v), seq_lens)
     cs = cache.struct()
     _check(lib().kvbfp_decode_attn_mod(C.byref(cs), _ptr(q), _dt(q), n_q_heads,
@@ -411,7 +418,7 @@ def decode_attn_mod(cache, q, seq_lens, mod, perm_k=None, inv_perm_v=None, softm
 def decode_attn_mass(cache, q, seq_lens, mass, mod=None, perm_k=None, inv_perm_v=None, softmax_scale=0.0, out=None,
                      workspace=None, stream=None):
     """kvbfp_decode_attn_mass: decode_attn_mod that adds every token's softmax weight to mass f32 [B, H_kv, max_seq]."""
-    q = _dev(q)
+    q = _query(q, ("B", "H_q", "d"))
     f = cache.fmt
     n_q_heads, out, workspace, ms = _attn_buffers(cache, q, 1, True, mod, out, workspace, stream, (perm_k, inv_perm_v), seq_lens, mass)
     cs = cache.struct()

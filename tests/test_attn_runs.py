@@ -101,3 +101,30 @@ def test_channel_table_is_read_before_the_last_barrier_of_a_run():
     end = code.index("c = cn;", read)
     sync = "named_sync(bar_id, 128);"
     assert code.index(sync, write) < read < code.rindex(sync, write, end)
+
+
+# ----------------------------------------------------------------------------------------------- refusals
+def test_queries_of_another_rank_are_refused():
+    """One token's queries given as a tree's would be read far past their end, a tree's as one token's in part."""
+    cache = B.Cache(2, 2, D, 64, 32, 4, device="cpu")
+    lens, mass = torch.zeros(2, dtype=torch.int32), torch.zeros(2, 2, 64)
+    one, tree = torch.zeros(2, 4, D), torch.zeros(2, 3, 4, D)
+    for q in (one, tree[:, 0, 0], tree[None]):
+        with pytest.raises(ValueError, match="expected .B, T, H_q, d."):
+            B.tree_attn(cache, q, lens)
+    for q in (tree, one[:, 0]):
+        with pytest.raises(ValueError, match="expected .B, H_q, d."):
+            B.decode_attn_mod(cache, q, lens, None)
+        with pytest.raises(ValueError, match="expected .B, H_q, d."):
+            B.decode_attn_mass(cache, q, lens, mass)
+
+
+@pytest.mark.gpu
+def test_queries_of_another_rank_launch_nothing():
+    cache, perm, _, q, lens = long_case(6, 2, 2, 2, 64, 4, torch.bfloat16, 4, 32)
+    mass, before = torch.zeros(2, 2, 64, device="cuda"), B.launch_count()
+    for call in (lambda: B.tree_attn(cache, q[:, 0].contiguous(), lens), lambda: B.decode_attn_mod(cache, q, lens, None),
+                 lambda: B.decode_attn_mass(cache, q, lens, mass)):
+        with pytest.raises(ValueError, match="expected"):
+            call()
+    assert B.launch_count() == before
