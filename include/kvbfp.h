@@ -252,6 +252,8 @@ kvbfp_status kvbfp_decode_attn_rope(const kvbfp_cache* cache, const void* q, kvb
  *   cap      x = softcap * tanh(x / softcap)              (0: none)
  *   bias     x = x - slopes[h] * (pos_q - pos_k)          (NULL: none; h = query head)
  *   visible  pos_k < prefix[b], or pos_k >= first[b] and pos_q - pos_k < window   (NULL / 0: no such limit)
+ * The cap is applied in fp32: with bf16 queries to some 2e-7 of a cap of up to 64 and to some 2e-6 of the capped score
+ * under larger ones, with fp32 queries to fp32 accuracy.
  * first[b] is where the current document begins, prefix[b] tokens stay visible whatever the window hides.  Values are
  * read clamped to [0, cached tokens].  A query that sees nothing gives zeros.
  */

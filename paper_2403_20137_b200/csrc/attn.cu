@@ -269,7 +269,8 @@ kvbfp_status attn_common(const AttnCall& c) {
     a.perm_k = c.perm_k; a.inv_perm_v = c.inv_perm_v;
     a.scale = c.softmax_scale > 0.f ? c.softmax_scale : 1.0f / sqrtf((float)f.head_dim);
     if (c.mod) {
-        a.softcap = c.mod->softcap; a.window = c.mod->window; a.slopes = c.mod->slopes;
+        // (2^126: so that neither its inverse nor its multiples leave the fp32 range; scores that it would cap are near the end of that range themselves)
+        a.softcap = fminf(c.mod->softcap, 0x1p126f); a.window = c.mod->window; a.slopes = c.mod->slopes;
         a.first = c.mod->first; a.prefix = c.mod->prefix;
     }
     a.out = c.out;

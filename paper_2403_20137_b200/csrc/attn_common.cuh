@@ -10,6 +10,17 @@
 namespace kvbfp {
 namespace {
 
+// tanh as 1 - 2 / (1 + e^2x) is off by some 2e-7 whatever its value, which a cap multiplies: fine for caps up to this one
+// (2e-5 of a score at most), while larger ones would lose the scores they are meant to leave alone.
+constexpr float kCapFast = 64.f;
+// tanh to about 2e-6 of its value: the Taylor series x - x^3/3 + 2x^5/15 - 17x^7/315 + 62x^9/2835 below 1/4 (the next term is
+// 9e-9 of the value there), the exponential above.
+__device__ __forceinline__ float tanh_relative(float x) {
+    const float s = x * x;
+    const float small = x * fmaf(s, fmaf(s, fmaf(s, fmaf(s, 62.f / 2835.f, -17.f / 315.f), 2.f / 15.f), -1.f / 3.f), 1.f);
+    return fabsf(x) < 0.25f ? small : 1.f - __fdividef(2.f, 1.f + ex2_approx(x * 2.8853900817779268f));
+}
+
 // Depth of drafted token i, and what a query row (draft-major, group-minor) needs of itself; rows behind R see no draft.
 __device__ __forceinline__ int draft_depth(const AttnArgs& a, int b, int i) {
     return a.depth ? min(max(a.depth[(int64_t)b * a.n_draft + i], 0), a.n_draft - 1) : i;

@@ -450,6 +450,10 @@ __global__ void __launch_bounds__(kAttnWarps * 32, attn_rows_blocks(!F32)) attn_
                 float mul = plain;
                 if (a.softcap > 0.f) {
                     mul = a.softcap * to_log2;
+                    if (!F32 && a.softcap > kCapFast) {
+#pragma unroll
+                        for (int x = 0; x < 8; ++x) sc[x >> 2][x & 3] = tanh_relative(sc[x >> 2][x & 3] * cap_in);
+                    } else
 #pragma unroll
                     for (int x = 0; x < 8; ++x) {
                         float& y = sc[x >> 2][x & 3];

@@ -103,6 +103,28 @@ def test_channel_table_is_read_before_the_last_barrier_of_a_run():
     assert code.index(sync, write) < read < code.rindex(sync, write, end)
 
 
+# ----------------------------------------------------------------------------------------------- caps of any size
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("T,group", [(1, 3), (10, 1), (9, 3), (20, 3)])
+@pytest.mark.parametrize("cap", [65.0, 1e5, 1e8, 1e30, 3e38])
+def test_large_caps_leave_scores_alone(cap, T, group, bits, dtype):
+    """The error of a capped score goes by the score, not by the cap: 2^-18 of it (the tanh's 1.5e-6 and three fp32
+    roundings), on top of the product's own (24 steps of 2^-23 of the sum of |q k|, which is at least the score)."""
+    cache, perm, perm_v, q, lens = long_case(7, 3, 2, group, 416, T, dtype, bits, 32, empty=0.0)
+    mod, kw = B.ScoreMod(softcap=cap), dict(perm_k=perm, inv_perm_v=inverse(perm_v))
+    drafts = torch.full((3,), T, dtype=torch.int32, device="cuda")
+    if T == 1:
+        got = B.decode_attn_mod(cache, q[:, 0].contiguous(), lens, mod, **kw)[:, None]
+        out, amp, reach = wide_reference(cache, q, lens, perm, perm_v, mod)
+    else:
+        mask, depth = trees(3, T, drafts, 8)
+        got = B.tree_attn(cache, q, lens, tree_mask=mask, depth=depth, mod=mod, **kw)
+        out, amp, reach = wide_reference(cache, q, lens, perm, perm_v, mod, drafts=drafts, mask=mask, depth=depth)
+    check(got, out, amp, reach * (1.0 + 2.0 ** -18 / (24 * 2.0 ** -23)))
+
+
 # ----------------------------------------------------------------------------------------------- refusals
 def test_queries_of_another_rank_are_refused():
     """One token's queries given as a tree's would be read far past their end, a tree's as one token's in part."""
