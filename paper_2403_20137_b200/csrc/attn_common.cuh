@@ -13,6 +13,7 @@ namespace {
 // tanh as 1 - 2 / (1 + e^2x) is off by some 2e-7 whatever its value, which a cap multiplies: fine for caps up to this one
 // (2e-5 of a score at most), while larger ones would lose the scores they are meant to leave alone.
 constexpr float kCapFast = 64.f;
+__device__ __forceinline__ float finite_factor(float x) { return fminf(x, 1e38f); }      // (0 times it, or three times it, has to stay 0)
 // tanh to about 2e-6 of its value: the Taylor series x - x^3/3 + 2x^5/15 - 17x^7/315 + 62x^9/2835 below 1/4 (the next term is
 // 9e-9 of the value there), the exponential above.
 __device__ __forceinline__ float tanh_relative(float x) {

@@ -574,7 +574,7 @@ __global__ void __launch_bounds__(UGeo<P, N>::THREADS, 1) attn_umma(const AttnAr
                     tmem_wait_ld(raw);
                 }
                 if (a.softcap > 0.f) {
-                    const float in = cap_in * __uint_as_float(k_top << 23);
+                    const float in = finite_factor(cap_in * __uint_as_float(k_top << 23));
                     const float to_x = up * __uint_as_float(k_top << 23), inv_cap = 1.f / a.softcap;      // (in two steps: their product may be too small)
                     mul = a.softcap * to_log2;
                     if (a.softcap > kCapFast) change_scores<C>(tm_s, raw, [&](float y, int) { return tanh_relative(y * to_x * inv_cap); });

@@ -125,6 +125,26 @@ def test_large_caps_leave_scores_alone(cap, T, group, bits, dtype):
     check(got, out, amp, reach * (1.0 + 2.0 ** -18 / (24 * 2.0 ** -23)))
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("T", [3, 12, 40])
+@pytest.mark.parametrize("grow,scale", [(2.0 ** 100, 0.0), (1.0, 1e20)])
+def test_small_caps_and_large_factors(grow, scale, T, dtype):
+    """The smallest cap turns every score into almost nothing, also where scale / cap or the cached magnitudes over it
+    leave the fp32 range: rows of zeros (scores 0) and others weigh all they see alike."""
+    g = torch.Generator(device="cuda").manual_seed(9)
+    k, v = (torch.randn(2, 288, 2, D, generator=g, device="cuda") for _ in range(2))
+    cache = B.Cache(2, 2, D, 288, 32, 4)
+    B.append(cache, k * grow, v, i32(0, 0))
+    q = torch.randn(2, T, 2, D, generator=g, device="cuda").to(dtype)
+    q[:, ::2] = 0.0
+    mod, lens, drafts = B.ScoreMod(softcap=1e-20), i32(200, 7), i32(T, T)
+    mask, depth = trees(2, T, drafts, 8, chain=True)
+    got = B.tree_attn(cache, q, lens, mod=mod, softmax_scale=scale)
+    out, amp, _ = wide_reference(cache, q, lens, None, None, mod, scale=scale, drafts=drafts, mask=mask, depth=depth)
+    check(got, out, amp, torch.zeros_like(amp[..., 0]))
+
+
 # ----------------------------------------------------------------------------------------------- refusals
 def test_queries_of_another_rank_are_refused():
     """One token's queries given as a tree's would be read far past their end, a tree's as one token's in part."""
