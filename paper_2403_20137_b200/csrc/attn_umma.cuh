@@ -575,10 +575,13 @@ __global__ void __launch_bounds__(UGeo<P, N>::THREADS, 1) attn_umma(const AttnAr
                 }
                 if (a.softcap > 0.f) {
                     const float in = finite_factor(cap_in * __uint_as_float(k_top << 23));
-                    const float to_x = up * __uint_as_float(k_top << 23), inv_cap = 1.f / a.softcap;      // (in two steps: their product may be too small)
                     mul = a.softcap * to_log2;
-                    if (a.softcap > kCapFast) change_scores<C>(tm_s, raw, [&](float y, int) { return tanh_relative(y * to_x * inv_cap); });
-                    else change_scores<C>(tm_s, raw, [&](float y, int) { return fmaf(-2.f, rcp_approx(1.f + ex2_approx(y * in)), 1.f); });      // tanh x = 1 - 2 / (1 + e^2x): about 2e-7 absolute
+                    if (a.softcap > kCapFast) {
+                        const float to_x = up * __uint_as_float(k_top << 23), inv_cap = 1.f / a.softcap;      // (in two steps: their product may be too small)
+                        change_scores<C>(tm_s, raw, [&](float y, int) { return tanh_relative(y * to_x * inv_cap); });
+                    } else {
+                        change_scores<C>(tm_s, raw, [&](float y, int) { return fmaf(-2.f, rcp_approx(1.f + ex2_approx(y * in)), 1.f); });      // tanh x = 1 - 2 / (1 + e^2x): about 2e-7 absolute
+                    }
                 }
                 const bool masked = a.slopes != nullptr || !(tt + kUTile <= sv.ctx && (tt >= clear_lo || tt + kUTile <= sv.pf));
                 if (masked) {
