@@ -117,7 +117,8 @@ __global__ void __launch_bounds__(128) attn_merge(const AttnArgs a, int64_t n_ro
 }
 
 // mass[b, h, t] += sum over the group's query heads of 2^(score - lse).  tile / 4 lanes per tile, four tokens a lane;
-// the tiles are those the scores were written for.  Memory-bound: 4 G + 8 bytes a token.
+// the tiles are those the scores were written for.  Hidden tokens are skipped, not added as zeros: the sum of a query that
+// is not finite is NaN.  Memory-bound: 4 G + 8 bytes a token.
 __global__ void __launch_bounds__(128) attn_mass(const AttnArgs a) {
     pdl_wait();
     pdl_trigger();
@@ -142,13 +143,17 @@ __global__ void __launch_bounds__(128) attn_mass(const AttnArgs a) {
             float4 acc = *to;
             const float* y = a.scores + ((int64_t)b * a.n_q_heads + h * a.group) * max_seq + tok;
             const float* ls = a.lse + (int64_t)b * a.n_q_heads + h * a.group;
+            const int from = max(sv.first, a.window > 0 ? sv.ctx - a.window : 0);
+            bool see[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) see[e] = tok + e < sv.ctx && (tok + e >= from || tok + e < sv.pf);
             for (int q = 0; q < a.group; ++q) {
                 const float4 s = *reinterpret_cast<const float4*>(y + (int64_t)q * max_seq);
                 const float z = ls[q];
-                acc.x += exp2f(s.x - z);
-                if (tok + 1 < sv.ctx) acc.y += exp2f(s.y - z);       // (behind the end there is nothing of this call)
-                if (tok + 2 < sv.ctx) acc.z += exp2f(s.z - z);
-                if (tok + 3 < sv.ctx) acc.w += exp2f(s.w - z);
+                if (see[0]) acc.x += exp2f(s.x - z);
+                if (see[1]) acc.y += exp2f(s.y - z);
+                if (see[2]) acc.z += exp2f(s.z - z);
+                if (see[3]) acc.w += exp2f(s.w - z);
             }
             *to = acc;
         }

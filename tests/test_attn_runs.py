@@ -145,6 +145,31 @@ def test_small_caps_and_large_factors(grow, scale, T, dtype):
     check(got, out, amp, torch.zeros_like(amp[..., 0]))
 
 
+# ----------------------------------------------------------------------------------------------- weights
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_hidden_tokens_keep_their_weights_whatever_the_query(bad, bits, dtype):
+    """A query that is not finite makes its own visible tokens' weights NaN, not those of tokens it does not see."""
+    cache, perm, perm_v, q, _ = long_case(10, 2, 2, 2, 480, 1, dtype, bits, 32)
+    lens = i32(467, 201)
+    mod = B.ScoreMod(window=77, prefix=i32(3, 9), first=i32(0, 130))
+    q[0, 0, 1, 5] = bad                        # first sequence, first kv head
+    mass = torch.rand(2, 2, 480, device="cuda")
+    mass[0, 0, 40] = -0.0
+    before = mass.clone()
+    B.decode_attn_mass(cache, q[:, 0].contiguous(), lens, mass, mod=mod, perm_k=perm)
+    t = torch.arange(480, device="cuda")
+    for b, (n, first, prefix) in enumerate(((467, 0, 3), (201, 130, 9))):
+        see = (t < prefix) | ((t >= first) & (n - 1 - t < 77) & (t < n))
+        for h in range(2):
+            assert torch.equal(mass[b, h, ~see].view(torch.int32), before[b, h, ~see].view(torch.int32))
+            moved = mass[b, h, see]
+            assert bool(torch.isnan(moved).all() if (b, h) == (0, 0) else torch.isfinite(moved).all())
+    assert B.device_status() == 0
+
+
 # ----------------------------------------------------------------------------------------------- refusals
 def test_queries_of_another_rank_are_refused():
     """One token's queries given as a tree's would be read far past their end, a tree's as one token's in part."""
