@@ -322,7 +322,7 @@ kvbfp_status kvbfp_decode_attn_mass(const kvbfp_cache* cache, const void* q, kvb
  * rows go to rows 0.. of `dst`, their masses to dst_mass [batch, n_kv_heads, dst max_seq], whose entries behind them
  * are set to zero; packed rows of dst behind them are left as they are.
  *   dst       another cache of the same batch, heads, block and mantissa width with max_seq >= budget that shares no
- *             memory with src (nor dst_mass with mass), or src itself (then dst_mass is mass)
+ *             memory with src in any of the planes (nor dst_mass with mass), or src itself (then dst_mass is mass)
  *   new_lens  [batch] i32 out: min(seq_lens, budget); may be seq_lens
  *   kept      [batch, n_kv_heads, budget] i32 out: the kept positions, -1 behind the last
  * Heads keep different tokens, so row numbers are no positions any more: keys have to be cached with their position

@@ -352,10 +352,11 @@ kvbfp_status set_caches(const kvbfp_cache* src, const kvbfp_cache* dst, MoveArgs
     }
     if (same != 0 && (same != 4 || f.max_seq != d.max_seq)) return KVBFP_ERR_INVALID_ARG;
     const size_t pairs = (size_t)f.batch * f.n_kv_heads;
-    for (int i = 0; i < 4 && same == 0; ++i) {        // different caches must not overlap
-        const size_t row = (i & 1) ? row_e_bytes(f) : row_m_bytes(f);
-        const uintptr_t x = (uintptr_t)from[i], y = (uintptr_t)to[i];
-        if (x < y + pairs * d.max_seq * row && y < x + pairs * f.max_seq * row) return KVBFP_ERR_INVALID_ARG;
+    for (int x = 0; x < 16 && same == 0; ++x) {        // different caches must not overlap, whichever planes
+        const int i = x >> 2, j = x & 3;
+        const size_t row_i = (i & 1) ? row_e_bytes(f) : row_m_bytes(f), row_j = (j & 1) ? row_e_bytes(f) : row_m_bytes(f);
+        const uintptr_t s = (uintptr_t)from[i], t = (uintptr_t)to[j];
+        if (s < t + pairs * d.max_seq * row_j && t < s + pairs * f.max_seq * row_i) return KVBFP_ERR_INVALID_ARG;
     }
     return KVBFP_OK;
 }

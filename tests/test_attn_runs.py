@@ -1,5 +1,6 @@
 """Attention over the packed cache where every worker of the kernels has several tiles and several runs (tiles of one
 sequence, head and row tile), against fp64 matrix products on the dequantised cache."""
+import ctypes as C
 import math
 import os
 
@@ -194,4 +195,20 @@ def test_queries_of_another_rank_launch_nothing():
                  lambda: B.decode_attn_mass(cache, q, lens, mass)):
         with pytest.raises(ValueError, match="expected"):
             call()
+    assert B.launch_count() == before
+
+
+def test_caches_that_share_memory_across_planes_are_refused():
+    """Another cache whose K lies where the source's V does would be written while it is read."""
+    L, vp = B.lib(), C.c_void_p
+    f, small = B.Format(1, 2, 128, 64, 32, 4), B.Format(1, 2, 128, 32, 32, 4)
+    src = B.CacheStruct(f, 0x100000, 0x200000, 0x300000, 0x400000)          # 8192, 512, 8192, 512 bytes
+    good = [0x500000, 0x600000, 0x700000, 0x800000]
+    before = B.launch_count()
+    for i in range(4):
+        for at in (0x100000, 0x200000, 0x300000, 0x400000, 0x101ff0, 0x2001f0, 0x301ff0, 0x4001f0, 0x300000 - 16):
+            planes = good[:i] + [at] + good[i + 1:]
+            dst = B.CacheStruct(small, *planes)
+            assert L.kvbfp_gather_rows(C.byref(src), C.byref(dst), vp(16), 1, 4, vp(16), None, None, None) == B.ERR_INVALID_ARG
+            assert L.kvbfp_evict(C.byref(src), vp(16), vp(0x10000), 16, 4, 4, C.byref(dst), vp(0x20000), vp(16), vp(16), None) == B.ERR_INVALID_ARG
     assert B.launch_count() == before
