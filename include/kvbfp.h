@@ -336,7 +336,7 @@ kvbfp_status kvbfp_evict(const kvbfp_cache* src, const int32_t* seq_lens, const 
  * Moves listed rows together in all four planes: row src_base[b] + index[b, h, i] of src becomes row dst_base[b] + i
  * of dst, i < count[b].  With src = dst and both bases the context length this commits the accepted branch of a
  * drafted tree.
- *   index     [batch, index_heads, n_index] i32, index_heads 1 (all heads alike) or n_kv_heads; in place no source
+ *   index     [batch, index_heads, n_index] i32, n_index <= 2^30, index_heads 1 (all heads alike) or n_kv_heads; in place no source
  *             row may lie below its destination
  *   count     [batch] i32, read clamped to [0, n_index];  src_base, dst_base [batch] i32 or NULL (0)
  *   dst       as in kvbfp_evict

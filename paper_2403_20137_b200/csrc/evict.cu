@@ -370,6 +370,7 @@ extern "C" kvbfp_status kvbfp_gather_rows(const kvbfp_cache* src, const kvbfp_ca
     using namespace kvbfp;
     MoveArgs a = {};
     if (!index || !count || n_index < 1) return KVBFP_ERR_INVALID_ARG;
+    if (n_index > 1 << 30) return KVBFP_ERR_UNSUPPORTED;      // (move_rows counts in 32 bits, a chunk past the end)
     kvbfp_status st = set_caches(src, dst, &a);
     if (st != KVBFP_OK) return st;
     if (index_heads != 1 && index_heads != src->fmt.n_kv_heads) return KVBFP_ERR_INVALID_ARG;

@@ -212,3 +212,11 @@ def test_caches_that_share_memory_across_planes_are_refused():
             assert L.kvbfp_gather_rows(C.byref(src), C.byref(dst), vp(16), 1, 4, vp(16), None, None, None) == B.ERR_INVALID_ARG
             assert L.kvbfp_evict(C.byref(src), vp(16), vp(0x10000), 16, 4, 4, C.byref(dst), vp(0x20000), vp(16), vp(16), None) == B.ERR_INVALID_ARG
     assert B.launch_count() == before
+
+
+def test_index_lists_past_two_to_the_thirty_are_refused():
+    """The kernel counts rows of a list in 32 bits, 128 at a time."""
+    L, vp = B.lib(), C.c_void_p
+    src = B.CacheStruct(B.Format(1, 2, 128, 64, 32, 4), 0x100000, 0x200000, 0x300000, 0x400000)
+    for n in ((1 << 30) + 1, (1 << 31) - 1):
+        assert L.kvbfp_gather_rows(C.byref(src), C.byref(src), vp(16), 1, n, vp(16), None, None, None) == B.ERR_UNSUPPORTED
