@@ -437,7 +437,11 @@ def evict(cache, seq_lens, mass, budget, n_sink=0, n_recent=0, dst=None, dst_mas
     place, in cache and mass."""
     f = cache.fmt
     if dst is None:
+        if dst_mass is not None and dst_mass is not mass:
+            raise ValueError("dst_mass: in place (no dst) the weights move inside mass")
         dst, dst_mass = cache, mass
+    elif dst_mass is None:
+        raise ValueError("dst_mass: another cache needs weights of its own")
     d = dst.fmt
     if kept is None:
         kept = _empty((f.batch, f.n_kv_heads, budget), torch.int32, mass.device, stream)

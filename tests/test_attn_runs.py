@@ -220,3 +220,13 @@ def test_index_lists_past_two_to_the_thirty_are_refused():
     src = B.CacheStruct(B.Format(1, 2, 128, 64, 32, 4), 0x100000, 0x200000, 0x300000, 0x400000)
     for n in ((1 << 30) + 1, (1 << 31) - 1):
         assert L.kvbfp_gather_rows(C.byref(src), C.byref(src), vp(16), 1, n, vp(16), None, None, None) == B.ERR_UNSUPPORTED
+
+
+def test_evict_takes_both_destinations_or_none():
+    """Weights of their own without a cache of their own were left empty, and the given ones overwritten, without a word."""
+    cache, small = (B.Cache(1, 2, D, n, 32, 4, device="cpu") for n in (64, 32))
+    lens, mass, other = torch.zeros(1, dtype=torch.int32), torch.zeros(1, 2, 64), torch.zeros(1, 2, 32)
+    with pytest.raises(ValueError, match="dst_mass"):
+        B.evict(cache, lens, mass, 16, dst_mass=other)
+    with pytest.raises(ValueError, match="dst_mass"):
+        B.evict(cache, lens, mass, 16, dst=small)
