@@ -104,6 +104,165 @@ def test_channel_table_is_read_before_the_last_barrier_of_a_run():
     assert code.index(sync, write) < read < code.rindex(sync, write, end)
 
 
+ALL_FMT = [(bits, block) for bits in (4, 6, 8) for block in (16, 32, 64, 128)]
+
+
+def check_long(got, out, amp, reach, max_seq, cap=0.0, lean=0.0):
+    """The bound of check() with what it leaves out: a sum over S tokens has S / 16 steps of O that cut (2^-23 each) and
+    S / 8 additions of weights (2^-24 each), S 2^-26 in all; a bias of up to `lean` is rounded four times; each of some
+    ten moves of the reference rounds sums twice.  Weights of fp32 queries: three bf16 terms, 2^-24 and twice 2^-22 of exp2."""
+    d = 24 * 2.0 ** -23 * reach + cap * 2.0 ** -21 + lean * 2.0 ** -22
+    w = (2.0 ** -8 if got.dtype == torch.bfloat16 else 2.0 ** -20) + max_seq * 2.0 ** -26 + 2.0 ** -19
+    bound = amp * (2 * d[..., None] + w) * 1.01 + 2.0 ** (-8 if got.dtype == torch.bfloat16 else -24) * out.abs() * 1.01 + 1e-35
+    worst = float(((got.double() - out).abs() / bound).max())
+    assert bool(torch.isfinite(got).all()) and worst <= 1.0, f"error is {worst:.3g} of the bound"
+
+
+def all_mods(batch, heads, lens, cap=25.0):
+    """Cap, bias, window, document and prefix at once; -> the mod and the largest bias."""
+    slopes = torch.linspace(0.0, 0.01, heads, device="cuda")
+    mod = B.ScoreMod(softcap=cap, slopes=slopes, window=1500, first=(lens // 5).contiguous(),
+                     prefix=torch.arange(batch, dtype=torch.int32, device="cuda") * 3)
+    return mod, 0.01 * int(lens.max())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("modified", [False, True])
+@pytest.mark.parametrize("bits,block", ALL_FMT)
+@pytest.mark.parametrize("T,group", [(16, 1), (7, 4), (16, 4), (33, 2)])
+def test_wide_trees_over_many_runs(T, group, bits, block, modified):
+    """Every instance of the wide kernel with some ten tiles a worker: stages and barriers used over and over, sums
+    carried over tiles while their references rise, runs that begin and end inside (sequence, head) pairs."""
+    batch, heads, max_seq = 64, 8, 2080
+    cache, perm, perm_v, q, lens = long_case(20 + T, batch, heads, group, max_seq, T, torch.bfloat16, bits, block)
+    drafts = torch.tensor([max(0, T - b % 5) for b in range(batch)], dtype=torch.int32, device="cuda")
+    mask, depth = trees(batch, T, drafts, 21)
+    mod, lean = all_mods(batch, heads * group, lens) if modified else (B.ScoreMod(), 0.0)
+    kw = dict(draft_lens=drafts, tree_mask=mask, depth=depth, perm_k=perm, inv_perm_v=inverse(perm_v), mod=mod)
+    got = B.tree_attn(cache, q, lens, **kw)
+    ref = wide_reference(cache, q, lens, perm, perm_v, mod, drafts=drafts, mask=mask, depth=depth)
+    check_long(got, *ref, max_seq, cap=mod.softcap, lean=lean)
+    for b in range(5):
+        assert bool((got[b, max(0, T - b):] == 0).all())
+    assert torch.equal(B.tree_attn(cache, q, lens, **kw), got) and B.device_status() == 0
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("modified", [False, True])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("bits,block", ALL_FMT)
+@pytest.mark.parametrize("T,group", [(1, 1), (1, 5), (4, 2), (3, 4)])
+def test_narrow_calls_over_many_runs(T, group, bits, block, dtype, modified):
+    """The same for the narrow kernel (and 12 bf16 rows): single tokens and small trees, some ten tiles a warp."""
+    batch, heads, max_seq = 64, 8, 4112 if bits == 4 else 2064
+    cache, perm, perm_v, q, lens = long_case(30 + T, batch, heads, group, max_seq, T, dtype, bits, block)
+    mod, lean = all_mods(batch, heads * group, lens) if modified else (B.ScoreMod(), 0.0)
+    kw = dict(perm_k=perm, inv_perm_v=inverse(perm_v), mod=mod)
+    if T == 1:
+        call = lambda: B.decode_attn_mod(cache, q[:, 0].contiguous(), lens, **kw)[:, None]
+        ref = wide_reference(cache, q, lens, perm, perm_v, mod)
+    else:
+        drafts = torch.full((batch,), T, dtype=torch.int32, device="cuda")
+        mask, depth = trees(batch, T, drafts, 31)
+        call = lambda: B.tree_attn(cache, q, lens, tree_mask=mask, depth=depth, **kw)
+        ref = wide_reference(cache, q, lens, perm, perm_v, mod, drafts=drafts, mask=mask, depth=depth)
+    got = call()
+    check_long(got, *ref, max_seq, cap=mod.softcap, lean=lean)
+    assert torch.equal(call(), got) and B.device_status() == 0
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("bits,block", [(4, 32), (6, 16), (8, 128)])
+@pytest.mark.parametrize("group,modified", [(1, False), (4, True)])
+def test_weights_over_many_runs(bits, block, group, modified, dtype):
+    """Attention weights where every warp has several tiles, added to what is there; their sum is the number of heads."""
+    batch, heads, max_seq = 64, 8, 4112 if bits == 4 else 2064
+    cache, perm, perm_v, q, lens = long_case(40, batch, heads, group, max_seq, 1, dtype, bits, block)
+    mod, lean = all_mods(batch, heads * group, lens) if modified else (B.ScoreMod(), 0.0)
+    mass = torch.rand(batch, heads, max_seq, device="cuda")
+    before, w = mass.clone(), torch.zeros(batch, heads, max_seq, dtype=torch.float64, device="cuda")
+    q1 = q[:, 0].contiguous()
+    got = B.decode_attn_mass(cache, q1, lens, mass, mod=mod, perm_k=perm, inv_perm_v=inverse(perm_v))
+    ref = wide_reference(cache, q, lens, perm, perm_v, mod, weights=w)
+    check_long(got[:, None], *ref, max_seq, cap=mod.softcap, lean=lean)
+    assert torch.equal(got, B.decode_attn_mod(cache, q1, lens, mod, perm_k=perm, inv_perm_v=inverse(perm_v)))
+    # a weight: twice the score's error, exp2 twice, the sum (S 2^-27 and the moves of the reference); a rounding per addition
+    d = 24 * 2.0 ** -23 * float(ref[2].max()) + mod.softcap * 2.0 ** -21 + lean * 2.0 ** -22
+    bound = w * (2 * d + 2.0 ** -19 + max_seq * 2.0 ** -27) + (group + 1) * 2.0 ** -24 * (mass.double() + w) + 1e-30
+    assert bool(((mass.double() - before.double() - w).abs() <= bound).all())
+    assert torch.equal(mass[w == 0], before[w == 0]) and B.device_status() == 0
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T,group", [(12, 1), (10, 2), (20, 2), (17, 4)])
+def test_non_finite_queries_of_wide_trees_stay_in_their_rows(T, group):
+    """More than eight rows: each width of the wide kernel."""
+    cache, perm, perm_v, q, _ = long_case(50, 2, 2, group, 416, T, torch.bfloat16, 4, 32)
+    lens = i32(380, 200)
+    clean = B.tree_attn(cache, q, lens, perm_k=perm, inv_perm_v=inverse(perm_v))
+    bad = q.clone()
+    bad[0, 3, 0, 17] = float("nan")
+    bad[1, T - 1, 2 * group - 1, 90] = float("inf")
+    bad[1, 5, 0, 2] = -float("inf")
+    got = B.tree_attn(cache, bad, lens, perm_k=perm, inv_perm_v=inverse(perm_v))
+    rows = torch.zeros(2, T, 2 * group, dtype=torch.bool)
+    rows[0, 3, 0] = rows[1, T - 1, 2 * group - 1] = rows[1, 5, 0] = True
+    assert torch.equal(got[~rows], clean[~rows]) and bool(torch.isnan(got[rows]).all())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("bits,block", [(4, 32), (6, 16), (6, 128), (8, 32)])
+@pytest.mark.parametrize("T,group", [(3, 1), (12, 1), (9, 3), (20, 3)])
+@pytest.mark.parametrize("power", [113, -95])
+def test_cached_magnitudes_at_the_ends_of_the_range(power, T, group, bits, block, dtype):
+    """Keys and values around 2^113 (loud channels near 2^117) and 2^-95, each width; the scale makes up for the keys."""
+    g = torch.Generator(device="cuda").manual_seed(60 + T)
+    s = 2.0 ** power
+    k, v = (torch.randn(2, 304, 2, D, generator=g, device="cuda") * s for _ in range(2))
+    k[..., [3, 77, 120]] *= 3.0
+    cache = B.Cache(2, 2, D, 304, block, bits)
+    B.append(cache, k, v, i32(0, 0))
+    q = torch.randn(2, T, 2 * group, D, generator=g, device="cuda").to(dtype)
+    lens, drafts, scale = i32(280, 130), i32(T, T), 2.0 ** -power / math.sqrt(D)
+    mask, depth = trees(2, T, drafts, 61)
+    got = B.tree_attn(cache, q, lens, tree_mask=mask, depth=depth, softmax_scale=scale)
+    out, amp, reach = wide_reference(cache, q, lens, None, None, B.ScoreMod(), scale=scale, drafts=drafts, mask=mask, depth=depth)
+    check(got / s, out / s, amp / s, reach)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("bits,block", ALL_FMT)
+@pytest.mark.parametrize("T", [1, 5])
+@pytest.mark.parametrize("top", [4.0, 0.06])
+def test_fp32_queries_keep_every_bit(top, T, bits, block):
+    """Queries with one channel and keys that are powers of two in it: the product is exact in three bf16 terms (two
+    would lose 2^-18 of it), so the scores' error is that of three fp32 roundings; weights in three terms.  Bound: a score
+    is off by 4 x 2^-24 of the largest, exp2 by 2^-22 in weight and sum, sums and third terms by 2^-22 in all."""
+    g = torch.Generator(device="cuda").manual_seed(80 + T)
+    n = 40
+    k = torch.zeros(4, 48, 2, D, device="cuda")
+    k[..., 9] = torch.tensor([1.0, -1.0, 2.0, -2.0, 0.5], device="cuda").repeat(10)[:48][None, :, None]
+    v = torch.randn(4, 48, 2, D, generator=g, device="cuda")
+    cache = B.Cache(4, 2, D, 48, block, bits)
+    B.append(cache, k, v, i32(0, 0, 0, 0))
+    q = torch.zeros(4, T, 6, D, device="cuda")
+    q[..., 9] = (torch.rand(4, T, 6, generator=g, device="cuda") * 0.5 + 0.5) * (top / 2)
+    lens = i32(n, 2, 3, 1)
+    if T == 1:
+        got = B.decode_attn_mod(cache, q[:, 0].contiguous(), lens, None, softmax_scale=1.0)[:, None]
+        out, amp, _ = wide_reference(cache, q, lens, None, None, B.ScoreMod(), scale=1.0)
+    else:
+        drafts = i32(T, T, T, T)
+        mask, depth = trees(4, T, drafts, 81, chain=True)
+        got = B.tree_attn(cache, q, lens, softmax_scale=1.0)
+        out, amp, _ = wide_reference(cache, q, lens, None, None, B.ScoreMod(), scale=1.0, drafts=drafts, mask=mask, depth=depth)
+    bound = amp * (2 * 4 * 2.0 ** -24 * top + 2 * 2.0 ** -22 + 2.0 ** -22) + 2.0 ** -24 * out.abs() + 1e-35
+    worst = float(((got.double() - out).abs() / bound).max())
+    assert worst <= 1.0, f"error is {worst:.3g} of the bound"
+
+
 # ----------------------------------------------------------------------------------------------- caps of any size
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
