@@ -332,7 +332,7 @@ __global__ void __launch_bounds__(kAttnWarps * 32, attn_rows_blocks(!F32)) attn_
     for (int s = 0; s < STAGES && issued < n_mine; ++s) issue();
 
     const int R = a.n_draft * a.group;
-    const float up = a.scale * kValueUp, to_log2 = 1.4426950408889634f, plain = up * to_log2;
+    const float up = a.scale * kValueUp, to_log2 = 1.4426950408889634f, plain = finite_factor(up * to_log2);
     const float cap_in = a.softcap > 0.f ? finite_factor(up / a.softcap) : 0.f;
     // lane offsets inside a 16-token group: K rows of column g in both score tiles, V rows of the lane's four k positions
     int ko[2], ke[2], vo[4], ve[4];

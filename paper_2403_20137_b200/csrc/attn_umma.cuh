@@ -567,7 +567,7 @@ __global__ void __launch_bounds__(UGeo<P, N>::THREADS, 1) attn_umma(const AttnAr
                 // ---- scores
                 const uint32_t tm_s = tmt + G_::TM_S + (it & 1) * N + half * C;
                 const int tt = tile_token(sv, k, kUTile);
-                float mul = up * to_log2 * __uint_as_float(k_top << 23);
+                float mul = finite_factor(up * to_log2 * __uint_as_float(k_top << 23));
                 uint32_t raw[C];
                 if (KEEP) {
                     tmem_ld<C>(tm_s, raw);
@@ -577,7 +577,7 @@ __global__ void __launch_bounds__(UGeo<P, N>::THREADS, 1) attn_umma(const AttnAr
                     const float in = finite_factor(cap_in * __uint_as_float(k_top << 23));
                     mul = a.softcap * to_log2;
                     if (a.softcap > kCapFast) {
-                        const float to_x = up * __uint_as_float(k_top << 23), inv_cap = 1.f / a.softcap;      // (in two steps: their product may be too small)
+                        const float to_x = finite_factor(up * __uint_as_float(k_top << 23)), inv_cap = 1.f / a.softcap;      // (in two steps: their product may be too small)
                         change_scores<C>(tm_s, raw, [&](float y, int) { return tanh_relative(y * to_x * inv_cap); });
                     } else {
                         change_scores<C>(tm_s, raw, [&](float y, int) { return fmaf(-2.f, rcp_approx(1.f + ex2_approx(y * in)), 1.f); });      // tanh x = 1 - 2 / (1 + e^2x): about 2e-7 absolute

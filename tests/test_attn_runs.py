@@ -233,6 +233,25 @@ def test_cached_magnitudes_at_the_ends_of_the_range(power, T, group, bits, block
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("cap", [0.0, 1e6])
+@pytest.mark.parametrize("T", [3, 12, 40])
+@pytest.mark.parametrize("power,scale", [(100, 2.0 ** 60), (0, 3e38)])
+def test_scores_of_zero_stay_zero_under_any_scale(power, scale, T, cap, dtype):
+    """The scale times the cached magnitudes may leave the fp32 range: rows of zeros weigh all they see alike."""
+    g = torch.Generator(device="cuda").manual_seed(90)
+    k, v = (torch.randn(2, 288, 2, D, generator=g, device="cuda") for _ in range(2))
+    cache = B.Cache(2, 2, D, 288, 32, 4)
+    B.append(cache, k * 2.0 ** power, v, i32(0, 0))
+    q = torch.zeros(2, T, 2, D, device="cuda", dtype=dtype)
+    mod, lens, drafts = B.ScoreMod(softcap=cap), i32(200, 7), i32(T, T)
+    mask, depth = trees(2, T, drafts, 8, chain=True)
+    got = B.tree_attn(cache, q, lens, mod=mod, softmax_scale=scale)
+    out, amp, reach = wide_reference(cache, q, lens, None, None, mod, scale=scale, drafts=drafts, mask=mask, depth=depth)
+    check(got, out, amp, reach)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("bits,block", ALL_FMT)
 @pytest.mark.parametrize("T", [1, 5])
 @pytest.mark.parametrize("top", [4.0, 0.06])
