@@ -286,7 +286,9 @@ size_t kvbfp_attn_workspace_bytes(const kvbfp_format* fmt, int32_t n_q_heads, in
  * n_q_heads, perm_k, inv_perm_v, softmax_scale as in kvbfp_decode_attn.  bf16 queries are used exactly, softmax
  * weights are rounded to bf16 for the product with V and the output to bf16; fp32 queries give fp32 accuracy (slower).
  * Sums, maxima and scores are fp32 in both.  With bf16 queries cached magnitudes of 2^118 and above are out of range
- * (results unspecified), and rows of magnitudes below 2^-100 may count as zeros.  Lengths beyond the cache are read clamped and set KVBFP_FLAG_POSITION.
+ * (results unspecified).  Blocks of magnitudes below 2^-100 may count as zeros; with more than eight bf16 rows per kv head
+ * a cached value counts to within 2^-120 of the largest of its row.  Lengths beyond the cache are read clamped and set
+ * KVBFP_FLAG_POSITION.
  * The result does not depend on anything but the arguments (no atomics).
  */
 kvbfp_status kvbfp_tree_attn(const kvbfp_cache* cache, const void* q, kvbfp_dtype dt, int32_t n_q_heads,

@@ -104,23 +104,26 @@ __global__ void __launch_bounds__(128) umma_prep(const AttnArgs a) {
 // steps.  One bf16x2 fma turns two of them into (field - offset) times the block's weight, exactly; nothing is or-ed
 // under an exponent and fields need no shift to bit 0, which takes a third of the integer instructions out (the integer
 // pipe bounds the conversion).  For the multiplier 2^133 to stay in range the weights are relative to the row's largest
-// exponent E (2^-8 for the block that has it, down to 2^-108); 2^E comes back as a factor per token: on the scores for K,
+// exponent E (2^-8 for the block that has it, down to bf16's last step); 2^E comes back as a factor per token: on the scores for K,
 // on the weights P for V.
 struct UW {
     uint32_t s, s2, c;      // multipliers of fields at bit 0 and higher up, -offset * weight
 };
-// Weights of two blocks, `below` (16-bit halves) steps of two below the row's largest exponent.
+// Weights of two blocks, `below` (16-bit halves) steps of two below the row's largest exponent.  The other two are products
+// of the first, so that far below (from 125 steps on, where no bf16 number is left) all three run out into zeros together.
 template <int P>
 __device__ __forceinline__ void umma_weights(uint32_t below, UW& a, UW& b) {
     uint32_t d;
-    asm("min.s16x2 %0, %1, %2;" : "=r"(d) : "r"(below), "r"(100u * 0x00010001u));
-    const uint32_t s = 0x7E007E00u - d * 0x80u;                                      // 2^(133 - 8 - d)
+    asm("min.s16x2 %0, %1, %2;" : "=r"(d) : "r"(below), "r"(252u * 0x00010001u));
+    const uint32_t s = 0x7E007E00u - d * 0x80u;                                      // 2^(133 - 8 - d), 0 at 252
+    const uint32_t s2 = mul_bf16x2(s, P == 4 ? 0x3D803D80u : 0x3E803E80u);           // / 16, / 4
+    const uint32_t c = mul_bf16x2(s, P == 4 ? 0x80088008u : P == 6 ? 0x80208020u : 0x80808080u);      // -8, -32, -128 times 2^-133
     a.s = prmt(s, 0u, 0x1010u);
     b.s = prmt(s, 0u, 0x3232u);
-    a.s2 = a.s - (P == 4 ? 0x02000200u : 0x01000100u);                               // / 16, / 4
-    b.s2 = b.s - (P == 4 ? 0x02000200u : 0x01000100u);
-    a.c = a.s + (P == 4 ? 0x3F003F00u : P == 6 ? 0x40004000u : 0x41004100u);         // -8, -32, -128 times 2^(-8 - d)
-    b.c = b.s + (P == 4 ? 0x3F003F00u : P == 6 ? 0x40004000u : 0x41004100u);
+    a.s2 = prmt(s2, 0u, 0x1010u);
+    b.s2 = prmt(s2, 0u, 0x3232u);
+    a.c = prmt(c, 0u, 0x1010u);
+    b.c = prmt(c, 0u, 0x3232u);
 }
 __device__ __forceinline__ uint32_t max_s16x2(uint32_t a, uint32_t b) {
     uint32_t d;

@@ -252,6 +252,39 @@ def test_scores_of_zero_stay_zero_under_any_scale(power, scale, T, cap, dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("bits", [4, 6, 8])
+@pytest.mark.parametrize("T,group", [(5, 1), (12, 1), (10, 2), (20, 2)])
+@pytest.mark.parametrize("gap", [60, 99, 110, 140])
+def test_blocks_far_apart_inside_a_row(gap, T, group, bits):
+    """Rows whose first block is 2^gap above the others.  A cached value counts to within 2^-120 of its row's largest: the
+    small blocks' outputs are right up to there, and smaller than that behind it."""
+    g = torch.Generator(device="cuda").manual_seed(70 + T)
+    k, v = (torch.randn(2, 304, 2, D, generator=g, device="cuda") for _ in range(2))
+    high = 2.0 ** (gap // 2)
+    low = high / 2.0 ** gap
+    v[..., :32] *= high
+    v[..., 32:] *= low
+    k[..., :32] = 0.0
+    k[..., 32:] *= low
+    k[..., 0] = high                                    # no query looks at it
+    cache = B.Cache(2, 2, D, 304, 32, bits)
+    B.append(cache, k, v, i32(0, 0))
+    q = torch.randn(2, T, 2 * group, D, generator=g, device="cuda").bfloat16()
+    q[..., :32] = 0.0
+    lens, drafts, scale = i32(280, 130), i32(T, T), 1.0 / low / math.sqrt(D)
+    mask, depth = trees(2, T, drafts, 61)
+    if gap > 120:                                       # the small blocks do not count: all scores are 0 then
+        q.zero_()
+    got = B.tree_attn(cache, q, lens, tree_mask=mask, depth=depth, softmax_scale=scale)
+    out, amp, reach = wide_reference(cache, q, lens, None, None, B.ScoreMod(), scale=scale, drafts=drafts, mask=mask, depth=depth)
+    check(got[..., :32] / high, out[..., :32] / high, amp[..., :32] / high, reach)
+    if gap > 120:
+        assert float(got[..., 32:].abs().max()) <= 2.0 ** -120 * float(v.abs().max()) + 1.01 * float(amp[..., 32:].max())
+    else:
+        check(got[..., 32:] / low, out[..., 32:] / low, amp[..., 32:] / low, reach)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("bits,block", ALL_FMT)
 @pytest.mark.parametrize("T", [1, 5])
 @pytest.mark.parametrize("top", [4.0, 0.06])
