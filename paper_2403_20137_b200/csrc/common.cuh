@@ -66,6 +66,8 @@ inline size_t row_e_bytes(const kvbfp_format& f) { return (size_t)(f.head_dim / 
 // predecessor) and pdl_trigger() after it, so that at most one kernel waits behind the running one and its blocks
 // never compete with blocks of the running kernel that have not started yet: the short kernels right after the
 // wait, the persistent decode kernels at their end (waiting blocks on an SM slow its streaming warps down).
+// What the kernel before wrote is read by plain loads: read-only ones (__ldg, const __restrict__) are taken to read what
+// never changes, so that they may be moved above the wait.
 __device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void pdl_trigger() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 

@@ -15,7 +15,7 @@ namespace {
 // SPLIT: a thread block per row, its four warps take every fourth partial and their results are merged through
 // shared memory (rows with many partials: long sequences cut into many ranges); else four rows per thread block.
 template <bool SPLIT>
-__global__ void __launch_bounds__(128) lse_merge(const float* __restrict__ partials, const int32_t* __restrict__ seq_lens,
+__global__ void __launch_bounds__(128) lse_merge(const float* partials, const int32_t* __restrict__ seq_lens,
                                                  const int32_t* __restrict__ inv_perm_v, float* __restrict__ out,
                                                  int n_rows, int n_q_heads, int group, int n_chunks, int chunk,
                                                  int len_cap, int n_warps, int item_tokens, int items_per_pair,

@@ -429,7 +429,7 @@ __device__ __forceinline__ int warp_max_byte(const uint8_t* p, int bytes, int la
 // instead of the query heads (see make_qfrag4h), in the scores and in P.V.
 template <int N, int NT, bool MHA>
 __global__ void __launch_bounds__(kWarps * 32, MHA ? kMinCtasSingle : (NT == 1 ? kMinCtas : 2))
-decode_mma4(DecodeArgs a, const int32_t* __restrict__ qmeta, const __grid_constant__ CUtensorMap k_map,
+decode_mma4(DecodeArgs a, const int32_t* qmeta, const __grid_constant__ CUtensorMap k_map,
             const __grid_constant__ CUtensorMap v_map) {
     using G_ = Geo4<N>;
     constexpr int ROW_E = G_::ROW_E;
@@ -599,7 +599,7 @@ decode_mma4(DecodeArgs a, const int32_t* __restrict__ qmeta, const __grid_consta
                     const uint4* s8 = src + (((int64_t)cr.b * Hkv + cr.hk) * NT + nt) * (2 * 32);
 #pragma unroll
                     for (int j = 0; j < 2; ++j) {
-                        const uint4 v = __ldg(s8 + j * 32 + lane);
+                        const uint4 v = s8[j * 32 + lane];
                         qi8[nt][4 * j] = v.x; qi8[nt][4 * j + 1] = v.y; qi8[nt][4 * j + 2] = v.z; qi8[nt][4 * j + 3] = v.w;
                     }
                     const int qn = 4 * nt + t;
@@ -615,7 +615,7 @@ decode_mma4(DecodeArgs a, const int32_t* __restrict__ qmeta, const __grid_consta
                     const uint4* s16 = src + (((int64_t)cr.b * Hkv + cr.hk) * NT + nt) * (4 * 32);
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        const uint4 v = __ldg(s16 + j * 32 + lane);
+                        const uint4 v = s16[j * 32 + lane];
                         qf[nt][2 * j] = make_uint2(v.x, v.y);
                         qf[nt][2 * j + 1] = make_uint2(v.z, v.w);
                     }

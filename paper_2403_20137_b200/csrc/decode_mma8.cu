@@ -156,7 +156,7 @@ struct Geo8 {
 __device__ __forceinline__ int tok8(int t, int k) { return 2 * t + (k & 1) + 4 * (k & 2); }
 
 template <int N, int NT>
-__global__ void __launch_bounds__(kWarps * 32, 3) decode_mma8(DecodeArgs a, const int32_t* __restrict__ qmeta,
+__global__ void __launch_bounds__(kWarps * 32, 3) decode_mma8(DecodeArgs a, const int32_t* qmeta,
                                                               const __grid_constant__ CUtensorMap k_map,
                                                               const __grid_constant__ CUtensorMap v_map) {
     pdl_wait();
@@ -293,7 +293,7 @@ __global__ void __launch_bounds__(kWarps * 32, 3) decode_mma8(DecodeArgs a, cons
                 const uint4* s8 = src + (((int64_t)cr.b * Hkv + cr.hk) * NT + nt) * (2 * 32);
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
-                    const uint4 v = __ldg(s8 + j * 32 + lane);
+                    const uint4 v = s8[j * 32 + lane];
                     qi8[nt][4 * j] = v.x; qi8[nt][4 * j + 1] = v.y; qi8[nt][4 * j + 2] = v.z; qi8[nt][4 * j + 3] = v.w;
                 }
 #pragma unroll
