@@ -382,6 +382,34 @@ def test_hidden_tokens_keep_their_weights_whatever_the_query(bad, bits, dtype):
     assert B.device_status() == 0
 
 
+# ----------------------------------------------------------------------------------------------- the smallest calls
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("bits,block", ALL_FMT)
+@pytest.mark.parametrize("group", [1, 8])
+def test_caches_of_one_group_of_tokens(bits, block, group, dtype):
+    """One head of 16 tokens, less than any tile: trees that fill it, single tokens, weights, eviction to one row."""
+    g = torch.Generator(device="cuda").manual_seed(100)
+    k, v = (torch.randn(1, 16, 1, D, generator=g, device="cuda") for _ in range(2))
+    cache = B.Cache(1, 1, D, 16, block, bits)
+    B.append(cache, k, v, i32(0))
+    q = torch.randn(1, 16, group, D, generator=g, device="cuda").to(dtype)
+    for n, T in ((0, 1), (0, 16), (3, 13), (15, 1), (7, 2)):
+        qt, drafts = q[:, :T].contiguous(), i32(T)
+        mask, depth = trees(1, T, drafts, 101)
+        got = B.tree_attn(cache, qt, i32(n), tree_mask=mask, depth=depth)
+        check(got, *wide_reference(cache, qt, i32(n), None, None, B.ScoreMod(), drafts=drafts, mask=mask, depth=depth))
+    for n in (1, 16):
+        q1, mass, w = q[:, 0].contiguous(), torch.zeros(1, 1, 16, device="cuda"), torch.zeros(1, 1, 16, dtype=torch.float64, device="cuda")
+        got = B.decode_attn_mass(cache, q1, i32(n), mass)
+        check(got[:, None], *wide_reference(cache, q[:, :1], i32(n), None, None, B.ScoreMod(), weights=w))
+        assert float((mass - w).abs().max()) <= 1e-5 * group
+    keep = int(mass[0, 0].argmax())
+    kept, new = B.evict(cache, i32(16), mass, 1)
+    assert kept.tolist() == [[[keep]]] and new.tolist() == [1]
+    assert B.device_status() == 0
+
+
 # ----------------------------------------------------------------------------------------------- refusals
 def test_queries_of_another_rank_are_refused():
     """One token's queries given as a tree's would be read far past their end, a tree's as one token's in part."""
