@@ -410,6 +410,38 @@ def test_caches_of_one_group_of_tokens(bits, block, group, dtype):
     assert B.device_status() == 0
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("bits", [4, 6, 8])
+def test_trees_far_into_a_long_cache(bits):
+    """Offsets past 32 bits in every width of tree and with weights: the second head's rows lie 3 GB and more into a plane,
+    its last ones more than twice that."""
+    H, S = 2, (1 << 25) + (1 << 24)
+    n = S - 80
+    g = torch.Generator(device="cuda").manual_seed(110)
+    k, v = (torch.randn(1, 304, H, D, generator=g, device="cuda") for _ in range(2))
+    small, cache = B.Cache(1, H, D, 304, 32, bits), B.Cache(1, H, D, S, 32, bits)
+    B.append(small, k, v, i32(0))
+    index = torch.arange(304, dtype=torch.int32, device="cuda")[None].contiguous()
+    B.gather_rows(small, index, i32(304), dst=cache, dst_base=i32(n - 264))
+    assert H * S * cache.fmt.row_m > 1 << 32
+    mod = B.ScoreMod(window=250)
+    for T, group, dtype in ((3, 2, torch.bfloat16), (12, 1, torch.bfloat16), (10, 3, torch.bfloat16), (20, 3, torch.bfloat16),
+                            (5, 2, torch.float32)):
+        q, drafts = torch.randn(1, T, H * group, D, generator=g, device="cuda").to(dtype), i32(T)
+        mask, depth = trees(1, T, drafts, 111)
+        got = B.tree_attn(cache, q, i32(n), tree_mask=mask, depth=depth, mod=mod)
+        want = B.tree_attn(small, q, i32(264), tree_mask=mask, depth=depth, mod=mod)
+        ref = wide_reference(small, q, i32(264), None, None, mod, drafts=drafts, mask=mask, depth=depth)
+        check(got, *ref)
+        check(want, *ref)
+    q1 = q[:, 0].contiguous()
+    mass, few = torch.zeros(1, H, S, device="cuda"), torch.zeros(1, H, 304, device="cuda")
+    B.decode_attn_mass(cache, q1, i32(n), mass, mod=mod)
+    B.decode_attn_mass(small, q1, i32(264), few, mod=mod)
+    assert float((mass[:, :, n - 264:n + 40] - few).abs().max()) <= 1e-6 * 2
+    assert float(mass[:, :, :n - 264].abs().max()) == 0.0 and B.device_status() == 0
+
+
 # ----------------------------------------------------------------------------------------------- refusals
 def test_queries_of_another_rank_are_refused():
     """One token's queries given as a tree's would be read far past their end, a tree's as one token's in part."""
