@@ -299,7 +299,9 @@ kvbfp_status kvbfp_tree_attn(const kvbfp_cache* cache, const void* q, kvbfp_dtyp
 
 /*
  * kvbfp_decode_attn with modified scores: q [batch, n_q_heads, head_dim] of `dt` is the last cached token, at position
- * seq_lens[b] - 1; out is of `dt`.  Cached tokens that the window hides from every query are not read.
+ * seq_lens[b] - 1; out is of `dt`.  Cached tokens that the window hides from every query are not read.  Types, range and
+ * accuracy are those of kvbfp_tree_attn: with bf16 queries the weights and the output are rounded to bf16, fewer bits than
+ * kvbfp_decode_attn keeps of the same queries; fp32 queries give fp32 accuracy.
  */
 kvbfp_status kvbfp_decode_attn_mod(const kvbfp_cache* cache, const void* q, kvbfp_dtype dt, int32_t n_q_heads,
                                    const int32_t* seq_lens, const int32_t* perm_k, const int32_t* inv_perm_v,

@@ -31,8 +31,9 @@
 //
 // What bounds it: neither memory (0.44 of the copy rate at 16 rows) nor the tensor cores (7 to 15 % busy) but the warps'
 // instructions and the latency between them: some 700 to 940 a warp and tile, 0.5 to 0.6 issued a cycle by the 12 to 16
-// warps that registers and shared memory allow.  16 x 32 heads of up to 8192 4-bit rows, 16 drafted tokens: 113 us; 8 x 8
-// heads of 32768 rows, 64 query rows: 154 us; 8 x 8 heads of up to 8191 8-bit rows, 256 capped query rows: 165 us.
+// warps that registers and shared memory allow.  16 x 32 heads of up to 8192 4-bit rows, 16 drafted tokens: 119 us; 8 x 8
+// heads of 32768 rows, 64 query rows: 156 us; 8 x 8 heads of up to 8191 8-bit rows, 256 capped query rows: 164 us.
+// (The instances for 64 rows spill 64 to 84 bytes a thread: 18 warps leave 96 registers.)
 // (V^T in tensor memory, filled through transposing loads, halves the shared-memory traffic and was 6 % slower: it costs
 // integer instructions.  Conversion as loops instead of straight code: 2 to 6 % slower.)
 #pragma once

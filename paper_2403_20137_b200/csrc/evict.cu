@@ -24,8 +24,8 @@ __device__ __forceinline__ uint32_t mass_key(float x) {
 // a histogram each in shared memory (the first, where most weights fall into a few bins, in four copies by lane: 95 -> 87
 // us for 16 x 32 x 8192 rows with the move), the cluster's summed through distributed shared memory; of equals to the
 // threshold the lowest positions are kept.  Counting is by integer atomics: the result does not depend on their order.  Each warp owns a contiguous piece of the region, so one scan over the warps' counts
-// places every kept row.  A thread keeps its keys in registers where they fit (CACHED: up to 8192 rows a block) and reads
-// them again otherwise.  What bounds it is the chain of passes, not the bytes (4 per row).
+// places every kept row.  A thread keeps its keys in registers where they fit (CACHED: up to 8192 rows a block; with
+// three blocks an SM some of them spill: 40 registers, 148 bytes) and reads them again otherwise.  What bounds it is the chain of passes, not the bytes (4 per row).
 template <int CS, bool CACHED>
 __global__ void __launch_bounds__(kSelThreads, CS == 1 ? 3 : 1) evict_select(const float* mass, const int32_t* seq_lens, int max_seq, int n_heads,
                                                             int budget, int n_sink, int n_recent, int32_t* kept, uint32_t* status) {
