@@ -720,8 +720,9 @@ __global__ void __launch_bounds__(UGeo<P, N>::THREADS, 1) attn_umma(const AttnAr
                     part[m_pos * kAttnPart + D + 1] = ls;
                 }
             }
-            // (read before the barrier: a warp that is through with its results writes the next head's table)
-            const int ch = a.inv_perm_v ? chan[slot_of] : slot_of;
+            // (read before the barrier: a warp that is through with its results writes the next head's table.  Cut to a channel: of
+            // an inv_perm_v that is no permutation some entries are never written.)
+            const int ch = a.inv_perm_v ? chan[slot_of] & (D - 1) : slot_of;
             wait(b_o(team), it - 1);
             __syncwarp();
             tmem_fence_after();

@@ -442,6 +442,29 @@ def test_trees_far_into_a_long_cache(bits):
     assert float(mass[:, :, :n - 264].abs().max()) == 0.0 and B.device_status() == 0
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("bits", [4, 6, 8])
+@pytest.mark.parametrize("T,group", [(1, 1), (3, 2), (12, 1), (10, 3), (20, 3)])
+def test_orders_that_are_no_permutation_stay_inside_the_output(T, group, bits):
+    """Channel orders that name a channel twice, or none that exists: the results are unspecified, the memory around them is
+    left alone."""
+    cache, _, _, q, lens = long_case(120, 4, 3, group, 416, T, torch.bfloat16, bits, 32)
+    around = torch.full((3, *q.shape), 7.0, dtype=q.dtype, device="cuda")
+    g = torch.Generator(device="cuda").manual_seed(121)
+    for order in (torch.zeros(3, D), torch.full((3, D), -1), torch.full((3, D), 1 << 30),
+                  torch.randint(-2 ** 31, 2 ** 31 - 1, (3, D), generator=g, device="cuda")):
+        order = order.to(torch.int32).cuda()
+        around.fill_(7.0)
+        B.tree_attn(cache, q, lens, perm_k=order, inv_perm_v=order, out=around[1])
+        assert bool((around[0] == 7.0).all()) and bool((around[2] == 7.0).all())
+    assert B.device_status() == 0
+
+
+def test_channel_table_entries_are_cut_to_a_channel():
+    with open(os.path.join(build.CSRC, "attn_umma.cuh")) as f:
+        assert "chan[slot_of] & (D - 1)" in f.read()
+
+
 # ----------------------------------------------------------------------------------------------- refusals
 def test_queries_of_another_rank_are_refused():
     """One token's queries given as a tree's would be read far past their end, a tree's as one token's in part."""
