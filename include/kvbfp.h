@@ -65,7 +65,8 @@ enum {
     KVBFP_FLAG_POSITION = 2u,      /* append: start_pos + n_new beyond max_seq, the sequence's rows are skipped;
                                       decode: a seq_len beyond max_seq is read as max_seq, a negative one as 0 */
     KVBFP_FLAG_LEN_HINT = 4u,      /* a seq_len exceeded max_len_hint: tokens past it unread */
-    KVBFP_FLAG_WAIT_TIMEOUT = 8u   /* an on-chip copy did not complete within its wait bound */
+    KVBFP_FLAG_WAIT_TIMEOUT = 8u,  /* an on-chip copy did not complete within its wait bound */
+    KVBFP_FLAG_PAGES = 16u         /* pages ran out: some sequences (or entries) did not get any */
 };
 
 /* Which decode kernel to run. */
@@ -350,6 +351,129 @@ kvbfp_status kvbfp_evict(const kvbfp_cache* src, const int32_t* seq_lens, const 
 kvbfp_status kvbfp_gather_rows(const kvbfp_cache* src, const kvbfp_cache* dst, const int32_t* index,
                                int32_t index_heads, int32_t n_index, const int32_t* count, const int32_t* src_base,
                                const int32_t* dst_base, void* stream);
+
+/*
+ * Pages (the paper has no counterpart; a server of many users cannot give each the longest cache).  A pool of pages is a
+ * kvbfp_cache whose format counts pages instead of sequences: batch = n_pages, max_seq = page_tokens; kvbfp_dequant and
+ * kvbfp_plane_bytes take it as it is.  One table serves the pools of all layers.
+ *   table  [batch, max_pages] i32: entry i of a sequence is the pool page of its tokens [i * page_tokens, (i+1) * page_tokens);
+ *          -1 (any negative number): none
+ *   refs   [n_pages] i32: table entries that name the page; 0: the page is free
+ *   lens   [batch] i32: tokens of each sequence
+ * page_tokens is a power of two from 16 to 1024.  The struct lives in host memory, the three arrays on the device (16-byte aligned).
+ */
+typedef struct {
+    int32_t batch, max_pages, n_pages, page_tokens;
+    int32_t* table;
+    int32_t* refs;      /* kvbfp_pages_* only; may be NULL elsewhere */
+    int32_t* lens;      /* kvbfp_pages_* only; may be NULL elsewhere */
+} kvbfp_pages;
+
+/*
+ * Gives pages back: those that lie wholly inside tokens [lo[b], hi[b]) of sequence b (the last, partly filled page counts as
+ * whole).  Their entries become -1 and their refs go down by one.  Where hi[b] reaches the sequence's end, the sequence is cut
+ * to lo[b] tokens: a finished sequence (0, max), a rejected tail (len, max), what a sliding window left behind (n_sink,
+ * len - window).
+ *   lo, hi  [batch] i32, or NULL: 0, no limit.  Negative lo is read as 0.
+ */
+kvbfp_status kvbfp_pages_free(const kvbfp_pages* pool, const int32_t* lo, const int32_t* hi, void* stream);
+
+/*
+ * Sequence dst[i] becomes a copy of sequence src[i] that shares its pages (refs go up), i < n.
+ *   src, dst  [n] i32.  dst[i] has to be empty (no pages), named once, and none of src; other pairs are skipped and set
+ *             KVBFP_FLAG_POSITION.  Negative src: the pair is skipped.
+ */
+kvbfp_status kvbfp_pages_fork(const kvbfp_pages* pool, const int32_t* src, const int32_t* dst, int32_t n, void* stream);
+
+/*
+ * Room for more[b] tokens behind each sequence's lens[b]; lens[b] grows by more[b].  New pages are the free pages of the lowest
+ * numbers, dealt out by sequence, then by token.  Where the first new token falls into a page that other entries name too, the
+ * sequence gets a page of its own in its place: pairs[b] = (old page, new page), to be copied by kvbfp_pages_copy in every
+ * layer's pool before it is written.  Of sequences that all write one page in this call and are its only owners the last keeps
+ * it.  When the free pages run out, that sequence and all behind it that need any (or are the last of such owners) are left as
+ * they were, lens[b] too, and KVBFP_FLAG_PAGES is set.  A sequence that passes the table's end gets the pages up to there and
+ * sets KVBFP_FLAG_PAGES; its length grows by more[b] all the same, and the calls that write or read tokens behind the end skip them
+ * (KVBFP_FLAG_POSITION).
+ *   more   [batch] i32, read as 0 where negative
+ *   pairs  [batch, 2] i32 out: (-1, -1) where nothing is to be copied
+ * batch <= 1024.
+ */
+kvbfp_status kvbfp_pages_reserve(const kvbfp_pages* pool, const int32_t* more, int32_t* pairs, void* stream);
+
+/*
+ * Packs the pages in use into the lowest numbers.
+ *   dst    pool itself (same arrays): pages in use behind the first n_used numbers move into the free numbers before them, the
+ *          k-th into the k-th.  Another pool of the same batch, max_pages and page_tokens: all pages in use move there, the
+ *          k-th to number k; its table, refs and lens are written whole.
+ *   moves  [n_pages, 2] i32 out: (from, to) of the pages to be copied by kvbfp_pages_copy, (-1, -1) behind the last
+ *   count  [1] i32 out: number of moves
+ *   workspace  kvbfp_pages_workspace_bytes(pool) bytes
+ * A dst of fewer pages than are in use takes the first ones; entries of the others become -1 and KVBFP_FLAG_PAGES is set.
+ */
+size_t kvbfp_pages_workspace_bytes(const kvbfp_pages* pool);
+kvbfp_status kvbfp_pages_compact(const kvbfp_pages* pool, const kvbfp_pages* dst, int32_t* moves, int32_t* count, void* workspace,
+                                 size_t workspace_bytes, void* stream);
+
+/*
+ * Copies whole pages in all four planes: page pairs[i][0] of src to page pairs[i][1] of dst.
+ *   pairs  [n, 2] i32; pairs with a negative number are skipped, others outside the pools are skipped and set
+ *          KVBFP_FLAG_POSITION.  No page may be the target of two pairs, nor, in place, the source of one and the target of another.
+ *   count  [1] i32 or NULL: only the first *count pairs
+ *   dst    src itself, or a pool of the same geometry (n_pages may differ) that shares no memory with it
+ */
+kvbfp_status kvbfp_pages_copy(const kvbfp_cache* src, const kvbfp_cache* dst, const int32_t* pairs, int32_t n,
+                              const int32_t* count, void* stream);
+
+/*
+ * A ragged batch of new tokens, one behind the other: sequence b has tokens [starts[b], starts[b+1]), the last of its seq_lens[b]
+ * tokens in the cache (so seq_lens counts them).
+ *
+ * kvbfp_norm_rope_append is the step from the projections to the cache: every head of q and k is normalised and rotated, k and
+ * v are cast and stored as kvbfp_append does it.  For channel c of a row x at position pos (all heads of q, or of k, alike):
+ *   y = x / sqrt(mean(x^2) + eps) * weight[c]        (weight NULL: y = x)
+ *   pairs (y_a, y_b) turn by pos * theta[i]          (theta NULL: no rotation), pairs as in kvbfp_rope_tables
+ * q goes to q_out rounded once; k and v to the sequence's position in the cache.  The stored codes of k are those of the formula
+ * in 64 bits: values are formed in fp32, and rows with one next to a rounding border again in fp64.
+ *   pages    host struct (cache is then its pool), or NULL: cache holds a sequence per batch entry
+ *   q, k, v  token i at q + i * q_stride (in elements, a multiple of 16 bytes): heads densely, so that the three may lie in one
+ *            array.  q may be NULL (then q_out too), or k and v together
+ *   n_tokens rows of q, k, v and q_out; starts is read clamped to it
+ *   q_weight, k_weight  [head_dim] f32 or NULL;  eps >= 0
+ *   theta    [head_dim / 2] f64: frequency of each pair (zero: that pair stays)
+ *   q_out    [n_tokens, n_q_heads, head_dim] of `dt`, channel order; may be q itself where that is dense
+ * Tokens outside the cache (or whose page is missing) are not stored and set KVBFP_FLAG_POSITION; their q is written all the
+ * same.  Rows behind starts[batch] are left as they were.  Non-finite keys or values set KVBFP_FLAG_NONFINITE.
+ */
+kvbfp_status kvbfp_norm_rope_append(const kvbfp_cache* cache, const kvbfp_pages* pages, const void* q, int64_t q_stride,
+                                    const void* k, int64_t k_stride, const void* v, int64_t v_stride, kvbfp_dtype dt,
+                                    int32_t n_q_heads, int32_t n_tokens, const int32_t* starts, const int32_t* seq_lens,
+                                    const float* q_weight, const float* k_weight, float eps, const double* theta,
+                                    int32_t half_split, const int32_t* perm_k, const int32_t* perm_v, void* q_out,
+                                    void* stream);
+
+/* Bytes of workspace of kvbfp_ragged_attn (0 on invalid arguments): batch sequences, n_tokens new tokens in all.  Contents need
+ * no initialisation; calls that may overlap on the GPU need one each. */
+size_t kvbfp_ragged_workspace_bytes(const kvbfp_format* fmt, int32_t batch, int32_t n_q_heads, int32_t n_tokens);
+
+/*
+ * Attention of a ragged batch of new tokens (their K and V are in the cache already) over the packed cache, contiguous or in
+ * pages: whole prompts, chunks of them and single tokens in one call.  The query at position p sees the tokens t <= p with
+ *   t < n_sink  or  p - t < window                   (window 0: all)
+ *   q          [n_tokens, n_q_heads, head_dim] of `dt`, original channel order
+ *   max_new    largest number of new tokens of a sequence: a hint for the choice of kernels, any value gives the result
+ *   pages      as in kvbfp_norm_rope_append; entries of pages that no query sees are not read.  Where one that is needed is
+ *              missing, KVBFP_FLAG_POSITION is set and the sequence's rows are unspecified
+ *   out        [n_tokens, n_q_heads, head_dim] of `dt`; zeros for tokens at negative positions.  Rows behind starts[batch] are
+ *              left as they were
+ * perm_k, inv_perm_v, softmax_scale as in kvbfp_decode_attn.  n_q_heads <= 8 n_kv_heads, batch <= 1024.  Types and accuracy as
+ * in kvbfp_tree_attn.  Lengths beyond the cache are read clamped and set KVBFP_FLAG_POSITION.  No atomics: the result depends on
+ * nothing but the arguments.
+ */
+kvbfp_status kvbfp_ragged_attn(const kvbfp_cache* cache, const kvbfp_pages* pages, const void* q, kvbfp_dtype dt,
+                               int32_t n_q_heads, int32_t n_tokens, int32_t batch, const int32_t* starts,
+                               const int32_t* seq_lens, int32_t max_new, int32_t window, int32_t n_sink,
+                               const int32_t* perm_k, const int32_t* inv_perm_v, float softmax_scale, void* out,
+                               void* workspace, size_t workspace_bytes, void* stream);
 
 /*
  * kvbfp_decode_attn for callers that must not allocate device memory (the paper has no counterpart:

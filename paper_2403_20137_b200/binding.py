@@ -16,7 +16,7 @@ OK = 0
 ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_ALIGNMENT, ERR_CAPACITY, ERR_WORKSPACE, ERR_CUDA = 1, 2, 3, 4, 5, 6
 F32, BF16 = 0, 1
 STAT_MAXABS, STAT_L2 = 0, 1
-FLAG_NONFINITE, FLAG_POSITION, FLAG_LEN_HINT, FLAG_WAIT_TIMEOUT = 1, 2, 4, 8
+FLAG_NONFINITE, FLAG_POSITION, FLAG_LEN_HINT, FLAG_WAIT_TIMEOUT, FLAG_PAGES = 1, 2, 4, 8, 16
 DECODE_AUTO, DECODE_SIMT, DECODE_MMA, DECODE_MMA_BF16 = 0, 1, 2, 3
 
 EXPORTS = ["kvbfp_version", "kvbfp_status_string", "kvbfp_last_cuda_error", "kvbfp_plane_bytes",
@@ -27,7 +27,9 @@ EXPORTS = ["kvbfp_version", "kvbfp_status_string", "kvbfp_last_cuda_error", "kvb
            "kvbfp_rope_tables", "kvbfp_rope_apply", "kvbfp_decode_attn_rope", "kvbfp_split_plan",
            "kvbfp_split_range_start", "kvbfp_split_range_of", "kvbfp_split_partial_slot",
            "kvbfp_selftest_wait_timeout", "kvbfp_attn_workspace_bytes", "kvbfp_tree_attn", "kvbfp_decode_attn_mod",
-           "kvbfp_decode_attn_mass", "kvbfp_evict", "kvbfp_gather_rows"]
+           "kvbfp_decode_attn_mass", "kvbfp_evict", "kvbfp_gather_rows", "kvbfp_pages_free", "kvbfp_pages_fork",
+           "kvbfp_pages_reserve", "kvbfp_pages_workspace_bytes", "kvbfp_pages_compact", "kvbfp_pages_copy",
+           "kvbfp_norm_rope_append", "kvbfp_ragged_workspace_bytes", "kvbfp_ragged_attn"]
 
 
 class KvbfpError(RuntimeError):
@@ -52,6 +54,11 @@ class Format(C.Structure):
 class CacheStruct(C.Structure):
     _fields_ = [("fmt", Format), ("k_mant", C.c_void_p), ("k_exp", C.c_void_p),
                 ("v_mant", C.c_void_p), ("v_exp", C.c_void_p)]
+
+
+class PagesStruct(C.Structure):
+    _fields_ = [("batch", C.c_int32), ("max_pages", C.c_int32), ("n_pages", C.c_int32), ("page_tokens", C.c_int32),
+                ("table", C.c_void_p), ("refs", C.c_void_p), ("lens", C.c_void_p)]
 
 
 class ScoreModStruct(C.Structure):
@@ -133,6 +140,22 @@ def lib():
                                   C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]
         L.kvbfp_gather_rows.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p,
                                         C.c_void_p, C.c_void_p]
+        L.kvbfp_pages_free.argtypes = [C.c_void_p] * 4
+        L.kvbfp_pages_fork.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p]
+        L.kvbfp_pages_reserve.argtypes = [C.c_void_p] * 4
+        L.kvbfp_pages_workspace_bytes.restype = C.c_size_t
+        L.kvbfp_pages_workspace_bytes.argtypes = [C.c_void_p]
+        L.kvbfp_pages_compact.argtypes = [C.c_void_p] * 5 + [C.c_size_t, C.c_void_p]
+        L.kvbfp_pages_copy.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p]
+        L.kvbfp_norm_rope_append.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p,
+                                             C.c_int64, C.c_int, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p,
+                                             C.c_void_p, C.c_float, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p,
+                                             C.c_void_p]
+        L.kvbfp_ragged_workspace_bytes.restype = C.c_size_t
+        L.kvbfp_ragged_workspace_bytes.argtypes = [C.c_void_p, C.c_int32, C.c_int32, C.c_int32]
+        L.kvbfp_ragged_attn.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_int32, C.c_int32, C.c_int32, C.c_void_p,
+                                        C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_float,
+                                        C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
         L.kvbfp_split_partial_slot.argtypes = [C.c_int32] * 4
         L.kvbfp_split_partial_slot.restype = C.c_int32
         _lib = L
@@ -203,9 +226,47 @@ class Cache:
              (lambda s: torch.full(s, fill, dtype=torch.uint8, device=device))
         self.k_mant, self.k_exp, self.v_mant, self.v_exp = mk(shape_m), mk(shape_e), mk(shape_m), mk(shape_e)
 
+    @classmethod
+    def of(cls, k_mant, k_exp, v_mant, v_exp, block, mant_bits):
+        """A cache (or pool of pages) in planes that are there already: uint8 [batch, n_kv_heads, max_seq, row bytes]."""
+        batch, heads, rows, _ = k_mant.shape
+        cache = cls.__new__(cls)
+        cache.fmt = Format(batch, heads, 8 * k_mant.shape[3] // mant_bits, rows, block, mant_bits)
+        for name, t, width in (("k_mant", k_mant, cache.fmt.row_m), ("k_exp", k_exp, cache.fmt.row_e),
+                               ("v_mant", v_mant, cache.fmt.row_m), ("v_exp", v_exp, cache.fmt.row_e)):
+            setattr(cache, name, _sized(name, _dev(t, torch.uint8), (batch, heads, rows, width)))
+        return cache
+
     def struct(self):
         return CacheStruct(self.fmt, self.k_mant.data_ptr(), self.k_exp.data_ptr(),
                            self.v_mant.data_ptr(), self.v_exp.data_ptr())
+
+
+class PagePool:
+    """Page table, reference counts and lengths of the sequences of a paged cache (kvbfp_pages).  The pages themselves are a
+    Cache of n_pages "sequences" of page_tokens tokens, one per layer; one PagePool serves them all."""
+
+    def __init__(self, batch, max_pages, n_pages, page_tokens, device="cuda"):
+        self.table = torch.full((batch, max_pages), -1, dtype=torch.int32, device=device)
+        self.refs = torch.zeros(n_pages, dtype=torch.int32, device=device)
+        self.lens = torch.zeros(batch, dtype=torch.int32, device=device)
+        self.n_pages, self.page_tokens = n_pages, page_tokens
+
+    @classmethod
+    def of(cls, table, refs, lens, n_pages, page_tokens):
+        """Tables that are there already: i32 [batch, max_pages], [n_pages] (or None: attention and writes only), [batch]."""
+        pool = cls.__new__(cls)
+        pool.table, pool.n_pages, pool.page_tokens = _dev(table, torch.int32), n_pages, page_tokens
+        if table.dim() != 2:
+            raise ValueError(f"table: expected [batch, max_pages], got shape {tuple(table.shape)}")
+        pool.refs = _sized("refs", _dev(refs, torch.int32), (n_pages,))
+        pool.lens = _sized("lens", _dev(lens, torch.int32), (table.shape[0],))
+        return pool
+
+    def struct(self):
+        p = lambda t: None if t is None else t.data_ptr()
+        return PagesStruct(self.table.shape[0], self.table.shape[1], self.n_pages, self.page_tokens, p(self.table),
+                           p(self.refs), p(self.lens))
 
 
 def calibrate(x, n_heads, head_dim, stat=STAT_MAXABS, stream=None):
@@ -475,6 +536,157 @@ def gather_rows(cache, index, count, src_base=None, dst=None, dst_base=None, str
                                    _ptr(_sized("count", _dev(count, torch.int32), (f.batch,))),
                                    _ptr(_sized("src_base", _dev(src_base, torch.int32), (f.batch,))),
                                    _ptr(_sized("dst_base", _dev(dst_base, torch.int32), (f.batch,))), _stream(stream)))
+
+
+def _pool_on_device(pool, *tensors):
+    dev = torch.cuda.current_device()
+    for t in (pool.table, pool.refs, pool.lens, *tensors):
+        if t is not None and t.get_device() != dev:
+            raise ValueError("expected the pool and all tensors on the current device")
+    return pool.struct()
+
+
+def pages_free(pool, lo=None, hi=None, stream=None):
+    """kvbfp_pages_free: the pages wholly inside tokens [lo, hi) (i32 [batch]; None: 0, no limit) of each sequence."""
+    n = (pool.table.shape[0],)
+    ps = _pool_on_device(pool, lo, hi)
+    _check(lib().kvbfp_pages_free(C.byref(ps), _ptr(_sized("lo", _dev(lo, torch.int32), n)),
+                                  _ptr(_sized("hi", _dev(hi, torch.int32), n)), _stream(stream)))
+
+
+def pages_fork(pool, src, dst, stream=None):
+    """kvbfp_pages_fork: sequence dst[i] shares the pages of sequence src[i] (i32 [n])."""
+    ps = _pool_on_device(pool, src, dst)
+    _check(lib().kvbfp_pages_fork(C.byref(ps), _ptr(_dev(src, torch.int32)),
+                                  _ptr(_sized("dst", _dev(dst, torch.int32), src.shape)), src.numel(), _stream(stream)))
+
+
+def pages_reserve(pool, more, pairs=None, stream=None):
+    """kvbfp_pages_reserve -> pairs i32 [batch, 2]: the pages to be copied (pages_copy) before the tokens are written."""
+    n = pool.table.shape[0]
+    if pairs is None:
+        pairs = _empty((n, 2), torch.int32, more.device, stream)
+    ps = _pool_on_device(pool, more, pairs)
+    _check(lib().kvbfp_pages_reserve(C.byref(ps), _ptr(_sized("more", _dev(more, torch.int32), (n,))),
+                                     _ptr(_sized("pairs", _dev(pairs, torch.int32), (n, 2))), _stream(stream)))
+    return pairs
+
+
+def pages_compact(pool, dst=None, moves=None, count=None, workspace=None, stream=None):
+    """kvbfp_pages_compact -> (moves i32 [n_pages, 2], count i32 [1]) for pages_copy.  dst: another PagePool, or None: in
+    place."""
+    dev = pool.table.device
+    dst = pool if dst is None else dst
+    if moves is None:
+        moves = _empty((pool.n_pages, 2), torch.int32, dev, stream)
+    if count is None:
+        count = _empty((1,), torch.int32, dev, stream)
+    ps = _pool_on_device(pool, moves, count, workspace, dst.table, dst.refs, dst.lens)
+    ds = dst.struct()
+    if workspace is None:
+        workspace = _empty(int(lib().kvbfp_pages_workspace_bytes(C.byref(ps))), torch.uint8, dev, stream)
+    _check(lib().kvbfp_pages_compact(C.byref(ps), C.byref(ds), _ptr(_sized("moves", _dev(moves, torch.int32), (pool.n_pages, 2))),
+                                     _ptr(_sized("count", _dev(count, torch.int32), (1,))), _ptr(_dev(workspace, torch.uint8)),
+                                     workspace.numel(), _stream(stream)))
+    return moves, count
+
+
+def pages_copy(cache, pairs, count=None, dst=None, stream=None):
+    """kvbfp_pages_copy: page pairs[i, 0] of cache to page pairs[i, 1] of dst (None: cache itself); i32 [n, 2]."""
+    dst = cache if dst is None else dst
+    _same_device(cache, dst.k_mant, pairs, count)
+    if pairs.dim() != 2 or pairs.shape[1] != 2:
+        raise ValueError(f"pairs: expected [n, 2], got shape {tuple(pairs.shape)}")
+    cs, ds = cache.struct(), dst.struct()
+    _check(lib().kvbfp_pages_copy(C.byref(cs), C.byref(ds), _ptr(_dev(pairs, torch.int32)), pairs.shape[0],
+                                  _ptr(_sized("count", _dev(count, torch.int32), (1,))), _stream(stream)))
+
+
+def _rows(name, t, heads, head_dim):
+    """Rows [n, heads, head_dim] of tokens that may lie apart (heads densely): the stride from token to token."""
+    if t is None:
+        return 0
+    if not t.is_cuda or t.dim() != 3 or (heads is not None and t.shape[1] != heads) or t.shape[2] != head_dim:
+        raise ValueError(f"{name}: expected a CUDA tensor [n_tokens, {'heads' if heads is None else heads}, {head_dim}]")
+    if t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != head_dim):
+        raise ValueError(f"{name}: expected the heads of a token side by side")
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1] * head_dim
+
+
+def _ragged(cache, pool, starts, seq_lens):
+    """The sequences of a ragged call, and its pages' struct."""
+    n = cache.fmt.batch if pool is None else pool.table.shape[0]
+    _sized("starts", _dev(starts, torch.int32), (n + 1,))
+    _sized("seq_lens", _dev(seq_lens, torch.int32), (n,))
+    if pool is None:
+        return n, None
+    _same_device(cache, pool.table)
+    return n, pool.struct()
+
+
+def norm_rope_append(cache, q, k, v, starts, seq_lens, q_weight=None, k_weight=None, eps=1e-6, theta=None, half_split=False,
+                     perm_k=None, perm_v=None, pool=None, q_out=None, stream=None):
+    """kvbfp_norm_rope_append: q [n, H_q, d], k, v [n, H_kv, d] (views of one array will do: heads side by side, any token
+    stride) of the new tokens of a ragged batch -> q_out; k and v go to the cache (the pool's pages).  starts i32 [batch + 1],
+    seq_lens i32 [batch]; weights f32 [d]; theta f64 [d / 2].  q None (or k and v): only the others."""
+    f = cache.fmt
+    ref = q if q is not None else k
+    dt = _dt(ref)
+    _same_device(cache, q, k, v, starts, seq_lens, q_weight, k_weight, theta, perm_k, perm_v, q_out)
+    strides = [_rows(name, t, heads, f.head_dim) for name, t, heads in (("q", q, None), ("k", k, f.n_kv_heads), ("v", v, f.n_kv_heads))]
+    for name, t in (("k", k), ("v", v)):
+        if t is not None and (t.dtype != ref.dtype or t.shape[0] != ref.shape[0]):
+            raise ValueError(f"{name}: expected the type and number of tokens of q")
+    _, ps = _ragged(cache, pool, starts, seq_lens)
+    if q is not None and q_out is None:
+        q_out = _empty(q.shape, q.dtype, q.device, stream)
+    if q_out is not None:
+        _sized("q_out", _dev(q_out, ref.dtype), () if q is None else q.shape)
+    for name, t, n in (("q_weight", q_weight, f.head_dim), ("k_weight", k_weight, f.head_dim), ("theta", theta, f.head_dim // 2),
+                       ("perm_k", perm_k, f.n_kv_heads * f.head_dim), ("perm_v", perm_v, f.n_kv_heads * f.head_dim)):
+        if t is not None and t.numel() != n:
+            raise ValueError(f"{name}: expected {n} values, got {t.numel()}")
+    cs = cache.struct()
+    _check(lib().kvbfp_norm_rope_append(C.byref(cs), None if ps is None else C.byref(ps), _ptr(q), strides[0], _ptr(k), strides[1],
+                                        _ptr(v), strides[2], dt, 0 if q is None else q.shape[1], ref.shape[0], _ptr(starts),
+                                        _ptr(seq_lens), _ptr(_dev(q_weight, torch.float32)), _ptr(_dev(k_weight, torch.float32)),
+                                        float(eps), _ptr(_dev(theta, torch.float64)), int(half_split),
+                                        _ptr(_dev(perm_k, torch.int32)), _ptr(_dev(perm_v, torch.int32)), _ptr(q_out),
+                                        _stream(stream)))
+    return q_out
+
+
+def ragged_workspace_bytes(fmt, batch, n_q_heads, max_new):
+    """Workspace of ragged_attn for up to max_new new tokens of each of `batch` sequences."""
+    return int(lib().kvbfp_ragged_workspace_bytes(C.byref(fmt), batch, n_q_heads, batch * max_new))
+
+
+def ragged_attn(cache, q, starts, seq_lens, max_new, window=0, n_sink=0, perm_k=None, inv_perm_v=None, softmax_scale=0.0,
+                pool=None, out=None, workspace=None, stream=None):
+    """kvbfp_ragged_attn: q [n, H_q, d], the new tokens of a ragged batch, over the cache (the pool's pages) -> out of q's type.
+    starts i32 [batch + 1]; seq_lens i32 [batch], the new tokens included; max_new: most new tokens of a sequence (a hint)."""
+    f = cache.fmt
+    q = _query(q, ("n", "H_q", "d"))
+    n_q_heads = q.shape[1]
+    if q.shape[2] != f.head_dim:
+        raise ValueError(f"q: shape {tuple(q.shape)} does not fit a cache of head_dim {f.head_dim}")
+    _same_device(cache, q, starts, seq_lens, perm_k, inv_perm_v, out, workspace)
+    for t in (perm_k, inv_perm_v):
+        if t is not None and t.numel() != f.n_kv_heads * f.head_dim:
+            raise ValueError(f"permutation: expected {f.n_kv_heads} x {f.head_dim} values, got {t.numel()}")
+    batch, ps = _ragged(cache, pool, starts, seq_lens)
+    if out is None:
+        out = _empty(q.shape, q.dtype, q.device, stream)
+    _sized("out", _dev(out, q.dtype), q.shape)
+    if workspace is None:
+        workspace = _empty(int(lib().kvbfp_ragged_workspace_bytes(C.byref(f), batch, n_q_heads, q.shape[0])), torch.uint8, q.device, stream)
+    _dev(workspace, torch.uint8)
+    cs = cache.struct()
+    _check(lib().kvbfp_ragged_attn(C.byref(cs), None if ps is None else C.byref(ps), _ptr(q), _dt(q), n_q_heads, q.shape[0], batch,
+                                   _ptr(starts), _ptr(seq_lens), int(max_new), int(window), int(n_sink),
+                                   _ptr(_dev(perm_k, torch.int32)), _ptr(_dev(inv_perm_v, torch.int32)), float(softmax_scale),
+                                   _ptr(out), _ptr(workspace), workspace.numel(), _stream(stream)))
+    return out
 
 
 def device_status(stream=None):

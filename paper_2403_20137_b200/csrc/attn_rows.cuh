@@ -156,8 +156,8 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t x) {
 }
 
 // pi(q) of one query row (`q`; NULL: zeros) at a lane's k positions as B operand: [term][k step / 2].
-template <int P, bool F32>
-__device__ __forceinline__ void load_q(const AttnArgs& a, const void* q, int hk, int t, uint4 (&qr)[F32 ? 3 : 1][4]) {
+template <int P, bool F32, class Args>
+__device__ __forceinline__ void load_q(const Args& a, const void* q, int hk, int t, uint4 (&qr)[F32 ? 3 : 1][4]) {
     int at[32];           // channels of the lane's 32 slots
 #pragma unroll
     for (int i = 0; i < 8; ++i) {

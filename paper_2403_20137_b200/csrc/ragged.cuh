@@ -1,0 +1,214 @@
+// Attention of a ragged batch of new tokens over a contiguous or paged packed cache, causal, with a sliding window and first
+// tokens that stay visible: arguments, what a run of query rows sees, and the split of all tiles over the workers.
+//
+// The query rows of a (sequence, kv head) are its new tokens times the query heads of the group, token-major.  They are cut into
+// row tiles; an entry is a (sequence, row tile, kv head), its items are the cache tiles that any of its rows sees.  All items
+// (sequence, row tile, kv head, tile: the last fastest) are cut into one contiguous range per worker (attn.cuh); an entry that
+// ends in another worker's range than it begins in leaves partial results, at most two a worker, which ragged_merge joins.
+#pragma once
+#include "attn.cuh"
+#include "pages.cuh"
+
+namespace kvbfp {
+
+struct RaggedArgs {
+    kvbfp_format fmt;
+    TokenMap map;
+    const uint8_t *k_mant, *k_exp, *v_mant, *v_exp;
+    const void* q;                 // [n_tokens, Hq, d]
+    int q_is_bf16;                 // the output has the same type
+    int n_q_heads, group, batch, n_tokens;
+    const int32_t* starts;
+    const int32_t* lens;
+    const int32_t* perm_k;
+    const int32_t* inv_perm_v;
+    float scale;
+    int window, n_sink;
+    void* out;
+    int few_lo, few_hi;            // this kernel takes sequences of that many query rows per kv head: few_lo < rows <= few_hi
+    int rows_tile;                 // rows of a row tile
+    int part_rows;                 // rows of a partial
+    int workers;
+    int4* rec;                     // workspace: per worker the entry that ends in its range's first run and began before it:
+                                   // sequence, row tile, kv head, first worker (-1: none)
+    float* partials;               // workspace: [2 * workers, part_rows, kAttnPart]
+    float out_up;                  // sums of P and V as the kernel carries them -> values
+    uint32_t* status;
+};
+
+struct RaggedSeq {
+    int start, n;      // its rows of q: tokens [start, start + n)
+    int len, base;     // cached tokens, position of the first new one (negative: more new tokens than cached ones)
+    int clamped;
+};
+__device__ __forceinline__ RaggedSeq ragged_seq(const RaggedArgs& a, int b) {
+    RaggedSeq s;
+    s.start = min(max(a.starts[b], 0), a.n_tokens);
+    s.n = max(min(max(a.starts[b + 1], 0), a.n_tokens) - s.start, 0);
+    const int raw = a.lens[b];
+    s.len = min(max(raw, 0), a.map.cap);
+    s.clamped = s.len != raw;
+    s.base = s.len - s.n;
+    return s;
+}
+__device__ __forceinline__ int ragged_row_tiles(const RaggedArgs& a, const RaggedSeq& s, int rows_tile) {
+    const int64_t rows = (int64_t)s.n * a.group;
+    return rows > a.few_lo && rows <= a.few_hi ? (int)((rows + rows_tile - 1) / rows_tile) : 0;
+}
+
+// Tiles that the rows of row tile rt see: the first tokens' tiles [0, np), then those from `lo` on, n in all.
+struct RaggedView {
+    int p0, p1;        // positions of the first and last row
+    int lo, np, n;
+};
+__device__ __forceinline__ RaggedView ragged_view(const RaggedArgs& a, const RaggedSeq& s, int rt, int rows_tile, int tile) {
+    RaggedView v;
+    const int r0 = rt * rows_tile, r1 = min(s.n * a.group, r0 + rows_tile) - 1;
+    v.p0 = s.base + r0 / a.group;
+    v.p1 = s.base + r1 / a.group;
+    const int end = v.p1 + 1;
+    const int lo = a.window > 0 ? max(v.p0 - a.window + 1, 0) : 0;
+    int t0 = lo / tile, np = a.window > 0 ? (min(a.n_sink, max(end, 0)) + tile - 1) / tile : 0;
+    const int t1 = end > 0 ? (end + tile - 1) / tile : 0;
+    if (np >= t0) t0 = np = 0;
+    v.lo = t0;
+    v.np = np;
+    v.n = np + max(t1 - t0, 0);
+    return v;
+}
+__device__ __forceinline__ int ragged_token(const RaggedView& v, int k, int tile) { return (k < v.np ? k : k - v.np + v.lo) * tile; }
+
+struct RaggedCursor {      // an item: sequence, row tile, kv head, tile k of n
+    int b, rt, nrt, hk, k;
+    RaggedSeq s;
+    RaggedView v;
+};
+// To the first item of the next entry (b = batch: none).
+__device__ __forceinline__ void ragged_next(const RaggedArgs& a, RaggedCursor& c, int rows_tile, int tile) {
+    c.k = 0;
+    if (++c.hk < a.fmt.n_kv_heads) return;
+    c.hk = 0;
+    do {
+        if (++c.rt >= c.nrt) {
+            c.rt = 0;
+            do {
+                if (++c.b >= a.batch) return;
+                c.s = ragged_seq(a, c.b);
+                c.nrt = ragged_row_tiles(a, c.s, rows_tile);
+            } while (c.nrt == 0);
+        }
+        c.v = ragged_view(a, c.s, c.rt, rows_tile, tile);
+    } while (c.v.n == 0);
+}
+// To item `at` of sequence b, which has it (whole warp).
+__device__ __forceinline__ void ragged_seek(const RaggedArgs& a, RaggedCursor& c, int b, int at, int rows_tile, int tile) {
+    const int lane = threadIdx.x & 31, H = a.fmt.n_kv_heads;
+    c.b = b;
+    c.s = ragged_seq(a, b);
+    c.nrt = ragged_row_tiles(a, c.s, rows_tile);
+    c.rt = 0;
+    for (int r0 = 0; r0 < c.nrt; r0 += 32) {
+        int x = r0 + lane < c.nrt ? ragged_view(a, c.s, r0 + lane, rows_tile, tile).n * H : 0;
+        const int mine = x;
+#pragma unroll
+        for (int off = 1; off < 32; off <<= 1) {
+            const int y = __shfl_up_sync(0xffffffffu, x, off);
+            if (lane >= off) x += y;
+        }
+        const uint32_t past = __ballot_sync(0xffffffffu, x > at);
+        if (past) {
+            const int l = __ffs(past) - 1;
+            c.rt = r0 + l;
+            at -= __shfl_sync(0xffffffffu, x - mine, l);
+            break;
+        }
+        at -= __shfl_sync(0xffffffffu, x, 31);
+    }
+    c.v = ragged_view(a, c.s, c.rt, rows_tile, tile);
+    const int n = max(c.v.n, 1);
+    c.hk = at / n;
+    c.k = at - c.hk * n;
+}
+
+// Rows at negative positions see nothing; lengths outside the cache are reported (both by one thread, they are rare).
+static __device__ __noinline__ void ragged_edges(uint32_t* status, uint4* out, int64_t pieces, bool clamped) {
+    if (clamped) raise_flag(status, KVBFP_FLAG_POSITION);
+    for (int64_t i = 0; i < pieces; ++i) out[i] = make_uint4(0u, 0u, 0u, 0u);
+}
+
+// Items of every sequence, before it and in all: threads of a block together (THREADS of them).  s_items: room for 1024 + 1.
+// Afterwards s_items[b] holds the items before sequence b, s_items[batch] all.
+template <int THREADS>
+__device__ __forceinline__ void ragged_count(const RaggedArgs& a, int (&s_items)[kMaxPagedBatch + 1], int (&s_scan)[THREADS / 32], int rows_tile, int tile) {
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, H = a.fmt.n_kv_heads;
+    constexpr int kAlone = 8;                                  // row tiles that a thread counts by itself
+    bool many = false;
+    for (int b = tid; b < a.batch; b += THREADS) {
+        const RaggedSeq s = ragged_seq(a, b);
+        const int nrt = ragged_row_tiles(a, s, rows_tile);
+        int x = 0;
+        if (nrt <= kAlone) for (int r = 0; r < nrt; ++r) x += ragged_view(a, s, r, rows_tile, tile).n;
+        else x = -1;
+        s_items[b] = x < 0 ? x : x * H;
+        many |= x < 0;
+        if (blockIdx.x == 0 && nrt > 0 && (s.clamped || s.base < 0)) {
+            const int64_t row = (int64_t)a.n_q_heads * kHeadDim * (a.q_is_bf16 ? 2 : 4) / 16;
+            ragged_edges(a.status, reinterpret_cast<uint4*>(a.out) + s.start * row, (int64_t)min(s.n, max(-s.base, 0)) * row, s.clamped != 0);
+        }
+    }
+    if (__syncthreads_or(many)) {
+        for (int b = warp; b < a.batch; b += THREADS / 32) {
+            if (s_items[b] >= 0) continue;
+            const RaggedSeq s = ragged_seq(a, b);
+            const int nrt = ragged_row_tiles(a, s, rows_tile);
+            int x = 0;
+            for (int r = lane; r < nrt; r += 32) x += ragged_view(a, s, r, rows_tile, tile).n;
+            x = __reduce_add_sync(0xffffffffu, x);
+            if (lane == 0) s_items[b] = x * H;
+        }
+        __syncthreads();
+    }
+    const int per = (a.batch + THREADS - 1) / THREADS;
+    int mine = 0;
+    for (int i = 0; i < per; ++i)
+        if (tid * per + i < a.batch) mine += s_items[tid * per + i];
+    int x = mine;
+#pragma unroll
+    for (int off = 1; off < 32; off <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, x, off);
+        if (lane >= off) x += y;
+    }
+    if (lane == 31) s_scan[warp] = x;
+    __syncthreads();
+    x -= mine;
+    int total = 0;
+#pragma unroll
+    for (int w = 0; w < THREADS / 32; ++w) {
+        if (w < warp) x += s_scan[w];
+        total += s_scan[w];
+    }
+    for (int i = 0; i < per; ++i) {
+        const int b = tid * per + i;
+        if (b >= a.batch) break;
+        const int n = s_items[b];
+        s_items[b] = x;
+        x += n;
+    }
+    if (tid == 0) s_items[a.batch] = total;
+    __syncthreads();
+}
+// The sequence that item `at` belongs to.
+__device__ __forceinline__ int ragged_find(const RaggedArgs& a, const int* s_items, int at) {
+    int lo = 0, hi = a.batch - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (s_items[mid] <= at) lo = mid; else hi = mid - 1;
+    }
+    return lo;
+}
+// ragged_rows: items of eight rows, a worker per warp
+kvbfp_status launch_ragged_rows4(const RaggedArgs& a, int grid, cudaStream_t s);
+kvbfp_status launch_ragged_rows6(const RaggedArgs& a, int grid, cudaStream_t s);
+kvbfp_status launch_ragged_rows8(const RaggedArgs& a, int grid, cudaStream_t s);
+
+}  // namespace kvbfp
