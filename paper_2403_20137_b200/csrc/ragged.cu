@@ -102,25 +102,49 @@ __global__ void __launch_bounds__(128) ragged_merge(const RaggedArgs a) {
 }
 
 inline size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
-constexpr int kRowsWorkers = 3 * kAttnWarps * kAttnMaxSms;
 
-// Workspace regions in order; returns the size and, with `a`, sets the pointers.
-size_t lay_out(int64_t rows, RaggedArgs* a, uint8_t* base) {
-    const int part_rows = (int)(rows < 8 ? rows : 8);
-    size_t at = 0;
-    auto take = [&](size_t bytes) {
-        uint8_t* p = base + at;
-        at += up256(bytes);
-        return p;
-    };
-    uint8_t* rec = take((size_t)kRowsWorkers * sizeof(int4));
-    uint8_t* part = take((size_t)2 * kRowsWorkers * part_rows * kAttnPart * 4);
+// Sequences of up to kFewRows bf16 query rows per kv head go to ragged_rows (every eight rows read the cache anew), longer ones
+// to ragged_umma (256 rows a pass).
+constexpr int kFewRows = 8;
+struct Kernel {
+    int rows_tile, tile, max_workers;
+};
+inline Kernel kernel_of(bool umma, int mant_bits) {
+    return umma ? Kernel{256, 128, kAttnMaxSms} : Kernel{8, attn_rows_tile(mant_bits), 3 * kAttnWarps * kAttnMaxSms};
+}
+
+// Workspace of one of the two from `base` on; returns the size and, with `a`, sets the pointers.
+size_t lay_out(const Kernel& k, int64_t rows, RaggedArgs* a, uint8_t* base) {
+    const int part_rows = (int)(rows < k.rows_tile ? rows : k.rows_tile);
+    const size_t rec = up256((size_t)k.max_workers * sizeof(int4));
     if (a) {
+        a->rows_tile = k.rows_tile;
         a->part_rows = part_rows;
-        a->rec = reinterpret_cast<int4*>(rec);
-        a->partials = reinterpret_cast<float*>(part);
+        a->rec = reinterpret_cast<int4*>(base);
+        a->partials = reinterpret_cast<float*>(base + rec);
     }
-    return at;
+    return rec + up256((size_t)2 * k.max_workers * part_rows * kAttnPart * 4);
+}
+
+kvbfp_status launch_kernel(RaggedArgs a, bool umma, int64_t rows, uint8_t* workspace, int n_sm, cudaStream_t s) {
+    const int bits = a.fmt.mant_bits;
+    const Kernel k = kernel_of(umma, bits);
+    (void)lay_out(k, rows, &a, workspace);
+    const int64_t most = (rows / k.rows_tile + a.batch) * a.fmt.n_kv_heads * (a.map.cap / k.tile + 2);
+    const int per_block = umma ? 1 : kAttnWarps;
+    int64_t grid = (int64_t)n_sm * (umma ? 1 : attn_rows_blocks(a.q_is_bf16));
+    if (grid * per_block > k.max_workers) grid = k.max_workers / per_block;
+    if (grid > most) grid = most;
+    a.workers = (int)grid * per_block;
+    kvbfp_status st;
+    if (umma) st = bits == 4 ? launch_ragged_umma4(a, (int)grid, s) : bits == 6 ? launch_ragged_umma6(a, (int)grid, s) : launch_ragged_umma8(a, (int)grid, s);
+    else st = bits == 4 ? launch_ragged_rows4(a, (int)grid, s) : bits == 6 ? launch_ragged_rows6(a, (int)grid, s) : launch_ragged_rows8(a, (int)grid, s);
+    if (st != KVBFP_OK) return st;
+    // a block per row where an entry has one or two, a warp per row otherwise
+    if (a.part_rows <= 2) KVBFP_CUDA(launch_pdl(ragged_merge<true>, dim3(a.workers, a.part_rows), dim3(128), 0, s, a));
+    else KVBFP_CUDA(launch_pdl(ragged_merge<false>, dim3(a.workers, (a.part_rows + 3) / 4), dim3(128), 0, s, a));
+    KVBFP_LAUNCH_CHECK("ragged_merge");
+    return KVBFP_OK;
 }
 
 }  // namespace
@@ -130,7 +154,9 @@ extern "C" size_t kvbfp_ragged_workspace_bytes(const kvbfp_format* fmt, int32_t 
     using namespace kvbfp;
     if (check_format(fmt) != KVBFP_OK || n_q_heads < 1 || n_q_heads % fmt->n_kv_heads != 0 || n_tokens < 0 || batch < 1) return 0;
     if (batch > kMaxPagedBatch || n_q_heads / fmt->n_kv_heads > 8) return 0;
-    return lay_out((int64_t)n_tokens * (n_q_heads / fmt->n_kv_heads), nullptr, nullptr);
+    const int64_t rows = (int64_t)n_tokens * (n_q_heads / fmt->n_kv_heads);
+    const size_t few = lay_out(kernel_of(false, fmt->mant_bits), rows, nullptr, nullptr);
+    return rows > kFewRows ? few + lay_out(kernel_of(true, fmt->mant_bits), rows, nullptr, nullptr) : few;
 }
 
 extern "C" kvbfp_status kvbfp_ragged_attn(const kvbfp_cache* cache, const kvbfp_pages* pages, const void* q, kvbfp_dtype dt,
@@ -167,31 +193,26 @@ extern "C" kvbfp_status kvbfp_ragged_attn(const kvbfp_cache* cache, const kvbfp_
     a.window = window; a.n_sink = window > 0 ? n_sink : 0;
     a.out = out;
     const int64_t rows = (int64_t)n_tokens * group;
-    (void)lay_out(rows, &a, static_cast<uint8_t*>(workspace));
+    // items are counted in 32 bits
+    if ((rows / 8 + batch) * f.n_kv_heads * (a.map.cap / 32 + 2) >= (int64_t)1 << 31) return KVBFP_ERR_UNSUPPORTED;
     st = status_word(&a.status);
     if (st != KVBFP_OK) return st;
     int n_sm = 0;
     st = sm_count(&n_sm);
     if (st != KVBFP_OK) return st;
-    a.few_lo = 0;
-    a.few_hi = 0x7fffffff;
-    a.rows_tile = 8;
-    a.out_up = 256.f;
-    const int tile = attn_rows_tile(f.mant_bits);
-    // items are counted in 32 bits
-    const int64_t most = (rows / 8 + batch) * f.n_kv_heads * (a.map.cap / tile + 2);
-    if (most >= (int64_t)1 << 31) return KVBFP_ERR_UNSUPPORTED;
-    int64_t grid = (int64_t)n_sm * attn_rows_blocks(a.q_is_bf16);
-    if (grid * kAttnWarps > kRowsWorkers) grid = kRowsWorkers / kAttnWarps;
-    if (grid > most) grid = most;
-    a.workers = (int)grid * kAttnWarps;
-
     cudaStream_t s = (cudaStream_t)stream;
-    st = f.mant_bits == 4 ? launch_ragged_rows4(a, (int)grid, s) : f.mant_bits == 6 ? launch_ragged_rows6(a, (int)grid, s) : launch_ragged_rows8(a, (int)grid, s);
-    if (st != KVBFP_OK) return st;
-    // a block per row where an entry has one or two, a warp per row otherwise
-    if (a.part_rows <= 2) KVBFP_CUDA(launch_pdl(ragged_merge<true>, dim3(a.workers, a.part_rows), dim3(128), 0, s, a));
-    else KVBFP_CUDA(launch_pdl(ragged_merge<false>, dim3(a.workers, (a.part_rows + 3) / 4), dim3(128), 0, s, a));
-    KVBFP_LAUNCH_CHECK("ragged_merge");
-    return KVBFP_OK;
+    uint8_t* ws = static_cast<uint8_t*>(workspace);
+    const bool bf16 = dt == KVBFP_BF16;
+    const size_t few_bytes = lay_out(kernel_of(false, f.mant_bits), rows, nullptr, nullptr);
+    a.out_up = 256.f;
+    // The hint says whether any sequence may have many rows; where it says that none has, all go to ragged_rows, whatever they
+    // have.  Where some may, single tokens between them still do.
+    const bool many = bf16 && rows > kFewRows && (int64_t)max_new * group > kFewRows;
+    a.few_lo = 0;
+    a.few_hi = many ? kFewRows : 0x7fffffff;
+    st = !many || batch > 1 ? launch_kernel(a, false, rows, ws, n_sm, s) : KVBFP_OK;
+    if (st != KVBFP_OK || !many) return st;
+    a.few_lo = batch > 1 ? kFewRows : 0;
+    a.few_hi = 0x7fffffff;
+    return launch_kernel(a, true, rows, ws + few_bytes, n_sm, s);
 }

@@ -210,5 +210,9 @@ __device__ __forceinline__ int ragged_find(const RaggedArgs& a, const int* s_ite
 kvbfp_status launch_ragged_rows4(const RaggedArgs& a, int grid, cudaStream_t s);
 kvbfp_status launch_ragged_rows6(const RaggedArgs& a, int grid, cudaStream_t s);
 kvbfp_status launch_ragged_rows8(const RaggedArgs& a, int grid, cudaStream_t s);
+// ragged_umma: bf16 rows in items of 256, a worker per block, one block per SM
+kvbfp_status launch_ragged_umma4(const RaggedArgs& a, int grid, cudaStream_t s);
+kvbfp_status launch_ragged_umma6(const RaggedArgs& a, int grid, cudaStream_t s);
+kvbfp_status launch_ragged_umma8(const RaggedArgs& a, int grid, cudaStream_t s);
 
 }  // namespace kvbfp
