@@ -6,20 +6,24 @@
 //   O[rows x slots] += P . V                  P: tensor memory, V: shared memory (tokens the slow index)
 //
 // One persistent block per SM, a worker; tiles of 128 tokens.  A tile's packed rows are converted to bf16 once for 256 query
-// rows, by four warps that read them straight from the cache (a thread per token, the next tile's row already in registers,
-// so that pages need nothing but an address per thread).  The rows are two halves of 128, a warp group and an S and an O of their
-// own each: while one half's exponentials run, the tensor cores work for the other.  A thread owns a query row: its maximum, sum and
-// rescaling stay in the thread.  P takes the columns of the S it came from (two bf16 numbers a column), so that two S and two O fill
-// the 512 columns.  One warp issues all matrix instructions; they run in its order, which is what lets S of the next tile
-// overwrite P of this one without a wait.
+// rows, by eight warps that read them straight from the cache (a thread per token, the next tile's row already in registers,
+// so that pages need nothing but an address per thread).  The rows are two halves of 128, a warp group, an S and an O of
+// their own each: while one half's exponentials run, the tensor cores work for the other.  A thread owns a query row: maximum,
+// sum and rescaling stay in the thread.  P takes the columns of the S it came from (two bf16 numbers a column), so that two S
+// and two O fill the 512 columns.  One warp issues all matrix instructions, PV of a tile and S of the next one after the other
+// for each half; they run in its order, which is what lets the next S overwrite P without a wait, and tells the rows that O is
+// at rest.  (Every completion that it reports costs it some 250 cycles, so it reports S, the use of K and V, and O at the end of
+// a run only.  S in pieces of 64 tokens, so that a half need not wait for the tensor cores: a product with N = 64 takes them as
+// long as one with N = 128.  P handed over in two pieces: the second report costs more than the earlier start gives.)
 //
-//   warps 0..7   rows: S -> P, rescaling, pi(Q) into shared memory, results     (halves 0 and 1)
-//   warps 8..11  packed rows -> K, V in shared memory, two stages
-//   warp 12      matrix instructions
+//   warp 0        matrix instructions
+//   warp 1        where the tiles lie (2, 3: only there to give up their registers)
+//   warps 4..11   rows: S -> P, rescaling, pi(Q) into shared memory, results     (halves 0 and 1)
+//   warps 12..19  packed rows -> K (12..15), V in shared memory, two stages
 //
-// The reference maximum only moves when a score passes it by 8 (a factor 2^8 that fp32 sums and bf16 weights take without
-// harm); then O is rescaled in tensor memory, which waits for the products under way and is rare after a row's first tiles.
-// Tiles on the border of what rows see are masked in a pass of their own over S in tensor memory.
+// There is no pass for the maximum: P is formed under the row's reference, the maximum is taken on the side, and where a score
+// passes the reference by 2^16 the 64 scores are done again under a new one, after O was rescaled in tensor memory.  That
+// happens with a row's first tokens and hardly ever after.
 #pragma once
 #include "attn_rows.cuh"
 #include "ragged.cuh"
@@ -28,10 +32,19 @@
 namespace kvbfp {
 namespace {
 
-constexpr int kPRows = 256, kPTile = 128, kPThreads = 13 * 32;
-constexpr int kPQ = 0, kPK = 65536, kPV = 131072, kPEnd = 196608;      // shared memory: Q (two halves), K, V (two stages each)
+constexpr int kPRows = 256, kPTile = 128, kPThreads = 20 * 32;
+// shared memory: Q (two halves), K, V (two stages each), 32 lines of 128 bytes for each warp's results, barriers
+constexpr int kPQ = 0, kPK = 65536, kPV = 131072, kPOut = 196608, kPBars = kPOut + 8 * 4096, kPSmem = kPBars + 256;
+// A score may pass the reference maximum by so much (in powers of two) before the reference follows: P, its sums and O are
+// floating-point numbers, which lose nothing by a common factor, and have room for it.
+constexpr float kPSlack = 16.f;
 constexpr int kPPanel = kPTile * 128;                                  // 64 positions of 128 rows
-constexpr int kPSmem = kPEnd + 256;
+
+// Registers a thread after the split, of the 96 that the launch gives each: rows, packed rows, the rest (2 x 136 + 2 x 80 + 48 =
+// 5 x 96).
+constexpr int kPRegsRows = 136, kPRegsConv = 80, kPRegsRest = 48;
+template <int N> __device__ __forceinline__ void regs_more() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N> __device__ __forceinline__ void regs_less() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
 
 // Slot at position m of a converted row: the order the fields unpack in.
 template <int P>
@@ -83,7 +96,36 @@ __device__ __forceinline__ void prompt_convert(const uint32_t (&w)[P], const AW&
     }
 }
 
-__device__ __noinline__ bool prompt_wait_slow(uint32_t bar, uint32_t parity) { return mbar_wait_bounded(bar, parity); }
+// Matrix instructions whose descriptors differ in their lower words only (all operands here: groups of eight lines 1024 bytes
+// apart, 128-byte swizzle), which is what their registers hold.
+constexpr uint32_t kPDescUpper = (1024u >> 4) | (1u << 14) | (2u << 29);
+__device__ __forceinline__ uint32_t prompt_desc(uint32_t smem_addr, uint32_t lbo) { return ((smem_addr >> 4) & 0x3fffu) | ((lbo >> 4) & 0x3fffu) << 16; }
+// Eight steps of 16 positions (two panels) of S; eight steps of 16 tokens of O.  The whole warp calls, one thread issues.
+__device__ __forceinline__ void prompt_s(uint32_t d, uint32_t q, uint32_t k, uint32_t idesc) {
+    asm volatile("{\n\t.reg .pred e;\n\t.reg .b64 x, y;\n\telect.sync _|e, 0xffffffff;\n\tmov.b64 x, {%1, %4};\n\tmov.b64 y, {%2, %4};\n\t"
+                 "@e tcgen05.mma.cta_group::1.kind::f16 [%0], x, y, %3, 0;\n\t"
+                 "add.s64 x, x, 2;\n\tadd.s64 y, y, 2;\n\t@e tcgen05.mma.cta_group::1.kind::f16 [%0], x, y, %3, 1;\n\t"
+                 "add.s64 x, x, 2;\n\tadd.s64 y, y, 2;\n\t@e tcgen05.mma.cta_group::1.kind::f16 [%0], x, y, %3, 1;\n\t"
+                 "add.s64 x, x, 2;\n\tadd.s64 y, y, 2;\n\t@e tcgen05.mma.cta_group::1.kind::f16 [%0], x, y, %3, 1;\n\t"
+                 "add.s64 x, x, %5;\n\tadd.s64 y, y, %5;\n\t@e tcgen05.mma.cta_group::1.kind::f16 [%0], x, y, %3, 1;\n\t"
+                 "add.s64 x, x, 2;\n\tadd.s64 y, y, 2;\n\t@e tcgen05.mma.cta_group::1.kind::f16 [%0], x, y, %3, 1;\n\t"
+                 "add.s64 x, x, 2;\n\tadd.s64 y, y, 2;\n\t@e tcgen05.mma.cta_group::1.kind::f16 [%0], x, y, %3, 1;\n\t"
+                 "add.s64 x, x, 2;\n\tadd.s64 y, y, 2;\n\t@e tcgen05.mma.cta_group::1.kind::f16 [%0], x, y, %3, 1;\n\t}"
+                 ::"r"(d), "r"(q), "r"(k), "r"(idesc), "n"(kPDescUpper), "n"((kPPanel >> 4) - 6) : "memory");
+}
+__device__ __forceinline__ void prompt_o(uint32_t d, uint32_t p, uint32_t v, uint32_t idesc, bool add) {
+    asm volatile("{\n\t.reg .pred p, e;\n\t.reg .b64 y;\n\t.reg .b32 x;\n\telect.sync _|e, 0xffffffff;\n\tmov.b64 y, {%2, %4};\n\tsetp.ne.u32 p, %5, 0;\n\t"
+                 "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], y, %3, p;\n\t"
+                 "add.u32 x, %1, 8;\n\tadd.s64 y, y, 128;\n\t@e tcgen05.mma.cta_group::1.kind::f16 [%0], [x], y, %3, 1;\n\t"
+                 "add.u32 x, %1, 16;\n\tadd.s64 y, y, 128;\n\t@e tcgen05.mma.cta_group::1.kind::f16 [%0], [x], y, %3, 1;\n\t"
+                 "add.u32 x, %1, 24;\n\tadd.s64 y, y, 128;\n\t@e tcgen05.mma.cta_group::1.kind::f16 [%0], [x], y, %3, 1;\n\t"
+                 "add.u32 x, %1, 32;\n\tadd.s64 y, y, 128;\n\t@e tcgen05.mma.cta_group::1.kind::f16 [%0], [x], y, %3, 1;\n\t"
+                 "add.u32 x, %1, 40;\n\tadd.s64 y, y, 128;\n\t@e tcgen05.mma.cta_group::1.kind::f16 [%0], [x], y, %3, 1;\n\t"
+                 "add.u32 x, %1, 48;\n\tadd.s64 y, y, 128;\n\t@e tcgen05.mma.cta_group::1.kind::f16 [%0], [x], y, %3, 1;\n\t"
+                 "add.u32 x, %1, 56;\n\tadd.s64 y, y, 128;\n\t@e tcgen05.mma.cta_group::1.kind::f16 [%0], [x], y, %3, 1;\n\t}"
+                 ::"r"(d), "r"(p), "r"(v), "r"(idesc), "n"(kPDescUpper), "r"((uint32_t)add) : "memory");
+}
+__device__ __forceinline__ bool prompt_wait_slow(uint32_t bar, uint32_t parity) { return mbar_wait_bounded(bar, parity); }
 
 template <int P, bool N16>
 __global__ void __launch_bounds__(kPThreads, 1) ragged_umma(const RaggedArgs a) {
@@ -91,26 +133,30 @@ __global__ void __launch_bounds__(kPThreads, 1) ragged_umma(const RaggedArgs a) 
     extern __shared__ __align__(1024) uint8_t smem[];
     __shared__ int s_scan[kPThreads / 32];
     __shared__ uint32_t s_tmem;
+    __shared__ RaggedCursor s_at[8];         // of each warp of rows, while it needs its registers
+    __shared__ int64_t s_rows[16][8];        // of a tile, by its number mod 16: the plane's row of every 16th token, -1: not to be read
+    __shared__ int s_flags[16];      // of a tile: 1 it begins a run, 2 its entry has rows in half 1, 4 it ends a run
     int (&s_items)[kMaxPagedBatch + 1] = *reinterpret_cast<int (*)[kMaxPagedBatch + 1]>(smem);      // (until rows come here)
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const uint32_t base = smem_u32(smem), bars = base + kPEnd;
-    auto b_kf = [&](int s) { return bars + 8 * s; };            // K of a stage converted
-    auto b_ke = [&](int s) { return bars + 16 + 8 * s; };       //   and used
-    auto b_vf = [&](int s) { return bars + 32 + 8 * s; };
-    auto b_ve = [&](int s) { return bars + 48 + 8 * s; };
-    auto b_s = [&](int h) { return bars + 64 + 8 * h; };        // S of a half done
-    auto b_p = [&](int h) { return bars + 80 + 8 * h; };        // P written
-    auto b_o = [&](int h) { return bars + 96 + 8 * h; };        // O done
-    auto b_q = [&](int h) { return bars + 112 + 8 * h; };       // pi(Q) of a run there
+    const uint32_t base = smem_u32(smem), bars = base + kPBars;
+    // step j of a block: K of its tile j and V of its tile j - 1
+    auto b_full = [&](int j) { return bars + 8 * (j & 1); };                    // both converted
+    auto b_s = [&](int h, int j) { return bars + 16 + 16 * h + 8 * (j & 1); };  // S of tile j, half h done; h = 1: all of step j
+    auto b_p = [&](int h) { return bars + 48 + 8 * h; };                        // P of a half written
+    auto b_o = [&](int h) { return bars + 64 + 8 * h; };                        // O of a run done
+    auto b_q = [&](int h) { return bars + 80 + 8 * h; };                        // pi(Q) of a run there
+    auto b_plan = [&](int i) { return bars + 96 + 8 * ((i >> 3) & 1); };        // rows and flags of tile i and its batch of eight there
+    auto b_used = [&](int i) { return bars + 112 + 8 * ((i >> 3) & 1); };       //   and used
     if (tid == 0) {
         for (int i = 0; i < 2; ++i) {
-            mbar_init(b_kf(i), 4); mbar_init(b_ke(i), 1); mbar_init(b_vf(i), 4); mbar_init(b_ve(i), 1);
-            mbar_init(b_s(i), 1); mbar_init(b_p(i), 4); mbar_init(b_o(i), 1); mbar_init(b_q(i), 4);
+            mbar_init(b_full(i), 8); mbar_init(b_s(i, 0), 1); mbar_init(b_s(i, 1), 1);
+            mbar_init(b_p(i), 4); mbar_init(b_o(i), 1); mbar_init(b_q(i), 4);
+            mbar_init(b_plan(8 * i), 1); mbar_init(b_used(8 * i), 9);
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         fence_async_shared();
     }
-    if (warp == 12) tmem_alloc(smem_u32(&s_tmem), 512);
+    if (warp == 0) tmem_alloc(smem_u32(&s_tmem), 512);
     tmem_fence_before();
     __syncthreads();
     tmem_fence_after();
@@ -130,6 +176,11 @@ __global__ void __launch_bounds__(kPThreads, 1) ragged_umma(const RaggedArgs a) 
         ragged_next(a, c, kPRows, kPTile);
         return true;
     };
+    auto park = [&]() {
+        __syncwarp();
+        if (lane == 0) s_at[warp - 4] = c;
+        __syncwarp();
+    };
     auto two = [&]() { return c.s.n * a.group > c.rt * kPRows + 128; };       // does the entry have rows in half 1
     bool dead = false;                 // a wait ran out: no more waits, the flag is up, results are void
     auto wait = [&](uint32_t bar, int phase) {
@@ -139,49 +190,81 @@ __global__ void __launch_bounds__(kPThreads, 1) ragged_umma(const RaggedArgs a) 
         }
     };
 
-    if (warp == 12) {
-        // ================================================================ matrix instructions
-        constexpr uint32_t id_s = umma_idesc(128, 128, false, false), id_o = umma_idesc(128, 128, false, true);
-        const uint64_t qd = umma_desc<128>(base + kPQ, 16, 1024), kd = umma_desc<128>(base + kPK, 16, 1024);
-        const uint64_t vd = umma_desc<128>(base + kPV, kPPanel, 1024);
-        int n_run[2] = {0, 0}, n_tile[2] = {0, 0};        // runs and tiles of each half so far
-        auto qk = [&](int i, int h, bool first, bool last_half) {
-            if (first) wait(b_q(h), n_run[h]++);
-            if (h == 0) wait(b_kf(i & 1), i >> 1);
-            __syncwarp();
-            tmem_fence_after();
-#pragma unroll
-            for (int ks = 0; ks < 8; ++ks) {
-                const uint32_t step = ((ks >> 2) * kPPanel + (ks & 3) * 32) >> 4;
-                umma_ss(tm + 128 * h, qd + ((h * 32768) >> 4) + step, kd + (((i & 1) * 32768) >> 4) + step, id_s, ks > 0);
+    if (warp == 2 || warp == 3) {
+        regs_less<kPRegsRest>();
+    } else if (warp == 1) {
+        // ================================================================ what comes: rows and flags of the tiles, up to 16 ahead
+        // (one warp walks the tiles for the nine that only need to know where they are)
+        regs_less<kPRegsRest>();
+        bool first = true;
+        for (int i = 0; i < n_mine; ++i) {
+            if (i >= 16 && (i & 7) == 0) wait(b_used(i), (i >> 4) - 1);
+            if (lane < 8) {
+                // are any of the 16 tokens seen: they begin at `tok`, the last row sees up to p1, the first from p0 - window + 1 on
+                const int tok = ragged_token(c.v, c.k, kPTile) + 16 * lane;
+                int64_t row = -1;
+                if (tok <= c.v.p1 && (a.window == 0 || tok + 15 > c.v.p0 - a.window || tok < a.n_sink)) {
+                    const int page = token_page(a.map, c.b, tok);
+                    if (page >= 0) row = ((int64_t)page * H + c.hk) * a.fmt.max_seq + token_row(a.map, tok);
+                    else raise_flag(a.status, KVBFP_FLAG_POSITION);
+                }
+                s_rows[i & 15][lane] = row;
             }
-            umma_commit(b_s(h));
-            if (last_half) umma_commit(b_ke(i & 1));
-        };
-        auto pv = [&](int i, int h, bool first, bool last_half) {
-            if (h == 0) wait(b_vf(i & 1), i >> 1);
-            wait(b_p(h), n_tile[h]++);
-            __syncwarp();
-            tmem_fence_after();
-#pragma unroll
-            for (int ks = 0; ks < 8; ++ks)
-                umma_ts(tm + 256 + 128 * h, tm + 128 * h + ks * 8, vd + (((i & 1) * 32768 + ks * 2048) >> 4), id_o, ks > 0 || !first);
-            umma_commit(b_o(h));
-            if (last_half) umma_commit(b_ve(i & 1));
-        };
-        bool first = true, both = n_mine > 0 && two();
-        if (n_mine > 0) {
-            qk(0, 0, true, !both);
-            if (both) qk(0, 1, true, true);
+            int flags = (first ? 1 : 0) | (two() ? 2 : 0);
+            first = i + 1 == n_mine || next_tile();
+            if (first) flags |= 4;
+            if (lane == 0) s_flags[i & 15] = flags;
+            if ((i & 7) == 7 || i + 1 == n_mine) {
+                __syncwarp();
+                if (lane == 0) mbar_arrive(b_plan(i));
+            }
         }
-        for (int i = 0; i < n_mine && !__any_sync(0xffffffffu, dead); ++i) {
-            const bool more = i + 1 < n_mine, first_next = more && next_tile(), both_next = more && two();
-            pv(i, 0, first, !both);
-            if (more) qk(i + 1, 0, first_next, !both_next);
-            if (both) pv(i, 1, first, true);
-            if (both_next) qk(i + 1, 1, first_next, true);
-            first = first_next;
-            both = both_next;
+    } else if (warp == 0) {
+        // ================================================================ matrix instructions
+        // (one warp for both halves: their products alternate, and so the halves fall half a period apart)
+        regs_less<kPRegsRest>();
+        constexpr uint32_t id_s = umma_idesc(128, 128, false, false), id_o = umma_idesc(128, 128, false, true);
+        const int n = __shfl_sync(0xffffffffu, n_mine, 0);
+        const uint32_t tmu = __shfl_sync(0xffffffffu, tm, 0);
+        const uint32_t qd = prompt_desc(base + kPQ, 16), kd = prompt_desc(base + kPK, 16), vd = prompt_desc(base + kPV, kPPanel);
+        int runs = 0;                 // parities of the runs of the halves so far (bits 0 and 1)
+        int now = 0, next = 0;        // flags of tiles j - 1 and j
+        for (int j = 0; j <= n && n > 0; ++j) {
+            const int st = j & 1;
+            wait(b_full(j), j >> 1);
+            now = next;
+            next = 0;
+            if (j < n) {
+                if ((j & 7) == 0) wait(b_plan(j), j >> 4);
+                next = __shfl_sync(0xffffffffu, *(volatile int*)&s_flags[j & 15], 0);
+                if ((j & 7) == 7 && lane == 0) mbar_arrive(b_used(j));
+            }
+#pragma unroll 1
+            for (int h = 0; h < 2; ++h) {
+                const uint32_t tmh = tmu + 128 * h;
+                if (j > 0) {                             // O of tile j - 1
+                    wait(b_p(h), j - 1);
+                    __syncwarp();
+                    tmem_fence_after();
+                    if (h == 0 || (now & 2)) {
+                        prompt_o(tmh + 256, tmh, vd + ((st * 32768) >> 4), id_o, !(now & 1));
+                        if (now & 4) umma_commit(b_o(h));
+                    }
+                }
+                if (j < n) {                             // S of tile j
+                    if (h == 0 || (next & 2)) {
+                        if (next & 1) {
+                            wait(b_q(h), runs >> h);
+                            runs ^= 1 << h;
+                            __syncwarp();
+                            tmem_fence_after();
+                        }
+                        prompt_s(tmh, qd + ((h * 32768) >> 4), kd + ((st * 32768) >> 4), id_s);
+                    }
+                    umma_commit(b_s(h, j));
+                }
+            }
+            if (__any_sync(0xffffffffu, dead)) break;
         }
         if (__any_sync(0xffffffffu, dead)) {
             // let what was issued come to its end before the memory goes
@@ -189,26 +272,20 @@ __global__ void __launch_bounds__(kPThreads, 1) ragged_umma(const RaggedArgs a) 
             (void)mbar_wait_bounded(b_o(0), 0);
             (void)mbar_wait_bounded(b_o(0), 1);
         }
-    } else if (warp >= 8) {
+    } else if (warp >= 12) {
         // ================================================================ packed rows to bf16
+        regs_less<kPRegsConv>();
         const int r = tid & 127, row_e = D / a.fmt.block;
         const uint32_t sel = row_e == 4 ? 0x3210u : row_e == 2 ? 0x1100u : 0x0000u;
-        uint32_t kw[4][P], vw[4][P], ke[2] = {0, 0}, ve[2] = {0, 0};
-        int page = -1;                // of this thread's token of the next tile to load, -1: not seen by any row
-        auto look_up = [&]() {
-            page = -1;
-            const int tok = ragged_token(c.v, c.k, kPTile) + r;
-            if (tok <= c.v.p1 && (a.window == 0 || tok > c.v.p0 - a.window || tok < a.n_sink)) {
-                page = token_page(a.map, c.b, tok);
-                if (page < 0) raise_flag(a.status, KVBFP_FLAG_POSITION);
-            }
-        };
-        int64_t row = -1;             // the token's row in the planes, of the tile to load
-        auto to_row = [&]() {
-            const int tok = ragged_token(c.v, c.k, kPTile) + r;
-            row = page >= 0 ? ((int64_t)page * H + c.hk) * a.fmt.max_seq + token_row(a.map, tok) : -1;
-        };
-        auto load = [&](const uint8_t* mant, const uint8_t* exps, uint32_t (&w)[4][P], uint32_t (&e)[2]) {
+        const int plane = (warp - 12) >> 2;                  // K, V
+        const uint8_t *mant = plane ? a.v_mant : a.k_mant, *exps = plane ? a.v_exp : a.k_exp;
+        const uint32_t stages = base + (plane ? kPV : kPK);
+        uint32_t w[4][P], e[2] = {0, 0};
+        auto load = [&](int i) {             // this thread's row of tile i
+            if ((i & 7) == 0) wait(b_plan(i), i >> 4);
+            int64_t row = *(volatile int64_t*)&s_rows[i & 15][r >> 4];
+            __syncwarp();
+            if ((i & 7) == 7 && lane == 0) mbar_arrive(b_used(i));
             if (row < 0) {
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
@@ -217,6 +294,7 @@ __global__ void __launch_bounds__(kPThreads, 1) ragged_umma(const RaggedArgs a) 
                 e[0] = e[1] = 0u;
                 return;
             }
+            row += r & 15;
             const uint4* p = reinterpret_cast<const uint4*>(mant + row * ROW_M);
 #pragma unroll
             for (int x = 0; x < P; ++x) {
@@ -235,7 +313,7 @@ __global__ void __launch_bounds__(kPThreads, 1) ragged_umma(const RaggedArgs a) 
                 e[0] = row_e == 4 ? *reinterpret_cast<const uint32_t*>(q) : row_e == 2 ? *reinterpret_cast<const uint16_t*>(q) : *q;
             }
         };
-        auto convert = [&](uint32_t to, const uint32_t (&w)[4][P], const uint32_t (&e)[2]) {
+        auto convert = [&](uint32_t to) {
             const uint32_t eb = N16 ? 0u : prmt(e[0], 0u, sel);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
@@ -254,62 +332,68 @@ __global__ void __launch_bounds__(kPThreads, 1) ragged_umma(const RaggedArgs a) 
             fence_async_shared();
             __syncwarp();
         };
-        int ahead = 0;                // tiles whose row is known
-        auto step = [&]() {           // to the next tile's row; its successor's page is asked for
-            to_row();
-            if (++ahead < n_mine) {
-                (void)next_tile();
-                look_up();
-            }
-        };
-        if (n_mine > 0) {
-            look_up();
-            step();
-            load(a.k_mant, a.k_exp, kw, ke);
-            load(a.v_mant, a.v_exp, vw, ve);
-        }
+        if (n_mine > 0) load(0);
+        if (n_mine > 0 && plane && lane == 0) mbar_arrive(b_full(0));        // (no V in the first step, no K in the last)
         for (int i = 0; i < n_mine; ++i) {
-            const int st = i & 1;
-            const bool more = i + 1 < n_mine;
-            if (i >= 2) wait(b_ke(st), (i >> 1) - 1);
-            convert(base + kPK + st * 32768, kw, ke);
-            if (lane == 0) mbar_arrive(b_kf(st));
-            if (more) {
-                step();
-                load(a.k_mant, a.k_exp, kw, ke);
-            }
-            if (i >= 2) wait(b_ve(st), (i >> 1) - 1);
-            convert(base + kPV + st * 32768, vw, ve);
-            if (lane == 0) mbar_arrive(b_vf(st));
-            if (more) load(a.v_mant, a.v_exp, vw, ve);
+            const int j = i + plane;
+            if (j >= 2) wait(b_s(1, j), (j >> 1) - 1);
+            convert(stages + (j & 1) * 32768);
+            if (lane == 0) mbar_arrive(b_full(j));
+            if (i + 1 < n_mine) load(i + 1);
+        }
+        if (n_mine > 0 && !plane) {
+            if (n_mine >= 2) wait(b_s(1, n_mine), (n_mine >> 1) - 1);
+            if (lane == 0) mbar_arrive(b_full(n_mine));
         }
     } else {
         // ================================================================ rows
-        const int h = warp >> 2, w4 = warp & 3, r = tid & 127;                   // half, quarter of its rows, row
+        regs_more<kPRegsRows>();
+        const int h = (warp >> 2) - 1, w4 = warp & 3, r = tid & 127;                   // half, quarter of its rows, row
         const uint32_t tms = tm + 128 * h + ((uint32_t)w4 << 21), tmo = tms + 256;      // lane field: 32 * quarter << 16
         const uint32_t q_at = base + kPQ + h * 32768;
         const float mul = finite_factor(a.scale * kValueUp * 1.4426950408889634f);      // scores to log2 units
         int4 rec = make_int4(-1, 0, 0, 0);
-        // pi(Q) of the entry at the cursor, this warp's 32 rows: a lane has four positions
+        // This lane's row of q among the warp's 32 rows of the entry at a cursor (NULL: behind the last)
+        auto q_row = [&](const RaggedCursor& e) -> const uint8_t* {
+            const int row = e.rt * kPRows + h * 128 + w4 * 32 + lane, i = row / a.group;
+            if (row >= e.s.n * a.group) return nullptr;
+            return static_cast<const uint8_t*>(a.q) + ((int64_t)(e.s.start + i) * a.n_q_heads + e.hk * a.group + row - i * a.group) * (2 * D);
+        };
+        // pi(Q) of the entry at the cursor, this warp's 32 rows: as they are first, then slot by slot (a lane has four positions)
         auto write_q = [&]() {
-            const int row0 = c.rt * kPRows + h * 128 + w4 * 32, R = c.s.n * a.group;
+            const uint64_t mine = reinterpret_cast<uint64_t>(q_row(c));
+#pragma unroll
+            for (int x = 0; x < 32; x += 2) {
+                const uint64_t src = __shfl_sync(0xffffffffu, mine, x + (lane >> 4));
+                const uint32_t dst = q_at + prompt_place(w4 * 32 + x + (lane >> 4), lane & 15);
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src ? src + (lane & 15) * 16 : reinterpret_cast<uint64_t>(a.q)), "r"(src ? 16 : 0) : "memory");
+            }
+            asm volatile("cp.async.commit_group;" ::: "memory");
             int ch[4];
 #pragma unroll
             for (int x = 0; x < 4; ++x) {
                 const int slot = prompt_slot<P>(4 * lane + x);
                 ch[x] = a.perm_k ? a.perm_k[c.hk * D + slot] & (D - 1) : slot;
             }
-            const unsigned short* q = static_cast<const unsigned short*>(a.q);
+            {          // the rows of the run after this one on their way to the L2 cache
+                RaggedCursor e = c;
+                ragged_next(a, e, kPRows, kPTile);
+                if (e.b < a.batch) {
+                    const uint8_t* p = q_row(e);
+                    if (p) asm volatile("prefetch.global.L2 [%0];\n\tprefetch.global.L2 [%0+128];" ::"l"(p));
+                }
+            }
+            asm volatile("cp.async.wait_group 0;" ::: "memory");
+            __syncwarp();
 #pragma unroll 1
             for (int x0 = 0; x0 < 32; x0 += 8) {
                 uint32_t v[8][4];
 #pragma unroll
-                for (int x = 0; x < 8; ++x) {
-                    const int row = row0 + x0 + x, i = row / a.group;
-                    const unsigned short* p = q + ((int64_t)(c.s.start + i) * a.n_q_heads + c.hk * a.group + row - i * a.group) * D;
+                for (int x = 0; x < 8; ++x)
 #pragma unroll
-                    for (int y = 0; y < 4; ++y) v[x][y] = row < R ? p[ch[y]] : 0u;
-                }
+                    for (int y = 0; y < 4; ++y)
+                        asm volatile("ld.shared.u16 %0, [%1];" : "=r"(v[x][y]) : "r"(q_at + prompt_place(w4 * 32 + x0 + x, ch[y] >> 3) + (ch[y] & 7) * 2) : "memory");
+                __syncwarp();
 #pragma unroll
                 for (int x = 0; x < 8; ++x) {
                     const uint32_t at = q_at + prompt_place(w4 * 32 + x0 + x, lane >> 1) + (lane & 1) * 8;
@@ -320,7 +404,20 @@ __global__ void __launch_bounds__(kPThreads, 1) ragged_umma(const RaggedArgs a) 
             __syncwarp();
             if (lane == 0) mbar_arrive(b_q(h));
         };
-        int n_tile = 0;               // tiles of this half so far
+        // 128 bytes of this warp's rows from shared memory to where each lane's row goes (0: nowhere), whole lines at a time
+        const uint32_t line = base + kPOut + (warp - 4) * 4096;
+        auto flush = [&](uint64_t to) {
+            __syncwarp();
+#pragma unroll
+            for (int x = 0; x < 32; x += 4) {
+                const int row = x + (lane >> 3);
+                const uint64_t p = __shfl_sync(0xffffffffu, to, row);
+                const uint4 v = lds128(line + row * 128 + (((lane & 7) ^ (row & 7)) << 4));
+                if (p) reinterpret_cast<uint4*>(p)[lane & 7] = v;
+            }
+            __syncwarp();
+        };
+        int n_run = 0;                // runs of this half so far
         if (n_mine > 0 && (h == 0 || two())) write_q();
         for (int it = 0; it < n_mine;) {
             // ---- a run: tiles [k0, k1) of one entry
@@ -330,95 +427,96 @@ __global__ void __launch_bounds__(kPThreads, 1) ragged_umma(const RaggedArgs a) 
             const int pos = c.s.base + min(row, R - 1) / a.group;
             const int pos_lo = c.s.base + min(row - r, R - 1) / a.group, pos_hi = c.s.base + min(row - r + 127, R - 1) / a.group;
             const int see_lo = a.window > 0 ? pos - a.window + 1 : 0;
-            float m = -3.4028235e38f;
-            F2 l2 = f2(0.f, 0.f);
-            if (here) {
-                for (int k = k0; k < k1; ++k, ++n_tile) {
-                    const int tt = ragged_token(c.v, k, kPTile);
-                    wait(b_s(h), n_tile);
-                    __syncwarp();
-                    tmem_fence_after();
+            const int v_np = c.v.np, v_lo = c.v.lo;
+            float m = -3.4028235e38f, l = 0.f;
+            park();
+            for (int k = k0; k < k1; ++k) {
+                const int tt = (k < v_np ? k : k - v_np + v_lo) * kPTile, tile = it + k - k0;
+                wait(b_s(h, tile), tile >> 1);
+                __syncwarp();
+                tmem_fence_after();
+                if (here) {
                     const bool clear = tt + 127 <= pos_lo && (a.window == 0 || tt > pos_hi - a.window || tt + 128 <= a.n_sink);
-                    if (!clear) {
-#pragma unroll 1
-                        for (int j = 0; j < 4; ++j) {
-                            uint32_t s[32];
-                            tmem_ld<32>(tms + 32 * j, s);
-                            const int t0 = tt + 32 * j;
-                            // bits of the tokens seen: up to pos, from see_lo on or among the first ones
-                            auto below = [](int n) { return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u; };
-                            const uint32_t see = below(pos - t0 + 1) & (~below(see_lo - t0) | below(a.n_sink - t0));
-                            tmem_wait_ld(s);
-#pragma unroll
-                            for (int e = 0; e < 32; ++e) s[e] = (see >> e) & 1u ? s[e] : 0xff800000u;
-                            tmem_st<32>(tms + 32 * j, s);
-                        }
-                        tmem_wait_st();
-                    }
-                    float top = -INFINITY;
-                    {
-                        uint32_t s[2][32];
-                        tmem_ld<32>(tms, s[0]);
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            tmem_wait_ld(s[j & 1]);
-                            if (j < 3) tmem_ld<32>(tms + 32 * (j + 1), s[(j + 1) & 1]);
-                            float t0 = __uint_as_float(s[j & 1][0]), t1 = __uint_as_float(s[j & 1][1]);
-#pragma unroll
-                            for (int e = 2; e < 32; e += 4) {
-                                t0 = max3(t0, __uint_as_float(s[j & 1][e]), __uint_as_float(s[j & 1][e + 1]));
-                                if (e + 3 < 32) t1 = max3(t1, __uint_as_float(s[j & 1][e + 2]), __uint_as_float(s[j & 1][e + 3]));
-                            }
-                            top = max3(top, t0, t1);
-                        }
-                    }
-                    top *= mul;
-                    const bool grow = top > m + 8.f;
-                    if (__any_sync(0xffffffffu, grow)) {
-                        const float x = fmaxf(m, top), al = ex2_approx(m - x);
-                        m = x;
-                        l2 = f2_mul(l2, f2(al, al));
-                        if (k > k0) {
-                            wait(b_o(h), n_tile - 1);
-                            __syncwarp();
-                            tmem_fence_after();
-#pragma unroll 1
-                            for (int j = 0; j < 4; ++j) {
-                                uint32_t o[32];
-                                tmem_ld<32>(tmo + 32 * j, o);
-                                tmem_wait_ld(o);
-#pragma unroll
-                                for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * al);
-                                tmem_st<32>(tmo + 32 * j, o);
-                            }
-                            tmem_wait_st();
-                        }
-                    }
-                    const F2 mul2 = f2(mul, mul), neg2 = f2(-m, -m);
+                    // 32 tokens at a time, the next ones on their way.  P is formed under the reference there is; where a score
+                    // passes it by kPSlack (a run's first tokens, hardly ever else) the reference is raised and the scores, which
+                    // are still there, are read again.
                     uint32_t s[2][32];
                     tmem_ld<32>(tms, s[0]);
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        tmem_wait_ld(s[j & 1]);
+                        uint32_t (&v)[32] = s[j & 1];
+                        tmem_wait_ld(v);
                         if (j < 3) tmem_ld<32>(tms + 32 * (j + 1), s[(j + 1) & 1]);
                         uint32_t p[16];
+                        F2 sum;
+                        auto form = [&]() {          // P of the 32 scores; the largest score, in log2 units
+                            if (!clear) {            // hidden ones -inf: tokens up to pos are seen, from see_lo on or among the first ones
+                                const int t0 = tt + 32 * j;
+                                auto below = [](int n) { return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u; };
+                                const uint32_t see = below(pos - t0 + 1) & (~below(see_lo - t0) | below(a.n_sink - t0));
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) {
-                            float x0, x1;
-                            f2_split(f2_fma(f2(__uint_as_float(s[j & 1][2 * e]), __uint_as_float(s[j & 1][2 * e + 1])), mul2, neg2), x0, x1);
-                            x0 = ex2_approx(x0);
-                            x1 = ex2_approx(x1);
-                            l2 = f2_add(l2, f2(x0, x1));
-                            p[e] = pack_bf16x2_rn(x0, x1);
+                                for (int e = 0; e < 32; ++e) v[e] = (see >> e) & 1u ? v[e] : 0xff800000u;
+                            }
+                            const F2 mul2 = f2(mul, mul), neg2 = f2(-m, -m);
+                            float t[2] = {-INFINITY, -INFINITY};
+                            F2 sums[2] = {f2(0.f, 0.f), f2(0.f, 0.f)};
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) {
+                                const float s0 = __uint_as_float(v[2 * e]), s1 = __uint_as_float(v[2 * e + 1]);
+                                float x0, x1;
+                                f2_split(f2_fma(f2(s0, s1), mul2, neg2), x0, x1);
+                                t[e & 1] = max3(t[e & 1], s0, s1);
+                                x0 = ex2_approx(x0);
+                                x1 = ex2_approx(x1);
+                                sums[e & 1] = f2_add(sums[e & 1], f2(x0, x1));
+                                p[e] = pack_bf16x2_rn(x0, x1);
+                            }
+                            sum = f2_add(sums[0], sums[1]);
+                            return mul * fmaxf(t[0], t[1]);
+                        };
+                        const float top = form();
+                        if (__any_sync(0xffffffffu, top > m + kPSlack)) {
+                            // (whole numbers, so that what is there is scaled by a power of two)
+                            const float y = fmaxf(m, ceilf(top)), al = ex2_approx(m - y);
+                            m = y;
+                            l *= al;
+                            if (k > k0) {         // O is at rest: S came behind all products before it
+#pragma unroll 1
+                                for (int x = 0; x < 16; ++x) {
+                                    uint32_t o[8];
+                                    tmem_ld<8>(tmo + 8 * x, o);
+                                    tmem_wait_ld(o);
+#pragma unroll
+                                    for (int e = 0; e < 8; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * al);
+                                    tmem_st<8>(tmo + 8 * x, o);
+                                }
+                            }
+                            const uint32_t al2 = pack_bf16x2_rn(al, al);
+#pragma unroll 1
+                            for (int x = 0; x < 2 * j; ++x) {          // and P of this tile's tokens before
+                                uint32_t o[8];
+                                tmem_ld<8>(tms + 8 * x, o);
+                                tmem_wait_ld(o);
+#pragma unroll
+                                for (int e = 0; e < 8; ++e) o[e] = mul_bf16x2(o[e], al2);
+                                tmem_st<8>(tms + 8 * x, o);
+                            }
+                            tmem_ld<32>(tms + 32 * j, v);
+                            tmem_wait_ld(v);
+                            (void)form();
                         }
                         tmem_st<16>(tms + 16 * j, p);
+                        float a0, a1;
+                        f2_split(sum, a0, a1);
+                        l += a0 + a1;
                     }
                     tmem_wait_st();
-                    tmem_fence_before();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(b_p(h));
                 }
+                tmem_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(b_p(h));
             }
+            c = s_at[warp - 4];
             it += k1 - k0;
             // ---- the run's result; pi(Q) of the next run first where it need not wait for it
             const bool whole = k0 == 0 && k1 == n_tiles;
@@ -433,12 +531,12 @@ __global__ void __launch_bounds__(kPThreads, 1) ragged_umma(const RaggedArgs a) 
             const bool staged = whole && a.inv_perm_v != nullptr;
             if (next_here && !staged) write_q();
             if (here) {
-                float la, lb;
-                f2_split(l2, la, lb);
-                const float l = la + lb, inv = l != 0.f ? kValueUp / l : 0.f;
-                wait(b_o(h), n_tile - 1);
+                const float inv = l != 0.f ? kValueUp / l : 0.f;
+                wait(b_o(h), n_run++);
                 __syncwarp();
                 tmem_fence_after();
+                const uint32_t my_line = line + lane * 128;
+                const uint64_t to = !wanted ? 0 : whole ? reinterpret_cast<uint64_t>(static_cast<__nv_bfloat16*>(a.out) + out_row * D) : reinterpret_cast<uint64_t>(part);
 #pragma unroll 1
                 for (int j = 0; j < 4; ++j) {
                     uint32_t o[32];
@@ -450,19 +548,17 @@ __global__ void __launch_bounds__(kPThreads, 1) ragged_umma(const RaggedArgs a) 
 #pragma unroll
                         for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(o[8 * x + prompt_pos<P>(e)]);
                         if (!whole) {
-                            if (wanted) {
-                                float4* to = reinterpret_cast<float4*>(part + 32 * j + 8 * x);
-                                to[0] = make_float4(v[0], v[1], v[2], v[3]);
-                                to[1] = make_float4(v[4], v[5], v[6], v[7]);
-                            }
+                            sts128(my_line + (((2 * x) ^ (lane & 7)) << 4), __float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+                            sts128(my_line + (((2 * x + 1) ^ (lane & 7)) << 4), __float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7]));
                             continue;
                         }
 #pragma unroll
                         for (int e = 0; e < 8; ++e) v[e] = l != 0.f ? v[e] * inv : 0.f;
-                        const uint32_t y0 = pack_bf16x2_rn(v[0], v[1]), y1 = pack_bf16x2_rn(v[2], v[3]), y2 = pack_bf16x2_rn(v[4], v[5]), y3 = pack_bf16x2_rn(v[6], v[7]);
-                        if (staged) sts128(q_at + prompt_place(r, 4 * j + x), y0, y1, y2, y3);
-                        else if (wanted) reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(a.out) + out_row * D)[4 * j + x] = make_uint4(y0, y1, y2, y3);
+                        const uint32_t at = staged ? q_at + prompt_place(r, 4 * j + x) : my_line + (((4 * (j & 1) + x) ^ (lane & 7)) << 4);
+                        sts128(at, pack_bf16x2_rn(v[0], v[1]), pack_bf16x2_rn(v[2], v[3]), pack_bf16x2_rn(v[4], v[5]), pack_bf16x2_rn(v[6], v[7]));
                     }
+                    if (!whole) flush(to ? to + 128 * j : 0);
+                    else if (!staged && (j & 1)) flush(to ? to + 64 * (j - 1) : 0);
                 }
                 tmem_fence_before();
                 if (!whole && wanted) {
@@ -476,26 +572,25 @@ __global__ void __launch_bounds__(kPThreads, 1) ragged_umma(const RaggedArgs a) 
                     for (int x = 0; x < 4; ++x) sl[x] = a.inv_perm_v[hk * D + 4 * lane + x] & (D - 1);
 #pragma unroll 1
                     for (int x = 0; x < 32; ++x) {
-                        const int64_t to = __shfl_sync(0xffffffffu, out_row, x);
+                        const uint64_t p = __shfl_sync(0xffffffffu, to, x);
                         uint32_t v[4];
 #pragma unroll
                         for (int y = 0; y < 4; ++y)
                             asm volatile("ld.shared.u16 %0, [%1];" : "=r"(v[y]) : "r"(q_at + prompt_place(w4 * 32 + x, sl[y] >> 3) + (sl[y] & 7) * 2) : "memory");
-                        if (__shfl_sync(0xffffffffu, (int)wanted, x))
-                            *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(a.out) + to * D + 4 * lane) = make_uint2(v[0] | v[1] << 16, v[2] | v[3] << 16);
+                        if (p) reinterpret_cast<uint2*>(p)[lane] = make_uint2(v[0] | v[1] << 16, v[2] | v[3] << 16);
                     }
                     __syncwarp();
                 }
             }
             if (next_here && staged) write_q();
         }
-        if (tid == 0) a.rec[me] = rec;
+        if (tid == 128) a.rec[me] = rec;
     }
     __syncwarp();
     tmem_fence_before();
     __syncthreads();
     tmem_fence_after();
-    if (warp == 12) tmem_dealloc(tm, 512);
+    if (warp == 0) tmem_dealloc(tm, 512);
     pdl_trigger();
 }
 
