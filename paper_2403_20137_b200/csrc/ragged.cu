@@ -106,6 +106,9 @@ inline size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
 // Sequences of up to kFewRows bf16 query rows per kv head go to ragged_rows (every eight rows read the cache anew), longer ones
 // to ragged_umma (256 rows a pass).
 constexpr int kFewRows = 8;
+// What beginning and ending an entry costs ragged_umma, in tiles: 14 000 cycles (pi(Q), the first scores, the results) against
+// 4700 a tile.
+constexpr int kEntryTiles = 3;
 struct Kernel {
     int rows_tile, tile, max_workers;
 };
@@ -130,12 +133,13 @@ kvbfp_status launch_kernel(RaggedArgs a, bool umma, int64_t rows, uint8_t* works
     const int bits = a.fmt.mant_bits;
     const Kernel k = kernel_of(umma, bits);
     (void)lay_out(k, rows, &a, workspace);
-    const int64_t most = (rows / k.rows_tile + a.batch) * a.fmt.n_kv_heads * (a.map.cap / k.tile + 2);
+    const int64_t most = (rows / k.rows_tile + a.batch) * a.fmt.n_kv_heads * (a.map.cap / k.tile + 2 + kEntryTiles);
     const int per_block = umma ? 1 : kAttnWarps;
     int64_t grid = (int64_t)n_sm * (umma ? 1 : attn_rows_blocks(a.q_is_bf16));
     if (grid * per_block > k.max_workers) grid = k.max_workers / per_block;
     if (grid > most) grid = most;
     a.workers = (int)grid * per_block;
+    a.extra = umma ? kEntryTiles : 0;
     kvbfp_status st;
     if (umma) st = bits == 4 ? launch_ragged_umma4(a, (int)grid, s) : bits == 6 ? launch_ragged_umma6(a, (int)grid, s) : launch_ragged_umma8(a, (int)grid, s);
     else st = bits == 4 ? launch_ragged_rows4(a, (int)grid, s) : bits == 6 ? launch_ragged_rows6(a, (int)grid, s) : launch_ragged_rows8(a, (int)grid, s);
@@ -194,7 +198,7 @@ extern "C" kvbfp_status kvbfp_ragged_attn(const kvbfp_cache* cache, const kvbfp_
     a.out = out;
     const int64_t rows = (int64_t)n_tokens * group;
     // items are counted in 32 bits
-    if ((rows / 8 + batch) * f.n_kv_heads * (a.map.cap / 32 + 2) >= (int64_t)1 << 31) return KVBFP_ERR_UNSUPPORTED;
+    if ((rows / 8 + batch) * f.n_kv_heads * (a.map.cap / 32 + 2 + kEntryTiles) >= (int64_t)1 << 31) return KVBFP_ERR_UNSUPPORTED;
     st = status_word(&a.status);
     if (st != KVBFP_OK) return st;
     int n_sm = 0;

@@ -3,7 +3,8 @@
 //
 // The query rows of a (sequence, kv head) are its new tokens times the query heads of the group, token-major.  They are cut into
 // row tiles; an entry is a (sequence, row tile, kv head), its items are the cache tiles that any of its rows sees.  All items
-// (sequence, row tile, kv head, tile: the last fastest) are cut into one contiguous range per worker (attn.cuh); an entry that
+// (sequence, row tile, kv head, tile: the last fastest) are cut into one contiguous range per worker (attn.cuh), where an entry
+// may count for `extra` items more than it has (what beginning and ending it costs), which come before its first; an entry that
 // ends in another worker's range than it begins in leaves partial results, at most two a worker, which ragged_merge joins.
 #pragma once
 #include "attn.cuh"
@@ -28,6 +29,7 @@ struct RaggedArgs {
     int few_lo, few_hi;            // this kernel takes sequences of that many query rows per kv head: few_lo < rows <= few_hi
     int rows_tile;                 // rows of a row tile
     int part_rows;                 // rows of a partial
+    int extra;                     // items that an entry counts for on top of its tiles
     int workers;
     int4* rec;                     // workspace: per worker the entry that ends in its range's first run and began before it:
                                    // sequence, row tile, kv head, first worker (-1: none)
@@ -100,34 +102,42 @@ __device__ __forceinline__ void ragged_next(const RaggedArgs& a, RaggedCursor& c
         c.v = ragged_view(a, c.s, c.rt, rows_tile, tile);
     } while (c.v.n == 0);
 }
-// To item `at` of sequence b, which has it (whole warp).
-__device__ __forceinline__ void ragged_seek(const RaggedArgs& a, RaggedCursor& c, int b, int at, int rows_tile, int tile) {
+// To item `at` of sequence b, which has it (whole warp).  Returns where in its entry that is (below a.extra: before its first
+// tile, where the cursor stands then); `before`: the sequence's entries before it.
+__device__ __forceinline__ int ragged_seek(const RaggedArgs& a, RaggedCursor& c, int b, int at, int rows_tile, int tile, int& before) {
     const int lane = threadIdx.x & 31, H = a.fmt.n_kv_heads;
     c.b = b;
     c.s = ragged_seq(a, b);
     c.nrt = ragged_row_tiles(a, c.s, rows_tile);
     c.rt = 0;
+    before = 0;
     for (int r0 = 0; r0 < c.nrt; r0 += 32) {
-        int x = r0 + lane < c.nrt ? ragged_view(a, c.s, r0 + lane, rows_tile, tile).n * H : 0;
+        const int n = r0 + lane < c.nrt ? ragged_view(a, c.s, r0 + lane, rows_tile, tile).n : 0;
+        int x = n > 0 ? (n + a.extra) * H : 0;
         const int mine = x;
 #pragma unroll
         for (int off = 1; off < 32; off <<= 1) {
             const int y = __shfl_up_sync(0xffffffffu, x, off);
             if (lane >= off) x += y;
         }
-        const uint32_t past = __ballot_sync(0xffffffffu, x > at);
+        const uint32_t past = __ballot_sync(0xffffffffu, x > at), some = __ballot_sync(0xffffffffu, n > 0);
         if (past) {
             const int l = __ffs(past) - 1;
             c.rt = r0 + l;
             at -= __shfl_sync(0xffffffffu, x - mine, l);
+            before += __popc(some & ((1u << l) - 1u)) * H;
             break;
         }
         at -= __shfl_sync(0xffffffffu, x, 31);
+        before += __popc(some) * H;
     }
     c.v = ragged_view(a, c.s, c.rt, rows_tile, tile);
-    const int n = max(c.v.n, 1);
-    c.hk = at / n;
-    c.k = at - c.hk * n;
+    const int n = c.v.n + a.extra;
+    c.hk = at / max(n, 1);
+    at -= c.hk * n;
+    before += c.hk;
+    c.k = max(at - a.extra, 0);
+    return at;
 }
 
 // Rows at negative positions see nothing; lengths outside the cache are reported (both by one thread, they are rare).
@@ -136,21 +146,29 @@ static __device__ __noinline__ void ragged_edges(uint32_t* status, uint4* out, i
     for (int64_t i = 0; i < pieces; ++i) out[i] = make_uint4(0u, 0u, 0u, 0u);
 }
 
-// Items of every sequence, before it and in all: threads of a block together (THREADS of them).  s_items: room for 1024 + 1.
-// Afterwards s_items[b] holds the items before sequence b, s_items[batch] all.
+// Items and entries of every sequence, before it and in all: threads of a block together (THREADS of them).  s_items, s_entries:
+// room for 1024 + 1.  Afterwards entry b of them holds what comes before sequence b, entry `batch` all.
 template <int THREADS>
-__device__ __forceinline__ void ragged_count(const RaggedArgs& a, int (&s_items)[kMaxPagedBatch + 1], int (&s_scan)[THREADS / 32], int rows_tile, int tile) {
+__device__ __forceinline__ void ragged_count(const RaggedArgs& a, int* s_items, int* s_entries, int (&s_scan)[2][THREADS / 32], int rows_tile, int tile) {
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, H = a.fmt.n_kv_heads;
     constexpr int kAlone = 8;                                  // row tiles that a thread counts by itself
     bool many = false;
     for (int b = tid; b < a.batch; b += THREADS) {
         const RaggedSeq s = ragged_seq(a, b);
         const int nrt = ragged_row_tiles(a, s, rows_tile);
-        int x = 0;
-        if (nrt <= kAlone) for (int r = 0; r < nrt; ++r) x += ragged_view(a, s, r, rows_tile, tile).n;
-        else x = -1;
-        s_items[b] = x < 0 ? x : x * H;
-        many |= x < 0;
+        int x = 0, e = 0;
+        if (nrt <= kAlone) {
+            for (int r = 0; r < nrt; ++r) {
+                const int n = ragged_view(a, s, r, rows_tile, tile).n;
+                x += n;
+                e += n > 0;
+            }
+        } else {
+            e = -1;
+            many = true;
+        }
+        s_items[b] = (x + max(e, 0) * a.extra) * H;
+        s_entries[b] = e * H;
         if (blockIdx.x == 0 && nrt > 0 && (s.clamped || s.base < 0)) {
             const int64_t row = (int64_t)a.n_q_heads * kHeadDim * (a.q_is_bf16 ? 2 : 4) / 16;
             ragged_edges(a.status, reinterpret_cast<uint4*>(a.out) + s.start * row, (int64_t)min(s.n, max(-s.base, 0)) * row, s.clamped != 0);
@@ -158,43 +176,70 @@ __device__ __forceinline__ void ragged_count(const RaggedArgs& a, int (&s_items)
     }
     if (__syncthreads_or(many)) {
         for (int b = warp; b < a.batch; b += THREADS / 32) {
-            if (s_items[b] >= 0) continue;
+            if (s_entries[b] >= 0) continue;
             const RaggedSeq s = ragged_seq(a, b);
             const int nrt = ragged_row_tiles(a, s, rows_tile);
-            int x = 0;
-            for (int r = lane; r < nrt; r += 32) x += ragged_view(a, s, r, rows_tile, tile).n;
+            int x = 0, e = 0;
+            for (int r = lane; r < nrt; r += 32) {
+                const int n = ragged_view(a, s, r, rows_tile, tile).n;
+                x += n;
+                e += n > 0;
+            }
             x = __reduce_add_sync(0xffffffffu, x);
-            if (lane == 0) s_items[b] = x * H;
+            e = __reduce_add_sync(0xffffffffu, e);
+            if (lane == 0) {
+                s_items[b] = (x + e * a.extra) * H;
+                s_entries[b] = e * H;
+            }
         }
         __syncthreads();
     }
     const int per = (a.batch + THREADS - 1) / THREADS;
-    int mine = 0;
+    int x = 0, e = 0;
     for (int i = 0; i < per; ++i)
-        if (tid * per + i < a.batch) mine += s_items[tid * per + i];
-    int x = mine;
+        if (tid * per + i < a.batch) {
+            x += s_items[tid * per + i];
+            e += s_entries[tid * per + i];
+        }
+    const int mine_x = x, mine_e = e;
 #pragma unroll
     for (int off = 1; off < 32; off <<= 1) {
-        const int y = __shfl_up_sync(0xffffffffu, x, off);
-        if (lane >= off) x += y;
+        const int y = __shfl_up_sync(0xffffffffu, x, off), z = __shfl_up_sync(0xffffffffu, e, off);
+        if (lane >= off) {
+            x += y;
+            e += z;
+        }
     }
-    if (lane == 31) s_scan[warp] = x;
+    if (lane == 31) {
+        s_scan[0][warp] = x;
+        s_scan[1][warp] = e;
+    }
     __syncthreads();
-    x -= mine;
-    int total = 0;
+    x -= mine_x;
+    e -= mine_e;
+    int total_x = 0, total_e = 0;
 #pragma unroll
     for (int w = 0; w < THREADS / 32; ++w) {
-        if (w < warp) x += s_scan[w];
-        total += s_scan[w];
+        if (w < warp) {
+            x += s_scan[0][w];
+            e += s_scan[1][w];
+        }
+        total_x += s_scan[0][w];
+        total_e += s_scan[1][w];
     }
     for (int i = 0; i < per; ++i) {
         const int b = tid * per + i;
         if (b >= a.batch) break;
-        const int n = s_items[b];
+        const int nx = s_items[b], ne = s_entries[b];
         s_items[b] = x;
-        x += n;
+        s_entries[b] = e;
+        x += nx;
+        e += ne;
     }
-    if (tid == 0) s_items[a.batch] = total;
+    if (tid == 0) {
+        s_items[a.batch] = total_x;
+        s_entries[a.batch] = total_e;
+    }
     __syncthreads();
 }
 // The sequence that item `at` belongs to.
@@ -206,6 +251,7 @@ __device__ __forceinline__ int ragged_find(const RaggedArgs& a, const int* s_ite
     }
     return lo;
 }
+
 // ragged_rows: items of eight rows, a worker per warp
 kvbfp_status launch_ragged_rows4(const RaggedArgs& a, int grid, cudaStream_t s);
 kvbfp_status launch_ragged_rows6(const RaggedArgs& a, int grid, cudaStream_t s);

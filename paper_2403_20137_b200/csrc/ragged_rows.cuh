@@ -21,8 +21,8 @@ __global__ void __launch_bounds__(kAttnWarps * 32, attn_rows_blocks(!F32)) ragge
     constexpr int D = kHeadDim, ROW_M = G_::ROW_M, STAGES = G_::STAGES, TILE = G_::TILE, ROWS = kRows, SPLIT = F32 ? 3 : 1;
     constexpr int GROUP = 16 * ROW_M;
     extern __shared__ __align__(1024) uint8_t smem[];
-    __shared__ int s_scan[kAttnWarps];
-    int (&s_items)[kMaxPagedBatch + 1] = *reinterpret_cast<int (*)[kMaxPagedBatch + 1]>(smem);      // (until the copies begin)
+    __shared__ int s_scan[2][kAttnWarps];
+    int* s_items = reinterpret_cast<int*>(smem);      // (until the copies begin)
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
     const int row_e = D / a.fmt.block, exp_half = TILE * row_e;
     // mantissa tiles of all warps and stages first (whole swizzle periods), then the exponent bytes, then the rest
@@ -38,7 +38,7 @@ __global__ void __launch_bounds__(kAttnWarps * 32, attn_rows_blocks(!F32)) ragge
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
     pdl_wait();
-    ragged_count<kAttnWarps * 32>(a, s_items, s_scan, ROWS, TILE);
+    ragged_count<kAttnWarps * 32>(a, s_items, s_items + kMaxPagedBatch + 1, s_scan, ROWS, TILE);
     const int H = a.fmt.n_kv_heads, n_items = s_items[a.batch];
     const int workers = min(a.workers, n_items), me = blockIdx.x + gridDim.x * warp;      // neighbouring ranges on different SMs
     const int i0 = me < workers ? worker_start(me, n_items, workers) : 0;
@@ -53,7 +53,10 @@ __global__ void __launch_bounds__(kAttnWarps * 32, attn_rows_blocks(!F32)) ragge
         return;
     }
     RaggedCursor cc;
-    ragged_seek(a, cc, b_first, at_first, ROWS, TILE);
+    {
+        int before;
+        (void)ragged_seek(a, cc, b_first, at_first, ROWS, TILE, before);
+    }
 
     // ---- copies: the same items, STAGES ahead (every lane keeps the cursor; a lane per piece of a tile issues)
     RaggedCursor pc = cc;

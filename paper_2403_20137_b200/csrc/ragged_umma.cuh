@@ -131,12 +131,12 @@ template <int P, bool N16>
 __global__ void __launch_bounds__(kPThreads, 1) ragged_umma(const RaggedArgs a) {
     constexpr int D = kHeadDim, ROW_M = D * P / 8;
     extern __shared__ __align__(1024) uint8_t smem[];
-    __shared__ int s_scan[kPThreads / 32];
+    __shared__ int s_scan[2][kPThreads / 32];
     __shared__ uint32_t s_tmem;
     __shared__ RaggedCursor s_at[8];         // of each warp of rows, while it needs its registers
     __shared__ int64_t s_rows[16][8];        // of a tile, by its number mod 16: the plane's row of every 16th token, -1: not to be read
     __shared__ int s_flags[16];      // of a tile: 1 it begins a run, 2 its entry has rows in half 1, 4 it ends a run
-    int (&s_items)[kMaxPagedBatch + 1] = *reinterpret_cast<int (*)[kMaxPagedBatch + 1]>(smem);      // (until rows come here)
+    int *s_items = reinterpret_cast<int*>(smem), *s_entries = s_items + kMaxPagedBatch + 1;      // (until rows come here)
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const uint32_t base = smem_u32(smem), bars = base + kPBars;
     // step j of a block: K of its tile j and V of its tile j - 1
@@ -162,15 +162,26 @@ __global__ void __launch_bounds__(kPThreads, 1) ragged_umma(const RaggedArgs a) 
     tmem_fence_after();
     const uint32_t tm = __shfl_sync(0xffffffffu, s_tmem, 0);
     pdl_wait();
-    ragged_count<kPThreads>(a, s_items, s_scan, kPRows, kPTile);
+    ragged_count<kPThreads>(a, s_items, s_entries, s_scan, kPRows, kPTile);
     const int H = a.fmt.n_kv_heads, n_items = s_items[a.batch], me = blockIdx.x;
     const int workers = min(a.workers, n_items);
-    const int i0 = me < workers ? worker_start(me, n_items, workers) : 0;
-    const int n_mine = me < workers ? worker_start(me + 1, n_items, workers) - i0 : 0;
-    const int b_first = ragged_find(a, s_items, i0), at_first = i0 - s_items[b_first];
-    __syncthreads();
+    // this block's tiles: from its first item to its successor's
     RaggedCursor c;
-    if (n_mine > 0) ragged_seek(a, c, b_first, at_first, kPRows, kPTile);
+    int n_mine = 0, first_worker = 0;         // tiles; the worker that the entry of the first one begins in
+    if (me < workers) {
+        auto tiles_before = [&](int item, int& at) {
+            const int b = ragged_find(a, s_items, item);
+            int before;
+            at = ragged_seek(a, c, b, item - s_items[b], kPRows, kPTile, before);
+            return item - at + c.k - a.extra * (s_entries[b] + before);
+        };
+        int at;
+        n_mine = me + 1 < workers ? tiles_before(worker_start(me + 1, n_items, workers), at) : n_items - a.extra * s_entries[a.batch];
+        const int item = worker_start(me, n_items, workers);
+        n_mine -= tiles_before(item, at);
+        first_worker = worker_of(item - at + a.extra, n_items, workers);
+    }
+    __syncthreads();
     auto next_tile = [&]() {           // true: the next tile begins another run
         if (++c.k < c.v.n) return false;
         ragged_next(a, c, kPRows, kPTile);
@@ -520,7 +531,7 @@ __global__ void __launch_bounds__(kPThreads, 1) ragged_umma(const RaggedArgs a) 
             it += k1 - k0;
             // ---- the run's result; pi(Q) of the next run first where it need not wait for it
             const bool whole = k0 == 0 && k1 == n_tiles;
-            if (k0 > 0 && k1 == n_tiles) rec = make_int4(c.b, c.rt, c.hk, worker_of(i0 + it - n_tiles, n_items, workers));
+            if (k0 > 0 && k1 == n_tiles) rec = make_int4(c.b, c.rt, c.hk, first_worker);
             const int i = row / a.group, hk = c.hk;
             const bool wanted = here && row < R && (!whole || pos >= 0);
             const int64_t out_row = (int64_t)(c.s.start + i) * a.n_q_heads + hk * a.group + row - i * a.group;
