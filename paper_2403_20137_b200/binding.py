@@ -244,29 +244,44 @@ class Cache:
 
 class PagePool:
     """Page table, reference counts and lengths of the sequences of a paged cache (kvbfp_pages).  The pages themselves are a
-    Cache of n_pages "sequences" of page_tokens tokens, one per layer; one PagePool serves them all."""
+    Cache of n_pages "sequences" of page_tokens tokens, one per layer; one PagePool serves them all.  Its tensors are given
+    once; their contents change."""
 
     def __init__(self, batch, max_pages, n_pages, page_tokens, device="cuda"):
-        self.table = torch.full((batch, max_pages), -1, dtype=torch.int32, device=device)
-        self.refs = torch.zeros(n_pages, dtype=torch.int32, device=device)
-        self.lens = torch.zeros(batch, dtype=torch.int32, device=device)
-        self.n_pages, self.page_tokens = n_pages, page_tokens
+        self._set(torch.full((batch, max_pages), -1, dtype=torch.int32, device=device),
+                  torch.zeros(n_pages, dtype=torch.int32, device=device),
+                  torch.zeros(batch, dtype=torch.int32, device=device), n_pages, page_tokens)
 
     @classmethod
     def of(cls, table, refs, lens, n_pages, page_tokens):
         """Tables that are there already: i32 [batch, max_pages], [n_pages] (or None: attention and writes only), [batch]."""
-        pool = cls.__new__(cls)
-        pool.table, pool.n_pages, pool.page_tokens = _dev(table, torch.int32), n_pages, page_tokens
         if table.dim() != 2:
             raise ValueError(f"table: expected [batch, max_pages], got shape {tuple(table.shape)}")
-        pool.refs = _sized("refs", _dev(refs, torch.int32), (n_pages,))
-        pool.lens = _sized("lens", _dev(lens, torch.int32), (table.shape[0],))
+        pool = cls.__new__(cls)
+        pool._set(_dev(table, torch.int32), _sized("refs", _dev(refs, torch.int32), (n_pages,)),
+                  _sized("lens", _dev(lens, torch.int32), (table.shape[0],)), n_pages, page_tokens)
         return pool
 
-    def struct(self):
+    def _set(self, table, refs, lens, n_pages, page_tokens):
         p = lambda t: None if t is None else t.data_ptr()
-        return PagesStruct(self.table.shape[0], self.table.shape[1], self.n_pages, self.page_tokens, p(self.table),
-                           p(self.refs), p(self.lens))
+        self._tensors = (table, refs, lens)
+        self._struct = PagesStruct(table.shape[0], table.shape[1], n_pages, page_tokens, p(table), p(refs), p(lens))
+        self._ref = C.byref(self._struct)
+        self._where = {t.get_device() for t in self._tensors if t is not None}
+        self.batch, self.n_pages, self.page_tokens = table.shape[0], n_pages, page_tokens
+
+    table = property(lambda self: self._tensors[0])
+    refs = property(lambda self: self._tensors[1])
+    lens = property(lambda self: self._tensors[2])
+
+    def struct(self):
+        return self._struct
+
+    def on(self, dev):
+        """The struct for a call on device `dev`."""
+        if self._where != {dev}:
+            raise ValueError("expected the pool and all tensors on the current device")
+        return self._ref
 
 
 def calibrate(x, n_heads, head_dim, stat=STAT_MAXABS, stream=None):
@@ -318,9 +333,11 @@ def dequant_all(cache, which, n_tok, perm=None, t0=0, out_dtype=torch.float32, s
     (the layout append() takes)."""
     mant, exp8 = (cache.k_mant, cache.k_exp) if which == "k" else (cache.v_mant, cache.v_exp)
     f = cache.fmt
-    out = torch.empty(f.batch, n_tok, f.n_kv_heads, f.head_dim, dtype=out_dtype, device=mant.device)
-    _check(lib().kvbfp_dequant(C.byref(f), _ptr(mant), _ptr(exp8), -1, -1, t0, n_tok,
-                               _ptr(_dev(perm, torch.int32)), _ptr(out), _dt(out), _stream(stream)))
+    out = torch.empty((f.batch, n_tok, f.n_kv_heads, f.head_dim), dtype=out_dtype, device=mant.device)
+    rc = lib().kvbfp_dequant(C.byref(f), mant.data_ptr(), exp8.data_ptr(), -1, -1, t0, n_tok, _ptr(_dev(perm, torch.int32)),
+                             out.data_ptr(), _dt(out), _stream(stream))
+    if rc:
+        _check(rc)
     return out
 
 
@@ -538,90 +555,113 @@ def gather_rows(cache, index, count, src_base=None, dst=None, dst_base=None, str
                                    _ptr(_sized("dst_base", _dev(dst_base, torch.int32), (f.batch,))), _stream(stream)))
 
 
-def _pool_on_device(pool, *tensors):
+def _at(name, t, dtype, dev, shape=None):
+    """Pointer of an argument (None: none), which has to be a contiguous tensor of that type (and shape) on device `dev`."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.get_device() != dev or not t.is_contiguous() or (shape is not None and t.shape != shape):
+        _dev(t, dtype)
+        if t.get_device() != dev:
+            raise ValueError("expected the cache and all tensors on the current device")
+        _sized(name, t, shape)
+    return t.data_ptr()
+
+
+def _count(name, t, n):
+    if t is not None and t.numel() != n:
+        raise ValueError(f"{name}: expected {n} values, got {t.numel()}")
+
+
+def _here(cache, stream):
+    """(current device, which has to be the cache's; stream)"""
     dev = torch.cuda.current_device()
-    for t in (pool.table, pool.refs, pool.lens, *tensors):
-        if t is not None and t.get_device() != dev:
-            raise ValueError("expected the pool and all tensors on the current device")
-    return pool.struct()
+    if cache.k_mant.get_device() != dev:
+        raise ValueError("expected the cache and all tensors on the current device")
+    return dev, torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
+
+
+def _pool_call(pool, stream):
+    dev = torch.cuda.current_device()
+    return dev, torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream, pool.on(dev)
 
 
 def pages_free(pool, lo=None, hi=None, stream=None):
     """kvbfp_pages_free: the pages wholly inside tokens [lo, hi) (i32 [batch]; None: 0, no limit) of each sequence."""
-    n = (pool.table.shape[0],)
-    ps = _pool_on_device(pool, lo, hi)
-    _check(lib().kvbfp_pages_free(C.byref(ps), _ptr(_sized("lo", _dev(lo, torch.int32), n)),
-                                  _ptr(_sized("hi", _dev(hi, torch.int32), n)), _stream(stream)))
+    dev, st, ref = _pool_call(pool, stream)
+    n = (pool.batch,)
+    rc = lib().kvbfp_pages_free(ref, _at("lo", lo, torch.int32, dev, n), _at("hi", hi, torch.int32, dev, n), st)
+    if rc:
+        _check(rc)
 
 
 def pages_fork(pool, src, dst, stream=None):
     """kvbfp_pages_fork: sequence dst[i] shares the pages of sequence src[i] (i32 [n])."""
-    ps = _pool_on_device(pool, src, dst)
-    _check(lib().kvbfp_pages_fork(C.byref(ps), _ptr(_dev(src, torch.int32)),
-                                  _ptr(_sized("dst", _dev(dst, torch.int32), src.shape)), src.numel(), _stream(stream)))
+    dev, st, ref = _pool_call(pool, stream)
+    rc = lib().kvbfp_pages_fork(ref, _at("src", src, torch.int32, dev), _at("dst", dst, torch.int32, dev, src.shape), src.numel(), st)
+    if rc:
+        _check(rc)
 
 
 def pages_reserve(pool, more, pairs=None, stream=None):
     """kvbfp_pages_reserve -> pairs i32 [batch, 2]: the pages to be copied (pages_copy) before the tokens are written."""
-    n = pool.table.shape[0]
+    dev, st, ref = _pool_call(pool, stream)
+    n = pool.batch
+    at = _at("more", more, torch.int32, dev, (n,))
     if pairs is None:
-        pairs = _empty((n, 2), torch.int32, more.device, stream)
-    ps = _pool_on_device(pool, more, pairs)
-    _check(lib().kvbfp_pages_reserve(C.byref(ps), _ptr(_sized("more", _dev(more, torch.int32), (n,))),
-                                     _ptr(_sized("pairs", _dev(pairs, torch.int32), (n, 2))), _stream(stream)))
+        pairs = more.new_empty((n, 2)) if stream is None else _empty((n, 2), torch.int32, more.device, stream)
+    rc = lib().kvbfp_pages_reserve(ref, at, _at("pairs", pairs, torch.int32, dev, (n, 2)), st)
+    if rc:
+        _check(rc)
     return pairs
 
 
 def pages_compact(pool, dst=None, moves=None, count=None, workspace=None, stream=None):
     """kvbfp_pages_compact -> (moves i32 [n_pages, 2], count i32 [1]) for pages_copy.  dst: another PagePool, or None: in
     place."""
-    dev = pool.table.device
-    dst = pool if dst is None else dst
+    dev, st, ref = _pool_call(pool, stream)
+    where = pool.table.device
     if moves is None:
-        moves = _empty((pool.n_pages, 2), torch.int32, dev, stream)
+        moves = _empty((pool.n_pages, 2), torch.int32, where, stream)
     if count is None:
-        count = _empty((1,), torch.int32, dev, stream)
-    ps = _pool_on_device(pool, moves, count, workspace, dst.table, dst.refs, dst.lens)
-    ds = dst.struct()
+        count = _empty((1,), torch.int32, where, stream)
     if workspace is None:
-        workspace = _empty(int(lib().kvbfp_pages_workspace_bytes(C.byref(ps))), torch.uint8, dev, stream)
-    _check(lib().kvbfp_pages_compact(C.byref(ps), C.byref(ds), _ptr(_sized("moves", _dev(moves, torch.int32), (pool.n_pages, 2))),
-                                     _ptr(_sized("count", _dev(count, torch.int32), (1,))), _ptr(_dev(workspace, torch.uint8)),
-                                     workspace.numel(), _stream(stream)))
+        workspace = _empty(int(lib().kvbfp_pages_workspace_bytes(ref)), torch.uint8, where, stream)
+    _check(lib().kvbfp_pages_compact(ref, ref if dst is None else dst.on(dev), _at("moves", moves, torch.int32, dev, (pool.n_pages, 2)),
+                                     _at("count", count, torch.int32, dev, (1,)), _at("workspace", workspace, torch.uint8, dev),
+                                     workspace.numel(), st))
     return moves, count
 
 
 def pages_copy(cache, pairs, count=None, dst=None, stream=None):
     """kvbfp_pages_copy: page pairs[i, 0] of cache to page pairs[i, 1] of dst (None: cache itself); i32 [n, 2]."""
-    dst = cache if dst is None else dst
-    _same_device(cache, dst.k_mant, pairs, count)
+    dev, st = _here(cache, stream)
     if pairs.dim() != 2 or pairs.shape[1] != 2:
         raise ValueError(f"pairs: expected [n, 2], got shape {tuple(pairs.shape)}")
-    cs, ds = cache.struct(), dst.struct()
-    _check(lib().kvbfp_pages_copy(C.byref(cs), C.byref(ds), _ptr(_dev(pairs, torch.int32)), pairs.shape[0],
-                                  _ptr(_sized("count", _dev(count, torch.int32), (1,))), _stream(stream)))
+    cs = C.byref(cache.struct())
+    ds = cs
+    if dst is not None:
+        _here(dst, stream)
+        ds = C.byref(dst.struct())
+    rc = lib().kvbfp_pages_copy(cs, ds, _at("pairs", pairs, torch.int32, dev), pairs.shape[0], _at("count", count, torch.int32, dev, (1,)), st)
+    if rc:
+        _check(rc)
 
 
-def _rows(name, t, heads, head_dim):
-    """Rows [n, heads, head_dim] of tokens that may lie apart (heads densely): the stride from token to token."""
+def _rows(name, t, dtype, n, heads, head_dim, dev):
+    """Rows [n, heads, head_dim] of tokens that may lie apart (heads densely): pointer, stride from token to token."""
     if t is None:
-        return 0
-    if not t.is_cuda or t.dim() != 3 or (heads is not None and t.shape[1] != heads) or t.shape[2] != head_dim:
-        raise ValueError(f"{name}: expected a CUDA tensor [n_tokens, {'heads' if heads is None else heads}, {head_dim}]")
-    if t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != head_dim):
+        return None, 0
+    shape = t.shape
+    if t.dtype is not dtype or t.get_device() != dev or len(shape) != 3 or shape[0] != n or shape[1] != heads or shape[2] != head_dim:
+        if t.dtype is not dtype:
+            raise TypeError(f"{name}: expected {dtype}, got {t.dtype}")
+        if t.get_device() != dev:
+            raise ValueError("expected the cache and all tensors on the current device")
+        raise ValueError(f"{name}: expected shape {(n, heads, head_dim)}, got {tuple(shape)}")
+    step = t.stride()
+    if step[2] != 1 or (heads > 1 and step[1] != head_dim):
         raise ValueError(f"{name}: expected the heads of a token side by side")
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1] * head_dim
-
-
-def _ragged(cache, pool, starts, seq_lens):
-    """The sequences of a ragged call, and its pages' struct."""
-    n = cache.fmt.batch if pool is None else pool.table.shape[0]
-    _sized("starts", _dev(starts, torch.int32), (n + 1,))
-    _sized("seq_lens", _dev(seq_lens, torch.int32), (n,))
-    if pool is None:
-        return n, None
-    _same_device(cache, pool.table)
-    return n, pool.struct()
+    return t.data_ptr(), step[0] if n > 1 else heads * head_dim
 
 
 def norm_rope_append(cache, q, k, v, starts, seq_lens, q_weight=None, k_weight=None, eps=1e-6, theta=None, half_split=False,
@@ -629,30 +669,36 @@ def norm_rope_append(cache, q, k, v, starts, seq_lens, q_weight=None, k_weight=N
     """kvbfp_norm_rope_append: q [n, H_q, d], k, v [n, H_kv, d] (views of one array will do: heads side by side, any token
     stride) of the new tokens of a ragged batch -> q_out; k and v go to the cache (the pool's pages).  starts i32 [batch + 1],
     seq_lens i32 [batch]; weights f32 [d]; theta f64 [d / 2].  q None (or k and v): only the others."""
+    dev, st = _here(cache, stream)
     f = cache.fmt
     ref = q if q is not None else k
+    if ref.dim() != 3:
+        raise ValueError(f"{'q' if q is not None else 'k'}: expected [n, heads, head_dim], got shape {tuple(ref.shape)}")
+    n, hq, dtype, d, hk = ref.shape[0], 0 if q is None else q.shape[1], ref.dtype, f.head_dim, f.n_kv_heads
     dt = _dt(ref)
-    _same_device(cache, q, k, v, starts, seq_lens, q_weight, k_weight, theta, perm_k, perm_v, q_out)
-    strides = [_rows(name, t, heads, f.head_dim) for name, t, heads in (("q", q, None), ("k", k, f.n_kv_heads), ("v", v, f.n_kv_heads))]
-    for name, t in (("k", k), ("v", v)):
-        if t is not None and (t.dtype != ref.dtype or t.shape[0] != ref.shape[0]):
-            raise ValueError(f"{name}: expected the type and number of tokens of q")
-    _, ps = _ragged(cache, pool, starts, seq_lens)
-    if q is not None and q_out is None:
-        q_out = _empty(q.shape, q.dtype, q.device, stream)
-    if q_out is not None:
-        _sized("q_out", _dev(q_out, ref.dtype), () if q is None else q.shape)
-    for name, t, n in (("q_weight", q_weight, f.head_dim), ("k_weight", k_weight, f.head_dim), ("theta", theta, f.head_dim // 2),
-                       ("perm_k", perm_k, f.n_kv_heads * f.head_dim), ("perm_v", perm_v, f.n_kv_heads * f.head_dim)):
-        if t is not None and t.numel() != n:
-            raise ValueError(f"{name}: expected {n} values, got {t.numel()}")
-    cs = cache.struct()
-    _check(lib().kvbfp_norm_rope_append(C.byref(cs), None if ps is None else C.byref(ps), _ptr(q), strides[0], _ptr(k), strides[1],
-                                        _ptr(v), strides[2], dt, 0 if q is None else q.shape[1], ref.shape[0], _ptr(starts),
-                                        _ptr(seq_lens), _ptr(_dev(q_weight, torch.float32)), _ptr(_dev(k_weight, torch.float32)),
-                                        float(eps), _ptr(_dev(theta, torch.float64)), int(half_split),
-                                        _ptr(_dev(perm_k, torch.int32)), _ptr(_dev(perm_v, torch.int32)), _ptr(q_out),
-                                        _stream(stream)))
+    qp, qs = _rows("q", q, dtype, n, hq, d, dev)
+    kp, ks = _rows("k", k, dtype, n, hk, d, dev)
+    vp, vs = _rows("v", v, dtype, n, hk, d, dev)
+    if pool is None:
+        batch, ps = f.batch, None
+    else:
+        batch, ps = pool.batch, pool.on(dev)
+    if q_out is None and q is not None:
+        q_out = _empty(q.shape, dtype, q.device, stream)
+    if perm_k is not None:
+        _count("perm_k", perm_k, hk * d)
+    if perm_v is not None:
+        _count("perm_v", perm_v, hk * d)
+    rc = lib().kvbfp_norm_rope_append(C.byref(cache.struct()), ps, qp, qs, kp, ks, vp, vs, dt, hq, n,
+                                      _at("starts", starts, torch.int32, dev, (batch + 1,)),
+                                      _at("seq_lens", seq_lens, torch.int32, dev, (batch,)),
+                                      _at("q_weight", q_weight, torch.float32, dev, (d,)),
+                                      _at("k_weight", k_weight, torch.float32, dev, (d,)), eps,
+                                      _at("theta", theta, torch.float64, dev, (d // 2,)), 1 if half_split else 0,
+                                      _at("perm_k", perm_k, torch.int32, dev), _at("perm_v", perm_v, torch.int32, dev),
+                                      _at("q_out", q_out, dtype, dev, () if q is None else q.shape), st)
+    if rc:
+        _check(rc)
     return q_out
 
 
@@ -665,27 +711,34 @@ def ragged_attn(cache, q, starts, seq_lens, max_new, window=0, n_sink=0, perm_k=
                 pool=None, out=None, workspace=None, stream=None):
     """kvbfp_ragged_attn: q [n, H_q, d], the new tokens of a ragged batch, over the cache (the pool's pages) -> out of q's type.
     starts i32 [batch + 1]; seq_lens i32 [batch], the new tokens included; max_new: most new tokens of a sequence (a hint)."""
+    dev, st = _here(cache, stream)
     f = cache.fmt
-    q = _query(q, ("n", "H_q", "d"))
-    n_q_heads = q.shape[1]
-    if q.shape[2] != f.head_dim:
-        raise ValueError(f"q: shape {tuple(q.shape)} does not fit a cache of head_dim {f.head_dim}")
-    _same_device(cache, q, starts, seq_lens, perm_k, inv_perm_v, out, workspace)
-    for t in (perm_k, inv_perm_v):
-        if t is not None and t.numel() != f.n_kv_heads * f.head_dim:
-            raise ValueError(f"permutation: expected {f.n_kv_heads} x {f.head_dim} values, got {t.numel()}")
-    batch, ps = _ragged(cache, pool, starts, seq_lens)
+    shape = q.shape
+    if len(shape) != 3 or shape[2] != f.head_dim:
+        raise ValueError(f"q: expected [n, H_q, {f.head_dim}], got shape {tuple(shape)}")
+    n, n_q_heads, dtype = shape[0], shape[1], q.dtype
+    dt = _dt(q)
+    qp = _at("q", q, dtype, dev)
+    if pool is None:
+        batch, ps = f.batch, None
+    else:
+        batch, ps = pool.batch, pool.on(dev)
+    if perm_k is not None:
+        _count("perm_k", perm_k, f.n_kv_heads * f.head_dim)
+    if inv_perm_v is not None:
+        _count("inv_perm_v", inv_perm_v, f.n_kv_heads * f.head_dim)
     if out is None:
-        out = _empty(q.shape, q.dtype, q.device, stream)
-    _sized("out", _dev(out, q.dtype), q.shape)
+        out = torch.empty_like(q) if stream is None else _empty(shape, dtype, q.device, stream)
     if workspace is None:
-        workspace = _empty(int(lib().kvbfp_ragged_workspace_bytes(C.byref(f), batch, n_q_heads, q.shape[0])), torch.uint8, q.device, stream)
-    _dev(workspace, torch.uint8)
-    cs = cache.struct()
-    _check(lib().kvbfp_ragged_attn(C.byref(cs), None if ps is None else C.byref(ps), _ptr(q), _dt(q), n_q_heads, q.shape[0], batch,
-                                   _ptr(starts), _ptr(seq_lens), int(max_new), int(window), int(n_sink),
-                                   _ptr(_dev(perm_k, torch.int32)), _ptr(_dev(inv_perm_v, torch.int32)), float(softmax_scale),
-                                   _ptr(out), _ptr(workspace), workspace.numel(), _stream(stream)))
+        workspace = _empty(int(lib().kvbfp_ragged_workspace_bytes(C.byref(f), batch, n_q_heads, n)), torch.uint8, q.device, stream)
+    rc = lib().kvbfp_ragged_attn(C.byref(cache.struct()), ps, qp, dt, n_q_heads, n, batch,
+                                 _at("starts", starts, torch.int32, dev, (batch + 1,)),
+                                 _at("seq_lens", seq_lens, torch.int32, dev, (batch,)), max_new, window, n_sink,
+                                 _at("perm_k", perm_k, torch.int32, dev), _at("inv_perm_v", inv_perm_v, torch.int32, dev),
+                                 softmax_scale, _at("out", out, dtype, dev, shape),
+                                 _at("workspace", workspace, torch.uint8, dev), workspace.numel(), st)
+    if rc:
+        _check(rc)
     return out
 
 
