@@ -22,6 +22,48 @@ __device__ __forceinline__ float tanh_relative(float x) {
     return fabsf(x) < 0.25f ? small : 1.f - __fdividef(2.f, 1.f + ex2_approx(x * 2.8853900817779268f));
 }
 
+// Stored fields to bf16 numbers without or-ing them under an exponent: a field within the low eight bits of a 16-bit half is,
+// read as bf16, the field times 2^-133 (attn_umma and ragged_umma).
+struct UW {
+    uint32_t s, s2, c;      // multipliers of fields at bit 0 and higher up, -offset * weight
+};
+// 32 slots as 16 bf16 pairs (four 16-byte pieces).
+template <int P>
+__device__ __forceinline__ void convert32(const uint32_t (&w)[P], const UW& g0, const UW& g1, uint32_t (&r)[16]) {
+    if (P == 4) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const UW& g = j < 2 ? g0 : g1;
+            const uint32_t y = w[j] >> 8;
+            r[4 * j] = fma_bf16x2(w[j] & 0x000F000Fu, g.s, g.c);
+            r[4 * j + 1] = fma_bf16x2(w[j] & 0x00F000F0u, g.s2, g.c);
+            r[4 * j + 2] = fma_bf16x2(y & 0x000F000Fu, g.s, g.c);
+            r[4 * j + 3] = fma_bf16x2(y & 0x00F000F0u, g.s2, g.c);
+        }
+    } else if (P == 8) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const UW& g = j < 4 ? g0 : g1;
+            r[2 * j] = fma_bf16x2(w[j] & 0x00FF00FFu, g.s, g.c);
+            r[2 * j + 1] = fma_bf16x2(prmt(w[j], 0u, 0x4341u), g.s, g.c);
+        }
+    } else {
+        // eight slots are two runs of three bytes; a 16-bit half holds bytes 0, 1 (then 1, 2) of the first run, the other
+        // half those of the second: slots 0 | 4, 1 | 5 and 2 | 6, 3 | 7
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int b = 6 * j, word = b >> 2;                      // first byte of the eight slots: 0, 6, 12, 18
+            const bool odd = (b & 3) != 0;
+            const uint32_t lo = prmt(w[word], w[(word + 1) % P], odd ? 0x6532u : 0x4310u), hi = prmt(w[word], w[(word + 1) % P], odd ? 0x7643u : 0x5421u);
+            const UW& g = j < 2 ? g0 : g1;
+            r[4 * j] = fma_bf16x2(lo & 0x003F003Fu, g.s, g.c);
+            r[4 * j + 1] = fma_bf16x2((lo >> 4) & 0x00FC00FCu, g.s2, g.c);
+            r[4 * j + 2] = fma_bf16x2((hi >> 2) & 0x00FC00FCu, g.s2, g.c);
+            r[4 * j + 3] = fma_bf16x2((hi >> 8) & 0x00FC00FCu, g.s2, g.c);
+        }
+    }
+}
+
 // Depth of drafted token i, and what a query row (draft-major, group-minor) needs of itself; rows behind R see no draft.
 __device__ __forceinline__ int draft_depth(const AttnArgs& a, int b, int i) {
     return a.depth ? min(max(a.depth[(int64_t)b * a.n_draft + i], 0), a.n_draft - 1) : i;

@@ -140,6 +140,7 @@ kvbfp_status launch_kernel(RaggedArgs a, bool umma, int64_t rows, uint8_t* works
     if (grid > most) grid = most;
     a.workers = (int)grid * per_block;
     a.extra = umma ? kEntryTiles : 0;
+    a.out_up = umma ? 65536.f : 256.f;
     kvbfp_status st;
     if (umma) st = bits == 4 ? launch_ragged_umma4(a, (int)grid, s) : bits == 6 ? launch_ragged_umma6(a, (int)grid, s) : launch_ragged_umma8(a, (int)grid, s);
     else st = bits == 4 ? launch_ragged_rows4(a, (int)grid, s) : bits == 6 ? launch_ragged_rows6(a, (int)grid, s) : launch_ragged_rows8(a, (int)grid, s);
@@ -208,7 +209,6 @@ extern "C" kvbfp_status kvbfp_ragged_attn(const kvbfp_cache* cache, const kvbfp_
     uint8_t* ws = static_cast<uint8_t*>(workspace);
     const bool bf16 = dt == KVBFP_BF16;
     const size_t few_bytes = lay_out(kernel_of(false, f.mant_bits), rows, nullptr, nullptr);
-    a.out_up = 256.f;
     // The hint says whether any sequence may have many rows; where it says that none has, all go to ragged_rows, whatever they
     // have.  Where some may, single tokens between them still do.
     const bool many = bf16 && rows > kFewRows && (int64_t)max_new * group > kFewRows;

@@ -60,9 +60,36 @@ __device__ __forceinline__ constexpr int prompt_pos(int s) {
 // Byte place of 16-byte piece p (8 positions) of row r.
 __device__ __forceinline__ uint32_t prompt_place(int r, int p) { return (p >> 3) * kPPanel + r * 128 + (((p & 7) ^ (r & 7)) << 4); }
 
-// 32 slots of a packed row to 16 bf16 pairs in position order.
+// Cached values are carried times 2^-16 here.  Fields become bf16 numbers by one fma (convert32) while the block's weight times
+// 2^133 is one, up to exponent bytes of kPFast (values below 2^11 to 2^16); rows with larger ones are rare and take the longer way, over an
+// exponent or-ed in.
+constexpr int kPDown = 16;
 template <int P>
-__device__ __forceinline__ void prompt_convert(const uint32_t (&w)[P], const AW& g0, const AW& g1, uint32_t (&r)[16]) {
+constexpr int kPFast = 135 + P;
+// Weights of a block, its exponent byte `e2` in both halves: multipliers 2^(e - 127 - (P - 2) - 16 + 133), the same for fields
+// further up, -2^(P-1) times the weight.  Blocks below 2^-110 turn into zeros.
+template <int P>
+__device__ __forceinline__ UW prompt_weights(uint32_t e2) {
+    uint32_t e;
+    asm("max.s16x2 %0, %1, %2;" : "=r"(e) : "r"(e2), "r"(15u * 0x00010001u));
+    UW w;
+    w.s = e * 0x80u + (119u - P) * 0x00800080u;
+    w.s2 = w.s - (P == 4 ? 4u : 2u) * 0x00800080u;
+    w.c = e * 0x80u - 15u * 0x00800080u + 0x80008000u;
+    return w;
+}
+template <int P>
+__device__ __forceinline__ AW prompt_weights_large(uint32_t e2) {
+    AW w;
+    asm("max.s16x2 %0, %1, %2;" : "=r"(w.s) : "r"(e2), "r"((P - 2 + kPDown) * 0x00010001u));
+    w.s = w.s * 0x80u - (P - 2 + kPDown) * 0x00800080u;
+    w.c = mul_bf16x2(w.s, AFmt<P>::bias);
+    w.s16 = (P == 8) ? mul_bf16x2(w.s, 0x41804180u) : 0u;
+    return w;
+}
+// 32 slots of a packed row to 16 bf16 pairs in position order, for any exponent byte.
+template <int P>
+__device__ __forceinline__ void prompt_convert_large(const uint32_t (&w)[P], const AW& g0, const AW& g1, uint32_t (&r)[16]) {
     if (P == 4) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -286,59 +313,95 @@ __global__ void __launch_bounds__(kPThreads, 1) ragged_umma(const RaggedArgs a) 
     } else if (warp >= 12) {
         // ================================================================ packed rows to bf16
         regs_less<kPRegsConv>();
-        const int r = tid & 127, row_e = D / a.fmt.block;
-        const uint32_t sel = row_e == 4 ? 0x3210u : row_e == 2 ? 0x1100u : 0x0000u;
-        const int plane = (warp - 12) >> 2;                  // K, V
+        // LANES lanes to a row, 128 / LANES slots each.  8 bits: four, so that whole lines are read (a thread per row reads 16 bytes of
+        // 32 rows at a time: four chunks over 14 000 rows each 3.0 ms, 2.65 this way).  4 and 6 bits: one, whose weights serve a
+        // whole row (2.18 ms against 2.28 with four; 6 bits 689 us against 775 for a prompt of 8192).
+        constexpr int LANES = P == 8 ? 4 : 1, ROWS = LANES;        // rows of a thread
+        const int row_e = D / a.fmt.block, w4 = warp & 3, u = lane % LANES, flip = u >> 1;      // (flip: below)
+        const int plane = (warp - 12) >> 2;                 // K, V
         const uint8_t *mant = plane ? a.v_mant : a.k_mant, *exps = plane ? a.v_exp : a.k_exp;
         const uint32_t stages = base + (plane ? kPV : kPK);
-        uint32_t w[4][P], e[2] = {0, 0};
-        auto load = [&](int i) {             // this thread's row of tile i
+        const uint32_t sel = row_e == 4 ? 0x3210u : row_e == 2 ? 0x1100u : 0x0000u;
+        const int e_at = N16 ? 2 * u : row_e == 4 ? u : row_e == 2 ? flip : 0;
+        uint32_t w[4][P], e[4];              // 32 slots each: of four rows, or a whole row (then e: its exponent bytes)
+        auto row_of = [&](int x) { return LANES == 1 ? 32 * w4 + lane : 32 * w4 + 8 * x + (lane >> 2); };
+        auto load = [&](int i) {             // the rows of tile i
             if ((i & 7) == 0) wait(b_plan(i), i >> 4);
-            int64_t row = *(volatile int64_t*)&s_rows[i & 15][r >> 4];
+            int64_t first[2];
+#pragma unroll
+            for (int x = 0; x < 2; ++x) first[x] = *(volatile int64_t*)&s_rows[i & 15][2 * w4 + (LANES == 1 ? lane >> 4 : x)];
             __syncwarp();
             if ((i & 7) == 7 && lane == 0) mbar_arrive(b_used(i));
-            if (row < 0) {
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
+            for (int x = 0; x < ROWS; ++x) {
+                const int64_t f = first[x >> 1], row = f + (row_of(x) & 15);
+                if (f < 0) {
 #pragma unroll
-                    for (int x = 0; x < P; ++x) w[j][x] = 0u;
-                e[0] = e[1] = 0u;
-                return;
-            }
-            row += r & 15;
-            const uint4* p = reinterpret_cast<const uint4*>(mant + row * ROW_M);
+                    for (int z = 0; z < 4; ++z) {
+                        if (LANES != 1 && z != x) continue;
+                        e[z] = 0u;
 #pragma unroll
-            for (int x = 0; x < P; ++x) {
-                const uint4 y = p[x];
-                w[(4 * x) / P][(4 * x) % P] = y.x;
-                w[(4 * x + 1) / P][(4 * x + 1) % P] = y.y;
-                w[(4 * x + 2) / P][(4 * x + 2) % P] = y.z;
-                w[(4 * x + 3) / P][(4 * x + 3) % P] = y.w;
-            }
-            const uint8_t* q = exps + row * row_e;
-            if (N16) {
-                const uint2 y = *reinterpret_cast<const uint2*>(q);
-                e[0] = y.x;
-                e[1] = y.y;
-            } else {
-                e[0] = row_e == 4 ? *reinterpret_cast<const uint32_t*>(q) : row_e == 2 ? *reinterpret_cast<const uint16_t*>(q) : *q;
+                        for (int y = 0; y < P; ++y) w[z][y] = 0u;
+                    }
+                    continue;
+                }
+                const uint8_t *p = mant + row * ROW_M + 4 * P * u, *q = exps + row * row_e;
+                if (LANES == 1) {
+#pragma unroll
+                    for (int y = 0; y < P; ++y) {
+                        const uint4 v = reinterpret_cast<const uint4*>(p)[y];
+                        w[(4 * y) / P][(4 * y) % P] = v.x;
+                        w[(4 * y + 1) / P][(4 * y + 1) % P] = v.y;
+                        w[(4 * y + 2) / P][(4 * y + 2) % P] = v.z;
+                        w[(4 * y + 3) / P][(4 * y + 3) % P] = v.w;
+                    }
+                    if (N16) {
+                        const uint2 v = *reinterpret_cast<const uint2*>(q);
+                        e[0] = v.x;
+                        e[1] = v.y;
+                    } else {
+                        e[0] = row_e == 4 ? *reinterpret_cast<const uint32_t*>(q) : row_e == 2 ? *reinterpret_cast<const uint16_t*>(q) : *q;
+                    }
+                } else {
+                    // (the lanes of a row's second half take the halves of their 32 slots the other way round, so that eight lanes store to
+                    // all banks)
+#pragma unroll
+                    for (int y = 0; y < 2; ++y) {
+                        const uint4 v = *reinterpret_cast<const uint4*>(p + 16 * (flip ^ y));
+                        w[x][(4 * y) % P] = v.x;
+                        w[x][(4 * y + 1) % P] = v.y;
+                        w[x][(4 * y + 2) % P] = v.z;
+                        w[x][(4 * y + 3) % P] = v.w;
+                    }
+                    e[x] = N16 ? *reinterpret_cast<const uint16_t*>(q + e_at) : q[e_at];
+                }
             }
         };
         auto convert = [&](uint32_t to) {
-            const uint32_t eb = N16 ? 0u : prmt(e[0], 0u, sel);
+            uint32_t top = e[0];
+            if (LANES == 1) top = N16 ? vmaxu4(e[0], e[1]) : prmt(e[0], 0u, sel);
+            else
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                AW g0, g1;
-                if (N16) {
-                    g0 = aw_make<P>(prmt(e[j >> 1], 0u, 0x4040u + 0x0101u * (2 * (j & 1))));
-                    g1 = aw_make<P>(prmt(e[j >> 1], 0u, 0x4040u + 0x0101u * (2 * (j & 1) + 1)));
+                for (int x = 1; x < 4; ++x) top = vmaxu4(top, e[x]);
+            const bool large = __vcmpgtu4(top, kPFast<P> * 0x01010101u) != 0u;
+            const bool slow = __any_sync(0xffffffffu, large);
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                // exponent bytes of the 32 slots' halves, as they lie in w, in both halves of a word
+                uint32_t e0, e1;
+                if (LANES == 1) {
+                    e0 = N16 ? prmt(e[x >> 1], 0u, 0x4040u + 0x0101u * (2 * (x & 1))) : prmt(top, 0u, 0x4040u + 0x0101u * x);
+                    e1 = N16 ? prmt(e[x >> 1], 0u, 0x4040u + 0x0101u * (2 * (x & 1) + 1)) : e0;
                 } else {
-                    g0 = g1 = aw_make<P>(prmt(eb, 0u, 0x4040u + 0x0101u * j));
+                    e0 = N16 ? prmt(e[x], 0u, flip ? 0x4141u : 0x4040u) : e[x] * 0x00010001u;
+                    e1 = N16 ? prmt(e[x], 0u, flip ? 0x4040u : 0x4141u) : e0;
                 }
-                uint32_t x[16];
-                prompt_convert<P>(w[j], g0, g1, x);
+                uint32_t v[16];
+                if (!slow) convert32<P>(w[x], prompt_weights<P>(e0), prompt_weights<P>(e1), v);
+                else prompt_convert_large<P>(w[x], prompt_weights_large<P>(e0), prompt_weights_large<P>(e1), v);
 #pragma unroll
-                for (int y = 0; y < 4; ++y) sts128(to + prompt_place(r, 4 * j + y), x[4 * y], x[4 * y + 1], x[4 * y + 2], x[4 * y + 3]);
+                for (int y = 0; y < 4; ++y)
+                    sts128(to + prompt_place(row_of(x), LANES == 1 ? 4 * x + y : 4 * u + (y ^ (2 * flip))), v[4 * y], v[4 * y + 1], v[4 * y + 2], v[4 * y + 3]);
             }
             fence_async_shared();
             __syncwarp();
@@ -362,7 +425,7 @@ __global__ void __launch_bounds__(kPThreads, 1) ragged_umma(const RaggedArgs a) 
         const int h = (warp >> 2) - 1, w4 = warp & 3, r = tid & 127;                   // half, quarter of its rows, row
         const uint32_t tms = tm + 128 * h + ((uint32_t)w4 << 21), tmo = tms + 256;      // lane field: 32 * quarter << 16
         const uint32_t q_at = base + kPQ + h * 32768;
-        const float mul = finite_factor(a.scale * kValueUp * 1.4426950408889634f);      // scores to log2 units
+        const float mul = finite_factor(a.scale * (float)(1 << kPDown) * 1.4426950408889634f);      // scores to log2 units
         int4 rec = make_int4(-1, 0, 0, 0);
         // This lane's row of q among the warp's 32 rows of the entry at a cursor (NULL: behind the last)
         auto q_row = [&](const RaggedCursor& e) -> const uint8_t* {
@@ -542,7 +605,7 @@ __global__ void __launch_bounds__(kPThreads, 1) ragged_umma(const RaggedArgs a) 
             const bool staged = whole && a.inv_perm_v != nullptr;
             if (next_here && !staged) write_q();
             if (here) {
-                const float inv = l != 0.f ? kValueUp / l : 0.f;
+                const float inv = l != 0.f ? (float)(1 << kPDown) / l : 0.f;
                 wait(b_o(h), n_run++);
                 __syncwarp();
                 tmem_fence_after();
