@@ -4,17 +4,18 @@
 //   y = x / sqrt(mean(x^2) + eps) * w ;  (y_a, y_b) -> (y_a cos - y_b sin, y_a sin + y_b cos), angle = position * theta[pair]
 //
 // A warp takes two neighbouring tokens, sixteen lanes each, and walks heads: queries, keys, values.  A lane holds four
-// rotation pairs of its token's rows, so that sine and cosine are formed once per token (four a lane, in registers) and serve
-// all heads, and no pair crosses lanes.  Rows come through a ring of shared-memory stages per warp that asynchronous copies
-// fill some heads ahead.  Keys pass through shared memory once more for the permutation, then a lane owns eight stored slots and
-// casts them as kvbfp_append does (sixteen lanes to a row).
+// rotation pairs of its token's rows, so that sine and cosine are formed once per token (four a lane, in registers, times the
+// norm's weights) and serve all heads, and no pair crosses lanes.  The rows of the next heads are on their way while the ones
+// before are worked on (they pass through registers only: a ring of shared-memory stages cost more instructions than its
+// asynchronous copies hid).  Keys, and values with a permutation, are parked in shared memory and picked up slot by slot; then a
+// lane owns eight stored slots and casts them as kvbfp_append does (sixteen lanes to a row).
 //
 // Codes of keys.  Values next to a rounding border fall on the side that fp32 errors pick, which would make the cache depend on
 // the order of operations.  The error of a value is bounded by kErr times the magnitude of its pair; a row with a value (or
-// block maximum) that close to a border is formed and cast again in fp64, four rows in a thousand (4 bits) to one in twenty (8
+// block maximum) that close to a border is formed and cast again in fp64, one row in some five hundred (4 bits) to one in thirty (8
 // bits).  So the codes are those of the formula.
 //
-// What bounds it: memory for whole prompts.  Bytes of a token: 2 (Hq + Hkv) es 128 ... read and written once.
+// What bounds it: instructions (a row takes some 25 a lane for queries, 75 for keys, 45 for values), then memory.
 #include <atomic>
 
 #include "pages.cuh"
@@ -25,7 +26,6 @@ namespace kvbfp {
 namespace {
 
 constexpr int kWWarps = 8;            // warps of a block, each on its own
-__host__ __device__ constexpr int write_ring(int type_bytes) { return type_bytes == 2 ? 4 : 3; }      // heads in flight (48 KB a block)
 
 struct WriteArgs {
     const void* src[3];               // q, k, v
@@ -46,18 +46,10 @@ struct WriteArgs {
 };
 
 // fp32 error of a normalised and rotated value, relative to the sum of its pair's magnitudes (in units of 2^-24): the norm's
-// factor and its two products 3, sine and cosine of an angle rounded once 4 (the angle is 3.14 at most: half a step is 2; the
-// functions are good to 2), the product and the sum 2; rounded up.
-constexpr float kErr = 10.f / 16777216.f;
-
-// Squares summed in fp64: their sum's square root inverted to fp32's last bit by one step of Newton's from an fp32 start.
-__device__ __forceinline__ float inv_rms64(double ss, float eps) {
-    const double m = ss * (1.0 / kHeadDim) + (double)eps;
-    const double i0 = (double)rsqrtf((float)m);
-    const double i1 = i0 * (1.5 - 0.5 * m * i0 * i0);
-    // outside fp32's range (or nothing to invert) the start is no start: the long way
-    return (float)((m > 1e-30 && m < 1e30) ? i1 : 1.0 / sqrt(m));
-}
+// factor 9 (squares summed in ten roundings, halved by the square root; the function itself 4), its product 1, sine and cosine of
+// an angle rounded once 4 (the angle is 3.14 at most: half a step is 2; the functions are good to 2), their product with the
+// weight 1, the product and the sum 2; rounded up.
+constexpr float kErr = 18.f / 16777216.f;
 
 template <int P, int N>
 struct Cast {
@@ -129,6 +121,47 @@ __device__ __forceinline__ bool cast32(const float (&v)[8], const float (&err)[8
     }
     return near;
 }
+// Eight bf16 numbers of a lane, in pairs, cast and written as pairs (as in append_rows: everything the cast does to a bf16
+// number stays inside bf16).  4 bits: pair j is slots j and j + 4, 6 bits: 2 j and 2 j + 1.  Returns whether all are finite.
+template <int P, int N>
+__device__ __forceinline__ bool cast_bf16(uint32_t (&f)[4], bool stored, uint8_t* mrow, uint8_t* erow, int sub) {
+    using C = Cast<P, N>;
+    auto top2 = [](uint32_t a, uint32_t b) { uint32_t d; asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b)); return d; };
+    uint32_t m = top2(top2(f[0] & 0x7fff7fffu, f[1] & 0x7fff7fffu), top2(f[2] & 0x7fff7fffu, f[3] & 0x7fff7fffu));
+#pragma unroll
+    for (int off = 1; off < C::LANES; off <<= 1) m = top2(m, __shfl_xor_sync(0xffffffffu, m, off));
+    int e8 = (int)(max(m & 0xffffu, m >> 16) >> 7);
+    const bool finite = e8 != 255;
+    if (!finite) e8 = 254;
+    const int k = 127 - e8 + (P - 2), k1 = k >> 1, k2 = k - k1;
+    constexpr uint32_t BASE = 0x43404340u;                       // bf16 192.0 twice
+    constexpr uint32_t MAGIC = BASE + C::EXC * 0x10001u, LO = MAGIC - C::QMAX * 0x10001u, HI = MAGIC + C::QMAX * 0x10001u;
+    const uint32_t s1 = ((uint32_t)(k1 + 127) << 7) * 0x10001u, s2 = ((uint32_t)(k2 + 127) << 7) * 0x10001u;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        f[j] = fma_bf16x2(mul_bf16x2(f[j], s1), s2, MAGIC);
+        asm("max.bf16x2 %0, %0, %1;" : "+r"(f[j]) : "r"(LO));    // (a NaN falls to the lower bound)
+        asm("min.bf16x2 %0, %0, %1;" : "+r"(f[j]) : "r"(HI));
+    }
+    if (!stored) return finite;
+    if (P == 4) {
+        reinterpret_cast<uint32_t*>(mrow)[sub] = ((f[3] * 16u + f[2]) * 16u + f[1]) * 16u + f[0] - BASE * 0x1111u;
+    } else {
+        uint32_t t[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const uint32_t c = f[j] - BASE;
+            t[j] = (c | (c >> 10)) & 0xfffu;
+        }
+        const uint32_t lo = t[0] + (t[1] << 12) + (t[2] << 24), hi = (t[2] >> 8) + (t[3] << 4);
+        uint16_t* o = reinterpret_cast<uint16_t*>(mrow + sub * 6);
+        o[0] = (uint16_t)lo;
+        o[1] = (uint16_t)(lo >> 16);
+        o[2] = (uint16_t)hi;
+    }
+    if ((sub % C::LANES) == 0) erow[sub / C::LANES] = (uint8_t)e8;
+    return finite;
+}
 // The same of values in fp64.
 template <int P, int N>
 __device__ __forceinline__ void cast64(const double (&v)[8], uint32_t (&f)[8], int& e8) {
@@ -149,16 +182,26 @@ __device__ __forceinline__ void cast64(const double (&v)[8], uint32_t (&f)[8], i
 }
 
 // Four pairs of a key row in fp64 (a call: few rows come here).
-__device__ __noinline__ void turn64(const float (&a)[4], const float (&b)[4], const float* wa, const float* wb, double inv,
+__device__ __noinline__ void turn64(const float (&a)[4], const float (&b)[4], const float (&wa)[4], const float (&wb)[4], double inv,
                                     const double* theta, int pos, double (&ya)[4], double (&yb)[4]) {
 #pragma unroll 1
     for (int j = 0; j < 4; ++j) {
-        const double xa = (double)a[j] * inv * (wa ? (double)wa[j] : 1.0), xb = (double)b[j] * inv * (wb ? (double)wb[j] : 1.0);
+        const double xa = (double)a[j] * inv * (double)wa[j], xb = (double)b[j] * inv * (double)wb[j];
         double sn = 0.0, cs = 1.0;
         if (theta) sincos((double)pos * theta[j], &sn, &cs);
         ya[j] = xa * cs - xb * sn;
         yb[j] = xa * sn + xb * cs;
     }
+}
+
+// 1 / sqrt(mean(x^2) + eps) of a row that sixteen lanes hold.
+__device__ __forceinline__ float inv_rms(const F2 (&xa)[2], const F2 (&xb)[2], float eps) {
+    float s0, s1;
+    f2_split(f2_fma(xa[0], xa[0], f2_fma(xa[1], xa[1], f2_fma(xb[0], xb[0], f2_mul(xb[1], xb[1])))), s0, s1);
+    float ss = s0 + s1;
+#pragma unroll
+    for (int off = 8; off; off >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, off);
+    return rsqrtf(fmaf(ss, 1.f / kHeadDim, eps));
 }
 
 // HALF: pairs (i, i + 64), else (2i, 2i + 1).  A lane's pairs are 4 sub .. 4 sub + 3 in both.
@@ -167,29 +210,46 @@ __device__ __forceinline__ int chan_a(int sub, int j) { return HALF ? 4 * sub + 
 template <bool HALF>
 __device__ __forceinline__ int chan_b(int sub, int j) { return HALF ? 64 + 4 * sub + j : 8 * sub + 2 * j + 1; }
 
+// A lane's share of a row: two runs of four channels (HALF) or eight channels, and the pairs in it.
+template <typename T>
+struct Share {
+    uint32_t w[2 * sizeof(T)];
+};
 template <typename T, bool HALF>
-__device__ __forceinline__ void read_pairs(const uint8_t* row, int sub, float (&a)[4], float (&b)[4]) {
+__device__ __forceinline__ Share<T> load_share(const T* row, int sub) {
+    Share<T> x;
+    const uint8_t* p = reinterpret_cast<const uint8_t*>(row);
     if (sizeof(T) == 2) {
         if (HALF) {
-            const uint2 x = *reinterpret_cast<const uint2*>(row + 8 * sub), y = *reinterpret_cast<const uint2*>(row + 128 + 8 * sub);
-            a[0] = __uint_as_float(x.x << 16); a[1] = __uint_as_float(x.x & 0xffff0000u);
-            a[2] = __uint_as_float(x.y << 16); a[3] = __uint_as_float(x.y & 0xffff0000u);
-            b[0] = __uint_as_float(y.x << 16); b[1] = __uint_as_float(y.x & 0xffff0000u);
-            b[2] = __uint_as_float(y.y << 16); b[3] = __uint_as_float(y.y & 0xffff0000u);
+            const uint2 a = *reinterpret_cast<const uint2*>(p + 8 * sub), b = *reinterpret_cast<const uint2*>(p + 128 + 8 * sub);
+            x.w[0] = a.x; x.w[1] = a.y; x.w[2] = b.x; x.w[3] = b.y;
         } else {
-            const uint4 x = *reinterpret_cast<const uint4*>(row + 16 * sub);
-            const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-            for (int j = 0; j < 4; ++j) { a[j] = __uint_as_float(w[j] << 16); b[j] = __uint_as_float(w[j] & 0xffff0000u); }
+            const uint4 a = *reinterpret_cast<const uint4*>(p + 16 * sub);
+            x.w[0] = a.x; x.w[1] = a.y; x.w[2] = a.z; x.w[3] = a.w;
         }
     } else {
-        const float4 x = *reinterpret_cast<const float4*>(row + (HALF ? 16 * sub : 32 * sub));
-        const float4 y = *reinterpret_cast<const float4*>(row + (HALF ? 256 + 16 * sub : 32 * sub + 16));
-        if (HALF) {
-            a[0] = x.x; a[1] = x.y; a[2] = x.z; a[3] = x.w; b[0] = y.x; b[1] = y.y; b[2] = y.z; b[3] = y.w;
-        } else {
-            a[0] = x.x; b[0] = x.y; a[1] = x.z; b[1] = x.w; a[2] = y.x; b[2] = y.y; a[3] = y.z; b[3] = y.w;
-        }
+        const uint4 a = *reinterpret_cast<const uint4*>(p + (HALF ? 16 * sub : 32 * sub)), b = *reinterpret_cast<const uint4*>(p + (HALF ? 256 + 16 * sub : 32 * sub + 16));
+        x.w[0] = a.x; x.w[1] = a.y; x.w[2] = a.z; x.w[3] = a.w;
+        x.w[(4) % (2 * sizeof(T))] = b.x; x.w[5 % (2 * sizeof(T))] = b.y; x.w[6 % (2 * sizeof(T))] = b.z; x.w[7 % (2 * sizeof(T))] = b.w;
+    }
+    return x;
+}
+// The eight numbers of a share in memory order.
+template <typename T>
+__device__ __forceinline__ void share_values(const Share<T>& x, float (&v)[8]) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        v[i] = sizeof(T) == 4 ? __uint_as_float(x.w[i % (2 * sizeof(T))]) : (i & 1) ? __uint_as_float(x.w[i / 2] & 0xffff0000u) : __uint_as_float(x.w[i / 2] << 16);
+}
+// Its pairs, two by two: a[j] = pairs 2 j and 2 j + 1.
+template <typename T, bool HALF>
+__device__ __forceinline__ void share_pairs(const Share<T>& x, F2 (&a)[2], F2 (&b)[2]) {
+    float v[8];
+    share_values<T>(x, v);
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        a[j] = HALF ? f2(v[2 * j], v[2 * j + 1]) : f2(v[4 * j], v[4 * j + 2]);
+        b[j] = HALF ? f2(v[4 + 2 * j], v[4 + 2 * j + 1]) : f2(v[4 * j + 1], v[4 * j + 3]);
     }
 }
 template <typename T, bool HALF>
@@ -216,48 +276,33 @@ __device__ __forceinline__ void write_pairs(T* row, int sub, const float (&a)[4]
 }
 
 template <int P, int N, typename T, bool HALF>
-__global__ void __launch_bounds__(kWWarps * 32) norm_rope_append(const WriteArgs a) {
-    constexpr int D = kHeadDim, ROW_M = D * P / 8, ROW_E = D / N, ROW_IN = D * (int)sizeof(T), RING = write_ring(sizeof(T));
-    constexpr int PARK = 2 * D + 4;             // floats of a parked row (value and error bound, or fp64 values), off the other's banks
-    __shared__ __align__(16) uint8_t ring[kWWarps][RING][2][ROW_IN];
+__global__ void __launch_bounds__(kWWarps * 32, 2) norm_rope_append(const WriteArgs a) {
+    constexpr int D = kHeadDim, ROW_M = D * P / 8, ROW_E = D / N;
+    constexpr int QB = sizeof(T) == 2 ? 4 : 2, KB = 2;          // query (key, value) rows of a lane under way
+    constexpr int PARK = 2 * D + 8;             // floats of a parked row (value and error bound, or fp64 values), off the other's banks
     __shared__ __align__(16) float park[kWWarps][2][PARK];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, sub = lane & 15, grp = lane >> 4;
     pdl_wait();
     pdl_trigger();
     // the warp's unit: two tokens, a run of heads
-    const int n_heads = a.heads[0] + a.heads[1] + a.heads[2];
+    const int hq = a.heads[0], hk = a.heads[1], n_heads = hq + 2 * hk;
     const int h0 = blockIdx.y * a.head_chunk, h1 = min(n_heads, h0 + a.head_chunk);
     const int tok = 2 * (blockIdx.x * kWWarps + warp) + grp;
     const int first = min(max(a.starts[0], 0), a.n_tokens), end = min(max(a.starts[a.batch], 0), a.n_tokens);
     const bool live = tok < end && tok >= first;
     if (__all_sync(0xffffffffu, !live)) return;
 
-    auto source = [&](int h) -> const T* {
-        int s = 0;
-        if (h >= a.heads[0]) {
-            s = 1;
-            h -= a.heads[0];
-            if (h >= a.heads[1]) {
-                s = 2;
-                h -= a.heads[1];
-            }
-        }
-        const T* base = static_cast<const T*>(s == 0 ? a.src[0] : s == 1 ? a.src[1] : a.src[2]);
-        const int64_t stride = s == 0 ? a.stride[0] : s == 1 ? a.stride[1] : a.stride[2];
-        return base + (int64_t)tok * stride + h * D;
-    };
-    const uint32_t my_ring = smem_u32(&ring[warp][0][grp][0]);
-    auto issue = [&](int h) {
-        if (h < h1 && live) {
-            const uint4* p = reinterpret_cast<const uint4*>(source(h)) + sub;
-            const uint32_t dst = my_ring + ((h - h0) % RING) * (2 * ROW_IN) + 16 * sub;
-            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(p) : "memory");
-            if (sizeof(T) == 4) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + 256), "l"(p + 16) : "memory");
-        }
-        asm volatile("cp.async.commit_group;" ::: "memory");
-    };
+    // heads of each kind in the run, and its first rows on their way
+    const int q0 = min(h0, hq), q1 = min(h1, hq), k0 = min(max(h0 - hq, 0), hk), k1 = min(max(h1 - hq, 0), hk);
+    const int v0 = max(h0 - hq - hk, 0), v1 = max(h1 - hq - hk, 0);
+    const int at = live ? tok : max(first, min(tok, end - 1));           // (a token that exists: read, but not used)
+    const T* q_in = static_cast<const T*>(a.src[0]) + (int64_t)at * a.stride[0] + q0 * D;
+    const T* k_in = static_cast<const T*>(a.src[1]) + (int64_t)at * a.stride[1] + k0 * D;
+    const T* v_in = static_cast<const T*>(a.src[2]) + (int64_t)at * a.stride[2] + v0 * D;
+    Share<T> qx[QB];
 #pragma unroll
-    for (int i = 0; i < RING; ++i) issue(h0 + i);
+    for (int i = 0; i < QB; ++i)
+        if (q0 + i < q1) qx[i] = load_share<T, HALF>(q_in + i * D, sub);
 
     // ---- sequence and position: the last sequence that starts at or before the token
     int b = 0;
@@ -279,139 +324,248 @@ __global__ void __launch_bounds__(kWWarps * 32) norm_rope_append(const WriteArgs
         stored = pg >= 0;
         row0 = (int64_t)max(pg, 0) * a.map.n_heads * a.map.rows + token_row(a.map, pos);
     }
-    if (live && !stored && sub == 0 && blockIdx.y == 0 && a.heads[1]) raise_flag(a.status, KVBFP_FLAG_POSITION);
+    if (live && !stored && sub == 0 && blockIdx.y == 0 && hk) raise_flag(a.status, KVBFP_FLAG_POSITION);
 
-    float cs[4], sn[4];
+    F2 cs[2], sn[2];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        cs[j] = 1.f;
-        sn[j] = 0.f;
-        if (a.theta && h0 < a.heads[0] + a.heads[1]) sincos_reduced((double)pos * a.theta[4 * sub + j], &sn[j], &cs[j]);
+    for (int j = 0; j < 2; ++j) {
+        float c[2] = {1.f, 1.f}, n[2] = {0.f, 0.f};
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+            if (a.theta && h0 < hq + hk) sincos_reduced((double)pos * a.theta[4 * sub + 2 * j + e], &n[e], &c[e]);
+        cs[j] = f2(c[0], c[1]);
+        sn[j] = f2(n[0], n[1]);
     }
-    float wa[4], wb[4];
-    auto weights = [&](const float* w) {
+    // rotation with the norm's weights in it: y_a = x_a ac - x_b bs, y_b = x_b bc + x_a as
+    F2 wa[2], wb[2], ac[2], as[2], bc[2], bs[2];
+    auto tables = [&](const float* w) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            wa[j] = w ? w[chan_a<HALF>(sub, j)] : 1.f;
-            wb[j] = w ? w[chan_b<HALF>(sub, j)] : 1.f;
+        for (int j = 0; j < 2; ++j) {
+            wa[j] = wb[j] = f2(1.f, 1.f);
+            if (w) {
+                wa[j] = f2(w[chan_a<HALF>(sub, 2 * j)], w[chan_a<HALF>(sub, 2 * j + 1)]);
+                wb[j] = f2(w[chan_b<HALF>(sub, 2 * j)], w[chan_b<HALF>(sub, 2 * j + 1)]);
+            }
+            ac[j] = f2_mul(wa[j], cs[j]);
+            as[j] = f2_mul(wa[j], sn[j]);
+            bc[j] = f2_mul(wb[j], cs[j]);
+            bs[j] = f2_mul(wb[j], f2_mul(sn[j], f2(-1.f, -1.f)));
         }
     };
-    weights(h0 < a.heads[0] ? a.weight[0] : a.weight[1]);
-    float* mine = &park[warp][grp][0];
-
-    for (int h = h0; h < h1; ++h) {
-        asm volatile("cp.async.wait_group %0;" ::"n"(RING - 1) : "memory");
-        __syncwarp();
-        const uint8_t* row = &ring[warp][(h - h0) % RING][grp][0];
-        const int kind = h < a.heads[0] ? 0 : h < a.heads[0] + a.heads[1] ? 1 : 2;
-        const int head = h - (kind == 0 ? 0 : kind == 1 ? a.heads[0] : a.heads[0] + a.heads[1]);
-        if (h == a.heads[0] && h != h0) weights(a.weight[1]);
-        float xa[4], xb[4];
-        if (kind == 0) {
-            read_pairs<T, HALF>(row, sub, xa, xb);
-            __syncwarp();
-            issue(h + RING);
-            if (a.weight[0]) {
-                float ss = 0.f;
+    // ---- queries
+    if (q0 < q1) {
+        tables(a.weight[0]);
+        T* out = static_cast<T*>(a.q_out) + ((int64_t)tok * hq + q0) * D;
+        for (int h = q0; h < q1; h += QB) {
+            Share<T> next[QB];
+            q_in += QB * D;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) ss = fmaf(xa[j], xa[j], fmaf(xb[j], xb[j], ss));
+            for (int i = 0; i < QB; ++i)
+                if (h + QB + i < q1) next[i] = load_share<T, HALF>(q_in + i * D, sub);
 #pragma unroll
-                for (int off = 8; off; off >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, off);
-                const float inv = rsqrtf(fmaf(ss, 1.f / D, a.eps));
+            for (int i = 0; i < QB; ++i) {
+                if (h + i >= q1) break;
+                F2 xa[2], xb[2];
+                share_pairs<T, HALF>(qx[i], xa, xb);
+                if (a.weight[0]) {
+                    const float inv = inv_rms(xa, xb, a.eps);
+                    const F2 inv2 = f2(inv, inv);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) { xa[j] = xa[j] * inv * wa[j]; xb[j] = xb[j] * inv * wb[j]; }
-            }
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float y = fmaf(xa[j], cs[j], -(xb[j] * sn[j]));
-                xb[j] = fmaf(xb[j], cs[j], xa[j] * sn[j]);
-                xa[j] = y;
-            }
-            if (live) write_pairs<T, HALF>(static_cast<T*>(a.q_out) + ((int64_t)tok * a.heads[0] + head) * D, sub, xa, xb);
-            continue;
-        }
-        uint8_t* mrow = a.mant[kind - 1] + (row0 + (int64_t)head * a.map.rows) * ROW_M;
-        uint8_t* erow = a.exp8[kind - 1] + (row0 + (int64_t)head * a.map.rows) * ROW_E;
-        const int32_t* perm = kind == 1 ? a.perm[0] : a.perm[1];
-        int at[8];
-        if (perm) {
-            const int4* pp = reinterpret_cast<const int4*>(perm + head * D + sub * 8);
-            const int4 p0 = __ldg(pp), p1 = __ldg(pp + 1);
-            at[0] = p0.x & (D - 1); at[1] = p0.y & (D - 1); at[2] = p0.z & (D - 1); at[3] = p0.w & (D - 1);
-            at[4] = p1.x & (D - 1); at[5] = p1.y & (D - 1); at[6] = p1.z & (D - 1); at[7] = p1.w & (D - 1);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) at[i] = sub * 8 + i;
-        }
-        float v[8], err[8];
-        uint32_t f[8];
-        int e8;
-        bool finite;
-        if (kind == 2) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                v[i] = sizeof(T) == 2 ? __uint_as_float((uint32_t)reinterpret_cast<const unsigned short*>(row)[at[i]] << 16)
-                                      : reinterpret_cast<const float*>(row)[at[i]];
-            __syncwarp();
-            issue(h + RING);
-            (void)cast32<P, N, false>(v, v, f, e8, finite);
-        } else {
-            read_pairs<T, HALF>(row, sub, xa, xb);
-            __syncwarp();
-            issue(h + RING);
-            double ss = 0.0;
-            float inv = 1.f;
-            if (a.weight[1]) {
-#pragma unroll
-                for (int j = 0; j < 4; ++j) ss = fma((double)xa[j], (double)xa[j], fma((double)xb[j], (double)xb[j], ss));
-#pragma unroll
-                for (int off = 8; off; off >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, off);
-                inv = inv_rms64(ss, a.eps);
-            }
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float ya = xa[j] * inv * wa[j], yb = xb[j] * inv * wb[j];
-                const float e = (a.weight[1] || a.theta) ? kErr * (fabsf(ya) + fabsf(yb)) : 0.f;
-                *reinterpret_cast<float2*>(mine + 2 * chan_a<HALF>(sub, j)) = make_float2(fmaf(ya, cs[j], -(yb * sn[j])), e);
-                *reinterpret_cast<float2*>(mine + 2 * chan_b<HALF>(sub, j)) = make_float2(fmaf(yb, cs[j], ya * sn[j]), e);
-            }
-            __syncwarp();
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float2 x = *reinterpret_cast<const float2*>(mine + 2 * at[i]);
-                v[i] = x.x;
-                err[i] = x.y;
-            }
-            __syncwarp();
-            const bool near = cast32<P, N, true>(v, err, f, e8, finite);
-            if (__any_sync(0xffffffffu, near && finite && stored)) {
-                double ya[4], yb[4], inv64 = 1.0;
-                if (a.weight[1]) inv64 = 1.0 / sqrt(ss * (1.0 / D) + (double)a.eps);
-                turn64(xa, xb, a.weight[1] ? wa : nullptr, a.weight[1] ? wb : nullptr, inv64, a.theta ? a.theta + 4 * sub : nullptr, pos, ya, yb);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    *reinterpret_cast<double*>(mine + 2 * chan_a<HALF>(sub, j)) = ya[j];
-                    *reinterpret_cast<double*>(mine + 2 * chan_b<HALF>(sub, j)) = yb[j];
+                    for (int j = 0; j < 2; ++j) {
+                        xa[j] = f2_mul(xa[j], inv2);
+                        xb[j] = f2_mul(xb[j], inv2);
+                    }
                 }
-                __syncwarp();
-                double w[8];
+                float ya[4], yb[4];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) w[i] = *reinterpret_cast<const double*>(mine + 2 * at[i]);
-                __syncwarp();
-                uint32_t f64[8];
-                int e64;
-                cast64<P, N>(w, f64, e64);
-                if (finite) {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) f[i] = f64[i];
-                    e8 = e64;
+                for (int j = 0; j < 2; ++j) {
+                    f2_split(f2_fma(xa[j], ac[j], f2_mul(xb[j], bs[j])), ya[2 * j], ya[2 * j + 1]);
+                    f2_split(f2_fma(xb[j], bc[j], f2_mul(xa[j], as[j])), yb[2 * j], yb[2 * j + 1]);
                 }
+                if (live) write_pairs<T, HALF>(out + i * D, sub, ya, yb);
             }
+            out += QB * D;
+#pragma unroll
+            for (int i = 0; i < QB; ++i) qx[i] = next[i];
         }
-        if (live && !finite) raise_flag(a.status, KVBFP_FLAG_NONFINITE);
-        if (stored) put_row<P, N>(f, e8, mrow, erow, sub);
     }
-    asm volatile("cp.async.wait_group 0;" ::: "memory");
+    float* mine = &park[warp][grp][0];
+    // where this lane's eight slots of head `head` find their channels
+    auto slots = [&](const int32_t* perm, int head, int (&at)[8]) {
+        const int4* pp = reinterpret_cast<const int4*>(perm + head * D + sub * 8);
+        const int4 p0 = __ldg(pp), p1 = __ldg(pp + 1);
+        at[0] = p0.x & (D - 1); at[1] = p0.y & (D - 1); at[2] = p0.z & (D - 1); at[3] = p0.w & (D - 1);
+        at[4] = p1.x & (D - 1); at[5] = p1.y & (D - 1); at[6] = p1.z & (D - 1); at[7] = p1.w & (D - 1);
+    };
+    // ---- keys
+    if (k0 < k1) {
+        tables(a.weight[1]);
+        const bool moved = a.weight[1] || a.theta;
+        Share<T> kx[KB];
+#pragma unroll
+        for (int i = 0; i < KB; ++i)
+            if (k0 + i < k1) kx[i] = load_share<T, HALF>(k_in + i * D, sub);
+        for (int h = k0; h < k1; h += KB) {
+            Share<T> next[KB];
+            k_in += KB * D;
+#pragma unroll
+            for (int i = 0; i < KB; ++i)
+                if (h + KB + i < k1) next[i] = load_share<T, HALF>(k_in + i * D, sub);
+#pragma unroll
+            for (int i = 0; i < KB; ++i) {
+                if (h + i >= k1) break;
+                int at[8];
+                if (a.perm[0]) {
+                    slots(a.perm[0], h + i, at);
+                } else {
+#pragma unroll
+                    for (int x = 0; x < 8; ++x) at[x] = sub * 8 + x;
+                }
+                F2 xa[2], xb[2];
+                share_pairs<T, HALF>(kx[i], xa, xb);
+                const float inv = a.weight[1] ? inv_rms(xa, xb, a.eps) : 1.f;
+                const F2 inv2 = f2(inv, inv);
+                float y[2][4], err[4];
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const F2 na = f2_mul(xa[j], inv2), nb = f2_mul(xb[j], inv2);
+                    f2_split(f2_fma(na, ac[j], f2_mul(nb, bs[j])), y[0][2 * j], y[0][2 * j + 1]);
+                    f2_split(f2_fma(nb, bc[j], f2_mul(na, as[j])), y[1][2 * j], y[1][2 * j + 1]);
+                    float ma[2], mb[2];
+                    f2_split(f2_mul(na, wa[j]), ma[0], ma[1]);
+                    f2_split(f2_mul(nb, wb[j]), mb[0], mb[1]);
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) err[2 * j + e] = moved ? kErr * (fabsf(ma[e]) + fabsf(mb[e])) : 0.f;
+                }
+                // (value, bound) of each channel
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    if (HALF) {
+                        *reinterpret_cast<float4*>(mine + 2 * chan_a<HALF>(sub, 2 * j)) = make_float4(y[0][2 * j], err[2 * j], y[0][2 * j + 1], err[2 * j + 1]);
+                        *reinterpret_cast<float4*>(mine + 2 * chan_b<HALF>(sub, 2 * j)) = make_float4(y[1][2 * j], err[2 * j], y[1][2 * j + 1], err[2 * j + 1]);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 2; ++e)
+                            *reinterpret_cast<float4*>(mine + 2 * chan_a<HALF>(sub, 2 * j + e)) = make_float4(y[0][2 * j + e], err[2 * j + e], y[1][2 * j + e], err[2 * j + e]);
+                    }
+                }
+                __syncwarp();
+                float v[8], ev[8];
+#pragma unroll
+                for (int x = 0; x < 8; ++x) {
+                    const float2 z = *reinterpret_cast<const float2*>(mine + 2 * at[x]);
+                    v[x] = z.x;
+                    ev[x] = z.y;
+                }
+                __syncwarp();
+                uint32_t f[8];
+                int e8;
+                bool finite;
+                const bool near = cast32<P, N, true>(v, ev, f, e8, finite);
+                if (__any_sync(0xffffffffu, near && finite && stored)) {
+                    double za[4], zb[4], inv64 = 1.0;
+                    float pa[4], pb[4], qa[4], qb[4];
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        f2_split(xa[j], pa[2 * j], pa[2 * j + 1]);
+                        f2_split(xb[j], pb[2 * j], pb[2 * j + 1]);
+                        f2_split(wa[j], qa[2 * j], qa[2 * j + 1]);
+                        f2_split(wb[j], qb[2 * j], qb[2 * j + 1]);
+                    }
+                    if (a.weight[1]) {
+                        double ss = 0.0;
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) ss = fma((double)pa[j], (double)pa[j], fma((double)pb[j], (double)pb[j], ss));
+#pragma unroll
+                        for (int off = 8; off; off >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, off);
+                        inv64 = 1.0 / sqrt(ss * (1.0 / D) + (double)a.eps);
+                    }
+                    turn64(pa, pb, qa, qb, inv64, a.theta ? a.theta + 4 * sub : nullptr, pos, za, zb);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        *reinterpret_cast<double*>(mine + 2 * chan_a<HALF>(sub, j)) = za[j];
+                        *reinterpret_cast<double*>(mine + 2 * chan_b<HALF>(sub, j)) = zb[j];
+                    }
+                    __syncwarp();
+                    double w[8];
+#pragma unroll
+                    for (int x = 0; x < 8; ++x) w[x] = *reinterpret_cast<const double*>(mine + 2 * at[x]);
+                    __syncwarp();
+                    uint32_t f64[8];
+                    int e64;
+                    cast64<P, N>(w, f64, e64);
+                    if (finite) {
+#pragma unroll
+                        for (int x = 0; x < 8; ++x) f[x] = f64[x];
+                        e8 = e64;
+                    }
+                }
+                if (live && !finite) raise_flag(a.status, KVBFP_FLAG_NONFINITE);
+                const int64_t row = row0 + (int64_t)(h + i) * a.map.rows;
+                if (stored) put_row<P, N>(f, e8, a.mant[0] + row * ROW_M, a.exp8[0] + row * ROW_E, sub);
+            }
+#pragma unroll
+            for (int i = 0; i < KB; ++i) kx[i] = next[i];
+        }
+    }
+    // ---- values
+    if (v0 < v1) {
+        Share<T> vx[KB];
+#pragma unroll
+        for (int i = 0; i < KB; ++i)
+            if (v0 + i < v1) vx[i] = load_share<T, false>(v_in + i * D, sub);
+        for (int h = v0; h < v1; h += KB) {
+            Share<T> next[KB];
+            v_in += KB * D;
+#pragma unroll
+            for (int i = 0; i < KB; ++i)
+                if (h + KB + i < v1) next[i] = load_share<T, false>(v_in + i * D, sub);
+#pragma unroll
+            for (int i = 0; i < KB; ++i) {
+                if (h + i >= v1) break;
+                const int64_t row = row0 + (int64_t)(h + i) * a.map.rows;
+                uint8_t *mrow = a.mant[1] + row * ROW_M, *erow = a.exp8[1] + row * ROW_E;
+                bool finite;
+                int at[8];
+                if (a.perm[1]) slots(a.perm[1], h + i, at);
+                if (sizeof(T) == 2 && P != 8) {
+                    uint32_t f[4];
+                    if (a.perm[1]) {
+                        *reinterpret_cast<uint4*>(mine + 4 * sub) = make_uint4(vx[i].w[0], vx[i].w[1], vx[i].w[2], vx[i].w[3]);
+                        __syncwarp();
+                        uint32_t e[8];
+#pragma unroll
+                        for (int x = 0; x < 8; ++x) e[x] = reinterpret_cast<const unsigned short*>(mine)[at[x]];
+                        __syncwarp();
+#pragma unroll
+                        for (int x = 0; x < 4; ++x) f[x] = P == 4 ? prmt(e[x], e[x + 4], 0x5410u) : prmt(e[2 * x], e[2 * x + 1], 0x5410u);
+                    } else {
+#pragma unroll
+                        for (int x = 0; x < 4; ++x) f[x] = P == 4 ? prmt(vx[i].w[x >> 1], vx[i].w[2 + (x >> 1)], (x & 1) ? 0x7632u : 0x5410u) : vx[i].w[x];
+                    }
+                    finite = cast_bf16<P == 8 ? 4 : P, N>(f, stored, mrow, erow, sub);
+                } else {
+                    float v[8];
+                    share_values<T>(vx[i], v);
+                    if (a.perm[1]) {
+                        *reinterpret_cast<float4*>(mine + 8 * sub) = make_float4(v[0], v[1], v[2], v[3]);
+                        *reinterpret_cast<float4*>(mine + 8 * sub + 4) = make_float4(v[4], v[5], v[6], v[7]);
+                        __syncwarp();
+#pragma unroll
+                        for (int x = 0; x < 8; ++x) v[x] = mine[at[x]];
+                        __syncwarp();
+                    }
+                    uint32_t f[8];
+                    int e8;
+                    (void)cast32<P, N, false>(v, v, f, e8, finite);
+                    if (stored) put_row<P, N>(f, e8, mrow, erow, sub);
+                }
+                if (live && !finite) raise_flag(a.status, KVBFP_FLAG_NONFINITE);
+            }
+#pragma unroll
+            for (int i = 0; i < KB; ++i) vx[i] = next[i];
+        }
+    }
 }
 
 template <int P, int N, typename T, bool HALF>
