@@ -276,7 +276,7 @@ __device__ __forceinline__ void write_pairs(T* row, int sub, const float (&a)[4]
 }
 
 template <int P, int N, typename T, bool HALF>
-__global__ void __launch_bounds__(kWWarps * 32, 2) norm_rope_append(const WriteArgs a) {
+__global__ void __launch_bounds__(kWWarps * 32, 3) norm_rope_append(const WriteArgs a) {
     constexpr int D = kHeadDim, ROW_M = D * P / 8, ROW_E = D / N;
     constexpr int QB = sizeof(T) == 2 ? 4 : 2, KB = 2;          // query (key, value) rows of a lane under way
     constexpr int PARK = 2 * D + 8;             // floats of a parked row (value and error bound, or fp64 values), off the other's banks
