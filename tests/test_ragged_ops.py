@@ -446,6 +446,24 @@ def test_norm_rope_append_parts(norm, rope, dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_norm_rope_append_far_ranges(dtype):
+    """Rows whose squares leave the fp32 range, or vanish in it, are normalised like any other; rows of zeros give zeros."""
+    news, lens = [24], [24]
+    cache, pool, q, k, v, w, theta, starts, n, pos, perm, perm_v = write_case(news, lens, 2, 2, 4, 32, 16, dtype, 8)
+    for scale, eps in ((2.0 ** 100, 1e-6), (2.0 ** 70, 0.0), (2.0 ** -70, 0.0), (2.0 ** -100, 0.0)):
+        x = [(t.float() * scale).to(dtype) for t in (q, k)]
+        if eps:
+            x[0][3], x[1][5] = 0.0, 0.0
+        before = planes(cache)
+        out = B.norm_rope_append(cache, x[0], x[1], v.contiguous(), starts, n, q_weight=w[0], k_weight=w[1], eps=eps, theta=theta,
+                                 perm_k=perm, perm_v=perm_v, pool=pool)
+        check_q(out, rotated64(x[0], w[0], eps, theta, False, pos))
+        check_write(cache, pool, before, rotated64(x[1], w[1], eps, theta, False, pos), v.double(), news, lens, perm, perm_v, 4, 32)
+    assert B.device_status() == 0
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("bits", [4, 8])
 def test_norm_rope_append_codes_next_to_borders(bits):
     """A million keys: every code that of the formula in 64 bits, those next to a border too."""
