@@ -466,8 +466,9 @@ size_t kvbfp_ragged_workspace_bytes(const kvbfp_format* fmt, int32_t batch, int3
  *   out        [n_tokens, n_q_heads, head_dim] of `dt`; zeros for tokens at negative positions.  Rows behind starts[batch] are
  *              left as they were
  * perm_k, inv_perm_v, softmax_scale as in kvbfp_decode_attn.  n_q_heads <= 8 n_kv_heads, batch <= 1024.  Types and accuracy as
- * in kvbfp_tree_attn.  Lengths beyond the cache are read clamped and set KVBFP_FLAG_POSITION.  No atomics: the result depends on
- * nothing but the arguments.
+ * in kvbfp_tree_attn.  Lengths beyond the cache are read clamped and set KVBFP_FLAG_POSITION; so do starts that decrease
+ * (out is unspecified then).  No atomics: the result depends on nothing but the arguments.  KVBFP_ERR_UNSUPPORTED where the pieces
+ * of work pass 2^31 (bf16: from some 10^6 new tokens over a cache of as many on; f32: from some 10^5).
  */
 kvbfp_status kvbfp_ragged_attn(const kvbfp_cache* cache, const kvbfp_pages* pages, const void* q, kvbfp_dtype dt,
                                int32_t n_q_heads, int32_t n_tokens, int32_t batch, const int32_t* starts,

@@ -195,11 +195,10 @@ extern "C" kvbfp_status kvbfp_ragged_attn(const kvbfp_cache* cache, const kvbfp_
     a.q = q; a.q_is_bf16 = dt == KVBFP_BF16; a.n_q_heads = n_q_heads; a.group = group; a.batch = batch; a.n_tokens = n_tokens;
     a.starts = starts; a.lens = seq_lens; a.perm_k = perm_k; a.inv_perm_v = inv_perm_v;
     a.scale = softmax_scale > 0.f ? softmax_scale : 1.0f / sqrtf((float)f.head_dim);
-    a.window = window; a.n_sink = window > 0 ? n_sink : 0;
+    a.window = window < a.map.cap ? window : 0;          // (a window of the whole cache hides nothing)
+    a.n_sink = a.window == 0 ? 0 : n_sink < a.map.cap ? n_sink : a.map.cap;
     a.out = out;
     const int64_t rows = (int64_t)n_tokens * group;
-    // items are counted in 32 bits
-    if ((rows / 8 + batch) * f.n_kv_heads * (a.map.cap / 32 + 2 + kEntryTiles) >= (int64_t)1 << 31) return KVBFP_ERR_UNSUPPORTED;
     st = status_word(&a.status);
     if (st != KVBFP_OK) return st;
     int n_sm = 0;
@@ -210,8 +209,14 @@ extern "C" kvbfp_status kvbfp_ragged_attn(const kvbfp_cache* cache, const kvbfp_
     const bool bf16 = dt == KVBFP_BF16;
     const size_t few_bytes = lay_out(kernel_of(false, f.mant_bits), rows, nullptr, nullptr);
     // The hint says whether any sequence may have many rows; where it says that none has, all go to ragged_rows, whatever they
-    // have.  Where some may, single tokens between them still do.
-    const bool many = bf16 && rows > kFewRows && (int64_t)max_new * group > kFewRows;
+    // have.  Where some may, single tokens between them still do.  Items are counted in 32 bits.
+    const auto countable = [&](const Kernel& k, int64_t row_tiles) {
+        return row_tiles * f.n_kv_heads * (a.map.cap / k.tile + 2 + kEntryTiles) < (int64_t)1 << 31;
+    };
+    const Kernel k_few = kernel_of(false, f.mant_bits), k_many = kernel_of(true, f.mant_bits);
+    const bool all_few = countable(k_few, rows / k_few.rows_tile + batch);
+    const bool many = bf16 && rows > kFewRows && ((int64_t)max_new * group > kFewRows || !all_few);
+    if (many ? !countable(k_few, batch) || !countable(k_many, rows / k_many.rows_tile + batch) : !all_few) return KVBFP_ERR_UNSUPPORTED;
     a.few_lo = 0;
     a.few_hi = many ? kFewRows : 0x7fffffff;
     st = !many || batch > 1 ? launch_kernel(a, false, rows, ws, n_sm, s) : KVBFP_OK;

@@ -147,14 +147,16 @@ static __device__ __noinline__ void ragged_edges(uint32_t* status, uint4* out, i
 }
 
 // Items and entries of every sequence, before it and in all: threads of a block together (THREADS of them).  s_items, s_entries:
-// room for 1024 + 1.  Afterwards entry b of them holds what comes before sequence b, entry `batch` all.
+// room for 1024 + 1.  Starts that decrease (reported) leave nothing to do: sequences that overlap could be more items than 32 bits
+// count.  Afterwards entry b of them holds what comes before sequence b, entry `batch` all.
 template <int THREADS>
 __device__ __forceinline__ void ragged_count(const RaggedArgs& a, int* s_items, int* s_entries, int (&s_scan)[2][THREADS / 32], int rows_tile, int tile) {
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, H = a.fmt.n_kv_heads;
     constexpr int kAlone = 8;                                  // row tiles that a thread counts by itself
-    bool many = false;
+    bool many = false, back = false;
     for (int b = tid; b < a.batch; b += THREADS) {
         const RaggedSeq s = ragged_seq(a, b);
+        back |= min(max(a.starts[b + 1], 0), a.n_tokens) < s.start;
         const int nrt = ragged_row_tiles(a, s, rows_tile);
         int x = 0, e = 0;
         if (nrt <= kAlone) {
@@ -174,7 +176,12 @@ __device__ __forceinline__ void ragged_count(const RaggedArgs& a, int* s_items, 
             ragged_edges(a.status, reinterpret_cast<uint4*>(a.out) + s.start * row, (int64_t)min(s.n, max(-s.base, 0)) * row, s.clamped != 0);
         }
     }
-    if (__syncthreads_or(many)) {
+    if (__syncthreads_or(many || back)) {
+        if (__syncthreads_or(back)) {
+            if (back && blockIdx.x == 0) raise_flag(a.status, KVBFP_FLAG_POSITION);
+            for (int b = tid; b < a.batch; b += THREADS) s_items[b] = s_entries[b] = 0;
+            __syncthreads();
+        }
         for (int b = warp; b < a.batch; b += THREADS / 32) {
             if (s_entries[b] >= 0) continue;
             const RaggedSeq s = ragged_seq(a, b);

@@ -264,6 +264,48 @@ def test_ragged_attn_flags(page, dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_ragged_attn_starts_that_decrease(dtype):
+    """Flagged, nothing is attended; the next call is served."""
+    news, lens = [3, 60, 2], [100, 60, 80]
+    args = batch_of(news, lens, 1, 2, 4, 32, 16, dtype, 5)
+    cache, pool, q, starts, n, perm, perm_v = args
+    n = i32(100, 66, 80)                     # (no tokens before the first position)
+    for bad in (i32(0, 63, 3, 65), i32(5, 0, 65, 65), i32(0, 3, 63, 62)):
+        for hint in (2, 60):
+            got = B.ragged_attn(cache, q, bad, n, hint, perm_k=perm, inv_perm_v=inverse(perm_v), pool=pool, out=torch.full_like(q, 5.0))
+            assert bool((got == 5.0).all())
+            assert B.device_status() == B.FLAG_POSITION
+    attend_and_check(args, news, lens)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_ragged_attn_largest_window(dtype):
+    """Windows and numbers of first tokens up to the largest integer, rows before the first position among them."""
+    news, lens = [40, 1], [90, 70]
+    cache, pool, q, starts, n, perm, perm_v = batch_of(news, lens, 1, 2, 4, 32, 16, dtype, 5)
+    n[0] = 30                                            # ten tokens before the first position
+    ref = reference(cache, pool, q[10:].contiguous(), [30, 1], [30, 70], perm, perm_v)
+    for window, sink in ((2 ** 31 - 1, 0), (2 ** 31 - 1, 2 ** 31 - 1), (96, 3), (1, 2 ** 31 - 1), (95, 0)):
+        got = B.ragged_attn(cache, q, starts, n, 40, window=window, n_sink=sink, perm_k=perm, inv_perm_v=inverse(perm_v), pool=pool)
+        assert bool((got[:10] == 0).all())
+        check(got[10:], *ref)
+    assert B.device_status() == 0
+
+
+@pytest.mark.gpu
+def test_ragged_attn_long_prompts_are_not_refused():
+    """131072 new tokens of 32 heads count few enough items: a batch of that size whose sequences are empty."""
+    cache = B.Cache(1, 8, D, 131072, 32, 4)
+    q = torch.empty(131072, 32, D, dtype=torch.bfloat16, device="cuda")
+    out = torch.full((131072, 32, D), 3.0, dtype=torch.bfloat16, device="cuda")
+    for hint in (131072, 0):
+        B.ragged_attn(cache, q, i32(0, 0), i32(0), hint, out=out)
+    assert bool((out == 3.0).all()) and B.device_status() == 0
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("scale", [2.0 ** 90, 2.0 ** -90])
 def test_ragged_attn_large_and_small_values(scale):
     news, lens = [1, 100], [150, 130]
