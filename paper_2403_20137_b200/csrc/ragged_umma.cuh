@@ -6,8 +6,8 @@
 //   O[rows x slots] += P . V                  P: tensor memory, V: shared memory (tokens the slow index)
 //
 // One persistent block per SM, a worker; tiles of 128 tokens.  A tile's packed rows are converted to bf16 once for 256 query
-// rows, by eight warps that read them straight from the cache (a thread per token, the next tile's row already in registers,
-// so that pages need nothing but an address per thread).  The rows are two halves of 128, a warp group, an S and an O of
+// rows, by eight warps that read them straight from the cache, the next tile's already in registers, so that pages need nothing
+// but an address per row.  The rows are two halves of 128, a warp group, an S and an O of
 // their own each: while one half's exponentials run, the tensor cores work for the other.  A thread owns a query row: maximum,
 // sum and rescaling stay in the thread.  P takes the columns of the S it came from (two bf16 numbers a column), so that two S
 // and two O fill the 512 columns.  One warp issues all matrix instructions, PV of a tile and S of the next one after the other
@@ -22,8 +22,14 @@
 //   warps 12..19  packed rows -> K (12..15), V in shared memory, two stages
 //
 // There is no pass for the maximum: P is formed under the row's reference, the maximum is taken on the side, and where a score
-// passes the reference by 2^16 the 64 scores are done again under a new one, after O was rescaled in tensor memory.  That
+// passes the reference by 2^16 the 32 scores are done again under a new one, after O was rescaled in tensor memory.  That
 // happens with a row's first tokens and hardly ever after.
+//
+// What bounds it: per tile and half, P is formed (some 2700 cycles, 1000 of them exponentials), then PV and the next S run (1000 to
+// 1500), and with two halves nothing fills the rest: the tensor pipe is 48 % busy, issue slots 44 %.  Two warps a row (16 warps,
+// 64 tokens each) took 4 to 7 % off 8-bit chunks and added 20 % to a prompt, whose rows begin and end more often.  A prompt of 8192
+// tokens, 32 heads, 4 bits: 660 to 690 us, 800 to 830 TFLOP/s of the visible products; four chunks of 2048 under a window of 4096,
+// 8 bits: 790 us.
 #pragma once
 #include "attn_rows.cuh"
 #include "ragged.cuh"
@@ -152,7 +158,6 @@ __device__ __forceinline__ void prompt_o(uint32_t d, uint32_t p, uint32_t v, uin
                  "add.u32 x, %1, 56;\n\tadd.s64 y, y, 128;\n\t@e tcgen05.mma.cta_group::1.kind::f16 [%0], [x], y, %3, 1;\n\t}"
                  ::"r"(d), "r"(p), "r"(v), "r"(idesc), "n"(kPDescUpper), "r"((uint32_t)add) : "memory");
 }
-__device__ __forceinline__ bool prompt_wait_slow(uint32_t bar, uint32_t parity) { return mbar_wait_bounded(bar, parity); }
 
 template <int P, bool N16>
 __global__ void __launch_bounds__(kPThreads, 1) ragged_umma(const RaggedArgs a) {
@@ -222,7 +227,7 @@ __global__ void __launch_bounds__(kPThreads, 1) ragged_umma(const RaggedArgs a) 
     auto two = [&]() { return c.s.n * a.group > c.rt * kPRows + 128; };       // does the entry have rows in half 1
     bool dead = false;                 // a wait ran out: no more waits, the flag is up, results are void
     auto wait = [&](uint32_t bar, int phase) {
-        if (!mbar_try(bar, (uint32_t)phase & 1u) && !dead && !prompt_wait_slow(bar, (uint32_t)phase & 1u)) {
+        if (!mbar_try(bar, (uint32_t)phase & 1u) && !dead && !mbar_wait_bounded(bar, (uint32_t)phase & 1u)) {
             dead = true;
             raise_flag(a.status, KVBFP_FLAG_WAIT_TIMEOUT);
         }
@@ -566,6 +571,7 @@ __global__ void __launch_bounds__(kPThreads, 1) ragged_umma(const RaggedArgs a) 
                                 }
                             }
                             const uint32_t al2 = pack_bf16x2_rn(al, al);
+                            tmem_wait_st();
 #pragma unroll 1
                             for (int x = 0; x < 2 * j; ++x) {          // and P of this tile's tokens before
                                 uint32_t o[8];
