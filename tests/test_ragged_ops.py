@@ -306,6 +306,77 @@ def test_ragged_attn_long_prompts_are_not_refused():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("bits,block", [(4, 16), (4, 32), (6, 64), (8, 32)])
+@pytest.mark.parametrize("page", [0, 16, 128])
+def test_ragged_attn_hidden_rows_may_hold_anything(page, bits, block, dtype):
+    """Rows behind the sequences, in pages of no sequence, before the window: all ones, exponent bytes too (no row that was
+    written holds them)."""
+    news, lens, window, sink = [1, 130, 5], [201, 390, 77], 64, 5
+    cache, pool, q, starts, n, perm, perm_v = batch_of(news, lens, 2, 2, bits, block, page, dtype, 31)
+    ref = reference(cache, pool, q, news, lens, perm, perm_v, window, sink)
+    seen = torch.zeros(cache.fmt.batch, cache.fmt.max_seq, dtype=torch.bool, device="cuda")
+    for b, (new, ln) in enumerate(zip(news, lens)):
+        for t in [*range(sink), *range(max(ln - new - window + 1, 0), ln)]:
+            if pool is None:
+                seen[b, t] = True
+            else:
+                seen[int(pool.table[b, t // page]), t % page] = True
+    for name in ("k_mant", "k_exp", "v_mant", "v_exp"):
+        x = getattr(cache, name)
+        x.masked_fill_(~seen[:, None, :, None], 255)
+    kw = dict(perm_k=perm, inv_perm_v=inverse(perm_v), pool=pool)
+    check(B.ragged_attn(cache, q, starts, n, 130, window=window, n_sink=sink, **kw), *ref)
+    check(B.ragged_attn(cache, q, starts, n, 1, window=window, n_sink=sink, **kw), *ref)
+    assert B.device_status() == 0
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_ragged_attn_bad_queries_stay_alone(dtype):
+    """A query of NaN or infinities spoils its own row only."""
+    news, lens = [1, 200, 2], [90, 333, 70]
+    args = batch_of(news, lens, 2, 2, 4, 32, 32, dtype, 32)
+    q = args[2]
+    ref = reference(args[0], args[1], q, news, lens, args[5], args[6])
+    good = torch.ones(q.shape[:2], dtype=torch.bool, device="cuda")
+    for at, value in (((0, 1), math.nan), ((50, 2), math.inf), ((51, 0), -math.inf), ((201, 3), math.nan)):
+        q[at[0], at[1], 17:40] = value
+        good[at] = False
+    got = attend(args, news)
+    check(got[good], *(x[good] for x in ref))
+    assert not bool(torch.isfinite(got[~good]).all(-1).any())
+
+
+@pytest.mark.gpu
+def test_ragged_attn_graphs_share_a_workspace():
+    """Two captured calls of different batches over one workspace, replayed in turn."""
+    calls = []
+    for news, lens, seed in (([1, 300, 2], [700, 300, 90], 41), ([9, 1, 64], [9, 5000, 600], 42)):
+        args = batch_of(news, lens, 2, 2, 4, 32, 32, torch.bfloat16, seed)
+        calls.append((args, news, reference(args[0], args[1], args[2], news, lens, args[5], args[6])))
+    need = max(B.ragged_workspace_bytes(a[0].fmt, 3, 4, sum(n)) for a, n, _ in calls)
+    ws = torch.full((need,), 255, dtype=torch.uint8, device="cuda")
+    outs = [torch.zeros_like(a[2]) for a, _, _ in calls]
+    kws = [dict(out=o, workspace=ws) for o in outs]
+    for (a, n, _), kw in zip(calls, kws):
+        attend(a, n, **kw)
+    torch.cuda.synchronize()
+    graphs = []
+    for (a, n, _), kw in zip(calls, kws):
+        inv = inverse(a[6])
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            B.ragged_attn(a[0], a[2], a[3], a[4], max(n), perm_k=a[5], inv_perm_v=inv, pool=a[1], **kw)
+        graphs.append((g, inv))
+    for i in (0, 1, 1, 0, 1, 0):
+        outs[i].zero_()
+        graphs[i][0].replay()
+        check(outs[i], *calls[i][2])
+    assert B.device_status() == 0
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("scale", [2.0 ** 90, 2.0 ** -90])
 def test_ragged_attn_large_and_small_values(scale):
     news, lens = [1, 100], [150, 130]
