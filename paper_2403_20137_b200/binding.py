@@ -333,9 +333,9 @@ def dequant_all(cache, which, n_tok, perm=None, t0=0, out_dtype=torch.float32, s
     (the layout append() takes)."""
     mant, exp8 = (cache.k_mant, cache.k_exp) if which == "k" else (cache.v_mant, cache.v_exp)
     f = cache.fmt
-    out = torch.empty((f.batch, n_tok, f.n_kv_heads, f.head_dim), dtype=out_dtype, device=mant.device)
-    rc = lib().kvbfp_dequant(C.byref(f), mant.data_ptr(), exp8.data_ptr(), -1, -1, t0, n_tok, _ptr(_dev(perm, torch.int32)),
-                             out.data_ptr(), _dt(out), _stream(stream))
+    out = mant.new_empty((f.batch, n_tok, f.n_kv_heads, f.head_dim), dtype=out_dtype)
+    rc = lib().kvbfp_dequant(C.byref(f), mant.data_ptr(), exp8.data_ptr(), -1, -1, t0, n_tok,
+                             None if perm is None else _ptr(_dev(perm, torch.int32)), out.data_ptr(), _dt(out), _stream(stream))
     if rc:
         _check(rc)
     return out
