@@ -17,7 +17,7 @@
 // those of the formula.
 //
 // What bounds it: instructions (issue slots 47 % busy, memory 32 %), most of them in the casts.  Four prompts of 8192 tokens, 32
-// query and 8 kv heads, 4 bits: 123 us, floor 71.
+// query and 8 kv heads, 4 bits: 121 us, floor 71.
 #include <atomic>
 
 #include "pages.cuh"
@@ -587,9 +587,11 @@ kvbfp_status launch_write(WriteArgs a, cudaStream_t s) {
     if (st != KVBFP_OK) return st;
     const int n_heads = a.heads[0] + a.heads[1] + a.heads[2];
     const int64_t pairs = ((int64_t)a.n_tokens + 1) / 2, gx = (pairs + kWWarps - 1) / kWWarps;
-    // few tokens: heads spread over the blocks too, down to one head a warp
+    // few tokens: heads spread over the blocks too, down to one head a warp.  Up to four rounds of three blocks an SM in halves, whose
+    // last round is shorter (3 and 4 prompts 95.8 -> 93.1, 122.8 -> 120.5 us); later what a warp begins with costs more (6 and 14
+    // prompts 163.2 -> 165.1, 324 -> 345 us).
     int64_t chunks = (int64_t)n_sm * 4 / gx;
-    if (chunks < 1) chunks = 1;
+    if (chunks < 2) chunks = gx < (int64_t)n_sm * 12 ? 2 : 1;
     if (chunks > n_heads) chunks = n_heads;
     a.head_chunk = (int)((n_heads + chunks - 1) / chunks);
     const dim3 grid((unsigned)gx, (unsigned)((n_heads + a.head_chunk - 1) / a.head_chunk));
