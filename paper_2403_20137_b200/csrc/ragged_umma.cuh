@@ -25,11 +25,13 @@
 // passes the reference by 2^16 the 32 scores are done again under a new one, after O was rescaled in tensor memory.  That
 // happens with a row's first tokens and hardly ever after.
 //
-// What bounds it: per tile and half, P is formed (some 2700 cycles, 1000 of them exponentials), then PV and the next S run (1000 to
-// 1500), and with two halves nothing fills the rest: the tensor pipe is 48 % busy, issue slots 44 %.  Two warps a row (16 warps,
-// 64 tokens each) took 4 to 7 % off 8-bit chunks and added 20 % to a prompt, whose rows begin and end more often.  A prompt of 8192
-// tokens, 32 heads, 4 bits: 660 to 690 us, 800 to 830 TFLOP/s of the visible products; four chunks of 2048 under a window of 4096,
-// 8 bits: 790 us.
+// What bounds it: the matrix instructions of a tile, one after the other.  The 16 of a half take 1400 to 1700 cycles from the first
+// issue to the last (64 each at the pipe's rate; both operands of S come from shared memory, which conversion and results use
+// too), and waits and reports some 400 more; so a tile takes 4500 to 5000, the tensor pipe is 46 % busy, issue slots 40 %, and rows
+// and conversion wait half of the time.  Hence two warps a row (16 warps, 64 tokens each) took 4 to 7 % off 8-bit chunks only,
+// and added 20 % to a prompt, whose entries begin and end more often; unrolling the issuing loop over halves and stages added
+// 15 to 25 %.  A prompt of 8192 tokens, 32 heads, 4 bits: 660 to 690 us, 800 to 830 TFLOP/s of the visible products; four chunks
+// of 2048 under a window of 4096, 8 bits: 790 us.
 #pragma once
 #include "attn_rows.cuh"
 #include "ragged.cuh"
