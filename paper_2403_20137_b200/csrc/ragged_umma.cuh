@@ -21,16 +21,16 @@
 //   warps 4..11   rows: S -> P, rescaling, pi(Q) into shared memory, results     (halves 0 and 1)
 //   warps 12..19  packed rows -> K (12..15), V in shared memory, two stages
 //
-// There is no pass for the maximum: P is formed under the row's reference, the maximum is taken on the side, and where a score
-// passes the reference by 2^16 the 32 scores are done again under a new one, after O was rescaled in tensor memory.  That
-// happens with a row's first tokens and hardly ever after.
+// There is no pass for the maximum: P is formed under the row's reference, and where the sum of 32 weights passes 2^16 they are
+// done again under a new one, their scores' maximum, after O was rescaled in tensor memory.  That happens with a row's first
+// tokens and hardly ever after.  (With the maximum taken on the side of every score: a prompt of 8192 tokens 690 us against 660.)
 //
 // What bounds it: the matrix instructions of a tile, one after the other.  The 16 of a half take 1400 to 1700 cycles from the first
 // issue to the last (64 each at the pipe's rate; both operands of S come from shared memory, which conversion and results use
 // too), and waits and reports some 400 more; so a tile takes 4500 to 5000, the tensor pipe is 46 % busy, issue slots 40 %, and rows
 // and conversion wait half of the time.  Hence two warps a row (16 warps, 64 tokens each) took 4 to 7 % off 8-bit chunks only,
 // and added 20 % to a prompt, whose entries begin and end more often; unrolling the issuing loop over halves and stages added
-// 15 to 25 %.  A prompt of 8192 tokens, 32 heads, 4 bits: 660 to 690 us, 800 to 830 TFLOP/s of the visible products; four chunks
+// 15 to 25 %.  A prompt of 8192 X/s of the visible products; four chunks
 // of 2048 under a window of 4096, 8 bits: 790 us.
 #pragma once
 #include "attn_rows.cuh"
@@ -43,9 +43,9 @@ namespace {
 constexpr int kPRows = 256, kPTile = 128, kPThreads = 20 * 32;
 // shared memory: Q (two halves), K, V (two stages each), 32 lines of 128 bytes for each warp's results, barriers
 constexpr int kPQ = 0, kPK = 65536, kPV = 131072, kPOut = 196608, kPBars = kPOut + 8 * 4096, kPSmem = kPBars + 256;
-// A score may pass the reference maximum by so much (in powers of two) before the reference follows: P, its sums and O are
-// floating-point numbers, which lose nothing by a common factor, and have room for it.
-constexpr float kPSlack = 16.f;
+// So large may the sum of 32 weights become before the reference follows: P, its sums and O are floating-point numbers, which
+// lose nothing by a common factor, and have room for it.
+constexpr float kPLimit = 65536.f;
 constexpr int kPPanel = kPTile * 128;                                  // 64 positions of 128 rows
 
 // Registers a thread after the split, of the 96 that the launch gives each: rows, packed rows, the rest (2 x 136 + 2 x 80 + 48 =
@@ -518,9 +518,9 @@ __global__ void __launch_bounds__(kPThreads, 1) ragged_umma(const RaggedArgs a) 
                 tmem_fence_after();
                 if (here) {
                     const bool clear = tt + 127 <= pos_lo && (a.window == 0 || tt > pos_hi - a.window || tt + 128 <= a.n_sink);
-                    // 32 tokens at a time, the next ones on their way.  P is formed under the reference there is; where a score
-                    // passes it by kPSlack (a run's first tokens, hardly ever else) the reference is raised and the scores, which
-                    // are still there, are read again.
+                    // 32 tokens at a time, the next ones on their way.  P is formed under the reference there is; where its sum
+                    // passes kPLimit (a run's first tokens, hardly ever else) the scores, which are still there, are read again
+                    // and the reference goes up to their maximum.
                     uint32_t s[2][32];
                     tmem_ld<32>(tms, s[0]);
 #pragma unroll
@@ -529,34 +529,41 @@ __global__ void __launch_bounds__(kPThreads, 1) ragged_umma(const RaggedArgs a) 
                         tmem_wait_ld(v);
                         if (j < 3) tmem_ld<32>(tms + 32 * (j + 1), s[(j + 1) & 1]);
                         uint32_t p[16];
-                        F2 sum;
-                        auto form = [&]() {          // P of the 32 scores; the largest score, in log2 units
-                            if (!clear) {            // hidden ones -inf: tokens up to pos are seen, from see_lo on or among the first ones
-                                const int t0 = tt + 32 * j;
-                                auto below = [](int n) { return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u; };
-                                const uint32_t see = below(pos - t0 + 1) & (~below(see_lo - t0) | below(a.n_sink - t0));
+                        float sum;
+                        auto hide = [&]() {          // hidden ones -inf: tokens up to pos are seen, from see_lo on or among the first ones
+                            if (clear) return;
+                            const int t0 = tt + 32 * j;
+                            auto below = [](int n) { return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u; };
+                            const uint32_t see = below(pos - t0 + 1) & (~below(see_lo - t0) | below(a.n_sink - t0));
 #pragma unroll
-                                for (int e = 0; e < 32; ++e) v[e] = (see >> e) & 1u ? v[e] : 0xff800000u;
-                            }
+                            for (int e = 0; e < 32; ++e) v[e] = (see >> e) & 1u ? v[e] : 0xff800000u;
+                        };
+                        auto form = [&]() {          // P of the 32 scores and its sum
                             const F2 mul2 = f2(mul, mul), neg2 = f2(-m, -m);
-                            float t[2] = {-INFINITY, -INFINITY};
                             F2 sums[2] = {f2(0.f, 0.f), f2(0.f, 0.f)};
 #pragma unroll
                             for (int e = 0; e < 16; ++e) {
-                                const float s0 = __uint_as_float(v[2 * e]), s1 = __uint_as_float(v[2 * e + 1]);
                                 float x0, x1;
-                                f2_split(f2_fma(f2(s0, s1), mul2, neg2), x0, x1);
-                                t[e & 1] = max3(t[e & 1], s0, s1);
+                                f2_split(f2_fma(f2(__uint_as_float(v[2 * e]), __uint_as_float(v[2 * e + 1])), mul2, neg2), x0, x1);
                                 x0 = ex2_approx(x0);
                                 x1 = ex2_approx(x1);
                                 sums[e & 1] = f2_add(sums[e & 1], f2(x0, x1));
                                 p[e] = pack_bf16x2_rn(x0, x1);
                             }
-                            sum = f2_add(sums[0], sums[1]);
-                            return mul * fmaxf(t[0], t[1]);
+                            float a0, a1;
+                            f2_split(f2_add(sums[0], sums[1]), a0, a1);
+                            sum = a0 + a1;
                         };
-                        const float top = form();
-                        if (__any_sync(0xffffffffu, top > m + kPSlack)) {
+                        hide();
+                        form();
+                        if (__any_sync(0xffffffffu, sum > kPLimit)) {
+                            tmem_ld<32>(tms + 32 * j, v);
+                            tmem_wait_ld(v);
+                            hide();
+                            float top = -INFINITY;
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) top = max3(top, __uint_as_float(v[2 * e]), __uint_as_float(v[2 * e + 1]));
+                            top *= mul;
                             // (whole numbers, so that what is there is scaled by a power of two)
                             const float y = fmaxf(m, ceilf(top)), al = ex2_approx(m - y);
                             m = y;
@@ -583,14 +590,10 @@ __global__ void __launch_bounds__(kPThreads, 1) ragged_umma(const RaggedArgs a) 
                                 for (int e = 0; e < 8; ++e) o[e] = mul_bf16x2(o[e], al2);
                                 tmem_st<8>(tms + 8 * x, o);
                             }
-                            tmem_ld<32>(tms + 32 * j, v);
-                            tmem_wait_ld(v);
-                            (void)form();
+                            form();
                         }
                         tmem_st<16>(tms + 16 * j, p);
-                        float a0, a1;
-                        f2_split(sum, a0, a1);
-                        l += a0 + a1;
+                        l += sum;
                     }
                     tmem_wait_st();
                 }
