@@ -23,15 +23,16 @@
 //
 // There is no pass for the maximum: P is formed under the row's reference, and where the sum of 32 weights passes 2^16 they are
 // done again under a new one, their scores' maximum, after O was rescaled in tensor memory.  That happens with a row's first
-// tokens and hardly ever after.  (With the maximum taken on the side of every score: a prompt of 8192 tokens 690 us against 660.)
+// tokens and hardly ever after.  (With the maximum taken on the side of every score: a prompt of 8192 tokens 690 us, 660 so.)
 //
-// What bounds it: the matrix instructions of a tile, one after the other.  The 16 of a half take 1400 to 1700 cycles from the first
-// issue to the last (64 each at the pipe's rate; both operands of S come from shared memory, which conversion and results use
-// too), and waits and reports some 400 more; so a tile takes 4500 to 5000, the tensor pipe is 46 % busy, issue slots 40 %, and rows
-// and conversion wait half of the time.  Hence two warps a row (16 warps, 64 tokens each) took 4 to 7 % off 8-bit chunks only,
-// and added 20 % to a prompt, whose entries begin and end more often; unrolling the issuing loop over halves and stages added
-// 15 to 25 %.  A prompt of 8192 X/s of the visible products; four chunks
-// of 2048 under a window of 4096, 8 bits: 790 us.
+// What bounds it: two chains of about the same length.  The matrix instructions of a tile, one half's after the other's: 16 take 1400
+// to 1700 cycles from the first issue to the last (64 each at the pipe's rate; both operands of S come from shared memory, which
+// conversion and results use too), and waits and reports some 400 more.  And a half by itself: P some 2200, its products, 250 for
+// each to learn of the other.  A tile takes some 4400; the tensor pipe is half busy.  Two warps a row (16 warps, 64 tokens each)
+// took 4 to 7 % off 8-bit chunks only, and added 20 % to a prompt, whose entries begin and end more often; unrolling the issuing
+// loop over halves and stages added 15 to 25 %; waiting for the next step's rows between the halves and not after them took 2 to
+// 4 % off.  A prompt of 8192 tokens, 32 heads, 4 bits: 644 us, 854 TFLOP/s of the visible products; four chunks of 2048 under a
+// window of 4096, 8 bits: 752 us.
 #pragma once
 #include "attn_rows.cuh"
 #include "ragged.cuh"
@@ -274,16 +275,18 @@ __global__ void __launch_bounds__(kPThreads, 1) ragged_umma(const RaggedArgs a) 
         const uint32_t qd = prompt_desc(base + kPQ, 16), kd = prompt_desc(base + kPK, 16), vd = prompt_desc(base + kPV, kPPanel);
         int runs = 0;                 // parities of the runs of the halves so far (bits 0 and 1)
         int now = 0, next = 0;        // flags of tiles j - 1 and j
+        auto flags_of = [&](int j) {       // of tile j, once what step j needs is converted
+            wait(b_full(j), j >> 1);
+            if (j >= n) return 0;
+            if ((j & 7) == 0) wait(b_plan(j), j >> 4);
+            const int f = __shfl_sync(0xffffffffu, *(volatile int*)&s_flags[j & 15], 0);
+            if ((j & 7) == 7 && lane == 0) mbar_arrive(b_used(j));
+            return f;
+        };
+        if (n > 0) next = flags_of(0);
         for (int j = 0; j <= n && n > 0; ++j) {
             const int st = j & 1;
-            wait(b_full(j), j >> 1);
-            now = next;
-            next = 0;
-            if (j < n) {
-                if ((j & 7) == 0) wait(b_plan(j), j >> 4);
-                next = __shfl_sync(0xffffffffu, *(volatile int*)&s_flags[j & 15], 0);
-                if ((j & 7) == 7 && lane == 0) mbar_arrive(b_used(j));
-            }
+            int after = 0;
 #pragma unroll 1
             for (int h = 0; h < 2; ++h) {
                 const uint32_t tmh = tmu + 128 * h;
@@ -307,8 +310,11 @@ __global__ void __launch_bounds__(kPThreads, 1) ragged_umma(const RaggedArgs a) 
                         prompt_s(tmh, qd + ((h * 32768) >> 4), kd + ((st * 32768) >> 4), id_s);
                     }
                     umma_commit(b_s(h, j));
+                    if (h == 0) after = flags_of(j + 1);          // (between the halves, where it costs nothing)
                 }
             }
+            now = next;
+            next = after;
             if (__any_sync(0xffffffffu, dead)) break;
         }
         if (__any_sync(0xffffffffu, dead)) {
