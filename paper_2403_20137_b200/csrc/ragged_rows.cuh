@@ -6,6 +6,11 @@
 // Pages.  A tile is copied in pieces of a page (or of the tile where pages are longer), a lane per piece; the piece's page
 // number was asked for one tile earlier, so that the copy does not wait for the table.  Pieces that no row sees are not copied:
 // what lies there in shared memory is converted all the same (any byte converts to a finite number) and masked.
+//
+// What bounds it: instructions, 357 per warp and 16 tokens, most of them the conversion of fields (integer pipe 56 % busy, issue slots
+// 61 %, three warps a scheduler).  16 tokens, 32 heads x 8192, 4 bits, pages of 64: 146 us, 3.9 TB/s; 8 tokens, 8 heads x up to
+// 32768, four query heads each, pages of 32: 65 us; one token under a window of 1000: 10.9 us with the merge.  V's words loaded
+// before the softmax: no gain (145 us; 8 bits 133 against 130).
 #pragma once
 #include "attn_rows.cuh"
 #include "ragged.cuh"
