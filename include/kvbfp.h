@@ -465,8 +465,9 @@ size_t kvbfp_ragged_workspace_bytes(const kvbfp_format* fmt, int32_t batch, int3
  *              missing, KVBFP_FLAG_POSITION is set and the sequence's rows are unspecified
  *   out        [n_tokens, n_q_heads, head_dim] of `dt`; zeros for tokens at negative positions.  Rows behind starts[batch] are
  *              left as they were
- * perm_k, inv_perm_v, softmax_scale as in kvbfp_decode_attn.  n_q_heads <= 8 n_kv_heads, batch <= 1024.  Types and accuracy as
- * in kvbfp_tree_attn.  Lengths beyond the cache are read clamped and set KVBFP_FLAG_POSITION; so do starts that decrease
+ * perm_k, inv_perm_v, softmax_scale as in kvbfp_decode_attn.  n_q_heads <= 8 n_kv_heads, batch <= 1024.  Types, range and
+ * accuracy as in kvbfp_tree_attn, but sequences of up to eight bf16 query rows per kv head (new tokens times n_q_heads / n_kv_heads;
+ * batch 1: rows of q) keep 16 bits of the softmax weights, as kvbfp_decode_attn does.  Lengths beyond the cache are read clamped and set KVBFP_FLAG_POSITION; so do starts that decrease
  * (out is unspecified then).  No atomics: the result depends on nothing but the arguments.  KVBFP_ERR_UNSUPPORTED where the pieces
  * of work pass 2^31 (bf16: from some 10^6 new tokens over a cache of as many on; f32: from some 10^5).
  */

@@ -112,8 +112,8 @@ constexpr int kEntryTiles = 3;
 struct Kernel {
     int rows_tile, tile, max_workers;
 };
-inline Kernel kernel_of(bool umma, int mant_bits) {
-    return umma ? Kernel{256, 128, kAttnMaxSms} : Kernel{8, attn_rows_tile(mant_bits), 3 * kAttnWarps * kAttnMaxSms};
+inline Kernel kernel_of(bool umma, int mant_bits, int few_tile = kFewRows) {
+    return umma ? Kernel{256, 128, kAttnMaxSms} : Kernel{few_tile, attn_rows_tile(mant_bits), 3 * kAttnWarps * kAttnMaxSms};
 }
 
 // Workspace of one of the two from `base` on; returns the size and, with `a`, sets the pointers.
@@ -129,9 +129,8 @@ size_t lay_out(const Kernel& k, int64_t rows, RaggedArgs* a, uint8_t* base) {
     return rec + up256((size_t)2 * k.max_workers * part_rows * kAttnPart * 4);
 }
 
-kvbfp_status launch_kernel(RaggedArgs a, bool umma, int64_t rows, uint8_t* workspace, int n_sm, cudaStream_t s) {
+kvbfp_status launch_kernel(RaggedArgs a, bool umma, const Kernel& k, int64_t rows, uint8_t* workspace, int n_sm, cudaStream_t s) {
     const int bits = a.fmt.mant_bits;
-    const Kernel k = kernel_of(umma, bits);
     (void)lay_out(k, rows, &a, workspace);
     const int64_t most = (rows / k.rows_tile + a.batch) * a.fmt.n_kv_heads * (a.map.cap / k.tile + 2 + kEntryTiles);
     const int per_block = umma ? 1 : kAttnWarps;
@@ -213,15 +212,19 @@ extern "C" kvbfp_status kvbfp_ragged_attn(const kvbfp_cache* cache, const kvbfp_
     const auto countable = [&](const Kernel& k, int64_t row_tiles) {
         return row_tiles * f.n_kv_heads * (a.map.cap / k.tile + 2 + kEntryTiles) < (int64_t)1 << 31;
     };
-    const Kernel k_few = kernel_of(false, f.mant_bits), k_many = kernel_of(true, f.mant_bits);
+    // ragged_rows: four bf16 rows an item where more are not expected (single tokens, or single tokens between longer sequences),
+    // whose second term of the weights costs 1 %; eight, which read the cache once for all of them (second term: 4.5 to 12 %), otherwise.
+    const int64_t hint = (int64_t)max_new * group;
+    const bool four = bf16 && (hint <= 4 || (hint > kFewRows && group <= 4)) && countable(kernel_of(false, f.mant_bits, 4), rows / 4 + batch);
+    const Kernel k_few = kernel_of(false, f.mant_bits, four ? 4 : kFewRows), k_many = kernel_of(true, f.mant_bits);
     const bool all_few = countable(k_few, rows / k_few.rows_tile + batch);
-    const bool many = bf16 && rows > kFewRows && ((int64_t)max_new * group > kFewRows || !all_few);
+    const bool many = bf16 && rows > kFewRows && (hint > kFewRows || !all_few);
     if (many ? !countable(k_few, batch) || !countable(k_many, rows / k_many.rows_tile + batch) : !all_few) return KVBFP_ERR_UNSUPPORTED;
     a.few_lo = 0;
     a.few_hi = many ? kFewRows : 0x7fffffff;
-    st = !many || batch > 1 ? launch_kernel(a, false, rows, ws, n_sm, s) : KVBFP_OK;
+    st = !many || batch > 1 ? launch_kernel(a, false, k_few, rows, ws, n_sm, s) : KVBFP_OK;
     if (st != KVBFP_OK || !many) return st;
     a.few_lo = batch > 1 ? kFewRows : 0;
     a.few_hi = 0x7fffffff;
-    return launch_kernel(a, true, rows, ws + few_bytes, n_sm, s);
+    return launch_kernel(a, true, k_many, rows, ws + few_bytes, n_sm, s);
 }

@@ -259,7 +259,7 @@ __device__ __forceinline__ int ragged_find(const RaggedArgs& a, const int* s_ite
     return lo;
 }
 
-// ragged_rows: items of eight rows, a worker per warp
+// ragged_rows: items of eight rows, or of four (by rows_tile), a worker per warp
 kvbfp_status launch_ragged_rows4(const RaggedArgs& a, int grid, cudaStream_t s);
 kvbfp_status launch_ragged_rows6(const RaggedArgs& a, int grid, cudaStream_t s);
 kvbfp_status launch_ragged_rows8(const RaggedArgs& a, int grid, cudaStream_t s);

@@ -7,9 +7,15 @@
 // number was asked for one tile earlier, so that the copy does not wait for the table.  Pieces that no row sees are not copied:
 // what lies there in shared memory is converted all the same (any byte converts to a finite number) and masked.
 //
+// Weights.  bf16 queries: P in two bf16 terms, hi = P rounded, lo = (P - hi) rounded (2^-16 relative at most, as many bits as
+// kvbfp_decode_attn keeps).  Items of up to four rows (TWICE) need no more products for it: the rows stand in the matrix
+// instruction's eight columns twice, and the second time P is lo; the columns' results are added at the end.  Items of eight
+// rows take a second product.  (One term: 146 and 65 us of the times below, 148 and 66 with TWICE, 164 and 72 with a second product; eight
+// 6-bit rows 129, 135.)  fp32 queries: three terms of q and P.
+//
 // What bounds it: instructions, 357 per warp and 16 tokens, most of them the conversion of fields (integer pipe 56 % busy, issue slots
-// 61 %, three warps a scheduler).  16 tokens, 32 heads x 8192, 4 bits, pages of 64: 146 us, 3.9 TB/s; 8 tokens, 8 heads x up to
-// 32768, four query heads each, pages of 32: 65 us; one token under a window of 1000: 10.9 us with the merge.  V's words loaded
+// 61 %, three warps a scheduler).  16 tokens, 32 heads x 8192, 4 bits, pages of 64: 148 us, 3.8 TB/s; 8 tokens, 8 heads x up to
+// 32768, four query heads each, pages of 32: 66 us; one token under a window of 1000: 11.3 us with the merge.  V's words loaded
 // before the softmax: no gain (145 us; 8 bits 133 against 130).
 #pragma once
 #include "attn_rows.cuh"
@@ -19,11 +25,12 @@
 namespace kvbfp {
 namespace {
 
-template <int P, bool N16, bool F32>
+template <int P, bool N16, bool F32, bool TWICE>
 __global__ void __launch_bounds__(kAttnWarps * 32, attn_rows_blocks(!F32)) ragged_rows(const RaggedArgs a, const __grid_constant__ CUtensorMap k_map,
                                                                                          const __grid_constant__ CUtensorMap v_map) {
     using G_ = AGeo<P>;
-    constexpr int D = kHeadDim, ROW_M = G_::ROW_M, STAGES = G_::STAGES, TILE = G_::TILE, ROWS = kRows, SPLIT = F32 ? 3 : 1;
+    constexpr int D = kHeadDim, ROW_M = G_::ROW_M, STAGES = G_::STAGES, TILE = G_::TILE, ROWS = TWICE ? 4 : kRows;
+    constexpr int SPLIT = F32 ? 3 : 1, TERMS = F32 ? 3 : TWICE ? 1 : 2;      // bf16 terms of q, of P in products of their own
     constexpr int GROUP = 16 * ROW_M;
     extern __shared__ __align__(1024) uint8_t smem[];
     __shared__ int s_scan[2][kAttnWarps];
@@ -127,6 +134,8 @@ __global__ void __launch_bounds__(kAttnWarps * 32, attn_rows_blocks(!F32)) ragge
 #pragma unroll
     for (int j = 0; j < 2; ++j) tk[j] = tok_of<P>(g >> 1, g & 1, j);
 
+    const float rest = !TWICE || t >= 2 ? -1.f : 0.f;         // is the next term what the one before left
+
     bool dead = false;            // a copy did not arrive: no more waits, no more work, the flag is up
     int it = 0;
     int4 rec = make_int4(-1, 0, 0, 0);
@@ -137,14 +146,14 @@ __global__ void __launch_bounds__(kAttnWarps * 32, attn_rows_blocks(!F32)) ragge
         const int k0 = cc.k, k1 = min(sv.n, k0 + n_mine - it);
         uint4 qr[SPLIT][4];           // k steps 2 i, 2 i + 1
         {
-            const int row = rt * ROWS + g, i = row / a.group;
+            const int row = rt * ROWS + (TWICE ? g & 3 : g), i = row / a.group;
             const int64_t at = ((int64_t)(cc.s.start + i) * a.n_q_heads + hk * a.group + row - i * a.group) * D;
             const void* q = F32 ? (const void*)(static_cast<const float*>(a.q) + at) : (const void*)(static_cast<const __nv_bfloat16*>(a.q) + at);
             load_q<P, F32>(a, row < R ? q : nullptr, hk, t, qr);
         }
         int pos[2];                   // of rows 2 t, 2 t + 1
 #pragma unroll
-        for (int e = 0; e < 2; ++e) pos[e] = cc.s.base + min(rt * ROWS + 2 * t + e, R - 1) / a.group;
+        for (int e = 0; e < 2; ++e) pos[e] = cc.s.base + min(rt * ROWS + 2 * (TWICE ? t & 1 : t) + e, R - 1) / a.group;
 
         float o[8][4];                // slots 16 g + 2 i (+ 1: upper pair) of rows 2 t, 2 t + 1
         float m_run[2], l_run[2];     // of rows 2 t, 2 t + 1
@@ -246,8 +255,8 @@ __global__ void __launch_bounds__(kAttnWarps * 32, attn_rows_blocks(!F32)) ragge
 #pragma unroll
                 for (int gr = 0; gr < 2; ++gr) {
                     const uint8_t *gm = stm + gr * GROUP, *ge = ste + gr * 16 * row_e;
-                    // P as B fragments: a token's pair of rows, transposed; fp32: three terms
-                    uint32_t pb[SPLIT][2];
+                    // P as B fragments: a token's pair of rows, transposed, in its terms
+                    uint32_t pb[TERMS][2];
 #pragma unroll
                     for (int j = 0; j < 2; ++j) {
                         float p0 = ex2_approx(fmaf(sc[gr][2 * j], mul, -m_run[0]));
@@ -255,10 +264,11 @@ __global__ void __launch_bounds__(kAttnWarps * 32, attn_rows_blocks(!F32)) ragge
                         l_run[0] += p0;
                         l_run[1] += p1;
 #pragma unroll
-                        for (int s = 0; s < SPLIT; ++s) {
-                            const uint32_t x = pack_bf16x2_rn(p0, p1);
-                            p0 -= __uint_as_float(x << 16);
-                            p1 -= __uint_as_float(x & 0xffff0000u);
+                        for (int s = 0; s < TERMS; ++s) {
+                            uint32_t x = pack_bf16x2_rn(p0, p1);
+                            p0 = fmaf(rest, __uint_as_float(x << 16), p0);
+                            p1 = fmaf(rest, __uint_as_float(x & 0xffff0000u), p1);
+                            if (TWICE) x = pack_bf16x2_rn(p0, p1);
                             pb[s][j] = transpose8(x);
                         }
                     }
@@ -290,10 +300,11 @@ __global__ void __launch_bounds__(kAttnWarps * 32, attn_rows_blocks(!F32)) ragge
                             if (F32) {
                                 float d[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                                for (int c = SPLIT - 1; c >= 0; --c) mma_bf16(d, xa[2 * h], xa[2 * h + 1], xb[2 * h], xb[2 * h + 1], pb[c][0], pb[c][1]);
+                                for (int c = TERMS - 1; c >= 0; --c) mma_bf16(d, xa[2 * h], xa[2 * h + 1], xb[2 * h], xb[2 * h + 1], pb[c][0], pb[c][1]);
                                 acc[0] += d[0]; acc[1] += d[1]; acc[2] += d[2]; acc[3] += d[3];
                             } else {
-                                mma_bf16(acc, xa[2 * h], xa[2 * h + 1], xb[2 * h], xb[2 * h + 1], pb[0][0], pb[0][1]);
+#pragma unroll
+                                for (int c = TERMS - 1; c >= 0; --c) mma_bf16(acc, xa[2 * h], xa[2 * h + 1], xb[2 * h], xb[2 * h + 1], pb[c][0], pb[c][1]);
                             }
                         }
                     }
@@ -303,7 +314,13 @@ __global__ void __launch_bounds__(kAttnWarps * 32, attn_rows_blocks(!F32)) ragge
             if (issued < n_mine) issue();
         }
 
-        // ---- the run's result: a lane holds slots [16 g, 16 g + 16) of rows 2 t and 2 t + 1
+        // ---- the run's result: a lane holds slots [16 g, 16 g + 16) of rows 2 t and 2 t + 1 (TWICE: t < 2)
+        if (TWICE) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) o[i][k] += __shfl_xor_sync(0xffffffffu, o[i][k], 2);
+        }
         const bool whole = k0 == 0 && k1 == sv.n;
         if (k0 > 0 && k1 == sv.n) rec = make_int4(b, rt, hk, worker_of(i0 + it - sv.n, n_items, workers));
 #pragma unroll
@@ -312,7 +329,7 @@ __global__ void __launch_bounds__(kAttnWarps * 32, attn_rows_blocks(!F32)) ragge
             l += __shfl_xor_sync(0xffffffffu, l, 4);
             l += __shfl_xor_sync(0xffffffffu, l, 8);
             l += __shfl_xor_sync(0xffffffffu, l, 16);
-            const int r = 2 * t + e, row = rt * ROWS + r;
+            const int r = 2 * t + e, row = r < ROWS ? rt * ROWS + r : R;      // (R: none)
             const int i = row / a.group, hq = hk * a.group + row - i * a.group;
             if (!whole) {
                 if (row < R) {
@@ -349,7 +366,7 @@ __global__ void __launch_bounds__(kAttnWarps * 32, attn_rows_blocks(!F32)) ragge
                 int sl[4];
 #pragma unroll
                 for (int c = 0; c < 4; ++c) sl[c] = ip[4 * lane + c] & (D - 1);
-                for (int tt = 0; tt < 4; ++tt) {
+                for (int tt = 0; tt < ROWS / 2; ++tt) {
                     if (rt * ROWS + 2 * tt + e >= R) break;
                     __syncwarp();
                     if (t == tt) {
@@ -381,9 +398,9 @@ __global__ void __launch_bounds__(kAttnWarps * 32, attn_rows_blocks(!F32)) ragge
     pdl_trigger();
 }
 
-template <int P, bool N16, bool F32>
+template <int P, bool N16, bool F32, bool TWICE>
 kvbfp_status launch_ragged(const RaggedArgs& a, int grid, cudaStream_t s) {
-    auto kernel = ragged_rows<P, N16, F32>;
+    auto kernel = ragged_rows<P, N16, F32, TWICE>;
     static std::atomic<bool> attr_set[64];      // per device; setting the attribute twice is harmless
     int dev = 0;
     KVBFP_CUDA(cudaGetDevice(&dev));
@@ -408,8 +425,9 @@ kvbfp_status launch_ragged(const RaggedArgs& a, int grid, cudaStream_t s) {
 template <int P>
 kvbfp_status launch_ragged_p(const RaggedArgs& a, int grid, cudaStream_t s) {
     const bool n16 = a.fmt.block == 16;
-    if (a.q_is_bf16) return n16 ? launch_ragged<P, true, false>(a, grid, s) : launch_ragged<P, false, false>(a, grid, s);
-    return n16 ? launch_ragged<P, true, true>(a, grid, s) : launch_ragged<P, false, true>(a, grid, s);
+    if (!a.q_is_bf16) return n16 ? launch_ragged<P, true, true, false>(a, grid, s) : launch_ragged<P, false, true, false>(a, grid, s);
+    if (a.rows_tile == 4) return n16 ? launch_ragged<P, true, false, true>(a, grid, s) : launch_ragged<P, false, false, true>(a, grid, s);
+    return n16 ? launch_ragged<P, true, false, false>(a, grid, s) : launch_ragged<P, false, false, false>(a, grid, s);
 }
 
 }  // namespace

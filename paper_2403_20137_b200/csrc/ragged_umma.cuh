@@ -25,6 +25,9 @@
 // done again under a new one, their scores' maximum, after O was rescaled in tensor memory.  That happens with a row's first
 // tokens and hardly ever after.  (With the maximum taken on the side of every score: a prompt of 8192 tokens 690 us, 660 so.)
 //
+// P is rounded to one bf16 term (2^-8 relative at most, at random; the output is rounded to bf16 too).  With a second term for what the
+// rounding leaves (P as many columns as S, 16 products a half for O instead of eight) a prompt of 8192 took 1126 us, chunks 1240.
+//
 // What bounds it: two chains of about the same length.  The matrix instructions of a tile, one half's after the other's: 16 take 1400
 // to 1700 cycles from the first issue to the last (64 each at the pipe's rate; both operands of S come from shared memory, which
 // conversion and results use too), and waits and reports some 400 more.  And a half by itself: P some 2200, its products, 250 for

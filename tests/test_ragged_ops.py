@@ -179,6 +179,24 @@ def test_ragged_attn_row_counts(group, new, bits):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("hint", [0, 1, 8])
+@pytest.mark.parametrize("bits,block", FMT)
+@pytest.mark.parametrize("group,news", [(1, [1, 4, 3]), (3, [1, 2, 1]), (4, [1, 1, 2]), (8, [1, 1, 1]), (5, [1, 0, 1])])
+def test_ragged_attn_weights_of_few_rows(group, news, bits, block, hint):
+    """Up to eight bf16 rows per kv head keep 16 bits of the weights.  Terms as in check(): two bf16 terms leave half a step of half a
+    step, 2^-16; a small scale, so that the bound of the scores does not hide it (weights all near one: outputs that cancel)."""
+    lens = [100, 77, 130]
+    args = batch_of(news, lens, 2, group, bits, block, 32, torch.bfloat16, group + bits + block)
+    cache, pool, q, starts, n, perm, perm_v = args
+    got = B.ragged_attn(cache, q, starts, n, hint, perm_k=perm, inv_perm_v=inverse(perm_v), pool=pool, softmax_scale=0.002).double()
+    out, amp, reach = reference(cache, pool, q, news, lens, perm, perm_v, scale=0.002)
+    bound = amp * (2 * 24 * 2.0 ** -23 * reach[..., None] + 2.0 ** -16 + 2.0 ** -20) * 1.01 + 2.0 ** -8 * out.abs() * 1.01
+    worst = float(((got - out).abs() / bound).max())
+    assert worst <= 1.0, f"error is {worst:.3g} of the bound"
+    assert B.device_status() == 0
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 def test_ragged_attn_long(dtype):
     """Work for every worker, entries that span several of them, ragged."""
