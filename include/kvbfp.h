@@ -437,7 +437,7 @@ kvbfp_status kvbfp_pages_copy(const kvbfp_cache* src, const kvbfp_cache* dst, co
  *   pages    host struct (cache is then its pool), or NULL: cache holds a sequence per batch entry
  *   q, k, v  token i at q + i * q_stride (in elements, a multiple of 16 bytes): heads densely, so that the three may lie in one
  *            array.  q may be NULL (then q_out too), or k and v together
- *   n_tokens rows of q, k, v and q_out; starts is read clamped to it
+ *   n_tokens rows of q, k, v and q_out; starts is read clamped to it.  0: nothing is done, q, k, v and q_out are not looked at
  *   q_weight, k_weight  [head_dim] f32 or NULL;  eps >= 0
  *   theta    [head_dim / 2] f64: frequency of each pair (zero: that pair stays)
  *   q_out    [n_tokens, n_q_heads, head_dim] of `dt`, channel order; may be q itself where that is dense
@@ -459,7 +459,7 @@ size_t kvbfp_ragged_workspace_bytes(const kvbfp_format* fmt, int32_t batch, int3
  * Attention of a ragged batch of new tokens (their K and V are in the cache already) over the packed cache, contiguous or in
  * pages: whole prompts, chunks of them and single tokens in one call.  The query at position p sees the tokens t <= p with
  *   t < n_sink  or  p - t < window                   (window 0: all)
- *   q          [n_tokens, n_q_heads, head_dim] of `dt`, original channel order
+ *   q          [n_tokens, n_q_heads, head_dim] of `dt`, original channel order.  n_tokens 0: nothing is done, q and out may be NULL
  *   max_new    largest number of new tokens of a sequence: a hint for the choice of kernels, any value gives the result
  *   pages      as in kvbfp_norm_rope_append; entries of pages that no query sees are not read.  Where one that is needed is
  *              missing, KVBFP_FLAG_POSITION is set and the sequence's rows are unspecified

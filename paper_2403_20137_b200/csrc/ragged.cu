@@ -174,7 +174,8 @@ extern "C" kvbfp_status kvbfp_ragged_attn(const kvbfp_cache* cache, const kvbfp_
     kvbfp_status st = check_format(&f);
     if (st == KVBFP_OK && pages) st = check_pool(f, pages);
     if (st != KVBFP_OK) return st;
-    if (!cache->k_mant || !cache->k_exp || !cache->v_mant || !cache->v_exp || !q || !starts || !seq_lens || !out) return KVBFP_ERR_INVALID_ARG;
+    if (!cache->k_mant || !cache->k_exp || !cache->v_mant || !cache->v_exp || !starts || !seq_lens) return KVBFP_ERR_INVALID_ARG;
+    if (n_tokens != 0 && (!q || !out)) return KVBFP_ERR_INVALID_ARG;          // (arrays of no tokens may well have no address)
     if (dt != KVBFP_F32 && dt != KVBFP_BF16) return KVBFP_ERR_INVALID_ARG;
     if (n_q_heads < 1 || n_q_heads % f.n_kv_heads != 0 || n_tokens < 0 || max_new < 0 || window < 0 || n_sink < 0) return KVBFP_ERR_INVALID_ARG;
     if (batch != (pages ? pages->batch : f.batch)) return KVBFP_ERR_INVALID_ARG;

@@ -631,7 +631,9 @@ extern "C" kvbfp_status kvbfp_norm_rope_append(const kvbfp_cache* cache, const k
     kvbfp_status st = check_format(&f);
     if (st == KVBFP_OK && pages) st = check_pool(f, pages);
     if (st != KVBFP_OK) return st;
-    if ((!q && !k) || (k == nullptr) != (v == nullptr) || (q == nullptr) != (q_out == nullptr) || !starts || !seq_lens) return KVBFP_ERR_INVALID_ARG;
+    if (!starts || !seq_lens) return KVBFP_ERR_INVALID_ARG;
+    // (arrays of no tokens may well have no address)
+    if (n_tokens != 0 && ((!q && !k) || (k == nullptr) != (v == nullptr) || (q == nullptr) != (q_out == nullptr))) return KVBFP_ERR_INVALID_ARG;
     if (k && (!cache->k_mant || !cache->k_exp || !cache->v_mant || !cache->v_exp)) return KVBFP_ERR_INVALID_ARG;
     if (dt != KVBFP_F32 && dt != KVBFP_BF16) return KVBFP_ERR_INVALID_ARG;
     if (n_tokens < 0 || !(eps >= 0.f) || eps > 3e38f) return KVBFP_ERR_INVALID_ARG;

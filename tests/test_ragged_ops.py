@@ -1114,3 +1114,43 @@ def test_ragged_refusals():
     assert call(ws=None) == B.ERR_WORKSPACE and call(size=need - 1) == B.ERR_WORKSPACE
     assert call(n=0) == B.OK
     assert B.launch_count() == before
+
+
+def test_calls_without_tokens():
+    """No new tokens: arrays without an address are no error, everything else is checked all the same."""
+    L = B.lib()
+    vp = C.c_void_p
+    before = B.launch_count()
+    f, cs, ps = structs()
+    need = L.kvbfp_ragged_workspace_bytes(C.byref(f), 3, 4, 0)
+
+    def write(n=0, st=16, ln=16, q=None, out=None, dt=1, pages=ps):
+        return L.kvbfp_norm_rope_append(C.byref(cs), C.byref(pages), vp(q), 512, None, 256, None, 256, dt, 4, n, vp(st), vp(ln), None, None, 1e-6,
+                                        None, 0, None, None, vp(out), None)
+
+    def attend(n=0, st=16, ln=16, q=None, out=None, dt=1, ws=16, new=0):
+        return L.kvbfp_ragged_attn(C.byref(cs), C.byref(ps), vp(q), dt, 4, n, 3, vp(st), vp(ln), new, 0, 0, None, None, 0.0, vp(out), vp(ws), need, None)
+    for call in (write, attend):
+        assert call() == B.OK and call(q=16) == B.OK and call(out=16) == B.OK
+        for kw in (dict(n=1), dict(n=-1), dict(st=None), dict(ln=None), dict(dt=3)):
+            assert call(**kw) == B.ERR_INVALID_ARG, kw
+        assert call(q=24) == B.ERR_ALIGNMENT
+    assert attend(new=-1) == B.ERR_INVALID_ARG and attend(ws=None) == B.ERR_WORKSPACE
+    assert write(pages=structs(n_pages=9)[2]) == B.ERR_INVALID_ARG
+    assert B.launch_count() == before
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("page", [0, 16])
+def test_steps_without_tokens(page):
+    """A step in which no sequence has new tokens, as a loop over steps makes it."""
+    cache, pool, _, _, n, perm, perm_v = batch_of([0, 0], [5, 40], 2, 2, 4, 32, page, torch.bfloat16, 1)
+    starts, before = i32(0, 0, 0), planes(cache)
+    for q in (torch.empty(0, 4, D, dtype=torch.bfloat16, device="cuda"), torch.empty(3, 8, D, dtype=torch.bfloat16, device="cuda")[:0, :4]):
+        k = torch.empty(0, 2, D, dtype=torch.bfloat16, device="cuda")
+        for args in ((q, k, k), (q, None, None), (None, k, k)):
+            got = B.norm_rope_append(cache, *args, starts, n, perm_k=perm, perm_v=perm_v, pool=pool)
+            assert got is None if args[0] is None else got.shape == q.shape
+        assert B.ragged_attn(cache, q, starts, n, 0, perm_k=perm, pool=pool).shape == q.shape
+    assert all(torch.equal(x, y) for x, y in zip(planes(cache), before))
+    assert B.device_status() == 0
