@@ -442,7 +442,8 @@ kvbfp_status kvbfp_pages_copy(const kvbfp_cache* src, const kvbfp_cache* dst, co
  *   theta    [head_dim / 2] f64: frequency of each pair (zero: that pair stays)
  *   q_out    [n_tokens, n_q_heads, head_dim] of `dt`, channel order; may be q itself where that is dense
  * Tokens outside the cache (or whose page is missing) are not stored and set KVBFP_FLAG_POSITION; their q is written all the
- * same.  Rows behind starts[batch] are left as they were.  Non-finite keys or values set KVBFP_FLAG_NONFINITE.
+ * same.  Rows behind starts[batch] are left as they were.  Starts that decrease set KVBFP_FLAG_POSITION; nothing is stored then
+ * and q_out is unspecified.  Non-finite keys or values set KVBFP_FLAG_NONFINITE.
  */
 kvbfp_status kvbfp_norm_rope_append(const kvbfp_cache* cache, const kvbfp_pages* pages, const void* q, int64_t q_stride,
                                     const void* k, int64_t k_stride, const void* v, int64_t v_stride, kvbfp_dtype dt,

@@ -287,6 +287,8 @@ __device__ __forceinline__ void write_pairs(T* row, int sub, const float (&a)[4]
     }
 }
 
+__device__ __forceinline__ int clamped_start(const WriteArgs& a, int b) { return min(max(a.starts[b], 0), a.n_tokens); }
+
 template <int P, int N, typename T, bool HALF>
 __global__ void __launch_bounds__(kWWarps * 32, 3) norm_rope_append(const WriteArgs a) {
     constexpr int D = kHeadDim, ROW_M = D * P / 8, ROW_E = D / N;
@@ -300,9 +302,16 @@ __global__ void __launch_bounds__(kWWarps * 32, 3) norm_rope_append(const WriteA
     const int hq = a.heads[0], hk = a.heads[1], n_heads = hq + 2 * hk;
     const int h0 = blockIdx.y * a.head_chunk, h1 = min(n_heads, h0 + a.head_chunk);
     const int tok = 2 * (blockIdx.x * kWWarps + warp) + grp;
-    const int first = min(max(a.starts[0], 0), a.n_tokens), end = min(max(a.starts[a.batch], 0), a.n_tokens);
+    const int first = clamped_start(a, 0), end = clamped_start(a, a.batch);
     const bool live = tok < end && tok >= first;
-    if (__all_sync(0xffffffffu, !live)) return;
+    // Starts that decrease leave nothing to do: which sequence a token belongs to is not known.
+    if (__all_sync(0xffffffffu, !live)) {
+        if (blockIdx.x + blockIdx.y + warp > 0) return;
+        bool back = false;
+        for (int i = lane; i < a.batch; i += 32) back |= clamped_start(a, i + 1) < clamped_start(a, i);
+        if (back) raise_flag(a.status, KVBFP_FLAG_POSITION);
+        return;
+    }
 
     // heads of each kind in the run, and its first rows on their way
     const int q0 = min(h0, hq), q1 = min(h1, hq), k0 = min(max(h0 - hq, 0), hk), k1 = min(max(h1 - hq, 0), hk);
@@ -321,14 +330,20 @@ __global__ void __launch_bounds__(kWWarps * 32, 3) norm_rope_append(const WriteA
     {
         const int t0 = __shfl_sync(0xffffffffu, tok, 0), t1 = __shfl_sync(0xffffffffu, tok, 16);
         int n0 = 0, n1 = 0;
+        bool back = false;
         for (int i = 0; i < a.batch; i += 32) {
-            const int s = i + lane < a.batch ? a.starts[i + lane] : 0x7fffffff;
+            const int s = i + lane < a.batch ? clamped_start(a, i + lane) : 0x7fffffff;
+            if (i + lane < a.batch) back |= clamped_start(a, i + lane + 1) < s;
             n0 += __popc(__ballot_sync(0xffffffffu, s <= t0));
             n1 += __popc(__ballot_sync(0xffffffffu, s <= t1));
         }
+        if (__any_sync(0xffffffffu, back)) {
+            if (lane == 0) raise_flag(a.status, KVBFP_FLAG_POSITION);
+            return;
+        }
         b = min(max((grp ? n1 : n0) - 1, 0), a.batch - 1);
     }
-    const int len = a.lens[b], pos = len - min(max(a.starts[b + 1], 0), a.n_tokens) + tok;
+    const int len = a.lens[b], pos = len - clamped_start(a, b + 1) + tok;
     int64_t row0 = 0;             // row of head 0; heads follow map.rows rows on
     bool stored = live && pos >= 0 && pos < a.map.cap;
     if (stored) {

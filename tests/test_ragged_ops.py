@@ -649,6 +649,27 @@ def test_norm_rope_append_flags(page):
     assert B.device_status() == B.FLAG_NONFINITE
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("batch", [3, 40])
+@pytest.mark.parametrize("page", [0, 16])
+def test_norm_rope_append_starts_that_decrease(page, batch):
+    """Flagged, nothing is stored; the next call is served."""
+    news, lens = [3, 60, 2] + [1] * (batch - 3), [100, 60, 80] + [50] * (batch - 3)
+    cache, pool, q, k, v, w, theta, starts, n, pos, perm, perm_v = write_case(news, lens, 2, 2, 4, 32, page, torch.bfloat16, 4)
+    before, good, rows = planes(cache), starts.tolist(), q.shape[0]
+    kw = dict(q_weight=w[0], k_weight=w[1], theta=theta, perm_k=perm, perm_v=perm_v, pool=pool)
+    swapped = good[:batch - 1] + [good[batch], good[batch - 1]]
+    for bad in ([0, 63, 3] + good[3:], [5, 0] + good[2:], swapped, [0] * batch + [-3], [rows, 0] + [0] * (batch - 1), [0, rows] + [0] * (batch - 1)):
+        B.norm_rope_append(cache, q, k, v, i32(*bad), n, **kw)
+        down = any(min(max(y, 0), rows) < min(max(x, 0), rows) for x, y in zip(bad, bad[1:]))
+        assert B.device_status() == (B.FLAG_POSITION if down else 0), bad
+        assert all(torch.equal(x, y) for x, y in zip(planes(cache), before)), bad
+    out = B.norm_rope_append(cache, q, k, v, starts, n, **kw)
+    check_q(out, rotated64(q, w[0], 1e-6, theta, False, pos))
+    check_write(cache, pool, before, rotated64(k, w[1], 1e-6, theta, False, pos), v.double(), news, lens, perm, perm_v, 4, 32)
+    assert B.device_status() == 0
+
+
 # ----------------------------------------------------------------------------------------------- pages
 class Model:
     """The pages' bookkeeping step by step."""
