@@ -195,8 +195,7 @@ __global__ void __launch_bounds__(kPThreads, 1) ragged_umma(const RaggedArgs a) 
         fence_async_shared();
     }
     // (so that a warp whose wait for the plan ran out finds rows that are not to be read)
-    if (tid < 128) s_rows[tid >> 3][tid & 7] = -1;
-    else if (tid < 128 + 16) s_flags[tid - 128] = 0;
+    if (tid < 16 * 8) (&s_rows[0][0])[tid] = -1;
     if (warp == 0) tmem_alloc(smem_u32(&s_tmem), 512);
     tmem_fence_before();
     __syncthreads();
