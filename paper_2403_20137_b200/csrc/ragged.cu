@@ -6,11 +6,28 @@
 namespace kvbfp {
 namespace {
 
+// Tokens at negative positions see nothing: zeros, by all threads of the grid.
+__device__ __noinline__ void ragged_zeros(const RaggedArgs& a) {
+    const int lane = threadIdx.x & 31, row = a.n_q_heads * kHeadDim * (a.q_is_bf16 ? 2 : 4) / 16;
+    const int64_t me = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * blockDim.x + threadIdx.x, step = (int64_t)gridDim.x * gridDim.y * blockDim.x;
+    for (int b0 = 0; b0 < a.batch; b0 += 32) {
+        RaggedSeq s = {};
+        if (b0 + lane < a.batch) s = ragged_seq(a, b0 + lane);
+        const int mine = ragged_row_tiles(a, s, a.rows_tile) > 0 ? min(s.n, max(-s.base, 0)) : 0;
+        for (uint32_t some = __ballot_sync(0xffffffffu, mine > 0); some; some &= some - 1) {
+            const int l = __ffs(some) - 1;
+            uint4* to = static_cast<uint4*>(a.out) + (int64_t)__shfl_sync(0xffffffffu, s.start, l) * row;
+            const int64_t pieces = (int64_t)__shfl_sync(0xffffffffu, mine, l) * row;
+            for (int64_t i = me; i < pieces; i += step) to[i] = make_uint4(0u, 0u, 0u, 0u);
+        }
+    }
+}
+
 // out = sum_w 2^(m_w - m) o_w / sum_w 2^(m_w - m) l_w over the workers that share an entry.  The block of worker w serves the
 // entry that ends in w's first run: with SPLIT a row (blockIdx.y) by four warps that take every fourth partial, else a row per
 // warp.  Most blocks find that their worker has none.
 template <bool SPLIT>
-__global__ void __launch_bounds__(128) ragged_merge(const RaggedArgs a) {
+__global__ void __launch_bounds__(128) ragged_merge(const __grid_constant__ RaggedArgs a) {
     constexpr int D = kHeadDim;
     __shared__ float so[4][D];
     __shared__ float sml[4][2];
@@ -19,6 +36,7 @@ __global__ void __launch_bounds__(128) ragged_merge(const RaggedArgs a) {
     pdl_trigger();
     const int w1 = blockIdx.x;
     const int4 rec = a.rec[w1];
+    if (*a.edge) ragged_zeros(a);
     if (rec.x < 0) return;
     const int b = rec.x, rt = rec.y, hk = rec.z, w0 = rec.w;
     const int r = SPLIT ? (int)blockIdx.y : (int)blockIdx.y * 4 + warp, row = rt * a.rows_tile + r;
@@ -119,11 +137,12 @@ inline Kernel kernel_of(bool umma, int mant_bits, int few_tile = kFewRows) {
 // Workspace of one of the two from `base` on; returns the size and, with `a`, sets the pointers.
 size_t lay_out(const Kernel& k, int64_t rows, RaggedArgs* a, uint8_t* base) {
     const int part_rows = (int)(rows < k.rows_tile ? rows : k.rows_tile);
-    const size_t rec = up256((size_t)k.max_workers * sizeof(int4));
+    const size_t rec = up256((size_t)k.max_workers * sizeof(int4)) + 256;
     if (a) {
         a->rows_tile = k.rows_tile;
         a->part_rows = part_rows;
         a->rec = reinterpret_cast<int4*>(base);
+        a->edge = reinterpret_cast<int*>(base + rec - 256);
         a->partials = reinterpret_cast<float*>(base + rec);
     }
     return rec + up256((size_t)2 * k.max_workers * part_rows * kAttnPart * 4);

@@ -33,6 +33,7 @@ struct RaggedArgs {
     int workers;
     int4* rec;                     // workspace: per worker the entry that ends in its range's first run and began before it:
                                    // sequence, row tile, kv head, first worker (-1: none)
+    int* edge;                     // workspace: does a sequence of this kernel have tokens at negative positions
     float* partials;               // workspace: [2 * workers, part_rows, kAttnPart]
     float out_up;                  // sums of P and V as the kernel carries them -> values
     uint32_t* status;
@@ -140,20 +141,15 @@ __device__ __forceinline__ int ragged_seek(const RaggedArgs& a, RaggedCursor& c,
     return at;
 }
 
-// Rows at negative positions see nothing; lengths outside the cache are reported (both by one thread, they are rare).
-static __device__ __noinline__ void ragged_edges(uint32_t* status, uint4* out, int64_t pieces, bool clamped) {
-    if (clamped) raise_flag(status, KVBFP_FLAG_POSITION);
-    for (int64_t i = 0; i < pieces; ++i) out[i] = make_uint4(0u, 0u, 0u, 0u);
-}
-
 // Items and entries of every sequence, before it and in all: threads of a block together (THREADS of them).  s_items, s_entries:
 // room for 1024 + 1.  Starts that decrease (reported) leave nothing to do: sequences that overlap could be more items than 32 bits
-// count.  Afterwards entry b of them holds what comes before sequence b, entry `batch` all.
+// count.  Afterwards entry b of them holds what comes before sequence b, entry `batch` all.  Lengths outside the cache are reported,
+// tokens at negative positions noted for the merge, by the first block.
 template <int THREADS>
 __device__ __forceinline__ void ragged_count(const RaggedArgs& a, int* s_items, int* s_entries, int (&s_scan)[2][THREADS / 32], int rows_tile, int tile) {
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, H = a.fmt.n_kv_heads;
     constexpr int kAlone = 8;                                  // row tiles that a thread counts by itself
-    bool many = false, back = false;
+    bool many = false, back = false, edge = false;
     for (int b = tid; b < a.batch; b += THREADS) {
         const RaggedSeq s = ragged_seq(a, b);
         back |= min(max(a.starts[b + 1], 0), a.n_tokens) < s.start;
@@ -171,10 +167,14 @@ __device__ __forceinline__ void ragged_count(const RaggedArgs& a, int* s_items, 
         }
         s_items[b] = (x + max(e, 0) * a.extra) * H;
         s_entries[b] = e * H;
-        if (blockIdx.x == 0 && nrt > 0 && (s.clamped || s.base < 0)) {
-            const int64_t row = (int64_t)a.n_q_heads * kHeadDim * (a.q_is_bf16 ? 2 : 4) / 16;
-            ragged_edges(a.status, reinterpret_cast<uint4*>(a.out) + s.start * row, (int64_t)min(s.n, max(-s.base, 0)) * row, s.clamped != 0);
+        if (blockIdx.x == 0 && nrt > 0) {
+            edge |= s.base < 0;
+            if (s.clamped) raise_flag(a.status, KVBFP_FLAG_POSITION);
         }
+    }
+    if (blockIdx.x == 0) {
+        edge = __syncthreads_or(edge);
+        if (tid == 0) *a.edge = edge;
     }
     if (__syncthreads_or(many || back)) {
         if (__syncthreads_or(back)) {

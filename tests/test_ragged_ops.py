@@ -299,6 +299,31 @@ def test_ragged_attn_starts_that_decrease(dtype):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("hint", [1, 20000])
+def test_ragged_attn_many_rows_before_the_first_position(dtype, hint):
+    """Long sequences whose lengths were not raised, among others: their rows are zeros (all but the last seven of the third),
+    the others' right.  More than 32 sequences."""
+    news, lens = [1, 20000, 3000, 5] + [0, 2] * 20, [700, 0, 7, 90] + [0, 0] * 20
+    some = [1, 0, 7, 5] + [0] * 40
+    g = torch.Generator().manual_seed(3)
+    args = batch_of(some, lens, 1, 4, 4, 32, 16, dtype, 3)
+    cache, pool, few, _, n, perm, perm_v = args
+    ref = reference(cache, pool, few, some, lens, perm, perm_v)
+    q = torch.randn(sum(news), 4, D, generator=g).to(dtype).cuda()
+    at = torch.cat([torch.arange(1), torch.arange(22994, 23001), torch.arange(23001, 23006)]).cuda()
+    q[at] = few
+    starts = i32(*np.concatenate([[0], np.cumsum(news)]).tolist())
+    out = torch.full((q.shape[0] + 3, 4, D), 5.0, dtype=dtype, device="cuda")
+    got = B.ragged_attn(cache, torch.cat([q, q[:3]]), starts, n, hint, perm_k=perm, inv_perm_v=inverse(perm_v), pool=pool, out=out)
+    check(got[at], *ref)
+    rest = torch.ones(got.shape[0], dtype=torch.bool, device="cuda")
+    rest[at], rest[-3:] = False, False
+    assert bool((got[rest] == 0).all()) and bool((got[-3:] == 5.0).all())
+    assert B.device_status() == 0
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 def test_ragged_attn_largest_window(dtype):
     """Windows and numbers of first tokens up to the largest integer, rows before the first position among them."""
     news, lens = [40, 1], [90, 70]
