@@ -79,14 +79,17 @@ __global__ void __launch_bounds__(128) pages_fork(Pool p, const int32_t* src, co
     if (tid == 0) p.lens[d] = len;
 }
 
-// Sum over the block of what the threads before this one have; `total`: of all of them.  One barrier before the next use.
+// Sum over the block of what the threads before this one have; `total`: of all of them.  One barrier before the next use.  Sums end
+// at kSumEnd: 1024 sequences may ask for 2^37 pages in all, and no pool has more than 2^28.  (A thread's own share is 2^27 at most,
+// so what is left of an ended sum without it is above any pool still.)
+constexpr int kSumEnd = 1 << 29;
 __device__ __forceinline__ int block_before(int mine, int (&s_warp)[32], int& total) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     int x = mine;
 #pragma unroll
     for (int off = 1; off < 32; off <<= 1) {
         const int y = __shfl_up_sync(0xffffffffu, x, off);
-        if (lane >= off) x += y;
+        if (lane >= off) x = min(x + y, kSumEnd);
     }
     if (lane == 31) s_warp[warp] = x;
     __syncthreads();
@@ -94,7 +97,7 @@ __device__ __forceinline__ int block_before(int mine, int (&s_warp)[32], int& to
 #pragma unroll
     for (int off = 1; off < 32; off <<= 1) {
         const int y = __shfl_up_sync(0xffffffffu, w, off);
-        if (lane >= off) w += y;
+        if (lane >= off) w = min(w + y, kSumEnd);
     }
     total = __shfl_sync(0xffffffffu, w, 31);
     const int before = warp ? __shfl_sync(0xffffffffu, w, (warp + 31) & 31) : 0;

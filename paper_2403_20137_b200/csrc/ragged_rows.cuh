@@ -341,7 +341,7 @@ __global__ void __launch_bounds__(kAttnWarps * 32, attn_rows_blocks(!F32)) ragge
                 }
                 continue;
             }
-            const bool wanted = row < R && pos[e] >= 0;            // (rows before the first position: zeros, written already)
+            const bool wanted = row < R && pos[e] >= 0;            // (rows before the first position: zeros, by the merge)
             const float inv = l != 0.f ? kValueUp / l : 0.f;
             float v[16];
 #pragma unroll

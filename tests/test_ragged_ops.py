@@ -864,6 +864,22 @@ def test_pages_run_out():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("few", [0, 3])
+def test_pages_reserve_counts_past_32_bits(few):
+    """1024 sequences that ask for some 2^31 pages between them: those that find pages get them, the others stay as they were."""
+    pool = B.PagePool(1024, 1 << 21, 100, 16)
+    more = torch.full((1024,), 1 << 25, dtype=torch.int32, device="cuda")
+    more[:few] = 17
+    pairs = B.pages_reserve(pool, more)
+    want = torch.zeros(1024, dtype=torch.int32, device="cuda")
+    want[:few] = 17
+    assert torch.equal(pool.lens, want)
+    assert pool.table[:few, :2].flatten().tolist() == list(range(2 * few))
+    assert int((pool.table >= 0).sum()) == 2 * few and int(pool.refs.sum()) == 2 * few
+    assert bool((pairs == -1).all()) and B.device_status() == B.FLAG_PAGES
+
+
+@pytest.mark.gpu
 def test_pages_fork_skips_what_it_must():
     pool = B.PagePool(6, 2, 12, 16)
     B.pages_reserve(pool, i32(20, 5, 0, 0, 0, 0))
