@@ -11,9 +11,9 @@
 // lane owns eight stored slots and casts them as kvbfp_append does (sixteen lanes to a row).
 //
 // Codes of keys.  Values next to a rounding border fall on the side that fp32 errors pick, which would make the cache depend on
-// the order of operations.  The error of a value is bounded by kErr times the magnitude of its pair; a row with a value (or
-// block maximum) that close to a border is formed and cast again in fp64.  (By arithmetic about one row of random keys in a thousand
-// at 4 bits, in 60 at 8: 128 slots, twice a bound of some 4e-6 of the distance of borders, or 16 times that.)  So the codes are
+// the order of operations.  The error of a value is bounded by kErr times the magnitude of its pair (and kErrLow); a row with a value (or
+// block maximum) that close to a border is formed and cast again in fp64.  (By arithmetic about one row of random keys in 800
+// at 4 bits, in 50 at 8: 128 slots, twice a bound of some 5e-6 of the distance of borders, or 16 times that.)  So the codes are
 // those of the formula.
 //
 // What bounds it: instructions (issue slots 47 % busy, memory 32 %), most of them in the casts.  Four prompts of 8192 tokens, 32
@@ -50,8 +50,10 @@ struct WriteArgs {
 // fp32 error of a normalised and rotated value, relative to the sum of its pair's magnitudes (in units of 2^-24): the norm's
 // factor 9 (squares summed in ten roundings, halved by the square root; the function itself 4), its product 1, sine and cosine of
 // an angle rounded once 4 (the angle is 3.14 at most: half a step is 2; the functions are good to 2), their product with the
-// weight 1, the product and the sum 2; rounded up.
-constexpr float kErr = 18.f / 16777216.f;
+// weight 1, the product and the sum 2; rows beyond 2^126, whose factor is a subnormal number, 4 more; rounded up.  kErrLow: what
+// results in the subnormal range add, half a step of 2^-149 each: two products and their sum, and where the weights are that small
+// two entries of the table, times normalised values of 11.4 at most (the square root of 128).
+constexpr float kErr = 22.f / 16777216.f, kErrLow = 0x1p-145f;
 
 template <int P, int N>
 struct Cast {
@@ -462,7 +464,7 @@ __global__ void __launch_bounds__(kWWarps * 32, 3) norm_rope_append(const WriteA
                     f2_split(f2_mul(na, wa[j]), ma[0], ma[1]);
                     f2_split(f2_mul(nb, wb[j]), mb[0], mb[1]);
 #pragma unroll
-                    for (int e = 0; e < 2; ++e) err[2 * j + e] = moved ? kErr * (fabsf(ma[e]) + fabsf(mb[e])) : 0.f;
+                    for (int e = 0; e < 2; ++e) err[2 * j + e] = moved ? fmaf(kErr, fabsf(ma[e]) + fabsf(mb[e]), kErrLow) : 0.f;
                 }
                 // (value, bound) of each channel
 #pragma unroll

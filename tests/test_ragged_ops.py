@@ -642,6 +642,28 @@ def test_norm_rope_append_codes_next_to_borders(bits):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("what", ["small keys", "small weights", "large keys"])
+def test_norm_rope_append_codes_at_the_ends_of_the_range(what, bits):
+    """Keys rotated in the subnormal range, weights there, rows whose norm's factor is there: every code that of the formula."""
+    n = 16384
+    g = torch.Generator().manual_seed(17)
+    k = torch.randn(n, 2, D, generator=g)
+    if what == "large keys":
+        k = torch.sign(k) * (1.0 + torch.rand(n, 2, D, generator=g)) * 0.999
+    scale = {"small keys": 2.0 ** -133, "small weights": 1.0, "large keys": 2.0 ** 126}[what]
+    k = (k.bfloat16().double() * scale).float().cuda()
+    w = None if what == "small keys" else (1.0 + 0.2 * torch.randn(D, generator=g).cuda()) * (2.0 ** -131 if what == "small weights" else 1.0)
+    theta = 10000.0 ** (-2.0 * torch.arange(64, dtype=torch.float64, device="cuda") / D)
+    cache = B.Cache(1, 2, D, n, 32, bits, fill=0)
+    before = planes(cache)
+    B.norm_rope_append(cache, None, k, k, i32(0, n), i32(n), k_weight=w, eps=0.0, theta=theta, half_split=True)
+    pos = torch.arange(n, device="cuda")
+    check_write(cache, None, before, rotated64(k, w, 0.0, theta, True, pos), k.double(), [n], [n], None, None, bits, 32)
+    assert B.device_status() == 0
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("page", [0, 16])
 def test_norm_rope_append_flags(page):
     """Positions before the first and behind the cache, missing pages, tokens of no sequence: not stored; q is written for all
