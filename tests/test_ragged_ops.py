@@ -577,6 +577,26 @@ def test_norm_rope_append(half, page, bits, block, dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("half,page,bits,block,packed", [(False, 64, 4, 32, True), (True, 0, 6, 16, False), (True, 64, 8, 32, True), (False, 0, 4, 128, False)])
+@pytest.mark.parametrize("tokens,hq,heads", [(1500, 13, 5), (4000, 13, 5), (2300, 7, 9), (9000, 5, 7), (30001, 6, 3)])
+def test_norm_rope_append_runs_of_heads(tokens, hq, heads, half, page, bits, block, packed, dtype):
+    """Enough tokens that a warp walks several heads: runs that end inside the queries, cross from them to keys and on to values, odd
+    rests, whole tokens; values with a permutation and without."""
+    news = [tokens - 1007, 0, 1000, 7]
+    lens = [news[0] + 33, 5, 1000, 400]
+    cache, pool, q, k, v, w, theta, starts, n, pos, perm, perm_v = write_case(news, lens, hq, heads, bits, block, page, dtype, tokens + bits, packed=packed)
+    if not packed:
+        perm_v = None
+    before = planes(cache)
+    out = B.norm_rope_append(cache, q, k, v, starts, n, q_weight=w[0], k_weight=w[1], eps=1e-5, theta=theta, half_split=half, perm_k=perm,
+                             perm_v=perm_v, pool=pool)
+    check_q(out, rotated64(q, w[0], 1e-5, theta, half, pos))
+    check_write(cache, pool, before, rotated64(k, w[1], 1e-5, theta, half, pos), v.double(), news, lens, perm, perm_v, bits, block)
+    assert B.device_status() == 0
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("norm,rope", [(False, True), (True, False), (False, False)])
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 def test_norm_rope_append_parts(norm, rope, dtype):
