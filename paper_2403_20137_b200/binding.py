@@ -704,7 +704,7 @@ def norm_rope_append(cache, q, k, v, starts, seq_lens, q_weight=None, k_weight=N
 
 def ragged_workspace_bytes(fmt, batch, n_q_heads, max_new):
     """Workspace of ragged_attn for up to max_new new tokens of each of `batch` sequences."""
-    return int(lib().kvbfp_ragged_workspace_bytes(C.byref(fmt), batch, n_q_heads, batch * max_new))
+    return int(lib().kvbfp_ragged_workspace_bytes(C.byref(fmt), batch, n_q_heads, min(batch * max_new, 2 ** 31 - 1)))
 
 
 def ragged_attn(cache, q, starts, seq_lens, max_new, window=0, n_sink=0, perm_k=None, inv_perm_v=None, softmax_scale=0.0,

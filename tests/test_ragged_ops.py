@@ -1258,3 +1258,10 @@ def test_steps_without_tokens(page):
         assert B.ragged_attn(cache, q, starts, n, 0, perm_k=perm, pool=pool).shape == q.shape
     assert all(torch.equal(x, y) for x, y in zip(planes(cache), before))
     assert B.device_status() == 0
+
+
+@pytest.mark.parametrize("batch,most", [(512, 1 << 23), (1024, 1 << 26), (3, 1 << 30)])
+def test_ragged_workspace_of_long_batches(batch, most):
+    """Batches whose tokens pass 32 bits: as much as the most that a call takes."""
+    f = structs()[0]
+    assert B.ragged_workspace_bytes(f, batch, 4, most) == B.ragged_workspace_bytes(f, batch, 4, (1 << 26) // batch) > 0
