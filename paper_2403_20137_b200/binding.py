@@ -235,6 +235,8 @@ class Cache:
         for name, t, width in (("k_mant", k_mant, cache.fmt.row_m), ("k_exp", k_exp, cache.fmt.row_e),
                                ("v_mant", v_mant, cache.fmt.row_m), ("v_exp", v_exp, cache.fmt.row_e)):
             setattr(cache, name, _sized(name, _dev(t, torch.uint8), (batch, heads, rows, width)))
+            if t.get_device() != k_mant.get_device():
+                raise ValueError(f"{name}: expected all planes on one device")
         return cache
 
     def struct(self):

@@ -1265,3 +1265,26 @@ def test_ragged_workspace_of_long_batches(batch, most):
     """Batches whose tokens pass 32 bits: as much as the most that a call takes."""
     f = structs()[0]
     assert B.ragged_workspace_bytes(f, batch, 4, most) == B.ragged_workspace_bytes(f, batch, 4, (1 << 26) // batch) > 0
+
+
+class Plane:
+    """What Cache.of looks at of a plane (no second device is needed)."""
+    dtype, is_cuda = torch.uint8, True
+
+    def __init__(self, shape, device):
+        self.shape, self.device = shape, device
+
+    def is_contiguous(self):
+        return True
+
+    def get_device(self):
+        return self.device
+
+
+@pytest.mark.parametrize("at", range(4))
+def test_cache_of_planes_on_two_devices(at):
+    """Calls look at the first plane's device: planes elsewhere are refused when the cache is put together."""
+    shapes = [(5, 2, 16, w) for w in (64, 4, 64, 4)]
+    assert B.Cache.of(*(Plane(s, 0) for s in shapes), 32, 4).fmt.head_dim == D
+    with pytest.raises(ValueError):
+        B.Cache.of(*(Plane(s, int(i == at)) for i, s in enumerate(shapes)), 32, 4)
