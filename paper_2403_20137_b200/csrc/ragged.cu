@@ -122,15 +122,19 @@ __global__ void __launch_bounds__(128) ragged_merge(const __grid_constant__ Ragg
 inline size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 // Sequences of up to kFewRows bf16 query rows per kv head go to ragged_rows (every eight rows read the cache anew), longer ones
-// to ragged_umma (256 rows a pass).
-constexpr int kFewRows = 8;
+// to ragged_umma (256 rows a pass).  us of both, 8 kv heads, 4 bits (8 bits), rows per kv head:
+//                                9 to 16             24               32
+//   16 x 8192 tokens      96 | 172 (139 | 192)  131 | 173 (195 | 193)  168 | 175 (256 | 195)
+//   1 x 32768             44 | 50  (55 | 54)    52 | 51   (69 | 54)    58 | 51   (80 | 55)
+//   64 x 512              39 | 88  (51 | 96)    50 | 89   (67 | 95)    61 | 90   (84 | 98)
+constexpr int kFewRows = 16, kRowsTile = 8;
 // What beginning and ending an entry costs ragged_umma, in tiles: 14 000 cycles (pi(Q), the first scores, the results) against
 // 4700 a tile.
 constexpr int kEntryTiles = 3;
 struct Kernel {
     int rows_tile, tile, max_workers;
 };
-inline Kernel kernel_of(bool umma, int mant_bits, int few_tile = kFewRows) {
+inline Kernel kernel_of(bool umma, int mant_bits, int few_tile = kRowsTile) {
     return umma ? Kernel{256, 128, kAttnMaxSms} : Kernel{few_tile, attn_rows_tile(mant_bits), 3 * kAttnWarps * kAttnMaxSms};
 }
 
@@ -234,17 +238,20 @@ extern "C" kvbfp_status kvbfp_ragged_attn(const kvbfp_cache* cache, const kvbfp_
     };
     // ragged_rows: four bf16 rows an item where more are not expected (single tokens, or single tokens between longer sequences),
     // whose second term of the weights costs 1 %; eight, which read the cache once for all of them (second term: 4.5 to 12 %), otherwise.
+    // (16 x 8192, 8 heads: four rows 50 us in fours, 55 in eights; eight rows 83, 59.)  In fours, only up to eight rows of a sequence
+    // stay with ragged_rows (8 bits, us of both: 8 rows 130 | 188, 16 rows 245 | 193).
     const int64_t hint = (int64_t)max_new * group;
     const bool four = bf16 && (hint <= 4 || (hint > kFewRows && group <= 4)) && countable(kernel_of(false, f.mant_bits, 4), rows / 4 + batch);
-    const Kernel k_few = kernel_of(false, f.mant_bits, four ? 4 : kFewRows), k_many = kernel_of(true, f.mant_bits);
+    const Kernel k_few = kernel_of(false, f.mant_bits, four ? 4 : kRowsTile), k_many = kernel_of(true, f.mant_bits);
     const bool all_few = countable(k_few, rows / k_few.rows_tile + batch);
     const bool many = bf16 && rows > kFewRows && (hint > kFewRows || !all_few);
     if (many ? !countable(k_few, batch) || !countable(k_many, rows / k_many.rows_tile + batch) : !all_few) return KVBFP_ERR_UNSUPPORTED;
+    const int few = four ? 8 : kFewRows;
     a.few_lo = 0;
-    a.few_hi = many ? kFewRows : 0x7fffffff;
+    a.few_hi = many ? few : 0x7fffffff;
     st = !many || batch > 1 ? launch_kernel(a, false, k_few, rows, ws, n_sm, s) : KVBFP_OK;
     if (st != KVBFP_OK || !many) return st;
-    a.few_lo = batch > 1 ? kFewRows : 0;
+    a.few_lo = batch > 1 ? few : 0;
     a.few_hi = 0x7fffffff;
     return launch_kernel(a, true, k_many, rows, ws + few_bytes, n_sm, s);
 }

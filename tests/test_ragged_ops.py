@@ -179,6 +179,20 @@ def test_ragged_attn_row_counts(group, new, bits):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("bits", [4, 6, 8])
+@pytest.mark.parametrize("group,news", [(1, [8, 9, 16, 17, 4, 5]), (4, [2, 3, 4, 5, 1, 0]), (8, [1, 2, 3, 1, 2, 3]), (5, [3, 4, 1, 2, 0, 3]), (4, [4])])
+def test_ragged_attn_rows_around_the_borders(group, news, bits):
+    """Rows per kv head around the numbers that choose a kernel and its items, every way of hinting at them."""
+    lens = [n + 170 + 61 * b for b, n in enumerate(news)]
+    args = batch_of(news, lens, 2, group, bits, 32, 32, torch.bfloat16, group + bits)
+    cache, pool, q, starts, n, perm, perm_v = args
+    ref = reference(cache, pool, q, news, lens, perm, perm_v)
+    for hint in (0, 1, 2, 3, max(news), 16, 17, 1000):
+        check(B.ragged_attn(cache, q, starts, n, hint, perm_k=perm, inv_perm_v=inverse(perm_v), pool=pool), *ref)
+    assert B.device_status() == 0
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("hint", [0, 1, 8])
 @pytest.mark.parametrize("bits,block", FMT)
 @pytest.mark.parametrize("group,news", [(1, [1, 4, 3]), (3, [1, 2, 1]), (4, [1, 1, 2]), (8, [1, 1, 1]), (5, [1, 0, 1])])
