@@ -4,7 +4,8 @@
 // the device because the lengths do.  Nothing depends on the order of atomics: reference counts only add and subtract, and new
 // pages are found by scanning the counts in page order (which also gives every run the same pages).
 // Four calls of a step (free, fork, reserve, copy; 8 x 4 branches) take 13.5 us in a graph; packing 16384 pages of 64 tokens x 8
-// heads into another pool 198 us, 0.88 of the copy rate.
+// heads into another pool 198 us, 0.88 of the copy rate.  Reserving scans the counts from the first page on until enough free ones are
+// found: where those are the last of 1000, 16384, 131072 pages 4.6, 7.6, 33 us.
 #include "pages.cuh"
 
 namespace kvbfp {

@@ -16,7 +16,7 @@
 // What bounds it: instructions, 357 per warp and 16 tokens, most of them the conversion of fields (integer pipe 56 % busy, issue slots
 // 61 %, three warps a scheduler).  16 tokens, 32 heads x 8192, 4 bits, pages of 64: 148 us, 3.8 TB/s; 8 tokens, 8 heads x up to
 // 32768, four query heads each, pages of 32: 66 us; one token under a window of 1000: 11.3 us with the merge.  V's words loaded
-// before the softmax: no gain (145 us; 8 bits 133 against 130).
+// before the softmax: no gain (a microsecond off the first, three on top of the second at 8 bits).
 #pragma once
 #include "attn_rows.cuh"
 #include "ragged.cuh"

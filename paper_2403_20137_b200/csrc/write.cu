@@ -16,8 +16,9 @@
 // at 4 bits, in 50 at 8: 128 slots, twice a bound of some 5e-6 of the distance of borders, or 16 times that.)  So the codes are
 // those of the formula.
 //
-// What bounds it: instructions (issue slots 47 % busy, memory 32 %), most of them in the casts.  Four prompts of 8192 tokens, 32
-// query and 8 kv heads, 4 bits: 121 us, floor 71.
+// What bounds it: instructions (issue slots 60 % busy while blocks run, 54 % over the launch), most of them in the casts, and the
+// parking of keys (shared-memory data pipe 58 %; memory 44 %).  Four ragged prompts of up to 8192 tokens, 32 query and 8 kv heads, 4
+// bits, two runs of heads a token: 121 us, floor 71.
 #include <atomic>
 
 #include "pages.cuh"
